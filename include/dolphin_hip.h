@@ -406,6 +406,39 @@ dol_status dol_iterate_backward_noalloc(const dol_dist *r0, const dol_dist *e, c
  * grad: device [batch, d->ld]. */
 dol_status dol_nll_grad(const dol_dist *d, const int32_t *target_col, float *grad, void *hip_stream);
 
+/* ---- Training the network whose outputs become Distributions (the neural part of Fig. 2; Sec. 3.3 leaves its objective and its
+ * optimiser to the user): the loss over its classes, the update of its weights, the normalisation between its layers.
+ *
+ * Unlike Distributions these operate on matrices of either of two types.  Sums, softmax statistics and norms are held in 32 bits or
+ * more whatever the type, and a result is rounded once.  A call's workspace is device memory of the caller's, aligned to 256 bytes and
+ * of at least the size that the *_workspace call of the same arguments gives (host only); its contents do not matter before or after. */
+typedef enum { DOL_F32 = 0, DOL_BF16 = 1 } dol_dtype;
+typedef struct {
+    int32_t dtype;               /* dol_dtype */
+    int32_t rows, cols;
+    int64_t ld;                  /* elements between consecutive rows, >= cols */
+    void *data;                  /* device, row-major */
+} dol_matrix;
+
+/* Softmax cross entropy of a linear layer over many classes, without its logits in memory:
+ *   l[i, v] = x[i] . weight[v] + bias[v],   lse[i] = log sum_v exp l[i, v],   loss[i] = lse[i] - l[i, target[i]].
+ *   x       [rows, width],   weight  [classes, width], same type
+ *   bias    device [classes] or NULL; -inf takes a class out
+ *   target  device [rows]; a row whose target is outside 0..classes-1 (-1, say) is left out: its loss is 0
+ *   loss, lse  device [rows], both written.  A row without any class above -inf has lse = -inf and loss = +inf.
+ * At most 2^22 rows and classes and 2^20 elements of a row (else DOL_EUNSUPPORTED); at least one class of one element. */
+dol_status dol_cross_entropy_workspace(const dol_matrix *x, const dol_matrix *weight, int32_t backward, int64_t *bytes);
+dol_status dol_cross_entropy(const dol_matrix *x, const dol_matrix *weight, const float *bias, const int32_t *target, float *loss,
+                             float *lse, void *workspace, int64_t workspace_bytes, void *hip_stream);
+/* Its gradients: dl[i, v] = grad_loss[i] (exp(l[i, v] - lse[i]) - [v = target[i]]) for the rows that count, 0 for rows that are left out
+ * or have no class (whatever x holds there, also NaN, and whatever grad_loss says);
+ *   grad_x = dl weight,   grad_weight = dl^T x,   grad_bias[v] = sum_i dl[i, v].
+ * lse as the forward call left it.  Each gradient is OVERWRITTEN, of the type of x (grad_bias: float); any may be NULL.  Sums are taken in
+ * a fixed order: two runs give the same bits.  With DOL_BF16 dl is rounded to bf16 before the two products.  rows == 0 writes zeros. */
+dol_status dol_cross_entropy_backward(const dol_matrix *x, const dol_matrix *weight, const float *bias, const int32_t *target,
+                                      const float *lse, const float *grad_loss, const dol_matrix *grad_x, const dol_matrix *grad_weight,
+                                      float *grad_bias, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
 /* Message of the calling thread's most recent failing call ("" if none). */
 const char *dol_last_error(void);
 /* Library version, e.g. "0.1.0". */

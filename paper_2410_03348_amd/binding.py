@@ -654,3 +654,86 @@ def nll_grad(d: Dist, target_col: torch.Tensor, grad: torch.Tensor, stream=None)
     """target_col: int32 device tensor [batch]; grad rows have stride d.ld."""
     assert target_col.dtype == torch.int32 and target_col.is_contiguous()
     _native.nll_grad(d._p, target_col.data_ptr(), grad.data_ptr(), None if stream is None else _handle(stream))
+
+
+# ---- training the network whose outputs become Distributions
+
+F32, BF16 = 0, 1
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+class _Matrix(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("ld", C.c_int64), ("data", C.c_void_p)]
+
+
+_matrix_p = C.POINTER(_Matrix)
+_lib.dol_cross_entropy_workspace.argtypes = [_matrix_p, _matrix_p, C.c_int32, C.POINTER(C.c_int64)]
+_lib.dol_cross_entropy.argtypes = [_matrix_p, _matrix_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+_lib.dol_cross_entropy_backward.argtypes = [_matrix_p, _matrix_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, _matrix_p, _matrix_p,
+                                            C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+
+
+def _matrix(t: torch.Tensor) -> _Matrix:
+    """A float32 or bfloat16 tensor [rows, cols] with neighbouring columns next to each other."""
+    assert t.is_cuda and t.dtype in _DTYPES and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1)
+    rows, cols = t.shape
+    assert rows <= 1 or t.stride(0) >= cols
+    return _Matrix(_DTYPES[t.dtype], rows, cols, t.stride(0) if rows > 1 else max(cols, 1), t.data_ptr())
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype=torch.float32):
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == dtype and t.shape == (n,) and t.is_contiguous()
+    return t.data_ptr()
+
+
+def _workspace(given: Optional[torch.Tensor], n: int, device, stream):
+    """(address, bytes, what keeps it): the caller's workspace, or n bytes of torch's allocator, which may hand them out again
+    once the stream that the call is on has passed it."""
+    if given is not None:
+        assert given.is_cuda and given.is_contiguous()
+        return given.data_ptr(), given.numel() * given.element_size(), given
+    if n == 0:
+        return None, 0, None
+    t = torch.empty(n, dtype=torch.uint8, device=device)
+    if stream is not None:
+        t.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+    return t.data_ptr(), n, t
+
+
+def cross_entropy_workspace(x: torch.Tensor, weight: torch.Tensor, backward: bool = False) -> int:
+    """Bytes that cross_entropy (or cross_entropy_backward) needs for these operands."""
+    n = C.c_int64()
+    _check(_lib.dol_cross_entropy_workspace(C.byref(_matrix(x)), C.byref(_matrix(weight)), int(backward), C.byref(n)))
+    return n.value
+
+
+def cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                  bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """loss[i] = lse[i] - (x[i] . weight[target[i]] + bias[target[i]]), lse the log of the sum of the exponentials over all classes.
+
+    x [rows, width], weight [classes, width] (float32 or bfloat16); target int32 [rows], rows outside 0..classes-1 are left out;
+    loss, lse float32 [rows]; bias float32 [classes]; workspace: any tensor of cross_entropy_workspace bytes, or None."""
+    mx, mw = _matrix(x), _matrix(weight)
+    need = C.c_int64()
+    if workspace is None:
+        _check(_lib.dol_cross_entropy_workspace(mx, mw, 0, need))
+    ws, n, _keep = _workspace(workspace, need.value, x.device, stream)
+    _check(_lib.dol_cross_entropy(mx, mw, _vector(bias, mw.rows), _vector(target, mx.rows, torch.int32), _vector(loss, mx.rows),
+                                  _vector(lse, mx.rows), ws, n, _stream(stream)))
+
+
+def cross_entropy_backward(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor,
+                           grad_x: Optional[torch.Tensor], grad_weight: Optional[torch.Tensor], bias: Optional[torch.Tensor] = None,
+                           grad_bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of sum_i grad_loss[i] loss[i]; lse as cross_entropy left it.  Gradients that are None are not computed."""
+    mx, mw = _matrix(x), _matrix(weight)
+    need = C.c_int64()
+    if workspace is None:
+        _check(_lib.dol_cross_entropy_workspace(mx, mw, 1, need))
+    ws, n, _keep = _workspace(workspace, need.value, x.device, stream)
+    _check(_lib.dol_cross_entropy_backward(mx, mw, _vector(bias, mw.rows), _vector(target, mx.rows, torch.int32), _vector(lse, mx.rows),
+                                           _vector(grad_loss, mx.rows), None if grad_x is None else _matrix(grad_x),
+                                           None if grad_weight is None else _matrix(grad_weight), _vector(grad_bias, mw.rows), ws, n,
+                                           _stream(stream)))

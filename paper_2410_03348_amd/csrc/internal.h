@@ -21,6 +21,9 @@ namespace dol {
 void set_error(const char *fmt, ...) __attribute__((format(printf, 1, 2)));
 dol_status fail(dol_status st, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 dol_status hip_fail(hipError_t e, const char *what);
+// Checks of the training operators' arguments (cross_entropy.hip).
+dol_status check_matrix(const dol_matrix *m, const char *name);
+dol_status check_workspace(const void *workspace, int64_t has, int64_t needs);
 
 #define DOL_HIP(call)                                        \
     do {                                                     \

@@ -1,0 +1,235 @@
+// Tiles of matrix products on the matrix cores, for the operators that are made of them (cross_entropy.hip, newton_schulz.hip).
+//
+// C[m, n] = sum_k A[m, k] * B[n, k], both operands row-major with k contiguous ("planes" of 16-bit elements), sums in 32 bits.
+// A number that 16 bits do not hold is the sum of up to three planes, and a product of such numbers the products of their
+// planes whose magnitudes a 32-bit sum would see:
+//   1 plane   bf16 or fp16 as it is                                     1 product
+//   2 planes  fp16, 22 bits and a sign: x = x0 + x1                     x0 y0 + x0 y1 + x1 y0        (dropped: 2^-24 of x y)
+//   3 planes  bf16, 24 bits over the whole range of a float             six products, x1 y2, x2 y1, x2 y2 dropped
+#pragma once
+
+#include "internal.h"
+#include "wave_util.h"
+
+namespace dol {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// v_mfma_f32_16x16x32: lane l gives row l & 15, k = 8 (l >> 4) .. + 7 of each operand and gets rows 4 (l >> 4) .. + 3 of column l & 15.
+template <typename V>
+struct Mfma;
+template <>
+struct Mfma<bf16x8> {
+    using E = __bf16;
+    __device__ static f32x4 go(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mfma<f16x8> {
+    using E = _Float16;
+    __device__ static f32x4 go(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+
+// Bits of x rounded to the nearest E.
+template <typename E>
+__device__ __forceinline__ uint32_t bits16(float x)
+{
+    return __builtin_bit_cast(uint16_t, static_cast<E>(x));
+}
+
+// x rounded to E, and what is left of it for the next plane (nothing, where x or its rounding is not finite: inf - inf is NaN).
+template <typename E>
+__device__ __forceinline__ uint32_t take_plane(float &x)
+{
+    const E h = static_cast<E>(x);
+    const float r = x - static_cast<float>(h);
+    x = r == r ? r : 0.0f;
+    return __builtin_bit_cast(uint16_t, h);
+}
+
+// 64 lanes' 16 bytes straight to LDS, lane l's at lds + 16 l (lds: the same in every lane).
+__device__ __forceinline__ void load_to_lds16(const void *g, uint32_t lds)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
+                                     (__attribute__((address_space(3))) void *)static_cast<uintptr_t>(lds), 16, 0, 0);
+}
+
+// Waits until at most N loads to LDS are on their way and every LDS read has returned.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+struct Planes {
+    const uint16_t *data;
+    int64_t ld;         // elements from row to row, a multiple of 8
+    int64_t plane;      // elements from plane to plane
+};
+
+// A tile of BM x BN by WM x WN wavefronts, ST stages of BK.  Rows lie in LDS as lines of 128 bytes (one row of 64 elements or two of
+// 32) whose 16-byte pieces are exchanged by an exclusive or with the line's number, so that eight neighbouring lanes of a read touch
+// all banks once.  The loads to LDS put lane l's piece at 16 l, so it is the lanes' addresses in memory that are exchanged.
+// A row of B that lane c of fragment j takes is 4 c + j of the wavefront's 64: a lane then holds four neighbouring columns of C in
+// acc[i][0..3], and a row of C leaves as 8- or 16-byte pieces, 16 lanes to a line.
+template <typename V_, int P_, int BM_, int BN_, int BK_, int WM_, int WN_, int ST_>
+struct MfmaTile {
+    using V = V_;
+    using E = typename Mfma<V>::E;
+    static constexpr int P = P_, BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, ST = ST_;
+    static constexpr int NW = WM * WN, NT = NW * 64;
+    static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
+    static constexpr int CPR = BK / 8, RPL = 64 / BK;                   // pieces to a row, rows to a line
+    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = P * (A_BYTES + B_BYTES);
+    static constexpr int LA = A_BYTES / (NT * 16), LB = B_BYTES / (NT * 16), LOADS = P * (LA + LB);
+    static constexpr int LDS = ST * STAGE > BM * BN * 2 ? ST * STAGE : BM * BN * 2;   // the epilogues lay out a tile of 16 bits
+    static_assert(NI == 4 && (BK == 32 || BK == 64) && A_BYTES % (NT * 16) == 0 && B_BYTES % (NT * 16) == 0 && ST >= 2, "tile");
+
+    __device__ static int key_a(int line) { return line & 7; }
+    __device__ static int key_b(int line) { return (RPL == 1 ? line >> 2 : line >> 1) & 7; }
+    template <bool IS_B>
+    __device__ static int place(int row, int c)
+    {
+        const int line = row / RPL, s = (row % RPL) * CPR + c;
+        return line * 128 + ((s ^ (IS_B ? key_b(line) : key_a(line))) << 4);
+    }
+
+    // This lane's offsets in bytes from the tile's first row; rows past the operand's end repeat its last one (the caller ignores them).
+    template <bool IS_B, int L>
+    __device__ static void offsets(uint32_t (&o)[L], int wave, int lane, int64_t first, int64_t rows, int64_t ld)
+    {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            const int line = (i * NW + wave) * 8 + (lane >> 3), s = (lane & 7) ^ (IS_B ? key_b(line) : key_a(line));
+            int64_t r = line * RPL + s / CPR;
+            r = first + r < rows ? r : rows - 1 - first;
+            o[i] = static_cast<uint32_t>(r * ld + (s % CPR) * 8) * 2;
+        }
+    }
+
+    // acc = rows m0.. of a (of M) times rows n0.. of b (of N), over elements k0 .. k0 + BK * steps of each row.
+    __device__ static void run(const Planes &a, int64_t m0, int64_t M, const Planes &b, int64_t n0, int64_t N, int64_t k0, int steps, char *smem,
+                               f32x4 (&acc)[MI][NI])
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int wm = wave / WN, wn = wave % WN;
+        const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)smem));
+        uint32_t ao[LA], bo[LB];
+        offsets<false>(ao, wave, lane, m0, M, a.ld);
+        offsets<true>(bo, wave, lane, n0, N, b.ld);
+        const char *ab = reinterpret_cast<const char *>(a.data + m0 * a.ld + k0), *bb = reinterpret_cast<const char *>(b.data + n0 * b.ld + k0);
+        auto issue = [&](int kt, int st) {
+            const uint32_t base = lds0 + st * STAGE + wave * 1024;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+#pragma unroll
+                for (int i = 0; i < LA; ++i)
+                    load_to_lds16(ab + (p * a.plane + static_cast<int64_t>(kt) * BK) * 2 + ao[i], base + p * A_BYTES + i * NW * 1024);
+#pragma unroll
+                for (int i = 0; i < LB; ++i)
+                    load_to_lds16(bb + (p * b.plane + static_cast<int64_t>(kt) * BK) * 2 + bo[i], base + P * A_BYTES + p * B_BYTES + i * NW * 1024);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < ST - 1; ++s)
+            if (s < steps) issue(s, s);
+        const int r16 = lane & 15, c4 = lane >> 4;
+        for (int kt = 0, st = 0; kt < steps; ++kt) {
+            // this step's loads have landed, here and (after the barrier) everywhere; the buffer read last is free again
+            if (kt + ST - 1 <= steps) wait_loads<LOADS * (ST - 2)>();
+            else wait_loads<0>();
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (kt + ST - 1 < steps) issue(kt + ST - 1, st == 0 ? ST - 1 : st - 1);
+            const char *sa = smem + st * STAGE, *sb = sa + P * A_BYTES;
+#pragma unroll
+            for (int kk = 0; kk < BK / 32; ++kk) {
+                V fa[P][MI], fb[P][NI];
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) fb[p][j] = *reinterpret_cast<const V *>(sb + p * B_BYTES + place<true>(wn * TN + r16 * 4 + j, kk * 4 + c4));
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) fa[p][i] = *reinterpret_cast<const V *>(sa + p * A_BYTES + place<false>(wm * TM + i * 16 + r16, kk * 4 + c4));
+                }
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) {      // small products first
+                        if constexpr (P == 3) {
+                            acc[i][j] = Mfma<V>::go(fa[2][i], fb[0][j], acc[i][j]);
+                            acc[i][j] = Mfma<V>::go(fa[0][i], fb[2][j], acc[i][j]);
+                            acc[i][j] = Mfma<V>::go(fa[1][i], fb[1][j], acc[i][j]);
+                        }
+                        if constexpr (P >= 2) {
+                            acc[i][j] = Mfma<V>::go(fa[1][i], fb[0][j], acc[i][j]);
+                            acc[i][j] = Mfma<V>::go(fa[0][i], fb[1][j], acc[i][j]);
+                        }
+                        acc[i][j] = Mfma<V>::go(fa[0][i], fb[0][j], acc[i][j]);
+                    }
+            }
+            st = st == ST - 1 ? 0 : st + 1;
+        }
+    }
+
+    // acc[i][j][e] is row row_of(i) + e and column col_of() + j of the tile.
+    __device__ static int row_of(int i) { return (threadIdx.x >> 6) / WN * TM + i * 16 + ((threadIdx.x & 63) >> 4) * 4; }
+    __device__ static int col_of() { return (threadIdx.x >> 6) % WN * TN + (threadIdx.x & 15) * 4; }
+
+    // Lays a plane of the tile out by columns and writes it as rows of the transpose: value(i, j, e) gives the bits of an element;
+    // out + n * ld + m receives element (m, n) for n < cols.  All threads call it; smem may hold anything else.  ld and out: multiples
+    // of 8 elements; the tile's BM rows must fit.
+    template <typename F>
+    __device__ static void store_transposed(char *smem, uint16_t *out, int64_t ld, int64_t cols, F value)
+    {
+        constexpr int PIECES = BM / 8;
+        lds_barrier();
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const int m = row_of(i), n = col_of() + j;
+                u32x2 w;
+                w[0] = value(i, j, 0) | value(i, j, 1) << 16, w[1] = value(i, j, 2) | value(i, j, 3) << 16;
+                *reinterpret_cast<u32x2 *>(smem + n * (BM * 2) + (((m >> 3) ^ ((n >> 2) & 15)) << 4) + (m & 4) * 2) = w;
+            }
+        lds_barrier();
+#pragma unroll 4
+        for (int t = threadIdx.x; t < BN * PIECES; t += NT) {
+            const int n = t / PIECES, c = t % PIECES;
+            if (n < cols) *reinterpret_cast<u32x4 *>(out + n * ld + c * 8) = *reinterpret_cast<const u32x4 *>(smem + n * (BM * 2) + ((c ^ ((n >> 2) & 15)) << 4));
+        }
+    }
+};
+
+// Tile w of tm x tn in an order that keeps neighbouring ones close in both directions: bands of `band` rows of tiles, column by column.
+__device__ __forceinline__ void tile_of(int w, int tm, int tn, int band, int &mt, int &nt)
+{
+    const int per = band * tn, b = w / per, first = b * band, height = min(tm - first, band), r = w - b * per;
+    mt = first + r % height, nt = r / height;
+}
+
+inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Hands out parts of a caller's workspace, 256 bytes apart.  With no memory it only counts.
+struct Carver {
+    char *base;
+    int64_t used = 0;
+    explicit Carver(void *p) : base(static_cast<char *>(p)) {}
+    template <typename T>
+    T *take(int64_t n)
+    {
+        T *p = base ? reinterpret_cast<T *>(base + used) : nullptr;
+        used += round_up(n * static_cast<int64_t>(sizeof(T)), 256);
+        return p;
+    }
+};
+
+}  // namespace dol

@@ -1,0 +1,289 @@
+"""dol_cross_entropy and its gradients against the definition in 64 bits, through the binding (needs an MI355X).
+
+Bars, from the rounding the operator states: u = 2^-24 (float) for sums and exponentials, w = 2^-8 for a number rounded to bf16.
+  a logit        |dl| <= L = 16 u sum_k |x_ik w_vk|  (its products exact or to 2^-24; a sum of n terms in 32 bits errs by some sqrt(n) u of
+                 their magnitudes, blocks of 16 and 32 at a time: 16 covers rows of 1 024)
+  lse, loss      L + 8 u (1 + |lse|), the exponentials' own roundings and that of the result
+  a gradient     its terms' magnitudes S times (2 max L + 32 u), and w (S + |result|) where dl and the result are bf16
+"""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+U, W8 = 2.0 ** -24, 2.0 ** -8
+
+
+@pytest.fixture(scope="module")
+def dol():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2410_03348_amd import binding
+    return binding
+
+
+def padded(t, pad, value=7.0):
+    """The same values as a view into a wider tensor whose other columns hold `value`."""
+    buf = torch.full((t.shape[0], t.shape[1] + pad), value, dtype=t.dtype, device="cuda")
+    buf[:, :t.shape[1]] = t
+    return buf, buf[:, :t.shape[1]]
+
+
+def make(n, d, v, dtype, seed=0, bias=True, scale=2.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(n, d, generator=gen, device="cuda").to(dtype)
+    w = (torch.randn(v, d, generator=gen, device="cuda") * scale / d ** 0.5).to(dtype)
+    b = torch.randn(v, generator=gen, device="cuda") * 0.5 if bias else None
+    t = torch.randint(0, v, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    g = torch.rand(n, generator=gen, device="cuda") * 2 - 0.5
+    return x, w, b, t, g
+
+
+def reference(x, w, b, t, g):
+    """Everything in 64 bits on the host; also the magnitudes that the bars are made of."""
+    x, w = x.detach().cpu().double().numpy(), w.detach().cpu().double().numpy()
+    t, g = t.cpu().numpy(), g.cpu().double().numpy()
+    v = w.shape[0]
+    kept = (t >= 0) & (t < v)
+    with np.errstate(all="ignore"):
+        logits = x @ w.T + (0.0 if b is None else b.cpu().double().numpy())
+        top = logits.max(axis=1)
+        base = np.where(np.isfinite(top), top, 0.0)
+        lse = base + np.log(np.exp(logits - base[:, None]).sum(axis=1))
+        loss = np.where(kept, np.where(lse == -np.inf, np.inf, lse - logits[np.arange(len(t)), np.where(kept, t, 0)]), 0.0)
+        counts = kept & (lse != -np.inf)
+        dl = np.where(counts[:, None], np.exp(logits - lse[:, None]), 0.0)
+    dl[np.flatnonzero(counts), t[counts]] -= 1.0
+    dl = np.where(counts[:, None], dl * g[:, None], 0.0)
+    xk = np.where(kept[:, None], x, 0.0)
+    err_l = 16 * U * (np.abs(xk) @ np.abs(w).T)
+    return dict(lse=lse, loss=loss, grad_x=dl @ w, grad_w=dl.T @ xk, grad_b=dl.sum(axis=0), kept=kept,
+                size_x=np.abs(dl) @ np.abs(w), size_w=np.abs(dl).T @ np.abs(xk), size_b=np.abs(dl).sum(axis=0), err_l=err_l)
+
+
+def within(got, want, bar, what):
+    got = got.detach().cpu().double().numpy()
+    assert got.shape == want.shape
+    fine = np.isfinite(want)
+    np.testing.assert_array_equal(got[~fine], want[~fine], err_msg=what)
+    off = np.abs(got - want)[fine] - np.broadcast_to(bar, want.shape)[fine]
+    assert off.size == 0 or off.max() <= 0, "%s: %g over its bar" % (what, off.max())
+
+
+def run_and_check(dol, x, w, b, t, g, pad=0):
+    n, d = x.shape
+    v = w.shape[0]
+    ref = reference(x, w, b, t, g)
+    loss, lse = torch.full((n,), 9.0, device="cuda"), torch.full((n,), 9.0, device="cuda")
+    gx_buf, gx = padded(torch.full_like(x, 5.0), pad)
+    gw_buf, gw = padded(torch.full_like(w, 5.0), pad)
+    gb = torch.full((v,), 5.0, device="cuda") if b is not None else None
+    # workspaces of exactly the size asked for, between guards that nothing may touch
+    for backward in (False, True):
+        size = dol.cross_entropy_workspace(x, w, backward)
+        guard = torch.full((size + 2048,), 77, dtype=torch.uint8, device="cuda")
+        ws = guard[1024:1024 + size]
+        if backward:
+            dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b, grad_bias=gb, workspace=ws)
+        else:
+            dol.cross_entropy(x, w, t, loss, lse, bias=b, workspace=ws)
+        assert bool((guard[:1024] == 77).all()) and bool((guard[1024 + size:] == 77).all())
+    top_l = ref["err_l"].max(axis=1, initial=0.0)
+    kept = ref["kept"]
+    bar = top_l + 8 * U * (1 + np.abs(np.where(np.isfinite(ref["lse"]), ref["lse"], 0.0)))
+    within(lse[torch.from_numpy(kept).cuda()], ref["lse"][kept], bar[kept], "lse")
+    within(loss, ref["loss"], 2 * bar, "loss")
+    rel = 2 * ref["err_l"].max(initial=0.0) + 32 * U
+    bf = x.dtype == torch.bfloat16
+    within(gx, ref["grad_x"], ref["size_x"] * (rel + W8 * bf) + W8 * bf * np.abs(ref["grad_x"]) + 1e-37, "grad_x")
+    within(gw, ref["grad_w"], ref["size_w"] * (rel + W8 * bf) + W8 * bf * np.abs(ref["grad_w"]) + 1e-37, "grad_weight")
+    if gb is not None:
+        within(gb, ref["grad_b"], ref["size_b"] * rel + 1e-37, "grad_bias")
+    if pad:
+        assert bool((gx_buf[:, d:] == 7).all()) and bool((gw_buf[:, d:] == 7).all())
+    return loss, lse, gx, gw, gb
+
+
+SIZES = [(1, 1, 1), (1, 16, 2), (64, 128, 10), (5, 7, 3), (129, 65, 257), (300, 64, 300), (257, 200, 1025), (40, 1024, 700), (700, 96, 129),
+         (2, 33, 9000), (1500, 24, 40)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,d,v", SIZES)
+def test_sizes(dol, n, d, v, dtype):
+    x, w, b, t, g = make(n, d, v, getattr(torch, dtype), seed=n + d + v)
+    run_and_check(dol, x, w, b, t, g)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("pad,shift", [(1, 0), (8, 0), (3, 1), (64, 8)])
+def test_strides_and_alignment(dol, dtype, pad, shift):
+    """Rows of any stride, from any element; the gradients' rows too, whose other columns stay as they are."""
+    x, w, b, t, g = make(150, 128 + shift, 200, getattr(torch, dtype), seed=pad)
+    x, w = padded(x, pad, float("nan"))[1][:, shift:], padded(w, pad, float("nan"))[1][:, shift:]
+    run_and_check(dol, x, w, b, t, g, pad)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_left_out(dol, dtype):
+    """Targets outside the classes: no loss, no gradient, and what such a row or its grad_loss holds reaches nobody."""
+    x, w, b, t, g = make(200, 64, 90, getattr(torch, dtype), seed=3)
+    t[::3] = -1
+    t[1::7] = 90
+    t[2::11] = 2 ** 31 - 1
+    out = (t < 0) | (t >= 90)
+    x[out] = float("nan")
+    x[5 * 3] = float("inf")
+    g[out] = float("nan")
+    loss, lse, gx, gw, gb = run_and_check(dol, x, w, b, t, g)
+    assert bool((loss[out] == 0).all()) and bool((gx[out] == 0).all())
+    # and all of them
+    t[:] = -5
+    loss, lse, gx, gw, gb = run_and_check(dol, x, w, b, t, g)
+    assert not loss.any() and not gx.any() and not gw.any() and not gb.any()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("v", [10, 300, 1000])
+def test_classes_taken_out(dol, dtype, v):
+    """A bias of -inf takes a class out: whole tiles of them, the target's own (loss +inf, gradient -g at the target), all of them."""
+    x, w, b, t, g = make(70, 32, v, getattr(torch, dtype), seed=v)
+    b[: v * 3 // 4] = float("-inf")
+    b[v - 1] = float("-inf")
+    loss, *_ = run_and_check(dol, x, w, b, t, g)
+    assert bool(torch.isinf(loss).any())
+    b[:] = float("-inf")
+    loss, lse, gx, gw, gb = run_and_check(dol, x, w, b, t, g)
+    assert bool((loss == float("inf")).all()) and bool((lse == float("-inf")).all()) and not gx.any() and not gw.any() and not gb.any()
+    b[:] = torch.finfo(torch.float32).min           # the type's lowest value is a number
+    b[v // 2] = 0.0
+    run_and_check(dol, x, w, b, torch.full_like(t, v // 2), g)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_nan_stays_in_its_row(dol, dtype):
+    x, w, b, t, g = make(150, 64, 400, getattr(torch, dtype), seed=8)
+    clean = run_and_check(dol, x, w, b, t, g)[0].clone()
+    x[77, 3] = float("nan")
+    n = x.shape[0]
+    loss, lse, gx, gw = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+    dol.cross_entropy(x, w, t, loss, lse, bias=b)
+    dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b)
+    others = torch.arange(n, device="cuda") != 77
+    assert bool(torch.isnan(loss[77])) and bool(torch.isnan(gx[77]).all()) and bool(torch.isfinite(gx[others]).all())
+    assert torch.equal(loss[others], clean[others])
+
+
+def test_large_logits_and_small_ones(dol):
+    """Logits of thousands, where every other class underflows, and a table of tiny numbers, where every class is as likely."""
+    x, w, b, t, g = make(100, 64, 500, torch.float32, seed=11, scale=800.0)
+    run_and_check(dol, x, w, b, t, g)
+    x, w, b, t, g = make(100, 64, 500, torch.float32, seed=12)
+    run_and_check(dol, x, w * 1e-30, None, t, g)
+
+
+def test_pieces_and_splits(dol):
+    """More classes than one piece of dl holds, and rows enough to split the k of both products."""
+    for dtype, n, d, v in ((torch.bfloat16, 8300, 64, 17000), (torch.float32, 5000, 40, 9000)):
+        x, w, b, t, g = make(n, d, v, dtype, seed=2)
+        t[::9] = -1
+        run_and_check(dol, x, w, b, t, g)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_same_bits_twice_and_any_subset(dol, dtype):
+    x, w, b, t, g = make(513, 72, 1500, getattr(torch, dtype), seed=21)
+    a = run_and_check(dol, x, w, b, t, g)
+    loss, lse, gx, gw, gb = (torch.empty_like(q) for q in a)
+    dol.cross_entropy(x, w, t, loss, lse, bias=b)
+    dol.cross_entropy_backward(x, w, t, lse, g, gx, None, bias=b)
+    dol.cross_entropy_backward(x, w, t, lse, g, None, gw, bias=b)
+    dol.cross_entropy_backward(x, w, t, lse, g, None, None, bias=b, grad_bias=gb)
+    for p, q in zip(a, (loss, lse, gx, gw, gb)):
+        assert torch.equal(p, q)
+
+
+def test_against_differences(dol):
+    """grad_x and grad_weight against central differences of the loss that the forward call gives."""
+    x, w, b, t, g = make(6, 20, 30, torch.float32, seed=31)
+    t[2] = -1
+
+    def value(x, w, b):
+        loss, lse = torch.empty(6, device="cuda"), torch.empty(6, device="cuda")
+        dol.cross_entropy(x, w, t, loss, lse, bias=b)
+        return (loss.double() * g.double()).sum(), lse
+
+    _, lse = value(x, w, b)
+    gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b, grad_bias=gb)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    h = 2.0 ** -7
+    for _ in range(4):
+        dx, dw, db = (torch.randn(q.shape, generator=gen, device="cuda") for q in (x, w, b))
+        num = (value(x + h * dx, w + h * dw, b + h * db)[0] - value(x - h * dx, w - h * dw, b - h * db)[0]) / (2 * h)
+        ana = (gx.double() * dx).sum() + (gw.double() * dw).sum() + (gb.double() * db).sum()
+        # differences err by h^2 of a third derivative (logits move by some 5 h: 125 h^2 / 6 of a loss of order 1 in each row) and by
+        # the losses' roundings over h
+        assert abs(float(num - ana)) <= 6 * 125 / 6 * h * h + 6 * 32 * U * 8 / h
+
+
+def test_on_another_stream_and_in_a_graph(dol):
+    x, w, b, t, g = make(300, 64, 700, torch.bfloat16, seed=41)
+    a = run_and_check(dol, x, w, b, t, g)
+    outs = [torch.empty_like(q) for q in a]
+    loss, lse, gx, gw, gb = outs
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    dol.cross_entropy(x, w, t, loss, lse, bias=b, stream=side)
+    dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b, grad_bias=gb, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    for p, q in zip(a, outs):
+        assert torch.equal(p, q)
+    wf = torch.empty(max(dol.cross_entropy_workspace(x, w), dol.cross_entropy_workspace(x, w, True)), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dol.cross_entropy(x, w, t, loss, lse, bias=b, workspace=wf)
+        dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b, grad_bias=gb, workspace=wf)
+    for _ in range(3):
+        for q in outs:
+            q.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for p, q in zip(a, outs):
+            assert torch.equal(p, q)
+
+
+def test_no_rows(dol):
+    x, w, b, t, g = make(4, 16, 20, torch.float32)
+    gw, gb, e = torch.full_like(w, 3.0), torch.full_like(b, 3.0), torch.empty(0, device="cuda")
+    dol.cross_entropy(x[:0], w, t[:0], e, e, bias=b)
+    dol.cross_entropy_backward(x[:0], w, t[:0], e, e, x[:0], gw, bias=b, grad_bias=gb)
+    assert not gw.any() and not gb.any()
+
+
+def test_refusals(dol):
+    x, w, b, t, g = make(8, 16, 20, torch.float32)
+    loss, lse = torch.full((8,), 9.0, device="cuda"), torch.full((8,), 9.0, device="cuda")
+    with pytest.raises(dol.DolError, match="ESHAPE"):
+        dol.cross_entropy(x[:, :15], w, t, loss, lse)
+    with pytest.raises(dol.DolError, match="types"):
+        dol.cross_entropy(x.bfloat16(), w, t, loss, lse)
+    with pytest.raises(dol.DolError, match="classes"):
+        dol.cross_entropy(x, w[:0], t, loss, lse)
+    with pytest.raises(dol.DolError, match="workspace has 16 bytes"):
+        dol.cross_entropy(x, w, t, loss, lse, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(dol.DolError, match="aligned"):
+        dol.cross_entropy(x, w, t, loss, lse, workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[16:])
+    with pytest.raises(dol.DolError, match="no gradient"):
+        dol.cross_entropy_backward(x, w, t, lse, g, None, None)
+    with pytest.raises(dol.DolError, match="ESHAPE"):
+        dol.cross_entropy_backward(x, w, t, lse, g, x[:4], None)
+    with pytest.raises(dol.DolError, match="another type"):
+        dol.cross_entropy_backward(x, w, t, lse, g, x.bfloat16(), None)
+    for bad in (x.double(), x.cpu(), x.t(), x[0]):
+        with pytest.raises(AssertionError):
+            dol.cross_entropy(bad, w, t, loss, lse)
+    with pytest.raises(AssertionError):
+        dol.cross_entropy(x, w, t.long(), loss, lse)
+    assert bool((loss == 9).all()) and bool((lse == 9).all())
