@@ -439,6 +439,19 @@ dol_status dol_cross_entropy_backward(const dol_matrix *x, const dol_matrix *wei
                                       const float *lse, const float *grad_loss, const dol_matrix *grad_x, const dol_matrix *grad_weight,
                                       float *grad_bias, void *workspace, int64_t workspace_bytes, void *hip_stream);
 
+/* An update's orthogonalisation by Newton-Schulz products: X = G / (|G| + eps) (Frobenius norm), then `steps` times
+ *   A = X X^T,   B = b A + c A A,   X <- a X + B X,   out = X
+ * with (a, b, c) = coefficients, host [3]; a matrix with more rows than columns is taken as its transpose, and so is its result.  Each
+ * singular value s of X becomes s (a + b s^2 + c s^4) in a step: those of G end near 1 while its singular vectors stay.
+ *   g, out   `batch` matrices of one size and type, g_stride and out_stride elements apart (ignored for one); out may be g
+ * DOL_F32 is as exact as sums of 32-bit numbers in 32 bits; DOL_BF16 takes its products of numbers of 11 bits, which with the result's
+ * own rounding leaves some 2.4e-3 of it.
+ * DOL_EUNSUPPORTED where the coefficients let singular values pass 64, for sides above 2^20 and for more than 65 535 matrices. */
+dol_status dol_newton_schulz_workspace(const dol_matrix *g, int32_t batch, int64_t *bytes);
+dol_status dol_newton_schulz(const dol_matrix *g, int64_t g_stride, const dol_matrix *out, int64_t out_stride, int32_t batch,
+                             int32_t steps, const float *coefficients, float eps, void *workspace, int64_t workspace_bytes,
+                             void *hip_stream);
+
 /* Message of the calling thread's most recent failing call ("" if none). */
 const char *dol_last_error(void);
 /* Library version, e.g. "0.1.0". */

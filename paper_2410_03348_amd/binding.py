@@ -737,3 +737,39 @@ def cross_entropy_backward(x: torch.Tensor, weight: torch.Tensor, target: torch.
                                            _vector(grad_loss, mx.rows), None if grad_x is None else _matrix(grad_x),
                                            None if grad_weight is None else _matrix(grad_weight), _vector(grad_bias, mw.rows), ws, n,
                                            _stream(stream)))
+
+
+_lib.dol_newton_schulz_workspace.argtypes = [_matrix_p, C.c_int32, C.POINTER(C.c_int64)]
+_lib.dol_newton_schulz.argtypes = [_matrix_p, C.c_int64, _matrix_p, C.c_int64, C.c_int32, C.c_int32, C.POINTER(C.c_float), C.c_float,
+                                   C.c_void_p, C.c_int64, C.c_void_p]
+
+
+def _matrices(t: torch.Tensor):
+    """(the first matrix, elements from one to the next, how many) of a tensor [rows, cols] or [batch, rows, cols]."""
+    assert t.dim() in (2, 3)
+    if t.dim() == 2:
+        return _matrix(t), 0, 1
+    b, rows, cols = t.shape
+    assert t.is_cuda and t.dtype in _DTYPES and (cols <= 1 or t.stride(2) == 1) and (rows <= 1 or t.stride(1) >= cols)
+    return _Matrix(_DTYPES[t.dtype], rows, cols, t.stride(1) if rows > 1 else max(cols, 1), t.data_ptr()), t.stride(0), b
+
+
+def newton_schulz_workspace(g: torch.Tensor) -> int:
+    m, _, batch = _matrices(g)
+    n = C.c_int64()
+    _check(_lib.dol_newton_schulz_workspace(m, batch, n))
+    return n.value
+
+
+def newton_schulz(g: torch.Tensor, out: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
+                  workspace: Optional[torch.Tensor] = None, stream=None):
+    """out = X after `steps` times X <- a X + (b A + c A A) X, A = X X^T, from X = g / (|g| + eps): g's singular vectors with singular
+    values near 1.  g, out: [rows, cols] or [batch, rows, cols], float32 or bfloat16; out may be g."""
+    mg, g_stride, batch = _matrices(g)
+    mo, out_stride, n_out = _matrices(out)
+    assert batch == n_out
+    need = C.c_int64()
+    if workspace is None:
+        _check(_lib.dol_newton_schulz_workspace(mg, batch, need))
+    ws, n, _keep = _workspace(workspace, need.value, g.device, stream)
+    _check(_lib.dol_newton_schulz(mg, g_stride, mo, out_stride, batch, steps, (C.c_float * 3)(*coefficients), eps, ws, n, _stream(stream)))

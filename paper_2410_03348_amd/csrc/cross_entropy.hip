@@ -315,23 +315,6 @@ struct Product {
     int64_t out_ld;
 };
 
-template <typename O>
-__device__ __forceinline__ void store4(O *p, f32x4 v, int n, bool vec)
-{
-    if (vec && n >= 4) {
-        if constexpr (sizeof(O) == 4) *reinterpret_cast<f32x4 *>(p) = v;
-        else {
-            u32x2 w;
-            w[0] = bits16<__bf16>(v[0]) | bits16<__bf16>(v[1]) << 16, w[1] = bits16<__bf16>(v[2]) | bits16<__bf16>(v[3]) << 16;
-            *reinterpret_cast<u32x2 *>(p) = w;
-        }
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (k < n) p[k] = static_cast<O>(v[k]);
-}
-
 template <typename T, typename O>
 __global__ void __launch_bounds__(T::NT, 2) xent_products_kernel(Product p0, Product p1)
 {

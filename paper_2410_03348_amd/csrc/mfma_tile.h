@@ -189,7 +189,7 @@ struct MfmaTile {
     template <typename F>
     __device__ static void store_transposed(char *smem, uint16_t *out, int64_t ld, int64_t cols, F value)
     {
-        constexpr int PIECES = BM / 8;
+        constexpr int PIECES = BM / 8, KEY = PIECES < 16 ? PIECES - 1 : 15;     // 16 lanes' columns, 4 apart, to different banks
         lds_barrier();
 #pragma unroll
         for (int i = 0; i < MI; ++i)
@@ -198,16 +198,34 @@ struct MfmaTile {
                 const int m = row_of(i), n = col_of() + j;
                 u32x2 w;
                 w[0] = value(i, j, 0) | value(i, j, 1) << 16, w[1] = value(i, j, 2) | value(i, j, 3) << 16;
-                *reinterpret_cast<u32x2 *>(smem + n * (BM * 2) + (((m >> 3) ^ ((n >> 2) & 15)) << 4) + (m & 4) * 2) = w;
+                *reinterpret_cast<u32x2 *>(smem + n * (BM * 2) + (((m >> 3) ^ ((n >> 2) & KEY)) << 4) + (m & 4) * 2) = w;
             }
         lds_barrier();
 #pragma unroll 4
         for (int t = threadIdx.x; t < BN * PIECES; t += NT) {
             const int n = t / PIECES, c = t % PIECES;
-            if (n < cols) *reinterpret_cast<u32x4 *>(out + n * ld + c * 8) = *reinterpret_cast<const u32x4 *>(smem + n * (BM * 2) + ((c ^ ((n >> 2) & 15)) << 4));
+            if (n < cols) *reinterpret_cast<u32x4 *>(out + n * ld + c * 8) = *reinterpret_cast<const u32x4 *>(smem + n * (BM * 2) + ((c ^ ((n >> 2) & KEY)) << 4));
         }
     }
 };
+
+// The first n (at most four) of v to p; `vec`: p is aligned to four elements.
+template <typename O>
+__device__ __forceinline__ void store4(O *p, f32x4 v, int n, bool vec)
+{
+    if (vec && n >= 4) {
+        if constexpr (sizeof(O) == 4) *reinterpret_cast<f32x4 *>(p) = v;
+        else {
+            u32x2 w;
+            w[0] = bits16<__bf16>(v[0]) | bits16<__bf16>(v[1]) << 16, w[1] = bits16<__bf16>(v[2]) | bits16<__bf16>(v[3]) << 16;
+            *reinterpret_cast<u32x2 *>(p) = w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (k < n) p[k] = static_cast<O>(v[k]);
+}
 
 // Tile w of tm x tn in an order that keeps neighbouring ones close in both directions: bands of `band` rows of tiles, column by column.
 __device__ __forceinline__ void tile_of(int w, int tm, int tn, int band, int &mt, int &nt)
