@@ -452,6 +452,32 @@ dol_status dol_newton_schulz(const dol_matrix *g, int64_t g_stride, const dol_ma
                              int32_t steps, const float *coefficients, float eps, void *workspace, int64_t workspace_bytes,
                              void *hip_stream);
 
+/* Group norm over channels-last activations followed by an activation function:
+ *   per sample and group: mean and var over the points and the group's channels / groups neighbouring channels, rstd = 1 / sqrt(var + eps);
+ *   xhat = (x - mean) rstd,   y = act(gamma xhat + beta).
+ *   x, y         [batch][points][channels], one type; y may be x
+ *   gamma, beta  device [channels] or NULL (1, 0)
+ *   mean, rstd   device [batch, groups], written where not NULL (the gradients need them)
+ * DOL_ACT_GELU is z Phi(z) with the normal distribution's own Phi, DOL_ACT_SILU z / (1 + exp(-z)); the slope of DOL_ACT_RELU at 0 is 0. */
+typedef enum { DOL_ACT_NONE = 0, DOL_ACT_RELU = 1, DOL_ACT_SILU = 2, DOL_ACT_GELU = 3 } dol_act;
+typedef struct {
+    int32_t dtype;               /* dol_dtype */
+    int32_t batch, points, channels;
+    int64_t ld_batch, ld_point;  /* elements between consecutive samples, points; channels are neighbours */
+    void *data;                  /* device */
+} dol_activations;
+dol_status dol_group_norm_workspace(const dol_activations *x, int32_t groups, int32_t backward, int64_t *bytes);
+dol_status dol_group_norm(const dol_activations *x, int32_t groups, const float *gamma, const float *beta, float eps, int32_t act,
+                          const dol_activations *y, float *mean, float *rstd, void *workspace, int64_t workspace_bytes, void *hip_stream);
+/* Its gradients, dz = grad_y act'(gamma xhat + beta):
+ *   grad_x = rstd (gamma dz - c1 - xhat c2),   c1, c2 the means over sample and group of gamma dz and of gamma dz xhat;
+ *   grad_gamma[c] = sum dz xhat,   grad_beta[c] = sum dz   over samples and points.
+ * x, gamma, beta, act, mean, rstd as in (and from) the forward call.  Each is OVERWRITTEN and may be NULL; grad_x may be grad_y or x.
+ * Sums are taken in a fixed order: two runs give the same bits. */
+dol_status dol_group_norm_backward(const dol_activations *x, int32_t groups, const float *gamma, const float *beta, int32_t act,
+                                   const float *mean, const float *rstd, const dol_activations *grad_y, const dol_activations *grad_x,
+                                   float *grad_gamma, float *grad_beta, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
 /* Message of the calling thread's most recent failing call ("" if none). */
 const char *dol_last_error(void);
 /* Library version, e.g. "0.1.0". */

@@ -773,3 +773,78 @@ def newton_schulz(g: torch.Tensor, out: torch.Tensor, steps: int = 5, coefficien
         _check(_lib.dol_newton_schulz_workspace(mg, batch, need))
     ws, n, _keep = _workspace(workspace, need.value, g.device, stream)
     _check(_lib.dol_newton_schulz(mg, g_stride, mo, out_stride, batch, steps, (C.c_float * 3)(*coefficients), eps, ws, n, _stream(stream)))
+
+
+class _Activations(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("points", C.c_int32), ("channels", C.c_int32), ("ld_batch", C.c_int64),
+                ("ld_point", C.c_int64), ("data", C.c_void_p)]
+
+
+_acts_p = C.POINTER(_Activations)
+_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+_lib.dol_group_norm_workspace.argtypes = [_acts_p, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
+_lib.dol_group_norm.argtypes = [_acts_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_int32, _acts_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                C.c_int64, C.c_void_p]
+_lib.dol_group_norm_backward.argtypes = [_acts_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, _acts_p, _acts_p,
+                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+
+
+def _activations(t: torch.Tensor) -> _Activations:
+    """A tensor [batch, points.., channels], neighbouring channels next to each other and points at one distance."""
+    assert t.is_cuda and t.dtype in _DTYPES and t.dim() >= 3
+    shape, stride = t.shape, t.stride()
+    channels, points = shape[-1], 1
+    assert channels <= 1 or stride[-1] == 1
+    ld = channels
+    for k in range(t.dim() - 2, 0, -1):             # from the innermost: each has to continue the one before
+        if shape[k] > 1:
+            assert points == 1 or stride[k] == ld * points
+            ld = stride[k] if points == 1 else ld
+        points *= shape[k]
+    assert points <= 1 or ld >= channels
+    return _Activations(_DTYPES[t.dtype], shape[0], points, channels, stride[0], max(ld, channels), t.data_ptr())
+
+
+def _statistics(t: Optional[torch.Tensor], batch: int, groups: int):
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.float32 and t.shape == (batch, groups) and t.is_contiguous()
+    return t.data_ptr()
+
+
+def group_norm_workspace(x: torch.Tensor, groups: int, backward: bool = False) -> int:
+    n = C.c_int64()
+    _check(_lib.dol_group_norm_workspace(_activations(x), groups, int(backward), n))
+    return n.value
+
+
+def group_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int, y: torch.Tensor,
+               mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor], eps: float = 1e-5, act: str = "none",
+               workspace: Optional[torch.Tensor] = None, stream=None):
+    """y = act(gamma * (x - mean) * rstd + beta), mean and variance over the points of a sample and the channels of a group.
+
+    x, y: [batch, points.., channels] (float32 or bfloat16; y may be x); gamma, beta: float32 [channels]; mean, rstd: float32
+    [batch, groups], written; act: "none", "relu", "silu" or "gelu"."""
+    mx = _activations(x)
+    need = C.c_int64()
+    if workspace is None:
+        _check(_lib.dol_group_norm_workspace(mx, groups, 0, need))
+    ws, n, _keep = _workspace(workspace, need.value, x.device, stream)
+    _check(_lib.dol_group_norm(mx, groups, _vector(gamma, mx.channels), _vector(beta, mx.channels), eps, _ACTS[act], _activations(y),
+                               _statistics(mean, mx.batch, groups), _statistics(rstd, mx.batch, groups), ws, n, _stream(stream)))
+
+
+def group_norm_backward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int, mean: torch.Tensor,
+                        rstd: torch.Tensor, grad_y: torch.Tensor, grad_x: Optional[torch.Tensor], grad_gamma: Optional[torch.Tensor],
+                        grad_beta: Optional[torch.Tensor], act: str = "none", workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of sum(grad_y * y); mean and rstd as group_norm left them.  Gradients that are None are not computed; grad_x may be
+    grad_y or x."""
+    mx = _activations(x)
+    need = C.c_int64()
+    if workspace is None:
+        _check(_lib.dol_group_norm_workspace(mx, groups, 1, need))
+    ws, n, _keep = _workspace(workspace, need.value, x.device, stream)
+    _check(_lib.dol_group_norm_backward(mx, groups, _vector(gamma, mx.channels), _vector(beta, mx.channels), _ACTS[act],
+                                        _statistics(mean, mx.batch, groups), _statistics(rstd, mx.batch, groups), _activations(grad_y),
+                                        None if grad_x is None else _activations(grad_x), _vector(grad_gamma, mx.channels),
+                                        _vector(grad_beta, mx.channels), ws, n, _stream(stream)))

@@ -35,6 +35,24 @@ dol_status check_workspace(const void *workspace, int64_t has, int64_t needs);
 // a (device, kernel) pair is seen (thread-safe) and is a table lookup afterwards.
 hipError_t allow_dynamic_lds(const void *kernel, size_t bytes);
 
+// ---------------------------------------------------------------- a caller's workspace
+
+inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Hands out parts of a caller's workspace, 256 bytes apart.  With no memory it only counts.
+struct Carver {
+    char *base;
+    int64_t used = 0;
+    explicit Carver(void *p) : base(static_cast<char *>(p)) {}
+    template <typename T>
+    T *take(int64_t n)
+    {
+        T *p = base ? reinterpret_cast<T *>(base + used) : nullptr;
+        used += round_up(n * static_cast<int64_t>(sizeof(T)), 256);
+        return p;
+    }
+};
+
 // ---------------------------------------------------------------- device arrays owned by plans
 
 template <typename T>

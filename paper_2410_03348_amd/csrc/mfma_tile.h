@@ -234,20 +234,4 @@ __device__ __forceinline__ void tile_of(int w, int tm, int tn, int band, int &mt
     mt = first + r % height, nt = r / height;
 }
 
-inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-
-// Hands out parts of a caller's workspace, 256 bytes apart.  With no memory it only counts.
-struct Carver {
-    char *base;
-    int64_t used = 0;
-    explicit Carver(void *p) : base(static_cast<char *>(p)) {}
-    template <typename T>
-    T *take(int64_t n)
-    {
-        T *p = base ? reinterpret_cast<T *>(base + used) : nullptr;
-        used += round_up(n * static_cast<int64_t>(sizeof(T)), 256);
-        return p;
-    }
-};
-
 }  // namespace dol
