@@ -7,12 +7,13 @@
 //
 // Forward: a tile of logits stays in the registers that the matrix cores leave it in; of each row it gives the largest logit and the
 // sum of the exponentials below it, which a second kernel joins over the tiles.
-// Backward: the classes are taken in pieces.  A piece's logits are computed once more, dl is rounded for the matrix cores and written
-// both ways round (a few tens of MB that the next launch reads), and grad_x and grad_w are two sets of tiles of one launch.
-// Everything is a product of rows with contiguous k (mfma_tile.h), so x and w are also laid out transposed, once a call.
+// Backward: the classes are taken in pieces.  A piece's logits are computed once more, dl is rounded for the matrix cores and written (a
+// hundred MB or so that the next launch reads), and grad_x and grad_w are two sets of tiles of one launch, which read dl, x and w as they
+// lie, along rows or across them (mfma_tile.h).
 #include "mfma_tile.h"
 
-#include <cfloat>
+#include <type_traits>
+#include <utility>
 
 namespace dol {
 namespace {
@@ -20,20 +21,36 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kFar = 1e38f;       // logits further from 0 (a bias of the type's lowest value) have no finite l log2e
 constexpr int kPad = 256;                               // rows and classes of a piece are filled up to a multiple of this
-constexpr int64_t kPieceBytes = int64_t(256) << 20;     // of dl both ways round (see pieces_of)
+constexpr int64_t kPieceBytes = int64_t(128) << 20;     // of dl
 constexpr int kUnits = 256;                             // compute units of the chip
 
-template <int P>
+// Tiles of logits, and of the two products that dl goes into in Q planes.
+template <int P, int Q>
 struct Shapes;
 template <>
-struct Shapes<1> {      // bf16
-    using Big = MfmaTile<bf16x8, 1, 256, 256, 64, 2, 4, 2>;
-    using Small = MfmaTile<bf16x8, 1, 128, 128, 64, 2, 2, 2>;
+struct Shapes<1, 1> {       // bf16
+    using Big = MfmaTile<bf16x8, 1, 1, kRows, kRows, 256, 256, 64, 2, 4, 2>;
+    using Small = MfmaTile<bf16x8, 1, 1, kRows, kRows, 128, 128, 64, 2, 2, 2>;
+    using BigX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 256, 256, 64, 2, 4, 2>;
+    using BigW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 256, 256, 64, 2, 4, 2>;
+    using SmallX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 128, 128, 64, 2, 2, 2>;
+    using SmallW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 128, 128, 64, 2, 2, 2>;
 };
 template <>
-struct Shapes<3> {      // float
-    using Big = MfmaTile<bf16x8, 3, 128, 256, 32, 2, 4, 2>;
-    using Small = MfmaTile<bf16x8, 3, 128, 128, 32, 2, 2, 2>;
+struct Shapes<1, 2> : Shapes<1, 1> {
+    using BigX = MfmaTile<bf16x8, 1, 2, kCols, kRows, 128, 128, 32, 2, 2, 2>;
+    using BigW = MfmaTile<bf16x8, 1, 2, kCols, kCols, 128, 128, 32, 2, 2, 2>;
+    using SmallX = BigX;
+    using SmallW = BigW;
+};
+template <>
+struct Shapes<3, 3> {       // float
+    using Big = MfmaTile<bf16x8, 3, 3, kRows, kRows, 128, 256, 32, 2, 4, 2>;
+    using Small = MfmaTile<bf16x8, 3, 3, kRows, kRows, 128, 128, 32, 2, 2, 2>;
+    using BigX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 128, 256, 32, 2, 4, 2>;
+    using BigW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 128, 256, 32, 2, 4, 2>;
+    using SmallX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 128, 128, 32, 2, 2, 2>;
+    using SmallW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 128, 128, 32, 2, 2, 2>;
 };
 
 template <int P>
@@ -45,17 +62,30 @@ __device__ __forceinline__ bool kept_row(int32_t target, int32_t classes) { retu
 
 // ---------------------------------------------------------------- layouts for the matrix cores
 
-// out[p][r][0..kp) = planes of src[r][0..cols), zeros behind; eight elements to a thread.
+// out[p][r][0..kp) = planes of src[r][0..cols), zeros behind and in rows past the source's; eight elements to a thread.  Rows whose target (if
+// given) names no class count as zeros, whatever they hold.
 template <typename S, int P>
-__global__ void __launch_bounds__(256) xent_pack_rows_kernel(const S *src, int64_t ld, int64_t rows, int32_t cols, uint16_t *out, int64_t kp)
+__global__ void __launch_bounds__(256) xent_pack_rows_kernel(const S *src, int64_t ld, int64_t rows, int32_t cols, const int32_t *target, int32_t classes,
+                                                             uint16_t *out, int64_t out_rows, int64_t kp, bool vec)
 {
     const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, per = kp / 8;
-    if (t >= rows * per) return;
+    if (t >= out_rows * per) return;
     const int64_t r = t / per;
     const int c = static_cast<int>(t - r * per) * 8;
+    const bool in = r < rows && (!target || kept_row(target[r], classes));
+    const S *from = src + r * ld + c;
     float v[8];
+    if (in && vec && c + 8 <= cols) {
+        struct alignas(16) Piece { S e[16 / sizeof(S)]; };
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? static_cast<float>(src[r * ld + c + k]) : 0.0f;
+        for (int h = 0; h < static_cast<int>(8 * sizeof(S) / 16); ++h) {
+            const Piece q = reinterpret_cast<const Piece *>(from)[h];
+#pragma unroll
+            for (int k = 0; k < static_cast<int>(16 / sizeof(S)); ++k) v[h * (16 / sizeof(S)) + k] = static_cast<float>(q.e[k]);
+        }
+    } else
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = in && c + k < cols ? static_cast<float>(from[k]) : 0.0f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         u32x4 w;
@@ -64,42 +94,7 @@ __global__ void __launch_bounds__(256) xent_pack_rows_kernel(const S *src, int64
             const uint32_t lo = take_plane<__bf16>(v[2 * k]), hi = take_plane<__bf16>(v[2 * k + 1]);
             w[k] = lo | hi << 16;
         }
-        *reinterpret_cast<u32x4 *>(out + (p * rows + r) * kp + c) = w;
-    }
-}
-
-// out[p][c][0..rp) = planes of src[0..rows)[c], zeros behind; a tile of 64 x 64 to a workgroup.  Rows whose target (if given) names no
-// class count as zeros, whatever they hold.
-template <typename S, int P>
-__global__ void __launch_bounds__(256) xent_pack_cols_kernel(const S *src, int64_t ld, int64_t rows, int32_t cols, const int32_t *target, int32_t classes,
-                                                             uint16_t *out, int64_t rp)
-{
-    __shared__ float tile[64][65];
-    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 64;
-    const int32_t c0 = static_cast<int32_t>(blockIdx.y) * 64;
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-#pragma unroll 4
-    for (int k = y; k < 64; k += 4) {
-        const int64_t r = r0 + k;
-        const bool in = r < rows && c0 + x < cols && (!target || kept_row(target[r], classes));
-        tile[k][x] = in ? static_cast<float>(src[r * ld + c0 + x]) : 0.0f;
-    }
-    __syncthreads();
-    const int q = threadIdx.x & 7;
-    for (int c = threadIdx.x >> 3; c < 64 && c0 + c < cols; c += 32) {
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = tile[q * 8 + k][c];
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            u32x4 w;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t lo = take_plane<__bf16>(v[2 * k]), hi = take_plane<__bf16>(v[2 * k + 1]);
-                w[k] = lo | hi << 16;
-            }
-            *reinterpret_cast<u32x4 *>(out + (static_cast<int64_t>(p) * cols + c0 + c) * rp + r0 + q * 8) = w;
-        }
+        *reinterpret_cast<u32x4 *>(out + (p * out_rows + r) * kp + c) = w;
     }
 }
 
@@ -172,11 +167,12 @@ __global__ void __launch_bounds__(T::NT, 2) xent_sums_kernel(Planes w, Planes x,
     }
 }
 
-// Joins the parts of a sample: sixty-four samples to a workgroup, a quarter of the parts to each of its wavefronts.
-__global__ void __launch_bounds__(256) xent_join_kernel(const float2 *part, int parts, int64_t n_pad, int32_t rows, int32_t classes, const int32_t *target,
-                                                        const float *at, float *loss, float *lse)
+// Joins the parts of a sample: sixty-four samples to a workgroup, a share of the parts to each of its wavefronts.
+constexpr int kJoinWaves = 16;
+__global__ void __launch_bounds__(kJoinWaves * 64) xent_join_kernel(const float2 *part, int parts, int64_t n_pad, int32_t rows, int32_t classes, const int32_t *target,
+                                                                    const float *at, float *loss, float *lse)
 {
-    __shared__ float2 red[4][64];
+    __shared__ float2 red[kJoinWaves][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int64_t n = static_cast<int64_t>(blockIdx.x) * 64 + lane;
     float top = -INFINITY, s = 0.0f;
@@ -187,11 +183,12 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2 *part, int 
         top = to;
     };
     if (n < rows)
-        for (int k = w; k < parts; k += 4) join(part[k * n_pad + n]);
+#pragma unroll 4
+        for (int k = w; k < parts; k += kJoinWaves) join(part[k * n_pad + n]);
     red[w][lane] = make_float2(top, s);
     __syncthreads();
     if (w != 0 || n >= rows) return;
-    for (int k = 1; k < 4; ++k) join(red[k][lane]);
+    for (int k = 1; k < min(parts, kJoinWaves); ++k) join(red[k][lane]);
     const float lg = kLn2 * log2f(s);
     lse[n] = s == 0.0f ? -INFINITY : top + lg;
     // (a row without any class left has lse = -inf and, by this rule, loss = +inf)
@@ -200,115 +197,100 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2 *part, int 
 
 // ---------------------------------------------------------------- backward
 
-// dl of one piece of classes, rounded to P planes: dl[p][sample][class of the piece] and dlt[p][class of the piece][sample], both filled up
-// with zeros to kPad.  bias_part[(nt * WN + wavefront column) * piece + class] = sums of the unrounded dl (if asked for).
-template <typename T>
-__global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes w, Planes x, int32_t classes, int32_t rows, int steps, int32_t first, int32_t piece,
+// dl of one piece of classes in Q planes: dl[q][sample][class of the piece], zeros in the samples and classes that there are not.  Rows of a
+// tile are samples, columns classes.  bias_part[(mt * WM + wavefront row) * piece + class] = sums of the unrounded dl (if asked for).
+template <typename T, int Q>
+__global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes w, int32_t rows, int32_t classes, int steps, int32_t first, int32_t piece,
                                                                 const float *bias, const int32_t *target, const float *lse, const float *grad_loss,
-                                                                uint16_t *dl, uint16_t *dlt, int64_t n_pad, float *bias_part)
+                                                                uint16_t *dl, int64_t n_pad, float *bias_part)
 {
     extern __shared__ __align__(128) char smem[];
-    const int tm = piece / T::BM, tn = static_cast<int>(n_pad / T::BN);
+    const int tm = static_cast<int>(n_pad / T::BM), tn = piece / T::BN;
     int mt, nt;
-    tile_of(xcd_contiguous(blockIdx.x, gridDim.x), tm, tn, 4, mt, nt);
+    tile_of(xcd_contiguous(blockIdx.x, gridDim.x), tm, tn, 8, mt, nt);
     f32x4 acc[T::MI][T::NI];
-    const int m0 = first + mt * T::BM;
-    // (a tile that lies wholly past the last class or sample repeats the last row; all of it is masked below)
-    T::run(w, min(m0, classes - 1), classes, x, min(nt * T::BN, rows - 1), rows, 0, steps, smem, acc);
-    const int n0 = nt * T::BN + T::col_of();
-    float off[T::NI], scale[T::NI], own[T::NI];
-    bool kept[T::NI];
-    int at[T::NI];
-    bool hit = false, far = false;
-#pragma unroll
-    for (int j = 0; j < T::NI; ++j) {
-        const int n = n0 + j;
-        const int32_t t = n < rows ? target[n] : -1;
-        const float z = n < rows ? lse[n] : 0.0f;
-        kept[j] = kept_row(t, classes) && z != -INFINITY;
-        const float g = kept[j] ? grad_loss[n] : 0.0f;
-        off[j] = kept[j] ? z : 0.0f;
-        scale[j] = g;
-        far |= !(__builtin_fabsf(off[j]) <= kFar);
-        // the target's own exp(l - lse) - 1 is small where the network is right: not taken as a difference
-        at[j] = kept[j] ? t - m0 - T::row_of(0) : -1;
-        own[j] = 0.0f;
-        if (at[j] >= 0 && at[j] < T::TM && (at[j] & 15) < 4) {
-            hit = true;
-            float l = 0.0f;
-#pragma unroll
-            for (int i = 0; i < T::MI; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) l = at[j] == i * 16 + e ? acc[i][j][e] : l;
-            own[j] = g * expm1f((bias ? l + bias[t] : l) - z);
+    const int m0 = mt * T::BM, n0 = first + nt * T::BN;
+    // (a tile that lies wholly past the last sample or class repeats the last row; it comes out as zeros all the same)
+    T::run(x, min(m0, rows - 1), rows, w, min(n0, classes - 1), classes, 0, steps, smem, acc);
+    // What a row of the tile needs.  exp(l - lse) = 2^(l log2e - off) 2^(-rest): what lse log2e loses to rounding goes into the row's factor.
+    // A row that does not count has off = inf and factor 0.
+    struct Row {
+        float off, factor;
+        int32_t target, far;
+    };
+    Row *info = reinterpret_cast<Row *>(smem);
+    lds_barrier();
+    for (int r = threadIdx.x; r < T::BM; r += T::NT) {
+        const int m = m0 + r;
+        Row q{INFINITY, 0.0f, -1, 0};
+        if (m < rows) {
+            const int32_t t = target[m];
+            const float z = lse[m];
+            if (kept_row(t, classes) && z != -INFINITY) {
+                const float g = grad_loss[m];
+                q.far = !(__builtin_fabsf(z) <= kFar);
+                q.off = z * kLog2e;
+                q.factor = g * __builtin_amdgcn_exp2f(-__builtin_fmaf(z, kLog2e, -q.off));
+                q.target = t;
+            }
         }
+        info[r] = q;
     }
-    auto fill = [&](auto exponential) {
+    lds_barrier();
+    const int n = n0 + T::col_of();
+    float b[T::NI], sum[T::NI];
 #pragma unroll
-        for (int i = 0; i < T::MI; ++i)
+    for (int j = 0; j < T::NI; ++j) b[j] = n + j >= classes ? -INFINITY : bias ? bias[n + j] : 0.0f, sum[j] = 0.0f;
+    uint16_t *to = dl + static_cast<int64_t>(m0) * piece + nt * T::BN + T::col_of();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int m = m0 + T::row_of(i) + e;
-                const bool in = m < classes;
-                const float b = bias && in ? bias[m] : 0.0f;
+    for (int i = 0; i < T::MI; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = T::row_of(i) + e;
+            const Row q = info[r];
+            float l[T::NI], v[T::NI];
+#pragma unroll
+            for (int j = 0; j < T::NI; ++j) {
+                l[j] = acc[i][j][e] + b[j];
+                v[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(l[j], kLog2e, -q.off)) * q.factor;
+            }
+            if (static_cast<uint32_t>(q.target - n) < T::NI || q.far) {
+                const float z = lse[m0 + r], g = grad_loss[m0 + r];
 #pragma unroll
                 for (int j = 0; j < T::NI; ++j) {
-                    const float p = exponential(acc[i][j][e] + b, j);
-                    acc[i][j][e] = in && kept[j] ? p : 0.0f;
+                    if (q.far) v[j] = __builtin_amdgcn_exp2f((l[j] - z) * kLog2e) * g;
+                    // the target's own exp(l - lse) - 1 is small where the network is right: not taken as a difference
+                    if (q.target == n + j) v[j] = g * expm1f(l[j] - z);
                 }
             }
-    };
-    if (!__any(far)) {
 #pragma unroll
-        for (int j = 0; j < T::NI; ++j) {
-            // exp(l - lse) = 2^(l log2e - off) 2^(-rest): what lse log2e loses to rounding goes into the factor of the row
-            const float z = off[j];
-            off[j] = z * kLog2e;
-            scale[j] *= __builtin_amdgcn_exp2f(-__builtin_fmaf(z, kLog2e, -off[j]));
-        }
-        fill([&](float l, int j) { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, kLog2e, -off[j])) * scale[j]; });
-    } else
-        fill([&](float l, int j) { return __builtin_amdgcn_exp2f((l - off[j]) * kLog2e) * scale[j]; });
-    if (hit)
+            for (int j = 0; j < T::NI; ++j) sum[j] += v[j];
 #pragma unroll
-        for (int j = 0; j < T::NI; ++j)
-#pragma unroll
-            for (int i = 0; i < T::MI; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = at[j] == i * 16 + e ? own[j] : acc[i][j][e];
-    if (bias_part) {
-        float *to = bias_part + static_cast<int64_t>(nt * T::WN + (threadIdx.x >> 6) % T::WN) * piece + mt * T::BM;
-#pragma unroll
-        for (int i = 0; i < T::MI; ++i) {
-            f32x4 s;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] = reduce16<AddOp>((acc[i][0][e] + acc[i][1][e]) + (acc[i][2][e] + acc[i][3][e]));
-            if ((threadIdx.x & 15) == 0) *reinterpret_cast<f32x4 *>(to + T::row_of(i)) = s;
-        }
-    }
-#pragma unroll 1
-    for (int p = 0; p < T::P; ++p) {
-        uint16_t *to = dlt + (static_cast<int64_t>(p) * piece + mt * T::BM) * n_pad + n0;
-#pragma unroll
-        for (int i = 0; i < T::MI; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                u32x2 v;
-                v[0] = bits16<__bf16>(acc[i][0][e]) | bits16<__bf16>(acc[i][1][e]) << 16;
-                v[1] = bits16<__bf16>(acc[i][2][e]) | bits16<__bf16>(acc[i][3][e]) << 16;
-                *reinterpret_cast<u32x2 *>(to + (T::row_of(i) + e) * n_pad) = v;
+            for (int p = 0; p < Q; ++p) {
+                u32x2 out;
+                const uint32_t w0 = take_plane<__bf16>(v[0]), w1 = take_plane<__bf16>(v[1]), w2 = take_plane<__bf16>(v[2]), w3 = take_plane<__bf16>(v[3]);
+                out[0] = w0 | w1 << 16, out[1] = w2 | w3 << 16;
+                *reinterpret_cast<u32x2 *>(to + (p * n_pad + r) * piece) = out;
             }
-        T::store_transposed(smem, dl + (p * n_pad + static_cast<int64_t>(nt) * T::BN) * piece + mt * T::BM, piece, T::BN,
-                            [&](int i, int j, int e) { float v = acc[i][j][e]; const uint32_t b = take_plane<__bf16>(v); acc[i][j][e] = v; return b; });
+        }
+    if (bias_part) {
+        f32x4 s;
+#pragma unroll
+        for (int j = 0; j < T::NI; ++j) s[j] = with_lane32<AddOp>(with_lane16<AddOp>(sum[j]));
+        if ((threadIdx.x & 63) < 16)
+            *reinterpret_cast<f32x4 *>(bias_part + static_cast<int64_t>(mt * T::WM + (threadIdx.x >> 6) / T::WN) * piece + nt * T::BN + T::col_of()) = s;
     }
 }
 
-// One set of tiles of the launch that follows: out = a b^T over `steps` steps, in `splits` shares of the steps.
+// One set of tiles of the launch that follows: out[n][m] = sum_k a[k][m] b(n, k), k in `splits` shares.  Rows of a tile are elements of x or w,
+// which lie side by side in `out` too.
 struct Product {
     Planes a, b;
-    int32_t M, N;               // rows of out, columns of out
+    int32_t M, N;               // columns of out, rows of out
+    int32_t wide, tall;         // what a and b have of them in memory
     int32_t tm, tn, splits, steps;
-    float *part;                // [splits][M][part_ld], or null: out is written
+    int64_t k, have;            // that count, and that there are of operands which lie across k
+    float *part;                // [splits][N][part_ld], or null: out is written
     int64_t part_ld;
     bool add;                   // to what part holds
     void *out;
@@ -316,40 +298,48 @@ struct Product {
 };
 
 template <typename T, typename O>
-__global__ void __launch_bounds__(T::NT, 2) xent_products_kernel(Product p0, Product p1)
+__device__ __forceinline__ void product_tile(const Product &p, int id, char *smem)
 {
-    extern __shared__ __align__(128) char smem[];
-    int id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int first = p0.tm * p0.tn * p0.splits;
-    const Product &p = id < first ? p0 : p1;
-    if (id >= first) id -= first;
     const int tiles = p.tm * p.tn, split = id / tiles;
     int mt, nt;
-    tile_of(id - split * tiles, p.tm, p.tn, 8, mt, nt);
+    tile_of(id - split * tiles, p.tm, p.tn, 4, mt, nt);
     const int s0 = static_cast<int>(static_cast<int64_t>(p.steps) * split / p.splits), s1 = static_cast<int>(static_cast<int64_t>(p.steps) * (split + 1) / p.splits);
+    const int64_t k0 = static_cast<int64_t>(s0) * T::BK;
     f32x4 acc[T::MI][T::NI];
-    T::run(p.a, static_cast<int64_t>(mt) * T::BM, p.M, p.b, static_cast<int64_t>(nt) * T::BN, p.N, static_cast<int64_t>(s0) * T::BK, s1 - s0, smem, acc);
-    const int n = nt * T::BN + T::col_of(), left = p.N - n;
+    T::run(p.a, static_cast<int64_t>(mt) * T::BM, p.wide, p.b, static_cast<int64_t>(nt) * T::BN, p.tall, k0, s1 - s0, smem, acc, p.have - k0);
     const bool vec = p.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (4 * sizeof(O) - 1)) == 0;
 #pragma unroll
-    for (int i = 0; i < T::MI; ++i)
+    for (int j = 0; j < T::NI; ++j) {
+        const int n = nt * T::BN + T::col_of(j);
+        if (n >= p.N) continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int m = mt * T::BM + T::row_of(i) + e;
-            if (m >= p.M || left <= 0) continue;
-            f32x4 v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+        for (int i = 0; i < T::MI; ++i) {
+            const int m = mt * T::BM + T::row_of(i);
+            if (m >= p.M) continue;
             if (p.part) {       // (its rows are filled up to whole fours)
-                f32x4 *to = reinterpret_cast<f32x4 *>(p.part + (static_cast<int64_t>(split) * p.M + m) * p.part_ld + n);
-                *to = p.add ? *to + v : v;
+                f32x4 *to = reinterpret_cast<f32x4 *>(p.part + (static_cast<int64_t>(split) * p.N + n) * p.part_ld + m);
+                *to = p.add ? *to + acc[i][j] : acc[i][j];
             } else
-                store4(static_cast<O *>(p.out) + m * p.out_ld + n, v, left, vec);
+                store4(static_cast<O *>(p.out) + n * p.out_ld + m, acc[i][j], p.M - m, vec);
         }
+    }
+}
+
+// grad_x's tiles (TX: dl along its rows) and grad_w's (TW: dl across them).
+template <typename TX, typename TW, typename O>
+__global__ void __launch_bounds__(TX::NT, 2) xent_products_kernel(Product px, Product pw)
+{
+    static_assert(TX::LDS == TW::LDS && TX::NT == TW::NT, "one launch");
+    extern __shared__ __align__(128) char smem[];
+    const int id = xcd_contiguous(blockIdx.x, gridDim.x), first = px.tm * px.tn * px.splits;
+    if (id < first) product_tile<TX, O>(px, id, smem);
+    else product_tile<TW, O>(pw, id - first, smem);
 }
 
 // out = the sum of the parts in their order, for one set or two; four columns to a thread.
 struct Sum {
     const float *part;
-    int32_t M, N, splits;
+    int32_t M, N, splits;       // rows, columns
     int64_t part_ld;
     void *out;
     int64_t out_ld;
@@ -368,12 +358,19 @@ __global__ void __launch_bounds__(256) xent_sum_parts_kernel(Sum s)
     store4(static_cast<O *>(s.out) + m * s.out_ld + n, v, s.N - n, vec);
 }
 
-__global__ void __launch_bounds__(256) xent_bias_kernel(const float *part, int parts, int32_t piece, int32_t n, float *out)
+// Sixty-four classes to a workgroup, a share of the parts to each of its wavefronts.
+__global__ void __launch_bounds__(kJoinWaves * 64) xent_bias_kernel(const float *part, int parts, int32_t piece, int32_t n, float *out)
 {
-    const int v = blockIdx.x * 256 + threadIdx.x;
-    if (v >= n) return;
+    __shared__ float red[kJoinWaves][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, v = blockIdx.x * 64 + lane;
     float s = 0.0f;
-    for (int k = 0; k < parts; ++k) s += part[static_cast<int64_t>(k) * piece + v];
+    if (v < n)
+#pragma unroll 4
+        for (int k = w; k < parts; k += kJoinWaves) s += part[static_cast<int64_t>(k) * piece + v];
+    red[w][lane] = s;
+    __syncthreads();
+    if (w != 0 || v >= n) return;
+    for (int k = 1; k < kJoinWaves; ++k) s += red[k][lane];
     out[v] = s;
 }
 
@@ -396,10 +393,10 @@ bool direct(const dol_matrix *m)            // can be read by the tiles as it is
 
 struct Layout {
     int32_t rows, width, classes;
-    int64_t kp, n_pad, v_pad;               // width, rows and classes as they are laid out
+    int64_t kp, n_pad;                      // width and rows as they are laid out
     int32_t piece, pieces;
     bool big;                               // tiles of logits
-    uint16_t *xp, *wp, *xt, *wt, *dl, *dlt;
+    uint16_t *xp, *wp, *dl;
     float2 *part;
     float *at, *bias_part, *part_x, *part_w;
     bool big_products;
@@ -410,64 +407,74 @@ struct Layout {
 
 int32_t tiles(int64_t n, int t) { return static_cast<int32_t>((n + t - 1) / t); }
 
-template <int P>
+template <int P, int Q>
 Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *workspace)
 {
-    using Big = typename Shapes<P>::Big;
-    using Small = typename Shapes<P>::Small;
+    using S = Shapes<P, Q>;
     Layout L{};
     L.rows = x->rows, L.width = x->cols, L.classes = w->rows;
     L.kp = round_up(L.width, 64), L.n_pad = round_up(L.rows, kPad);
     // Tiles of 256 x 256 (float 128 x 256) do more with what they load; smaller ones fill the chip sooner.
-    L.big = int64_t(tiles(L.classes, Big::BM)) * tiles(L.rows, Big::BN) >= kUnits * 3 / 4;
+    L.big = int64_t(tiles(L.classes, S::Big::BM)) * tiles(L.rows, S::Big::BN) >= kUnits * 3 / 4;
     Carver c(workspace);
-    if (!direct(x)) L.xp = c.take<uint16_t>(P * int64_t(L.rows) * L.kp);
+    if (backward || !direct(x)) L.xp = c.take<uint16_t>(P * (backward ? L.n_pad : L.rows) * L.kp);
     if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(L.classes) * L.kp);
     if (!backward) {
-        const int parts = L.big ? tiles(L.classes, Big::BM) * Big::WM : tiles(L.classes, Small::BM) * Small::WM;
+        const int parts = L.big ? tiles(L.classes, S::Big::BM) * S::Big::WM : tiles(L.classes, S::Small::BM) * S::Small::WM;
         L.part = c.take<float2>(int64_t(parts) * L.n_pad);
         L.at = c.take<float>(L.rows);
         L.bytes = c.used;
         return L;
     }
-    const int64_t most = std::max<int64_t>(kPad, kPieceBytes / (4 * P * L.n_pad) / kPad * kPad);
+    const int64_t most = std::max<int64_t>(kPad, kPieceBytes / (2 * Q * L.n_pad) / kPad * kPad);
     L.pieces = static_cast<int32_t>((L.classes + most - 1) / most);
     L.piece = static_cast<int32_t>(round_up((L.classes + L.pieces - 1) / L.pieces, kPad));
     L.pieces = tiles(L.classes, L.piece);
-    L.v_pad = int64_t(L.pieces) * L.piece;
-    L.xt = c.take<uint16_t>(P * int64_t(L.width) * L.n_pad);
-    L.wt = c.take<uint16_t>(P * int64_t(L.width) * L.v_pad);
-    L.dl = c.take<uint16_t>(P * L.n_pad * L.piece);
-    L.dlt = c.take<uint16_t>(P * L.n_pad * L.piece);
+    L.dl = c.take<uint16_t>(Q * L.n_pad * L.piece);
     L.bias_part = c.take<float>(L.n_pad / 64 * L.piece);
     // Both products of a piece share a launch: their k is split so that the launch has a workgroup of equal length for every place there
     // is, of at least 256 elements of k.
-    const int64_t kx = L.piece, kw = L.n_pad;
-    auto total = [&](int bm, int bn) { return (int64_t(tiles(L.rows, bm)) * kx + int64_t(tiles(std::min(L.piece, L.classes), bm)) * kw) * tiles(L.width, bn); };
-    L.big_products = total(Big::BM, Big::BN) / kUnits >= 1024;
-    const int64_t share = std::max<int64_t>(256, L.big_products ? total(Big::BM, Big::BN) / kUnits : total(Small::BM, Small::BN) / (2 * kUnits));
-    L.splits_x = static_cast<int32_t>(std::max<int64_t>(1, (kx + share / 2) / share));
-    L.splits_w = static_cast<int32_t>(std::max<int64_t>(1, (kw + share / 2) / share));
+    const int32_t n = std::min(L.piece, L.classes);
+    auto total = [&](int bm, int bn) { return (int64_t(tiles(L.rows, bn)) * n + int64_t(tiles(n, bn)) * L.rows) * tiles(L.width, bm); };
+    L.big_products = total(S::BigX::BM, S::BigX::BN) / kUnits >= 1024;
+    const int64_t share = std::max<int64_t>(256, L.big_products ? total(S::BigX::BM, S::BigX::BN) / kUnits : total(S::SmallX::BM, S::SmallX::BN) / (2 * kUnits));
+    L.splits_x = static_cast<int32_t>(std::max<int64_t>(1, (n + share / 2) / share));
+    L.splits_w = static_cast<int32_t>(std::max<int64_t>(1, (L.rows + share / 2) / share));
     L.part_ld = round_up(L.width, 4);
     if (L.splits_x > 1 || L.pieces > 1) L.part_x = c.take<float>(int64_t(L.splits_x) * L.rows * L.part_ld);
-    if (L.splits_w > 1) L.part_w = c.take<float>(int64_t(L.splits_w) * std::min(L.piece, L.classes) * L.part_ld);
+    if (L.splits_w > 1) L.part_w = c.take<float>(int64_t(L.splits_w) * n * L.part_ld);
     L.bytes = c.used;
     return L;
 }
 
+// dl in bf16 is off by 2^-9 or so in every term of a gradient.  Sums over many rows average that out; with few rows, where the products
+// cost little, a second plane takes it away.
+constexpr int32_t kFewRows = 512;
+
+template <typename F>
+auto with_planes(const dol_matrix *x, F f)
+{
+    if (x->dtype == DOL_F32) return f(std::integral_constant<int, 3>(), std::integral_constant<int, 3>());
+    if (x->rows <= kFewRows) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
+    return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+}
+
 unsigned blocks(int64_t n) { return static_cast<unsigned>((n + 255) / 256); }
 
+// Rows with contiguous k as the tiles read them: the matrix itself, or `out`, its planes in rows of kp elements (out_rows of them).
 template <int P>
-dol_status pack(const dol_matrix *m, uint16_t *out, int64_t kp, Planes *p, hipStream_t st)
+dol_status pack(const dol_matrix *m, const int32_t *target, int32_t classes, uint16_t *out, int64_t out_rows, int64_t kp, Planes *p, hipStream_t st)
 {
     using S = typename Source<P>::T;
     if (!out) {
         *p = Planes{static_cast<const uint16_t *>(m->data), m->ld, 0};
         return DOL_OK;
     }
-    xent_pack_rows_kernel<S, P><<<blocks(m->rows * (kp / 8)), 256, 0, st>>>(static_cast<const S *>(m->data), m->ld, m->rows, m->cols, out, kp);
+    const bool vec = !(reinterpret_cast<uintptr_t>(m->data) & 15) && m->ld % (16 / int64_t(sizeof(S))) == 0;
+    xent_pack_rows_kernel<S, P><<<blocks(out_rows * (kp / 8)), 256, 0, st>>>(static_cast<const S *>(m->data), m->ld, m->rows, m->cols, target, classes, out, out_rows, kp,
+                                                                            vec);
     DOL_HIP(hipGetLastError());
-    *p = Planes{out, kp, m->rows * kp};
+    *p = Planes{out, kp, out_rows * kp};
     return DOL_OK;
 }
 
@@ -478,47 +485,47 @@ dol_status launch_sums(const Layout &L, Planes w, Planes x, const float *bias, c
     const int tm = tiles(L.classes, T::BM), tn = tiles(L.rows, T::BN);
     xent_sums_kernel<T><<<tm * tn, T::NT, T::LDS, st>>>(w, x, L.classes, L.rows, static_cast<int>(L.kp / T::BK), bias, target, L.part, L.n_pad, L.at);
     DOL_HIP(hipGetLastError());
-    xent_join_kernel<<<tiles(L.rows, 64), 256, 0, st>>>(L.part, tm * T::WM, L.n_pad, L.rows, L.classes, target, L.at, loss, lse);
+    xent_join_kernel<<<tiles(L.rows, 64), kJoinWaves * 64, 0, st>>>(L.part, tm * T::WM, L.n_pad, L.rows, L.classes, target, L.at, loss, lse);
     DOL_HIP(hipGetLastError());
     return DOL_OK;
 }
 
-template <int P>
+template <int P, int Q>
 dol_status forward(const Layout &L, const dol_matrix *x, const dol_matrix *w, const float *bias, const int32_t *target, float *loss, float *lse, hipStream_t st)
 {
     Planes xp, wp;
-    if (dol_status s = pack<P>(x, L.xp, L.kp, &xp, st)) return s;
-    if (dol_status s = pack<P>(w, L.wp, L.kp, &wp, st)) return s;
-    return L.big ? launch_sums<typename Shapes<P>::Big>(L, wp, xp, bias, target, loss, lse, st)
-                 : launch_sums<typename Shapes<P>::Small>(L, wp, xp, bias, target, loss, lse, st);
+    if (dol_status s = pack<P>(x, nullptr, 0, L.xp, L.rows, L.kp, &xp, st)) return s;
+    if (dol_status s = pack<P>(w, nullptr, 0, L.wp, L.classes, L.kp, &wp, st)) return s;
+    return L.big ? launch_sums<typename Shapes<P, Q>::Big>(L, wp, xp, bias, target, loss, lse, st)
+                 : launch_sums<typename Shapes<P, Q>::Small>(L, wp, xp, bias, target, loss, lse, st);
 }
 
-template <typename T>
-dol_status launch_dlogits(const Layout &L, Planes w, Planes x, int32_t first, const float *bias, const int32_t *target, const float *lse,
+template <typename T, int Q>
+dol_status launch_dlogits(const Layout &L, Planes x, Planes w, int32_t first, const float *bias, const int32_t *target, const float *lse,
                           const float *grad_loss, float *grad_bias, hipStream_t st)
 {
-    DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(xent_dlogits_kernel<T>), T::LDS));
-    const int tm = L.piece / T::BM, tn = static_cast<int>(L.n_pad / T::BN);
-    xent_dlogits_kernel<T><<<tm * tn, T::NT, T::LDS, st>>>(w, x, L.classes, L.rows, static_cast<int>(L.kp / T::BK), first, L.piece, bias, target, lse, grad_loss,
-                                                           L.dl, L.dlt, L.n_pad, grad_bias ? L.bias_part : nullptr);
+    DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(xent_dlogits_kernel<T, Q>), T::LDS));
+    const int tm = static_cast<int>(L.n_pad / T::BM), tn = L.piece / T::BN;
+    xent_dlogits_kernel<T, Q><<<tm * tn, T::NT, T::LDS, st>>>(x, w, L.rows, L.classes, static_cast<int>(L.kp / T::BK), first, L.piece, bias, target, lse, grad_loss, L.dl,
+                                                              L.n_pad, grad_bias ? L.bias_part : nullptr);
     DOL_HIP(hipGetLastError());
     if (grad_bias) {
         const int32_t n = std::min(L.piece, L.classes - first);
-        xent_bias_kernel<<<blocks(n), 256, 0, st>>>(L.bias_part, tn * T::WN, L.piece, n, grad_bias + first);
+        xent_bias_kernel<<<tiles(n, 64), kJoinWaves * 64, 0, st>>>(L.bias_part, tm * T::WM, L.piece, n, grad_bias + first);
         DOL_HIP(hipGetLastError());
     }
     return DOL_OK;
 }
 
-template <typename T, typename O>
-dol_status launch_products(Product a, Product b, hipStream_t st)
+template <typename TX, typename TW, typename O>
+dol_status launch_products(Product x, Product w, hipStream_t st)
 {
-    DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(xent_products_kernel<T, O>), T::LDS));
-    for (Product *p : {&a, &b})
-        if (p->M > 0) p->tm = tiles(p->M, T::BM), p->tn = tiles(p->N, T::BN), p->steps /= T::BK;
-    const int n = a.tm * a.tn * a.splits + b.tm * b.tn * b.splits;
+    DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(xent_products_kernel<TX, TW, O>), TX::LDS));
+    for (Product *p : {&x, &w})
+        if (p->M > 0) p->tm = tiles(p->M, TX::BM), p->tn = tiles(p->N, TX::BN), p->steps = tiles(p->k, TX::BK);
+    const int n = x.tm * x.tn * x.splits + w.tm * w.tn * w.splits;
     if (n == 0) return DOL_OK;
-    xent_products_kernel<T, O><<<n, T::NT, T::LDS, st>>>(a, b);
+    xent_products_kernel<TX, TW, O><<<n, TX::NT, TX::LDS, st>>>(x, w);
     DOL_HIP(hipGetLastError());
     return DOL_OK;
 }
@@ -526,49 +533,41 @@ dol_status launch_products(Product a, Product b, hipStream_t st)
 template <typename O>
 dol_status sum_parts(const Product &p, hipStream_t st)
 {
-    const Sum s{p.part, p.M, p.N, p.splits, p.part_ld, p.out, p.out_ld};
-    xent_sum_parts_kernel<O><<<blocks(int64_t(p.M) * ((p.N + 3) / 4)), 256, 0, st>>>(s);
+    const Sum s{p.part, p.N, p.M, p.splits, p.part_ld, p.out, p.out_ld};
+    xent_sum_parts_kernel<O><<<blocks(int64_t(s.M) * ((s.N + 3) / 4)), 256, 0, st>>>(s);
     DOL_HIP(hipGetLastError());
     return DOL_OK;
 }
 
-template <int P>
+template <int P, int Q>
 dol_status reverse(const Layout &L, const dol_matrix *x, const dol_matrix *w, const float *bias, const int32_t *target, const float *lse,
                    const float *grad_loss, const dol_matrix *grad_x, const dol_matrix *grad_w, float *grad_bias, hipStream_t st)
 {
     using S = typename Source<P>::T;
-    using Big = typename Shapes<P>::Big;
-    using Small = typename Shapes<P>::Small;
+    using Z = Shapes<P, Q>;
     Planes xp, wp;
-    if (dol_status s = pack<P>(x, L.xp, L.kp, &xp, st)) return s;
-    if (dol_status s = pack<P>(w, L.wp, L.kp, &wp, st)) return s;
-    if (grad_w) {
-        xent_pack_cols_kernel<S, P><<<dim3(static_cast<unsigned>(L.n_pad / 64), tiles(L.width, 64)), 256, 0, st>>>(
-            static_cast<const S *>(x->data), x->ld, L.rows, L.width, target, L.classes, L.xt, L.n_pad);
-        DOL_HIP(hipGetLastError());
-    }
-    if (grad_x) {
-        xent_pack_cols_kernel<S, P><<<dim3(static_cast<unsigned>(L.v_pad / 64), tiles(L.width, 64)), 256, 0, st>>>(
-            static_cast<const S *>(w->data), w->ld, L.classes, L.width, nullptr, 0, L.wt, L.v_pad);
-        DOL_HIP(hipGetLastError());
-    }
+    // x is always laid out, with zeros in the rows that do not count: as k of grad_w they would meet dl's zeros with whatever they hold
+    if (dol_status s = pack<P>(x, target, L.classes, L.xp, L.n_pad, L.kp, &xp, st)) return s;
+    if (dol_status s = pack<P>(w, nullptr, 0, L.wp, L.classes, L.kp, &wp, st)) return s;
     for (int32_t k = 0; k < L.pieces; ++k) {
         const int32_t first = k * L.piece, n = std::min(L.piece, L.classes - first);
-        if (dol_status s = L.big ? launch_dlogits<Big>(L, wp, xp, first, bias, target, lse, grad_loss, grad_bias, st)
-                                 : launch_dlogits<Small>(L, wp, xp, first, bias, target, lse, grad_loss, grad_bias, st))
+        if (dol_status s = L.big ? launch_dlogits<typename Z::Big, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, st)
+                                 : launch_dlogits<typename Z::Small, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, st))
             return s;
+        const Planes dl{L.dl, L.piece, L.n_pad * L.piece};
         Product a{}, b{};
         if (grad_x) {
-            a.a = Planes{L.dl, L.piece, L.n_pad * L.piece}, a.b = Planes{L.wt + first, L.v_pad, L.width * L.v_pad};
-            a.M = L.rows, a.N = L.width, a.splits = L.splits_x, a.steps = L.piece;
+            a.a = Planes{wp.data + first * wp.ld, wp.ld, wp.plane}, a.b = dl;
+            a.M = L.width, a.N = L.rows, a.wide = static_cast<int32_t>(L.kp), a.tall = static_cast<int32_t>(L.n_pad), a.splits = L.splits_x, a.k = a.have = n;
             a.part = L.part_x, a.part_ld = L.part_ld, a.add = k > 0, a.out = grad_x->data, a.out_ld = grad_x->ld;
         }
         if (grad_w) {
-            b.a = Planes{L.dlt, L.n_pad, L.n_pad * L.piece}, b.b = Planes{L.xt, L.n_pad, L.width * L.n_pad};
-            b.M = n, b.N = L.width, b.splits = L.splits_w, b.steps = static_cast<int32_t>(L.n_pad);
+            b.a = xp, b.b = dl;
+            b.M = L.width, b.N = n, b.wide = static_cast<int32_t>(L.kp), b.tall = L.piece, b.splits = L.splits_w, b.k = L.rows, b.have = L.n_pad;
             b.part = L.part_w, b.part_ld = L.part_ld, b.out = static_cast<S *>(grad_w->data) + first * grad_w->ld, b.out_ld = grad_w->ld;
         }
-        if (dol_status s = L.big_products ? launch_products<Big, S>(a, b, st) : launch_products<Small, S>(a, b, st)) return s;
+        if (dol_status s = L.big_products ? launch_products<typename Z::BigX, typename Z::BigW, S>(a, b, st) : launch_products<typename Z::SmallX, typename Z::SmallW, S>(a, b, st))
+            return s;
         if (b.part)
             if (dol_status s = sum_parts<S>(b, st)) return s;
         if (a.part && k == L.pieces - 1)
@@ -631,7 +630,8 @@ dol_status dol_cross_entropy_workspace(const dol_matrix *x, const dol_matrix *we
 {
     if (dol_status s = check_operands(x, weight)) return s;
     if (!bytes) return fail(DOL_EINVAL, "bytes is NULL");
-    *bytes = x->rows == 0 ? 0 : (x->dtype == DOL_BF16 ? lay_out<1>(x, weight, backward, nullptr) : lay_out<3>(x, weight, backward, nullptr)).bytes;
+    *bytes = 0;
+    if (x->rows > 0) *bytes = with_planes(x, [&](auto p, auto q) { return lay_out<p.value, q.value>(x, weight, backward, nullptr); }).bytes;
     return DOL_OK;
 }
 
@@ -641,11 +641,11 @@ dol_status dol_cross_entropy(const dol_matrix *x, const dol_matrix *weight, cons
     if (dol_status s = check_operands(x, weight)) return s;
     if (x->rows == 0) return DOL_OK;
     if (!target || !loss || !lse) return fail(DOL_EINVAL, "target, loss or lse is NULL");
-    const bool bf = x->dtype == DOL_BF16;
-    const Layout L = bf ? lay_out<1>(x, weight, false, workspace) : lay_out<3>(x, weight, false, workspace);
-    if (dol_status s = check_workspace(workspace, workspace_bytes, L.bytes)) return s;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return bf ? forward<1>(L, x, weight, bias, target, loss, lse, st) : forward<3>(L, x, weight, bias, target, loss, lse, st);
+    return with_planes(x, [&](auto p, auto q) {
+        const Layout L = lay_out<p.value, q.value>(x, weight, false, workspace);
+        if (dol_status s = check_workspace(workspace, workspace_bytes, L.bytes)) return s;
+        return forward<p.value, q.value>(L, x, weight, bias, target, loss, lse, static_cast<hipStream_t>(hip_stream));
+    });
 }
 
 dol_status dol_cross_entropy_backward(const dol_matrix *x, const dol_matrix *weight, const float *bias, const int32_t *target, const float *lse,
@@ -663,17 +663,17 @@ dol_status dol_cross_entropy_backward(const dol_matrix *x, const dol_matrix *wei
     }
     if (!grad_x && !grad_weight && !grad_bias) return fail(DOL_EINVAL, "no gradient is asked for");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const bool bf = x->dtype == DOL_BF16;
     if (x->rows == 0) {                     // sums over no rows
-        if (dol_status s = bf ? zero<__bf16>(grad_weight, st) : zero<float>(grad_weight, st)) return s;
+        if (dol_status s = x->dtype == DOL_BF16 ? zero<__bf16>(grad_weight, st) : zero<float>(grad_weight, st)) return s;
         const dol_matrix b{DOL_F32, 1, weight->rows, weight->rows, grad_bias};
         return grad_bias ? zero<float>(&b, st) : DOL_OK;
     }
     if (!target || !lse || !grad_loss) return fail(DOL_EINVAL, "target, lse or grad_loss is NULL");
-    const Layout L = bf ? lay_out<1>(x, weight, true, workspace) : lay_out<3>(x, weight, true, workspace);
-    if (dol_status s = check_workspace(workspace, workspace_bytes, L.bytes)) return s;
-    return bf ? reverse<1>(L, x, weight, bias, target, lse, grad_loss, grad_x, grad_weight, grad_bias, st)
-              : reverse<3>(L, x, weight, bias, target, lse, grad_loss, grad_x, grad_weight, grad_bias, st);
+    return with_planes(x, [&](auto p, auto q) {
+        const Layout L = lay_out<p.value, q.value>(x, weight, true, workspace);
+        if (dol_status s = check_workspace(workspace, workspace_bytes, L.bytes)) return s;
+        return reverse<p.value, q.value>(L, x, weight, bias, target, lse, grad_loss, grad_x, grad_weight, grad_bias, st);
+    });
 }
 
 }  // extern "C"

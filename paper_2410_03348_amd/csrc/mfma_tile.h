@@ -70,68 +70,107 @@ struct Planes {
     int64_t plane;      // elements from plane to plane
 };
 
-// A tile of BM x BN by WM x WN wavefronts, ST stages of BK.  Rows lie in LDS as lines of 128 bytes (one row of 64 elements or two of
-// 32) whose 16-byte pieces are exchanged by an exclusive or with the line's number, so that eight neighbouring lanes of a read touch
-// all banks once.  The loads to LDS put lane l's piece at 16 l, so it is the lanes' addresses in memory that are exchanged.
-// A row of B that lane c of fragment j takes is 4 c + j of the wavefront's 64: a lane then holds four neighbouring columns of C in
-// acc[i][0..3], and a row of C leaves as 8- or 16-byte pieces, 16 lanes to a line.
-template <typename V_, int P_, int BM_, int BN_, int BK_, int WM_, int WN_, int ST_>
+// How an operand lies in memory: a row of the product to a row, k contiguous, or k to a row and the product's rows side by side.
+enum Order { kRows, kCols };
+
+// A tile of BM x BN by WM x WN wavefronts, ST stages of BK; A in PA planes, B in PB, ordered OA and OB.
+// kRows: rows lie in LDS as lines of 128 bytes (one row of 64 elements or two of 32) whose 16-byte pieces are exchanged by an exclusive or
+// with the line's number, so that eight neighbouring lanes of a read touch all banks once.  The loads to LDS put lane l's piece at 16 l, so
+// it is the lanes' addresses in memory that are exchanged.  A row of B that lane c of fragment j takes is 4 c + j of the wavefront's 64:
+// a lane then holds four neighbouring columns of C in acc[i][0..3], and a row of C leaves as 8- or 16-byte pieces, 16 lanes to a line.
+// kCols: a step's k lie one below the other, and ds_read_b64_tr_b16 hands them to the lanes: of 16 lanes lane 4 r + q names row r, columns
+// 4 q .. + 3 of a block of 4 x 16, and lane c gets column c of the four rows.  Pairs of pieces are exchanged by k, so that the 16 rows that a
+// wavefront reads at a time lie in all banks.  With A so, a lane's rows 4 (l >> 4) .. + 3 of C are neighbours in memory that is ordered by
+// columns of C, which leaves as 8- or 16-byte pieces; with B so, column c of fragment j is 16 j + c.
+template <typename V_, int PA_, int PB_, Order OA_, Order OB_, int BM_, int BN_, int BK_, int WM_, int WN_, int ST_>
 struct MfmaTile {
     using V = V_;
     using E = typename Mfma<V>::E;
-    static constexpr int P = P_, BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, ST = ST_;
+    static constexpr int PA = PA_, PB = PB_, BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, ST = ST_;
+    static constexpr Order OA = OA_, OB = OB_;
     static constexpr int NW = WM * WN, NT = NW * 64;
     static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
-    static constexpr int CPR = BK / 8, RPL = 64 / BK;                   // pieces to a row, rows to a line
-    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = P * (A_BYTES + B_BYTES);
-    static constexpr int LA = A_BYTES / (NT * 16), LB = B_BYTES / (NT * 16), LOADS = P * (LA + LB);
-    static constexpr int LDS = ST * STAGE > BM * BN * 2 ? ST * STAGE : BM * BN * 2;   // the epilogues lay out a tile of 16 bits
+    static constexpr int CPR = BK / 8, RPL = 64 / BK;                   // kRows: pieces to a row, rows to a line
+    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = PA * A_BYTES + PB * B_BYTES;
+    static constexpr int LA = A_BYTES / (NT * 16), LB = B_BYTES / (NT * 16), LOADS = PA * LA + PB * LB;
+    static constexpr int LDS = ST * STAGE;
     static_assert(NI == 4 && (BK == 32 || BK == 64) && A_BYTES % (NT * 16) == 0 && B_BYTES % (NT * 16) == 0 && ST >= 2, "tile");
 
     __device__ static int key_a(int line) { return line & 7; }
     __device__ static int key_b(int line) { return (RPL == 1 ? line >> 2 : line >> 1) & 7; }
+    __device__ static int key_k(int k) { return ((k & 3) | (k >> 1 & 4)) << 1; }
     template <bool IS_B>
     __device__ static int place(int row, int c)
     {
         const int line = row / RPL, s = (row % RPL) * CPR + c;
         return line * 128 + ((s ^ (IS_B ? key_b(line) : key_a(line))) << 4);
     }
+    // Row of B's wavefront tile that lane c of fragment j takes, and column of C there.
+    __device__ static int col_at(int j, int c) { return OB == kCols ? j * 16 + c : c * 4 + j; }
 
-    // This lane's offsets in bytes from the tile's first row; rows past the operand's end repeat its last one (the caller ignores them).
+    // This lane's offsets in bytes from the tile's first element.  Rows of the product past the operand's `rows` repeat its last one (kCols:
+    // its last eight): the caller ignores them.  kCols: k past `left` repeats the last one; only one operand may be so, the other has zeros there.
     template <bool IS_B, int L>
-    __device__ static void offsets(uint32_t (&o)[L], int wave, int lane, int64_t first, int64_t rows, int64_t ld)
+    __device__ static void offsets(uint32_t (&o)[L], int wave, int lane, int64_t first, int64_t rows, int64_t ld, int64_t left)
     {
+        constexpr int WIDE = IS_B ? BN : BM;
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            const int line = (i * NW + wave) * 8 + (lane >> 3), s = (lane & 7) ^ (IS_B ? key_b(line) : key_a(line));
-            int64_t r = line * RPL + s / CPR;
-            r = first + r < rows ? r : rows - 1 - first;
-            o[i] = static_cast<uint32_t>(r * ld + (s % CPR) * 8) * 2;
+            if constexpr ((IS_B ? OB : OA) == kRows) {
+                const int line = (i * NW + wave) * 8 + (lane >> 3), s = (lane & 7) ^ (IS_B ? key_b(line) : key_a(line));
+                int64_t r = line * RPL + s / CPR;
+                r = first + r < rows ? r : rows - 1 - first;
+                o[i] = static_cast<uint32_t>(r * ld + (s % CPR) * 8) * 2;
+            } else {
+                const int slot = (i * NW + wave) * 64 + lane, k = slot / (WIDE / 8);
+                int64_t c = ((slot % (WIDE / 8)) ^ key_k(k)) * 8;
+                c = first + c < rows ? c : rows - 8 - first;
+                o[i] = static_cast<uint32_t>((k < left ? k : left - 1) * ld + c) * 2;
+            }
         }
     }
 
-    // acc = rows m0.. of a (of M) times rows n0.. of b (of N), over elements k0 .. k0 + BK * steps of each row.
+    // kCols: element e of the fragment of 16 columns from `col`, of k 32 kk + 8 (lane >> 4) + e.
+    template <int WIDE>
+    __device__ static V columns(const char *base, int col, int kk, int lane)
+    {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const int k = kk * 32 + (lane >> 4) * 8 + (lane >> 2 & 3), c = (col >> 3) + (lane >> 1 & 1);
+        const char *at = base + k * (WIDE * 2) + ((c ^ key_k(k)) << 4) + (lane & 1) * 8;
+        using P = __attribute__((address_space(3))) s16x4 *;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(at)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(at + 4 * WIDE * 2));
+        return __builtin_bit_cast(V, static_cast<s16x8>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
+    }
+
+    // acc = rows m0.. of a (of M) times rows n0.. of b (of N), over k0 .. k0 + BK * steps.  kCols operands have `left` k from k0.
     __device__ static void run(const Planes &a, int64_t m0, int64_t M, const Planes &b, int64_t n0, int64_t N, int64_t k0, int steps, char *smem,
-                               f32x4 (&acc)[MI][NI])
+                               f32x4 (&acc)[MI][NI], int64_t left = INT64_MAX)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int wm = wave / WN, wn = wave % WN;
         const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)smem));
         uint32_t ao[LA], bo[LB];
-        offsets<false>(ao, wave, lane, m0, M, a.ld);
-        offsets<true>(bo, wave, lane, n0, N, b.ld);
-        const char *ab = reinterpret_cast<const char *>(a.data + m0 * a.ld + k0), *bb = reinterpret_cast<const char *>(b.data + n0 * b.ld + k0);
+        offsets<false>(ao, wave, lane, m0, M, a.ld, left);
+        offsets<true>(bo, wave, lane, n0, N, b.ld, left);
+        const char *ab = reinterpret_cast<const char *>(a.data + (OA == kRows ? m0 * a.ld + k0 : k0 * a.ld + m0));
+        const char *bb = reinterpret_cast<const char *>(b.data + (OB == kRows ? n0 * b.ld + k0 : k0 * b.ld + n0));
+        const int64_t as = (OA == kRows ? BK : BK * a.ld) * 2, bs = (OB == kRows ? BK : BK * b.ld) * 2;
         auto issue = [&](int kt, int st) {
             const uint32_t base = lds0 + st * STAGE + wave * 1024;
+            if constexpr (OA == kCols || OB == kCols)
+                if (kt > 0 && static_cast<int64_t>(kt + 1) * BK > left) {       // (never past the first step of a later share)
+                    offsets<false>(ao, wave, lane, m0, M, a.ld, left - static_cast<int64_t>(kt) * BK);
+                    offsets<true>(bo, wave, lane, n0, N, b.ld, left - static_cast<int64_t>(kt) * BK);
+                }
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
+            for (int p = 0; p < PA; ++p)
 #pragma unroll
-                for (int i = 0; i < LA; ++i)
-                    load_to_lds16(ab + (p * a.plane + static_cast<int64_t>(kt) * BK) * 2 + ao[i], base + p * A_BYTES + i * NW * 1024);
+                for (int i = 0; i < LA; ++i) load_to_lds16(ab + p * a.plane * 2 + kt * as + ao[i], base + p * A_BYTES + i * NW * 1024);
 #pragma unroll
-                for (int i = 0; i < LB; ++i)
-                    load_to_lds16(bb + (p * b.plane + static_cast<int64_t>(kt) * BK) * 2 + bo[i], base + P * A_BYTES + p * B_BYTES + i * NW * 1024);
-            }
+            for (int p = 0; p < PB; ++p)
+#pragma unroll
+                for (int i = 0; i < LB; ++i) load_to_lds16(bb + p * b.plane * 2 + kt * bs + bo[i], base + PA * A_BYTES + p * B_BYTES + i * NW * 1024);
         };
 #pragma unroll
         for (int i = 0; i < MI; ++i)
@@ -148,44 +187,46 @@ struct MfmaTile {
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (kt + ST - 1 < steps) issue(kt + ST - 1, st == 0 ? ST - 1 : st - 1);
-            const char *sa = smem + st * STAGE, *sb = sa + P * A_BYTES;
+            const char *sa = smem + st * STAGE, *sb = sa + PA * A_BYTES;
 #pragma unroll
             for (int kk = 0; kk < BK / 32; ++kk) {
-                V fa[P][MI], fb[P][NI];
+                V fa[PA][MI], fb[PB][NI];
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
+                for (int p = 0; p < PB; ++p)
 #pragma unroll
-                    for (int j = 0; j < NI; ++j) fb[p][j] = *reinterpret_cast<const V *>(sb + p * B_BYTES + place<true>(wn * TN + r16 * 4 + j, kk * 4 + c4));
+                    for (int j = 0; j < NI; ++j) {
+                        if constexpr (OB == kRows) fb[p][j] = *reinterpret_cast<const V *>(sb + p * B_BYTES + place<true>(wn * TN + col_at(j, r16), kk * 4 + c4));
+                        else fb[p][j] = columns<BN>(sb + p * B_BYTES, wn * TN + j * 16, kk, lane);
+                    }
 #pragma unroll
-                    for (int i = 0; i < MI; ++i) fa[p][i] = *reinterpret_cast<const V *>(sa + p * A_BYTES + place<false>(wm * TM + i * 16 + r16, kk * 4 + c4));
-                }
+                for (int p = 0; p < PA; ++p)
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) {
+                        if constexpr (OA == kRows) fa[p][i] = *reinterpret_cast<const V *>(sa + p * A_BYTES + place<false>(wm * TM + i * 16 + r16, kk * 4 + c4));
+                        else fa[p][i] = columns<BM>(sa + p * A_BYTES, wm * TM + i * 16, kk, lane);
+                    }
+                constexpr int ORDERS = PA > PB ? PA : PB;
 #pragma unroll
                 for (int i = 0; i < MI; ++i)
 #pragma unroll
-                    for (int j = 0; j < NI; ++j) {      // small products first
-                        if constexpr (P == 3) {
-                            acc[i][j] = Mfma<V>::go(fa[2][i], fb[0][j], acc[i][j]);
-                            acc[i][j] = Mfma<V>::go(fa[0][i], fb[2][j], acc[i][j]);
-                            acc[i][j] = Mfma<V>::go(fa[1][i], fb[1][j], acc[i][j]);
-                        }
-                        if constexpr (P >= 2) {
-                            acc[i][j] = Mfma<V>::go(fa[1][i], fb[0][j], acc[i][j]);
-                            acc[i][j] = Mfma<V>::go(fa[0][i], fb[1][j], acc[i][j]);
-                        }
-                        acc[i][j] = Mfma<V>::go(fa[0][i], fb[0][j], acc[i][j]);
-                    }
+                    for (int j = 0; j < NI; ++j)
+#pragma unroll
+                        for (int o = ORDERS - 1; o >= 0; --o)       // small products first
+#pragma unroll
+                            for (int p = PA - 1; p >= 0; --p)
+                                if (p <= o && o - p < PB) acc[i][j] = Mfma<V>::go(fa[p][i], fb[o - p][j], acc[i][j]);
             }
             st = st == ST - 1 ? 0 : st + 1;
         }
     }
 
-    // acc[i][j][e] is row row_of(i) + e and column col_of() + j of the tile.
+    // acc[i][j][e] is row row_of(i) + e and column col_of(j) of the tile.
     __device__ static int row_of(int i) { return (threadIdx.x >> 6) / WN * TM + i * 16 + ((threadIdx.x & 63) >> 4) * 4; }
-    __device__ static int col_of() { return (threadIdx.x >> 6) % WN * TN + (threadIdx.x & 15) * 4; }
+    __device__ static int col_of(int j = 0) { return (threadIdx.x >> 6) % WN * TN + col_at(j, threadIdx.x & 15); }
 
     // Lays a plane of the tile out by columns and writes it as rows of the transpose: value(i, j, e) gives the bits of an element;
     // out + n * ld + m receives element (m, n) for n < cols.  All threads call it; smem may hold anything else.  ld and out: multiples
-    // of 8 elements; the tile's BM rows must fit.
+    // of 8 elements; the tile's BM rows must fit, and BM * BN * 2 bytes of LDS.
     template <typename F>
     __device__ static void store_transposed(char *smem, uint16_t *out, int64_t ld, int64_t cols, F value)
     {

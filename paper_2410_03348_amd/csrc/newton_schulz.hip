@@ -23,15 +23,15 @@ template <int P>
 struct Shapes;
 template <>
 struct Shapes<1> {
-    using Big = MfmaTile<f16x8, 1, 256, 256, 64, 2, 4, 2>;
-    using Mid = MfmaTile<f16x8, 1, 128, 128, 64, 2, 2, 2>;
-    using Small = MfmaTile<f16x8, 1, 64, 64, 64, 4, 1, 3>;
+    using Big = MfmaTile<f16x8, 1, 1, kRows, kRows, 256, 256, 64, 2, 4, 2>;
+    using Mid = MfmaTile<f16x8, 1, 1, kRows, kRows, 128, 128, 64, 2, 2, 2>;
+    using Small = MfmaTile<f16x8, 1, 1, kRows, kRows, 64, 64, 64, 4, 1, 3>;
 };
 template <>
 struct Shapes<2> {
-    using Big = MfmaTile<f16x8, 2, 256, 256, 32, 2, 4, 2>;
-    using Mid = MfmaTile<f16x8, 2, 128, 128, 32, 2, 2, 2>;
-    using Small = MfmaTile<f16x8, 2, 64, 64, 32, 4, 1, 3>;
+    using Big = MfmaTile<f16x8, 2, 2, kRows, kRows, 256, 256, 32, 2, 4, 2>;
+    using Mid = MfmaTile<f16x8, 2, 2, kRows, kRows, 128, 128, 32, 2, 2, 2>;
+    using Small = MfmaTile<f16x8, 2, 2, kRows, kRows, 64, 64, 32, 4, 1, 3>;
 };
 
 // Powers of two that X, A and B are stored times.
@@ -202,11 +202,11 @@ __global__ void __launch_bounds__(T::NT, 2) ns_symmetric_kernel(const uint16_t *
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             f32x4 old = {0, 0, 0, 0};
-            if constexpr (POLY) old = read4(src + at + static_cast<int64_t>(T::row_of(i) + e) * mp + T::col_of(), plane, T::P);
+            if constexpr (POLY) old = read4(src + at + static_cast<int64_t>(T::row_of(i) + e) * mp + T::col_of(), plane, T::PA);
 #pragma unroll
             for (int j = 0; j < T::NI; ++j) acc[i][j][e] = POLY ? __builtin_fmaf(beta, old[j], alpha * acc[i][j][e]) : alpha * acc[i][j][e];
         }
-    store_planes<T>(acc, smem, dst + at, mp, T::P, mt != nt ? dst + across : nullptr, mp, mt != nt ? T::P : 0, out_plane);
+    store_planes<T>(acc, smem, dst + at, mp, T::PA, mt != nt ? dst + across : nullptr, mp, mt != nt ? T::PA : 0, out_plane);
 }
 
 // rows x cols of X' = alpha (B X) + beta X: both operands' rows (X's transpose and B, or B and X's transpose) give the tile, `old` holds X
@@ -441,11 +441,11 @@ dol_status symmetric(const Layout &L, int32_t batch, bool poly, int k, float alp
     const int64_t plane = int64_t(L.mp) * L.mp;
     if (poly) {
         if (dol_status s = ready(ns_symmetric_kernel<T, true>, T::LDS)) return s;
-        ns_symmetric_kernel<T, true><<<grid, T::NT, T::LDS, st>>>(L.a, T::P * plane, L.mp, plane, L.mp, L.mp / T::BK, alpha, beta, L.b, T::P * plane, plane);
+        ns_symmetric_kernel<T, true><<<grid, T::NT, T::LDS, st>>>(L.a, T::PA * plane, L.mp, plane, L.mp, L.mp / T::BK, alpha, beta, L.b, T::PA * plane, plane);
     } else {
         const int64_t xplane = int64_t(L.mp) * L.np;
         if (dol_status s = ready(ns_symmetric_kernel<T, false>, T::LDS)) return s;
-        ns_symmetric_kernel<T, false><<<grid, T::NT, T::LDS, st>>>(L.x[k], 2 * xplane, L.np, xplane, L.mp, L.np / T::BK, alpha, beta, L.a, T::P * plane, plane);
+        ns_symmetric_kernel<T, false><<<grid, T::NT, T::LDS, st>>>(L.x[k], 2 * xplane, L.np, xplane, L.mp, L.np / T::BK, alpha, beta, L.a, T::PA * plane, plane);
     }
     DOL_HIP(hipGetLastError());
     return DOL_OK;
@@ -459,12 +459,12 @@ dol_status apply(const Layout &L, int32_t batch, int k, bool last, float alpha, 
     const Planes xt{L.xt[k], L.mp, xplane}, b{L.b, L.mp, plane};
     Apply p{};
     p.a = turn ? xt : b, p.b = turn ? b : xt;
-    p.a_stride = turn ? 2 * xplane : T::P * plane, p.b_stride = turn ? T::P * plane : 2 * xplane;
+    p.a_stride = turn ? 2 * xplane : T::PA * plane, p.b_stride = turn ? T::PA * plane : 2 * xplane;
     p.old = turn ? L.xt[k] : L.x[k], p.old_stride = 2 * xplane;
     p.rows = turn ? L.np : L.mp, p.cols = turn ? L.mp : L.np, p.steps = L.mp / T::BK;
     p.alpha = alpha, p.beta = beta;
     if (last) p.out = out->data, p.out_ld = out->ld, p.out_stride = out_stride, p.out_rows = out->rows, p.out_cols = out->cols;
-    else p.to = L.x[k ^ 1], p.turned = L.xt[k ^ 1], p.turned_planes = T::P == 2 || L.tall ? 2 : 1;
+    else p.to = L.x[k ^ 1], p.turned = L.xt[k ^ 1], p.turned_planes = T::PA == 2 || L.tall ? 2 : 1;
     if (dol_status s = ready(ns_apply_kernel<T, O>, T::LDS)) return s;
     ns_apply_kernel<T, O><<<dim3(static_cast<unsigned>(p.rows / T::BM * (p.cols / T::BN)), static_cast<unsigned>(batch)), T::NT, T::LDS, st>>>(p);
     DOL_HIP(hipGetLastError());
