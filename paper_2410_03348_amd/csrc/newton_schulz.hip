@@ -2,7 +2,7 @@
 //   A = X X^T,   B = b A + c A A,   X <- a X + B X
 // so that every singular value s of X becomes s (a + b s^2 + c s^4); a matrix taller than wide is taken as its transpose.
 //
-// All three are products of rows with contiguous k (mfma_tile.h): X is kept both ways round, A and B are symmetric.  Numbers lie as fp16
+// X lies one way, as wide rows: A's tiles read it along k, X's own across k (mfma_tile.h); A and B are symmetric.  Numbers lie as fp16
 // times a power of two that their bounds allow: singular values stay below a bound known beforehand, and no element is above them.
 // float: two planes each, 22 bits, three products: as exact as 32-bit sums of 32-bit numbers (an error of a step's X grows with the
 // steps after it, up to a^steps = 485 times for directions whose singular value is near 0, so there is nothing to spare).
@@ -19,19 +19,26 @@ constexpr int kPad = 256;           // rows and columns are filled up with zeros
 constexpr int kNormParts = 256;     // workgroups that share a matrix's sum of squares
 constexpr int kUnits = 256;
 
+// Tiles of the symmetric products, of B X with X's columns as the tile's rows, and (for a tall result) as its columns.
 template <int P>
 struct Shapes;
 template <>
 struct Shapes<1> {
-    using Big = MfmaTile<f16x8, 1, 1, kRows, kRows, 256, 256, 64, 2, 4, 2>;
-    using Mid = MfmaTile<f16x8, 1, 1, kRows, kRows, 128, 128, 64, 2, 2, 2>;
-    using Small = MfmaTile<f16x8, 1, 1, kRows, kRows, 64, 64, 64, 4, 1, 3>;
+    template <Order A, Order B>
+    using Big = MfmaTile<f16x8, 1, 1, A, B, 256, 256, 64, 2, 4, 2>;
+    template <Order A, Order B>
+    using Mid = MfmaTile<f16x8, 1, 1, A, B, 128, 128, 64, 2, 2, 2>;
+    template <Order A, Order B>
+    using Small = MfmaTile<f16x8, 1, 1, A, B, 64, 64, 64, 4, 1, 3>;
 };
 template <>
 struct Shapes<2> {
-    using Big = MfmaTile<f16x8, 2, 2, kRows, kRows, 256, 256, 32, 2, 4, 2>;
-    using Mid = MfmaTile<f16x8, 2, 2, kRows, kRows, 128, 128, 32, 2, 2, 2>;
-    using Small = MfmaTile<f16x8, 2, 2, kRows, kRows, 64, 64, 32, 4, 1, 3>;
+    template <Order A, Order B>
+    using Big = MfmaTile<f16x8, 2, 2, A, B, 256, 256, 32, 2, 4, 2>;
+    template <Order A, Order B>
+    using Mid = MfmaTile<f16x8, 2, 2, A, B, 128, 128, 32, 2, 2, 2>;
+    template <Order A, Order B>
+    using Small = MfmaTile<f16x8, 2, 2, A, B, 64, 64, 32, 4, 1, 3>;
 };
 
 // Powers of two that X, A and B are stored times.
@@ -74,10 +81,10 @@ __global__ void __launch_bounds__(256) ns_norm_kernel(const S *g, int64_t ld, in
     if (threadIdx.x == 0) part[static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// X [mp][np] and its transpose, two planes each, from g (transposed where it is taller than wide); a tile of 64 x 64 to a workgroup.
+// X [mp][np] in two planes, from g (transposed where it is taller than wide); a tile of 64 x 64 to a workgroup.
 template <typename S>
 __global__ void __launch_bounds__(256) ns_first_kernel(const S *g, int64_t ld, int64_t stride, int32_t rows, int32_t cols, bool tall, const double *part, int parts,
-                                                       float eps, int scale, uint16_t *x, uint16_t *xt, int32_t mp, int32_t np)
+                                                       float eps, int scale, uint16_t *x, int32_t mp, int32_t np)
 {
     __shared__ float tile[64][65];
     __shared__ double total;
@@ -91,7 +98,6 @@ __global__ void __launch_bounds__(256) ns_first_kernel(const S *g, int64_t ld, i
     __syncthreads();
     const double f = ldexp(1.0, scale) / (sqrt(total) + static_cast<double>(eps));
     const S *src = g + blockIdx.z * stride;
-    const int32_t gr = tall ? np : mp, gc = tall ? mp : np;       // padded rows and columns of g
     const int32_t r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;     // in g
     const int cx = threadIdx.x & 63, cy = threadIdx.x >> 6;
 #pragma unroll 4
@@ -101,26 +107,24 @@ __global__ void __launch_bounds__(256) ns_first_kernel(const S *g, int64_t ld, i
     }
     __syncthreads();
     const int64_t plane = static_cast<int64_t>(mp) * np;
-    uint16_t *straight = (tall ? xt : x) + blockIdx.z * 2 * plane, *turned = (tall ? x : xt) + blockIdx.z * 2 * plane;
+    uint16_t *dst = x + blockIdx.z * 2 * plane;
     const int q = threadIdx.x & 7;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int k = (threadIdx.x >> 3) + h * 32;
-        for (int way = 0; way < 2; ++way) {
-            float v[8];
+        float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = way ? tile[q * 8 + e][k] : tile[k][q * 8 + e];
-            uint16_t *to = way ? turned + static_cast<int64_t>(c0 + k) * gr + r0 + q * 8 : straight + static_cast<int64_t>(r0 + k) * gc + c0 + q * 8;
+        for (int e = 0; e < 8; ++e) v[e] = tall ? tile[q * 8 + e][k] : tile[k][q * 8 + e];
+        uint16_t *to = dst + (tall ? static_cast<int64_t>(c0 + k) * np + r0 + q * 8 : static_cast<int64_t>(r0 + k) * np + c0 + q * 8);
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                u32x4 w;
+        for (int p = 0; p < 2; ++p) {
+            u32x4 w;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t lo = take_plane<_Float16>(v[2 * e]), hi = take_plane<_Float16>(v[2 * e + 1]);
-                    w[e] = lo | hi << 16;
-                }
-                *reinterpret_cast<u32x4 *>(to + p * plane) = w;
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t lo = take_plane<_Float16>(v[2 * e]), hi = take_plane<_Float16>(v[2 * e + 1]);
+                w[e] = lo | hi << 16;
             }
+            *reinterpret_cast<u32x4 *>(to + p * plane) = w;
         }
     }
 }
@@ -140,42 +144,18 @@ __device__ __forceinline__ f32x4 read4(const uint16_t *p, int64_t plane, int pla
     return v;
 }
 
-// Planes of the tile to rows of `to` and to rows of its transpose `turned` (either may be null), taking them out of acc.
-template <typename T>
-__device__ __forceinline__ void store_planes(f32x4 (&acc)[T::MI][T::NI], char *smem, uint16_t *to, int64_t ld, int planes, uint16_t *turned, int64_t turned_ld,
-                                             int turned_planes, int64_t plane)
+// Four neighbouring elements to P planes.
+template <int P>
+__device__ __forceinline__ void write4(uint16_t *to, int64_t plane, f32x4 v)
 {
-#pragma unroll 1
-    for (int p = 0; p < max(planes, turned_planes); ++p) {
-        if (to && p < planes) {
 #pragma unroll
-            for (int i = 0; i < T::MI; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    u32x2 v;
-                    v[0] = bits16<_Float16>(acc[i][0][e]) | bits16<_Float16>(acc[i][1][e]) << 16;
-                    v[1] = bits16<_Float16>(acc[i][2][e]) | bits16<_Float16>(acc[i][3][e]) << 16;
-                    *reinterpret_cast<u32x2 *>(to + p * plane + (T::row_of(i) + e) * ld + T::col_of()) = v;
-                }
-        }
-        if (turned && p < turned_planes)
-            T::store_transposed(smem, turned + p * plane, turned_ld, T::BN, [&](int i, int j, int e) {
-                float v = acc[i][j][e];
-                const uint32_t b = take_plane<_Float16>(v);
-                acc[i][j][e] = v;
-                return b;
-            });
-        else
-#pragma unroll
-            for (int i = 0; i < T::MI; ++i)
-#pragma unroll
-                for (int j = 0; j < T::NI; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float v = acc[i][j][e];
-                        take_plane<_Float16>(v);
-                        acc[i][j][e] = v;
-                    }
+    for (int p = 0; p < P; ++p) {
+        float r[4] = {v[0], v[1], v[2], v[3]};
+        u32x2 w;
+        const uint32_t w0 = take_plane<_Float16>(r[0]), w1 = take_plane<_Float16>(r[1]), w2 = take_plane<_Float16>(r[2]), w3 = take_plane<_Float16>(r[3]);
+        w[0] = w0 | w1 << 16, w[1] = w2 | w3 << 16;
+        *reinterpret_cast<u32x2 *>(to + p * plane) = w;
+        v = f32x4{r[0], r[1], r[2], r[3]};
     }
 }
 
@@ -196,66 +176,71 @@ __global__ void __launch_bounds__(T::NT, 2) ns_symmetric_kernel(const uint16_t *
     f32x4 acc[T::MI][T::NI];
     const Planes p{src, ld, plane};
     T::run(p, mt * T::BM, mp, p, nt * T::BN, mp, 0, steps, smem, acc);
-    const int64_t at = static_cast<int64_t>(mt) * T::BM * mp + nt * T::BN, across = static_cast<int64_t>(nt) * T::BN * mp + mt * T::BM;
+    const int64_t m0 = mt * T::BM, n = nt * T::BN + T::col_of();
 #pragma unroll
-    for (int i = 0; i < T::MI; ++i)
+    for (int i = 0; i < T::MI; ++i) {
+        const int64_t m = m0 + T::row_of(i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            f32x4 old = {0, 0, 0, 0};
-            if constexpr (POLY) old = read4(src + at + static_cast<int64_t>(T::row_of(i) + e) * mp + T::col_of(), plane, T::PA);
+            f32x4 v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]}, old = {0, 0, 0, 0};
+            if constexpr (POLY) old = read4(src + (m + e) * mp + n, plane, T::PA);
 #pragma unroll
-            for (int j = 0; j < T::NI; ++j) acc[i][j][e] = POLY ? __builtin_fmaf(beta, old[j], alpha * acc[i][j][e]) : alpha * acc[i][j][e];
+            for (int j = 0; j < T::NI; ++j) acc[i][j][e] = v[j] = POLY ? __builtin_fmaf(beta, old[j], alpha * v[j]) : alpha * v[j];
+            write4<T::PA>(dst + (m + e) * mp + n, out_plane, v);
         }
-    store_planes<T>(acc, smem, dst + at, mp, T::PA, mt != nt ? dst + across : nullptr, mp, mt != nt ? T::PA : 0, out_plane);
+        if (mt != nt)
+#pragma unroll
+            for (int j = 0; j < T::NI; ++j) write4<T::PA>(dst + (n + j) * mp + m, out_plane, acc[i][j]);
+    }
 }
 
-// rows x cols of X' = alpha (B X) + beta X: both operands' rows (X's transpose and B, or B and X's transpose) give the tile, `old` holds X
-// in the tile's orientation.  Either planes of X' both ways round, or (out) the result.
+// X' = alpha (B X) + beta X, X' [mp][np] in two planes, or (out) the result.  TURN: a tile's columns are X's columns and out is tall.
 struct Apply {
-    Planes a, b;
-    int64_t a_stride, b_stride;
-    const uint16_t *old;
-    int64_t old_stride;
-    int32_t rows, cols;             // filled up
-    int steps;
+    const uint16_t *x, *b;
+    int64_t x_stride, b_stride;
+    int32_t mp, np;
     float alpha, beta;
-    uint16_t *to, *turned;
-    int turned_planes;
+    uint16_t *to;
     void *out;
     int64_t out_ld, out_stride;
     int32_t out_rows, out_cols;
 };
 
-template <typename T, typename O>
+template <typename T, typename O, bool TURN>
 __global__ void __launch_bounds__(T::NT, 2) ns_apply_kernel(Apply p)
 {
     extern __shared__ __align__(128) char smem[];
-    const int tm = p.rows / T::BM, tn = p.cols / T::BN;
+    const int tm = (TURN ? p.mp : p.np) / T::BM, tn = (TURN ? p.np : p.mp) / T::BN;
     int mt, nt;
     tile_of(xcd_contiguous(blockIdx.x, gridDim.x), tm, tn, 4, mt, nt);
-    const int64_t z = blockIdx.y, plane = static_cast<int64_t>(p.rows) * p.cols;
-    const uint16_t *old = p.old + z * p.old_stride;
+    const int64_t z = blockIdx.y, plane = static_cast<int64_t>(p.mp) * p.np;
+    const uint16_t *x = p.x + z * p.x_stride;
+    const Planes px{x, p.np, plane}, pb{p.b + z * p.b_stride, p.mp, static_cast<int64_t>(p.mp) * p.mp};
     f32x4 acc[T::MI][T::NI];
-    T::run(Planes{p.a.data + z * p.a_stride, p.a.ld, p.a.plane}, mt * T::BM, p.rows, Planes{p.b.data + z * p.b_stride, p.b.ld, p.b.plane}, nt * T::BN, p.cols, 0, p.steps,
-           smem, acc);
-    const int64_t at = static_cast<int64_t>(mt) * T::BM * p.cols + nt * T::BN;
-    const int n = nt * T::BN + T::col_of();
+    T::run(TURN ? pb : px, mt * T::BM, TURN ? p.mp : p.np, TURN ? px : pb, nt * T::BN, TURN ? p.np : p.mp, 0, p.mp / T::BK, smem, acc, p.mp);
     const bool vec = p.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(static_cast<O *>(p.out) + z * p.out_stride) & (4 * sizeof(O) - 1)) == 0;
 #pragma unroll
-    for (int i = 0; i < T::MI; ++i)
+    for (int i = 0; i < T::MI; ++i) {
+        const int64_t m = static_cast<int64_t>(mt) * T::BM + T::row_of(i);      // four rows of the tile from here: neighbours in memory
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = T::row_of(i) + e;
-            const f32x4 x = read4(old + at + static_cast<int64_t>(row) * p.cols + T::col_of(), plane, 2);
+        for (int j = 0; j < T::NI; ++j) {
+            const int64_t n = static_cast<int64_t>(nt) * T::BN + T::col_of(j);
+            f32x4 old;
+            if constexpr (TURN) {
 #pragma unroll
-            for (int j = 0; j < T::NI; ++j) acc[i][j][e] = __builtin_fmaf(p.beta, x[j], p.alpha * acc[i][j][e]);
-            if (p.out && mt * T::BM + row < p.out_rows && n < p.out_cols)
-                store4(static_cast<O *>(p.out) + z * p.out_stride + static_cast<int64_t>(mt * T::BM + row) * p.out_ld + n,
-                       f32x4{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]}, p.out_cols - n, vec);
+                for (int e = 0; e < 4; ++e) old[e] = half_of(x[plane + (m + e) * p.np + n]) + half_of(x[(m + e) * p.np + n]);
+            } else
+                old = read4(x + n * p.np + m, plane, 2);
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(p.beta, old[e], p.alpha * acc[i][j][e]);
+            if (TURN || p.out) {
+                if (n < p.out_rows && m < p.out_cols)
+                    store4(static_cast<O *>(p.out) + z * p.out_stride + n * p.out_ld + m, v, static_cast<int>(p.out_cols - m), vec);
+            } else
+                write4<2>(p.to + z * p.x_stride + n * p.np + m, plane, v);
         }
-    if (p.out) return;
-    store_planes<T>(acc, smem, p.to + z * p.old_stride + at, p.cols, 2, p.turned + z * p.old_stride + static_cast<int64_t>(nt) * T::BN * p.rows + mt * T::BM, p.rows,
-                    p.turned_planes, plane);
+    }
 }
 
 // ---------------------------------------------------------------- small matrices
@@ -388,7 +373,7 @@ struct Layout {
     bool tall;
     int32_t m, n, mp, np;           // the wide orientation, and filled up
     double *part;
-    uint16_t *x[2], *xt[2], *a, *b;
+    uint16_t *x[2], *a, *b;
     int64_t bytes;
 };
 
@@ -402,7 +387,7 @@ Layout lay_out(const dol_matrix *g, int32_t batch, int planes, void *workspace)
     Carver c(workspace);
     const int64_t x = 2 * int64_t(L.mp) * L.np * batch, a = planes * int64_t(L.mp) * L.mp * batch;
     L.part = c.take<double>(int64_t(kNormParts) * batch);
-    for (int k = 0; k < 2; ++k) L.x[k] = c.take<uint16_t>(x), L.xt[k] = c.take<uint16_t>(x);
+    for (int k = 0; k < 2; ++k) L.x[k] = c.take<uint16_t>(x);
     L.a = c.take<uint16_t>(a), L.b = c.take<uint16_t>(a);
     L.bytes = c.used;
     return L;
@@ -451,22 +436,16 @@ dol_status symmetric(const Layout &L, int32_t batch, bool poly, int k, float alp
     return DOL_OK;
 }
 
-template <typename T, typename O>
+template <typename T, typename O, bool TURN>
 dol_status apply(const Layout &L, int32_t batch, int k, bool last, float alpha, float beta, const dol_matrix *out, int64_t out_stride, hipStream_t st)
 {
-    const int64_t xplane = int64_t(L.mp) * L.np, plane = int64_t(L.mp) * L.mp;
-    const bool turn = last && L.tall;       // the result's own orientation
-    const Planes xt{L.xt[k], L.mp, xplane}, b{L.b, L.mp, plane};
     Apply p{};
-    p.a = turn ? xt : b, p.b = turn ? b : xt;
-    p.a_stride = turn ? 2 * xplane : T::PA * plane, p.b_stride = turn ? T::PA * plane : 2 * xplane;
-    p.old = turn ? L.xt[k] : L.x[k], p.old_stride = 2 * xplane;
-    p.rows = turn ? L.np : L.mp, p.cols = turn ? L.mp : L.np, p.steps = L.mp / T::BK;
-    p.alpha = alpha, p.beta = beta;
+    p.x = L.x[k], p.b = L.b, p.x_stride = 2 * int64_t(L.mp) * L.np, p.b_stride = T::PA * int64_t(L.mp) * L.mp;
+    p.mp = L.mp, p.np = L.np, p.alpha = alpha, p.beta = beta, p.to = L.x[k ^ 1];
     if (last) p.out = out->data, p.out_ld = out->ld, p.out_stride = out_stride, p.out_rows = out->rows, p.out_cols = out->cols;
-    else p.to = L.x[k ^ 1], p.turned = L.xt[k ^ 1], p.turned_planes = T::PA == 2 || L.tall ? 2 : 1;
-    if (dol_status s = ready(ns_apply_kernel<T, O>, T::LDS)) return s;
-    ns_apply_kernel<T, O><<<dim3(static_cast<unsigned>(p.rows / T::BM * (p.cols / T::BN)), static_cast<unsigned>(batch)), T::NT, T::LDS, st>>>(p);
+    if (dol_status s = ready(ns_apply_kernel<T, O, TURN>, T::LDS)) return s;
+    const int rows = TURN ? L.mp : L.np, cols = TURN ? L.np : L.mp;
+    ns_apply_kernel<T, O, TURN><<<dim3(static_cast<unsigned>(rows / T::BM * (cols / T::BN)), static_cast<unsigned>(batch)), T::NT, T::LDS, st>>>(p);
     DOL_HIP(hipGetLastError());
     return DOL_OK;
 }
@@ -487,15 +466,13 @@ template <int P, typename S>
 dol_status newton_schulz(const Layout &L, const dol_matrix *g, int64_t g_stride, const dol_matrix *out, int64_t out_stride, int32_t batch, int32_t steps,
                          const float *k, float eps, Scales e, hipStream_t st)
 {
-    using Big = typename Shapes<P>::Big;
-    using Mid = typename Shapes<P>::Mid;
-    using Small = typename Shapes<P>::Small;
+    using Z = Shapes<P>;
     const int parts = static_cast<int>(std::min<int64_t>(kNormParts, (int64_t(g->rows) * g->cols + 4095) / 4096));
     ns_norm_kernel<S><<<dim3(parts, batch), 256, 0, st>>>(static_cast<const S *>(g->data), g->ld, g_stride, g->rows, g->cols, L.part);
     DOL_HIP(hipGetLastError());
     const int32_t gr = L.tall ? L.np : L.mp, gc = L.tall ? L.mp : L.np;
     ns_first_kernel<S><<<dim3(gr / 64, gc / 64, batch), 256, 0, st>>>(static_cast<const S *>(g->data), g->ld, g_stride, g->rows, g->cols, L.tall, L.part, parts, eps, e.x, L.x[0],
-                                                                      L.xt[0], L.mp, L.np);
+                                                                      L.mp, L.np);
     DOL_HIP(hipGetLastError());
     auto two = [](int n) { return std::ldexp(1.0f, n); };
     // the largest tiles that fill the chip
@@ -508,17 +485,25 @@ dol_status newton_schulz(const Layout &L, const dol_matrix *g, int64_t g_stride,
         for (int poly = 0; poly < 2; ++poly) {
             const float alpha = poly ? k[2] * two(e.b - 2 * e.a) : two(e.a - 2 * e.x), beta = poly ? k[1] * two(e.b - e.a) : 0.0f;
             const int size = size_of(L.mp, L.mp, true);
-            if (dol_status s = size == 2 ? symmetric<Big>(L, batch, poly, from, alpha, beta, st)
-                                         : size == 1 ? symmetric<Mid>(L, batch, poly, from, alpha, beta, st) : symmetric<Small>(L, batch, poly, from, alpha, beta, st))
+            if (dol_status s = size == 2   ? symmetric<typename Z::template Big<kRows, kRows>>(L, batch, poly, from, alpha, beta, st)
+                               : size == 1 ? symmetric<typename Z::template Mid<kRows, kRows>>(L, batch, poly, from, alpha, beta, st)
+                                           : symmetric<typename Z::template Small<kRows, kRows>>(L, batch, poly, from, alpha, beta, st))
                 return s;
         }
         const bool last = t == steps - 1;
         const float alpha = last ? two(-e.b - e.x) : two(-e.b), beta = last ? k[0] * two(-e.x) : k[0];
         const int size = size_of(L.mp, L.np, false);
-        if (dol_status s = size == 2 ? apply<Big, S>(L, batch, from, last, alpha, beta, out, out_stride, st)
-                                     : size == 1 ? apply<Mid, S>(L, batch, from, last, alpha, beta, out, out_stride, st)
-                                                 : apply<Small, S>(L, batch, from, last, alpha, beta, out, out_stride, st))
-            return s;
+        if (last && L.tall) {
+            if (dol_status s = size == 2   ? apply<typename Z::template Big<kRows, kCols>, S, true>(L, batch, from, last, alpha, beta, out, out_stride, st)
+                               : size == 1 ? apply<typename Z::template Mid<kRows, kCols>, S, true>(L, batch, from, last, alpha, beta, out, out_stride, st)
+                                           : apply<typename Z::template Small<kRows, kCols>, S, true>(L, batch, from, last, alpha, beta, out, out_stride, st))
+                return s;
+        } else {
+            if (dol_status s = size == 2   ? apply<typename Z::template Big<kCols, kRows>, S, false>(L, batch, from, last, alpha, beta, out, out_stride, st)
+                               : size == 1 ? apply<typename Z::template Mid<kCols, kRows>, S, false>(L, batch, from, last, alpha, beta, out, out_stride, st)
+                                           : apply<typename Z::template Small<kCols, kRows>, S, false>(L, batch, from, last, alpha, beta, out, out_stride, st))
+                return s;
+        }
     }
     return DOL_OK;
 }
