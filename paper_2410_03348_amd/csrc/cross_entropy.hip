@@ -113,6 +113,7 @@ __global__ void __launch_bounds__(T::NT, 2) xent_sums_kernel(Planes w, Planes x,
     int mt, nt;
     tile_of(xcd_contiguous(blockIdx.x, gridDim.x), tm, tn, 4, mt, nt);
     f32x4 acc[T::MI][T::NI];
+    T::clear(acc);
     T::run(w, static_cast<int64_t>(mt) * T::BM, classes, x, static_cast<int64_t>(nt) * T::BN, rows, 0, steps, smem, acc);
     const int m0 = mt * T::BM, n0 = nt * T::BN + T::col_of();
     if (bias || m0 + T::BM > classes) {
@@ -209,6 +210,7 @@ __global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes
     int mt, nt;
     tile_of(xcd_contiguous(blockIdx.x, gridDim.x), tm, tn, 8, mt, nt);
     f32x4 acc[T::MI][T::NI];
+    T::clear(acc);
     const int m0 = mt * T::BM, n0 = first + nt * T::BN;
     // (a tile that lies wholly past the last sample or class repeats the last row; it comes out as zeros all the same)
     T::run(x, min(m0, rows - 1), rows, w, min(n0, classes - 1), classes, 0, steps, smem, acc);
@@ -306,6 +308,7 @@ __device__ __forceinline__ void product_tile(const Product &p, int id, char *sme
     const int s0 = static_cast<int>(static_cast<int64_t>(p.steps) * split / p.splits), s1 = static_cast<int>(static_cast<int64_t>(p.steps) * (split + 1) / p.splits);
     const int64_t k0 = static_cast<int64_t>(s0) * T::BK;
     f32x4 acc[T::MI][T::NI];
+    T::clear(acc);
     T::run(p.a, static_cast<int64_t>(mt) * T::BM, p.wide, p.b, static_cast<int64_t>(nt) * T::BN, p.tall, k0, s1 - s0, smem, acc, p.have - k0);
     const bool vec = p.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (4 * sizeof(O) - 1)) == 0;
 #pragma unroll

@@ -150,7 +150,15 @@ struct MfmaTile {
         return __builtin_bit_cast(V, static_cast<s16x8>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
     }
 
-    // acc = rows m0.. of a (of M) times rows n0.. of b (of N), over k0 .. k0 + BK * steps.  kCols operands have `left` k from k0.
+    __device__ static void clear(f32x4 (&acc)[MI][NI])
+    {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    }
+
+    // acc += rows m0.. of a (of M) times rows n0.. of b (of N), over k0 .. k0 + BK * steps.  kCols operands have `left` k from k0.
     __device__ static void run(const Planes &a, int64_t m0, int64_t M, const Planes &b, int64_t n0, int64_t N, int64_t k0, int steps, char *smem,
                                f32x4 (&acc)[MI][NI], int64_t left = INT64_MAX)
     {
@@ -182,10 +190,6 @@ struct MfmaTile {
 #pragma unroll
                 for (int i = 0; i < LB; ++i) load_to_lds16(pb + p * b.plane * 2 + bo[i], base + PA * A_BYTES + p * B_BYTES + i * NW * 1024);
         };
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
         const int r16 = lane & 15, c4 = lane >> 4;
         auto read = [&](int st, int kk, V (&fa)[PA][MI], V (&fb)[PB][NI]) {
             const char *sa = smem + st * STAGE, *sb = sa + PA * A_BYTES;
@@ -207,14 +211,14 @@ struct MfmaTile {
         auto products = [&](const V (&fa)[PA][MI], const V (&fb)[PB][NI]) {
             constexpr int ORDERS = PA > PB ? PA : PB;
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
+            for (int o = ORDERS - 1; o >= 0; --o)       // small products first; a sum's own products apart, for each waits for the one before
 #pragma unroll
-                for (int j = 0; j < NI; ++j)
+                for (int p = PA - 1; p >= 0; --p)
+                    if (p <= o && o - p < PB)
 #pragma unroll
-                    for (int o = ORDERS - 1; o >= 0; --o)       // small products first
+                        for (int i = 0; i < MI; ++i)
 #pragma unroll
-                        for (int p = PA - 1; p >= 0; --p)
-                            if (p <= o && o - p < PB) acc[i][j] = Mfma<V>::go(fa[p][i], fb[o - p][j], acc[i][j]);
+                            for (int j = 0; j < NI; ++j) acc[i][j] = Mfma<V>::go(fa[p][i], fb[o - p][j], acc[i][j]);
         };
         if constexpr (HALVES) {
             // The halves of a step have registers of their own: while one half's products run the next one's operands are read, the last

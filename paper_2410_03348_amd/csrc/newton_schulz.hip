@@ -16,7 +16,7 @@ namespace dol {
 namespace {
 
 constexpr int kPad = 256;           // rows and columns are filled up with zeros, which stay zeros
-constexpr int kNormParts = 256;     // workgroups that share a matrix's sum of squares
+constexpr int kNormParts = 1024;    // workgroups that share a matrix's sum of squares, at most
 constexpr int kUnits = 256;
 
 // Tiles of the symmetric products, of B X with X's columns as the tile's rows, and (for a tall result) as its columns.
@@ -38,7 +38,7 @@ struct Shapes<2> {
     template <Order A, Order B>
     using Mid = MfmaTile<f16x8, 2, 2, A, B, 128, 128, 32, 2, 2, 2>;
     template <Order A, Order B>
-    using Small = MfmaTile<f16x8, 2, 2, A, B, 64, 64, 32, 4, 1, 3>;
+    using Small = MfmaTile<f16x8, 2, 2, A, B, 64, 64, 64, 4, 1, 3>;
 };
 
 // Powers of two that X, A and B are stored times.
@@ -56,13 +56,14 @@ __global__ void __launch_bounds__(256) ns_norm_kernel(const S *g, int64_t ld, in
     const S *src = g + blockIdx.y * stride;
     double s = 0.0;
     const int64_t n = static_cast<int64_t>(rows) * cols;
-    const bool flat = ld == cols && n % 4 == 0 && (reinterpret_cast<uintptr_t>(src) & (4 * sizeof(S) - 1)) == 0;
-    if (flat) {
-        for (int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; t < n / 4; t += static_cast<int64_t>(gridDim.x) * 256) {
-            struct alignas(4 * sizeof(S)) Four { S v[4]; };
-            const Four q = *reinterpret_cast<const Four *>(src + t * 4);
+    constexpr int E = 16 / sizeof(S);
+    if (ld == cols && n % E == 0 && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+        struct alignas(16) Piece { S v[E]; };
+#pragma unroll 4
+        for (int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; t < n / E; t += static_cast<int64_t>(gridDim.x) * 256) {
+            const Piece q = reinterpret_cast<const Piece *>(src)[t];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < E; ++k) {
                 const double v = static_cast<float>(q.v[k]);
                 s = __builtin_fma(v, v, s);
             }
@@ -173,17 +174,23 @@ __global__ void __launch_bounds__(T::NT, 2) ns_symmetric_kernel(const uint16_t *
     const int nt = id - mt * (mt + 1) / 2;
     const uint16_t *src = in + blockIdx.y * in_stride;
     uint16_t *dst = out + blockIdx.y * out_stride;
-    f32x4 acc[T::MI][T::NI];
-    const Planes p{src, ld, plane};
-    T::run(p, mt * T::BM, mp, p, nt * T::BN, mp, 0, steps, smem, acc);
     const int64_t m0 = mt * T::BM, n = nt * T::BN + T::col_of();
+    f32x4 early[4];         // small tiles have the registers to ask for A beforehand
+    if constexpr (POLY && T::MI == 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) early[e] = read4(src + (m0 + T::row_of(0) + e) * mp + n, plane, T::PA);
+    f32x4 acc[T::MI][T::NI];
+    T::clear(acc);
+    const Planes p{src, ld, plane};
+    T::run(p, m0, mp, p, nt * T::BN, mp, 0, steps, smem, acc);
 #pragma unroll
     for (int i = 0; i < T::MI; ++i) {
         const int64_t m = m0 + T::row_of(i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             f32x4 v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]}, old = {0, 0, 0, 0};
-            if constexpr (POLY) old = read4(src + (m + e) * mp + n, plane, T::PA);
+            if constexpr (POLY && T::MI == 1) old = early[e];
+            else if constexpr (POLY) old = read4(src + (m + e) * mp + n, plane, T::PA);
 #pragma unroll
             for (int j = 0; j < T::NI; ++j) acc[i][j][e] = v[j] = POLY ? __builtin_fmaf(beta, old[j], alpha * v[j]) : alpha * v[j];
             write4<T::PA>(dst + (m + e) * mp + n, out_plane, v);
@@ -216,7 +223,19 @@ __global__ void __launch_bounds__(T::NT, 2) ns_apply_kernel(Apply p)
     const int64_t z = blockIdx.y, plane = static_cast<int64_t>(p.mp) * p.np;
     const uint16_t *x = p.x + z * p.x_stride;
     const Planes px{x, p.np, plane}, pb{p.b + z * p.b_stride, p.mp, static_cast<int64_t>(p.mp) * p.mp};
-    f32x4 acc[T::MI][T::NI];
+    f32x4 acc[T::MI][T::NI];        // begins with beta / alpha X: read while the first operands are on their way
+    const float begin = p.beta / p.alpha;
+#pragma unroll
+    for (int i = 0; i < T::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < T::NI; ++j) {
+            const int64_t m = static_cast<int64_t>(mt) * T::BM + T::row_of(i), n = static_cast<int64_t>(nt) * T::BN + T::col_of(j);
+            if constexpr (TURN) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = begin * (half_of(x[plane + (m + e) * p.np + n]) + half_of(x[(m + e) * p.np + n]));
+            } else
+                acc[i][j] = begin * read4(x + n * p.np + m, plane, 2);
+        }
     T::run(TURN ? pb : px, mt * T::BM, TURN ? p.mp : p.np, TURN ? px : pb, nt * T::BN, TURN ? p.np : p.mp, 0, p.mp / T::BK, smem, acc, p.mp);
     const bool vec = p.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(static_cast<O *>(p.out) + z * p.out_stride) & (4 * sizeof(O) - 1)) == 0;
 #pragma unroll
@@ -225,15 +244,7 @@ __global__ void __launch_bounds__(T::NT, 2) ns_apply_kernel(Apply p)
 #pragma unroll
         for (int j = 0; j < T::NI; ++j) {
             const int64_t n = static_cast<int64_t>(nt) * T::BN + T::col_of(j);
-            f32x4 old;
-            if constexpr (TURN) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) old[e] = half_of(x[plane + (m + e) * p.np + n]) + half_of(x[(m + e) * p.np + n]);
-            } else
-                old = read4(x + n * p.np + m, plane, 2);
-            f32x4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(p.beta, old[e], p.alpha * acc[i][j][e]);
+            const f32x4 v = p.alpha * acc[i][j];
             if (TURN || p.out) {
                 if (n < p.out_rows && m < p.out_cols)
                     store4(static_cast<O *>(p.out) + z * p.out_stride + n * p.out_ld + m, v, static_cast<int>(p.out_cols - m), vec);
@@ -475,10 +486,10 @@ dol_status newton_schulz(const Layout &L, const dol_matrix *g, int64_t g_stride,
                                                                       L.mp, L.np);
     DOL_HIP(hipGetLastError());
     auto two = [](int n) { return std::ldexp(1.0f, n); };
-    // the largest tiles that fill the chip
+    // the largest tiles that fill the chip: of 256 x 256 half of it (a unit takes one), of 128 x 128 all of it (two)
     auto size_of = [&](int64_t rows, int64_t cols, bool half) {
-        auto fills = [&](int t) { return rows % t == 0 && cols % t == 0 && rows / t * (cols / t) * batch >= (half ? 2 : 1) * kUnits * 3 / 4; };
-        return fills(256) ? 2 : fills(128) ? 1 : rows % 128 == 0 && cols % 128 == 0 && rows * cols * batch >= 128 * 128 * 64 ? 1 : 0;
+        auto many = [&](int t) { return rows % t || cols % t ? 0 : (half ? rows / t * (rows / t + 1) / 2 : rows / t * (cols / t)) * batch; };
+        return many(256) >= kUnits / 2 ? 2 : many(128) >= 2 * kUnits ? 1 : 0;
     };
     for (int32_t t = 0; t < steps; ++t) {
         const int from = t & 1;
