@@ -69,8 +69,21 @@ __device__ __forceinline__ float act_of(float z, float *slope)
         if (SLOPE) *slope = s * __builtin_fmaf(z, 1.0f - s, 1.0f);
         return z * s;
     } else if constexpr (ACT == DOL_ACT_GELU) {
-        const float cdf = __builtin_fmaf(0.5f, erff(z * 0.70710678118654752440f), 0.5f);
-        if (SLOPE) *slope = __builtin_fmaf(z * 0.39894228040143267794f, __builtin_amdgcn_exp2f(z * z * -0.72134752044448170368f), cdf);
+        // Phi(-|z|) = exp(-z^2 / 2) t q(t), t = 1 / (1 + 0.3 |z| / sqrt 2): a polynomial fitted to erfcx(x) / t, off by 4e-8 of it at most
+        // up to |z| = 19, where the exponential has vanished; the slope has the same exponential.  (The library's erff takes twice as long.)
+        const float bell = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170368f);
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.21213203435596425732f, 1.0f));
+        float q = -0.063308546f;
+        q = __builtin_fmaf(q, t, 0.23591424f);
+        q = __builtin_fmaf(q, t, -0.242347969f);
+        q = __builtin_fmaf(q, t, 0.258526498f);
+        q = __builtin_fmaf(q, t, -0.0370258253f);
+        q = __builtin_fmaf(q, t, 0.103193045f);
+        q = __builtin_fmaf(q, t, 0.0752343293f);
+        q = __builtin_fmaf(q, t, 0.0852118725f);
+        q = __builtin_fmaf(q, t, 0.084602376f);
+        const float tail = q * t * bell, cdf = z < 0.0f ? tail : 1.0f - tail;
+        if (SLOPE) *slope = __builtin_fmaf(z * 0.39894228040143267794f, bell, cdf);
         return z * cdf;
     } else if constexpr (ACT == DOL_ACT_RELU) {
         if (SLOPE) *slope = z > 0.0f ? 1.0f : z == z ? 0.0f : z;
@@ -114,12 +127,32 @@ __device__ __forceinline__ Place place_of(int slice)
     return p;
 }
 
+// The sum of n values `step` floats apart, eight of them on their way at a time.
+__device__ __forceinline__ float sum_strided(const float *p, int n, int step)
+{
+    float s[2] = {0.0f, 0.0f};
+    int k = 0;
+    for (; k + 8 <= n; k += 8) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = p[(k + e) * step];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e & 1] += v[e];
+    }
+    float v[7];
+#pragma unroll
+    for (int e = 0; e < 7; ++e) v[e] = k + e < n ? p[(k + e) * step] : 0.0f;
+#pragma unroll
+    for (int e = 0; e < 7; ++e) s[e & 1] += v[e];
+    return s[0] + s[1];
+}
+
 // Threads' sums of their channels over the rows of the workgroup, for Q quantities: to[q * slice + c] afterwards, for all threads.
-// buf: Q * (rows * slice + threads) floats, `to` apart from it.
+// buf: Q * (rows * slice + threads) floats, `to` apart from it.  A channel's rows are summed in shares of some eight and these in turn.
 template <int V, int Q>
 __device__ __forceinline__ void sum_rows(const float (&s)[Q][V], const Place &p, int slice, float *buf, float *to)
 {
-    const int size = p.rows * slice, shares = max(1, min(p.rows, static_cast<int>(blockDim.x) / slice));
+    const int size = p.rows * slice, shares = max(1, min((p.rows + 7) / 8, static_cast<int>(blockDim.x) / slice));
     float *mid = buf + Q * size;
     if (p.in)
 #pragma unroll
@@ -131,33 +164,61 @@ __device__ __forceinline__ void sum_rows(const float (&s)[Q][V], const Place &p,
         const int share = threadIdx.x / slice, c = threadIdx.x - share * slice;
         if (share < shares)
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                float x = 0.0f;
-                for (int r = share; r < p.rows; r += shares) x += buf[q * size + r * slice + c];
-                mid[q * blockDim.x + threadIdx.x] = x;
-            }
+            for (int q = 0; q < Q; ++q)
+                mid[q * blockDim.x + threadIdx.x] = sum_strided(buf + q * size + share * slice + c, (p.rows - share + shares - 1) / shares, shares * slice);
         lds_barrier();
         for (int t = threadIdx.x; t < Q * slice; t += blockDim.x) {
             const int q = t / slice, ch = t - q * slice;
-            float x = 0.0f;
-            for (int k = 0; k < shares; ++k) x += mid[q * blockDim.x + k * slice + ch];
-            to[t] = x;
+            to[t] = sum_strided(mid + q * blockDim.x + ch, shares, slice);
         }
     } else
         for (int t = threadIdx.x; t < Q * slice; t += blockDim.x) {
             const int q = t / slice, ch = t - q * slice;
-            float x = 0.0f;
-            for (int r = 0; r < p.rows; ++r) x += buf[q * size + r * slice + ch];
-            to[t] = x;
+            to[t] = sum_strided(buf + q * size + ch, p.rows, slice);
         }
     lds_barrier();
 }
+
+// The group, from the slice's first, of each of the channels lane * V ..: one division, for a division takes some thirty instructions.
+template <int V>
+__device__ __forceinline__ void groups_of(int (&g)[V], const Place &p, int per)
+{
+    int at = p.lane * V / per, rest = p.lane * V - at * per;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        g[v] = at;
+        if (++rest == per) rest = 0, ++at;
+    }
+}
+
+constexpr int kFewChannels = 16;    // of a group: summed by a thread, and by a wavefront above
 
 __device__ __forceinline__ float sum_of_wave(float x)
 {
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
     return x;
+}
+
+// done(g, sum over the channels c of a group of value(g, c)) for g below n.
+template <typename F, typename D>
+__device__ __forceinline__ void each_group(int n, int per, F value, D done)
+{
+    if (per <= kFewChannels) {
+        for (int g = threadIdx.x; g < n; g += blockDim.x) {
+            float t = 0.0f;
+#pragma unroll 4
+            for (int c = 0; c < per; ++c) t += value(g, c);
+            done(g, t);
+        }
+        return;
+    }
+    for (int g = threadIdx.x >> 6; g < n; g += blockDim.x >> 6) {
+        float t = 0.0f;
+        for (int c = threadIdx.x & 63; c < per; c += 64) t += value(g, c);
+        t = sum_of_wave(t);
+        if ((threadIdx.x & 63) == 0) done(g, t);
+    }
 }
 
 // ---------------------------------------------------------------- slabs
@@ -172,74 +233,65 @@ __global__ void __launch_bounds__(kSlabThreads) group_norm_slab_forward_kernel(S
     const Place p = place_of<V>(s.slice);
     float *sums = lds, *gmean = sums + s.slice, *grstd = gmean + groups, *buf = grstd + groups;
     const float count = static_cast<float>(s.points) * static_cast<float>(s.per);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    const T *src = x.at<T>(b, 0, c0 + p.lane * V);
+    const T *src = x.at<T>(b, p.row, c0 + p.lane * V);
+    const int64_t step = p.rows * x.ld_point;
+    const int have = p.in && p.row < s.points ? (s.points - p.row + p.rows - 1) / p.rows : 0;        // vectors of this thread
     Vec<T, V> in[K];
-    float sum[1][V] = {};
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int64_t pt = p.row + static_cast<int64_t>(k) * p.rows;
-        if (p.in && pt < s.points) in[k] = *reinterpret_cast<const Vec<T, V> *>(src + pt * x.ld_point);
-    }
+    float sum[1][V] = {}, f[V], o[V];
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (p.in && p.row + static_cast<int64_t>(k) * p.rows < s.points)
+        if (k < have) in[k] = *reinterpret_cast<const Vec<T, V> *>(src + k * step);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = c0 + p.lane * V + v;
+        f[v] = p.in && gamma ? gamma[c] : 1.0f, o[v] = p.in && beta ? beta[c] : 0.0f;
+    }
+    int gi[V];
+    groups_of(gi, p, s.per);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (k < have)
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[0][v] += in[k].get(v);
     sum_rows<V, 1>(sum, p, s.slice, buf, sums);
-    for (int g = wave; g < groups; g += waves) {
-        float t = 0.0f;
-        for (int c = lane; c < s.per; c += 64) t += sums[g * s.per + c];
-        t = sum_of_wave(t);
-        if (lane == 0) gmean[g] = t / count;
-    }
+    each_group(groups, s.per, [&](int g, int c) { return sums[g * s.per + c]; }, [&](int g, float t) { gmean[g] = t / count; });
     lds_barrier();
     float m[V], sq[1][V] = {};
 #pragma unroll
-    for (int v = 0; v < V; ++v) m[v] = p.in ? gmean[(p.lane * V + v) / s.per] : 0.0f;
+    for (int v = 0; v < V; ++v) m[v] = p.in ? gmean[gi[v]] : 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (p.in && p.row + static_cast<int64_t>(k) * p.rows < s.points)
+        if (k < have)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float d = in[k].get(v) - m[v];
                 sq[0][v] = __builtin_fmaf(d, d, sq[0][v]);
             }
     sum_rows<V, 1>(sq, p, s.slice, buf, sums);
-    for (int g = wave; g < groups; g += waves) {
-        float t = 0.0f;
-        for (int c = lane; c < s.per; c += 64) t += sums[g * s.per + c];
-        t = sum_of_wave(t);
-        if (lane == 0) {
-            const float r = 1.0f / sqrtf(t / count + eps);
-            grstd[g] = r;
-            const int64_t at = static_cast<int64_t>(b) * s.groups + c0 / s.per + g;
-            if (mean) mean[at] = gmean[g];
-            if (rstd) rstd[at] = r;
-        }
-    }
+    each_group(groups, s.per, [&](int g, int c) { return sums[g * s.per + c]; }, [&](int g, float t) {
+        const float r = 1.0f / sqrtf(t / count + eps);
+        grstd[g] = r;
+        const int64_t at = static_cast<int64_t>(b) * s.groups + c0 / s.per + g;
+        if (mean) mean[at] = gmean[g];
+        if (rstd) rstd[at] = r;
+    });
     lds_barrier();
-    if (!p.in) return;
-    float f[V], o[V];
+    if (have == 0) return;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int c = p.lane * V + v;
-        f[v] = grstd[c / s.per] * (gamma ? gamma[c0 + c] : 1.0f), o[v] = beta ? beta[c0 + c] : 0.0f;
-    }
-    T *dst = y.at<T>(b, 0, c0 + p.lane * V);
+    for (int v = 0; v < V; ++v) f[v] *= grstd[gi[v]];
+    T *dst = y.at<T>(b, p.row, c0 + p.lane * V);
+    const int64_t out_step = p.rows * y.ld_point;
     with_act(act, [&](auto A) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int64_t pt = p.row + static_cast<int64_t>(k) * p.rows;
-            if (pt < s.points) {
+        for (int k = 0; k < K; ++k)
+            if (k < have) {
                 Vec<T, V> out;
                 float z[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) z[v] = act_of<decltype(A)::value, false>(__builtin_fmaf(in[k].get(v) - m[v], f[v], o[v]), nullptr);
                 out.set(z);
-                *reinterpret_cast<Vec<T, V> *>(dst + pt * y.ld_point) = out;
+                *reinterpret_cast<Vec<T, V> *>(dst + k * out_step) = out;
             }
-        }
     });
 }
 
@@ -254,29 +306,30 @@ __global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_ker
     const Place p = place_of<V>(s.slice);
     float *sums = lds, *c12 = sums + 2 * s.slice, *buf = c12 + 2 * groups;
     const float count = static_cast<float>(s.points) * static_cast<float>(s.per);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    const T *src = x.at<T>(b, 0, c0 + p.lane * V), *up = dy.at<T>(b, 0, c0 + p.lane * V);
+    const T *src = x.at<T>(b, p.row, c0 + p.lane * V), *up = dy.at<T>(b, p.row, c0 + p.lane * V);
+    const int64_t step = p.rows * x.ld_point, up_step = p.rows * dy.ld_point;
+    const int have = p.in && p.row < s.points ? (s.points - p.row + p.rows - 1) / p.rows : 0;
     Vec<T, V> in[K], gr[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int64_t pt = p.row + static_cast<int64_t>(k) * p.rows;
-        if (p.in && pt < s.points) {
-            in[k] = *reinterpret_cast<const Vec<T, V> *>(src + pt * x.ld_point);
-            gr[k] = *reinterpret_cast<const Vec<T, V> *>(up + pt * dy.ld_point);
+    for (int k = 0; k < K; ++k)
+        if (k < have) {
+            in[k] = *reinterpret_cast<const Vec<T, V> *>(src + k * step);
+            gr[k] = *reinterpret_cast<const Vec<T, V> *>(up + k * up_step);
         }
-    }
-    float m[V], f[V], o[V], sum[2][V] = {}, dz[K][V];        // z = (x - m) f + o
+    int gi[V];
+    groups_of(gi, p, s.per);
+    float m[V], r[V], f[V], o[V], sum[2][V] = {}, dz[K][V];        // z = (x - m) f + o
     if (p.in)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = c0 + p.lane * V + v;
-            const int64_t g = static_cast<int64_t>(b) * s.groups + c / s.per;
-            m[v] = mean[g], f[v] = gamma ? rstd[g] * gamma[c] : rstd[g], o[v] = beta ? beta[c] : 0.0f;
+            const int64_t g = static_cast<int64_t>(b) * s.groups + c0 / s.per + gi[v];
+            m[v] = mean[g], r[v] = rstd[g], f[v] = gamma ? r[v] * gamma[c] : r[v], o[v] = beta ? beta[c] : 0.0f;
         }
     with_act(act, [&](auto A) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (p.in && p.row + static_cast<int64_t>(k) * p.rows < s.points)
+            if (k < have)
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const float d = in[k].get(v) - m[v];
@@ -288,7 +341,7 @@ __global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_ker
     });
     if (p.in)               // of dz xhat
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[1][v] *= rstd[static_cast<int64_t>(b) * s.groups + (c0 + p.lane * V + v) / s.per];
+        for (int v = 0; v < V; ++v) sum[1][v] *= r[v];
     sum_rows<V, 2>(sum, p, s.slice, buf, sums);
     if (sums_out)
         for (int t = threadIdx.x; t < 2 * s.slice; t += blockDim.x) {
@@ -296,35 +349,30 @@ __global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_ker
             sums_out[(static_cast<int64_t>(q) * s.batch + b) * s.channels + c0 + c] = sums[t];
         }
     if (!dx.data) return;
-    for (int t = wave; t < 2 * groups; t += waves) {
-        const int q = t / groups, g = t - q * groups;
-        float a = 0.0f;
-        for (int c = lane; c < s.per; c += 64) a = __builtin_fmaf(sums[q * s.slice + g * s.per + c], gamma ? gamma[c0 + g * s.per + c] : 1.0f, a);
-        a = sum_of_wave(a);
-        if (lane == 0) c12[t] = a / count;
-    }
+    each_group(
+        2 * groups, s.per,
+        [&](int t, int c) {
+            const int q = t >= groups, ch = (t - q * groups) * s.per + c;
+            return gamma ? sums[q * s.slice + ch] * gamma[c0 + ch] : sums[q * s.slice + ch];
+        },
+        [&](int t, float a) { c12[t] = a / count; });
     lds_barrier();
-    if (!p.in) return;
-    T *dst = dx.at<T>(b, 0, c0 + p.lane * V);
+    if (have == 0) return;
+    T *dst = dx.at<T>(b, p.row, c0 + p.lane * V);
+    const int64_t out_step = p.rows * dx.ld_point;
     float k1[V], k2[V];     // rstd c1, rstd^2 c2
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int g = (p.lane * V + v) / s.per;
-        const float r = rstd[static_cast<int64_t>(b) * s.groups + c0 / s.per + g];
-        k1[v] = r * c12[g], k2[v] = r * r * c12[groups + g];
-    }
+    for (int v = 0; v < V; ++v) k1[v] = r[v] * c12[gi[v]], k2[v] = r[v] * r[v] * c12[groups + gi[v]];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int64_t pt = p.row + static_cast<int64_t>(k) * p.rows;
-        if (pt < s.points) {
+    for (int k = 0; k < K; ++k)
+        if (k < have) {
             Vec<T, V> out;
             float g[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) g[v] = __builtin_fmaf(f[v], dz[k][v], -__builtin_fmaf(in[k].get(v) - m[v], k2[v], k1[v]));
             out.set(g);
-            *reinterpret_cast<Vec<T, V> *>(dst + pt * dx.ld_point) = out;
+            *reinterpret_cast<Vec<T, V> *>(dst + k * out_step) = out;
         }
-    }
 }
 
 // grad_beta, grad_gamma = the samples' sums added up; sixty-four channels to a workgroup, a share of the samples to each wavefront.
@@ -619,11 +667,12 @@ Plan plan_of(const dol_activations *x, int32_t groups, int vec, bool backward)
     Shape &s = p.s;
     s.batch = x->batch, s.points = x->points, s.channels = x->channels, s.groups = groups, s.per = x->channels / groups;
     const int e = x->dtype == DOL_F32 ? 4 : 2;
-    // A slab is a set of whole groups, in whole vectors, of at least 32 bytes to a point (below, a line of memory is shared by too many
-    // workgroups).  Wider ones are taken up to 64 bytes while there is a workgroup for every compute unit, and beyond while there are four.
+    // A slab is a set of whole groups, in whole vectors, of at least 16 bytes to a point.  Wider ones are taken up to 64 bytes while there
+    // are two workgroups to a compute unit, and beyond while there are four.  (A line of memory is then shared by slabs of one sample, which
+    // run on one XCD, at the same time.)
     for (int k = 1; k <= groups; ++k) {
         const int64_t slice = int64_t(k) * s.per, lanes = slice / vec;
-        if (groups % k || slice % vec || (slice * e < 32 && k < groups)) continue;
+        if (groups % k || slice % vec || (slice * e < 16 && k < groups)) continue;
         int vecs = kFewVecs;
         int64_t threads = round_up((s.points + vecs - 1) / int64_t(vecs) * lanes, 64);
         if (threads > kSlabThreads / 2) {
@@ -632,7 +681,7 @@ Plan plan_of(const dol_activations *x, int32_t groups, int vec, bool backward)
             if (threads > (backward ? kSlabThreadsBack : kSlabThreads)) break;
         }
         const int64_t workgroups = int64_t(s.batch) * (groups / k);
-        if (p.threads && !(workgroups >= 4 * kUnits || (int64_t(s.slice) * e < 64 && workgroups >= kUnits))) break;
+        if (p.threads && !(workgroups >= 4 * kUnits || (int64_t(s.slice) * e < 64 && workgroups >= 2 * kUnits))) break;
         p.vecs = vecs, p.threads = static_cast<int>(threads), s.slice = static_cast<int32_t>(slice), s.slices = groups / k;
     }
     if (p.threads) {
