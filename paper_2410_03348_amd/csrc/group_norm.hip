@@ -50,6 +50,8 @@ struct Vec<__bf16, 1> {
 struct Shape {
     int32_t batch, points, channels, groups, per;       // per: channels of a group
     int32_t slice, slices;                              // channels that a workgroup takes; how many such
+    int32_t lanes, rows;                                // threads to a point of the slice; points that a workgroup takes at a time
+    float count, per_lanes, per_per, per_count;         // a group's elements; reciprocals of lanes, per and count
     int32_t chunk, chunks;                              // points that a workgroup of the shared-out form takes; how many such
 };
 
@@ -109,115 +111,74 @@ __device__ __forceinline__ void with_act(int act, F f)
     else f(Act<DOL_ACT_NONE>());
 }
 
+// t / count to the last bit or so: the product with the reciprocal, and what it is off by.
+__device__ __forceinline__ float mean_of(float t, const Shape &s)
+{
+    const float m = t * s.per_count;
+    return __builtin_fmaf(__builtin_fmaf(-m, s.count, t), s.per_count, m);
+}
+
+__device__ __forceinline__ float rstd_of(float var, float eps) { return 1.0f / __builtin_amdgcn_sqrtf(var + eps); }
+
 // ---------------------------------------------------------------- sums over the threads of a workgroup
+
+// A workgroup of a small tensor runs its code once, and waits for every line of it: divisions are made of the host's reciprocals, and
+// the sums are loops (written out they took 3 400 of a workgroup's 16 800 clocks at 784 x 4 floats, each of the two).
 
 // Where a thread stands in a slab or a chunk: `lanes` threads of V channels make a row of the slice, `rows` such rows the workgroup.
 struct Place {
-    int lanes, rows, lane, row;
+    int rows, lane, row;
     bool in;
 };
 
-template <int V>
-__device__ __forceinline__ Place place_of(int slice)
+// floor(x / d) for x below 8192 and r = 1 / d rounded: (x + 1/2) / d is at least 1 / (2 d) from the next whole number.
+__device__ __forceinline__ int small_quotient(int x, float r) { return static_cast<int>((static_cast<float>(x) + 0.5f) * r); }
+
+__device__ __forceinline__ Place place_of(const Shape &s)
 {
     Place p;
-    p.lanes = slice / V, p.rows = blockDim.x / p.lanes;
-    p.row = threadIdx.x / p.lanes, p.lane = threadIdx.x - p.row * p.lanes;
-    p.in = p.row < p.rows;
+    p.rows = s.rows, p.row = small_quotient(threadIdx.x, s.per_lanes);
+    p.lane = threadIdx.x - p.row * s.lanes, p.in = p.row < p.rows;
     return p;
 }
 
-// The sum of n values `step` floats apart, eight of them on their way at a time.
-__device__ __forceinline__ float sum_strided(const float *p, int n, int step)
-{
-    float s[2] = {0.0f, 0.0f};
-    int k = 0;
-    for (; k + 8 <= n; k += 8) {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = p[(k + e) * step];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e & 1] += v[e];
-    }
-    float v[7];
-#pragma unroll
-    for (int e = 0; e < 7; ++e) v[e] = k + e < n ? p[(k + e) * step] : 0.0f;
-#pragma unroll
-    for (int e = 0; e < 7; ++e) s[e & 1] += v[e];
-    return s[0] + s[1];
-}
+__device__ __forceinline__ float sum_of_wave(float x) { return with_lane32<AddOp>(reduce32<AddOp>(x)); }
 
-// Threads' sums of their channels over the rows of the workgroup, for Q quantities: to[q * slice + c] afterwards, for all threads.
-// buf: Q * (rows * slice + threads) floats, `to` apart from it.  A channel's rows are summed in shares of some eight and these in turn.
+// Threads' values of their channels, for Q quantities, to buf[q * size + row * pitch + channel], pitch odd.
 template <int V, int Q>
-__device__ __forceinline__ void sum_rows(const float (&s)[Q][V], const Place &p, int slice, float *buf, float *to)
+__device__ __forceinline__ void put_rows(const float (&s)[Q][V], const Place &p, int pitch, float *buf)
 {
-    const int size = p.rows * slice, shares = max(1, min((p.rows + 7) / 8, static_cast<int>(blockDim.x) / slice));
-    float *mid = buf + Q * size;
     if (p.in)
 #pragma unroll
         for (int q = 0; q < Q; ++q)
 #pragma unroll
-            for (int v = 0; v < V; ++v) buf[q * size + p.row * slice + p.lane * V + v] = s[q][v];
-    lds_barrier();
-    if (shares > 1) {
-        const int share = threadIdx.x / slice, c = threadIdx.x - share * slice;
-        if (share < shares)
-#pragma unroll
-            for (int q = 0; q < Q; ++q)
-                mid[q * blockDim.x + threadIdx.x] = sum_strided(buf + q * size + share * slice + c, (p.rows - share + shares - 1) / shares, shares * slice);
-        lds_barrier();
-        for (int t = threadIdx.x; t < Q * slice; t += blockDim.x) {
-            const int q = t / slice, ch = t - q * slice;
-            to[t] = sum_strided(mid + q * blockDim.x + ch, shares, slice);
-        }
-    } else
-        for (int t = threadIdx.x; t < Q * slice; t += blockDim.x) {
-            const int q = t / slice, ch = t - q * slice;
-            to[t] = sum_strided(buf + q * size + ch, p.rows, slice);
-        }
+            for (int v = 0; v < V; ++v) buf[(q * p.rows + p.row) * pitch + p.lane * V + v] = s[q][v];
     lds_barrier();
 }
 
-// The group, from the slice's first, of each of the channels lane * V ..: one division, for a division takes some thirty instructions.
-template <int V>
-__device__ __forceinline__ void groups_of(int (&g)[V], const Place &p, int per)
+// The sum of a block of rows x columns values, taken by a wavefront; the same in all lanes.
+__device__ __forceinline__ float sum_block(const float *buf, int rows, int pitch, int columns)
 {
-    int at = p.lane * V / per, rest = p.lane * V - at * per;
+    const int lane = threadIdx.x & 63;
+    const bool along = rows >= columns;
+    const int outer = along ? columns : rows, inner = along ? rows : columns, step = along ? pitch : 1, stride = along ? 1 : pitch;
+    float t = 0.0f;
+#pragma unroll 1
+    for (int k = 0; k < outer; ++k)
+#pragma unroll 2
+        for (int e = lane; e < inner; e += 64) t += buf[k * stride + e * step];
+    return sum_of_wave(t);
+}
+
+// The group, from the slice's first, of each of the channels lane * V ..
+template <int V>
+__device__ __forceinline__ void groups_of(int (&g)[V], const Place &p, const Shape &s)
+{
+    int at = small_quotient(p.lane * V, s.per_per), rest = p.lane * V - at * s.per;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         g[v] = at;
-        if (++rest == per) rest = 0, ++at;
-    }
-}
-
-constexpr int kFewChannels = 16;    // of a group: summed by a thread, and by a wavefront above
-
-__device__ __forceinline__ float sum_of_wave(float x)
-{
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-    return x;
-}
-
-// done(g, sum over the channels c of a group of value(g, c)) for g below n.
-template <typename F, typename D>
-__device__ __forceinline__ void each_group(int n, int per, F value, D done)
-{
-    if (per <= kFewChannels) {
-        for (int g = threadIdx.x; g < n; g += blockDim.x) {
-            float t = 0.0f;
-#pragma unroll 4
-            for (int c = 0; c < per; ++c) t += value(g, c);
-            done(g, t);
-        }
-        return;
-    }
-    for (int g = threadIdx.x >> 6; g < n; g += blockDim.x >> 6) {
-        float t = 0.0f;
-        for (int c = threadIdx.x & 63; c < per; c += 64) t += value(g, c);
-        t = sum_of_wave(t);
-        if ((threadIdx.x & 63) == 0) done(g, t);
+        if (++rest == s.per) rest = 0, ++at;
     }
 }
 
@@ -229,54 +190,56 @@ __global__ void __launch_bounds__(kSlabThreads) group_norm_slab_forward_kernel(S
 {
     extern __shared__ __align__(16) float lds[];
     const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int b = id / s.slices, c0 = (id - b * s.slices) * s.slice, groups = s.slice / s.per;
-    const Place p = place_of<V>(s.slice);
-    float *sums = lds, *gmean = sums + s.slice, *grstd = gmean + groups, *buf = grstd + groups;
-    const float count = static_cast<float>(s.points) * static_cast<float>(s.per);
+    const int b = id / s.slices, sl = id - b * s.slices, c0 = sl * s.slice, groups = s.groups / s.slices, pitch = s.slice | 1;
+    const int64_t g0 = static_cast<int64_t>(b) * s.groups + sl * groups;
+    const Place p = place_of(s);
+    float *gmean = lds, *grstd = gmean + groups, *buf = grstd + groups;
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const T *src = x.at<T>(b, p.row, c0 + p.lane * V);
     const int64_t step = p.rows * x.ld_point;
-    const int have = p.in && p.row < s.points ? (s.points - p.row + p.rows - 1) / p.rows : 0;        // vectors of this thread
+    const int left = p.in ? s.points - p.row : 0;           // vector k is there where k * rows < left
     Vec<T, V> in[K];
     float sum[1][V] = {}, f[V], o[V];
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (k < have) in[k] = *reinterpret_cast<const Vec<T, V> *>(src + k * step);
+        if (k * p.rows < left) in[k] = *reinterpret_cast<const Vec<T, V> *>(src + k * step);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int c = c0 + p.lane * V + v;
         f[v] = p.in && gamma ? gamma[c] : 1.0f, o[v] = p.in && beta ? beta[c] : 0.0f;
     }
     int gi[V];
-    groups_of(gi, p, s.per);
+    groups_of(gi, p, s);
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (k < have)
+        if (k * p.rows < left)
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[0][v] += in[k].get(v);
-    sum_rows<V, 1>(sum, p, s.slice, buf, sums);
-    each_group(groups, s.per, [&](int g, int c) { return sums[g * s.per + c]; }, [&](int g, float t) { gmean[g] = t / count; });
+    put_rows<V, 1>(sum, p, pitch, buf);
+#pragma unroll 1
+    for (int g = wave; g < groups; g += waves) gmean[g] = mean_of(sum_block(buf + g * s.per, p.rows, pitch, s.per), s);
     lds_barrier();
     float m[V], sq[1][V] = {};
 #pragma unroll
     for (int v = 0; v < V; ++v) m[v] = p.in ? gmean[gi[v]] : 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (k < have)
+        if (k * p.rows < left)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float d = in[k].get(v) - m[v];
                 sq[0][v] = __builtin_fmaf(d, d, sq[0][v]);
             }
-    sum_rows<V, 1>(sq, p, s.slice, buf, sums);
-    each_group(groups, s.per, [&](int g, int c) { return sums[g * s.per + c]; }, [&](int g, float t) {
-        const float r = 1.0f / sqrtf(t / count + eps);
+    put_rows<V, 1>(sq, p, pitch, buf);
+#pragma unroll 1
+    for (int g = wave; g < groups; g += waves) {
+        const float r = rstd_of(sum_block(buf + g * s.per, p.rows, pitch, s.per) * s.per_count, eps);
         grstd[g] = r;
-        const int64_t at = static_cast<int64_t>(b) * s.groups + c0 / s.per + g;
-        if (mean) mean[at] = gmean[g];
-        if (rstd) rstd[at] = r;
-    });
+        if (mean && (threadIdx.x & 63) == 0) mean[g0 + g] = gmean[g];
+        if (rstd && (threadIdx.x & 63) == 0) rstd[g0 + g] = r;
+    }
     lds_barrier();
-    if (have == 0) return;
+    if (left <= 0) return;
 #pragma unroll
     for (int v = 0; v < V; ++v) f[v] *= grstd[gi[v]];
     T *dst = y.at<T>(b, p.row, c0 + p.lane * V);
@@ -284,7 +247,7 @@ __global__ void __launch_bounds__(kSlabThreads) group_norm_slab_forward_kernel(S
     with_act(act, [&](auto A) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (k < have) {
+            if (k * p.rows < left) {
                 Vec<T, V> out;
                 float z[V];
 #pragma unroll
@@ -302,34 +265,35 @@ __global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_ker
 {
     extern __shared__ __align__(16) float lds[];
     const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int b = id / s.slices, c0 = (id - b * s.slices) * s.slice, groups = s.slice / s.per;
-    const Place p = place_of<V>(s.slice);
+    const int b = id / s.slices, sl = id - b * s.slices, c0 = sl * s.slice, groups = s.groups / s.slices, pitch = s.slice | 1;
+    const int64_t g0 = static_cast<int64_t>(b) * s.groups + sl * groups;
+    const Place p = place_of(s);
     float *sums = lds, *c12 = sums + 2 * s.slice, *buf = c12 + 2 * groups;
-    const float count = static_cast<float>(s.points) * static_cast<float>(s.per);
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const T *src = x.at<T>(b, p.row, c0 + p.lane * V), *up = dy.at<T>(b, p.row, c0 + p.lane * V);
     const int64_t step = p.rows * x.ld_point, up_step = p.rows * dy.ld_point;
-    const int have = p.in && p.row < s.points ? (s.points - p.row + p.rows - 1) / p.rows : 0;
+    const int left = p.in ? s.points - p.row : 0;
     Vec<T, V> in[K], gr[K];
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (k < have) {
+        if (k * p.rows < left) {
             in[k] = *reinterpret_cast<const Vec<T, V> *>(src + k * step);
             gr[k] = *reinterpret_cast<const Vec<T, V> *>(up + k * up_step);
         }
     int gi[V];
-    groups_of(gi, p, s.per);
+    groups_of(gi, p, s);
     float m[V], r[V], f[V], o[V], sum[2][V] = {}, dz[K][V];        // z = (x - m) f + o
     if (p.in)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = c0 + p.lane * V + v;
-            const int64_t g = static_cast<int64_t>(b) * s.groups + c0 / s.per + gi[v];
+            const int64_t g = g0 + gi[v];
             m[v] = mean[g], r[v] = rstd[g], f[v] = gamma ? r[v] * gamma[c] : r[v], o[v] = beta ? beta[c] : 0.0f;
         }
     with_act(act, [&](auto A) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (k < have)
+            if (k * p.rows < left)
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const float d = in[k].get(v) - m[v];
@@ -342,22 +306,40 @@ __global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_ker
     if (p.in)               // of dz xhat
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[1][v] *= r[v];
-    sum_rows<V, 2>(sum, p, s.slice, buf, sums);
-    if (sums_out)
+    put_rows<V, 2>(sum, p, pitch, buf);
+    if (p.rows >= 16) {     // a wavefront to a channel, or a thread where there are few rows
+#pragma unroll 1
+        for (int t = wave; t < 2 * s.slice; t += waves) {
+            const int q = t >= s.slice;
+            sums[t] = sum_block(buf + q * p.rows * pitch + t - q * s.slice, p.rows, pitch, 1);
+        }
+    } else
+#pragma unroll 1
         for (int t = threadIdx.x; t < 2 * s.slice; t += blockDim.x) {
-            const int q = t / s.slice, c = t - q * s.slice;
-            sums_out[(static_cast<int64_t>(q) * s.batch + b) * s.channels + c0 + c] = sums[t];
+            const int q = t >= s.slice;
+            const float *from = buf + q * p.rows * pitch + t - q * s.slice;
+            float a = 0.0f;
+#pragma unroll 4
+            for (int k = 0; k < p.rows; ++k) a += from[k * pitch];
+            sums[t] = a;
+        }
+    lds_barrier();
+    if (sums_out)
+#pragma unroll 1
+        for (int t = threadIdx.x; t < 2 * s.slice; t += blockDim.x) {
+            const int q = t >= s.slice;
+            sums_out[(static_cast<int64_t>(q) * s.batch + b) * s.channels + c0 + t - q * s.slice] = sums[t];
         }
     if (!dx.data) return;
-    each_group(
-        2 * groups, s.per,
-        [&](int t, int c) {
-            const int q = t >= groups, ch = (t - q * groups) * s.per + c;
-            return gamma ? sums[q * s.slice + ch] * gamma[c0 + ch] : sums[q * s.slice + ch];
-        },
-        [&](int t, float a) { c12[t] = a / count; });
+#pragma unroll 1
+    for (int t = wave; t < 2 * groups; t += waves) {
+        const int q = t >= groups, ch = (t - q * groups) * s.per;
+        float a = 0.0f;
+        for (int c = threadIdx.x & 63; c < s.per; c += 64) a = __builtin_fmaf(sums[q * s.slice + ch + c], gamma ? gamma[c0 + ch + c] : 1.0f, a);
+        c12[t] = sum_of_wave(a) * s.per_count;
+    }
     lds_barrier();
-    if (have == 0) return;
+    if (left <= 0) return;
     T *dst = dx.at<T>(b, p.row, c0 + p.lane * V);
     const int64_t out_step = p.rows * dx.ld_point;
     float k1[V], k2[V];     // rstd c1, rstd^2 c2
@@ -365,7 +347,7 @@ __global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_ker
     for (int v = 0; v < V; ++v) k1[v] = r[v] * c12[gi[v]], k2[v] = r[v] * r[v] * c12[groups + gi[v]];
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (k < have) {
+        if (k * p.rows < left) {
             Vec<T, V> out;
             float g[V];
 #pragma unroll
@@ -417,7 +399,7 @@ __global__ void __launch_bounds__(kPartThreads) group_norm_part_forward_kernel(S
     __shared__ float red[2][kPartThreads * V];
     __shared__ float counts[kPartThreads];
     const int b = blockIdx.z, c0 = blockIdx.y * s.slice, width = min(s.slice, s.channels - c0);
-    const Place p = place_of<V>(s.slice);
+    const Place p = place_of(s);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * s.chunk, end = min(first + s.chunk, static_cast<int64_t>(s.points));
     const bool in = p.in && p.lane * V < width;
     float mean[V] = {}, m2[V] = {}, have = 0.0f;
@@ -480,13 +462,13 @@ __global__ void __launch_bounds__(256) group_norm_finish_forward_kernel(Shape s,
     float t = 0.0f;
     const int n = s.chunks * s.per;
     for (int k = threadIdx.x; k < n; k += 256) t += p[static_cast<int64_t>(k / s.per) * s.channels + k % s.per].x * points_of(k / s.per);
-    const float count = static_cast<float>(s.points) * static_cast<float>(s.per), m = all(t) / count;
+    const float m = mean_of(all(t), s);
     t = 0.0f;
     for (int k = threadIdx.x; k < n; k += 256) {
         const float2 q = p[static_cast<int64_t>(k / s.per) * s.channels + k % s.per];
         t += __builtin_fmaf((q.x - m) * (q.x - m), points_of(k / s.per), q.y);
     }
-    const float r = 1.0f / sqrtf(all(t) / count + eps);
+    const float r = rstd_of(all(t) * s.per_count, eps);
     if (threadIdx.x == 0) {
         mean[at] = m, rstd[at] = r;
         if (mean_out) mean_out[at] = m;
@@ -500,7 +482,7 @@ __global__ void __launch_bounds__(kPartThreads) group_norm_map_kernel(Shape s, T
                                                                       const float2 *c12, int act, Tensor out)
 {
     const int b = s.batch - 1 - blockIdx.z, c0 = blockIdx.y * s.slice, width = min(s.slice, s.channels - c0);
-    const Place p = place_of<V>(s.slice);
+    const Place p = place_of(s);
     if (!p.in || p.lane * V >= width) return;
     float m[V], r[V], ga[V], be[V], c1[V], c2[V];
 #pragma unroll
@@ -543,10 +525,9 @@ template <typename T, int V>
 __global__ void __launch_bounds__(kPartThreads) group_norm_part_backward_kernel(Shape s, Tensor x, Tensor dy, const float *gamma, const float *beta, const float *mean,
                                                                                 const float *rstd, int act, float2 *part)
 {
-    __shared__ float buf[2 * (kPartThreads * V + kPartThreads)];
-    __shared__ float sums[2 * kPartLanes * V];
+    __shared__ float buf[2 * kPartThreads * (V + 1)];
     const int b = blockIdx.z, c0 = blockIdx.y * s.slice, width = min(s.slice, s.channels - c0);
-    const Place p = place_of<V>(s.slice);
+    const Place p = place_of(s);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * s.chunk, end = min(first + s.chunk, static_cast<int64_t>(s.points));
     float sum[2][V] = {};
     if (p.in && p.lane * V < width) {
@@ -573,9 +554,14 @@ __global__ void __launch_bounds__(kPartThreads) group_norm_part_backward_kernel(
             }
         });
     }
-    sum_rows<V, 2>(sum, p, s.slice, buf, sums);
-    for (int c = threadIdx.x; c < width; c += kPartThreads)
-        part[(static_cast<int64_t>(b) * s.chunks + blockIdx.x) * s.channels + c0 + c] = make_float2(sums[c], sums[s.slice + c]);
+    const int pitch = s.slice | 1;
+    put_rows<V, 2>(sum, p, pitch, buf);
+    for (int c = threadIdx.x; c < width; c += kPartThreads) {
+        float a[2] = {0.0f, 0.0f};
+#pragma unroll 4
+        for (int k = 0; k < p.rows; ++k) a[0] += buf[k * pitch + c], a[1] += buf[(p.rows + k) * pitch + c];
+        part[(static_cast<int64_t>(b) * s.chunks + blockIdx.x) * s.channels + c0 + c] = make_float2(a[0], a[1]);
+    }
 }
 
 // Joins a group's parts: its channels' sums over the sample (sums as group_norm_slab_backward_kernel leaves them) and c1, c2.
@@ -600,8 +586,7 @@ __global__ void __launch_bounds__(256) group_norm_finish_backward_kernel(Shape s
     if (lane == 0) red[0][w] = c1, red[1][w] = c2;
     __syncthreads();
     if (threadIdx.x == 0) {
-        const float count = static_cast<float>(s.points) * static_cast<float>(s.per);
-        c12[at] = make_float2(((red[0][0] + red[0][1]) + (red[0][2] + red[0][3])) / count, ((red[1][0] + red[1][1]) + (red[1][2] + red[1][3])) / count);
+        c12[at] = make_float2(((red[0][0] + red[0][1]) + (red[0][2] + red[0][3])) * s.per_count, ((red[1][0] + red[1][1]) + (red[1][2] + red[1][3])) * s.per_count);
     }
 }
 
@@ -684,15 +669,19 @@ Plan plan_of(const dol_activations *x, int32_t groups, int vec, bool backward)
         if (p.threads && !(workgroups >= 4 * kUnits || (int64_t(s.slice) * e < 64 && workgroups >= 2 * kUnits))) break;
         p.vecs = vecs, p.threads = static_cast<int>(threads), s.slice = static_cast<int32_t>(slice), s.slices = groups / k;
     }
+    s.per_per = 1.0f / static_cast<float>(s.per), s.count = static_cast<float>(s.points) * static_cast<float>(s.per), s.per_count = 1.0f / s.count;
+    auto place = [&](int threads) { s.lanes = s.slice / vec, s.rows = threads / s.lanes, s.per_lanes = 1.0f / static_cast<float>(s.lanes); };
     if (p.threads) {
+        place(p.threads);
         const size_t q = backward ? 2 : 1;
         p.lds = 4 * (q * s.slice + 2 * (s.slice / s.per) + q * p.threads * (vec + 1));
         return p;
     }
     s.slice = std::min<int32_t>(s.channels, kPartLanes * vec);
     s.slices = (s.channels + s.slice - 1) / s.slice;
+    place(kPartThreads);
     // eight workgroups to a compute unit, if that leaves a thread sixteen points
-    const int64_t want = std::max<int64_t>(1, 8 * kUnits / (int64_t(s.batch) * s.slices)), rows = kPartThreads / (s.slice / vec);
+    const int64_t want = std::max<int64_t>(1, 8 * kUnits / (int64_t(s.batch) * s.slices)), rows = s.rows;
     s.chunks = static_cast<int32_t>(std::min(want, (s.points + rows * 16 - 1) / (rows * 16)));
     s.chunk = static_cast<int32_t>((int64_t(s.points) + s.chunks - 1) / s.chunks);
     s.chunks = static_cast<int32_t>((int64_t(s.points) + s.chunk - 1) / s.chunk);
