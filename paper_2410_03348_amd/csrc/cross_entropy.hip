@@ -30,27 +30,27 @@ struct Shapes;
 template <>
 struct Shapes<1, 1> {       // bf16
     using Big = MfmaTile<bf16x8, 1, 1, kRows, kRows, 256, 256, 64, 2, 4, 2>;
-    using Small = MfmaTile<bf16x8, 1, 1, kRows, kRows, 128, 128, 64, 2, 2, 2>;
+    using Small = MfmaTile<bf16x8, 1, 1, kRows, kRows, 128, 128, 64, 4, 2, 2>;
     using BigX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 256, 256, 64, 2, 4, 2>;
     using BigW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 256, 256, 64, 2, 4, 2>;
-    using SmallX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 128, 128, 64, 2, 2, 2>;
-    using SmallW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 128, 128, 64, 2, 2, 2>;
+    using SmallX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 128, 128, 64, 4, 2, 2>;
+    using SmallW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 128, 128, 64, 4, 2, 2>;
 };
 template <>
 struct Shapes<1, 2> : Shapes<1, 1> {
-    using BigX = MfmaTile<bf16x8, 1, 2, kCols, kRows, 128, 128, 32, 2, 2, 2>;
-    using BigW = MfmaTile<bf16x8, 1, 2, kCols, kCols, 128, 128, 32, 2, 2, 2>;
+    using BigX = MfmaTile<bf16x8, 1, 2, kCols, kRows, 128, 128, 32, 4, 2, 2>;
+    using BigW = MfmaTile<bf16x8, 1, 2, kCols, kCols, 128, 128, 32, 4, 2, 2>;
     using SmallX = BigX;
     using SmallW = BigW;
 };
 template <>
 struct Shapes<3, 3> {       // float
     using Big = MfmaTile<bf16x8, 3, 3, kRows, kRows, 128, 256, 32, 2, 4, 2>;
-    using Small = MfmaTile<bf16x8, 3, 3, kRows, kRows, 128, 128, 32, 2, 2, 2>;
+    using Small = MfmaTile<bf16x8, 3, 3, kRows, kRows, 128, 128, 32, 4, 2, 2>;
     using BigX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 128, 256, 32, 2, 4, 2>;
     using BigW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 128, 256, 32, 2, 4, 2>;
-    using SmallX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 128, 128, 32, 2, 2, 2>;
-    using SmallW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 128, 128, 32, 2, 2, 2>;
+    using SmallX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 128, 128, 32, 4, 2, 2>;
+    using SmallW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 128, 128, 32, 4, 2, 2>;
 };
 
 template <int P>
@@ -434,7 +434,7 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
     L.piece = static_cast<int32_t>(round_up((L.classes + L.pieces - 1) / L.pieces, kPad));
     L.pieces = tiles(L.classes, L.piece);
     L.dl = c.take<uint16_t>(Q * L.n_pad * L.piece);
-    L.bias_part = c.take<float>(L.n_pad / 64 * L.piece);
+    L.bias_part = c.take<float>(L.n_pad / 32 * L.piece);
     // Both products of a piece share a launch: their k is split so that the launch has a workgroup of equal length for every place there
     // is, of at least 256 elements of k.
     const int32_t n = std::min(L.piece, L.classes);

@@ -15,7 +15,6 @@
 namespace dol {
 namespace {
 
-constexpr int kPad = 256;           // rows and columns are filled up with zeros, which stay zeros
 constexpr int kNormParts = 1024;    // workgroups that share a matrix's sum of squares, at most
 constexpr int kUnits = 256;
 
@@ -27,7 +26,7 @@ struct Shapes<1> {
     template <Order A, Order B>
     using Big = MfmaTile<f16x8, 1, 1, A, B, 256, 256, 64, 2, 4, 2>;
     template <Order A, Order B>
-    using Mid = MfmaTile<f16x8, 1, 1, A, B, 128, 128, 64, 2, 2, 2>;
+    using Mid = MfmaTile<f16x8, 1, 1, A, B, 128, 128, 64, 4, 2, 2>;
     template <Order A, Order B>
     using Small = MfmaTile<f16x8, 1, 1, A, B, 64, 64, 64, 4, 1, 3>;
 };
@@ -36,7 +35,7 @@ struct Shapes<2> {
     template <Order A, Order B>
     using Big = MfmaTile<f16x8, 2, 2, A, B, 256, 256, 32, 2, 4, 2>;
     template <Order A, Order B>
-    using Mid = MfmaTile<f16x8, 2, 2, A, B, 128, 128, 32, 2, 2, 2>;
+    using Mid = MfmaTile<f16x8, 2, 2, A, B, 128, 128, 32, 4, 2, 2>;
     template <Order A, Order B>
     using Small = MfmaTile<f16x8, 2, 2, A, B, 64, 64, 64, 4, 1, 3>;
 };
@@ -393,7 +392,8 @@ Layout lay_out(const dol_matrix *g, int32_t batch, int planes, void *workspace)
     Layout L{};
     L.tall = g->rows > g->cols;
     L.m = L.tall ? g->cols : g->rows, L.n = L.tall ? g->rows : g->cols;
-    auto pad = [](int32_t v) { return static_cast<int32_t>(round_up(v, v > 1024 ? kPad : v > 256 ? 128 : 64)); };
+    // rows and columns are filled up with zeros, which stay zeros
+    auto pad = [](int32_t v) { return static_cast<int32_t>(round_up(v, v > 1920 ? 256 : v > 256 ? 128 : 64)); };
     L.mp = pad(L.m), L.np = pad(L.n);
     Carver c(workspace);
     const int64_t x = 2 * int64_t(L.mp) * L.np * batch, a = planes * int64_t(L.mp) * L.mp * batch;
@@ -486,10 +486,12 @@ dol_status newton_schulz(const Layout &L, const dol_matrix *g, int64_t g_stride,
                                                                       L.mp, L.np);
     DOL_HIP(hipGetLastError());
     auto two = [](int n) { return std::ldexp(1.0f, n); };
-    // the largest tiles that fill the chip: of 256 x 256 half of it (a unit takes one), of 128 x 128 all of it (two)
+    // The largest tiles that fill the chip well enough: larger ones load less for what they do, and loads bound them all.  Of 256 x 256
+    // half a chip (2000 x 2000 stays below, 4096 x 4096 takes 1.68 ms so and 1.87 with 128 x 128); of 128 x 128 from these numbers on, beside
+    // 64 x 64, us: float 2000 x 2000 937 / 1 343, 1400 x 1500 635 / 737; bf16 2000 x 2000 389 / 468, but 1024 x 3000 with 192 tiles 258 / 246.
     auto size_of = [&](int64_t rows, int64_t cols, bool half) {
         auto many = [&](int t) { return rows % t || cols % t ? 0 : (half ? rows / t * (rows / t + 1) / 2 : rows / t * (cols / t)) * batch; };
-        return many(256) >= kUnits / 2 ? 2 : many(128) >= 2 * kUnits ? 1 : 0;
+        return many(256) >= kUnits / 2 ? 2 : many(128) >= (P == 1 ? (half ? 192 : 256) : (half ? 100 : 128)) ? 1 : 0;
     };
     for (int32_t t = 0; t < steps; ++t) {
         const int from = t & 1;
