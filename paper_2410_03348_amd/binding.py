@@ -662,29 +662,19 @@ F32, BF16 = 0, 1
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-class _Matrix(C.Structure):
-    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("ld", C.c_int64), ("data", C.c_void_p)]
-
-
-_matrix_p = C.POINTER(_Matrix)
-_lib.dol_cross_entropy_workspace.argtypes = [_matrix_p, _matrix_p, C.c_int32, C.POINTER(C.c_int64)]
-_lib.dol_cross_entropy.argtypes = [_matrix_p, _matrix_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
-_lib.dol_cross_entropy_backward.argtypes = [_matrix_p, _matrix_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, _matrix_p, _matrix_p,
-                                            C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
-
-
-def _matrix(t: torch.Tensor) -> _Matrix:
-    """A float32 or bfloat16 tensor [rows, cols] with neighbouring columns next to each other."""
-    assert t.is_cuda and t.dtype in _DTYPES and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1)
-    rows, cols = t.shape
-    assert rows <= 1 or t.stride(0) >= cols
-    return _Matrix(_DTYPES[t.dtype], rows, cols, t.stride(0) if rows > 1 else max(cols, 1), t.data_ptr())
+def _matrix(t: torch.Tensor):
+    """dol_matrix's fields of a float32 or bfloat16 tensor [rows, cols] with neighbouring columns next to each other."""
+    dtype = _DTYPES.get(t.dtype)
+    assert t.is_cuda and dtype is not None and t.dim() == 2
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    assert (cols <= 1 or step == 1) and (rows <= 1 or ld >= cols)
+    return dtype, rows, cols, ld if rows > 1 else max(cols, 1), t.data_ptr()
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype=torch.float32):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == dtype and t.shape == (n,) and t.is_contiguous()
+    assert t.is_cuda and t.dtype is dtype and t.shape == (n,) and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -704,9 +694,7 @@ def _workspace(given: Optional[torch.Tensor], n: int, device, stream):
 
 def cross_entropy_workspace(x: torch.Tensor, weight: torch.Tensor, backward: bool = False) -> int:
     """Bytes that cross_entropy (or cross_entropy_backward) needs for these operands."""
-    n = C.c_int64()
-    _check(_lib.dol_cross_entropy_workspace(C.byref(_matrix(x)), C.byref(_matrix(weight)), int(backward), C.byref(n)))
-    return n.value
+    return _native.cross_entropy_workspace(_matrix(x), _matrix(weight), int(backward))
 
 
 def cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
@@ -716,12 +704,10 @@ def cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, l
     x [rows, width], weight [classes, width] (float32 or bfloat16); target int32 [rows], rows outside 0..classes-1 are left out;
     loss, lse float32 [rows]; bias float32 [classes]; workspace: any tensor of cross_entropy_workspace bytes, or None."""
     mx, mw = _matrix(x), _matrix(weight)
-    need = C.c_int64()
-    if workspace is None:
-        _check(_lib.dol_cross_entropy_workspace(mx, mw, 0, need))
-    ws, n, _keep = _workspace(workspace, need.value, x.device, stream)
-    _check(_lib.dol_cross_entropy(mx, mw, _vector(bias, mw.rows), _vector(target, mx.rows, torch.int32), _vector(loss, mx.rows),
-                                  _vector(lse, mx.rows), ws, n, _stream(stream)))
+    rows, classes = mx[1], mw[1]
+    ws, n, _keep = _workspace(workspace, _native.cross_entropy_workspace(mx, mw, 0) if workspace is None else 0, x.device, stream)
+    _native.cross_entropy(mx, mw, _vector(bias, classes), _vector(target, rows, torch.int32), _vector(loss, rows), _vector(lse, rows), ws, n,
+                          _handle(stream))
 
 
 def cross_entropy_backward(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor,
@@ -729,19 +715,11 @@ def cross_entropy_backward(x: torch.Tensor, weight: torch.Tensor, target: torch.
                            grad_bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """Gradients of sum_i grad_loss[i] loss[i]; lse as cross_entropy left it.  Gradients that are None are not computed."""
     mx, mw = _matrix(x), _matrix(weight)
-    need = C.c_int64()
-    if workspace is None:
-        _check(_lib.dol_cross_entropy_workspace(mx, mw, 1, need))
-    ws, n, _keep = _workspace(workspace, need.value, x.device, stream)
-    _check(_lib.dol_cross_entropy_backward(mx, mw, _vector(bias, mw.rows), _vector(target, mx.rows, torch.int32), _vector(lse, mx.rows),
-                                           _vector(grad_loss, mx.rows), None if grad_x is None else _matrix(grad_x),
-                                           None if grad_weight is None else _matrix(grad_weight), _vector(grad_bias, mw.rows), ws, n,
-                                           _stream(stream)))
-
-
-_lib.dol_newton_schulz_workspace.argtypes = [_matrix_p, C.c_int32, C.POINTER(C.c_int64)]
-_lib.dol_newton_schulz.argtypes = [_matrix_p, C.c_int64, _matrix_p, C.c_int64, C.c_int32, C.c_int32, C.POINTER(C.c_float), C.c_float,
-                                   C.c_void_p, C.c_int64, C.c_void_p]
+    rows, classes = mx[1], mw[1]
+    ws, n, _keep = _workspace(workspace, _native.cross_entropy_workspace(mx, mw, 1) if workspace is None else 0, x.device, stream)
+    _native.cross_entropy_backward(mx, mw, _vector(bias, classes), _vector(target, rows, torch.int32), _vector(lse, rows),
+                                   _vector(grad_loss, rows), None if grad_x is None else _matrix(grad_x),
+                                   None if grad_weight is None else _matrix(grad_weight), _vector(grad_bias, classes), ws, n, _handle(stream))
 
 
 def _matrices(t: torch.Tensor):
@@ -751,14 +729,12 @@ def _matrices(t: torch.Tensor):
         return _matrix(t), 0, 1
     b, rows, cols = t.shape
     assert t.is_cuda and t.dtype in _DTYPES and (cols <= 1 or t.stride(2) == 1) and (rows <= 1 or t.stride(1) >= cols)
-    return _Matrix(_DTYPES[t.dtype], rows, cols, t.stride(1) if rows > 1 else max(cols, 1), t.data_ptr()), t.stride(0), b
+    return (_DTYPES[t.dtype], rows, cols, t.stride(1) if rows > 1 else max(cols, 1), t.data_ptr()), t.stride(0), b
 
 
 def newton_schulz_workspace(g: torch.Tensor) -> int:
     m, _, batch = _matrices(g)
-    n = C.c_int64()
-    _check(_lib.dol_newton_schulz_workspace(m, batch, n))
-    return n.value
+    return _native.newton_schulz_workspace(m, batch)
 
 
 def newton_schulz(g: torch.Tensor, out: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
@@ -768,29 +744,15 @@ def newton_schulz(g: torch.Tensor, out: torch.Tensor, steps: int = 5, coefficien
     mg, g_stride, batch = _matrices(g)
     mo, out_stride, n_out = _matrices(out)
     assert batch == n_out
-    need = C.c_int64()
-    if workspace is None:
-        _check(_lib.dol_newton_schulz_workspace(mg, batch, need))
-    ws, n, _keep = _workspace(workspace, need.value, g.device, stream)
-    _check(_lib.dol_newton_schulz(mg, g_stride, mo, out_stride, batch, steps, (C.c_float * 3)(*coefficients), eps, ws, n, _stream(stream)))
+    ws, n, _keep = _workspace(workspace, _native.newton_schulz_workspace(mg, batch) if workspace is None else 0, g.device, stream)
+    _native.newton_schulz(mg, g_stride, mo, out_stride, batch, steps, *coefficients, eps, ws, n, _handle(stream))
 
 
-class _Activations(C.Structure):
-    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("points", C.c_int32), ("channels", C.c_int32), ("ld_batch", C.c_int64),
-                ("ld_point", C.c_int64), ("data", C.c_void_p)]
-
-
-_acts_p = C.POINTER(_Activations)
 _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
-_lib.dol_group_norm_workspace.argtypes = [_acts_p, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
-_lib.dol_group_norm.argtypes = [_acts_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_int32, _acts_p, C.c_void_p, C.c_void_p, C.c_void_p,
-                                C.c_int64, C.c_void_p]
-_lib.dol_group_norm_backward.argtypes = [_acts_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, _acts_p, _acts_p,
-                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
 
 
-def _activations(t: torch.Tensor) -> _Activations:
-    """A tensor [batch, points.., channels], neighbouring channels next to each other and points at one distance."""
+def _activations(t: torch.Tensor):
+    """dol_activations' fields of a tensor [batch, points.., channels], neighbouring channels next to each other and points at one distance."""
     assert t.is_cuda and t.dtype in _DTYPES and t.dim() >= 3
     shape, stride = t.shape, t.stride()
     channels, points = shape[-1], 1
@@ -802,20 +764,18 @@ def _activations(t: torch.Tensor) -> _Activations:
             ld = stride[k] if points == 1 else ld
         points *= shape[k]
     assert points <= 1 or ld >= channels
-    return _Activations(_DTYPES[t.dtype], shape[0], points, channels, stride[0], max(ld, channels), t.data_ptr())
+    return _DTYPES[t.dtype], shape[0], points, channels, stride[0], max(ld, channels), t.data_ptr()
 
 
 def _statistics(t: Optional[torch.Tensor], batch: int, groups: int):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == torch.float32 and t.shape == (batch, groups) and t.is_contiguous()
+    assert t.is_cuda and t.dtype is torch.float32 and t.shape == (batch, groups) and t.is_contiguous()
     return t.data_ptr()
 
 
 def group_norm_workspace(x: torch.Tensor, groups: int, backward: bool = False) -> int:
-    n = C.c_int64()
-    _check(_lib.dol_group_norm_workspace(_activations(x), groups, int(backward), n))
-    return n.value
+    return _native.group_norm_workspace(_activations(x), groups, int(backward))
 
 
 def group_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int, y: torch.Tensor,
@@ -826,12 +786,10 @@ def group_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[to
     x, y: [batch, points.., channels] (float32 or bfloat16; y may be x); gamma, beta: float32 [channels]; mean, rstd: float32
     [batch, groups], written; act: "none", "relu", "silu" or "gelu"."""
     mx = _activations(x)
-    need = C.c_int64()
-    if workspace is None:
-        _check(_lib.dol_group_norm_workspace(mx, groups, 0, need))
-    ws, n, _keep = _workspace(workspace, need.value, x.device, stream)
-    _check(_lib.dol_group_norm(mx, groups, _vector(gamma, mx.channels), _vector(beta, mx.channels), eps, _ACTS[act], _activations(y),
-                               _statistics(mean, mx.batch, groups), _statistics(rstd, mx.batch, groups), ws, n, _stream(stream)))
+    batch, channels = mx[1], mx[3]
+    ws, n, _keep = _workspace(workspace, _native.group_norm_workspace(mx, groups, 0) if workspace is None else 0, x.device, stream)
+    _native.group_norm(mx, groups, _vector(gamma, channels), _vector(beta, channels), eps, _ACTS[act], _activations(y),
+                       _statistics(mean, batch, groups), _statistics(rstd, batch, groups), ws, n, _handle(stream))
 
 
 def group_norm_backward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int, mean: torch.Tensor,
@@ -840,11 +798,8 @@ def group_norm_backward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Op
     """Gradients of sum(grad_y * y); mean and rstd as group_norm left them.  Gradients that are None are not computed; grad_x may be
     grad_y or x."""
     mx = _activations(x)
-    need = C.c_int64()
-    if workspace is None:
-        _check(_lib.dol_group_norm_workspace(mx, groups, 1, need))
-    ws, n, _keep = _workspace(workspace, need.value, x.device, stream)
-    _check(_lib.dol_group_norm_backward(mx, groups, _vector(gamma, mx.channels), _vector(beta, mx.channels), _ACTS[act],
-                                        _statistics(mean, mx.batch, groups), _statistics(rstd, mx.batch, groups), _activations(grad_y),
-                                        None if grad_x is None else _activations(grad_x), _vector(grad_gamma, mx.channels),
-                                        _vector(grad_beta, mx.channels), ws, n, _stream(stream)))
+    batch, channels = mx[1], mx[3]
+    ws, n, _keep = _workspace(workspace, _native.group_norm_workspace(mx, groups, 1) if workspace is None else 0, x.device, stream)
+    _native.group_norm_backward(mx, groups, _vector(gamma, channels), _vector(beta, channels), _ACTS[act], _statistics(mean, batch, groups),
+                                _statistics(rstd, batch, groups), _activations(grad_y), None if grad_x is None else _activations(grad_x),
+                                _vector(grad_gamma, channels), _vector(grad_beta, channels), ws, n, _handle(stream))

@@ -62,20 +62,35 @@ __device__ __forceinline__ bool kept_row(int32_t target, int32_t classes) { retu
 
 // ---------------------------------------------------------------- layouts for the matrix cores
 
-// out[p][r][0..kp) = planes of src[r][0..cols), zeros behind and in rows past the source's; eight elements to a thread.  Rows whose target (if
-// given) names no class count as zeros, whatever they hold.
+// A matrix laid out for the tiles: out[p][r][0..kp) = planes of src[r][0..cols), zeros behind and in rows past the source's.  Rows that do
+// not count (if target and lse are given) are taken as zeros, whatever they hold.
+struct Pack {
+    const void *src;
+    int64_t ld, rows;
+    int32_t cols;
+    const int32_t *target;
+    const float *lse;
+    int32_t classes;
+    uint16_t *out;
+    int64_t out_rows, kp;
+    bool vec;
+    unsigned blocks;            // none where the matrix is read as it is
+};
+
+// Two of them in one launch, eight elements to a thread.
 template <typename S, int P>
-__global__ void __launch_bounds__(256) xent_pack_rows_kernel(const S *src, int64_t ld, int64_t rows, int32_t cols, const int32_t *target, int32_t classes,
-                                                             uint16_t *out, int64_t out_rows, int64_t kp, bool vec)
+__global__ void __launch_bounds__(256) xent_pack_kernel(Pack p0, Pack p1)
 {
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, per = kp / 8;
-    if (t >= out_rows * per) return;
+    const bool second = blockIdx.x >= p0.blocks;
+    const Pack &p = second ? p1 : p0;
+    const int64_t t = static_cast<int64_t>(blockIdx.x - (second ? p0.blocks : 0)) * 256 + threadIdx.x, per = p.kp / 8;
+    if (t >= p.out_rows * per) return;
     const int64_t r = t / per;
     const int c = static_cast<int>(t - r * per) * 8;
-    const bool in = r < rows && (!target || kept_row(target[r], classes));
-    const S *from = src + r * ld + c;
+    const bool in = r < p.rows && (!p.target || (kept_row(p.target[r], p.classes) && p.lse[r] != -INFINITY));
+    const S *from = static_cast<const S *>(p.src) + r * p.ld + c;
     float v[8];
-    if (in && vec && c + 8 <= cols) {
+    if (in && p.vec && c + 8 <= p.cols) {
         struct alignas(16) Piece { S e[16 / sizeof(S)]; };
 #pragma unroll
         for (int h = 0; h < static_cast<int>(8 * sizeof(S) / 16); ++h) {
@@ -85,16 +100,16 @@ __global__ void __launch_bounds__(256) xent_pack_rows_kernel(const S *src, int64
         }
     } else
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = in && c + k < cols ? static_cast<float>(from[k]) : 0.0f;
+        for (int k = 0; k < 8; ++k) v[k] = in && c + k < p.cols ? static_cast<float>(from[k]) : 0.0f;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
+    for (int q = 0; q < P; ++q) {
         u32x4 w;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t lo = take_plane<__bf16>(v[2 * k]), hi = take_plane<__bf16>(v[2 * k + 1]);
             w[k] = lo | hi << 16;
         }
-        *reinterpret_cast<u32x4 *>(out + (p * out_rows + r) * kp + c) = w;
+        *reinterpret_cast<u32x4 *>(p.out + (q * p.out_rows + r) * p.kp + c) = w;
     }
 }
 
@@ -339,42 +354,181 @@ __global__ void __launch_bounds__(TX::NT, 2) xent_products_kernel(Product px, Pr
     else product_tile<TW, O>(pw, id - first, smem);
 }
 
-// out = the sum of the parts in their order, for one set or two; four columns to a thread.
+// out[m][n] = the sum of its parts, in an order that the sizes fix.
 struct Sum {
     const float *part;
     int32_t M, N, splits;       // rows, columns
     int64_t part_ld;
     void *out;
     int64_t out_ld;
+    bool shared;                // four threads to four columns, each for a quarter of the parts
+    unsigned blocks;            // none where nothing is to be summed
 };
 
 template <typename O>
-__global__ void __launch_bounds__(256) xent_sum_parts_kernel(Sum s)
+__device__ __forceinline__ void sum_parts(const Sum &s, unsigned block)
 {
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, per = (s.N + 3) / 4;
-    if (t >= s.M * per) return;
+    __shared__ f32x4 red[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t t = s.shared ? static_cast<int64_t>(block) * 64 + lane : static_cast<int64_t>(block) * 256 + threadIdx.x, per = (s.N + 3) / 4;
+    const bool in = t < s.M * per;
     const int64_t m = t / per;
     const int n = static_cast<int>(t - m * per) * 4;
     f32x4 v = {0, 0, 0, 0};
-    for (int k = 0; k < s.splits; ++k) v += *reinterpret_cast<const f32x4 *>(s.part + (static_cast<int64_t>(k) * s.M + m) * s.part_ld + n);
+    if (in)
+#pragma unroll 8
+        for (int k = s.shared ? wave : 0; k < s.splits; k += s.shared ? 4 : 1) v += *reinterpret_cast<const f32x4 *>(s.part + (static_cast<int64_t>(k) * s.M + m) * s.part_ld + n);
+    if (s.shared) {
+        red[wave][lane] = v;
+        __syncthreads();
+        if (wave != 0) return;
+        v = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    }
     const bool vec = s.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(s.out) & (4 * sizeof(O) - 1)) == 0;
-    store4(static_cast<O *>(s.out) + m * s.out_ld + n, v, s.N - n, vec);
+    if (in) store4(static_cast<O *>(s.out) + m * s.out_ld + n, v, s.N - n, vec);
 }
 
-// Sixty-four classes to a workgroup, a share of the parts to each of its wavefronts.
-__global__ void __launch_bounds__(kJoinWaves * 64) xent_bias_kernel(const float *part, int parts, int32_t piece, int32_t n, float *out)
+// Up to three sums in one launch: of grad_x's, of grad_w's and of grad_bias's parts (one row of classes).
+template <typename O>
+__global__ void __launch_bounds__(256) xent_finish_kernel(Sum x, Sum w, Sum bias)
 {
-    __shared__ float red[kJoinWaves][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, v = blockIdx.x * 64 + lane;
-    float s = 0.0f;
-    if (v < n)
-#pragma unroll 4
-        for (int k = w; k < parts; k += kJoinWaves) s += part[static_cast<int64_t>(k) * piece + v];
-    red[w][lane] = s;
+    unsigned block = blockIdx.x;
+    if (block < x.blocks) return sum_parts<O>(x, block);
+    block -= x.blocks;
+    if (block < w.blocks) return sum_parts<O>(w, block);
+    sum_parts<float>(bias, block - w.blocks);
+}
+
+// ---------------------------------------------------------------- few classes
+
+// A head over a handful of classes is all launches: everything of 16 samples is done by one workgroup, forward in one launch, backward in
+// one and the sums over the workgroups.  Logits from the matrix cores (float as it is, v_mfma_f32_16x16x4; lane l: class l & 15 or sample
+// l & 15, and gets classes 4 (l >> 4) .. + 3 of sample l & 15), each of the four wavefronts over its share of the width, the first of which
+// joins them; both gradients from vector multiply-adds, a thread to a column: a row of dl is the same for all threads, and never rounded.
+constexpr int kFewRows16 = 16;
+
+template <typename S, int VT, bool BACK>
+__global__ void __launch_bounds__(256) xent_few_kernel(const S *x, int64_t ldx, const S *w, int64_t ldw, int32_t rows, int32_t width, int32_t classes, bool vec,
+                                                       const float *bias, const int32_t *target, float *loss, float *lse, const float *grad_loss, S *gx, int64_t ldgx,
+                                                       float *part, int64_t part_ld, float *bias_part)
+{
+    __shared__ f32x4 red[4][VT][64];
+    __shared__ float dl[BACK ? VT * 16 : 1][kFewRows16];        // transposed: a class to a row
+    __shared__ bool counts[kFewRows16];
+    constexpr int E = 16 / sizeof(S);                           // elements that a lane loads at a time
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, c4 = lane >> 4;
+    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * kFewRows16;
+    const int here = static_cast<int>(min(static_cast<int64_t>(kFewRows16), rows - r0));
+    struct alignas(16) Piece { S e[E]; };
+    auto load = [&](const S *row, int k) {
+        if (vec && k + E <= width) return *reinterpret_cast<const Piece *>(row + k);
+        Piece p;
+#pragma unroll
+        for (int e = 0; e < E; ++e) p.e[e] = k + e < width ? row[k + e] : static_cast<S>(0.0f);
+        return p;
+    };
+    {
+        const S *row = x + min(r0 + r16, static_cast<int64_t>(rows) - 1) * ldx;
+        f32x4 acc[VT];
+#pragma unroll
+        for (int t = 0; t < VT; ++t) acc[t] = f32x4{0, 0, 0, 0};
+        for (int k = wave * 4 * E; k < width; k += 16 * E) {
+            const Piece px = load(row, k + c4 * E);
+#pragma unroll
+            for (int t = 0; t < VT; ++t) {
+                const Piece pw = load(w + static_cast<int64_t>(min(t * 16 + r16, classes - 1)) * ldw, k + c4 * E);
+                if constexpr (sizeof(S) == 4) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(pw.e[e], px.e[e], acc[t], 0, 0, 0);
+                } else
+                    acc[t] = Mfma<bf16x8>::go(__builtin_bit_cast(bf16x8, pw), __builtin_bit_cast(bf16x8, px), acc[t]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < VT; ++t) red[wave][t][lane] = acc[t];
+    }
     __syncthreads();
-    if (w != 0 || v >= n) return;
-    for (int k = 1; k < kJoinWaves; ++k) s += red[k][lane];
-    out[v] = s;
+    if (wave == 0) {
+        const int64_t n = r0 + r16;
+        const int32_t goal = n < rows ? target[n] : -1;
+        f32x4 acc[VT];
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+            acc[t] = (red[0][t][lane] + red[1][t][lane]) + (red[2][t][lane] + red[3][t][lane]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int v = t * 16 + c4 * 4 + e;
+                acc[t][e] = v >= classes ? -INFINITY : bias ? acc[t][e] + bias[v] : acc[t][e];
+                top = fmaxf(top, acc[t][e]);
+            }
+        }
+        if constexpr (!BACK) {
+            top = with_lane32<MaxOp>(with_lane16<MaxOp>(top));
+            // the largest logit's own term is one: kept apart, what the others add to it is not rounded away
+            float ones = 0.0f, rest = 0.0f, at = 0.0f;
+#pragma unroll
+            for (int t = 0; t < VT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float l = acc[t][e];
+                    ones += l == top ? 1.0f : 0.0f;
+                    rest += l == top || l == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((l - top) * kLog2e);
+                    at += goal == t * 16 + c4 * 4 + e ? l : 0.0f;
+                }
+            ones = with_lane32<AddOp>(with_lane16<AddOp>(ones)), rest = with_lane32<AddOp>(with_lane16<AddOp>(rest)), at = with_lane32<AddOp>(with_lane16<AddOp>(at));
+            if (n < rows && c4 == 0) {
+                const float lg = log1pf(ones - 1.0f + rest);
+                lse[n] = top == -INFINITY ? top : top + lg;
+                loss[n] = !kept_row(goal, classes) ? 0.0f : top == -INFINITY ? INFINITY : lg + (top - at);
+            }
+        } else {
+            const float z = n < rows ? lse[n] : 0.0f;
+            const bool kept = kept_row(goal, classes) && z != -INFINITY;
+            const float g = kept ? grad_loss[n] : 0.0f;
+#pragma unroll
+            for (int t = 0; t < VT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int v = t * 16 + c4 * 4 + e;
+                    const float d = acc[t][e] - z, p = v == goal ? expm1f(d) : __builtin_amdgcn_exp2f(d * kLog2e);
+                    dl[v][r16] = kept && v < classes ? p * g : 0.0f;
+                }
+            if (c4 == 0) counts[r16] = kept;
+        }
+    }
+    if constexpr (BACK) {
+        __syncthreads();
+        for (int d = threadIdx.x; (gx || part) && d < width; d += 256) {
+            asm volatile("" ::: "memory");      // (dl is read from shared memory for every column: it does not fit into the registers)
+            float wv[VT * 16], gw[VT * 16], xv[16], gr[16] = {};
+#pragma unroll
+            for (int v = 0; v < VT * 16; ++v) wv[v] = v < classes ? static_cast<float>(w[v * ldw + d]) : 0.0f, gw[v] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) xv[k] = k < here && counts[k] ? static_cast<float>(x[(r0 + k) * ldx + d]) : 0.0f;
+#pragma unroll
+            for (int v = 0; v < VT * 16; ++v)
+                if (v < classes)
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4) {
+                        const f32x4 q = *reinterpret_cast<const f32x4 *>(&dl[v][k]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) gr[k + e] = __builtin_fmaf(q[e], wv[v], gr[k + e]), gw[v] = __builtin_fmaf(q[e], xv[k + e], gw[v]);
+                    }
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (gx && k < here) gx[(r0 + k) * ldgx + d] = static_cast<S>(gr[k]);
+            if (part)
+#pragma unroll
+                for (int v = 0; v < VT * 16; ++v)
+                    if (v < classes) part[(static_cast<int64_t>(blockIdx.x) * classes + v) * part_ld + d] = gw[v];
+        }
+        if (bias_part && static_cast<int>(threadIdx.x) < classes) {
+            float s = 0.0f;
+            for (int r = 0; r < here; ++r) s += dl[threadIdx.x][r];
+            bias_part[static_cast<int64_t>(blockIdx.x) * ((classes + 3) & ~3) + threadIdx.x] = s;
+        }
+    }
 }
 
 template <typename O>
@@ -394,6 +548,9 @@ bool direct(const dol_matrix *m)            // can be read by the tiles as it is
     return m->dtype == DOL_BF16 && m->cols % 64 == 0 && m->ld % 8 == 0 && m->ld <= kMostRows && !(reinterpret_cast<uintptr_t>(m->data) & 15);
 }
 
+int32_t tiles(int64_t n, int t) { return static_cast<int32_t>((n + t - 1) / t); }
+unsigned blocks(int64_t n) { return static_cast<unsigned>((n + 255) / 256); }
+
 struct Layout {
     int32_t rows, width, classes;
     int64_t kp, n_pad;                      // width and rows as they are laid out
@@ -405,10 +562,18 @@ struct Layout {
     bool big_products;
     int32_t splits_x, splits_w;
     int64_t part_ld;
+    bool few;                               // classes: the form of its own
     int64_t bytes;
 };
 
-int32_t tiles(int64_t n, int t) { return static_cast<int32_t>((n + t - 1) / t); }
+// A thread of the form for few classes holds a column of w and of its gradient, and each 16 samples leave a part of grad_w.  Forward and
+// backward, us, so / in general: float 64 x 128 into 10 classes 16 / 35, 1 000 x 256 into 32 30 / 58, 64 x 1 024 into 32 68 / 94,
+// 16 384 x 256 into 10 51 / 100; bf16 64 x 128 into 10 16 / 24, 8 192 x 1 024 into 8 61 / 63, 64 x 1 024 into 32 (not taken) 68 / 37.
+bool few_classes(const dol_matrix *x, const dol_matrix *w)
+{
+    return w->rows <= 32 && int64_t(w->rows) * w->cols <= (x->dtype == DOL_F32 ? 32768 : 8192) && x->rows <= 16384;
+}
+
 
 template <int P, int Q>
 Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *workspace)
@@ -416,6 +581,17 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
     using S = Shapes<P, Q>;
     Layout L{};
     L.rows = x->rows, L.width = x->cols, L.classes = w->rows;
+    L.part_ld = round_up(L.width, 4);
+    L.few = few_classes(x, w);
+    if (L.few) {
+        Carver c(workspace);
+        L.splits_w = tiles(L.rows, kFewRows16);
+        // (the same for both passes, though only the backward one writes it)
+        L.part_w = c.take<float>(int64_t(L.splits_w) * L.classes * L.part_ld);
+        L.bias_part = c.take<float>(int64_t(L.splits_w) * round_up(L.classes, 4));
+        L.bytes = c.used;
+        return L;
+    }
     L.kp = round_up(L.width, 64), L.n_pad = round_up(L.rows, kPad);
     // Tiles of 256 x 256 (float 128 x 256) do more with what they load; smaller ones fill the chip sooner.
     L.big = int64_t(tiles(L.classes, S::Big::BM)) * tiles(L.rows, S::Big::BN) >= kUnits * 3 / 4;
@@ -443,7 +619,6 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
     const int64_t share = std::max<int64_t>(256, L.big_products ? total(S::BigX::BM, S::BigX::BN) / kUnits : total(S::SmallX::BM, S::SmallX::BN) / (2 * kUnits));
     L.splits_x = static_cast<int32_t>(std::max<int64_t>(1, (n + share / 2) / share));
     L.splits_w = static_cast<int32_t>(std::max<int64_t>(1, (L.rows + share / 2) / share));
-    L.part_ld = round_up(L.width, 4);
     if (L.splits_x > 1 || L.pieces > 1) L.part_x = c.take<float>(int64_t(L.splits_x) * L.rows * L.part_ld);
     if (L.splits_w > 1) L.part_w = c.take<float>(int64_t(L.splits_w) * n * L.part_ld);
     L.bytes = c.used;
@@ -462,23 +637,66 @@ auto with_planes(const dol_matrix *x, F f)
     return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
 }
 
-unsigned blocks(int64_t n) { return static_cast<unsigned>((n + 255) / 256); }
-
 // Rows with contiguous k as the tiles read them: the matrix itself, or `out`, its planes in rows of kp elements (out_rows of them).
 template <int P>
-dol_status pack(const dol_matrix *m, const int32_t *target, int32_t classes, uint16_t *out, int64_t out_rows, int64_t kp, Planes *p, hipStream_t st)
+Pack pack_of(const dol_matrix *m, const int32_t *target, const float *lse, int32_t classes, uint16_t *out, int64_t out_rows, int64_t kp, Planes *p)
 {
     using S = typename Source<P>::T;
     if (!out) {
         *p = Planes{static_cast<const uint16_t *>(m->data), m->ld, 0};
-        return DOL_OK;
+        return Pack{};
     }
-    const bool vec = !(reinterpret_cast<uintptr_t>(m->data) & 15) && m->ld % (16 / int64_t(sizeof(S))) == 0;
-    xent_pack_rows_kernel<S, P><<<blocks(out_rows * (kp / 8)), 256, 0, st>>>(static_cast<const S *>(m->data), m->ld, m->rows, m->cols, target, classes, out, out_rows, kp,
-                                                                            vec);
-    DOL_HIP(hipGetLastError());
     *p = Planes{out, kp, out_rows * kp};
+    const bool vec = !(reinterpret_cast<uintptr_t>(m->data) & 15) && m->ld % (16 / int64_t(sizeof(S))) == 0;
+    return Pack{m->data, m->ld, m->rows, m->cols, target, lse, classes, out, out_rows, kp, vec, blocks(out_rows * (kp / 8))};
+}
+
+template <int P>
+dol_status launch_pack(const Pack &a, const Pack &b, hipStream_t st)
+{
+    if (a.blocks + b.blocks == 0) return DOL_OK;
+    xent_pack_kernel<typename Source<P>::T, P><<<a.blocks + b.blocks, 256, 0, st>>>(a, b);
+    DOL_HIP(hipGetLastError());
     return DOL_OK;
+}
+
+template <typename O>
+dol_status launch_finish(const Sum &x, const Sum &w, const Sum &bias, hipStream_t st)
+{
+    const unsigned n = x.blocks + w.blocks + bias.blocks;
+    if (n == 0) return DOL_OK;
+    xent_finish_kernel<O><<<n, 256, 0, st>>>(x, w, bias);
+    DOL_HIP(hipGetLastError());
+    return DOL_OK;
+}
+
+// (few parts are read as fast by a thread each; a loop over many of them waits for every load)
+Sum make_sum(const float *part, int32_t M, int32_t N, int32_t splits, int64_t part_ld, void *out, int64_t out_ld)
+{
+    const bool shared = splits >= 16;
+    const int64_t n = int64_t(M) * ((N + 3) / 4);
+    return Sum{part, M, N, splits, part_ld, out, out_ld, shared, static_cast<unsigned>(tiles(n, shared ? 64 : 256))};
+}
+
+template <typename S, bool BACK>
+dol_status launch_few(const Layout &L, const dol_matrix *x, const dol_matrix *w, const float *bias, const int32_t *target, float *loss, float *lse, const float *grad_loss,
+                      const dol_matrix *gx, const dol_matrix *gw, float *grad_bias, hipStream_t st)
+{
+    constexpr int64_t E = 16 / sizeof(S);
+    const bool vec = x->ld % E == 0 && w->ld % E == 0 && !((reinterpret_cast<uintptr_t>(x->data) | reinterpret_cast<uintptr_t>(w->data)) & 15);
+    auto go = [&](auto vt) {
+        xent_few_kernel<S, vt.value, BACK><<<L.splits_w, 256, 0, st>>>(static_cast<const S *>(x->data), x->ld, static_cast<const S *>(w->data), w->ld, L.rows, L.width, L.classes, vec,
+                                                                      bias, target, loss, lse, grad_loss, gx ? static_cast<S *>(gx->data) : nullptr, gx ? gx->ld : 0,
+                                                                      gw ? L.part_w : nullptr, L.part_ld, grad_bias ? L.bias_part : nullptr);
+    };
+    if (L.classes <= 16) go(std::integral_constant<int, 1>());
+    else go(std::integral_constant<int, 2>());
+    DOL_HIP(hipGetLastError());
+    if (!BACK) return DOL_OK;
+    Sum sw{}, sb{};
+    if (gw) sw = make_sum(L.part_w, L.classes, L.width, L.splits_w, L.part_ld, gw->data, gw->ld);
+    if (grad_bias) sb = make_sum(L.bias_part, 1, L.classes, L.splits_w, round_up(L.classes, 4), grad_bias, L.classes);
+    return launch_finish<S>(Sum{}, sw, sb, st);
 }
 
 template <typename T>
@@ -496,27 +714,24 @@ dol_status launch_sums(const Layout &L, Planes w, Planes x, const float *bias, c
 template <int P, int Q>
 dol_status forward(const Layout &L, const dol_matrix *x, const dol_matrix *w, const float *bias, const int32_t *target, float *loss, float *lse, hipStream_t st)
 {
+    if (L.few) return launch_few<typename Source<P>::T, false>(L, x, w, bias, target, loss, lse, nullptr, nullptr, nullptr, nullptr, st);
     Planes xp, wp;
-    if (dol_status s = pack<P>(x, nullptr, 0, L.xp, L.rows, L.kp, &xp, st)) return s;
-    if (dol_status s = pack<P>(w, nullptr, 0, L.wp, L.classes, L.kp, &wp, st)) return s;
+    const Pack a = pack_of<P>(x, nullptr, nullptr, 0, L.xp, L.rows, L.kp, &xp), b = pack_of<P>(w, nullptr, nullptr, 0, L.wp, L.classes, L.kp, &wp);
+    if (dol_status s = launch_pack<P>(a, b, st)) return s;
     return L.big ? launch_sums<typename Shapes<P, Q>::Big>(L, wp, xp, bias, target, loss, lse, st)
                  : launch_sums<typename Shapes<P, Q>::Small>(L, wp, xp, bias, target, loss, lse, st);
 }
 
 template <typename T, int Q>
 dol_status launch_dlogits(const Layout &L, Planes x, Planes w, int32_t first, const float *bias, const int32_t *target, const float *lse,
-                          const float *grad_loss, float *grad_bias, hipStream_t st)
+                          const float *grad_loss, float *grad_bias, Sum *bias_parts, hipStream_t st)
 {
     DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(xent_dlogits_kernel<T, Q>), T::LDS));
     const int tm = static_cast<int>(L.n_pad / T::BM), tn = L.piece / T::BN;
     xent_dlogits_kernel<T, Q><<<tm * tn, T::NT, T::LDS, st>>>(x, w, L.rows, L.classes, static_cast<int>(L.kp / T::BK), first, L.piece, bias, target, lse, grad_loss, L.dl,
                                                               L.n_pad, grad_bias ? L.bias_part : nullptr);
     DOL_HIP(hipGetLastError());
-    if (grad_bias) {
-        const int32_t n = std::min(L.piece, L.classes - first);
-        xent_bias_kernel<<<tiles(n, 64), kJoinWaves * 64, 0, st>>>(L.bias_part, tm * T::WM, L.piece, n, grad_bias + first);
-        DOL_HIP(hipGetLastError());
-    }
+    *bias_parts = grad_bias ? make_sum(L.bias_part, 1, std::min(L.piece, L.classes - first), tm * T::WM, L.piece, grad_bias + first, L.classes) : Sum{};
     return DOL_OK;
 }
 
@@ -533,13 +748,10 @@ dol_status launch_products(Product x, Product w, hipStream_t st)
     return DOL_OK;
 }
 
-template <typename O>
-dol_status sum_parts(const Product &p, hipStream_t st)
+Sum sum_of(const Product &p)
 {
-    const Sum s{p.part, p.N, p.M, p.splits, p.part_ld, p.out, p.out_ld};
-    xent_sum_parts_kernel<O><<<blocks(int64_t(s.M) * ((s.N + 3) / 4)), 256, 0, st>>>(s);
-    DOL_HIP(hipGetLastError());
-    return DOL_OK;
+    if (!p.part) return Sum{};
+    return make_sum(p.part, p.N, p.M, p.splits, p.part_ld, p.out, p.out_ld);
 }
 
 template <int P, int Q>
@@ -548,14 +760,16 @@ dol_status reverse(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
 {
     using S = typename Source<P>::T;
     using Z = Shapes<P, Q>;
+    if (L.few) return launch_few<S, true>(L, x, w, bias, target, nullptr, const_cast<float *>(lse), grad_loss, grad_x, grad_w, grad_bias, st);
     Planes xp, wp;
     // x is always laid out, with zeros in the rows that do not count: as k of grad_w they would meet dl's zeros with whatever they hold
-    if (dol_status s = pack<P>(x, target, L.classes, L.xp, L.n_pad, L.kp, &xp, st)) return s;
-    if (dol_status s = pack<P>(w, nullptr, 0, L.wp, L.classes, L.kp, &wp, st)) return s;
+    const Pack lx = pack_of<P>(x, target, lse, L.classes, L.xp, L.n_pad, L.kp, &xp), lw = pack_of<P>(w, nullptr, nullptr, 0, L.wp, L.classes, L.kp, &wp);
+    if (dol_status s = launch_pack<P>(lx, lw, st)) return s;
     for (int32_t k = 0; k < L.pieces; ++k) {
         const int32_t first = k * L.piece, n = std::min(L.piece, L.classes - first);
-        if (dol_status s = L.big ? launch_dlogits<typename Z::Big, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, st)
-                                 : launch_dlogits<typename Z::Small, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, st))
+        Sum sb{};
+        if (dol_status s = L.big ? launch_dlogits<typename Z::Big, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, &sb, st)
+                                 : launch_dlogits<typename Z::Small, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, &sb, st))
             return s;
         const Planes dl{L.dl, L.piece, L.n_pad * L.piece};
         Product a{}, b{};
@@ -571,10 +785,7 @@ dol_status reverse(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
         }
         if (dol_status s = L.big_products ? launch_products<typename Z::BigX, typename Z::BigW, S>(a, b, st) : launch_products<typename Z::SmallX, typename Z::SmallW, S>(a, b, st))
             return s;
-        if (b.part)
-            if (dol_status s = sum_parts<S>(b, st)) return s;
-        if (a.part && k == L.pieces - 1)
-            if (dol_status s = sum_parts<S>(a, st)) return s;
+        if (dol_status s = launch_finish<S>(k == L.pieces - 1 ? sum_of(a) : Sum{}, sum_of(b), sb, st)) return s;
     }
     return DOL_OK;
 }

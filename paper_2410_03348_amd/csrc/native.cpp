@@ -4,7 +4,8 @@
 //
 // Every function takes plain integers (addresses of the ctypes structures that binding.py owns, table handles, device
 // pointers; 0 or None = NULL), contiguous buffers of the stated item size where the ABI takes a host array, and the stream
-// last: an integer handle, or None for torch's current stream.  A status other than DOL_OK goes to the error callback set
+// last: an integer handle, or None for torch's current stream.  Matrices and activations come as tuples of their structure's
+// fields, in its order.  A status other than DOL_OK goes to the error callback set
 // with setup(), whose exception leaves the call.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -51,6 +52,13 @@ struct Args {
         if (bad) return 0;
         const long long x = PyLong_AsLongLong(v[k]);
         if (x == -1 && PyErr_Occurred()) bad = true;
+        return x;
+    }
+    double real(int k)
+    {
+        if (bad) return 0.0;
+        const double x = PyFloat_AsDouble(v[k]);
+        if (x == -1.0 && PyErr_Occurred()) bad = true;
         return x;
     }
     void *stream(int k)
@@ -196,6 +204,162 @@ PyObject *dtkp_fold_apply2(PyObject *, PyObject *const *v, Py_ssize_t n)
     DOL_CALL(dol_dtkp_fold_apply2(f, p, s));
 }
 
+// A structure of the ABI from the tuple of its n fields, the first `narrow` of them of 32 bits; None = NULL.
+bool fields(Args &a, int k, int64_t *to, int n, int narrow)
+{
+    if (a.bad || a.v[k] == Py_None) return false;
+    if (!PyTuple_Check(a.v[k]) || PyTuple_GET_SIZE(a.v[k]) != n) {
+        PyErr_Format(PyExc_TypeError, "argument %d: a tuple of %d fields wanted", k, n);
+        a.bad = true;
+        return false;
+    }
+    for (int f = 0; f < n && !a.bad; ++f) {
+        PyObject *o = PyTuple_GET_ITEM(a.v[k], f);
+        to[f] = f == n - 1 ? reinterpret_cast<intptr_t>(PyLong_AsVoidPtr(o)) : PyLong_AsLongLong(o);     // (the address is the last)
+        if (f < narrow && to[f] != static_cast<int32_t>(to[f]) && !PyErr_Occurred()) PyErr_Format(PyExc_OverflowError, "argument %d, field %d: past 32 bits", k, f);
+        if (PyErr_Occurred()) a.bad = true;
+    }
+    return !a.bad;
+}
+
+struct Matrix {
+    dol_matrix m{};
+    const bool given;
+
+    Matrix(Args &a, int k) : given(read(a, k)) {}
+    const dol_matrix *p() const { return given ? &m : nullptr; }
+
+private:
+    bool read(Args &a, int k)
+    {
+        int64_t f[5];
+        if (!fields(a, k, f, 5, 3)) return false;
+        m = dol_matrix{static_cast<int32_t>(f[0]), static_cast<int32_t>(f[1]), static_cast<int32_t>(f[2]), f[3], reinterpret_cast<void *>(f[4])};
+        return true;
+    }
+};
+
+struct Activations {
+    dol_activations m{};
+    const bool given;
+
+    Activations(Args &a, int k) : given(read(a, k)) {}
+    const dol_activations *p() const { return given ? &m : nullptr; }
+
+private:
+    bool read(Args &a, int k)
+    {
+        int64_t f[7];
+        if (!fields(a, k, f, 7, 4)) return false;
+        m = dol_activations{static_cast<int32_t>(f[0]), static_cast<int32_t>(f[1]), static_cast<int32_t>(f[2]), static_cast<int32_t>(f[3]), f[4], f[5],
+                            reinterpret_cast<void *>(f[6])};
+        return true;
+    }
+};
+
+PyObject *bytes(dol_status st, int64_t n) { return st == DOL_OK ? PyLong_FromLongLong(n) : done(st); }
+
+PyObject *cross_entropy_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 3);
+    Matrix x(a, 0), w(a, 1);
+    const int32_t back = static_cast<int32_t>(a.num(2));
+    if (a.bad) return nullptr;
+    int64_t need = 0;
+    const dol_status st = dol_cross_entropy_workspace(x.p(), w.p(), back, &need);
+    return bytes(st, need);
+}
+
+PyObject *cross_entropy(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 9);
+    Matrix x(a, 0), w(a, 1);
+    auto *b = a.ptr<float>(2);
+    auto *t = a.ptr<int32_t>(3);
+    auto *loss = a.ptr<float>(4), *lse = a.ptr<float>(5);
+    auto *ws = a.ptr<void>(6);
+    const int64_t have = a.num(7);
+    void *s = a.stream(8);
+    DOL_CALL(dol_cross_entropy(x.p(), w.p(), b, t, loss, lse, ws, have, s));
+}
+
+PyObject *cross_entropy_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 12);
+    Matrix x(a, 0), w(a, 1), gx(a, 6), gw(a, 7);
+    auto *b = a.ptr<float>(2);
+    auto *t = a.ptr<int32_t>(3);
+    auto *lse = a.ptr<float>(4), *g = a.ptr<float>(5), *gb = a.ptr<float>(8);
+    auto *ws = a.ptr<void>(9);
+    const int64_t have = a.num(10);
+    void *s = a.stream(11);
+    DOL_CALL(dol_cross_entropy_backward(x.p(), w.p(), b, t, lse, g, gx.p(), gw.p(), gb, ws, have, s));
+}
+
+PyObject *group_norm_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 3);
+    Activations x(a, 0);
+    const int32_t groups = static_cast<int32_t>(a.num(1)), back = static_cast<int32_t>(a.num(2));
+    if (a.bad) return nullptr;
+    int64_t need = 0;
+    const dol_status st = dol_group_norm_workspace(x.p(), groups, back, &need);
+    return bytes(st, need);
+}
+
+PyObject *group_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 12);
+    Activations x(a, 0), y(a, 6);
+    const int32_t groups = static_cast<int32_t>(a.num(1)), act = static_cast<int32_t>(a.num(5));
+    auto *gamma = a.ptr<float>(2), *beta = a.ptr<float>(3);
+    const float eps = static_cast<float>(a.real(4));
+    auto *mean = a.ptr<float>(7), *rstd = a.ptr<float>(8);
+    auto *ws = a.ptr<void>(9);
+    const int64_t have = a.num(10);
+    void *s = a.stream(11);
+    DOL_CALL(dol_group_norm(x.p(), groups, gamma, beta, eps, act, y.p(), mean, rstd, ws, have, s));
+}
+
+PyObject *group_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 14);
+    Activations x(a, 0), gy(a, 7), gx(a, 8);
+    const int32_t groups = static_cast<int32_t>(a.num(1)), act = static_cast<int32_t>(a.num(4));
+    auto *gamma = a.ptr<float>(2), *beta = a.ptr<float>(3);
+    auto *mean = a.ptr<float>(5), *rstd = a.ptr<float>(6);
+    auto *gg = a.ptr<float>(9), *gb = a.ptr<float>(10);
+    auto *ws = a.ptr<void>(11);
+    const int64_t have = a.num(12);
+    void *s = a.stream(13);
+    DOL_CALL(dol_group_norm_backward(x.p(), groups, gamma, beta, act, mean, rstd, gy.p(), gx.p(), gg, gb, ws, have, s));
+}
+
+PyObject *newton_schulz_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 2);
+    Matrix g(a, 0);
+    const int32_t batch = static_cast<int32_t>(a.num(1));
+    if (a.bad) return nullptr;
+    int64_t need = 0;
+    const dol_status st = dol_newton_schulz_workspace(g.p(), batch, &need);
+    return bytes(st, need);
+}
+
+PyObject *newton_schulz(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 13);
+    Matrix g(a, 0), o(a, 2);
+    const int64_t g_stride = a.num(1), o_stride = a.num(3);
+    const int32_t batch = static_cast<int32_t>(a.num(4)), steps = static_cast<int32_t>(a.num(5));
+    const float abc[3] = {static_cast<float>(a.real(6)), static_cast<float>(a.real(7)), static_cast<float>(a.real(8))};
+    const float eps = static_cast<float>(a.real(9));
+    auto *ws = a.ptr<void>(10);
+    const int64_t have = a.num(11);
+    void *s = a.stream(12);
+    DOL_CALL(dol_newton_schulz(g.p(), g_stride, o.p(), o_stride, batch, steps, abc, eps, ws, have, s));
+}
+
 // setup(fail, current_device, current_raw_stream)
 PyObject *setup(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
@@ -222,6 +386,14 @@ PyMethodDef g_methods[] = {
     {"dtkp_backward", DOL_FAST(dtkp_backward)},
     {"fold_apply2", DOL_FAST(fold_apply2)},
     {"dtkp_fold_apply2", DOL_FAST(dtkp_fold_apply2)},
+    {"cross_entropy_workspace", DOL_FAST(cross_entropy_workspace)},
+    {"cross_entropy", DOL_FAST(cross_entropy)},
+    {"cross_entropy_backward", DOL_FAST(cross_entropy_backward)},
+    {"newton_schulz_workspace", DOL_FAST(newton_schulz_workspace)},
+    {"newton_schulz", DOL_FAST(newton_schulz)},
+    {"group_norm_workspace", DOL_FAST(group_norm_workspace)},
+    {"group_norm", DOL_FAST(group_norm)},
+    {"group_norm_backward", DOL_FAST(group_norm_backward)},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -287,3 +287,43 @@ def test_refusals(dol):
     with pytest.raises(AssertionError):
         dol.cross_entropy(x, w, t.long(), loss, lse)
     assert bool((loss == 9).all()) and bool((lse == 9).all())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,d,v", [(1, 1, 1), (17, 255, 32), (17, 256, 33), (40, 1023, 32), (40, 1025, 32), (513, 2049, 4), (300, 16, 32), (9000, 130, 10)])
+def test_few_classes(dol, n, d, v, dtype):
+    """Both sides of where a head is small enough for a form of its own, and its odd sizes."""
+    x, w, b, t, g = make(n, d, v, getattr(torch, dtype), seed=v)
+    t[::7] = v
+    run_and_check(dol, x, w, b, t, g)
+    run_and_check(dol, x[:, :d], w, None, t, g, pad=3)
+
+
+@pytest.mark.parametrize("dtype,v", [("float32", 10), ("bfloat16", 10), ("bfloat16", 300)])
+def test_rows_without_a_class(dol, dtype, v):
+    """A row whose logits are all -inf: lse -inf, loss +inf, and no part in any gradient, whatever it holds."""
+    x, w, b, t, g = make(40, 64, v, getattr(torch, dtype), seed=3)
+    w = w.abs() + 0.125
+    out = []
+    for fill in (0.0, float("-inf")):
+        x[3] = fill
+        t[3] = v if fill == 0.0 else 1
+        loss, lse = torch.empty(40, device="cuda"), torch.empty(40, device="cuda")
+        gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+        dol.cross_entropy(x, w, t, loss, lse, bias=b)
+        dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b, grad_bias=gb)
+        out.append((gx, gw, gb))
+    assert float(lse[3]) == float("-inf") and float(loss[3]) == float("inf") and not gx[3].any()
+    assert all(torch.equal(p, q) for p, q in zip(*out))
+
+
+def test_nearly_certain_rows_of_few_classes(dol):
+    """p of the target within 2^-24 of one: loss and gradient are what the other classes leave, not zero."""
+    x, w = torch.zeros(20, 8, device="cuda"), torch.zeros(10, 8, device="cuda")
+    b = torch.zeros(10, device="cuda")
+    b[4] = 20.0
+    t = torch.full((20,), 4, dtype=torch.int32, device="cuda")
+    loss, lse = torch.empty(20, device="cuda"), torch.empty(20, device="cuda")
+    dol.cross_entropy(x, w, t, loss, lse, bias=b)
+    want = float(np.log1p(9 * np.exp(-20.0)))
+    assert abs(float(loss[0]) - want) <= 16 * U * want + 8 * U * want * 20
