@@ -76,7 +76,9 @@ struct Planes {
 // How an operand lies in memory: a row of the product to a row, k contiguous, or k to a row and the product's rows side by side.
 enum Order { kRows, kCols };
 
-// A tile of BM x BN by WM x WN wavefronts, ST stages of BK; A in PA planes, B in PB, ordered OA and OB.
+// A tile of BM x BN by WM x WN wavefronts, ST stages of BK; A in PA planes, B in PB, ordered OA and OB.  With WK = 2 there are two sets of
+// wavefronts, each for half of every step's k (join() adds them up): where a tile has one wavefront to a SIMD, a second one has something to
+// do while the first waits.
 // kRows: rows lie in LDS as lines of 128 bytes (one row of 64 elements or two of 32) whose 16-byte pieces are exchanged by an exclusive or
 // with the line's number, so that eight neighbouring lanes of a read touch all banks once.  The loads to LDS put lane l's piece at 16 l, so
 // it is the lanes' addresses in memory that are exchanged.  A row of B that lane c of fragment j takes is 4 c + j of the wavefront's 64:
@@ -85,20 +87,21 @@ enum Order { kRows, kCols };
 // 4 q .. + 3 of a block of 4 x 16, and lane c gets column c of the four rows.  Pairs of pieces are exchanged by k, so that the 16 rows that a
 // wavefront reads at a time lie in all banks.  With A so, a lane's rows 4 (l >> 4) .. + 3 of C are neighbours in memory that is ordered by
 // columns of C, which leaves as 8- or 16-byte pieces; with B so, column c of fragment j is 16 j + c.
-template <typename V_, int PA_, int PB_, Order OA_, Order OB_, int BM_, int BN_, int BK_, int WM_, int WN_, int ST_>
+template <typename V_, int PA_, int PB_, Order OA_, Order OB_, int BM_, int BN_, int BK_, int WM_, int WN_, int ST_, int WK_ = 1>
 struct MfmaTile {
     using V = V_;
     using E = typename Mfma<V>::E;
-    static constexpr int PA = PA_, PB = PB_, BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, ST = ST_;
+    static constexpr int PA = PA_, PB = PB_, BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, ST = ST_, WK = WK_;
     static constexpr Order OA = OA_, OB = OB_;
-    static constexpr int NW = WM * WN, NT = NW * 64;
+    static constexpr int NW = WM * WN * WK, NT = NW * 64;
     static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
     static constexpr int CPR = BK / 8, RPL = 64 / BK;                   // kRows: pieces to a row, rows to a line
     static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = PA * A_BYTES + PB * B_BYTES;
     static constexpr int LA = A_BYTES / (NT * 16), LB = B_BYTES / (NT * 16), LOADS = PA * LA + PB * LB;
     static constexpr int LDS = ST * STAGE;
-    static constexpr bool HALVES = BK == 64 && ST == 2 && PA == 1 && PB == 1;
-    static_assert(NI == 4 && (BK == 32 || BK == 64) && A_BYTES % (NT * 16) == 0 && B_BYTES % (NT * 16) == 0 && ST >= 2, "tile");
+    static constexpr bool HALVES = BK == 64 && ST == 2 && PA == 1 && PB == 1 && WK == 1;
+    static_assert(NI == 4 && (BK == 32 || BK == 64) && A_BYTES % (NT * 16) == 0 && B_BYTES % (NT * 16) == 0 && ST >= 2 && BK / 32 % WK == 0, "tile");
+    static_assert(WK == 1 || (WK == 2 && LDS >= BM * BN * 4), "the second set of sums");
 
     __device__ static int key_a(int line) { return line & 7; }
     __device__ static int key_b(int line) { return (RPL == 1 ? line >> 2 : line >> 1) & 7; }
@@ -163,7 +166,7 @@ struct MfmaTile {
                                f32x4 (&acc)[MI][NI], int64_t left = INT64_MAX)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int wm = wave / WN, wn = wave % WN;
+        const int wk = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN;
         const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)smem));
         uint32_t ao[LA], bo[LB];
         offsets<false>(ao, wave, lane, m0, M, a.ld, left);
@@ -275,9 +278,9 @@ struct MfmaTile {
                 else wait_and_meet<0>();
                 if (kt + ST - 1 < steps) issue(kt + ST - 1, st == 0 ? ST - 1 : st - 1);
 #pragma unroll
-                for (int kk = 0; kk < BK / 32; ++kk) {
+                for (int kk = 0; kk < BK / 32; kk += WK) {
                     V fa[PA][MI], fb[PB][NI];
-                    read(st, kk, fa, fb);
+                    read(st, kk + wk, fa, fb);
                     products(fa, fb);
                 }
                 st = st == ST - 1 ? 0 : st + 1;
@@ -285,8 +288,30 @@ struct MfmaTile {
         }
     }
 
+    // Whether this wavefront is of the set that begins with what acc is to begin with, and holds the sums after join().
+    __device__ static bool first_set() { return WK == 1 || threadIdx.x < WM * WN * 64; }
+
+    // The two sets' sums into the first one's.
+    __device__ static void join(f32x4 (&acc)[MI][NI], char *smem)
+    {
+        if constexpr (WK == 1) return;
+        f32x4 *at = reinterpret_cast<f32x4 *>(smem) + threadIdx.x % (WM * WN * 64);
+        lds_barrier();
+        if (!first_set())
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) at[(i * NI + j) * (WM * WN * 64)] = acc[i][j];
+        lds_barrier();
+        if (first_set())
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) acc[i][j] += at[(i * NI + j) * (WM * WN * 64)];
+    }
+
     // acc[i][j][e] is row row_of(i) + e and column col_of(j) of the tile.
-    __device__ static int row_of(int i) { return (threadIdx.x >> 6) / WN * TM + i * 16 + ((threadIdx.x & 63) >> 4) * 4; }
+    __device__ static int row_of(int i) { return (threadIdx.x >> 6) / WN % WM * TM + i * 16 + ((threadIdx.x & 63) >> 4) * 4; }
     __device__ static int col_of(int j = 0) { return (threadIdx.x >> 6) % WN * TN + col_at(j, threadIdx.x & 15); }
 };
 

@@ -28,16 +28,16 @@ struct Shapes<1> {
     template <Order A, Order B>
     using Mid = MfmaTile<f16x8, 1, 1, A, B, 128, 128, 64, 4, 2, 2>;
     template <Order A, Order B>
-    using Small = MfmaTile<f16x8, 1, 1, A, B, 64, 64, 64, 4, 1, 3>;
+    using Small = MfmaTile<f16x8, 1, 1, A, B, 64, 64, 64, 4, 1, 3, 2>;
 };
 template <>
 struct Shapes<2> {
     template <Order A, Order B>
     using Big = MfmaTile<f16x8, 2, 2, A, B, 256, 256, 32, 2, 4, 2>;
     template <Order A, Order B>
-    using Mid = MfmaTile<f16x8, 2, 2, A, B, 128, 128, 32, 4, 2, 2>;
+    using Mid = MfmaTile<f16x8, 2, 2, A, B, 128, 128, 64, 2, 2, 2, 2>;
     template <Order A, Order B>
-    using Small = MfmaTile<f16x8, 2, 2, A, B, 64, 64, 64, 4, 1, 3>;
+    using Small = MfmaTile<f16x8, 2, 2, A, B, 64, 64, 64, 4, 1, 3, 2>;
 };
 
 // Powers of two that X, A and B are stored times.
@@ -88,6 +88,12 @@ __global__ void __launch_bounds__(256) ns_first_kernel(const S *g, int64_t ld, i
 {
     __shared__ float tile[64][65];
     __shared__ double total;
+    const S *src = g + blockIdx.z * stride;
+    const int32_t r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;     // in g
+    const int cx = threadIdx.x & 63, cy = threadIdx.x >> 6;
+    float in[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) in[k] = r0 + k * 4 + cy < rows && c0 + cx < cols ? static_cast<float>(src[static_cast<int64_t>(r0 + k * 4 + cy) * ld + c0 + cx]) : 0.0f;
     if (threadIdx.x < 64) {
         double s = 0.0;
         for (int k = threadIdx.x; k < parts; k += 64) s += part[static_cast<int64_t>(blockIdx.z) * parts + k];
@@ -97,14 +103,8 @@ __global__ void __launch_bounds__(256) ns_first_kernel(const S *g, int64_t ld, i
     }
     __syncthreads();
     const double f = ldexp(1.0, scale) / (sqrt(total) + static_cast<double>(eps));
-    const S *src = g + blockIdx.z * stride;
-    const int32_t r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;     // in g
-    const int cx = threadIdx.x & 63, cy = threadIdx.x >> 6;
-#pragma unroll 4
-    for (int k = cy; k < 64; k += 4) {
-        const bool in = r0 + k < rows && c0 + cx < cols;
-        tile[k][cx] = in ? static_cast<float>(static_cast<double>(static_cast<float>(src[static_cast<int64_t>(r0 + k) * ld + c0 + cx])) * f) : 0.0f;
-    }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) tile[k * 4 + cy][cx] = static_cast<float>(static_cast<double>(in[k]) * f);
     __syncthreads();
     const int64_t plane = static_cast<int64_t>(mp) * np;
     uint16_t *dst = x + blockIdx.z * 2 * plane;
@@ -175,13 +175,15 @@ __global__ void __launch_bounds__(T::NT, 2) ns_symmetric_kernel(const uint16_t *
     uint16_t *dst = out + blockIdx.y * out_stride;
     const int64_t m0 = mt * T::BM, n = nt * T::BN + T::col_of();
     f32x4 early[4];         // small tiles have the registers to ask for A beforehand
-    if constexpr (POLY && T::MI == 1)
+    if (POLY && T::MI == 1 && T::first_set())
 #pragma unroll
         for (int e = 0; e < 4; ++e) early[e] = read4(src + (m0 + T::row_of(0) + e) * mp + n, plane, T::PA);
     f32x4 acc[T::MI][T::NI];
     T::clear(acc);
     const Planes p{src, ld, plane};
     T::run(p, m0, mp, p, nt * T::BN, mp, 0, steps, smem, acc);
+    T::join(acc, smem);
+    if (!T::first_set()) return;
 #pragma unroll
     for (int i = 0; i < T::MI; ++i) {
         const int64_t m = m0 + T::row_of(i);
@@ -224,18 +226,22 @@ __global__ void __launch_bounds__(T::NT, 2) ns_apply_kernel(Apply p)
     const Planes px{x, p.np, plane}, pb{p.b + z * p.b_stride, p.mp, static_cast<int64_t>(p.mp) * p.mp};
     f32x4 acc[T::MI][T::NI];        // begins with beta / alpha X: read while the first operands are on their way
     const float begin = p.beta / p.alpha;
+    T::clear(acc);
+    if (T::first_set())
 #pragma unroll
-    for (int i = 0; i < T::MI; ++i)
+        for (int i = 0; i < T::MI; ++i)
 #pragma unroll
-        for (int j = 0; j < T::NI; ++j) {
-            const int64_t m = static_cast<int64_t>(mt) * T::BM + T::row_of(i), n = static_cast<int64_t>(nt) * T::BN + T::col_of(j);
-            if constexpr (TURN) {
+            for (int j = 0; j < T::NI; ++j) {
+                const int64_t m = static_cast<int64_t>(mt) * T::BM + T::row_of(i), n = static_cast<int64_t>(nt) * T::BN + T::col_of(j);
+                if constexpr (TURN) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = begin * (half_of(x[plane + (m + e) * p.np + n]) + half_of(x[(m + e) * p.np + n]));
-            } else
-                acc[i][j] = begin * read4(x + n * p.np + m, plane, 2);
-        }
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = begin * (half_of(x[plane + (m + e) * p.np + n]) + half_of(x[(m + e) * p.np + n]));
+                } else
+                    acc[i][j] = begin * read4(x + n * p.np + m, plane, 2);
+            }
     T::run(TURN ? pb : px, mt * T::BM, TURN ? p.mp : p.np, TURN ? px : pb, nt * T::BN, TURN ? p.np : p.mp, 0, p.mp / T::BK, smem, acc, p.mp);
+    T::join(acc, smem);
+    if (!T::first_set()) return;
     const bool vec = p.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(static_cast<O *>(p.out) + z * p.out_stride) & (4 * sizeof(O) - 1)) == 0;
 #pragma unroll
     for (int i = 0; i < T::MI; ++i) {
@@ -487,11 +493,12 @@ dol_status newton_schulz(const Layout &L, const dol_matrix *g, int64_t g_stride,
     DOL_HIP(hipGetLastError());
     auto two = [](int n) { return std::ldexp(1.0f, n); };
     // The largest tiles that fill the chip well enough: larger ones load less for what they do, and loads bound them all.  Of 256 x 256
-    // half a chip (2000 x 2000 stays below, 4096 x 4096 takes 1.68 ms so and 1.87 with 128 x 128); of 128 x 128 from these numbers on, beside
-    // 64 x 64, us: float 2000 x 2000 937 / 1 343, 1400 x 1500 635 / 737; bf16 2000 x 2000 389 / 468, but 1024 x 3000 with 192 tiles 258 / 246.
+    // half a chip (float 4096 x 4096 takes 4.52 ms so and 4.77 with 128 x 128, bf16 1.67 and 1.87).  Of 128 x 128 from these numbers on,
+    // beside 64 x 64, us: float 1400 x 1500 400 / 486, 2000 x 2000 797 / 1 150, 1280 x 2500 423 / 592, but with 66 symmetric ones
+    // 599 / 400; bf16 1792 x 1792 312 / 372, 1280 x 2500 263 / 301, but with 192 of them for B X 246 / 230 and with 136 symmetric 433 / 399.
     auto size_of = [&](int64_t rows, int64_t cols, bool half) {
         auto many = [&](int t) { return rows % t || cols % t ? 0 : (half ? rows / t * (rows / t + 1) / 2 : rows / t * (cols / t)) * batch; };
-        return many(256) >= kUnits / 2 ? 2 : many(128) >= (P == 1 ? (half ? 192 : 256) : (half ? 100 : 128)) ? 1 : 0;
+        return many(256) >= kUnits / 2 ? 2 : many(128) >= (P == 1 ? 193 : half ? 100 : 128) ? 1 : 0;
     };
     for (int32_t t = 0; t < steps; ++t) {
         const int from = t & 1;
