@@ -156,17 +156,15 @@ __device__ __forceinline__ void put_rows(const float (&s)[Q][V], const Place &p,
     lds_barrier();
 }
 
-// The sum of a block of rows x columns values, taken by a wavefront; the same in all lanes.
-__device__ __forceinline__ float sum_block(const float *buf, int rows, int pitch, int columns)
+// The sum of a block of rows x columns values (below 8192), taken by a wavefront; the same in all lanes.
+__device__ __forceinline__ float sum_block(const float *buf, int rows, int pitch, int columns, float per_columns)
 {
-    const int lane = threadIdx.x & 63;
-    const bool along = rows >= columns;
-    const int outer = along ? columns : rows, inner = along ? rows : columns, step = along ? pitch : 1, stride = along ? 1 : pitch;
     float t = 0.0f;
-#pragma unroll 1
-    for (int k = 0; k < outer; ++k)
-#pragma unroll 2
-        for (int e = lane; e < inner; e += 64) t += buf[k * stride + e * step];
+#pragma unroll 4
+    for (int e = threadIdx.x & 63; e < rows * columns; e += 64) {
+        const int r = small_quotient(e, per_columns);
+        t += buf[r * pitch + e - r * columns];
+    }
     return sum_of_wave(t);
 }
 
@@ -217,7 +215,7 @@ __global__ void __launch_bounds__(kSlabThreads) group_norm_slab_forward_kernel(S
             for (int v = 0; v < V; ++v) sum[0][v] += in[k].get(v);
     put_rows<V, 1>(sum, p, pitch, buf);
 #pragma unroll 1
-    for (int g = wave; g < groups; g += waves) gmean[g] = mean_of(sum_block(buf + g * s.per, p.rows, pitch, s.per), s);
+    for (int g = wave; g < groups; g += waves) gmean[g] = mean_of(sum_block(buf + g * s.per, p.rows, pitch, s.per, s.per_per), s);
     lds_barrier();
     float m[V], sq[1][V] = {};
 #pragma unroll
@@ -233,7 +231,7 @@ __global__ void __launch_bounds__(kSlabThreads) group_norm_slab_forward_kernel(S
     put_rows<V, 1>(sq, p, pitch, buf);
 #pragma unroll 1
     for (int g = wave; g < groups; g += waves) {
-        const float r = rstd_of(sum_block(buf + g * s.per, p.rows, pitch, s.per) * s.per_count, eps);
+        const float r = rstd_of(sum_block(buf + g * s.per, p.rows, pitch, s.per, s.per_per) * s.per_count, eps);
         grstd[g] = r;
         if (mean && (threadIdx.x & 63) == 0) mean[g0 + g] = gmean[g];
         if (rstd && (threadIdx.x & 63) == 0) rstd[g0 + g] = r;
@@ -260,7 +258,7 @@ __global__ void __launch_bounds__(kSlabThreads) group_norm_slab_forward_kernel(S
 
 // sums[2][batch][channels]: of dz and of dz xhat over the sample's points.
 template <typename T, int V, int K>
-__global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_kernel(Shape s, Tensor x, const float *gamma, const float *beta, const float *mean, const float *rstd,
+__global__ void __launch_bounds__(kSlabThreadsBack, K == kFewVecs ? 4 : 2) group_norm_slab_backward_kernel(Shape s, Tensor x, const float *gamma, const float *beta, const float *mean, const float *rstd,
                                                                                Tensor dy, int act, Tensor dx, float *sums_out)
 {
     extern __shared__ __align__(16) float lds[];
@@ -280,38 +278,50 @@ __global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_ker
             in[k] = *reinterpret_cast<const Vec<T, V> *>(src + k * step);
             gr[k] = *reinterpret_cast<const Vec<T, V> *>(up + k * up_step);
         }
-    int gi[V];
-    groups_of(gi, p, s);
-    float m[V], r[V], f[V], o[V], sum[2][V] = {}, dz[K][V];        // z = (x - m) f + o
-    if (p.in)
+    float m[V], f[V], sum[2][V] = {}, dz[K][V];
+    if (p.in) {
+        int gi[V];
+        groups_of(gi, p, s);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int c = c0 + p.lane * V + v;
-            const int64_t g = g0 + gi[v];
-            m[v] = mean[g], r[v] = rstd[g], f[v] = gamma ? r[v] * gamma[c] : r[v], o[v] = beta ? beta[c] : 0.0f;
+            const float r = rstd[g0 + gi[v]];
+            m[v] = mean[g0 + gi[v]], f[v] = gamma ? r * gamma[c0 + p.lane * V + v] : r;
         }
-    with_act(act, [&](auto A) {
+    }
+    {
+        float o[V];         // z = (x - m) f + o
+        if (p.in)
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (k * p.rows < left)
+            for (int v = 0; v < V; ++v) o[v] = beta ? beta[c0 + p.lane * V + v] : 0.0f;
+        with_act(act, [&](auto A) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float d = in[k].get(v) - m[v];
-                    float slope;
-                    act_of<decltype(A)::value, true>(__builtin_fmaf(d, f[v], o[v]), &slope);
-                    dz[k][v] = gr[k].get(v) * slope;
-                    sum[0][v] += dz[k][v], sum[1][v] = __builtin_fmaf(dz[k][v], d, sum[1][v]);
-                }
-    });
-    if (p.in)               // of dz xhat
+            for (int k = 0; k < K; ++k)
+                if (k * p.rows < left)
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[1][v] *= r[v];
+                    for (int v = 0; v < V; ++v) {
+                        const float d = in[k].get(v) - m[v];
+                        float slope;
+                        act_of<decltype(A)::value, true>(__builtin_fmaf(d, f[v], o[v]), &slope);
+                        dz[k][v] = gr[k].get(v) * slope;
+                        sum[0][v] += dz[k][v], sum[1][v] = __builtin_fmaf(dz[k][v], d, sum[1][v]);
+                    }
+        });
+    }
+    // (what a later part needs of rstd and the groups it reads and works out again: registers decide how many workgroups a unit takes)
+    if (p.in) {             // of dz xhat
+        int gi[V];
+        groups_of(gi, p, s);
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[1][v] *= rstd[g0 + gi[v]];
+    }
     put_rows<V, 2>(sum, p, pitch, buf);
-    if (p.rows >= 16) {     // a wavefront to a channel, or a thread where there are few rows
+    // A wavefront to a sum, or a thread: some 170 clocks each and 28 a row.
+    const int threads = blockDim.x;
+    if (p.rows * ((2 * s.slice + threads - 1) / threads) > 6 * ((2 * s.slice + waves - 1) / waves)) {
 #pragma unroll 1
         for (int t = wave; t < 2 * s.slice; t += waves) {
             const int q = t >= s.slice;
-            sums[t] = sum_block(buf + q * p.rows * pitch + t - q * s.slice, p.rows, pitch, 1);
+            sums[t] = sum_block(buf + q * p.rows * pitch + t - q * s.slice, p.rows, pitch, 1, 1.0f);
         }
     } else
 #pragma unroll 1
@@ -343,8 +353,13 @@ __global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_ker
     T *dst = dx.at<T>(b, p.row, c0 + p.lane * V);
     const int64_t out_step = p.rows * dx.ld_point;
     float k1[V], k2[V];     // rstd c1, rstd^2 c2
+    int gi[V];
+    groups_of(gi, p, s);
 #pragma unroll
-    for (int v = 0; v < V; ++v) k1[v] = r[v] * c12[gi[v]], k2[v] = r[v] * r[v] * c12[groups + gi[v]];
+    for (int v = 0; v < V; ++v) {
+        const float r = rstd[g0 + gi[v]];
+        k1[v] = r * c12[gi[v]], k2[v] = r * r * c12[groups + gi[v]];
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k)
         if (k * p.rows < left) {
@@ -357,26 +372,26 @@ __global__ void __launch_bounds__(kSlabThreadsBack) group_norm_slab_backward_ker
         }
 }
 
-// grad_beta, grad_gamma = the samples' sums added up; sixty-four channels to a workgroup, a share of the samples to each wavefront.
+// grad_beta (blockIdx.y 0) and grad_gamma = the samples' sums added up; sixteen channels to a workgroup, every sixty-fourth sample to a thread.
 __global__ void __launch_bounds__(1024) group_norm_params_kernel(const float *sums, int32_t batch, int32_t channels, float *grad_gamma, float *grad_beta)
 {
-    __shared__ float red[2][16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int c = blockIdx.x * 64 + lane;
-    for (int q = 0; q < 2; ++q) {
-        float t = 0.0f;
-        if (c < channels)
-#pragma unroll 4
-            for (int b = w; b < batch; b += 16) t += sums[(static_cast<int64_t>(q) * batch + b) * channels + c];
-        red[q][w][lane] = t;
-    }
+    __shared__ float red[64][17];
+    float *out = blockIdx.y ? grad_gamma : grad_beta;
+    if (!out) return;
+    const int lane = threadIdx.x & 15, row = threadIdx.x >> 4, c = blockIdx.x * 16 + lane;
+    const float *from = sums + static_cast<int64_t>(blockIdx.y) * batch * channels + c;
+    float s = 0.0f;
+    if (c < channels)
+#pragma unroll 8
+        for (int b = row; b < batch; b += 64) s += from[static_cast<int64_t>(b) * channels];
+    red[row][lane] = s;
     __syncthreads();
-    if (w < 2 && c < channels) {
-        float t = 0.0f;
-        for (int k = 0; k < 16; ++k) t += red[w][k][lane];
-        float *to = w ? grad_gamma : grad_beta;
-        if (to) to[c] = t;
-    }
+    if (threadIdx.x >= 64) return;
+    s = 0.0f;               // a lane sixteen of them, and the four lanes of a channel meet
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += red[row * 16 + k][lane];
+    s = with_lane32<AddOp>(with_lane16<AddOp>(s));
+    if (row == 0 && c < channels) out[c] = s;
 }
 
 // ---------------------------------------------------------------- groups shared out over their points
@@ -655,12 +670,16 @@ Plan plan_of(const dol_activations *x, int32_t groups, int vec, bool backward)
     // A slab is a set of whole groups, in whole vectors, of at least 16 bytes to a point.  Wider ones are taken up to 64 bytes while there
     // are two workgroups to a compute unit, and beyond while there are four.  (A line of memory is then shared by slabs of one sample, which
     // run on one XCD, at the same time.)
+    // Backward, eight vectors of x and of dy to a thread leave a unit one workgroup, which loads, computes and stores in turn: taken only
+    // where slabs would else be narrower than 64 bytes.  Forward and backward, four / eight vectors, us: bf16 512 x 256 x 256 120 / 145,
+    // 512 x 512 x 64 61 / 69, float 512 x 256 x 256 162 / 194, but bf16 128 x 1024 x 256 (32 bytes in four) 125 / 118, float 184 / 172.
     for (int k = 1; k <= groups; ++k) {
         const int64_t slice = int64_t(k) * s.per, lanes = slice / vec;
         if (groups % k || slice % vec || (slice * e < 16 && k < groups)) continue;
         int vecs = kFewVecs;
         int64_t threads = round_up((s.points + vecs - 1) / int64_t(vecs) * lanes, 64);
         if (threads > kSlabThreads / 2) {
+            if (backward && p.threads && int64_t(s.slice) * e >= 64) break;
             vecs = backward ? kBackwardVecs : kForwardVecs;
             threads = round_up((s.points + vecs - 1) / int64_t(vecs) * lanes, 64);
             if (threads > (backward ? kSlabThreadsBack : kSlabThreads)) break;
@@ -769,7 +788,7 @@ dol_status reverse(const Plan &p, const Space &w, const dol_activations *x, cons
         }
     }
     if (params) {
-        group_norm_params_kernel<<<(s.channels + 63) / 64, 1024, 0, st>>>(w.sums, s.batch, s.channels, grad_gamma, grad_beta);
+        group_norm_params_kernel<<<dim3((s.channels + 15) / 16, 2), 1024, 0, st>>>(w.sums, s.batch, s.channels, grad_gamma, grad_beta);
         DOL_HIP(hipGetLastError());
     }
     return DOL_OK;
