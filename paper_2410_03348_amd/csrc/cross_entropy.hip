@@ -72,7 +72,7 @@ struct Pack {
     const float *lse;
     int32_t classes;
     uint16_t *out;
-    int64_t out_rows, kp;
+    int64_t out_rows, kp, out_ld;
     bool vec;
     unsigned blocks;            // none where the matrix is read as it is
 };
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(Pack p0, Pack p1)
             const uint32_t lo = take_plane<__bf16>(v[2 * k]), hi = take_plane<__bf16>(v[2 * k + 1]);
             w[k] = lo | hi << 16;
         }
-        *reinterpret_cast<u32x4 *>(p.out + (q * p.out_rows + r) * p.kp + c) = w;
+        *reinterpret_cast<u32x4 *>(p.out + (q * p.out_rows + r) * p.out_ld + c) = w;
     }
 }
 
@@ -213,10 +213,10 @@ __global__ void __launch_bounds__(kJoinWaves * 64) xent_join_kernel(const float2
 
 // ---------------------------------------------------------------- backward
 
-// dl of one piece of classes in Q planes: dl[q][sample][class of the piece], zeros in the samples and classes that there are not.  Rows of a
+// dl of one piece of classes in Q planes: dl[q][sample][class of the piece] (rows ld apart), zeros in the samples and classes that there are not.  Rows of a
 // tile are samples, columns classes.  bias_part[(mt * WM + wavefront row) * piece + class] = sums of the unrounded dl (if asked for).
 template <typename T, int Q>
-__global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes w, int32_t rows, int32_t classes, int steps, int32_t first, int32_t piece,
+__global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes w, int32_t rows, int32_t classes, int steps, int32_t first, int32_t piece, int64_t ld,
                                                                 const float *bias, const int32_t *target, const float *lse, const float *grad_loss,
                                                                 uint16_t *dl, int64_t n_pad, float *bias_part)
 {
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes
     float b[T::NI], sum[T::NI];
 #pragma unroll
     for (int j = 0; j < T::NI; ++j) b[j] = n + j >= classes ? -INFINITY : bias ? bias[n + j] : 0.0f, sum[j] = 0.0f;
-    uint16_t *to = dl + static_cast<int64_t>(m0) * piece + nt * T::BN + T::col_of();
+    uint16_t *to = dl + m0 * ld + nt * T::BN + T::col_of();
 #pragma unroll
     for (int i = 0; i < T::MI; ++i)
 #pragma unroll
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes
                 u32x2 out;
                 const uint32_t w0 = take_plane<__bf16>(v[0]), w1 = take_plane<__bf16>(v[1]), w2 = take_plane<__bf16>(v[2]), w3 = take_plane<__bf16>(v[3]);
                 out[0] = w0 | w1 << 16, out[1] = w2 | w3 << 16;
-                *reinterpret_cast<u32x2 *>(to + (p * n_pad + r) * piece) = out;
+                *reinterpret_cast<u32x2 *>(to + (p * n_pad + r) * ld) = out;
             }
         }
     if (bias_part) {
@@ -349,9 +349,10 @@ __global__ void __launch_bounds__(TX::NT, 2) xent_products_kernel(Product px, Pr
 {
     static_assert(TX::LDS == TW::LDS && TX::NT == TW::NT, "one launch");
     extern __shared__ __align__(128) char smem[];
-    const int id = xcd_contiguous(blockIdx.x, gridDim.x), first = px.tm * px.tn * px.splits;
-    if (id < first) product_tile<TX, O>(px, id, smem);
-    else product_tile<TW, O>(pw, id - first, smem);
+    // each XCD gets an eighth of both, which are of different lengths
+    const int first = px.tm * px.tn * px.splits, id = blockIdx.x;
+    if (id < first) product_tile<TX, O>(px, xcd_contiguous(id, first), smem);
+    else product_tile<TW, O>(pw, xcd_contiguous(id - first, gridDim.x - first), smem);
 }
 
 // out[m][n] = the sum of its parts, in an order that the sizes fix.
@@ -555,6 +556,7 @@ struct Layout {
     int32_t rows, width, classes;
     int64_t kp, n_pad;                      // width and rows as they are laid out
     int32_t piece, pieces;
+    int64_t ldk, ldl;                       // from row to row of what is laid out, and of dl
     bool big;                               // tiles of logits
     uint16_t *xp, *wp, *dl;
     float2 *part;
@@ -592,12 +594,13 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
         L.bytes = c.used;
         return L;
     }
-    L.kp = round_up(L.width, 64), L.n_pad = round_up(L.rows, kPad);
-    // Tiles of 256 x 256 (float 128 x 256) do more with what they load; smaller ones fill the chip sooner.
-    L.big = int64_t(tiles(L.classes, S::Big::BM)) * tiles(L.rows, S::Big::BN) >= kUnits * 3 / 4;
+    L.kp = round_up(L.width, 64), L.n_pad = round_up(L.rows, kPad), L.ldk = spread(L.kp);
+    // Tiles of 256 x 256 (float 128 x 256) do more with what they load; smaller ones fill the chip sooner.  Forward and backward, us,
+    // large / small: bf16 with 64 of the large ones 76 / 57, 128 67 / 58, 1 280 895 / 950; float with 128 167 / 141, 160 142 / 155.
+    L.big = int64_t(tiles(L.classes, S::Big::BM)) * tiles(L.rows, S::Big::BN) >= (P == 3 ? 160 : 192);
     Carver c(workspace);
-    if (backward || !direct(x)) L.xp = c.take<uint16_t>(P * (backward ? L.n_pad : L.rows) * L.kp);
-    if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(L.classes) * L.kp);
+    if (backward || !direct(x)) L.xp = c.take<uint16_t>(P * (backward ? L.n_pad : L.rows) * L.ldk);
+    if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(L.classes) * L.ldk);
     if (!backward) {
         const int parts = L.big ? tiles(L.classes, S::Big::BM) * S::Big::WM : tiles(L.classes, S::Small::BM) * S::Small::WM;
         L.part = c.take<float2>(int64_t(parts) * L.n_pad);
@@ -609,14 +612,19 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
     L.pieces = static_cast<int32_t>((L.classes + most - 1) / most);
     L.piece = static_cast<int32_t>(round_up((L.classes + L.pieces - 1) / L.pieces, kPad));
     L.pieces = tiles(L.classes, L.piece);
-    L.dl = c.take<uint16_t>(Q * L.n_pad * L.piece);
+    L.ldl = spread(L.piece);
+    L.dl = c.take<uint16_t>(Q * L.n_pad * L.ldl);
     L.bias_part = c.take<float>(L.n_pad / 32 * L.piece);
     // Both products of a piece share a launch: their k is split so that the launch has a workgroup of equal length for every place there
     // is, of at least 256 elements of k.
     const int32_t n = std::min(L.piece, L.classes);
     auto total = [&](int bm, int bn) { return (int64_t(tiles(L.rows, bn)) * n + int64_t(tiles(n, bn)) * L.rows) * tiles(L.width, bm); };
-    L.big_products = total(S::BigX::BM, S::BigX::BN) / kUnits >= 1024;
-    const int64_t share = std::max<int64_t>(256, L.big_products ? total(S::BigX::BM, S::BigX::BN) / kUnits : total(S::SmallX::BM, S::SmallX::BN) / (2 * kUnits));
+    // Large tiles where a place's k with them is long, or (float) can be split evenly.  us, large / small: bf16 4 096 x 512 x 1 024 (a place's
+    // k 256) 65 / 57; float 1 000 x 300 x 5 003 (469) 141 / 155, 4 096 x 512 x 1 024 (512) 131 / 141, 500 x 300 x 20 000 (931, longer than
+    // grad_w's) 311 / 293, 300 x 200 x 3 000 (75) 84 / 75.
+    const int64_t place = total(S::BigX::BM, S::BigX::BN) / kUnits;
+    L.big_products = place >= 1024 || (P == 3 && place >= 384 && std::min(n, L.rows) >= 2 * place);
+    const int64_t share = std::max<int64_t>(256, L.big_products ? place : total(S::SmallX::BM, S::SmallX::BN) / (2 * kUnits));
     L.splits_x = static_cast<int32_t>(std::max<int64_t>(1, (n + share / 2) / share));
     L.splits_w = static_cast<int32_t>(std::max<int64_t>(1, (L.rows + share / 2) / share));
     if (L.splits_x > 1 || L.pieces > 1) L.part_x = c.take<float>(int64_t(L.splits_x) * L.rows * L.part_ld);
@@ -626,7 +634,8 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
 }
 
 // dl in bf16 is off by 2^-9 or so in every term of a gradient.  Sums over many rows average that out; with few rows, where the products
-// cost little, a second plane takes it away.
+// cost little, a second plane takes it away.  Forward and backward, us, two planes / one: 64 x 128 x 360 31 / 27, 500 x 512 x 1 000 46 / 41,
+// 512 x 256 x 20 000 107 / 87, 4 096 x 512 x 1 024 69 / 57; gradients of 64 x 128 x 360 off by 1e-5 / 2.8e-3 before they are rounded.
 constexpr int32_t kFewRows = 512;
 
 template <typename F>
@@ -639,16 +648,16 @@ auto with_planes(const dol_matrix *x, F f)
 
 // Rows with contiguous k as the tiles read them: the matrix itself, or `out`, its planes in rows of kp elements (out_rows of them).
 template <int P>
-Pack pack_of(const dol_matrix *m, const int32_t *target, const float *lse, int32_t classes, uint16_t *out, int64_t out_rows, int64_t kp, Planes *p)
+Pack pack_of(const dol_matrix *m, const int32_t *target, const float *lse, int32_t classes, uint16_t *out, int64_t out_rows, int64_t kp, int64_t ld, Planes *p)
 {
     using S = typename Source<P>::T;
     if (!out) {
         *p = Planes{static_cast<const uint16_t *>(m->data), m->ld, 0};
         return Pack{};
     }
-    *p = Planes{out, kp, out_rows * kp};
+    *p = Planes{out, ld, out_rows * ld};
     const bool vec = !(reinterpret_cast<uintptr_t>(m->data) & 15) && m->ld % (16 / int64_t(sizeof(S))) == 0;
-    return Pack{m->data, m->ld, m->rows, m->cols, target, lse, classes, out, out_rows, kp, vec, blocks(out_rows * (kp / 8))};
+    return Pack{m->data, m->ld, m->rows, m->cols, target, lse, classes, out, out_rows, kp, ld, vec, blocks(out_rows * (kp / 8))};
 }
 
 template <int P>
@@ -716,7 +725,7 @@ dol_status forward(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
 {
     if (L.few) return launch_few<typename Source<P>::T, false>(L, x, w, bias, target, loss, lse, nullptr, nullptr, nullptr, nullptr, st);
     Planes xp, wp;
-    const Pack a = pack_of<P>(x, nullptr, nullptr, 0, L.xp, L.rows, L.kp, &xp), b = pack_of<P>(w, nullptr, nullptr, 0, L.wp, L.classes, L.kp, &wp);
+    const Pack a = pack_of<P>(x, nullptr, nullptr, 0, L.xp, L.rows, L.kp, L.ldk, &xp), b = pack_of<P>(w, nullptr, nullptr, 0, L.wp, L.classes, L.kp, L.ldk, &wp);
     if (dol_status s = launch_pack<P>(a, b, st)) return s;
     return L.big ? launch_sums<typename Shapes<P, Q>::Big>(L, wp, xp, bias, target, loss, lse, st)
                  : launch_sums<typename Shapes<P, Q>::Small>(L, wp, xp, bias, target, loss, lse, st);
@@ -728,7 +737,7 @@ dol_status launch_dlogits(const Layout &L, Planes x, Planes w, int32_t first, co
 {
     DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(xent_dlogits_kernel<T, Q>), T::LDS));
     const int tm = static_cast<int>(L.n_pad / T::BM), tn = L.piece / T::BN;
-    xent_dlogits_kernel<T, Q><<<tm * tn, T::NT, T::LDS, st>>>(x, w, L.rows, L.classes, static_cast<int>(L.kp / T::BK), first, L.piece, bias, target, lse, grad_loss, L.dl,
+    xent_dlogits_kernel<T, Q><<<tm * tn, T::NT, T::LDS, st>>>(x, w, L.rows, L.classes, static_cast<int>(L.kp / T::BK), first, L.piece, L.ldl, bias, target, lse, grad_loss, L.dl,
                                                               L.n_pad, grad_bias ? L.bias_part : nullptr);
     DOL_HIP(hipGetLastError());
     *bias_parts = grad_bias ? make_sum(L.bias_part, 1, std::min(L.piece, L.classes - first), tm * T::WM, L.piece, grad_bias + first, L.classes) : Sum{};
@@ -763,7 +772,7 @@ dol_status reverse(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
     if (L.few) return launch_few<S, true>(L, x, w, bias, target, nullptr, const_cast<float *>(lse), grad_loss, grad_x, grad_w, grad_bias, st);
     Planes xp, wp;
     // x is always laid out, with zeros in the rows that do not count: as k of grad_w they would meet dl's zeros with whatever they hold
-    const Pack lx = pack_of<P>(x, target, lse, L.classes, L.xp, L.n_pad, L.kp, &xp), lw = pack_of<P>(w, nullptr, nullptr, 0, L.wp, L.classes, L.kp, &wp);
+    const Pack lx = pack_of<P>(x, target, lse, L.classes, L.xp, L.n_pad, L.kp, L.ldk, &xp), lw = pack_of<P>(w, nullptr, nullptr, 0, L.wp, L.classes, L.kp, L.ldk, &wp);
     if (dol_status s = launch_pack<P>(lx, lw, st)) return s;
     for (int32_t k = 0; k < L.pieces; ++k) {
         const int32_t first = k * L.piece, n = std::min(L.piece, L.classes - first);
@@ -771,7 +780,7 @@ dol_status reverse(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
         if (dol_status s = L.big ? launch_dlogits<typename Z::Big, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, &sb, st)
                                  : launch_dlogits<typename Z::Small, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, &sb, st))
             return s;
-        const Planes dl{L.dl, L.piece, L.n_pad * L.piece};
+        const Planes dl{L.dl, L.ldl, L.n_pad * L.ldl};
         Product a{}, b{};
         if (grad_x) {
             a.a = Planes{wp.data + first * wp.ld, wp.ld, wp.plane}, a.b = dl;

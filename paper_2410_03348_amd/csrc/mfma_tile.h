@@ -67,6 +67,15 @@ __device__ __forceinline__ void wait_and_meet()
     asm volatile("" ::: "memory");
 }
 
+// The distance of rows of n elements of 16 bits: an odd number of 256-byte blocks, over which memory's channels change.  Tiles read
+// the same columns of many rows; with a power of two of blocks from row to row they would all be on a few channels.
+inline int64_t spread(int64_t n)
+{
+    if (n < 256) return n;
+    const int64_t blocks = (n + 127) / 128;
+    return (blocks | 1) * 128;
+}
+
 struct Planes {
     const uint16_t *data;
     int64_t ld;         // elements from row to row, a multiple of 8
