@@ -21,8 +21,9 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kFar = 1e38f;       // logits further from 0 (a bias of the type's lowest value) have no finite l log2e
 constexpr int kPad = 256;                               // rows and classes of a piece are filled up to a multiple of this
-constexpr int64_t kPieceBytes = int64_t(128) << 20;     // of dl
+constexpr int64_t kMostPieceBytes = int64_t(192) << 20; // of dl
 constexpr int kUnits = 256;                             // compute units of the chip
+constexpr int kLds = 160 * 1024;                        // of each
 
 // Tiles of logits, and of the two products that dl goes into in Q planes.
 template <int P, int Q>
@@ -576,6 +577,23 @@ bool few_classes(const dol_matrix *x, const dol_matrix *w)
     return w->rows <= 32 && int64_t(w->rows) * w->cols <= (x->dtype == DOL_F32 ? 32768 : 8192) && x->rows <= 16384;
 }
 
+// When `slots` places, each of which takes the next one as it becomes free, are done with n1 pieces of work of length a and then n2 of
+// length b.
+double done(int64_t n1, double a, int64_t n2, double b, int64_t slots)
+{
+    const int64_t late = n1 % slots;                    // so many places are free one a later than the others
+    double soon = n1 / slots * a, then = soon + a;
+    double end = late ? then : soon;
+    while (n2 > 0) {
+        if (late == 0 || soon <= then) soon += b, n2 -= slots - late, end = std::max(end, soon);
+        else then += b, n2 -= late, end = std::max(end, then);
+    }
+    return end;
+}
+
+// What a tile takes beside its products, in k, and what an element of a sum and a piece's launches take, in a tile's area times k (20 G of
+// which a unit's matrix cores do in a millisecond with one product of planes).
+constexpr double kAround = 160, kSumWeight = 6, kLaunchWeight = 256 * 256 * 256;
 
 template <int P, int Q>
 Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *workspace)
@@ -608,25 +626,43 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
         L.bytes = c.used;
         return L;
     }
-    const int64_t most = std::max<int64_t>(kPad, kPieceBytes / (2 * Q * L.n_pad) / kPad * kPad);
-    L.pieces = static_cast<int32_t>((L.classes + most - 1) / most);
-    L.piece = static_cast<int32_t>(round_up((L.classes + L.pieces - 1) / L.pieces, kPad));
-    L.pieces = tiles(L.classes, L.piece);
-    L.ldl = spread(L.piece);
-    L.dl = c.take<uint16_t>(Q * L.n_pad * L.ldl);
-    L.bias_part = c.take<float>(L.n_pad / 32 * L.piece);
-    // Both products of a piece share a launch: their k is split so that the launch has a workgroup of equal length for every place there
-    // is, of at least 256 elements of k.
-    const int32_t n = std::min(L.piece, L.classes);
-    auto total = [&](int bm, int bn) { return (int64_t(tiles(L.rows, bn)) * n + int64_t(tiles(n, bn)) * L.rows) * tiles(L.width, bm); };
     // Large tiles where a place's k with them is long, or (float) can be split evenly.  us, large / small: bf16 4 096 x 512 x 1 024 (a place's
     // k 256) 65 / 57; float 1 000 x 300 x 5 003 (469) 141 / 155, 4 096 x 512 x 1 024 (512) 131 / 141, 500 x 300 x 20 000 (931, longer than
     // grad_w's) 311 / 293, 300 x 200 x 3 000 (75) 84 / 75.
-    const int64_t place = total(S::BigX::BM, S::BigX::BN) / kUnits;
-    L.big_products = place >= 1024 || (P == 3 && place >= 384 && std::min(n, L.rows) >= 2 * place);
-    const int64_t share = std::max<int64_t>(256, L.big_products ? place : total(S::SmallX::BM, S::SmallX::BN) / (2 * kUnits));
-    L.splits_x = static_cast<int32_t>(std::max<int64_t>(1, (n + share / 2) / share));
-    L.splits_w = static_cast<int32_t>(std::max<int64_t>(1, (L.rows + share / 2) / share));
+    const int64_t most = std::max<int64_t>(kPad, kMostPieceBytes / (2 * Q * L.n_pad) / kPad * kPad), one = std::min<int64_t>(L.classes, most);
+    const int64_t place = (tiles(L.rows, S::BigX::BN) * one + tiles(one, S::BigX::BN) * int64_t(L.rows)) * tiles(L.width, S::BigX::BM) / kUnits;
+    L.big_products = place >= 1024 || (P == 3 && place >= 384 && std::min<int64_t>(one, L.rows) >= 2 * place);
+    // Pieces and shares so that the launches' workgroups come out even on the places there are.  Beside pieces of 128 MB and shares of one
+    // place's k, us, now / then: float 4 096 x 512 x 30 000 2 702 / 3 420, 2 000 x 256 x 60 000 1 562 / 1 957, 8 192 x 1 024 x 10 000 3 525 / 3 859;
+    // bf16 8 192 x 256 x 20 000 515 / 637, 1 000 x 512 x 20 000 148 / 167, 4 000 x 1 000 x 30 000 1 030 / 1 022.  Pieces of up to 256 MB: bf16
+    // 8 192 x 1 024 x 65 535 4 025 / 3 890, 8 192 x 256 x 20 000 508 / 515; of up to 128 MB: float 4 096 x 512 x 30 000 3 367.
+    const int bm = L.big ? S::Big::BM : S::Small::BM, bn = L.big ? S::Big::BN : S::Small::BN, lds = L.big ? S::Big::LDS : S::Small::LDS;
+    const int pm = L.big_products ? S::BigX::BM : S::SmallX::BM, pn = L.big_products ? S::BigX::BN : S::SmallX::BN, plds = L.big_products ? S::BigX::LDS : S::SmallX::LDS;
+    const int64_t places = kUnits * std::max(1, kLds / lds), product_places = kUnits * std::max(1, kLds / plds);
+    const int64_t fewest = (L.classes + most - 1) / most, spare = fewest == 1 ? 1 : std::min<int64_t>(fewest + 12, 4 * fewest);
+    constexpr double kProducts = P == 3 ? 6 : Q;        // of planes
+    double best = 0.0;
+    for (int64_t pieces = fewest; pieces <= spare; ++pieces) {
+        const int64_t piece = round_up((L.classes + pieces - 1) / pieces, kPad), n = std::min<int64_t>(piece, L.classes);
+        if (pieces > fewest && tiles(L.classes, piece) != pieces) continue;
+        // areas of tiles times their k, the same for both launches
+        const double logits = done(L.n_pad / bm * (piece / bn), L.kp + kAround, 0, 0.0, places) * bm * bn * (places / kUnits);
+        const int64_t tx = tiles(L.width, pm) * int64_t(tiles(L.rows, pn)), tw = tiles(L.width, pm) * int64_t(tiles(n, pn));
+        const int64_t even = (tx * n + tw * L.rows) / product_places;
+        for (int q = 6; q <= 20; ++q) {
+            const int64_t share = std::max<int64_t>(256, even * q / 10), sx = std::max<int64_t>(1, (n + share / 2) / share), sw = std::max<int64_t>(1, (L.rows + share / 2) / share);
+            const double sums = (sx > 1 ? double(sx) * L.rows : 0.0) + (sw > 1 ? double(sw) * n : 0.0);
+            const double products = done(tx * sx, double(n) / sx + kAround, tw * sw, double(L.rows) / sw + kAround, product_places) * pm * pn * (product_places / kUnits) +
+                                    sums * L.width * kSumWeight / kProducts;
+            const double all = pieces * (logits + products + kLaunchWeight / kProducts);
+            if (best == 0.0 || all < best)
+                best = all, L.piece = static_cast<int32_t>(piece), L.pieces = static_cast<int32_t>(tiles(L.classes, piece)), L.splits_x = static_cast<int32_t>(sx), L.splits_w = static_cast<int32_t>(sw);
+        }
+    }
+    const int32_t n = std::min(L.piece, L.classes);
+    L.ldl = spread(L.piece);
+    L.dl = c.take<uint16_t>(Q * L.n_pad * L.ldl);
+    L.bias_part = c.take<float>(L.n_pad / 32 * L.piece);
     if (L.splits_x > 1 || L.pieces > 1) L.part_x = c.take<float>(int64_t(L.splits_x) * L.rows * L.part_ld);
     if (L.splits_w > 1) L.part_w = c.take<float>(int64_t(L.splits_w) * n * L.part_ld);
     L.bytes = c.used;
