@@ -182,6 +182,8 @@ __device__ __forceinline__ void groups_of(int (&g)[V], const Place &p, const Sha
 
 // ---------------------------------------------------------------- slabs
 
+// A slab is read once, and kept.  Bytes bound it where there are many slabs: bf16 128 x 1024 x 256 28.9 us, 4.6 TB/s; small ones take a load,
+// two rounds of sums and the stores one after the other, float 64 x 784 x 32 8.9 us.
 template <typename T, int V, int K>
 __global__ void __launch_bounds__(kSlabThreads) group_norm_slab_forward_kernel(Shape s, Tensor x, const float *gamma, const float *beta, float eps, int act, Tensor y,
                                                                               float *mean, float *rstd)
@@ -256,7 +258,8 @@ __global__ void __launch_bounds__(kSlabThreads) group_norm_slab_forward_kernel(S
     });
 }
 
-// sums[2][batch][channels]: of dz and of dz xhat over the sample's points.
+// sums[2][batch][channels]: of dz and of dz xhat over the sample's points.  With eight vectors to a thread one workgroup is all that a unit
+// holds, and loads wait for the stores before: bf16 128 x 1024 x 256 68.7 us, 2.9 TB/s; with four two.
 template <typename T, int V, int K>
 __global__ void __launch_bounds__(kSlabThreadsBack, K == kFewVecs ? 4 : 2) group_norm_slab_backward_kernel(Shape s, Tensor x, const float *gamma, const float *beta, const float *mean, const float *rstd,
                                                                                Tensor dy, int act, Tensor dx, float *sums_out)
@@ -407,7 +410,7 @@ __device__ __forceinline__ void join(float &mean, float &m2, float have, float m
     m2 = m2 + m22 + d * d * have * f;
 }
 
-// part[batch][chunks][channels] = (mean, squared deviations) of a channel's points in a chunk.
+// part[batch][chunks][channels] = (mean, squared deviations) of a channel's points in a chunk.  Bytes bound it: bf16 16 x 65536 x 128 64 us, 4.2 TB/s.
 template <typename T, int V>
 __global__ void __launch_bounds__(kPartThreads) group_norm_part_forward_kernel(Shape s, Tensor x, float2 *part)
 {
@@ -492,6 +495,7 @@ __global__ void __launch_bounds__(256) group_norm_finish_forward_kernel(Shape s,
 }
 
 // y, or grad_x (BACKWARD; c12: a group's c1 and c2), of a chunk.  The last chunk first: what the sums read last may still be in cache.
+// bf16 16 x 65536 x 128 in 101 us, 5.3 TB/s, the rate of a copy.
 template <typename T, int V, bool BACKWARD>
 __global__ void __launch_bounds__(kPartThreads) group_norm_map_kernel(Shape s, Tensor x, Tensor dy, const float *gamma, const float *beta, const float *mean, const float *rstd,
                                                                       const float2 *c12, int act, Tensor out)
