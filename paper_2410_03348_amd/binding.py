@@ -117,7 +117,7 @@ def _fail(status: int):
     raise DolError(status, last_error())
 
 
-_native.setup(_fail, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+_native.setup(_fail, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.float32, torch.bfloat16)
 
 
 def _np_i32(x) -> np.ndarray:
@@ -662,20 +662,10 @@ F32, BF16 = 0, 1
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-def _matrix(t: torch.Tensor):
-    """dol_matrix's fields of a float32 or bfloat16 tensor [rows, cols] with neighbouring columns next to each other."""
-    dtype = _DTYPES.get(t.dtype)
-    assert t.is_cuda and dtype is not None and t.dim() == 2
-    (rows, cols), (ld, step) = t.shape, t.stride()
-    assert (cols <= 1 or step == 1) and (rows <= 1 or ld >= cols)
-    return dtype, rows, cols, ld if rows > 1 else max(cols, 1), t.data_ptr()
-
-
-def _vector(t: Optional[torch.Tensor], n: int, dtype=torch.float32):
-    if t is None:
-        return None
-    assert t.is_cuda and t.dtype is dtype and t.shape == (n,) and t.is_contiguous()
-    return t.data_ptr()
+# The calls below check tensors and take them apart in _native: matrix(t) and activations(t) give the fields of the structures,
+# values(t, dtype, sizes..) the address of a contiguous tensor, all of them None for None; AssertionError where a tensor does not fit.
+_matrix, _activations, _values = _native.matrix, _native.activations, _native.values
+_F, _I = torch.float32, torch.int32
 
 
 def _workspace(given: Optional[torch.Tensor], n: int, device, stream):
@@ -706,8 +696,8 @@ def cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, l
     mx, mw = _matrix(x), _matrix(weight)
     rows, classes = mx[1], mw[1]
     ws, n, _keep = _workspace(workspace, _native.cross_entropy_workspace(mx, mw, 0) if workspace is None else 0, x.device, stream)
-    _native.cross_entropy(mx, mw, _vector(bias, classes), _vector(target, rows, torch.int32), _vector(loss, rows), _vector(lse, rows), ws, n,
-                          _handle(stream))
+    _native.cross_entropy(mx, mw, _values(bias, _F, classes), _values(target, _I, rows), _values(loss, _F, rows), _values(lse, _F, rows),
+                          ws, n, _handle(stream))
 
 
 def cross_entropy_backward(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor,
@@ -717,16 +707,16 @@ def cross_entropy_backward(x: torch.Tensor, weight: torch.Tensor, target: torch.
     mx, mw = _matrix(x), _matrix(weight)
     rows, classes = mx[1], mw[1]
     ws, n, _keep = _workspace(workspace, _native.cross_entropy_workspace(mx, mw, 1) if workspace is None else 0, x.device, stream)
-    _native.cross_entropy_backward(mx, mw, _vector(bias, classes), _vector(target, rows, torch.int32), _vector(lse, rows),
-                                   _vector(grad_loss, rows), None if grad_x is None else _matrix(grad_x),
-                                   None if grad_weight is None else _matrix(grad_weight), _vector(grad_bias, classes), ws, n, _handle(stream))
+    _native.cross_entropy_backward(mx, mw, _values(bias, _F, classes), _values(target, _I, rows), _values(lse, _F, rows),
+                                   _values(grad_loss, _F, rows), _matrix(grad_x), _matrix(grad_weight), _values(grad_bias, _F, classes),
+                                   ws, n, _handle(stream))
 
 
 def _matrices(t: torch.Tensor):
     """(the first matrix, elements from one to the next, how many) of a tensor [rows, cols] or [batch, rows, cols]."""
-    assert t.dim() in (2, 3)
     if t.dim() == 2:
         return _matrix(t), 0, 1
+    assert t.dim() == 3
     b, rows, cols = t.shape
     assert t.is_cuda and t.dtype in _DTYPES and (cols <= 1 or t.stride(2) == 1) and (rows <= 1 or t.stride(1) >= cols)
     return (_DTYPES[t.dtype], rows, cols, t.stride(1) if rows > 1 else max(cols, 1), t.data_ptr()), t.stride(0), b
@@ -751,29 +741,6 @@ def newton_schulz(g: torch.Tensor, out: torch.Tensor, steps: int = 5, coefficien
 _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 
-def _activations(t: torch.Tensor):
-    """dol_activations' fields of a tensor [batch, points.., channels], neighbouring channels next to each other and points at one distance."""
-    assert t.is_cuda and t.dtype in _DTYPES and t.dim() >= 3
-    shape, stride = t.shape, t.stride()
-    channels, points = shape[-1], 1
-    assert channels <= 1 or stride[-1] == 1
-    ld = channels
-    for k in range(t.dim() - 2, 0, -1):             # from the innermost: each has to continue the one before
-        if shape[k] > 1:
-            assert points == 1 or stride[k] == ld * points
-            ld = stride[k] if points == 1 else ld
-        points *= shape[k]
-    assert points <= 1 or ld >= channels
-    return _DTYPES[t.dtype], shape[0], points, channels, stride[0], max(ld, channels), t.data_ptr()
-
-
-def _statistics(t: Optional[torch.Tensor], batch: int, groups: int):
-    if t is None:
-        return None
-    assert t.is_cuda and t.dtype is torch.float32 and t.shape == (batch, groups) and t.is_contiguous()
-    return t.data_ptr()
-
-
 def group_norm_workspace(x: torch.Tensor, groups: int, backward: bool = False) -> int:
     return _native.group_norm_workspace(_activations(x), groups, int(backward))
 
@@ -788,8 +755,8 @@ def group_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[to
     mx = _activations(x)
     batch, channels = mx[1], mx[3]
     ws, n, _keep = _workspace(workspace, _native.group_norm_workspace(mx, groups, 0) if workspace is None else 0, x.device, stream)
-    _native.group_norm(mx, groups, _vector(gamma, channels), _vector(beta, channels), eps, _ACTS[act], _activations(y),
-                       _statistics(mean, batch, groups), _statistics(rstd, batch, groups), ws, n, _handle(stream))
+    _native.group_norm(mx, groups, _values(gamma, _F, channels), _values(beta, _F, channels), eps, _ACTS[act], _activations(y),
+                       _values(mean, _F, batch, groups), _values(rstd, _F, batch, groups), ws, n, _handle(stream))
 
 
 def group_norm_backward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int, mean: torch.Tensor,
@@ -800,6 +767,7 @@ def group_norm_backward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Op
     mx = _activations(x)
     batch, channels = mx[1], mx[3]
     ws, n, _keep = _workspace(workspace, _native.group_norm_workspace(mx, groups, 1) if workspace is None else 0, x.device, stream)
-    _native.group_norm_backward(mx, groups, _vector(gamma, channels), _vector(beta, channels), _ACTS[act], _statistics(mean, batch, groups),
-                                _statistics(rstd, batch, groups), _activations(grad_y), None if grad_x is None else _activations(grad_x),
-                                _vector(grad_gamma, channels), _vector(grad_beta, channels), ws, n, _handle(stream))
+    _native.group_norm_backward(mx, groups, _values(gamma, _F, channels), _values(beta, _F, channels), _ACTS[act],
+                                _values(mean, _F, batch, groups), _values(rstd, _F, batch, groups), _activations(grad_y),
+                                _activations(grad_x), _values(grad_gamma, _F, channels), _values(grad_beta, _F, channels), ws, n,
+                                _handle(stream))

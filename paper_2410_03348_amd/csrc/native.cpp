@@ -11,6 +11,8 @@
 #include <Python.h>
 
 #include <cstdint>
+#include <initializer_list>
+#include <utility>
 
 #include "dolphin_hip.h"
 
@@ -360,15 +362,142 @@ PyObject *newton_schulz(PyObject *, PyObject *const *v, Py_ssize_t n)
     DOL_CALL(dol_newton_schulz(g.p(), g_stride, o.p(), o_stride, batch, steps, abc, eps, ws, have, s));
 }
 
-// setup(fail, current_device, current_raw_stream)
+// ---- a tensor's description, for the structures above (a Python function of the same checks takes about twice as long); None for None
+
+PyObject *g_float = nullptr, *g_bf16 = nullptr;             // torch.float32, torch.bfloat16
+PyObject *s_is_cuda = nullptr, *s_dtype = nullptr, *s_shape = nullptr, *s_stride = nullptr, *s_data_ptr = nullptr;
+
+struct Tensor {
+    static constexpr int kMost = 16;
+    int dims = 0;
+    int64_t size[kMost], stride[kMost];
+    PyObject *dtype = nullptr;
+
+    explicit Tensor(PyObject *t) : t_(t) {}
+    ~Tensor() { Py_XDECREF(dtype); }
+
+    // False with an error set where it is not a tensor of the device with at most kMost dimensions.
+    bool read()
+    {
+        PyObject *cuda = PyObject_GetAttr(t_, s_is_cuda);
+        const bool here = cuda == Py_True;
+        Py_XDECREF(cuda);
+        if (!cuda || !(here || refuse("not a device tensor"))) return false;
+        dtype = PyObject_GetAttr(t_, s_dtype);
+        return dtype && numbers(PyObject_GetAttr(t_, s_shape), size) && numbers(PyObject_CallMethodNoArgs(t_, s_stride), stride);
+    }
+    // dol_dtype, or -1.
+    int type() const { return dtype == g_float ? DOL_F32 : dtype == g_bf16 ? DOL_BF16 : -1; }
+    bool contiguous() const
+    {
+        int64_t want = 1;
+        for (int k = dims - 1; k >= 0; --k) {
+            if (size[k] == 0) return true;
+            if (size[k] != 1 && stride[k] != want) return false;
+            want *= size[k];
+        }
+        return true;
+    }
+    PyObject *address() const { return PyObject_CallMethodNoArgs(t_, s_data_ptr); }
+    // Always false, with an AssertionError set.
+    static bool refuse(const char *why)
+    {
+        PyErr_SetString(PyExc_AssertionError, why);
+        return false;
+    }
+
+private:
+    PyObject *t_;
+    bool numbers(PyObject *from, int64_t *to)
+    {
+        if (!from) return false;
+        const bool fits = PyTuple_Check(from) && PyTuple_GET_SIZE(from) <= kMost;
+        dims = fits ? static_cast<int>(PyTuple_GET_SIZE(from)) : 0;
+        for (int k = 0; k < dims; ++k) to[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(from, k));
+        Py_DECREF(from);
+        return fits ? !PyErr_Occurred() : refuse("too many dimensions");
+    }
+};
+
+PyObject *described(std::initializer_list<int64_t> numbers, PyObject *address)
+{
+    PyObject *r = address ? PyTuple_New(static_cast<Py_ssize_t>(numbers.size()) + 1) : nullptr;
+    if (!r) {
+        Py_XDECREF(address);
+        return nullptr;
+    }
+    Py_ssize_t k = 0;
+    for (int64_t n : numbers) PyTuple_SET_ITEM(r, k++, PyLong_FromLongLong(n));
+    PyTuple_SET_ITEM(r, k, address);
+    return r;
+}
+
+// matrix(tensor [rows, cols]): dol_matrix's fields; neighbouring columns next to each other.
+PyObject *matrix(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 1);
+    if (a.bad) return nullptr;
+    if (v[0] == Py_None) Py_RETURN_NONE;
+    Tensor t(v[0]);
+    if (!t.read()) return nullptr;
+    if (t.type() < 0 || t.dims != 2) return Tensor::refuse("a float32 or bfloat16 matrix wanted"), nullptr;
+    const int64_t rows = t.size[0], cols = t.size[1];
+    if ((cols > 1 && t.stride[1] != 1) || (rows > 1 && t.stride[0] < cols)) return Tensor::refuse("columns of a row next to each other wanted"), nullptr;
+    return described({t.type(), rows, cols, rows > 1 ? t.stride[0] : cols > 1 ? cols : 1}, t.address());
+}
+
+// activations(tensor [batch, points.., channels]): dol_activations' fields; neighbouring channels next to each other and points at one distance.
+PyObject *activations(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 1);
+    if (a.bad) return nullptr;
+    if (v[0] == Py_None) Py_RETURN_NONE;
+    Tensor t(v[0]);
+    if (!t.read()) return nullptr;
+    if (t.type() < 0 || t.dims < 3) return Tensor::refuse("float32 or bfloat16 activations [batch, points.., channels] wanted"), nullptr;
+    const int64_t channels = t.size[t.dims - 1];
+    int64_t points = 1, ld = channels;
+    bool good = channels <= 1 || t.stride[t.dims - 1] == 1;
+    for (int k = t.dims - 2; k > 0; --k) {              // from the innermost: each has to continue the one before
+        if (t.size[k] > 1) {
+            good = good && (points == 1 || t.stride[k] == ld * points);
+            if (points == 1) ld = t.stride[k];
+        }
+        points *= t.size[k];
+    }
+    if (!good || (points > 1 && ld < channels)) return Tensor::refuse("channels next to each other and points at one distance wanted"), nullptr;
+    return described({t.type(), t.size[0], points, channels, t.stride[0], ld > channels ? ld : channels}, t.address());
+}
+
+// values(tensor, dtype, size..): the address of a contiguous tensor of this type and these sizes.
+PyObject *values(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (n >= 1 && v[0] == Py_None) Py_RETURN_NONE;
+    if (n < 3) return PyErr_Format(PyExc_TypeError, "%zd arguments, at least 3 wanted", n);
+    Tensor t(v[0]);
+    if (!t.read()) return nullptr;
+    bool good = t.dtype == v[1] && t.dims == n - 2 && t.contiguous();
+    for (int k = 0; good && k < t.dims; ++k) good = PyLong_AsLongLong(v[k + 2]) == t.size[k];
+    if (PyErr_Occurred()) return nullptr;
+    if (!good) return Tensor::refuse("a contiguous tensor of another type or size wanted"), nullptr;
+    return t.address();
+}
+
+// setup(fail, current_device, current_raw_stream, float32, bfloat16)
 PyObject *setup(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
-    Args a(v, n, 3);
+    Args a(v, n, 5);
     if (a.bad) return nullptr;
-    PyObject **to[3] = {&g_fail, &g_device, &g_stream};
-    for (int k = 0; k < 3; ++k) {
+    PyObject **to[5] = {&g_fail, &g_device, &g_stream, &g_float, &g_bf16};
+    for (int k = 0; k < 5; ++k) {
         Py_INCREF(v[k]);
         Py_XSETREF(*to[k], v[k]);
+    }
+    const std::pair<PyObject **, const char *> names[] = {{&s_is_cuda, "is_cuda"}, {&s_dtype, "dtype"}, {&s_shape, "shape"}, {&s_stride, "stride"}, {&s_data_ptr, "data_ptr"}};
+    for (const auto &name : names) {
+        PyObject *s = PyUnicode_InternFromString(name.second);
+        if (!s) return nullptr;
+        Py_XSETREF(*name.first, s);
     }
     Py_RETURN_NONE;
 }
@@ -394,6 +523,9 @@ PyMethodDef g_methods[] = {
     {"group_norm_workspace", DOL_FAST(group_norm_workspace)},
     {"group_norm", DOL_FAST(group_norm)},
     {"group_norm_backward", DOL_FAST(group_norm_backward)},
+    {"matrix", DOL_FAST(matrix)},
+    {"activations", DOL_FAST(activations)},
+    {"values", DOL_FAST(values)},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
