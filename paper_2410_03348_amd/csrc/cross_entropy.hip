@@ -36,6 +36,9 @@ struct Shapes<1, 1> {       // bf16
     using BigW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 256, 256, 64, 2, 4, 2>;
     using SmallX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 128, 128, 64, 4, 2, 2>;
     using SmallW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 128, 128, 64, 4, 2, 2>;
+    using Tiny = MfmaTile<bf16x8, 1, 1, kRows, kRows, 64, 64, 64, 4, 1, 3>;
+    using TinyX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 64, 64, 64, 4, 1, 3>;
+    using TinyW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 64, 64, 64, 4, 1, 3>;
 };
 template <>
 struct Shapes<1, 2> : Shapes<1, 1> {
@@ -43,6 +46,8 @@ struct Shapes<1, 2> : Shapes<1, 1> {
     using BigW = MfmaTile<bf16x8, 1, 2, kCols, kCols, 128, 128, 32, 4, 2, 2>;
     using SmallX = BigX;
     using SmallW = BigW;
+    using TinyX = MfmaTile<bf16x8, 1, 2, kCols, kRows, 64, 64, 64, 4, 1, 3>;
+    using TinyW = MfmaTile<bf16x8, 1, 2, kCols, kCols, 64, 64, 64, 4, 1, 3>;
 };
 template <>
 struct Shapes<3, 3> {       // float
@@ -52,6 +57,9 @@ struct Shapes<3, 3> {       // float
     using BigW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 128, 256, 32, 2, 4, 2>;
     using SmallX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 128, 128, 32, 4, 2, 2>;
     using SmallW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 128, 128, 32, 4, 2, 2>;
+    using Tiny = MfmaTile<bf16x8, 3, 3, kRows, kRows, 64, 64, 64, 4, 1, 3>;
+    using TinyX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 64, 64, 64, 4, 1, 3>;
+    using TinyW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 64, 64, 64, 4, 1, 3>;
 };
 
 template <int P>
@@ -563,11 +571,11 @@ struct Layout {
     int64_t kp, n_pad;                      // width and rows as they are laid out
     int32_t piece, pieces;
     int64_t ldk, ldl;                       // from row to row of what is laid out, and of dl
-    bool big;                               // tiles of logits
+    int32_t size;                           // 2, 1, 0: of the logits' tiles
     uint16_t *xp, *wp, *dl;
     float2 *part;
     float *at, *bias_part, *part_x, *part_w;
-    bool big_products;
+    int32_t product_size;                   // and of the products'
     int32_t splits_x, splits_w;
     int64_t part_ld;
     bool few;                               // classes: the form of its own
@@ -596,6 +604,20 @@ double done(int64_t n1, double a, int64_t n2, double b, int64_t slots)
     return end;
 }
 
+template <typename T>
+struct Type { using Tile = T; };
+
+template <typename B, typename S, typename T, typename F>
+auto by_size(int size, B big, S small, T tiny, F f) { return size == 2 ? f(big) : size == 1 ? f(small) : f(tiny); }
+
+// Tiles of 64 x 64 below so many of 128 x 128 (of logits) or k of a place with them (of the products).  Forward and backward, us, 64 x 64 /
+// 128 x 128 in both: float 64 x 128 x 360 35 / 50, 100 x 100 x 1 000 33 / 50; bf16 26 / 32, 28 / 36.  Logits alone: float 300 x 256 x 3 000 (72
+// tiles) 66 / 70, bf16 50 x 512 x 20 000 (157) 85 / 70.  Products alone: float 300 x 256 x 3 000 (126) 70 / 66, 2 000 x 128 x 2 000 (250) 71 / 65;
+// bf16 300 x 256 x 3 000 36 / 40, 8 192 x 64 x 500 (253) 35 / 42, 700 x 700 x 7 000 105 / 93.
+constexpr int kTiny = 128;
+template <int P>
+constexpr int kTinyProducts = P == 3 ? 64 : 256;
+
 // What a tile takes beside its products, in k, and what an element of a sum and a piece's launches take, in a tile's area times k (20 G of
 // which a unit's matrix cores do in a millisecond with one product of planes).
 constexpr double kAround = 160, kSumWeight = 6, kLaunchWeight = 256 * 256 * 256;
@@ -618,14 +640,17 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
         return L;
     }
     L.kp = round_up(L.width, 64), L.n_pad = round_up(L.rows, kPad), L.ldk = spread(L.kp);
-    // Tiles of 256 x 256 (float 128 x 256) do more with what they load; smaller ones fill the chip sooner.  Forward and backward, us,
+    // Tiles of 256 x 256 (float 128 x 256) do more with what they load; smaller ones (128 x 128, 64 x 64) fill the chip sooner.  Forward and backward, us,
     // large / small: bf16 with 64 of the large ones 76 / 57, 128 67 / 58, 1 280 895 / 950; float with 128 167 / 141, 160 142 / 155.
-    L.big = int64_t(tiles(L.classes, S::Big::BM)) * tiles(L.rows, S::Big::BN) >= (P == 3 ? 160 : 192);
+    L.size = int64_t(tiles(L.classes, S::Big::BM)) * tiles(L.rows, S::Big::BN) >= (P == 3 ? 160 : 192) ? 2
+             : int64_t(tiles(L.classes, S::Small::BM)) * tiles(L.rows, S::Small::BN) >= kTiny              ? 1
+                                                                                                            : 0;
     Carver c(workspace);
     if (backward || !direct(x)) L.xp = c.take<uint16_t>(P * (backward ? L.n_pad : L.rows) * L.ldk);
     if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(L.classes) * L.ldk);
     if (!backward) {
-        const int parts = L.big ? tiles(L.classes, S::Big::BM) * S::Big::WM : tiles(L.classes, S::Small::BM) * S::Small::WM;
+        const int parts = by_size(L.size, Type<typename S::Big>(), Type<typename S::Small>(), Type<typename S::Tiny>(),
+                                  [&](auto z) { return tiles(L.classes, decltype(z)::Tile::BM) * decltype(z)::Tile::WM; });
         L.part = c.take<float2>(int64_t(parts) * L.n_pad);
         L.at = c.take<float>(L.rows);
         L.bytes = c.used;
@@ -636,13 +661,22 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
     // grad_w's) 311 / 293, 300 x 200 x 3 000 (75) 84 / 75.
     const int64_t most = std::max<int64_t>(kPad, kMostPieceBytes / (2 * Q * L.n_pad) / kPad * kPad), one = std::min<int64_t>(L.classes, most);
     const int64_t place = (tiles(L.rows, S::BigX::BN) * one + tiles(one, S::BigX::BN) * int64_t(L.rows)) * tiles(L.width, S::BigX::BM) / kUnits;
-    L.big_products = place >= 1024 || (P == 3 && place >= 384 && std::min<int64_t>(one, L.rows) >= 2 * place);
+    const bool big = place >= 1024 || (P == 3 && place >= 384 && std::min<int64_t>(one, L.rows) >= 2 * place);
+    const int64_t small = (tiles(L.rows, S::SmallX::BN) * one + tiles(one, S::SmallX::BN) * int64_t(L.rows)) * tiles(L.width, S::SmallX::BM);
+    L.product_size = big ? 2 : small >= kTinyProducts<P> * kUnits ? 1 : 0;
     // Pieces and shares so that the launches' workgroups come out even on the places there are.  Beside pieces of 128 MB and shares of one
     // place's k, us, now / then: float 4 096 x 512 x 30 000 2 702 / 3 420, 2 000 x 256 x 60 000 1 562 / 1 957, 8 192 x 1 024 x 10 000 3 525 / 3 859;
     // bf16 8 192 x 256 x 20 000 515 / 637, 1 000 x 512 x 20 000 148 / 167, 4 000 x 1 000 x 30 000 1 030 / 1 022.  Pieces of up to 256 MB: bf16
     // 8 192 x 1 024 x 65 535 4 025 / 3 890, 8 192 x 256 x 20 000 508 / 515; of up to 128 MB: float 4 096 x 512 x 30 000 3 367.
-    const int bm = L.big ? S::Big::BM : S::Small::BM, bn = L.big ? S::Big::BN : S::Small::BN, lds = L.big ? S::Big::LDS : S::Small::LDS;
-    const int pm = L.big_products ? S::BigX::BM : S::SmallX::BM, pn = L.big_products ? S::BigX::BN : S::SmallX::BN, plds = L.big_products ? S::BigX::LDS : S::SmallX::LDS;
+    int bm = 0, bn = 0, lds = 0, pm = 0, pn = 0, plds = 0;
+    by_size(L.size, Type<typename S::Big>(), Type<typename S::Small>(), Type<typename S::Tiny>(), [&](auto z) {
+        using T = typename decltype(z)::Tile;
+        bm = T::BM, bn = T::BN, lds = T::LDS;
+    });
+    by_size(L.product_size, Type<typename S::BigX>(), Type<typename S::SmallX>(), Type<typename S::TinyX>(), [&](auto z) {
+        using T = typename decltype(z)::Tile;
+        pm = T::BM, pn = T::BN, plds = T::LDS;
+    });
     const int64_t places = kUnits * std::max(1, kLds / lds), product_places = kUnits * std::max(1, kLds / plds);
     const int64_t fewest = (L.classes + most - 1) / most, spare = fewest == 1 ? 1 : std::min<int64_t>(fewest + 12, 4 * fewest);
     constexpr double kProducts = P == 3 ? 6 : Q;        // of planes
@@ -667,7 +701,7 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, bool backward, void *wo
     const int32_t n = std::min(L.piece, L.classes);
     L.ldl = spread(L.piece);
     L.dl = c.take<uint16_t>(Q * L.n_pad * L.ldl);
-    L.bias_part = c.take<float>(L.n_pad / 32 * L.piece);
+    L.bias_part = c.take<float>(L.n_pad / 16 * L.piece);
     if (L.splits_x > 1 || L.pieces > 1) L.part_x = c.take<float>(int64_t(L.splits_x) * L.rows * L.part_ld);
     if (L.splits_w > 1) L.part_w = c.take<float>(int64_t(L.splits_w) * n * L.part_ld);
     L.bytes = c.used;
@@ -768,8 +802,9 @@ dol_status forward(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
     Planes xp, wp;
     const Pack a = pack_of<P>(x, nullptr, nullptr, 0, L.xp, L.rows, L.kp, L.ldk, &xp), b = pack_of<P>(w, nullptr, nullptr, 0, L.wp, L.classes, L.kp, L.ldk, &wp);
     if (dol_status s = launch_pack<P>(a, b, st)) return s;
-    return L.big ? launch_sums<typename Shapes<P, Q>::Big>(L, wp, xp, bias, target, loss, lse, st)
-                 : launch_sums<typename Shapes<P, Q>::Small>(L, wp, xp, bias, target, loss, lse, st);
+    using Z = Shapes<P, Q>;
+    return by_size(L.size, Type<typename Z::Big>(), Type<typename Z::Small>(), Type<typename Z::Tiny>(),
+                   [&](auto z) { return launch_sums<typename decltype(z)::Tile>(L, wp, xp, bias, target, loss, lse, st); });
 }
 
 template <typename T, int Q>
@@ -818,8 +853,9 @@ dol_status reverse(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
     for (int32_t k = 0; k < L.pieces; ++k) {
         const int32_t first = k * L.piece, n = std::min(L.piece, L.classes - first);
         Sum sb{};
-        if (dol_status s = L.big ? launch_dlogits<typename Z::Big, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, &sb, st)
-                                 : launch_dlogits<typename Z::Small, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, &sb, st))
+        if (dol_status s = by_size(L.size, Type<typename Z::Big>(), Type<typename Z::Small>(), Type<typename Z::Tiny>(), [&](auto z) {
+                return launch_dlogits<typename decltype(z)::Tile, Q>(L, xp, wp, first, bias, target, lse, grad_loss, grad_bias, &sb, st);
+            }))
             return s;
         const Planes dl{L.dl, L.ldl, L.n_pad * L.ldl};
         Product a{}, b{};
@@ -833,7 +869,9 @@ dol_status reverse(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
             b.M = L.width, b.N = n, b.wide = static_cast<int32_t>(L.kp), b.tall = L.piece, b.splits = L.splits_w, b.k = L.rows, b.have = L.n_pad;
             b.part = L.part_w, b.part_ld = L.part_ld, b.out = static_cast<S *>(grad_w->data) + first * grad_w->ld, b.out_ld = grad_w->ld;
         }
-        if (dol_status s = L.big_products ? launch_products<typename Z::BigX, typename Z::BigW, S>(a, b, st) : launch_products<typename Z::SmallX, typename Z::SmallW, S>(a, b, st))
+        if (dol_status s = L.product_size == 2   ? launch_products<typename Z::BigX, typename Z::BigW, S>(a, b, st)
+                           : L.product_size == 1 ? launch_products<typename Z::SmallX, typename Z::SmallW, S>(a, b, st)
+                                                 : launch_products<typename Z::TinyX, typename Z::TinyW, S>(a, b, st))
             return s;
         if (dol_status s = launch_finish<S>(k == L.pieces - 1 ? sum_of(a) : Sum{}, sum_of(b), sb, st)) return s;
     }
