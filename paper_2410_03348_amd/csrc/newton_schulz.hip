@@ -557,7 +557,8 @@ dol_status dol_newton_schulz_workspace(const dol_matrix *g, int32_t batch, int64
 {
     if (dol_status s = check_operand(g, 0, batch, "g")) return s;
     if (!bytes) return fail(DOL_EINVAL, "bytes is NULL");
-    if (batch < 0 || batch > kMostBatch || g->rows > kMostSide || g->cols > kMostSide)
+    if (batch < 0) return fail(DOL_ESHAPE, "batch = %d", batch);
+    if (batch > kMostBatch || g->rows > kMostSide || g->cols > kMostSide)
         return fail(DOL_EUNSUPPORTED, "%d matrices of %d x %d: more than %d, or a side above %d", batch, g->rows, g->cols, kMostBatch, kMostSide);
     *bytes = batch == 0 || g->rows == 0 || g->cols == 0 || small(g) ? 0 : lay_out(g, batch, g->dtype == DOL_BF16 ? 1 : 2, nullptr).bytes;
     return DOL_OK;

@@ -1,0 +1,82 @@
+"""Arguments of the training calls that are refused before anything touches a device, and the sizes of their workspaces (no GPU)."""
+import pytest
+
+from paper_2410_03348_amd import binding as dol
+
+F32, BF16 = 0, 1
+
+
+def matrix(rows, cols, dtype=F32, ld=None, data=4096):
+    return dtype, rows, cols, cols if ld is None else ld, data
+
+
+def acts(batch, points, channels, dtype=F32, data=4096):
+    return dtype, batch, points, channels, points * channels, channels, data
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,width,classes", [(0, 1, 1), (1, 1, 1), (64, 128, 10), (100, 100, 1000), (8192, 1024, 65535), (1 << 22, 3, 2), (7, 1 << 20, 1)])
+def test_cross_entropy_workspace(rows, width, classes, dtype, backward):
+    n = dol._native.cross_entropy_workspace(matrix(rows, width, dtype), matrix(classes, width, dtype), backward)
+    assert 0 <= n < 1 << 38 and n % 256 == 0
+    assert n == dol._native.cross_entropy_workspace(matrix(rows, width, dtype), matrix(classes, width, dtype), backward)
+
+
+@pytest.mark.parametrize("x,w,why", [
+    (matrix(8, 16), matrix(20, 15), "ESHAPE"), (matrix(8, 16), matrix(20, 16, BF16), "types"), (matrix(8, 16), matrix(0, 16), "classes"),
+    (matrix(8, 0), matrix(4, 0), "classes"), (matrix(8, 16, 7), matrix(4, 16), "type"), (matrix((1 << 22) + 1, 16), matrix(4, 16), "more than"),
+    (matrix(8, 16, ld=15), matrix(4, 16), "ESHAPE"), (None, matrix(4, 16), "NULL")])
+def test_cross_entropy_refusals(x, w, why):
+    with pytest.raises(dol.DolError, match=why):
+        dol._native.cross_entropy_workspace(x, w, 0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_newton_schulz_workspace(dtype):
+    small, large = (dol._native.newton_schulz_workspace(matrix(r, c, dtype), 1) for r, c in ((10, 128), (1000, 777)))
+    assert small == 0 < large
+    assert dol._native.newton_schulz_workspace(matrix(777, 1000, dtype), 1) == large
+    assert dol._native.newton_schulz_workspace(matrix(1000, 777, dtype), 4) > 3 * large
+
+
+@pytest.mark.parametrize("g,batch,why", [(matrix(8, 16, 9), 1, "type"), (matrix(-1, 16), 1, "ESHAPE"), (matrix(8, 16), -1, "batch"), (None, 1, "NULL"),
+                                         (matrix((1 << 20) + 1, 100), 1, "EUNSUPPORTED")])
+def test_newton_schulz_refusals(g, batch, why):
+    with pytest.raises(dol.DolError, match=why):
+        dol._native.newton_schulz_workspace(g, batch)
+
+
+@pytest.mark.parametrize("x,groups,why", [(acts(2, 10, 12), 5, "groups"), (acts(2, 10, 12), 0, "groups"), (acts(2, 10, 12, 5), 4, "type"), (None, 1, "NULL"),
+                                          (acts(-1, 10, 12), 4, "ESHAPE")])
+def test_group_norm_refusals(x, groups, why):
+    with pytest.raises(dol.DolError, match=why):
+        dol._native.group_norm_workspace(x, groups, 0)
+
+
+def test_group_norm_workspace():
+    assert dol._native.group_norm_workspace(acts(64, 784, 32), 8, 0) == 0               # a slab of a sample at a time
+    assert dol._native.group_norm_workspace(acts(64, 784, 32), 8, 1) >= 2 * 64 * 32 * 4
+    assert dol._native.group_norm_workspace(acts(16, 65536, 128, BF16), 32, 0) > 0
+    assert dol._native.group_norm_workspace(acts(0, 10, 12), 4, 1) >= 0
+
+
+def test_tuples_of_another_shape_and_numbers_past_32_bits():
+    with pytest.raises(TypeError):
+        dol._native.cross_entropy_workspace((0, 1, 2), matrix(4, 16), 0)
+    with pytest.raises(OverflowError):
+        dol._native.cross_entropy_workspace(matrix(1 << 32, 16), matrix(4, 16), 0)
+    with pytest.raises(TypeError):
+        dol._native.cross_entropy_workspace(matrix(8, 16), matrix(4, 16))
+
+
+def test_host_tensors_are_refused():
+    torch = pytest.importorskip("torch")
+    for call in (dol._native.matrix, dol._native.activations):
+        with pytest.raises(AssertionError):
+            call(torch.zeros(2, 3, 4))
+    with pytest.raises(AssertionError):
+        dol._native.values(torch.zeros(3), torch.float32, 3)
+    assert dol._native.matrix(None) is None and dol._native.values(None, torch.float32, 3) is None
+    with pytest.raises(AttributeError):
+        dol._native.matrix(3)
