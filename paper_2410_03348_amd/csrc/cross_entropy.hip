@@ -10,6 +10,7 @@
 // Backward: the classes are taken in pieces.  A piece's logits are computed once more, dl is rounded for the matrix cores and written (a
 // hundred MB or so that the next launch reads), and grad_x and grad_w are two sets of tiles of one launch, which read dl, x and w as they
 // lie, along rows or across them (mfma_tile.h).
+// A few classes, whose logits a workgroup holds, have a form of their own (xent_few_kernel).
 #include "mfma_tile.h"
 
 #include <type_traits>

@@ -68,7 +68,8 @@ __device__ __forceinline__ void wait_and_meet()
 }
 
 // The distance of rows of n elements of 16 bits: an odd number of 256-byte blocks, over which memory's channels change.  Tiles read
-// the same columns of many rows; with a power of two of blocks from row to row they would all be on a few channels.
+// the same columns of many rows; with a power of two of blocks from row to row they would all be on a few channels.  Cross entropy's own
+// layouts and dl, rows so / as long as they are, us: float 4 096 x 512 x 1 024 135 / 139, bf16 8 192 x 256 x 20 000 618 / 632.
 inline int64_t spread(int64_t n)
 {
     if (n < 256) return n;
