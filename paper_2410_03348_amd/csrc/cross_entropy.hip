@@ -495,8 +495,9 @@ __global__ void __launch_bounds__(256) xent_few_kernel(const S *x, int64_t ldx, 
             ones = with_lane32<AddOp>(with_lane16<AddOp>(ones)), rest = with_lane32<AddOp>(with_lane16<AddOp>(rest)), at = with_lane32<AddOp>(with_lane16<AddOp>(at));
             if (n < rows && c4 == 0) {
                 const float lg = log1pf(ones - 1.0f + rest);
-                lse[n] = top == -INFINITY ? top : top + lg;
-                loss[n] = !kept_row(goal, classes) ? 0.0f : top == -INFINITY ? INFINITY : lg + (top - at);
+                const bool none = top == -INFINITY && rest == 0.0f;     // (a NaN is no largest logit either, but then rest is NaN)
+                lse[n] = none ? top : top + lg;
+                loss[n] = !kept_row(goal, classes) ? 0.0f : none ? INFINITY : lg + (top - at);
             }
         } else {
             const float z = n < rows ? lse[n] : 0.0f;

@@ -327,3 +327,31 @@ def test_nearly_certain_rows_of_few_classes(dol):
     dol.cross_entropy(x, w, t, loss, lse, bias=b)
     want = float(np.log1p(9 * np.exp(-20.0)))
     assert abs(float(loss[0]) - want) <= 16 * U * want + 8 * U * want * 20
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("v", [1, 10, 16, 17, 32, 33])
+def test_nan_reaches_its_row_and_the_sums(dol, dtype, v):
+    """A NaN in x, in a bias or in a whole row of logits is no missing class: the row's loss, lse and grad_x are NaN, and so is what sums over
+    it; other rows have what they had.  Left out, the row has no part in anything."""
+    n = 40
+    x, w, b, t, g = make(n, 64, v, getattr(torch, dtype), seed=v)
+    clean = run_and_check(dol, x, w, b, t, g)
+    x[7, 3] = float("nan")
+    others = torch.arange(n, device="cuda") != 7
+    got = [torch.empty_like(q) for q in clean]
+    loss, lse, gx, gw, gb = got
+    for bias in (b, None):
+        dol.cross_entropy(x, w, t, loss, lse, bias=bias)
+        dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=bias, grad_bias=gb)
+        assert bool(torch.isnan(loss[7])) and bool(torch.isnan(lse[7])) and bool(torch.isnan(gx[7]).all())
+        assert bool(torch.isnan(gw).all()) and bool(torch.isnan(gb).all()) and bool(torch.isfinite(gx[others]).all())
+        if bias is not None:
+            assert all(torch.equal(p[others], q[others]) for p, q in zip(got[:3], clean[:3]))
+    t[7] = -1
+    run_and_check(dol, x, w, b, t, g)
+    b[v // 2] = float("nan")
+    x[7, 3] = 0.0
+    dol.cross_entropy(x, w, t, loss, lse, bias=b)
+    dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b, grad_bias=gb)
+    assert bool(torch.isnan(loss[others]).all()) and bool(torch.isnan(lse).all()) and bool(torch.isnan(gx[others]).all()) and float(loss[7]) == 0
