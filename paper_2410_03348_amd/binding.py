@@ -669,16 +669,18 @@ _F, _I = torch.float32, torch.int32
 
 
 def _workspace(given: Optional[torch.Tensor], n: int, device, stream):
-    """(address, bytes, what keeps it): the caller's workspace, or n bytes of torch's allocator, which may hand them out again
-    once the stream that the call is on has passed it."""
+    """(address, bytes, what keeps it): the caller's workspace, or n bytes of torch's allocator.  Those are taken on the stream that the call
+    is on: whoever had them before and has them after is on it too, while work of the current stream may still use what that one freed."""
     if given is not None:
         assert given.is_cuda and given.is_contiguous()
         return given.data_ptr(), given.numel() * given.element_size(), given
     if n == 0:
         return None, 0, None
-    t = torch.empty(n, dtype=torch.uint8, device=device)
-    if stream is not None:
-        t.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+    if stream is None:
+        t = torch.empty(n, dtype=torch.uint8, device=device)
+    else:
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)):
+            t = torch.empty(n, dtype=torch.uint8, device=device)
     return t.data_ptr(), n, t
 
 

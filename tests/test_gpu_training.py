@@ -105,3 +105,51 @@ def test_a_step_in_a_graph(T):
         torch.cuda.synchronize()
         for k in eager.params:
             torch.testing.assert_close(caught.params[k], eager.params[k], rtol=1e-5, atol=1e-6)
+
+
+def test_calls_that_overlap_on_two_streams(T):
+    """Calls without a workspace of the caller's, one on the current stream and one on a side stream with no wait between them: their workspaces
+    are not the same memory, and each result is what the call alone gives."""
+    from paper_2410_03348_amd import binding as dol
+    side = torch.cuda.Stream()
+    # the allocator gives the current stream a block back at once; a call on the side stream does not get it
+    block = torch.empty(3 << 20, dtype=torch.uint8, device="cuda")
+    at = block.data_ptr()
+    del block
+    address, n, keep = dol._workspace(None, 3 << 20, "cuda", side)
+    assert not at <= address < at + n and not address <= at < address + n
+    assert dol._workspace(None, 4096, "cuda", side.cuda_stream)[0] not in (None, at)
+    del keep
+
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    calls = []
+    for k in range(2):
+        x, w = torch.randn(700, 96, generator=gen, device="cuda"), torch.randn(900, 96, generator=gen, device="cuda") * 0.2
+        t = torch.randint(0, 900, (700,), generator=gen, device="cuda", dtype=torch.int32)
+        g, m = torch.rand(700, generator=gen, device="cuda"), torch.randn(200, 300, generator=gen, device="cuda")
+        a = torch.randn(1, 40000, 16, generator=gen, device="cuda")
+        out = [torch.empty(700, device="cuda"), torch.empty(700, device="cuda"), torch.empty_like(x), torch.empty_like(w), torch.empty_like(m),
+               torch.empty_like(a), torch.empty(1, 2, device="cuda"), torch.empty(1, 2, device="cuda"), torch.empty_like(a), torch.empty(16, device="cuda")]
+
+        def call(stream, x=x, w=w, t=t, g=g, m=m, a=a, out=out):
+            loss, lse, gx, gw, u, y, mean, rstd, ga, gg = out
+            dol.cross_entropy(x, w, t, loss, lse, stream=stream)
+            dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, stream=stream)
+            dol.newton_schulz(m, u, stream=stream)
+            dol.group_norm(a, None, None, 2, y, mean, rstd, act="silu", stream=stream)
+            dol.group_norm_backward(a, None, None, 2, mean, rstd, y, ga, gg, None, act="silu", stream=stream)
+
+        call(None)
+        torch.cuda.synchronize()
+        calls.append((call, out, [q.clone() for q in out]))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for _, out, _ in calls:
+            for q in out:
+                q.zero_()
+        torch.cuda.synchronize()
+        calls[0][0](None)
+        calls[1][0](side)
+        torch.cuda.synchronize()
+        for _, out, want in calls:
+            assert all(torch.equal(p, q) for p, q in zip(out, want))

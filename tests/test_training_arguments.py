@@ -80,3 +80,40 @@ def test_host_tensors_are_refused():
     assert dol._native.matrix(None) is None and dol._native.values(None, torch.float32, 3) is None
     with pytest.raises(AttributeError):
         dol._native.matrix(3)
+
+
+def test_a_workspace_is_taken_on_the_stream_of_the_call(monkeypatch):
+    """The allocator hands out again, without waiting, what the same stream has freed: memory for a call on another stream than the current one
+    has to come from that stream's own."""
+    torch = pytest.importorskip("torch")
+    import contextlib
+
+    class Side:
+        pass
+
+    class External(Side):
+        def __init__(self, handle, device=None):
+            self.handle = handle
+
+    current, taken, empty = [None], [], torch.empty
+
+    @contextlib.contextmanager
+    def on(stream):
+        current.append(stream)
+        yield
+        current.pop()
+
+    def recorded(n, dtype, device):
+        taken.append(current[-1])
+        return empty(n, dtype=dtype)
+
+    monkeypatch.setattr(torch.cuda, "Stream", Side)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", External)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch, "empty", recorded)
+    side = Side()
+    dol._workspace(None, 512, "cuda", side)
+    dol._workspace(None, 512, "cuda", 4096)
+    dol._workspace(None, 512, "cuda", None)
+    assert taken[0] is side and taken[1].handle == 4096 and taken[2] is None
+    assert dol._workspace(None, 0, "cuda", side) == (None, 0, None) and len(taken) == 3
