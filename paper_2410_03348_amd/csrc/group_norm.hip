@@ -681,11 +681,11 @@ Plan plan_of(const dol_activations *x, int32_t groups, int vec, bool backward)
         const int64_t slice = int64_t(k) * s.per, lanes = slice / vec;
         if (groups % k || slice % vec || (slice * e < 16 && k < groups)) continue;
         int vecs = kFewVecs;
-        int64_t threads = round_up((s.points + vecs - 1) / int64_t(vecs) * lanes, 64);
+        int64_t threads = round_up((int64_t(s.points) + vecs - 1) / vecs * lanes, 64);
         if (threads > kSlabThreads / 2) {
             if (backward && p.threads && int64_t(s.slice) * e >= 64) break;
             vecs = backward ? kBackwardVecs : kForwardVecs;
-            threads = round_up((s.points + vecs - 1) / int64_t(vecs) * lanes, 64);
+            threads = round_up((int64_t(s.points) + vecs - 1) / vecs * lanes, 64);
             if (threads > (backward ? kSlabThreadsBack : kSlabThreads)) break;
         }
         const int64_t workgroups = int64_t(s.batch) * (groups / k);

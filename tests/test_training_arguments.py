@@ -117,3 +117,10 @@ def test_a_workspace_is_taken_on_the_stream_of_the_call(monkeypatch):
     dol._workspace(None, 512, "cuda", None)
     assert taken[0] is side and taken[1].handle == 4096 and taken[2] is None
     assert dol._workspace(None, 0, "cuda", side) == (None, 0, None) and len(taken) == 3
+
+
+@pytest.mark.parametrize("points", [2 ** 31 - 1, 2 ** 31 - 8, 2 ** 31 - 16, 2 ** 31 - 17])
+@pytest.mark.parametrize("backward", [0, 1])
+def test_group_norm_of_as_many_points_as_32_bits_count(points, backward):
+    """Far more than a slab holds: such a group is shared out over its points, eight workgroups to each of 256 units, a float2 from each."""
+    assert dol._native.group_norm_workspace(acts(1, points, 1), 1, backward) >= 8 * 256 * 8
