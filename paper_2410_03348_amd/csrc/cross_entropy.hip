@@ -243,22 +243,24 @@ __global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes
     // (a tile that lies wholly past the last sample or class repeats the last row; it comes out as zeros all the same)
     T::run(x, min(m0, rows - 1), rows, w, min(n0, classes - 1), classes, 0, steps, smem, acc);
     // What a row of the tile needs.  exp(l - lse) = 2^(l log2e - off) 2^(-rest): what lse log2e loses to rounding goes into the row's factor.
-    // A row that does not count has off = inf and factor 0.
+    // A row that does not count has off = inf and factor 0, which leaves 0 of any finite logit; what a bias or weight that is not finite leaves
+    // is taken away beside the rows that are far.
+    enum { kNear, kFarRow, kNoRow };
     struct Row {
         float off, factor;
-        int32_t target, far;
+        int32_t target, kind;
     };
     Row *info = reinterpret_cast<Row *>(smem);
     lds_barrier();
     for (int r = threadIdx.x; r < T::BM; r += T::NT) {
         const int m = m0 + r;
-        Row q{INFINITY, 0.0f, -1, 0};
+        Row q{INFINITY, 0.0f, -1, kNoRow};
         if (m < rows) {
             const int32_t t = target[m];
             const float z = lse[m];
             if (kept_row(t, classes) && z != -INFINITY) {
                 const float g = grad_loss[m];
-                q.far = !(__builtin_fabsf(z) <= kFar);
+                q.kind = __builtin_fabsf(z) <= kFar ? kNear : kFarRow;
                 q.off = z * kLog2e;
                 q.factor = g * __builtin_amdgcn_exp2f(-__builtin_fmaf(z, kLog2e, -q.off));
                 q.target = t;
@@ -284,11 +286,14 @@ __global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes
                 l[j] = acc[i][j][e] + b[j];
                 v[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(l[j], kLog2e, -q.off)) * q.factor;
             }
-            if (static_cast<uint32_t>(q.target - n) < T::NI || q.far) {
+            if (q.kind == kNoRow) {
+#pragma unroll
+                for (int j = 0; j < T::NI; ++j) v[j] = 0.0f;
+            } else if (static_cast<uint32_t>(q.target - n) < T::NI || q.kind == kFarRow) {
                 const float z = lse[m0 + r], g = grad_loss[m0 + r];
 #pragma unroll
                 for (int j = 0; j < T::NI; ++j) {
-                    if (q.far) v[j] = __builtin_amdgcn_exp2f((l[j] - z) * kLog2e) * g;
+                    if (q.kind == kFarRow) v[j] = __builtin_amdgcn_exp2f((l[j] - z) * kLog2e) * g;
                     // the target's own exp(l - lse) - 1 is small where the network is right: not taken as a difference
                     if (q.target == n + j) v[j] = g * expm1f(l[j] - z);
                 }

@@ -355,3 +355,27 @@ def test_nan_reaches_its_row_and_the_sums(dol, dtype, v):
     dol.cross_entropy(x, w, t, loss, lse, bias=b)
     dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b, grad_bias=gb)
     assert bool(torch.isnan(loss[others]).all()) and bool(torch.isnan(lse).all()) and bool(torch.isnan(gx[others]).all()) and float(loss[7]) == 0
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,d,v", [(40, 64, 10), (40, 64, 33), (300, 64, 700), (2000, 128, 2000)])
+def test_left_out_rows_beside_what_is_not_finite(dol, n, d, v, dtype):
+    """dl of a row that is left out, or has no class, is 0 whatever the biases and weights are: all rows so, all sums are zeros; some rows
+    so, their grad_x is zeros where a bias is NaN or infinite."""
+    x, w, b, t, g = make(n, d, v, getattr(torch, dtype), seed=v)
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    for bad in (float("nan"), float("inf")):
+        bias = b.clone()
+        bias[v // 3] = bad
+        some = t.clone()
+        some[::3] = -1
+        dol.cross_entropy(x, w, some, loss, lse, bias=bias)
+        dol.cross_entropy_backward(x, w, some, lse, g, gx, gw, bias=bias, grad_bias=gb)
+        assert not gx[::3].any() and not loss[::3].any()
+        weight = w.clone()
+        weight[v // 3, 2] = bad
+        for ww, bb in ((w, bias), (weight, b), (weight, bias)):
+            dol.cross_entropy(x, ww, torch.full_like(t, -1), loss, lse, bias=bb)
+            dol.cross_entropy_backward(x, ww, torch.full_like(t, -1), lse, g, None, gw, bias=bb, grad_bias=gb)
+            assert not loss.any() and not gw.any() and not gb.any()
