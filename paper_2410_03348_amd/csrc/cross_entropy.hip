@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(T::NT, 2) xent_sums_kernel(Planes w, Planes x,
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float l = acc[i][j][e];
-                    sum += l == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((l - top) * kLog2e);
+                    sum += l == -INFINITY ? 0.0f : l == top ? 1.0f : __builtin_amdgcn_exp2f((l - top) * kLog2e);      // (inf - inf is NaN)
                 }
             sum = with_lane32<AddOp>(with_lane16<AddOp>(sum));
         }
@@ -207,7 +207,8 @@ __global__ void __launch_bounds__(kJoinWaves * 64) xent_join_kernel(const float2
     auto join = [&](float2 p) {
         if (p.y == 0.0f) return;                    // no logit above -inf
         const float to = fmaxf(top, p.x);
-        s = (s == 0.0f ? 0.0f : s * __builtin_amdgcn_exp2f((top - to) * kLog2e)) + p.y * __builtin_amdgcn_exp2f((p.x - to) * kLog2e);
+        auto scale = [&](float from) { return from == to ? 1.0f : __builtin_amdgcn_exp2f((from - to) * kLog2e); };        // (inf - inf is NaN)
+        s = (s == 0.0f ? 0.0f : s * scale(top)) + p.y * scale(p.x);
         top = to;
     };
     if (n < rows)

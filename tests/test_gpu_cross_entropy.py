@@ -379,3 +379,25 @@ def test_left_out_rows_beside_what_is_not_finite(dol, n, d, v, dtype):
             dol.cross_entropy(x, ww, torch.full_like(t, -1), loss, lse, bias=bb)
             dol.cross_entropy_backward(x, ww, torch.full_like(t, -1), lse, g, None, gw, bias=bb, grad_bias=gb)
             assert not loss.any() and not gw.any() and not gb.any()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,d,v", [(40, 64, 10), (40, 64, 33), (300, 64, 700), (700, 64, 2600)])
+def test_a_logit_of_infinity(dol, n, d, v, dtype):
+    """The sum of the exponentials is inf and so is its log, for one such class or two in different tiles; the loss is inf, or NaN where the
+    target's own logit is inf too.  The other exponentials vanish beside it: grad_bias is -g at the targets."""
+    x, w, b, t, g = make(n, d, v, getattr(torch, dtype), seed=v)
+    loss, lse, gb = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(v, device="cuda")
+    t = (t % (v - 2)) + 1
+    t[0] = 0
+    for at in ((0,), (0, v - 1)):
+        bias = b.clone()
+        bias[list(at)] = float("inf")
+        dol.cross_entropy(x, w, t, loss, lse, bias=bias)
+        assert bool((lse == float("inf")).all()) and bool((loss[1:] == float("inf")).all()) and bool(torch.isnan(loss[0]))
+        dol.cross_entropy_backward(x, w, t, lse, g, None, None, bias=bias, grad_bias=gb)
+        want = torch.zeros(v, dtype=torch.float64, device="cuda").index_add_(0, t.long(), -g.double())
+        size = torch.zeros(v, dtype=torch.float64, device="cuda").index_add_(0, t.long(), g.double().abs())
+        rest = torch.ones(v, dtype=torch.bool, device="cuda")
+        rest[list(at)] = False
+        assert bool(torch.isnan(gb[list(at)]).all()) and bool(((gb.double() - want).abs() <= 32 * U * size)[rest].all())
