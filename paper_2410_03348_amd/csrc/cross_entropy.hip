@@ -68,6 +68,10 @@ struct Source { using T = float; };
 template <>
 struct Source<1> { using T = __bf16; };
 
+// Plane k of N.
+template <int N>
+__device__ __forceinline__ uint32_t plane_of(int k, float &x) { return N > 1 && k == 0 ? take_first_plane(x) : take_plane<__bf16>(x); }
+
 __device__ __forceinline__ bool kept_row(int32_t target, int32_t classes) { return target >= 0 && target < classes; }
 
 // ---------------------------------------------------------------- layouts for the matrix cores
@@ -116,7 +120,7 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(Pack p0, Pack p1)
         u32x4 w;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = take_plane<__bf16>(v[2 * k]), hi = take_plane<__bf16>(v[2 * k + 1]);
+            const uint32_t lo = plane_of<P>(q, v[2 * k]), hi = plane_of<P>(q, v[2 * k + 1]);
             w[k] = lo | hi << 16;
         }
         *reinterpret_cast<u32x4 *>(p.out + (q * p.out_rows + r) * p.out_ld + c) = w;
@@ -304,7 +308,7 @@ __global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes
 #pragma unroll
             for (int p = 0; p < Q; ++p) {
                 u32x2 out;
-                const uint32_t w0 = take_plane<__bf16>(v[0]), w1 = take_plane<__bf16>(v[1]), w2 = take_plane<__bf16>(v[2]), w3 = take_plane<__bf16>(v[3]);
+                const uint32_t w0 = plane_of<Q>(p, v[0]), w1 = plane_of<Q>(p, v[1]), w2 = plane_of<Q>(p, v[2]), w3 = plane_of<Q>(p, v[3]);
                 out[0] = w0 | w1 << 16, out[1] = w2 | w3 << 16;
                 *reinterpret_cast<u32x2 *>(to + (p * n_pad + r) * ld) = out;
             }

@@ -40,7 +40,7 @@ __device__ __forceinline__ uint32_t bits16(float x)
     return __builtin_bit_cast(uint16_t, static_cast<E>(x));
 }
 
-// x rounded to E, and what is left of it for the next plane (nothing, where x or its rounding is not finite: inf - inf is NaN).
+// x rounded to E, and what is left of it for the next plane (nothing, where x is not finite: inf - inf is NaN).
 template <typename E>
 __device__ __forceinline__ uint32_t take_plane(float &x)
 {
@@ -48,6 +48,16 @@ __device__ __forceinline__ uint32_t take_plane(float &x)
     const float r = x - static_cast<float>(h);
     x = r == r ? r : 0.0f;
     return __builtin_bit_cast(uint16_t, h);
+}
+
+// The first of several bf16 planes: what would round to infinity (from 3.396e38 on) takes the largest number instead, and the next planes have
+// the rest, infinity or NaN where that is what x is.
+__device__ __forceinline__ uint32_t take_first_plane(float &x)
+{
+    constexpr float kMost = 3.38953139e38f;
+    const uint32_t h = bits16<__bf16>(__builtin_amdgcn_fmed3f(x, -kMost, kMost));
+    x -= __uint_as_float(h << 16);
+    return h;
 }
 
 // 64 lanes' 16 bytes straight to LDS, lane l's at lds + 16 l (lds: the same in every lane).

@@ -401,3 +401,26 @@ def test_a_logit_of_infinity(dol, n, d, v, dtype):
         rest = torch.ones(v, dtype=torch.bool, device="cuda")
         rest[list(at)] = False
         assert bool(torch.isnan(gb[list(at)]).all()) and bool(((gb.double() - want).abs() <= 32 * U * size)[rest].all())
+
+
+@pytest.mark.parametrize("n,d,v", [(40, 64, 10), (40, 64, 33), (300, 64, 700), (2000, 128, 2000)])
+def test_numbers_at_the_end_of_the_range(dol, n, d, v):
+    """x, weight and grad_loss of 3.4e38, which bf16 does not hold: what 32 bits can say of the results is said."""
+    top = 3.4e38
+    x, w, b, t, g = make(n, d, v, torch.float32, seed=v)
+    x[5, 0], g[5] = top, 0.5
+    w[:, 0] = 2.0 ** -126 * torch.where(w[:, 0] > 0, 1.0, -1.0)
+    run_and_check(dol, x, w, b, t, g)
+    x, w, b, t, g = make(n, d, v, torch.float32, seed=v)
+    w[3, 0], t[t == 3] = -top, 4
+    x[:, 0] = 2.0 ** -126
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    dol.cross_entropy(x, w, t, loss, lse, bias=b)
+    ref = reference(x, w, b, t, g)
+    bar = ref["err_l"].max(axis=1) + 8 * U * (1 + np.abs(ref["lse"]))
+    within(lse, ref["lse"], bar, "lse")
+    within(loss, ref["loss"], 2 * bar, "loss")
+    for dtype in (torch.float32, torch.bfloat16)[: 1 + (n <= 512)]:
+        x, w, b, t, g = make(n, d, v, dtype, seed=v)
+        g[5] = top
+        run_and_check(dol, x * 2.0 ** -12, w * 2.0 ** -12, b, t, g)
