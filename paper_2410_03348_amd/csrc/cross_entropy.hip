@@ -291,16 +291,18 @@ __global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes
                 l[j] = acc[i][j][e] + b[j];
                 v[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(l[j], kLog2e, -q.off)) * q.factor;
             }
-            if (q.kind == kNoRow) {
+            if (static_cast<uint32_t>(q.target - n) < T::NI || q.kind != kNear) {
+                if (q.kind == kNoRow) {
 #pragma unroll
-                for (int j = 0; j < T::NI; ++j) v[j] = 0.0f;
-            } else if (static_cast<uint32_t>(q.target - n) < T::NI || q.kind == kFarRow) {
-                const float z = lse[m0 + r], g = grad_loss[m0 + r];
+                    for (int j = 0; j < T::NI; ++j) v[j] = 0.0f;
+                } else {
+                    const float z = lse[m0 + r], g = grad_loss[m0 + r];
 #pragma unroll
-                for (int j = 0; j < T::NI; ++j) {
-                    if (q.kind == kFarRow) v[j] = __builtin_amdgcn_exp2f((l[j] - z) * kLog2e) * g;
-                    // the target's own exp(l - lse) - 1 is small where the network is right: not taken as a difference
-                    if (q.target == n + j) v[j] = g * expm1f(l[j] - z);
+                    for (int j = 0; j < T::NI; ++j) {
+                        if (q.kind == kFarRow) v[j] = __builtin_amdgcn_exp2f((l[j] - z) * kLog2e) * g;
+                        // the target's own exp(l - lse) - 1 is small where the network is right: not taken as a difference
+                        if (q.target == n + j) v[j] = g * expm1f(l[j] - z);
+                    }
                 }
             }
 #pragma unroll
