@@ -56,6 +56,15 @@ struct Args {
         if (x == -1 && PyErr_Occurred()) bad = true;
         return x;
     }
+    int32_t num32(int k)
+    {
+        const int64_t x = num(k);
+        if (!bad && x != static_cast<int32_t>(x)) {
+            PyErr_Format(PyExc_OverflowError, "argument %d: past 32 bits", k);
+            bad = true;
+        }
+        return static_cast<int32_t>(x);
+    }
     double real(int k)
     {
         if (bad) return 0.0;
@@ -265,7 +274,7 @@ PyObject *cross_entropy_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     Args a(v, n, 3);
     Matrix x(a, 0), w(a, 1);
-    const int32_t back = static_cast<int32_t>(a.num(2));
+    const int32_t back = a.num32(2);
     if (a.bad) return nullptr;
     int64_t need = 0;
     const dol_status st = dol_cross_entropy_workspace(x.p(), w.p(), back, &need);
@@ -302,7 +311,7 @@ PyObject *group_norm_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     Args a(v, n, 3);
     Activations x(a, 0);
-    const int32_t groups = static_cast<int32_t>(a.num(1)), back = static_cast<int32_t>(a.num(2));
+    const int32_t groups = a.num32(1), back = a.num32(2);
     if (a.bad) return nullptr;
     int64_t need = 0;
     const dol_status st = dol_group_norm_workspace(x.p(), groups, back, &need);
@@ -313,7 +322,7 @@ PyObject *group_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     Args a(v, n, 12);
     Activations x(a, 0), y(a, 6);
-    const int32_t groups = static_cast<int32_t>(a.num(1)), act = static_cast<int32_t>(a.num(5));
+    const int32_t groups = a.num32(1), act = a.num32(5);
     auto *gamma = a.ptr<float>(2), *beta = a.ptr<float>(3);
     const float eps = static_cast<float>(a.real(4));
     auto *mean = a.ptr<float>(7), *rstd = a.ptr<float>(8);
@@ -327,7 +336,7 @@ PyObject *group_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     Args a(v, n, 14);
     Activations x(a, 0), gy(a, 7), gx(a, 8);
-    const int32_t groups = static_cast<int32_t>(a.num(1)), act = static_cast<int32_t>(a.num(4));
+    const int32_t groups = a.num32(1), act = a.num32(4);
     auto *gamma = a.ptr<float>(2), *beta = a.ptr<float>(3);
     auto *mean = a.ptr<float>(5), *rstd = a.ptr<float>(6);
     auto *gg = a.ptr<float>(9), *gb = a.ptr<float>(10);
@@ -341,7 +350,7 @@ PyObject *newton_schulz_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     Args a(v, n, 2);
     Matrix g(a, 0);
-    const int32_t batch = static_cast<int32_t>(a.num(1));
+    const int32_t batch = a.num32(1);
     if (a.bad) return nullptr;
     int64_t need = 0;
     const dol_status st = dol_newton_schulz_workspace(g.p(), batch, &need);
@@ -353,7 +362,7 @@ PyObject *newton_schulz(PyObject *, PyObject *const *v, Py_ssize_t n)
     Args a(v, n, 13);
     Matrix g(a, 0), o(a, 2);
     const int64_t g_stride = a.num(1), o_stride = a.num(3);
-    const int32_t batch = static_cast<int32_t>(a.num(4)), steps = static_cast<int32_t>(a.num(5));
+    const int32_t batch = a.num32(4), steps = a.num32(5);
     const float abc[3] = {static_cast<float>(a.real(6)), static_cast<float>(a.real(7)), static_cast<float>(a.real(8))};
     const float eps = static_cast<float>(a.real(9));
     auto *ws = a.ptr<void>(10);

@@ -124,3 +124,14 @@ def test_a_workspace_is_taken_on_the_stream_of_the_call(monkeypatch):
 def test_group_norm_of_as_many_points_as_32_bits_count(points, backward):
     """Far more than a slab holds: such a group is shared out over its points, eight workgroups to each of 256 units, a float2 from each."""
     assert dol._native.group_norm_workspace(acts(1, points, 1), 1, backward) >= 8 * 256 * 8
+
+
+def test_plain_numbers_past_32_bits():
+    """Not cut to the 32 bits of the C call, where they would name another size."""
+    big, null = 1 << 32, None
+    for call in (lambda: dol._native.group_norm_workspace(acts(2, 10, 12), big + 4, 1), lambda: dol._native.newton_schulz_workspace(matrix(100, 200), big + 1),
+                 lambda: dol._native.group_norm(acts(2, 10, 12), big + 4, null, null, 1e-5, 0, acts(2, 10, 12), null, null, null, 0, 0),
+                 lambda: dol._native.newton_schulz(matrix(10, 20), 0, matrix(10, 20), 0, 0, big + 5, 1.0, 0.0, 0.0, 0.0, null, 0, 0),
+                 lambda: dol._native.group_norm_backward(acts(0, 10, 12), -big + 4, null, null, 0, null, null, acts(0, 10, 12), acts(0, 10, 12), null, null, null, 0, 0)):
+        with pytest.raises(OverflowError):
+            call()
