@@ -627,7 +627,7 @@ dol_status check_activations(const dol_activations *t, const dol_activations *li
     if (like && (t->batch != like->batch || t->points != like->points || t->channels != like->channels))
         return fail(DOL_ESHAPE, "%s is %d x %d x %d, x is %d x %d x %d", name, t->batch, t->points, t->channels, like->batch, like->points, like->channels);
     if (t->ld_point < t->channels) return fail(DOL_ESHAPE, "%s.ld_point = %lld smaller than its %d channels", name, static_cast<long long>(t->ld_point), t->channels);
-    if (t->points > 0 && t->ld_batch < (t->points - 1) * t->ld_point + t->channels && t->batch > 1)
+    if (t->points > 0 && t->batch > 1 && !apart(t->points, t->ld_point, t->batch, t->ld_batch, t->channels))
         return fail(DOL_ESHAPE, "%s.ld_batch = %lld: samples overlap", name, static_cast<long long>(t->ld_batch));
     if (t->batch > 0 && t->points > 0 && t->channels > 0) {
         if (!t->data) return fail(DOL_EINVAL, "%s.data is NULL", name);

@@ -24,6 +24,11 @@ dol_status hip_fail(hipError_t e, const char *what);
 // Checks of the training operators' arguments (cross_entropy.hip).
 dol_status check_matrix(const dol_matrix *m, const char *name);
 dol_status check_workspace(const void *workspace, int64_t has, int64_t needs);
+// Whether `outer` sets of `inner` rows of n elements share none: sets one behind the other, or the rows of all sets side by side.
+inline bool apart(int64_t inner, int64_t ld_inner, int64_t outer, int64_t ld_outer, int64_t n)
+{
+    return ld_outer >= (inner - 1) * ld_inner + n || (ld_outer >= n && ld_inner >= (outer - 1) * ld_outer + n);
+}
 
 #define DOL_HIP(call)                                        \
     do {                                                     \

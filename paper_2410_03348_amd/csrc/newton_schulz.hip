@@ -573,7 +573,7 @@ dol_status dol_newton_schulz(const dol_matrix *g, int64_t g_stride, const dol_ma
     if (dol_status s = check_operand(out, out_stride, batch, "out")) return s;
     if (g->dtype != out->dtype) return fail(DOL_EINVAL, "g and out are of different types");
     if (g->rows != out->rows || g->cols != out->cols) return fail(DOL_ESHAPE, "g is %d x %d, out %d x %d", g->rows, g->cols, out->rows, out->cols);
-    if (batch > 1 && out_stride < int64_t(out->rows - 1) * out->ld + out->cols) return fail(DOL_ESHAPE, "out's matrices overlap: %lld elements apart", static_cast<long long>(out_stride));
+    if (batch > 1 && !apart(out->rows, out->ld, batch, out_stride, out->cols)) return fail(DOL_ESHAPE, "out's matrices overlap: %lld elements apart", static_cast<long long>(out_stride));
     if (steps < 1 || steps > 64) return fail(DOL_EINVAL, "%d steps, not 1 to 64", steps);
     if (!coefficients) return fail(DOL_EINVAL, "coefficients is NULL");
     if (!(eps >= 0.0f)) return fail(DOL_EINVAL, "eps = %g is not a number of at least 0", static_cast<double>(eps));

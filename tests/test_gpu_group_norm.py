@@ -261,3 +261,16 @@ def test_empty_and_refusals(dol):
     with pytest.raises(KeyError):
         dol.group_norm(x, gamma, beta, 2, y, None, None, act="swish")
     assert bool((y == 5).all()) and bool((mean == 5).all())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("b,p,c,groups", [(3, 150, 40, 5), (2, 30000, 20, 5), (4, 1, 8, 2)])
+def test_samples_side_by_side(dol, b, p, c, groups, dtype):
+    """Views of [points, batch, channels]: samples interleaved, in the inputs and in what is written."""
+    dtype = getattr(torch, dtype)
+    x, gamma, beta, dy = make(b, p, c, dtype, seed=14)
+    want = run_and_check(dol, x, gamma, beta, groups, dy)
+    views = [torch.empty(p, b, c, dtype=dtype, device="cuda").transpose(0, 1) for _ in range(4)]
+    views[0].copy_(x), views[1].copy_(dy)
+    got = run_and_check(dol, views[0], gamma, beta, groups, views[1], y=views[2], dx=views[3])
+    assert torch.equal(got["y"], want["y"]) and torch.equal(got["grad_x"], want["grad_x"])

@@ -180,3 +180,19 @@ def test_empty_and_refusals(dol):
         with pytest.raises(AssertionError):
             dol.newton_schulz(bad, out)
     assert bool((out == 5).all())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,cols", [(33, 70), (70, 33), (300, 200)])
+def test_matrices_side_by_side(dol, rows, cols, dtype):
+    """Views of [rows, batch, cols]: one row of each matrix after the other."""
+    dtype = getattr(torch, dtype)
+    g = normal((3, rows, cols), dtype, seed=10)
+    want = torch.empty_like(g)
+    dol.newton_schulz(g, want)
+    there, out = (torch.empty(rows, 3, cols, dtype=dtype, device="cuda").transpose(0, 1) for _ in range(2))
+    there.copy_(g)
+    dol.newton_schulz(there, out)
+    for k in range(3):
+        check(out[k], g[k])
+    assert torch.equal(out, want)

@@ -135,3 +135,12 @@ def test_plain_numbers_past_32_bits():
                  lambda: dol._native.group_norm_backward(acts(0, 10, 12), -big + 4, null, null, 0, null, null, acts(0, 10, 12), acts(0, 10, 12), null, null, null, 0, 0)):
         with pytest.raises(OverflowError):
             call()
+
+
+def test_layouts_with_samples_side_by_side():
+    """[points][batch][channels] in memory is as good as [batch][points][channels]; one element less to a point and samples overlap."""
+    for b, p, c, ld_batch, ld_point in ((3, 10, 12, 12, 36), (3, 10, 12, 13, 40), (2, 2, 4, 4, 8), (2, 2, 4, 8, 4)):
+        assert dol._native.group_norm_workspace((F32, b, p, c, ld_batch, ld_point, 4096), 2, 1) > 0
+    for b, p, c, ld_batch, ld_point in ((3, 10, 12, 12, 35), (3, 10, 12, 11, 40), (3, 10, 12, 0, 12), (2, 2, 4, 4, 4), (3, 10, 12, 119, 12)):
+        with pytest.raises(dol.DolError, match="overlap"):
+            dol._native.group_norm_workspace((F32, b, p, c, ld_batch, ld_point, 4096), 2, 1)
