@@ -430,6 +430,10 @@ typedef struct {
 dol_status dol_cross_entropy_workspace(const dol_matrix *x, const dol_matrix *weight, int32_t backward, int64_t *bytes);
 dol_status dol_cross_entropy(const dol_matrix *x, const dol_matrix *weight, const float *bias, const int32_t *target, float *loss,
                              float *lse, void *workspace, int64_t workspace_bytes, void *hip_stream);
+/* The kernels that multiply for these operands in the forward (backward = 0) or backward call and the tiles that they take, e.g.
+ * "xent_dlogits_kernel 128x128x64, xent_products_kernel 64x64x64"; "xent_few_kernel" where a few classes have a form of their own, ""
+ * where the operands are rejected or have no rows.  Host only; valid until the calling thread's next call of this function. */
+const char *dol_cross_entropy_kernel(const dol_matrix *x, const dol_matrix *weight, int32_t backward);
 /* Its gradients: dl[i, v] = grad_loss[i] (exp(l[i, v] - lse[i]) - [v = target[i]]) for the rows that count, 0 for rows that are left out
  * or have no class (whatever x holds there, also NaN, and whatever grad_loss says);
  *   grad_x = dl weight,   grad_weight = dl^T x,   grad_bias[v] = sum_i dl[i, v].
@@ -448,6 +452,8 @@ dol_status dol_cross_entropy_backward(const dol_matrix *x, const dol_matrix *wei
  * own rounding leaves some 2.4e-3 of it.
  * DOL_EUNSUPPORTED where the coefficients let singular values pass 64, for sides above 2^20 and for more than 65 535 matrices. */
 dol_status dol_newton_schulz_workspace(const dol_matrix *g, int32_t batch, int64_t *bytes);
+/* As dol_cross_entropy_kernel: "ns_symmetric_kernel 128x128, ns_apply_kernel 64x64", or "ns_small_kernel". */
+const char *dol_newton_schulz_kernel(const dol_matrix *g, int32_t batch);
 dol_status dol_newton_schulz(const dol_matrix *g, int64_t g_stride, const dol_matrix *out, int64_t out_stride, int32_t batch,
                              int32_t steps, const float *coefficients, float eps, void *workspace, int64_t workspace_bytes,
                              void *hip_stream);

@@ -689,6 +689,11 @@ def cross_entropy_workspace(x: torch.Tensor, weight: torch.Tensor, backward: boo
     return _native.cross_entropy_workspace(_matrix(x), _matrix(weight), int(backward))
 
 
+def cross_entropy_kernel(x: torch.Tensor, weight: torch.Tensor, backward: bool = False) -> str:
+    """The kernels that multiply for these operands, and their tiles."""
+    return _native.cross_entropy_kernel(_matrix(x), _matrix(weight), int(backward))
+
+
 def cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
                   bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """loss[i] = lse[i] - (x[i] . weight[target[i]] + bias[target[i]]), lse the log of the sum of the exponentials over all classes.
@@ -727,6 +732,12 @@ def _matrices(t: torch.Tensor):
 def newton_schulz_workspace(g: torch.Tensor) -> int:
     m, _, batch = _matrices(g)
     return _native.newton_schulz_workspace(m, batch)
+
+
+def newton_schulz_kernel(g: torch.Tensor) -> str:
+    """The kernels that multiply for these matrices, and their tiles."""
+    m, _, batch = _matrices(g)
+    return _native.newton_schulz_kernel(m, batch)
 
 
 def newton_schulz(g: torch.Tensor, out: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,

@@ -13,6 +13,7 @@
 // A few classes, whose logits a workgroup holds, have a form of their own (xent_few_kernel).
 #include "mfma_tile.h"
 
+#include <cstdio>
 #include <type_traits>
 #include <utility>
 
@@ -949,6 +950,25 @@ dol_status dol_cross_entropy_workspace(const dol_matrix *x, const dol_matrix *we
     *bytes = 0;
     if (x->rows > 0) *bytes = with_planes(x, [&](auto p, auto q) { return lay_out<p.value, q.value>(x, weight, backward, nullptr); }).bytes;
     return DOL_OK;
+}
+
+const char *dol_cross_entropy_kernel(const dol_matrix *x, const dol_matrix *weight, int32_t backward)
+{
+    static thread_local char name[96];
+    if (check_operands(x, weight) != DOL_OK || x->rows == 0) return "";
+    if (few_classes(x, weight)) return "xent_few_kernel";
+    with_planes(x, [&](auto p, auto q) {
+        using Z = Shapes<p.value, q.value>;
+        const Layout L = lay_out<p.value, q.value>(x, weight, backward, nullptr);
+        auto at = [&](const char *kernel, int have, auto z) {
+            using T = typename decltype(z)::Tile;
+            return snprintf(name + have, sizeof name - have, "%s%s %dx%dx%d", have ? ", " : "", kernel, T::BM, T::BN, T::BK);
+        };
+        const int n = by_size(L.size, Type<typename Z::Big>(), Type<typename Z::Small>(), Type<typename Z::Tiny>(),
+                              [&](auto z) { return at(backward ? "xent_dlogits_kernel" : "xent_sums_kernel", 0, z); });
+        if (backward) by_size(L.product_size, Type<typename Z::BigX>(), Type<typename Z::SmallX>(), Type<typename Z::TinyX>(), [&](auto z) { return at("xent_products_kernel", n, z); });
+    });
+    return name;
 }
 
 dol_status dol_cross_entropy(const dol_matrix *x, const dol_matrix *weight, const float *bias, const int32_t *target, float *loss, float *lse,

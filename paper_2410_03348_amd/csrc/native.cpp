@@ -281,6 +281,14 @@ PyObject *cross_entropy_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
     return bytes(st, need);
 }
 
+PyObject *cross_entropy_kernel(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 3);
+    Matrix x(a, 0), w(a, 1);
+    const int32_t back = a.num32(2);
+    return a.bad ? nullptr : PyUnicode_FromString(dol_cross_entropy_kernel(x.p(), w.p(), back));
+}
+
 PyObject *cross_entropy(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     Args a(v, n, 9);
@@ -355,6 +363,14 @@ PyObject *newton_schulz_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
     int64_t need = 0;
     const dol_status st = dol_newton_schulz_workspace(g.p(), batch, &need);
     return bytes(st, need);
+}
+
+PyObject *newton_schulz_kernel(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 2);
+    Matrix g(a, 0);
+    const int32_t batch = a.num32(1);
+    return a.bad ? nullptr : PyUnicode_FromString(dol_newton_schulz_kernel(g.p(), batch));
 }
 
 PyObject *newton_schulz(PyObject *, PyObject *const *v, Py_ssize_t n)
@@ -525,9 +541,11 @@ PyMethodDef g_methods[] = {
     {"fold_apply2", DOL_FAST(fold_apply2)},
     {"dtkp_fold_apply2", DOL_FAST(dtkp_fold_apply2)},
     {"cross_entropy_workspace", DOL_FAST(cross_entropy_workspace)},
+    {"cross_entropy_kernel", DOL_FAST(cross_entropy_kernel)},
     {"cross_entropy", DOL_FAST(cross_entropy)},
     {"cross_entropy_backward", DOL_FAST(cross_entropy_backward)},
     {"newton_schulz_workspace", DOL_FAST(newton_schulz_workspace)},
+    {"newton_schulz_kernel", DOL_FAST(newton_schulz_kernel)},
     {"newton_schulz", DOL_FAST(newton_schulz)},
     {"group_norm_workspace", DOL_FAST(group_norm_workspace)},
     {"group_norm", DOL_FAST(group_norm)},

@@ -11,6 +11,7 @@
 #include "mfma_tile.h"
 
 #include <cmath>
+#include <cstdio>
 
 namespace dol {
 namespace {
@@ -433,6 +434,17 @@ double bound_of(const float *k, double most, bool of_x)
     return top;
 }
 
+// Which tiles the symmetric products (half) or B X take: 2 is 256 x 256, 1 is 128 x 128, 0 is 64 x 64.
+// The largest that fill the chip well enough: larger ones load less for what they do, and loads bound them all.  Of 256 x 256
+// half a chip (float 4096 x 4096 takes 4.52 ms so and 4.77 with 128 x 128, bf16 1.67 and 1.87).  Of 128 x 128 from these numbers on,
+// beside 64 x 64, us: float 1400 x 1500 400 / 486, 2000 x 2000 797 / 1 150, 1280 x 2500 423 / 592, but with 66 symmetric ones
+// 599 / 400; bf16 1792 x 1792 312 / 372, 1280 x 2500 263 / 301, but with 192 of them for B X 246 / 230 and with 136 symmetric 433 / 399.
+int size_of(int planes, int64_t rows, int64_t cols, bool half, int32_t batch)
+{
+    auto many = [&](int t) { return rows % t || cols % t ? 0 : (half ? rows / t * (rows / t + 1) / 2 : rows / t * (cols / t)) * batch; };
+    return many(256) >= kUnits / 2 ? 2 : many(128) >= (planes == 1 ? 193 : half ? 100 : 128) ? 1 : 0;
+}
+
 template <typename K>
 dol_status ready(K kernel, int lds)
 {
@@ -497,19 +509,11 @@ dol_status newton_schulz(const Layout &L, const dol_matrix *g, int64_t g_stride,
                                                                       L.mp, L.np);
     DOL_HIP(hipGetLastError());
     auto two = [](int n) { return std::ldexp(1.0f, n); };
-    // The largest tiles that fill the chip well enough: larger ones load less for what they do, and loads bound them all.  Of 256 x 256
-    // half a chip (float 4096 x 4096 takes 4.52 ms so and 4.77 with 128 x 128, bf16 1.67 and 1.87).  Of 128 x 128 from these numbers on,
-    // beside 64 x 64, us: float 1400 x 1500 400 / 486, 2000 x 2000 797 / 1 150, 1280 x 2500 423 / 592, but with 66 symmetric ones
-    // 599 / 400; bf16 1792 x 1792 312 / 372, 1280 x 2500 263 / 301, but with 192 of them for B X 246 / 230 and with 136 symmetric 433 / 399.
-    auto size_of = [&](int64_t rows, int64_t cols, bool half) {
-        auto many = [&](int t) { return rows % t || cols % t ? 0 : (half ? rows / t * (rows / t + 1) / 2 : rows / t * (cols / t)) * batch; };
-        return many(256) >= kUnits / 2 ? 2 : many(128) >= (P == 1 ? 193 : half ? 100 : 128) ? 1 : 0;
-    };
     for (int32_t t = 0; t < steps; ++t) {
         const int from = t & 1;
         for (int poly = 0; poly < 2; ++poly) {
             const float alpha = poly ? k[2] * two(e.b - 2 * e.a) : two(e.a - 2 * e.x), beta = poly ? k[1] * two(e.b - e.a) : 0.0f;
-            const int size = size_of(L.mp, L.mp, true);
+            const int size = size_of(P, L.mp, L.mp, true, batch);
             if (dol_status s = size == 2   ? symmetric<typename Z::template Big<kRows, kRows>>(L, batch, poly, from, alpha, beta, st)
                                : size == 1 ? symmetric<typename Z::template Mid<kRows, kRows>>(L, batch, poly, from, alpha, beta, st)
                                            : symmetric<typename Z::template Small<kRows, kRows>>(L, batch, poly, from, alpha, beta, st))
@@ -517,7 +521,7 @@ dol_status newton_schulz(const Layout &L, const dol_matrix *g, int64_t g_stride,
         }
         const bool last = t == steps - 1;
         const float alpha = last ? two(-e.b - e.x) : two(-e.b), beta = last ? k[0] * two(-e.x) : k[0];
-        const int size = size_of(L.mp, L.np, false);
+        const int size = size_of(P, L.mp, L.np, false, batch);
         if (last && L.tall) {
             if (dol_status s = size == 2   ? apply<typename Z::template Big<kRows, kCols>, S, true>(L, batch, from, last, alpha, beta, out, out_stride, st)
                                : size == 1 ? apply<typename Z::template Mid<kRows, kCols>, S, true>(L, batch, from, last, alpha, beta, out, out_stride, st)
@@ -562,6 +566,19 @@ dol_status dol_newton_schulz_workspace(const dol_matrix *g, int32_t batch, int64
         return fail(DOL_EUNSUPPORTED, "%d matrices of %d x %d: more than %d, or a side above %d", batch, g->rows, g->cols, kMostBatch, kMostSide);
     *bytes = batch == 0 || g->rows == 0 || g->cols == 0 || small(g) ? 0 : lay_out(g, batch, g->dtype == DOL_BF16 ? 1 : 2, nullptr).bytes;
     return DOL_OK;
+}
+
+const char *dol_newton_schulz_kernel(const dol_matrix *g, int32_t batch)
+{
+    static thread_local char name[64];
+    int64_t needs = 0;
+    if (dol_newton_schulz_workspace(g, batch, &needs) != DOL_OK || batch == 0 || g->rows == 0 || g->cols == 0) return "";
+    if (small(g)) return "ns_small_kernel";
+    const int planes = g->dtype == DOL_BF16 ? 1 : 2;
+    const Layout L = lay_out(g, batch, planes, nullptr);
+    const int side[] = {64, 128, 256}, a = side[size_of(planes, L.mp, L.mp, true, batch)], b = side[size_of(planes, L.mp, L.np, false, batch)];
+    snprintf(name, sizeof name, "ns_symmetric_kernel %dx%d, ns_apply_kernel %dx%d", a, a, b, b);
+    return name;
 }
 
 dol_status dol_newton_schulz(const dol_matrix *g, int64_t g_stride, const dol_matrix *out, int64_t out_stride, int32_t batch, int32_t steps,

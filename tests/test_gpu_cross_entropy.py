@@ -424,3 +424,56 @@ def test_numbers_at_the_end_of_the_range(dol, n, d, v):
         x, w, b, t, g = make(n, d, v, dtype, seed=v)
         g[5] = top
         run_and_check(dol, x * 2.0 ** -12, w * 2.0 ** -12, b, t, g)
+
+
+# Every tile that logits and products can take, with several tiles and steps of k each way and remainders in all of them.
+FORMS = [("float32", 2000, 130, 2000, "128x128x32", "128x128x32"), ("float32", 1000, 300, 5200, "128x256x32", "128x256x32"),
+         ("float32", 300, 256, 3001, "64x64x64", "128x128x32"), ("bfloat16", 2000, 130, 2000, "128x128x64", "128x128x64"),
+         ("bfloat16", 2001, 192, 1999, "128x128x64", "128x128x64"), ("bfloat16", 2500, 320, 8200, "256x256x64", "256x256x64"),
+         ("bfloat16", 2500, 300, 8201, "256x256x64", "256x256x64"), ("bfloat16", 400, 130, 5000, "128x128x64", "128x128x32"),
+         ("bfloat16", 511, 200, 24401, "256x256x64", "128x128x32"), ("bfloat16", 300, 64, 300, "64x64x64", "64x64x64")]
+
+
+@pytest.mark.parametrize("dtype,n,d,v,logits,products", FORMS)
+def test_forms(dol, dtype, n, d, v, logits, products):
+    x, w, b, t, g = make(n, d, v, getattr(torch, dtype), seed=d)
+    assert dol.cross_entropy_kernel(x, w) == "xent_sums_kernel " + logits
+    assert dol.cross_entropy_kernel(x, w, True) == "xent_dlogits_kernel %s, xent_products_kernel %s" % (logits, products)
+    t[::11] = -1
+    got = run_and_check(dol, x, w, b, t, g)
+    again = [torch.empty_like(q) for q in got]
+    loss, lse, gx, gw, gb = again
+    dol.cross_entropy(x, w, t, loss, lse, bias=b)
+    dol.cross_entropy_backward(x, w, t, lse, g, gx, None, bias=b)
+    dol.cross_entropy_backward(x, w, t, lse, g, None, gw, bias=b, grad_bias=gb)
+    assert all(torch.equal(p, q) for p, q in zip(got, again))
+
+
+@pytest.mark.parametrize("dtype,n,d,v,logits,products", FORMS)
+def test_forms_with_masks_and_strides(dol, dtype, n, d, v, logits, products):
+    """Rows left out that hold NaN, classes taken out (the target's own among them, and whole tiles of them), rows of other strides."""
+    x, w, b, t, g = make(n, d, v, getattr(torch, dtype), seed=d + 1)
+    t[::7] = -1
+    t[3::29] = v
+    out = (t < 0) | (t >= v)
+    x[out], g[out] = float("nan"), float("nan")
+    b[v // 3: v // 3 + 600] = float("-inf")
+    b[v - 1] = float("-inf")
+    x, w = padded(x, 3, float("nan"))[1], padded(w, 5, float("nan"))[1]
+    assert dol.cross_entropy_kernel(x, w, True) == "xent_dlogits_kernel %s, xent_products_kernel %s" % (logits, products)
+    loss, _, gx, _, _ = run_and_check(dol, x, w, b, t, g, pad=3)
+    assert not loss[out].any() and not gx[out].any()
+    assert bool(torch.isinf(loss).any()) == bool((~out & torch.isinf(b[t.clamp(0, v - 1).long()])).any())
+
+
+@pytest.mark.parametrize("n,d,v", [(1, 50, 70), (64, 128, 360), (300, 64, 300), (512, 130, 5000), (511, 200, 24401)])
+def test_dl_of_few_rows_in_two_planes(dol, n, d, v):
+    """bf16 up to 512 rows: dl has 2^-17 of rounding in its two planes, so that the gradients err by that and by the rounding of the result."""
+    x, w, b, t, g = make(n, d, v, torch.bfloat16, seed=v)
+    ref = reference(x, w, b, t, g)
+    loss, lse, gx, gw = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+    dol.cross_entropy(x, w, t, loss, lse, bias=b)
+    dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b)
+    rel = 2 * ref["err_l"].max(initial=0.0) + 32 * U + 2.0 ** -17
+    within(gx, ref["grad_x"], ref["size_x"] * rel + W8 * np.abs(ref["grad_x"]) + 1e-37, "grad_x")
+    within(gw, ref["grad_w"], ref["size_w"] * rel + W8 * np.abs(ref["grad_w"]) + 1e-37, "grad_weight")

@@ -274,3 +274,12 @@ def test_samples_side_by_side(dol, b, p, c, groups, dtype):
     views[0].copy_(x), views[1].copy_(dy)
     got = run_and_check(dol, views[0], gamma, beta, groups, views[1], y=views[2], dx=views[3])
     assert torch.equal(got["y"], want["y"]) and torch.equal(got["grad_x"], want["grad_x"])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("b,p,c,groups", [(2, 2000, 24, 3), (3, 1024, 256, 32), (130, 520, 32, 1), (2, 2047, 16, 4)])
+def test_slabs_of_many_vectors_to_a_thread(dol, b, p, c, groups, dtype):
+    """Slabs that take eight vectors of x and of grad_y to a thread, and sixteen of x."""
+    x, gamma, beta, dy = make(b, p, c, getattr(torch, dtype), seed=p)
+    for act in ("silu", "none"):
+        run_and_check(dol, x, gamma, beta, groups, dy, act=act)

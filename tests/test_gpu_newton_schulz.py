@@ -196,3 +196,56 @@ def test_matrices_side_by_side(dol, rows, cols, dtype):
     for k in range(3):
         check(out[k], g[k])
     assert torch.equal(out, want)
+
+
+def check_on_device(got, g, steps=5):
+    """The bars of check, for a batch of matrices, with products in 64 bits on the device; float beside the same steps in 32 bits there."""
+    bf, tall = g.dtype == torch.bfloat16, g.shape[1] > g.shape[2]
+
+    def turned(x):
+        return x.transpose(1, 2).contiguous() if tall else x
+
+    def steps_of(x):
+        x = x / (x.norm(dim=(1, 2), keepdim=True) + 1e-7)
+        a, b, c = (float(np.float32(v)) for v in COEFFICIENTS)
+        out = [x]
+        for _ in range(steps):
+            gram = torch.stack([torch.mm(q, q.t().contiguous()) for q in x])
+            x = torch.stack([a * q + torch.mm(b * p + c * torch.mm(p, p), q) for p, q in zip(gram, x)])
+            out.append(x)
+        return out
+
+    xs = steps_of(turned(g.double()))
+    want = xs[-1]
+    assert bool(torch.isfinite(got).all())
+    err = (turned(got.double()) - want).norm(dim=(1, 2))
+    e = 8 * 2.0 ** -12 if bf else 16 * 2.0 ** -24
+    bar = e * sum(4.0 ** (steps - t) * x.norm(dim=(1, 2)) for t, x in enumerate(xs)) + (2.0 ** -8 * want.norm(dim=(1, 2)) if bf else 0.0)
+    assert bool((err <= bar).all()), (err / bar).max()
+    if bf:
+        assert bool((err <= 3.6e-3 * want.norm(dim=(1, 2))).all()), (err / want.norm(dim=(1, 2))).max()
+    else:
+        plain = (steps_of(turned(g))[-1].double() - want).norm(dim=(1, 2))
+        assert bool((err <= 4 * plain + 2.0 ** -22 * want.norm(dim=(1, 2))).all()), (err / plain).max()
+
+
+# Every tile of both products, wide and (in its last step turned) tall, square, a matrix and several; sides that no tile divides.
+FORMS = [("float32", 1, 1100, 1030, 64, 64), ("float32", 10, 500, 1000, 128, 128), ("float32", 10, 1000, 500, 128, 128), ("float32", 1, 1700, 1750, 128, 128),
+         ("float32", 43, 500, 511, 256, 256), ("float32", 43, 511, 500, 256, 256), ("float32", 1, 4000, 4095, 256, 256), ("bfloat16", 14, 300, 320, 64, 64),
+         ("bfloat16", 20, 500, 490, 128, 128), ("bfloat16", 20, 490, 500, 128, 128), ("bfloat16", 20, 500, 1000, 128, 256), ("bfloat16", 20, 1000, 500, 128, 256),
+         ("bfloat16", 1, 2300, 2400, 64, 128), ("bfloat16", 1, 2400, 2300, 64, 128), ("bfloat16", 43, 511, 500, 256, 256), ("bfloat16", 1, 4095, 4000, 256, 256),
+         ("bfloat16", 1, 4000, 4000, 256, 256)]
+
+
+@pytest.mark.parametrize("dtype,batch,rows,cols,symmetric,apply", FORMS)
+def test_forms(dol, dtype, batch, rows, cols, symmetric, apply):
+    g = normal((batch, rows, cols), getattr(torch, dtype), seed=rows + cols)
+    assert dol.newton_schulz_kernel(g) == "ns_symmetric_kernel %dx%d, ns_apply_kernel %dx%d" % (symmetric, symmetric, apply, apply)
+    out = torch.full((batch, rows, cols + 3), 7.0, dtype=g.dtype, device="cuda")
+    size = dol.newton_schulz_workspace(g)
+    guard = torch.full((size + 2048,), 77, dtype=torch.uint8, device="cuda")
+    dol.newton_schulz(g, out[:, :, :cols], workspace=guard[1024:1024 + size])
+    assert bool((guard[:1024] == 77).all()) and bool((guard[1024 + size:] == 77).all()) and bool((out[:, :, cols:] == 7).all())
+    check_on_device(out[:, :, :cols], g)
+    dol.newton_schulz(g, g)
+    assert torch.equal(g, out[:, :, :cols])

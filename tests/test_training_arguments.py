@@ -144,3 +144,19 @@ def test_layouts_with_samples_side_by_side():
     for b, p, c, ld_batch, ld_point in ((3, 10, 12, 12, 35), (3, 10, 12, 11, 40), (3, 10, 12, 0, 12), (2, 2, 4, 4, 4), (3, 10, 12, 119, 12)):
         with pytest.raises(dol.DolError, match="overlap"):
             dol._native.group_norm_workspace((F32, b, p, c, ld_batch, ld_point, 4096), 2, 1)
+
+
+def test_names_of_kernels():
+    """What the calls will launch, without a device; nothing for what they refuse."""
+    k = dol._native.cross_entropy_kernel
+    assert k(matrix(64, 128), matrix(10, 128), 0) == k(matrix(64, 128), matrix(10, 128), 1) == "xent_few_kernel"
+    assert k(matrix(8192, 1024, BF16), matrix(65535, 1024, BF16), 0) == "xent_sums_kernel 256x256x64"
+    assert k(matrix(8192, 1024, BF16), matrix(65535, 1024, BF16), 1) == "xent_dlogits_kernel 256x256x64, xent_products_kernel 256x256x64"
+    assert k(matrix(8, 16), matrix(20, 15), 0) == k(matrix(0, 16), matrix(20, 16), 1) == k(None, matrix(4, 16), 0) == ""
+    k = dol._native.newton_schulz_kernel
+    assert k(matrix(10, 128), 1) == "ns_small_kernel"
+    assert k(matrix(1000, 777), 1) == k(matrix(777, 1000), 1) == "ns_symmetric_kernel 64x64, ns_apply_kernel 64x64"
+    assert k(matrix(4096, 4096, BF16), 1) == "ns_symmetric_kernel 256x256, ns_apply_kernel 256x256"
+    assert k(matrix(10, 128), 0) == k(None, 1) == k(matrix(10, 128), -1) == ""
+    with pytest.raises(TypeError):
+        k(matrix(10, 128))
