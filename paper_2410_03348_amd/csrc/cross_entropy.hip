@@ -98,33 +98,34 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(Pack p0, Pack p1)
 {
     const bool second = blockIdx.x >= p0.blocks;
     const Pack &p = second ? p1 : p0;
-    const int64_t t = static_cast<int64_t>(blockIdx.x - (second ? p0.blocks : 0)) * 256 + threadIdx.x, per = p.kp / 8;
-    if (t >= p.out_rows * per) return;
-    const int64_t r = t / per;
-    const int c = static_cast<int>(t - r * per) * 8;
-    const bool in = r < p.rows && (!p.target || (kept_row(p.target[r], p.classes) && p.lse[r] != -INFINITY));
-    const S *from = static_cast<const S *>(p.src) + r * p.ld + c;
-    float v[8];
-    if (in && p.vec && c + 8 <= p.cols) {
-        struct alignas(16) Piece { S e[16 / sizeof(S)]; };
+    const int64_t per = p.kp / 8, all = p.out_rows * per;
+    for (int64_t t = static_cast<int64_t>(blockIdx.x - (second ? p0.blocks : 0)) * 256 + threadIdx.x; t < all; t += static_cast<int64_t>(p.blocks) * 256) {
+        const int64_t r = t / per;
+        const int c = static_cast<int>(t - r * per) * 8;
+        const bool in = r < p.rows && (!p.target || (kept_row(p.target[r], p.classes) && p.lse[r] != -INFINITY));
+        const S *from = static_cast<const S *>(p.src) + r * p.ld + c;
+        float v[8];
+        if (in && p.vec && c + 8 <= p.cols) {
+            struct alignas(16) Piece { S e[16 / sizeof(S)]; };
 #pragma unroll
-        for (int h = 0; h < static_cast<int>(8 * sizeof(S) / 16); ++h) {
-            const Piece q = reinterpret_cast<const Piece *>(from)[h];
+            for (int h = 0; h < static_cast<int>(8 * sizeof(S) / 16); ++h) {
+                const Piece q = reinterpret_cast<const Piece *>(from)[h];
 #pragma unroll
-            for (int k = 0; k < static_cast<int>(16 / sizeof(S)); ++k) v[h * (16 / sizeof(S)) + k] = static_cast<float>(q.e[k]);
+                for (int k = 0; k < static_cast<int>(16 / sizeof(S)); ++k) v[h * (16 / sizeof(S)) + k] = static_cast<float>(q.e[k]);
+            }
+        } else
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = in && c + k < p.cols ? static_cast<float>(from[k]) : 0.0f;
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            u32x4 w;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t lo = plane_of<P>(q, v[2 * k]), hi = plane_of<P>(q, v[2 * k + 1]);
+                w[k] = lo | hi << 16;
+            }
+            *reinterpret_cast<u32x4 *>(p.out + (q * p.out_rows + r) * p.out_ld + c) = w;
         }
-    } else
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = in && c + k < p.cols ? static_cast<float>(from[k]) : 0.0f;
-#pragma unroll
-    for (int q = 0; q < P; ++q) {
-        u32x4 w;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = plane_of<P>(q, v[2 * k]), hi = plane_of<P>(q, v[2 * k + 1]);
-            w[k] = lo | hi << 16;
-        }
-        *reinterpret_cast<u32x4 *>(p.out + (q * p.out_rows + r) * p.out_ld + c) = w;
     }
 }
 
@@ -398,22 +399,26 @@ __device__ __forceinline__ void sum_parts(const Sum &s, unsigned block)
 {
     __shared__ f32x4 red[4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t t = s.shared ? static_cast<int64_t>(block) * 64 + lane : static_cast<int64_t>(block) * 256 + threadIdx.x, per = (s.N + 3) / 4;
-    const bool in = t < s.M * per;
-    const int64_t m = t / per;
-    const int n = static_cast<int>(t - m * per) * 4;
-    f32x4 v = {0, 0, 0, 0};
-    if (in)
-#pragma unroll 8
-        for (int k = s.shared ? wave : 0; k < s.splits; k += s.shared ? 4 : 1) v += *reinterpret_cast<const f32x4 *>(s.part + (static_cast<int64_t>(k) * s.M + m) * s.part_ld + n);
-    if (s.shared) {
-        red[wave][lane] = v;
-        __syncthreads();
-        if (wave != 0) return;
-        v = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
-    }
+    const int64_t per = (s.N + 3) / 4, all = s.M * per;
     const bool vec = s.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(s.out) & (4 * sizeof(O) - 1)) == 0;
-    if (in) store4(static_cast<O *>(s.out) + m * s.out_ld + n, v, s.N - n, vec);
+    const int each = s.shared ? 64 : 256, at = s.shared ? lane : threadIdx.x;
+    for (int64_t first = static_cast<int64_t>(block) * each; first < all; first += static_cast<int64_t>(s.blocks) * each) {
+        const int64_t t = first + at, m = t / per;
+        const bool in = t < all;
+        const int n = static_cast<int>(t - m * per) * 4;
+        f32x4 v = {0, 0, 0, 0};
+        if (in)
+#pragma unroll 8
+            for (int k = s.shared ? wave : 0; k < s.splits; k += s.shared ? 4 : 1) v += *reinterpret_cast<const f32x4 *>(s.part + (static_cast<int64_t>(k) * s.M + m) * s.part_ld + n);
+        if (s.shared) {
+            red[wave][lane] = v;
+            __syncthreads();
+            v = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+            __syncthreads();
+            if (wave != 0) continue;
+        }
+        if (in) store4(static_cast<O *>(s.out) + m * s.out_ld + n, v, s.N - n, vec);
+    }
 }
 
 // Up to three sums in one launch: of grad_x's, of grad_w's and of grad_bias's parts (one row of classes).
@@ -581,6 +586,9 @@ bool direct(const dol_matrix *m)            // can be read by the tiles as it is
 int32_t tiles(int64_t n, int t) { return static_cast<int32_t>((n + t - 1) / t); }
 unsigned blocks(int64_t n) { return static_cast<unsigned>((n + 255) / 256); }
 
+// Launches have less than 2^32 threads: workgroups of what is done element by element, at most (each then takes several pieces in turn).
+constexpr int64_t kMostBlocks = 1 << 15;
+
 struct Layout {
     int32_t rows, width, classes;
     int64_t kp, n_pad;                      // width and rows as they are laid out
@@ -747,7 +755,7 @@ Pack pack_of(const dol_matrix *m, const int32_t *target, const float *lse, int32
     }
     *p = Planes{out, ld, out_rows * ld};
     const bool vec = !(reinterpret_cast<uintptr_t>(m->data) & 15) && m->ld % (16 / int64_t(sizeof(S))) == 0;
-    return Pack{m->data, m->ld, m->rows, m->cols, target, lse, classes, out, out_rows, kp, ld, vec, blocks(out_rows * (kp / 8))};
+    return Pack{m->data, m->ld, m->rows, m->cols, target, lse, classes, out, out_rows, kp, ld, vec, blocks(std::min(out_rows * (kp / 8), kMostBlocks * 256))};
 }
 
 template <int P>
@@ -774,7 +782,7 @@ Sum make_sum(const float *part, int32_t M, int32_t N, int32_t splits, int64_t pa
 {
     const bool shared = splits >= 16;
     const int64_t n = int64_t(M) * ((N + 3) / 4);
-    return Sum{part, M, N, splits, part_ld, out, out_ld, shared, static_cast<unsigned>(tiles(n, shared ? 64 : 256))};
+    return Sum{part, M, N, splits, part_ld, out, out_ld, shared, static_cast<unsigned>(std::min((n + (shared ? 63 : 255)) / (shared ? 64 : 256), kMostBlocks))};
 }
 
 template <typename S, bool BACK>
@@ -803,8 +811,14 @@ dol_status launch_sums(const Layout &L, Planes w, Planes x, const float *bias, c
 {
     DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(xent_sums_kernel<T>), T::LDS));
     const int tm = tiles(L.classes, T::BM), tn = tiles(L.rows, T::BN);
-    xent_sums_kernel<T><<<tm * tn, T::NT, T::LDS, st>>>(w, x, L.classes, L.rows, static_cast<int>(L.kp / T::BK), bias, target, L.part, L.n_pad, L.at);
-    DOL_HIP(hipGetLastError());
+    const int most = std::max(1, INT32_MAX / T::NT / tm);       // tiles of samples that a launch has the threads for
+    for (int t = 0; t < tn; t += most) {
+        const int64_t n = int64_t(t) * T::BN;
+        xent_sums_kernel<T><<<tm * std::min(most, tn - t), T::NT, T::LDS, st>>>(w, Planes{x.data + n * x.ld, x.ld, x.plane}, L.classes,
+                                                                               static_cast<int32_t>(std::min<int64_t>(L.rows - n, int64_t(most) * T::BN)),
+                                                                               static_cast<int>(L.kp / T::BK), bias, target + n, L.part + n, L.n_pad, L.at + n);
+        DOL_HIP(hipGetLastError());
+    }
     xent_join_kernel<<<tiles(L.rows, 64), kJoinWaves * 64, 0, st>>>(L.part, tm * T::WM, L.n_pad, L.rows, L.classes, target, L.at, loss, lse);
     DOL_HIP(hipGetLastError());
     return DOL_OK;

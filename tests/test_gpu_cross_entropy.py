@@ -477,3 +477,50 @@ def test_dl_of_few_rows_in_two_planes(dol, n, d, v):
     rel = 2 * ref["err_l"].max(initial=0.0) + 32 * U + 2.0 ** -17
     within(gx, ref["grad_x"], ref["size_x"] * rel + W8 * np.abs(ref["grad_x"]) + 1e-37, "grad_x")
     within(gw, ref["grad_w"], ref["size_w"] * rel + W8 * np.abs(ref["grad_w"]) + 1e-37, "grad_weight")
+
+
+def rows_in_64_bits(x, w, b, t, at):
+    """lse and loss of some rows (all of whose targets count), products in 64 bits on the device, and their bars."""
+    xd, wd, t = x[at].double(), w.double(), t[at].long()
+    logits = torch.mm(xd, wd.t().contiguous()) + (0 if b is None else b.double())
+    lse = torch.logsumexp(logits, 1)
+    bar = 16 * U * torch.mm(xd.abs(), wd.t().abs().contiguous()).max(1).values + 8 * U * (1 + lse.abs())
+    return lse, lse - logits.gather(1, t[:, None])[:, 0], bar
+
+
+def test_more_elements_than_a_round_of_workgroups(dol):
+    """A million rows: what is laid out, and what is summed up of grad_x, takes its workgroups more than once."""
+    n, d, v = (1 << 20) + 5, 72, 300
+    x, w, b, t, g = make(n, d, v, torch.bfloat16, seed=1)
+    t[::5] = -1
+    loss, lse = torch.full((n,), 9.0, device="cuda"), torch.full((n,), 9.0, device="cuda")
+    gx, gw, gb = torch.full_like(x, 9.0), torch.full_like(w, 9.0), torch.full_like(b, 9.0)
+    dol.cross_entropy(x, w, t, loss, lse, bias=b)
+    dol.cross_entropy_backward(x, w, t, lse, g, gx, gw, bias=b, grad_bias=gb)
+    kept = torch.nonzero(t >= 0)[:, 0]
+    want_lse, want, bar = rows_in_64_bits(x, w, b, t, kept)
+    assert bool(((lse[kept].double() - want_lse).abs() <= bar).all()) and bool(((loss[kept].double() - want).abs() <= 2 * bar).all())
+    assert not loss[::5].any() and not gx[::5].any()
+    xd, wd = x[kept].double(), w.double()
+    dl = torch.exp(torch.mm(xd, wd.t().contiguous()) + b.double() - want_lse[:, None])
+    dl[torch.arange(kept.numel(), device="cuda"), t[kept].long()] -= 1
+    dl *= g[kept].double()[:, None]
+    rel = 2 * float(bar.max()) + 32 * U + W8
+    for got, ref, size in ((gx[kept], torch.mm(dl, wd), torch.mm(dl.abs(), wd.abs())),
+                           (gw, torch.mm(dl.t().contiguous(), xd), torch.mm(dl.abs().t().contiguous(), xd.abs()))):
+        assert bool(((got.double() - ref).abs() <= rel * size + W8 * ref.abs() + 1e-37).all())
+    assert bool(((gb.double() - dl.sum(0)).abs() <= (rel - W8) * dl.abs().sum(0)).all())
+
+
+def test_more_tiles_than_a_launch_has_threads_for(dol):
+    """2^22 rows into 2^17 classes: 2^23 tiles of 512 threads."""
+    n, d, v = 1 << 22, 16, 1 << 17
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("60 GB of memory")
+    x, w, b, t, g = make(n, d, v, torch.bfloat16, seed=2, bias=False)
+    loss, lse = torch.full((n,), -9.0, device="cuda"), torch.full((n,), -9.0, device="cuda")
+    dol.cross_entropy(x, w, t, loss, lse)
+    at = torch.cat([torch.arange(0, n, n // 500, device="cuda"), torch.arange(n - 300, n, device="cuda")])
+    want_lse, want, bar = rows_in_64_bits(x, w, None, t, at)
+    assert bool(((lse[at].double() - want_lse).abs() <= bar).all()) and bool(((loss[at].double() - want).abs() <= 2 * bar).all())
+    assert bool((lse > -9).all()) and bool(torch.isfinite(loss).all())
