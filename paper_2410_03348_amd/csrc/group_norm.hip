@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(kPartThreads) group_norm_part_forward_kernel(S
 __global__ void __launch_bounds__(256) group_norm_finish_forward_kernel(Shape s, const float2 *part, float eps, float *mean, float *rstd, float *mean_out, float *rstd_out)
 {
     __shared__ float red[4];
-    const int64_t at = blockIdx.x, b = at / s.groups, g = at - b * s.groups;
+    const int64_t b = blockIdx.y, g = blockIdx.x, at = b * s.groups + g;
     const float2 *p = part + b * s.chunks * s.channels + g * s.per;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     auto points_of = [&](int k) { return static_cast<float>(min(s.chunk, s.points - k * s.chunk)); };
@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(kPartThreads) group_norm_part_backward_kernel(
 __global__ void __launch_bounds__(256) group_norm_finish_backward_kernel(Shape s, const float2 *part, const float *gamma, float *sums, float2 *c12)
 {
     __shared__ float red[2][4];
-    const int64_t at = blockIdx.x, b = at / s.groups, g = at - b * s.groups;
+    const int64_t b = blockIdx.y, g = blockIdx.x, at = b * s.groups + g;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     float c1 = 0.0f, c2 = 0.0f;
     for (int c = w; c < s.per; c += 4) {            // a wavefront to a channel, a lane to every sixty-fourth chunk
@@ -689,6 +689,7 @@ Plan plan_of(const dol_activations *x, int32_t groups, int vec, bool backward)
             if (threads > (backward ? kSlabThreadsBack : kSlabThreads)) break;
         }
         const int64_t workgroups = int64_t(s.batch) * (groups / k);
+        if (workgroups * threads > INT32_MAX) continue;         // (a launch has less than 2^32 threads)
         if (p.threads && !(workgroups >= 4 * kUnits || (int64_t(s.slice) * e < 64 && workgroups >= 2 * kUnits))) break;
         p.vecs = vecs, p.threads = static_cast<int>(threads), s.slice = static_cast<int32_t>(slice), s.slices = groups / k;
     }
@@ -763,7 +764,7 @@ dol_status forward(const Plan &p, const Space &w, const dol_activations *x, cons
     const dim3 grid(s.chunks, s.slices, s.batch);
     group_norm_part_forward_kernel<T, V><<<grid, kPartThreads, 0, st>>>(s, tensor_of(x), w.part);
     DOL_HIP(hipGetLastError());
-    group_norm_finish_forward_kernel<<<s.batch * s.groups, 256, 0, st>>>(s, w.part, eps, w.mean, w.rstd, mean, rstd);
+    group_norm_finish_forward_kernel<<<dim3(s.groups, s.batch), 256, 0, st>>>(s, w.part, eps, w.mean, w.rstd, mean, rstd);
     DOL_HIP(hipGetLastError());
     group_norm_map_kernel<T, V, false><<<grid, kPartThreads, 0, st>>>(s, tensor_of(x), Tensor{}, gamma, beta, w.mean, w.rstd, nullptr, act, tensor_of(y));
     DOL_HIP(hipGetLastError());
@@ -784,7 +785,7 @@ dol_status reverse(const Plan &p, const Space &w, const dol_activations *x, cons
         const dim3 grid(s.chunks, s.slices, s.batch);
         group_norm_part_backward_kernel<T, V><<<grid, kPartThreads, 0, st>>>(s, tensor_of(x), tensor_of(dy), gamma, beta, mean, rstd, act, w.part);
         DOL_HIP(hipGetLastError());
-        group_norm_finish_backward_kernel<<<s.batch * s.groups, 256, 0, st>>>(s, w.part, gamma, w.sums, w.c12);
+        group_norm_finish_backward_kernel<<<dim3(s.groups, s.batch), 256, 0, st>>>(s, w.part, gamma, w.sums, w.c12);
         DOL_HIP(hipGetLastError());
         if (dx) {
             group_norm_map_kernel<T, V, true><<<grid, kPartThreads, 0, st>>>(s, tensor_of(x), tensor_of(dy), gamma, beta, mean, rstd, w.c12, act, tensor_of(dx));

@@ -283,3 +283,23 @@ def test_slabs_of_many_vectors_to_a_thread(dol, b, p, c, groups, dtype):
     x, gamma, beta, dy = make(b, p, c, getattr(torch, dtype), seed=p)
     for act in ("silu", "none"):
         run_and_check(dol, x, gamma, beta, groups, dy, act=act)
+
+
+def test_more_slabs_than_a_launch_has_threads_for(dol):
+    """65 535 samples of one point, 4 093 groups of eight channels; some of the samples against the definition."""
+    b, c, groups = 65535, 8 * 4093, 4093
+    if torch.cuda.mem_get_info()[0] < 70 << 30:
+        pytest.skip("70 GB of memory")
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    x = torch.empty(b, 1, c, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    dy = x.roll(1, 0)
+    gamma, beta = torch.rand(c, generator=gen, device="cuda") + 0.5, torch.randn(c, generator=gen, device="cuda") * 0.3
+    y, mean, rstd, dx = torch.zeros_like(x), torch.zeros(b, groups, device="cuda"), torch.zeros(b, groups, device="cuda"), torch.zeros_like(x)
+    dol.group_norm(x, gamma, beta, groups, y, mean, rstd, act="silu")
+    dol.group_norm_backward(x, gamma, beta, groups, mean, rstd, dy, dx, None, None, act="silu")
+    at = [0, 1, 7, 1024, 30000, 65533, 65534]
+    want, bars = reference(x[at], gamma, beta, groups, 1e-5, "silu", dy[at])
+    for name, got in (("y", y), ("mean", mean), ("rstd", rstd), ("grad_x", dx)):
+        off = np.abs(got[at].cpu().double().numpy() - want[name]) - bars[name] - (W8 * np.abs(want[name]) if name in ("y", "grad_x") else 0.0) - 1e-37
+        assert off.max() <= 0, "%s: %g over its bar" % (name, off.max())
+    assert bool((rstd > 0).all()) and bool(torch.isfinite(rstd).all())

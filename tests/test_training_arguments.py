@@ -160,3 +160,12 @@ def test_names_of_kernels():
     assert k(matrix(10, 128), 0) == k(None, 1) == k(matrix(10, 128), -1) == ""
     with pytest.raises(TypeError):
         k(matrix(10, 128))
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+def test_group_norm_of_more_slabs_than_a_launch_has_threads_for(backward):
+    """65 535 samples of 4 093 groups, a wavefront to each: more than 2^32 threads.  The shared-out form needs space for its parts."""
+    parts = 65535 * 8 * 4093 * 8
+    assert dol._native.group_norm_workspace(acts(65535, 1, 8 * 4093, BF16), 4093, backward) >= parts
+    # with fewer samples the slabs' own: nothing forward, two sums of a channel and sample backward
+    assert dol._native.group_norm_workspace(acts(4000, 1, 8 * 4093, BF16), 4093, backward) == 8 * 4000 * 8 * 4093 * backward
