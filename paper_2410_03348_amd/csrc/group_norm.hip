@@ -689,7 +689,7 @@ Plan plan_of(const dol_activations *x, int32_t groups, int vec, bool backward)
             if (threads > (backward ? kSlabThreadsBack : kSlabThreads)) break;
         }
         const int64_t workgroups = int64_t(s.batch) * (groups / k);
-        if (workgroups * threads > INT32_MAX) continue;         // (a launch has less than 2^32 threads)
+        if (workgroups * threads >> 32) continue;               // (a launch has less than 2^32 threads)
         if (p.threads && !(workgroups >= 4 * kUnits || (int64_t(s.slice) * e < 64 && workgroups >= 2 * kUnits))) break;
         p.vecs = vecs, p.threads = static_cast<int>(threads), s.slice = static_cast<int32_t>(slice), s.slices = groups / k;
     }
