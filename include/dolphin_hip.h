@@ -425,7 +425,9 @@ typedef struct {
  *   x       [rows, width],   weight  [classes, width], same type
  *   bias    device [classes] or NULL; -inf takes a class out
  *   target  device [rows]; a row whose target is outside 0..classes-1 (-1, say) is left out: its loss is 0
- *   loss, lse  device [rows], both written.  A row without any class above -inf has lse = -inf and loss = +inf.
+ *   loss, lse  device [rows], both written.  A row whose logits are all -inf has lse = -inf and loss = +inf; a NaN among them makes both
+ *           NaN, a +inf lse = +inf.  (DOL_F32 multiplies in parts of numbers, but for a few classes (dol_cross_entropy_kernel): an infinity in
+ *           x or weight makes its logits NaN.)
  * At most 2^22 rows and classes and 2^20 elements of a row (else DOL_EUNSUPPORTED); at least one class of one element. */
 dol_status dol_cross_entropy_workspace(const dol_matrix *x, const dol_matrix *weight, int32_t backward, int64_t *bytes);
 dol_status dol_cross_entropy(const dol_matrix *x, const dol_matrix *weight, const float *bias, const int32_t *target, float *loss,
@@ -438,7 +440,9 @@ const char *dol_cross_entropy_kernel(const dol_matrix *x, const dol_matrix *weig
  * or have no class (whatever x holds there, also NaN, and whatever grad_loss says);
  *   grad_x = dl weight,   grad_weight = dl^T x,   grad_bias[v] = sum_i dl[i, v].
  * lse as the forward call left it.  Each gradient is OVERWRITTEN, of the type of x (grad_bias: float); any may be NULL.  Sums are taken in
- * a fixed order: two runs give the same bits.  With DOL_BF16 dl is rounded to bf16 before the two products.  rows == 0 writes zeros. */
+ * a fixed order: two runs give the same bits.  rows == 0 writes zeros.  DOL_BF16 above 512 rows rounds dl to bf16 before the two
+ * products, which with the results' own rounding leaves gradients off by some 2.4e-3; up to 512 rows dl keeps 16 bits, and in the form for a
+ * few classes all: they are off by the results' rounding, 1.7e-3. */
 dol_status dol_cross_entropy_backward(const dol_matrix *x, const dol_matrix *weight, const float *bias, const int32_t *target,
                                       const float *lse, const float *grad_loss, const dol_matrix *grad_x, const dol_matrix *grad_weight,
                                       float *grad_bias, void *workspace, int64_t workspace_bytes, void *hip_stream);
@@ -447,7 +451,8 @@ dol_status dol_cross_entropy_backward(const dol_matrix *x, const dol_matrix *wei
  *   A = X X^T,   B = b A + c A A,   X <- a X + B X,   out = X
  * with (a, b, c) = coefficients, host [3]; a matrix with more rows than columns is taken as its transpose, and so is its result.  Each
  * singular value s of X becomes s (a + b s^2 + c s^4) in a step: those of G end near 1 while its singular vectors stay.
- *   g, out   `batch` matrices of one size and type, g_stride and out_stride elements apart (ignored for one); out may be g
+ *   g, out   `batch` matrices of one size and type, g_stride and out_stride elements apart (ignored for one), one behind the other or
+ *            with their rows side by side; out may be g
  * DOL_F32 is as exact as sums of 32-bit numbers in 32 bits; DOL_BF16 takes its products of numbers of 11 bits, which with the result's
  * own rounding leaves some 2.4e-3 of it.
  * DOL_EUNSUPPORTED where the coefficients let singular values pass 64, for sides above 2^20 and for more than 65 535 matrices. */
@@ -469,7 +474,7 @@ typedef enum { DOL_ACT_NONE = 0, DOL_ACT_RELU = 1, DOL_ACT_SILU = 2, DOL_ACT_GEL
 typedef struct {
     int32_t dtype;               /* dol_dtype */
     int32_t batch, points, channels;
-    int64_t ld_batch, ld_point;  /* elements between consecutive samples, points; channels are neighbours */
+    int64_t ld_batch, ld_point;  /* elements between consecutive samples, points, whichever is the larger; channels are neighbours */
     void *data;                  /* device */
 } dol_activations;
 dol_status dol_group_norm_workspace(const dol_activations *x, int32_t groups, int32_t backward, int64_t *bytes);

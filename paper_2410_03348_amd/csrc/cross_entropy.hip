@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(Pack p0, Pack p1)
 // over these classes, top the largest logit among them; at[sample] = l of the target.
 // The exponentials are taken as 2^(l log2e - c), c = top log2e rounded: one multiply-add a logit.  What c lost is the same factor in all of
 // them, and divided out of the sum as the top's own term: that is 1 to the bit, and a row whose other classes vanish has lse = top.
-// The product bounds it: 8 192 x 1 024 into 65 535 in bf16 970 us, 1 133 TFLOP/s.
+// The product bounds it: 8 192 x 1 024 into 65 535 in bf16 927 to 970 us, 1 133 to 1 186 TFLOP/s.
 template <typename T>
 __global__ void __launch_bounds__(T::NT, 2) xent_sums_kernel(Planes w, Planes x, int32_t classes, int32_t rows, int steps, const float *bias, const int32_t *target,
                                                              float2 *part, int64_t n_pad, float *at)
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kJoinWaves * 64) xent_join_kernel(const float2
 
 // dl of one piece of classes in Q planes: dl[q][sample][class of the piece] (rows ld apart), zeros in the samples and classes that there are not.  Rows of a
 // tile are samples, columns classes.  bias_part[(mt * WM + wavefront row) * piece + class] = sums of the unrounded dl (if asked for).
-// The product bounds it, and the exponentials and stores behind it: 8 192 x 1 024 into 65 535 in bf16 1 142 us in all, 963 TFLOP/s.
+// The product bounds it, and the exponentials and stores behind it: 8 192 x 1 024 into 65 535 in bf16 1 132 us in all, 972 TFLOP/s.
 template <typename T, int Q>
 __global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes w, int32_t rows, int32_t classes, int steps, int32_t first, int32_t piece, int64_t ld,
                                                                 const float *bias, const int32_t *target, const float *lse, const float *grad_loss,
@@ -371,7 +371,8 @@ __device__ __forceinline__ void product_tile(const Product &p, int id, char *sme
 }
 
 // grad_x's tiles (TX: dl along its rows) and grad_w's (TW: dl across them), in one launch since each alone seldom fills the chip.  Loads into
-// LDS bound it: 8 192 x 1 024 into 65 535 in bf16 1 890 us in all, 1 163 TFLOP/s; float 1 000 x 300 into 5 003 51 us, 700 TFLOP/s of planes.
+// LDS bound it: 8 192 x 1 024 into 65 535 in bf16 1 821 to 1 890 us in all, 1 163 to 1 207 TFLOP/s; float 1 000 x 300 into 5 003 51 us, 700 TFLOP/s of
+// planes.  (256 x 256 in bf16 has 4 registers more than there are, which it spills.)
 template <typename TX, typename TW, typename O>
 __global__ void __launch_bounds__(TX::NT, 2) xent_products_kernel(Product px, Product pw)
 {
@@ -641,8 +642,8 @@ constexpr int kTiny = 128;
 template <int P>
 constexpr int kTinyProducts = P == 3 ? 64 : 256;
 
-// What a tile takes beside its products, in k, and what an element of a sum and a piece's launches take, in a tile's area times k (20 G of
-// which a unit's matrix cores do in a millisecond with one product of planes).
+// What a tile takes beside its products, in k, and what an element of a sum and a piece's launches take, in a tile's area times k (some 2.2 G of
+// which a unit does in a millisecond with one product of planes, at the rates above: a piece's launches some 7.6 us).
 constexpr double kAround = 160, kSumWeight = 6, kLaunchWeight = 256 * 256 * 256;
 
 template <int P, int Q>

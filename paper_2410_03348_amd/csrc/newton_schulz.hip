@@ -206,7 +206,8 @@ __global__ void __launch_bounds__(T::NT, 2) ns_symmetric_kernel(const uint16_t *
 }
 
 // X' = alpha (B X) + beta X, X' [mp][np] in two planes, or (out) the result.  TURN: a tile's columns are X's columns and out is tall.
-// Loads into LDS bound it: bf16 4096 x 4096 150 us, 919 TFLOP/s; float 1000 x 777 16 us.
+// Loads into LDS bound it, and in bf16 with 256 x 256 tiles the registers: the operand that lies across k keeps its addresses beside 224 registers of sums
+// and halves, so that 22 are spilled (TURN: 67).  bf16 4096 x 4096 148 us, 929 TFLOP/s, where such a loop alone does 1 256; float 1000 x 777 16 us.
 struct Apply {
     const uint16_t *x, *b;
     int64_t x_stride, b_stride;

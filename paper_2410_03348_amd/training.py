@@ -14,7 +14,8 @@ The network in front of a Dolphin program (Fig. 2 of the paper) and what trains 
       grad h, gamma, beta                                        dol.group_norm_backward
       w1, w2: momentum, its orthogonalisation as the update      dol.newton_schulz
 
-``step`` only issues asynchronous calls on the current stream, on buffers that the constructor allocates.
+``step`` only issues asynchronous calls on the current stream.  What passes between the library's calls is in buffers that the constructor
+allocates; logits, masks, torch's temporaries and the calls' workspaces come from torch's allocator, which has them again a step later.
 
     python -m paper_2410_03348_amd.training        # trains on seeded synthetic digits and prints its course
 """
