@@ -21,7 +21,9 @@ namespace dol {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr float kFar = 1e38f;       // logits further from 0 (a bias of the type's lowest value) have no finite l log2e
+// Logits further from 0 (masks of -1e10, of the type's lowest value) are subtracted from each other before they are multiplied by log2e: what
+// rounding takes from l log2e, 2^-24 of it, is an exponent of its own, 1/16 here and 512 at 1e10.
+constexpr float kFar = 1e6f;
 constexpr int kPad = 256;                               // rows and classes of a piece are filled up to a multiple of this
 constexpr int64_t kMostPieceBytes = int64_t(192) << 20; // of dl
 constexpr int kUnits = 256;                             // compute units of the chip

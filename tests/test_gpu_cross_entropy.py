@@ -524,3 +524,20 @@ def test_more_tiles_than_a_launch_has_threads_for(dol):
     want_lse, want, bar = rows_in_64_bits(x, w, None, t, at)
     assert bool(((lse[at].double() - want_lse).abs() <= bar).all()) and bool(((loss[at].double() - want).abs() <= 2 * bar).all())
     assert bool((lse > -9).all()) and bool(torch.isfinite(loss).all())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,d,v", [(40, 64, 10), (40, 64, 300), (300, 64, 3001), (2000, 130, 2000)])
+def test_logits_far_from_zero(dol, n, d, v, dtype):
+    """Masks of every finite size over part of the classes, whole tiles of them, and a class that stands far above or all others far below:
+    exponentials of differences, whatever the logits themselves are."""
+    x, w, b, t, g = make(n, d, v, getattr(torch, dtype), seed=n + v)
+    for far in (-2e6, -1e8, -1e10, -1e20, -1e30, -1e37, -3e38):
+        bias = b.clone()
+        bias[: v * 3 // 4] = far
+        run_and_check(dol, x, w, bias, torch.full_like(t, v - 1), g)
+    t = t % (v - 1) + 1
+    for far in (2e6, 1e8, 3e9, 1e10, 1e20, 1e30, 1e38, -1e8, -1e10, -1e20, -1e30, -1e38):
+        bias = torch.full_like(b, min(0.0, 2 * far))
+        bias[0] = far
+        run_and_check(dol, x, w, bias, t, g)
