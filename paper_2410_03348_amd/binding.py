@@ -133,10 +133,15 @@ def _handle(stream):
     return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else stream if stream is None else int(stream)
 
 
+def _current() -> int:
+    """The handle of torch's current stream alone: 0.2 us against 2.9 for a stream object, of 7 for a whole call."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
 def _stream(stream) -> C.c_void_p:
     """A torch stream, a raw handle, or None = torch's current stream."""
-    if stream is None:                   # the handle alone: 0.2 us against 2.9 for a stream object, of 7 for a whole call
-        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+    if stream is None:
+        return C.c_void_p(_current())
     if isinstance(stream, torch.cuda.Stream):
         return C.c_void_p(stream.cuda_stream)
     return C.c_void_p(int(stream))
@@ -676,7 +681,7 @@ def _workspace(given: Optional[torch.Tensor], n: int, device, stream):
         return given.data_ptr(), given.numel() * given.element_size(), given
     if n == 0:
         return None, 0, None
-    if stream is None:
+    if stream is None or _handle(stream) == _current():
         t = torch.empty(n, dtype=torch.uint8, device=device)
     else:
         with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)):

@@ -89,7 +89,7 @@ def test_a_workspace_is_taken_on_the_stream_of_the_call(monkeypatch):
     import contextlib
 
     class Side:
-        pass
+        cuda_stream = 8192
 
     class External(Side):
         def __init__(self, handle, device=None):
@@ -111,12 +111,17 @@ def test_a_workspace_is_taken_on_the_stream_of_the_call(monkeypatch):
     monkeypatch.setattr(torch.cuda, "ExternalStream", External)
     monkeypatch.setattr(torch.cuda, "stream", on)
     monkeypatch.setattr(torch, "empty", recorded)
+    monkeypatch.setattr(dol, "_current", lambda: 0)
     side = Side()
     dol._workspace(None, 512, "cuda", side)
     dol._workspace(None, 512, "cuda", 4096)
     dol._workspace(None, 512, "cuda", None)
     assert taken[0] is side and taken[1].handle == 4096 and taken[2] is None
     assert dol._workspace(None, 0, "cuda", side) == (None, 0, None) and len(taken) == 3
+    monkeypatch.setattr(dol, "_current", lambda: 8192)
+    dol._workspace(None, 512, "cuda", side)                 # (the current one by name: no need to enter it)
+    dol._workspace(None, 512, "cuda", 4096)
+    assert taken[3] is None and taken[4].handle == 4096
 
 
 @pytest.mark.parametrize("points", [2 ** 31 - 1, 2 ** 31 - 8, 2 ** 31 - 16, 2 ** 31 - 17])
