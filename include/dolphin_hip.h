@@ -464,7 +464,8 @@ dol_status dol_newton_schulz(const dol_matrix *g, int64_t g_stride, const dol_ma
                              void *hip_stream);
 
 /* Group norm over channels-last activations followed by an activation function:
- *   per sample and group: mean and var over the points and the group's channels / groups neighbouring channels, rstd = 1 / sqrt(var + eps);
+ *   per sample and group: mean and var over the points and the group's channels / groups neighbouring channels, rstd = 1 / sqrt(var + eps)
+ *   (in 32 bits; var + eps below 2^-126 counts as 0, and rstd is inf);
  *   xhat = (x - mean) rstd,   y = act(gamma xhat + beta).
  *   x, y         [batch][points][channels], one type; y may be x
  *   gamma, beta  device [channels] or NULL (1, 0)

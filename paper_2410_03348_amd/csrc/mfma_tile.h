@@ -5,7 +5,7 @@
 // planes whose magnitudes a 32-bit sum would see:
 //   1 plane   bf16 or fp16 as it is                                     1 product
 //   2 planes  fp16, 22 bits and a sign: x = x0 + x1                     x0 y0 + x0 y1 + x1 y0        (dropped: 2^-24 of x y)
-//   3 planes  bf16, 24 bits over the whole range of a float             six products, x1 y2, x2 y1, x2 y2 dropped
+//   3 planes  bf16, 24 bits of numbers from 2^-109 to a float's largest six products, x1 y2, x2 y1, x2 y2 dropped
 #pragma once
 
 #include "internal.h"
