@@ -490,6 +490,26 @@ dol_status dol_group_norm_backward(const dol_activations *x, int32_t groups, con
                                    const float *mean, const float *rstd, const dol_activations *grad_y, const dol_activations *grad_x,
                                    float *grad_gamma, float *grad_beta, void *workspace, int64_t workspace_bytes, void *hip_stream);
 
+/* The buffers of a network's gradients (or of what is made of them), which a training program keeps: `count` of them, buffer t at data[t]
+ * with size[t] >= 0 neighbouring elements of type dtype[t] (dol_dtype).  All three arrays are host memory, read during the call only.
+ * The handle owns a device copy of the list on the current device; the buffers are the caller's and outlive it. */
+typedef struct dol_tensor_list dol_tensor_list;
+dol_status dol_tensor_list_create(int32_t count, const int32_t *dtype, const int64_t *size, void *const *data, dol_tensor_list **list);
+/* Synchronises the device before releasing the device copy.  NULL is ignored. */
+void dol_tensor_list_destroy(dol_tensor_list *list);
+/* The global norm: norm[0] = sqrt(sum of the squares of all elements of all buffers), device; squares and their sum in 64 bits, in a
+ * fixed order.  A buffer that is in the list twice counts twice. */
+dol_status dol_grad_norm_workspace(const dol_tensor_list *grads, int64_t *bytes);
+dol_status dol_grad_norm(const dol_tensor_list *grads, float *norm, void *workspace, int64_t workspace_bytes, void *hip_stream);
+/* Clipping by it:  coef[0] = min(1, max_norm / (norm + eps)),   out = coef grads, each element rounded once.
+ *   out         a list of the same types and sizes, or `grads` itself (in place).  No two buffers of either list share memory, nor a
+ *               buffer of `grads` with another than its own of `out` (DOL_EINVAL)
+ *   norm, coef  device [1], both written.  A norm that is not finite leaves max_norm / (norm + eps) as it comes: NaN makes all of
+ *               `out` NaN, infinity the infinite elements NaN and the others 0 (max_norm infinite as well: NaN)
+ * Workspace as dol_grad_norm. */
+dol_status dol_clip_grads(const dol_tensor_list *grads, const dol_tensor_list *out, double max_norm, double eps, float *norm, float *coef,
+                          void *workspace, int64_t workspace_bytes, void *hip_stream);
+
 /* Message of the calling thread's most recent failing call ("" if none). */
 const char *dol_last_error(void);
 /* Library version, e.g. "0.1.0". */

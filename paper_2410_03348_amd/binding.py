@@ -7,6 +7,7 @@ There is no fallback: if the shared library is missing, import fails.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -789,3 +790,68 @@ def group_norm_backward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Op
                                 _values(mean, _F, batch, groups), _values(rstd, _F, batch, groups), _activations(grad_y),
                                 _activations(grad_x), _values(grad_gamma, _F, channels), _values(grad_beta, _F, channels), ws, n,
                                 _handle(stream))
+
+
+_lib.dol_tensor_list_create.argtypes = [C.c_int32, _i32p, C.POINTER(C.c_int64), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p)]
+_lib.dol_tensor_list_destroy.argtypes = [C.c_void_p]
+_lib.dol_tensor_list_destroy.restype = None
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether the tensor's elements fill one stretch of memory, in whatever order its dimensions lie."""
+    want = 1
+    for stride, size in sorted((st, n) for n, st in zip(t.shape, t.stride()) if n != 1):
+        if stride != want:
+            return t.numel() == 0
+        want *= size
+    return True
+
+
+class TensorList:
+    """The buffers of a network's gradients, in the order given: float32 or bfloat16 tensors of one device, each without gaps in memory.
+    Keeps the tensors, whose memory the calls use; made once for buffers that a program keeps."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        dtype, size, data = (C.c_int32 * max(n, 1))(), (C.c_int64 * max(n, 1))(), (C.c_void_p * max(n, 1))()
+        for k, t in enumerate(self.tensors):
+            assert t.is_cuda and t.device == self.tensors[0].device and t.dtype in _DTYPES and _dense(t)
+            dtype[k], size[k], data[k] = _DTYPES[t.dtype], t.numel(), t.data_ptr()
+        self.device = self.tensors[0].device if n else None
+        # two lists whose tensors lie in memory in another order are not each other's results; None = the order of the dimensions
+        self._orders = None if all(t.is_contiguous() for t in self.tensors) else [(tuple(t.shape), t.stride()) for t in self.tensors]
+        self._h = None
+        h = C.c_void_p()
+        with torch.cuda.device(self.device) if n else contextlib.nullcontext():
+            _check(_lib.dol_tensor_list_create(n, dtype, size, data, C.byref(h)))
+        self._h = h.value
+
+    def destroy(self):
+        if self._h:
+            _lib.dol_tensor_list_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            self.destroy()
+
+
+def grad_norm_workspace(grads: TensorList) -> int:
+    """Bytes that grad_norm and clip_grads need for this list."""
+    return _native.grad_norm_workspace(grads._h)
+
+
+def grad_norm(grads: TensorList, norm: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
+    """norm float32 [1]: the root of the sum of the squares of all elements of all tensors."""
+    ws, n, _keep = _workspace(workspace, _native.grad_norm_workspace(grads._h) if workspace is None else 0, norm.device, stream)
+    _native.grad_norm(grads._h, _values(norm, _F, 1), ws, n, _handle(stream))
+
+
+def clip_grads(grads: TensorList, max_norm: float, norm: torch.Tensor, coef: torch.Tensor, out: Optional[TensorList] = None, eps: float = 1e-6,
+               workspace: Optional[torch.Tensor] = None, stream=None):
+    """out = coef * grads (None: in place), coef = min(1, max_norm / (norm + eps)), norm as grad_norm gives it; norm, coef: float32 [1]."""
+    out = grads if out is None else out
+    assert out is grads or out._orders == grads._orders
+    ws, n, _keep = _workspace(workspace, _native.grad_norm_workspace(grads._h) if workspace is None else 0, norm.device, stream)
+    _native.clip_grads(grads._h, out._h, max_norm, eps, _values(norm, _F, 1), _values(coef, _F, 1), ws, n, _handle(stream))

@@ -387,6 +387,39 @@ PyObject *newton_schulz(PyObject *, PyObject *const *v, Py_ssize_t n)
     DOL_CALL(dol_newton_schulz(g.p(), g_stride, o.p(), o_stride, batch, steps, abc, eps, ws, have, s));
 }
 
+PyObject *grad_norm_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 1);
+    auto *l = a.ptr<dol_tensor_list>(0);
+    if (a.bad) return nullptr;
+    int64_t need = 0;
+    const dol_status st = dol_grad_norm_workspace(l, &need);
+    return bytes(st, need);
+}
+
+PyObject *grad_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 5);
+    auto *l = a.ptr<dol_tensor_list>(0);
+    auto *norm = a.ptr<float>(1);
+    auto *ws = a.ptr<void>(2);
+    const int64_t have = a.num(3);
+    void *s = a.stream(4);
+    DOL_CALL(dol_grad_norm(l, norm, ws, have, s));
+}
+
+PyObject *clip_grads(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 9);
+    auto *l = a.ptr<dol_tensor_list>(0), *o = a.ptr<dol_tensor_list>(1);
+    const double most = a.real(2), eps = a.real(3);
+    auto *norm = a.ptr<float>(4), *coef = a.ptr<float>(5);
+    auto *ws = a.ptr<void>(6);
+    const int64_t have = a.num(7);
+    void *s = a.stream(8);
+    DOL_CALL(dol_clip_grads(l, o, most, eps, norm, coef, ws, have, s));
+}
+
 // ---- a tensor's description, for the structures above (a Python function of the same checks takes about twice as long); None for None
 
 PyObject *g_float = nullptr, *g_bf16 = nullptr;             // torch.float32, torch.bfloat16
@@ -550,6 +583,9 @@ PyMethodDef g_methods[] = {
     {"group_norm_workspace", DOL_FAST(group_norm_workspace)},
     {"group_norm", DOL_FAST(group_norm)},
     {"group_norm_backward", DOL_FAST(group_norm_backward)},
+    {"grad_norm_workspace", DOL_FAST(grad_norm_workspace)},
+    {"grad_norm", DOL_FAST(grad_norm)},
+    {"clip_grads", DOL_FAST(clip_grads)},
     {"matrix", DOL_FAST(matrix)},
     {"activations", DOL_FAST(activations)},
     {"values", DOL_FAST(values)},
