@@ -245,7 +245,7 @@ def _own_residual_norm(s):
                       scale=s["scale"], eps=NORM_EPS)
     keys = ["h", "y", "rstd_h"] + (["rstd_u"] if s["post"] else [])
     if s["train"]:
-        dol.residual_norm_backward(s["u"], s["gamma_u"], s["gates"], s["gamma_y"], s["h"], s["rstd_u"], s["rstd_h"], s["grad_h"], s["grad_y"],
+        dol.residual_norm_backward(s["x"], s["u"], s["gamma_u"], s["gates"], s["gamma_y"], s["rstd_u"], s["rstd_h"], s["grad_h"], s["grad_y"],
                                    s["grad_x"], s["grad_u"], s["grad_gamma_u"], s["grad_gates"], s["grad_gamma_y"], norm_u=s["post"],
                                    scale=s["scale"])
         keys += ["grad_x", "grad_u", "grad_gamma_y"] + (["grad_gamma_u"] if s["post"] else []) + (["grad_gates"] if s["gates"] is not None else [])
