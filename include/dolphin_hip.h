@@ -490,6 +490,35 @@ dol_status dol_group_norm_backward(const dol_activations *x, int32_t groups, con
                                    const float *mean, const float *rstd, const dol_activations *grad_y, const dol_activations *grad_x,
                                    float *grad_gamma, float *grad_beta, void *workspace, int64_t workspace_bytes, void *hip_stream);
 
+/* Where one block of a network ends and the next begins: the norm behind a block, its gate, the stream of activations that it is added
+ * to, and the norm in front of the next block.  With rms(v) = 1 / sqrt(mean of a row's v^2 + eps), in 32 bits:
+ *   v = gamma_u u rstd_u, rstd_u = rms(u), where norm_u is not 0;   v = u where it is
+ *   h = x + scale gate v
+ *   y = gamma_y h rstd_h, rstd_h = rms(h) of h before it is rounded
+ *   x         [rows, cols] or NULL = 0: what the blocks before have left;   u  [rows, cols]: what this one computed
+ *   gamma_u, gamma_y  device [cols] or NULL = 1
+ *   gate      [gates, cols] or NULL = 1, of the type of u; gates divides rows, and row i has gate i / (rows / gates): one for all rows, one
+ *             for a sample of neighbouring rows, or one for each row
+ *   h, y      [rows, cols], of the type of u; either may be NULL, and either may be x or u
+ *   rstd_u, rstd_h  device [rows], written where not NULL (the gradients need them)
+ * At least one column, and at most 2^24; numbers whose squares pass a float's range are off its definition. */
+dol_status dol_residual_norm(const dol_matrix *x, const dol_matrix *u, int32_t norm_u, const float *gamma_u, const dol_matrix *gate,
+                             float scale, const float *gamma_y, float eps, const dol_matrix *h, const dol_matrix *y, float *rstd_u,
+                             float *rstd_h, void *hip_stream);
+/* Its gradients, from grad_h (NULL = 0), what h gets from further on, and grad_y (NULL = 0):
+ *   dh = grad_h + rstd_h (gamma_y grad_y - hhat mean(gamma_y grad_y hhat)), hhat = h rstd_h;   grad_x = dh;   dv = scale gate dh
+ *   grad_u = rstd_u (gamma_u dv - uhat mean(gamma_u dv uhat)), uhat = u rstd_u, where norm_u is not 0;   dv where it is
+ *   grad_gate[g] = scale sum dh v over the gate's rows,   grad_gamma_u = sum dv uhat,   grad_gamma_y = sum grad_y hhat over all rows.
+ * x, u, gamma_u, gate, scale, gamma_y as in, rstd_u and rstd_h from the forward call (rstd_h only with grad_y, rstd_u only with norm_u); h is
+ * made again from them, unrounded.  Each is OVERWRITTEN and may be NULL; grad_x and grad_u, each its own, may be grad_h, grad_y, x or u.
+ * Sums are taken in a fixed order: two runs give the same bits. */
+dol_status dol_residual_norm_workspace(const dol_matrix *u, const dol_matrix *gate, int64_t *bytes);
+dol_status dol_residual_norm_backward(const dol_matrix *x, const dol_matrix *u, int32_t norm_u, const float *gamma_u, const dol_matrix *gate,
+                                      float scale, const float *gamma_y, const float *rstd_u, const float *rstd_h, const dol_matrix *grad_h,
+                                      const dol_matrix *grad_y, const dol_matrix *grad_x, const dol_matrix *grad_u, float *grad_gamma_u,
+                                      const dol_matrix *grad_gate, float *grad_gamma_y, void *workspace, int64_t workspace_bytes,
+                                      void *hip_stream);
+
 /* The buffers of a network's gradients (or of what is made of them), which a training program keeps: `count` of them, buffer t at data[t]
  * with size[t] >= 0 neighbouring elements of type dtype[t] (dol_dtype).  All three arrays are host memory, read during the call only.
  * The handle owns a device copy of the list on the current device; the buffers are the caller's and outlive it. */

@@ -792,6 +792,42 @@ def group_norm_backward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Op
                                 _handle(stream))
 
 
+def residual_norm(x: Optional[torch.Tensor], u: torch.Tensor, gamma_u: Optional[torch.Tensor], gate: Optional[torch.Tensor],
+                  gamma_y: Optional[torch.Tensor], h: Optional[torch.Tensor], y: Optional[torch.Tensor], rstd_u: Optional[torch.Tensor] = None,
+                  rstd_h: Optional[torch.Tensor] = None, norm_u: bool = True, scale: float = 1.0, eps: float = 1e-6, stream=None):
+    """h = x + scale * gate * v, v = gamma_u * u * rstd_u (u itself without norm_u); y = gamma_y * h * rstd_h; rstd of a row = 1 / sqrt(mean of
+    its squares + eps).
+
+    x (None = 0), u, h, y: [rows, cols] (float32 or bfloat16; h and y may be x or u, either may be None); gate: [gates, cols] of that type, where
+    gates divides rows and each gate serves rows / gates neighbours; gamma_u, gamma_y: float32 [cols]; rstd_u, rstd_h: float32 [rows], written."""
+    mu = _matrix(u)
+    rows, cols = mu[1], mu[2]
+    _native.residual_norm(_matrix(x), mu, int(norm_u), _values(gamma_u, _F, cols), _matrix(gate), scale, _values(gamma_y, _F, cols), eps, _matrix(h),
+                          _matrix(y), _values(rstd_u, _F, rows), _values(rstd_h, _F, rows), _handle(stream))
+
+
+def residual_norm_workspace(u: torch.Tensor, gate: Optional[torch.Tensor] = None) -> int:
+    """Bytes that residual_norm_backward needs for these operands; residual_norm needs none."""
+    return _native.residual_norm_workspace(_matrix(u), _matrix(gate))
+
+
+def residual_norm_backward(x: Optional[torch.Tensor], u: torch.Tensor, gamma_u: Optional[torch.Tensor], gate: Optional[torch.Tensor],
+                           gamma_y: Optional[torch.Tensor], rstd_u: Optional[torch.Tensor], rstd_h: Optional[torch.Tensor],
+                           grad_h: Optional[torch.Tensor], grad_y: Optional[torch.Tensor], grad_x: Optional[torch.Tensor],
+                           grad_u: Optional[torch.Tensor], grad_gamma_u: Optional[torch.Tensor], grad_gate: Optional[torch.Tensor],
+                           grad_gamma_y: Optional[torch.Tensor], norm_u: bool = True, scale: float = 1.0,
+                           workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of sum(grad_h * h) + sum(grad_y * y); rstd_u and rstd_h as residual_norm left them.  Gradients that are None are not
+    computed; grad_x and grad_u may be grad_h, grad_y, x or u, but not one tensor."""
+    mu, mg = _matrix(u), _matrix(gate)
+    rows, cols = mu[1], mu[2]
+    ws, n, _keep = _workspace(workspace, _native.residual_norm_workspace(mu, mg) if workspace is None else 0, u.device, stream)
+    _native.residual_norm_backward(_matrix(x), mu, int(norm_u), _values(gamma_u, _F, cols), mg, scale, _values(gamma_y, _F, cols),
+                                   _values(rstd_u, _F, rows), _values(rstd_h, _F, rows), _matrix(grad_h), _matrix(grad_y), _matrix(grad_x),
+                                   _matrix(grad_u), _values(grad_gamma_u, _F, cols), _matrix(grad_gate), _values(grad_gamma_y, _F, cols), ws, n,
+                                   _handle(stream))
+
+
 _lib.dol_tensor_list_create.argtypes = [C.c_int32, _i32p, C.POINTER(C.c_int64), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p)]
 _lib.dol_tensor_list_destroy.argtypes = [C.c_void_p]
 _lib.dol_tensor_list_destroy.restype = None

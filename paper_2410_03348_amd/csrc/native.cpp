@@ -387,6 +387,43 @@ PyObject *newton_schulz(PyObject *, PyObject *const *v, Py_ssize_t n)
     DOL_CALL(dol_newton_schulz(g.p(), g_stride, o.p(), o_stride, batch, steps, abc, eps, ws, have, s));
 }
 
+PyObject *residual_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 13);
+    Matrix x(a, 0), u(a, 1), gate(a, 4), h(a, 8), y(a, 9);
+    const int32_t norm_u = a.num32(2);
+    auto *gamma_u = a.ptr<float>(3), *gamma_y = a.ptr<float>(6);
+    const float scale = static_cast<float>(a.real(5)), eps = static_cast<float>(a.real(7));
+    auto *rstd_u = a.ptr<float>(10), *rstd_h = a.ptr<float>(11);
+    void *s = a.stream(12);
+    DOL_CALL(dol_residual_norm(x.p(), u.p(), norm_u, gamma_u, gate.p(), scale, gamma_y, eps, h.p(), y.p(), rstd_u, rstd_h, s));
+}
+
+PyObject *residual_norm_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 2);
+    Matrix u(a, 0), gate(a, 1);
+    if (a.bad) return nullptr;
+    int64_t need = 0;
+    const dol_status st = dol_residual_norm_workspace(u.p(), gate.p(), &need);
+    return bytes(st, need);
+}
+
+PyObject *residual_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 19);
+    Matrix x(a, 0), u(a, 1), gate(a, 4), gh(a, 9), gy(a, 10), gx(a, 11), gu(a, 12), gg(a, 14);
+    const int32_t norm_u = a.num32(2);
+    auto *gamma_u = a.ptr<float>(3), *gamma_y = a.ptr<float>(6);
+    const float scale = static_cast<float>(a.real(5));
+    auto *rstd_u = a.ptr<float>(7), *rstd_h = a.ptr<float>(8), *ggu = a.ptr<float>(13), *ggy = a.ptr<float>(15);
+    auto *ws = a.ptr<void>(16);
+    const int64_t have = a.num(17);
+    void *s = a.stream(18);
+    DOL_CALL(dol_residual_norm_backward(x.p(), u.p(), norm_u, gamma_u, gate.p(), scale, gamma_y, rstd_u, rstd_h, gh.p(), gy.p(), gx.p(), gu.p(), ggu, gg.p(), ggy,
+                                        ws, have, s));
+}
+
 PyObject *grad_norm_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     Args a(v, n, 1);
@@ -583,6 +620,9 @@ PyMethodDef g_methods[] = {
     {"group_norm_workspace", DOL_FAST(group_norm_workspace)},
     {"group_norm", DOL_FAST(group_norm)},
     {"group_norm_backward", DOL_FAST(group_norm_backward)},
+    {"residual_norm", DOL_FAST(residual_norm)},
+    {"residual_norm_workspace", DOL_FAST(residual_norm_workspace)},
+    {"residual_norm_backward", DOL_FAST(residual_norm_backward)},
     {"grad_norm_workspace", DOL_FAST(grad_norm_workspace)},
     {"grad_norm", DOL_FAST(grad_norm)},
     {"clip_grads", DOL_FAST(clip_grads)},

@@ -40,3 +40,27 @@ def test_host_tensors_are_refused_in_lists():
     torch = pytest.importorskip("torch")
     with pytest.raises(AssertionError):
         dol.TensorList([torch.zeros(3)])
+
+
+def matrix(rows, cols, dtype=F32, ld=None, data=4096):
+    return dtype, rows, cols, cols if ld is None else ld, data
+
+
+@pytest.mark.parametrize("u,gate,why", [
+    (None, None, "NULL"), (matrix(8, 16, 7), None, "type"), (matrix(8, 0), None, "columns"), (matrix(8, (1 << 24) + 1), None, "EUNSUPPORTED"),
+    (matrix(8, 16, ld=15), None, "ESHAPE"), (matrix(8, 16), matrix(3, 16), "divide"), (matrix(8, 16), matrix(0, 16), "divide"),
+    (matrix(8, 16), matrix(16, 16), "divide"), (matrix(8, 16), matrix(4, 15), "columns"), (matrix(8, 16), matrix(4, 16, BF16), "type"),
+    (matrix(-1, 16), None, "ESHAPE")])
+def test_residual_norm_refusals(u, gate, why):
+    with pytest.raises(dol.DolError, match=why):
+        dol._native.residual_norm_workspace(u, gate)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,gates,cols", [(1, 1, 1), (64, 0, 32), (64, 8, 4096), (1 << 20, 1 << 19, 8), (1 << 20, 1 << 10, 512), (100, 50, 40000), (1 << 20, 1 << 20, 32),
+                                             ((1 << 31) - 1, 1, 4), (1 << 30, 1 << 25, 4)])
+def test_residual_norm_workspace(rows, gates, cols, dtype):
+    """Sums over rows leave a part to a workgroup: no more than the tensors themselves but for small ones, and as much as a row's sums where rows are read twice."""
+    n = dol._native.residual_norm_workspace(matrix(rows, cols, dtype), matrix(gates, cols, dtype) if gates else None)
+    assert 0 < n and n % 256 == 0 and n <= max(3 * 1024 * (cols + 64) * 4, 3 * rows * cols * 4 + rows * 8) + 4096
+    assert dol._native.residual_norm_workspace(matrix(0, cols, dtype), None) == 0
