@@ -229,12 +229,16 @@ def _plain_clip(s):
 def _own_linear(s):
     from paper_2410_03348_amd import binding as dol
     z = s["z"] if s["train"] else None
-    dol.linear(s["x"], s["weight"], s["y"], bias=s["bias"], act=s["act"], residual=s["stream"], z=z)
+    if z is not None and z.dtype == torch.bfloat16 and "rest" not in s:
+        s["rest"] = torch.empty(z.shape, dtype=torch.uint8, device=DEV)         # kept beside z
+    rest = s.get("rest")
+    dol.linear(s["x"], s["weight"], s["y"], bias=s["bias"], act=s["act"], residual=s["stream"], z=z, z_rest=rest)
     out = {"y": s["y"]}
     if s["train"]:
         if z is not None:
             out["z"] = z
-        dol.linear_backward(s["x"], s["weight"], s["grad_y"], s["grad_x"], s["grad_weight"], grad_bias=s["grad_bias"], act=s["act"], z=z)
+        dol.linear_backward(s["x"], s["weight"], s["grad_y"], s["grad_x"], s["grad_weight"], grad_bias=s["grad_bias"], act=s["act"], z=z,
+                            z_rest=rest)
         out["grad_x"], out["grad_weight"], out["grad_bias"] = s["grad_x"], s["grad_weight"], s["grad_bias"]
     return out
 
