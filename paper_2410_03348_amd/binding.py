@@ -792,6 +792,43 @@ def group_norm_backward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Op
                                 _handle(stream))
 
 
+def linear_workspace(x: torch.Tensor, weight: torch.Tensor, backward: bool = False) -> int:
+    """Bytes that linear (or linear_backward) needs for these operands."""
+    return _native.linear_workspace(_matrix(x), _matrix(weight), int(backward))
+
+
+def linear_kernel(x: torch.Tensor, weight: torch.Tensor, backward: bool = False) -> str:
+    """The kernel that multiplies for these operands, and its tiles."""
+    return _native.linear_kernel(_matrix(x), _matrix(weight), int(backward))
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, y: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
+           residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None, z_rest: Optional[torch.Tensor] = None,
+           workspace: Optional[torch.Tensor] = None, stream=None):
+    """y = act(z) + residual, z = x weight^T + bias.
+
+    x [rows, width], weight [out, width] (float32 or bfloat16); y, residual, z [rows, out] of that type, y may be the residual; bias float32
+    [out]; act: "none", "relu", "silu" or "gelu".  The gradients need z where act is not "none"; z_rest uint8 [rows, out], beside a z in bfloat16,
+    keeps grad_bias as exact as sums in 32 bits."""
+    mx, mw = _matrix(x), _matrix(weight)
+    rows, out = mx[1], mw[1]
+    ws, n, _keep = _workspace(workspace, _native.linear_workspace(mx, mw, 0) if workspace is None else 0, x.device, stream)
+    _native.linear(mx, mw, _values(bias, _F, out), _ACTS[act], _matrix(residual), _matrix(y), _matrix(z), _values(z_rest, torch.uint8, rows, out), ws, n,
+                   _handle(stream))
+
+
+def linear_backward(x: torch.Tensor, weight: torch.Tensor, grad_y: torch.Tensor, grad_x: Optional[torch.Tensor],
+                    grad_weight: Optional[torch.Tensor], grad_bias: Optional[torch.Tensor] = None, act: str = "none",
+                    z: Optional[torch.Tensor] = None, z_rest: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                    stream=None):
+    """Gradients of sum(grad_y * y); z and z_rest as linear left them.  Gradients that are None are not computed; the residual's is grad_y."""
+    mx, mw = _matrix(x), _matrix(weight)
+    rows, out = mx[1], mw[1]
+    ws, n, _keep = _workspace(workspace, _native.linear_workspace(mx, mw, 1) if workspace is None else 0, x.device, stream)
+    _native.linear_backward(mx, mw, _ACTS[act], _matrix(z), _values(z_rest, torch.uint8, rows, out), _matrix(grad_y), _matrix(grad_x),
+                            _matrix(grad_weight), _values(grad_bias, _F, out), ws, n, _handle(stream))
+
+
 def residual_norm(x: Optional[torch.Tensor], u: torch.Tensor, gamma_u: Optional[torch.Tensor], gate: Optional[torch.Tensor],
                   gamma_y: Optional[torch.Tensor], h: Optional[torch.Tensor], y: Optional[torch.Tensor], rstd_u: Optional[torch.Tensor] = None,
                   rstd_h: Optional[torch.Tensor] = None, norm_u: bool = True, scale: float = 1.0, eps: float = 1e-6, stream=None):

@@ -11,11 +11,9 @@
 // hundred MB or so that the next launch reads), and grad_x and grad_w are two sets of tiles of one launch, which read dl, x and w as they
 // lie, along rows or across them (mfma_tile.h).
 // A few classes, whose logits a workgroup holds, have a form of their own (xent_few_kernel).
-#include "mfma_tile.h"
+#include "mfma_products.h"
 
 #include <cstdio>
-#include <type_traits>
-#include <utility>
 
 namespace dol {
 namespace {
@@ -26,109 +24,15 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 constexpr float kFar = 1e6f;
 constexpr int kPad = 256;                               // rows and classes of a piece are filled up to a multiple of this
 constexpr int64_t kMostPieceBytes = int64_t(192) << 20; // of dl
-constexpr int kUnits = 256;                             // compute units of the chip
-constexpr int kLds = 160 * 1024;                        // of each
-
-// Tiles of logits, and of the two products that dl goes into in Q planes.
-template <int P, int Q>
-struct Shapes;
-template <>
-struct Shapes<1, 1> {       // bf16
-    using Big = MfmaTile<bf16x8, 1, 1, kRows, kRows, 256, 256, 64, 2, 4, 2>;
-    using Small = MfmaTile<bf16x8, 1, 1, kRows, kRows, 128, 128, 64, 4, 2, 2>;
-    using BigX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 256, 256, 64, 2, 4, 2>;
-    using BigW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 256, 256, 64, 2, 4, 2>;
-    using SmallX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 128, 128, 64, 4, 2, 2>;
-    using SmallW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 128, 128, 64, 4, 2, 2>;
-    using Tiny = MfmaTile<bf16x8, 1, 1, kRows, kRows, 64, 64, 64, 4, 1, 3>;
-    using TinyX = MfmaTile<bf16x8, 1, 1, kCols, kRows, 64, 64, 64, 4, 1, 3>;
-    using TinyW = MfmaTile<bf16x8, 1, 1, kCols, kCols, 64, 64, 64, 4, 1, 3>;
-};
-template <>
-struct Shapes<1, 2> : Shapes<1, 1> {
-    using BigX = MfmaTile<bf16x8, 1, 2, kCols, kRows, 128, 128, 32, 4, 2, 2>;
-    using BigW = MfmaTile<bf16x8, 1, 2, kCols, kCols, 128, 128, 32, 4, 2, 2>;
-    using SmallX = BigX;
-    using SmallW = BigW;
-    using TinyX = MfmaTile<bf16x8, 1, 2, kCols, kRows, 64, 64, 64, 4, 1, 3>;
-    using TinyW = MfmaTile<bf16x8, 1, 2, kCols, kCols, 64, 64, 64, 4, 1, 3>;
-};
-template <>
-struct Shapes<3, 3> {       // float
-    using Big = MfmaTile<bf16x8, 3, 3, kRows, kRows, 128, 256, 32, 2, 4, 2>;
-    using Small = MfmaTile<bf16x8, 3, 3, kRows, kRows, 128, 128, 32, 4, 2, 2>;
-    using BigX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 128, 256, 32, 2, 4, 2>;
-    using BigW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 128, 256, 32, 2, 4, 2>;
-    using SmallX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 128, 128, 32, 4, 2, 2>;
-    using SmallW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 128, 128, 32, 4, 2, 2>;
-    using Tiny = MfmaTile<bf16x8, 3, 3, kRows, kRows, 64, 64, 64, 4, 1, 3>;
-    using TinyX = MfmaTile<bf16x8, 3, 3, kCols, kRows, 64, 64, 64, 4, 1, 3>;
-    using TinyW = MfmaTile<bf16x8, 3, 3, kCols, kCols, 64, 64, 64, 4, 1, 3>;
-};
-
-template <int P>
-struct Source { using T = float; };
-template <>
-struct Source<1> { using T = __bf16; };
-
-// Plane k of N.
-template <int N>
-__device__ __forceinline__ uint32_t plane_of(int k, float &x) { return N > 1 && k == 0 ? take_first_plane(x) : take_plane<__bf16>(x); }
-
-__device__ __forceinline__ bool kept_row(int32_t target, int32_t classes) { return target >= 0 && target < classes; }
 
 // ---------------------------------------------------------------- layouts for the matrix cores
-
-// A matrix laid out for the tiles: out[p][r][0..kp) = planes of src[r][0..cols), zeros behind and in rows past the source's.  Rows that do
-// not count (if target and lse are given) are taken as zeros, whatever they hold.
-struct Pack {
-    const void *src;
-    int64_t ld, rows;
-    int32_t cols;
-    const int32_t *target;
-    const float *lse;
-    int32_t classes;
-    uint16_t *out;
-    int64_t out_rows, kp, out_ld;
-    bool vec;
-    unsigned blocks;            // none where the matrix is read as it is
-};
 
 // Two of them in one launch, eight elements to a thread.  Bytes bound it: 8 192 x 1 024 of bf16 in 9.5 us, 3.5 TB/s.
 template <typename S, int P>
 __global__ void __launch_bounds__(256) xent_pack_kernel(Pack p0, Pack p1)
 {
-    const bool second = blockIdx.x >= p0.blocks;
-    const Pack &p = second ? p1 : p0;
-    const int64_t per = p.kp / 8, all = p.out_rows * per;
-    for (int64_t t = static_cast<int64_t>(blockIdx.x - (second ? p0.blocks : 0)) * 256 + threadIdx.x; t < all; t += static_cast<int64_t>(p.blocks) * 256) {
-        const int64_t r = t / per;
-        const int c = static_cast<int>(t - r * per) * 8;
-        const bool in = r < p.rows && (!p.target || (kept_row(p.target[r], p.classes) && p.lse[r] != -INFINITY));
-        const S *from = static_cast<const S *>(p.src) + r * p.ld + c;
-        float v[8];
-        if (in && p.vec && c + 8 <= p.cols) {
-            struct alignas(16) Piece { S e[16 / sizeof(S)]; };
-#pragma unroll
-            for (int h = 0; h < static_cast<int>(8 * sizeof(S) / 16); ++h) {
-                const Piece q = reinterpret_cast<const Piece *>(from)[h];
-#pragma unroll
-                for (int k = 0; k < static_cast<int>(16 / sizeof(S)); ++k) v[h * (16 / sizeof(S)) + k] = static_cast<float>(q.e[k]);
-            }
-        } else
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = in && c + k < p.cols ? static_cast<float>(from[k]) : 0.0f;
-#pragma unroll
-        for (int q = 0; q < P; ++q) {
-            u32x4 w;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t lo = plane_of<P>(q, v[2 * k]), hi = plane_of<P>(q, v[2 * k + 1]);
-                w[k] = lo | hi << 16;
-            }
-            *reinterpret_cast<u32x4 *>(p.out + (q * p.out_rows + r) * p.out_ld + c) = w;
-        }
-    }
+    if (blockIdx.x < p0.blocks) pack_rows<S, P>(p0, blockIdx.x);
+    else pack_rows<S, P>(p1, blockIdx.x - p0.blocks);
 }
 
 // ---------------------------------------------------------------- forward
@@ -328,50 +232,6 @@ __global__ void __launch_bounds__(T::NT, 2) xent_dlogits_kernel(Planes x, Planes
     }
 }
 
-// One set of tiles of the launch that follows: out[n][m] = sum_k a[k][m] b(n, k), k in `splits` shares.  Rows of a tile are elements of x or w,
-// which lie side by side in `out` too.
-struct Product {
-    Planes a, b;
-    int32_t M, N;               // columns of out, rows of out
-    int32_t wide, tall;         // what a and b have of them in memory
-    int32_t tm, tn, splits, steps;
-    int64_t k, have;            // that count, and that there are of operands which lie across k
-    float *part;                // [splits][N][part_ld], or null: out is written
-    int64_t part_ld;
-    bool add;                   // to what part holds
-    void *out;
-    int64_t out_ld;
-};
-
-template <typename T, typename O>
-__device__ __forceinline__ void product_tile(const Product &p, int id, char *smem)
-{
-    const int tiles = p.tm * p.tn, split = id / tiles;
-    int mt, nt;
-    tile_of(id - split * tiles, p.tm, p.tn, 4, mt, nt);
-    const int s0 = static_cast<int>(static_cast<int64_t>(p.steps) * split / p.splits), s1 = static_cast<int>(static_cast<int64_t>(p.steps) * (split + 1) / p.splits);
-    const int64_t k0 = static_cast<int64_t>(s0) * T::BK;
-    f32x4 acc[T::MI][T::NI];
-    T::clear(acc);
-    T::run(p.a, static_cast<int64_t>(mt) * T::BM, p.wide, p.b, static_cast<int64_t>(nt) * T::BN, p.tall, k0, s1 - s0, smem, acc, p.have - k0);
-    const bool vec = p.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (4 * sizeof(O) - 1)) == 0;
-#pragma unroll
-    for (int j = 0; j < T::NI; ++j) {
-        const int n = nt * T::BN + T::col_of(j);
-        if (n >= p.N) continue;
-#pragma unroll
-        for (int i = 0; i < T::MI; ++i) {
-            const int m = mt * T::BM + T::row_of(i);
-            if (m >= p.M) continue;
-            if (p.part) {       // (its rows are filled up to whole fours)
-                f32x4 *to = reinterpret_cast<f32x4 *>(p.part + (static_cast<int64_t>(split) * p.N + n) * p.part_ld + m);
-                *to = p.add ? *to + acc[i][j] : acc[i][j];
-            } else
-                store4(static_cast<O *>(p.out) + n * p.out_ld + m, acc[i][j], p.M - m, vec);
-        }
-    }
-}
-
 // grad_x's tiles (TX: dl along its rows) and grad_w's (TW: dl across them), in one launch since each alone seldom fills the chip.  Loads into
 // LDS bound it: 8 192 x 1 024 into 65 535 in bf16 1 821 to 1 890 us in all, 1 163 to 1 207 TFLOP/s; float 1 000 x 300 into 5 003 51 us, 700 TFLOP/s of
 // planes.  (256 x 256 in bf16 has 4 registers more than there are, which it spills.)
@@ -384,44 +244,6 @@ __global__ void __launch_bounds__(TX::NT, 2) xent_products_kernel(Product px, Pr
     const int first = px.tm * px.tn * px.splits, id = blockIdx.x;
     if (id < first) product_tile<TX, O>(px, xcd_contiguous(id, first), smem);
     else product_tile<TW, O>(pw, xcd_contiguous(id - first, gridDim.x - first), smem);
-}
-
-// out[m][n] = the sum of its parts, in an order that the sizes fix.
-struct Sum {
-    const float *part;
-    int32_t M, N, splits;       // rows, columns
-    int64_t part_ld;
-    void *out;
-    int64_t out_ld;
-    bool shared;                // four threads to four columns, each for a quarter of the parts
-    unsigned blocks;            // none where nothing is to be summed
-};
-
-template <typename O>
-__device__ __forceinline__ void sum_parts(const Sum &s, unsigned block)
-{
-    __shared__ f32x4 red[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t per = (s.N + 3) / 4, all = s.M * per;
-    const bool vec = s.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(s.out) & (4 * sizeof(O) - 1)) == 0;
-    const int each = s.shared ? 64 : 256, at = s.shared ? lane : threadIdx.x;
-    for (int64_t first = static_cast<int64_t>(block) * each; first < all; first += static_cast<int64_t>(s.blocks) * each) {
-        const int64_t t = first + at, m = t / per;
-        const bool in = t < all;
-        const int n = static_cast<int>(t - m * per) * 4;
-        f32x4 v = {0, 0, 0, 0};
-        if (in)
-#pragma unroll 8
-            for (int k = s.shared ? wave : 0; k < s.splits; k += s.shared ? 4 : 1) v += *reinterpret_cast<const f32x4 *>(s.part + (static_cast<int64_t>(k) * s.M + m) * s.part_ld + n);
-        if (s.shared) {
-            red[wave][lane] = v;
-            __syncthreads();
-            v = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
-            __syncthreads();
-            if (wave != 0) continue;
-        }
-        if (in) store4(static_cast<O *>(s.out) + m * s.out_ld + n, v, s.N - n, vec);
-    }
 }
 
 // Up to three sums in one launch: of grad_x's, of grad_w's and of grad_bias's parts (one row of classes).
@@ -578,20 +400,6 @@ __global__ void __launch_bounds__(256) xent_zero_kernel(O *out, int64_t ld, int6
 
 // ---------------------------------------------------------------- host side
 
-constexpr int32_t kMostRows = 1 << 22;      // of either operand: a lane's offsets into a tile of dl fit 32 bits
-constexpr int32_t kMostWidth = 1 << 20;     // of a row: 64 columns to a workgroup of a grid's second dimension
-
-bool direct(const dol_matrix *m)            // can be read by the tiles as it is
-{
-    return m->dtype == DOL_BF16 && m->cols % 64 == 0 && m->ld % 8 == 0 && m->ld <= kMostRows && !(reinterpret_cast<uintptr_t>(m->data) & 15);
-}
-
-int32_t tiles(int64_t n, int t) { return static_cast<int32_t>((n + t - 1) / t); }
-unsigned blocks(int64_t n) { return static_cast<unsigned>((n + 255) / 256); }
-
-// Launches have less than 2^32 threads: workgroups of what is done element by element, at most (each then takes several pieces in turn).
-constexpr int64_t kMostBlocks = 1 << 15;
-
 struct Layout {
     int32_t rows, width, classes;
     int64_t kp, n_pad;                      // width and rows as they are laid out
@@ -615,26 +423,6 @@ bool few_classes(const dol_matrix *x, const dol_matrix *w)
 {
     return w->rows <= 32 && int64_t(w->rows) * w->cols <= (x->dtype == DOL_F32 ? 32768 : 8192) && x->rows <= 16384;
 }
-
-// When `slots` places, each of which takes the next one as it becomes free, are done with n1 pieces of work of length a and then n2 of
-// length b.
-double done(int64_t n1, double a, int64_t n2, double b, int64_t slots)
-{
-    const int64_t late = n1 % slots;                    // so many places are free one a later than the others
-    double soon = n1 / slots * a, then = soon + a;
-    double end = late ? then : soon;
-    while (n2 > 0) {
-        if (late == 0 || soon <= then) soon += b, n2 -= slots - late, end = std::max(end, soon);
-        else then += b, n2 -= late, end = std::max(end, then);
-    }
-    return end;
-}
-
-template <typename T>
-struct Type { using Tile = T; };
-
-template <typename B, typename S, typename T, typename F>
-auto by_size(int size, B big, S small, T tiny, F f) { return size == 2 ? f(big) : size == 1 ? f(small) : f(tiny); }
 
 // Tiles of 64 x 64 below so many of 128 x 128 (of logits) or k of a place with them (of the products).  Forward and backward, us, 64 x 64 /
 // 128 x 128 in both: float 64 x 128 x 360 35 / 50, 100 x 100 x 1 000 33 / 50; bf16 26 / 32, 28 / 36.  Logits alone: float 300 x 256 x 3 000 (72
@@ -747,20 +535,6 @@ auto with_planes(const dol_matrix *x, F f)
     return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
 }
 
-// Rows with contiguous k as the tiles read them: the matrix itself, or `out`, its planes in rows of kp elements (out_rows of them).
-template <int P>
-Pack pack_of(const dol_matrix *m, const int32_t *target, const float *lse, int32_t classes, uint16_t *out, int64_t out_rows, int64_t kp, int64_t ld, Planes *p)
-{
-    using S = typename Source<P>::T;
-    if (!out) {
-        *p = Planes{static_cast<const uint16_t *>(m->data), m->ld, 0};
-        return Pack{};
-    }
-    *p = Planes{out, ld, out_rows * ld};
-    const bool vec = !(reinterpret_cast<uintptr_t>(m->data) & 15) && m->ld % (16 / int64_t(sizeof(S))) == 0;
-    return Pack{m->data, m->ld, m->rows, m->cols, target, lse, classes, out, out_rows, kp, ld, vec, blocks(std::min(out_rows * (kp / 8), kMostBlocks * 256))};
-}
-
 template <int P>
 dol_status launch_pack(const Pack &a, const Pack &b, hipStream_t st)
 {
@@ -778,14 +552,6 @@ dol_status launch_finish(const Sum &x, const Sum &w, const Sum &bias, hipStream_
     xent_finish_kernel<O><<<n, 256, 0, st>>>(x, w, bias);
     DOL_HIP(hipGetLastError());
     return DOL_OK;
-}
-
-// (few parts are read as fast by a thread each; a loop over many of them waits for every load)
-Sum make_sum(const float *part, int32_t M, int32_t N, int32_t splits, int64_t part_ld, void *out, int64_t out_ld)
-{
-    const bool shared = splits >= 16;
-    const int64_t n = int64_t(M) * ((N + 3) / 4);
-    return Sum{part, M, N, splits, part_ld, out, out_ld, shared, static_cast<unsigned>(std::min((n + (shared ? 63 : 255)) / (shared ? 64 : 256), kMostBlocks))};
 }
 
 template <typename S, bool BACK>
@@ -863,12 +629,6 @@ dol_status launch_products(Product x, Product w, hipStream_t st)
     xent_products_kernel<TX, TW, O><<<n, TX::NT, TX::LDS, st>>>(x, w);
     DOL_HIP(hipGetLastError());
     return DOL_OK;
-}
-
-Sum sum_of(const Product &p)
-{
-    if (!p.part) return Sum{};
-    return make_sum(p.part, p.N, p.M, p.splits, p.part_ld, p.out, p.out_ld);
 }
 
 template <int P, int Q>

@@ -1,0 +1,674 @@
+// A linear layer with what follows it, and its gradients.
+//
+//   z = x w^T + bias,   y = act(z) + residual
+//   dz = grad_y act'(z),   grad_x = dz w,   grad_w = dz^T x,   grad_bias[o] = sum_i dz[i, o]
+//
+// A tile of z stays in the registers that the matrix cores leave it in, and y (and z, where the gradients need it) is written from there.  Few
+// tiles share out their k, and a second launch adds up the shares and does the rest.  Up to 64 rows are no work for tiles: every weight is read for
+// them once, which is what bounds the call, straight from memory into the operands of the matrix cores (linear_few_kernel).
+// Backward: dz is rounded for the matrix cores and written, with its sums over rows beside it, and grad_x and grad_w are two sets of tiles
+// of one launch (mfma_products.h).
+#include "activation.h"
+#include "loose.h"
+#include "mfma_products.h"
+
+#include <cstdio>
+
+namespace dol {
+namespace {
+
+// What a call leaves of z.
+struct Result {
+    const float *bias;
+    const void *residual;
+    int64_t residual_ld;
+    void *y, *z;
+    int64_t y_ld, z_ld;
+    uint8_t *rest;              // [rows][cols]
+    int32_t rows, cols, act;
+    bool vec;                   // four neighbouring columns from a multiple of four on are aligned to their size, in all of them
+};
+
+// What rounding z to bf16 leaves, in 256ths of a step, of -128 .. 127: of the float's 24 bits 16 are kept, so that sums of act'(z) in 32 bits are
+// off by 2^-17 and not 2^-9 a term.  The bits of a float count its steps across powers of two as well.
+__device__ __forceinline__ uint32_t rest_of(float z)
+{
+    const int r = static_cast<int>(__float_as_uint(z) - (bits16<__bf16>(z) << 16));
+    return __builtin_isfinite(z) ? static_cast<uint32_t>(min((r + 128) >> 8, 127)) & 0xFF : 0;
+}
+
+__device__ __forceinline__ float with_rest(float z, uint32_t rest)
+{
+    return __uint_as_float(__float_as_uint(z) + (static_cast<uint32_t>(static_cast<int8_t>(rest)) << 8));
+}
+
+// Columns c .. c + 3 of row r of z to what the call leaves; n of them are there.
+template <typename S, typename A>
+__device__ __forceinline__ void leave(const Result &o, A, int64_t r, int c, f32x4 z)
+{
+    const int n = o.cols - c;
+    S *y = static_cast<S *>(o.y) + r * o.y_ld + c;
+    if (o.bias)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[k] += k < n ? o.bias[c + k] : 0.0f;
+    if (o.z) {
+        store4(static_cast<S *>(o.z) + r * o.z_ld + c, z, n, o.vec);
+        if (sizeof(S) == 2 && o.rest) {
+            uint8_t *to = o.rest + r * o.cols + c;
+            if (o.vec && n >= 4) *reinterpret_cast<uint32_t *>(to) = rest_of(z[0]) | rest_of(z[1]) << 8 | rest_of(z[2]) << 16 | rest_of(z[3]) << 24;
+            else
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (k < n) to[k] = static_cast<uint8_t>(rest_of(z[k]));
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) z[k] = act_of<A::value, false>(z[k], nullptr);
+    if (o.residual) {
+        const S *from = static_cast<const S *>(o.residual) + r * o.residual_ld + c;
+        if (o.vec && n >= 4) {
+            struct alignas(4 * sizeof(S)) Four { S e[4]; };
+            const Four q = *reinterpret_cast<const Four *>(from);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[k] += static_cast<float>(q.e[k]);
+        } else
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < n) z[k] += static_cast<float>(from[k]);
+    }
+    store4(y, z, n, o.vec);
+}
+
+// ---------------------------------------------------------------- tiles
+
+struct Tiles {
+    int32_t tm, tn, splits, steps;
+    float *part;                // [splits][rows][part_ld], or null: one share
+    int64_t part_ld;
+};
+
+template <typename T, typename S>
+__global__ void __launch_bounds__(T::NT, 2) linear_tiles_kernel(Planes x, Planes w, Tiles g, Result o)
+{
+    extern __shared__ __align__(128) char smem[];
+    const int id = xcd_contiguous(blockIdx.x, gridDim.x), each = g.tm * g.tn, split = id / each;
+    int mt, nt;
+    tile_of(id - split * each, g.tm, g.tn, 8, mt, nt);
+    const int s0 = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<int64_t>(g.steps) * split / g.splits));
+    const int s1 = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<int64_t>(g.steps) * (split + 1) / g.splits));
+    f32x4 acc[T::MI][T::NI];
+    T::clear(acc);
+    const int m0 = __builtin_amdgcn_readfirstlane(mt * T::BM), n0 = __builtin_amdgcn_readfirstlane(nt * T::BN);     // (quotients, in vector registers)
+    T::run(x, m0, o.rows, w, n0, o.cols, static_cast<int64_t>(s0) * T::BK, s1 - s0, smem, acc);
+    const int c = n0 + T::col_of();
+    if (c >= o.cols) return;
+    auto rows = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < T::MI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t r = m0 + T::row_of(i) + e;
+                if (r < o.rows) f(r, f32x4{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]});
+            }
+    };
+    if (g.part) rows([&](int64_t r, f32x4 z) { *reinterpret_cast<f32x4 *>(g.part + (split * static_cast<int64_t>(o.rows) + r) * g.part_ld + c) = z; });
+    else rows([&](int64_t r, f32x4 z) { with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, z); }); });
+}
+
+// The shares of k added up, in their order, and what follows.
+template <typename S>
+__global__ void __launch_bounds__(256) linear_join_kernel(const float *part, int64_t part_ld, int splits, Result o)
+{
+    const int64_t per = (o.cols + 3) / 4, all = o.rows * per;
+    for (int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; t < all; t += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t r = t / per;
+        const int c = static_cast<int>(t - r * per) * 4;
+        f32x4 z = {0, 0, 0, 0};
+#pragma unroll 8
+        for (int k = 0; k < splits; ++k) z += *reinterpret_cast<const f32x4 *>(part + (static_cast<int64_t>(k) * o.rows + r) * part_ld + c);
+        with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, z); });
+    }
+}
+
+// ---------------------------------------------------------------- few rows
+
+// Sixteen outs and up to 16 R rows to a workgroup, whose wavefronts share out its k.  A lane loads 32 neighbouring bytes of the row of w (l & 15) and
+// of rows of x, four lanes a line of 128; which of a product's k these are does not matter, as long as both operands agree.
+// float as it is, by v_mfma_f32_16x16x4.
+constexpr int kFewWaves = 16;
+
+template <typename S, int R>
+__global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(const S *x, int64_t ldx, const S *w, int64_t ldw, int32_t width, int32_t each, int32_t groups, float *part,
+                                                                    int64_t part_ld, Result o)
+{
+    constexpr int V = kLooseElements<S>, STEP = 8 * V;       // k of a step: two vectors to each of four lanes
+    __shared__ f32x4 red[kFewWaves][R][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int group = blockIdx.x % groups, split = blockIdx.x / groups;
+    const int64_t k0 = static_cast<int64_t>(split * waves + wave) * each, k1 = min(k0 + each, static_cast<int64_t>(width));
+    const S *from_w = w + min(group * 16 + (lane & 15), o.cols - 1) * ldw, *from_x[R];
+    f32x4 acc[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) from_x[r] = x + min(r * 16 + (lane & 15), o.rows - 1) * ldx, acc[r] = f32x4{0, 0, 0, 0};
+    auto products = [&](const Loose<S> (&a)[2], const Loose<S> (&b)[R][2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if constexpr (sizeof(S) == 2) acc[r] = Mfma<bf16x8>::go(__builtin_bit_cast(bf16x8, a[h]), __builtin_bit_cast(bf16x8, b[r][h]), acc[r]);
+                else
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(loose_get(a[h], e), loose_get(b[r][h], e), acc[r], 0, 0, 0);
+            }
+    };
+    int64_t k = k0 + (lane >> 4) * (2 * V);
+    constexpr int U = R == 1 ? 4 : 2;
+    const int64_t whole = k0 + (k1 > k0 ? (k1 - k0) / (U * STEP) * (U * STEP) : 0);
+    for (int64_t at = k0; at < whole; at += U * STEP, k += U * STEP) {
+        Loose<S> a[U][2], b[U][R][2];
+#pragma unroll
+        for (int q = 0; q < U; ++q)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) a[q][h] = *reinterpret_cast<const Loose<S> *>(from_w + k + q * STEP + h * V);
+#pragma unroll
+        for (int q = 0; q < U; ++q)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) b[q][r][h] = *reinterpret_cast<const Loose<S> *>(from_x[r] + k + q * STEP + h * V);
+#pragma unroll
+        for (int q = 0; q < U; ++q) products(a[q], b[q]);
+    }
+    for (int64_t at = max(whole, k0); at < k1; at += STEP, k += STEP) {
+        Loose<S> a[2], b[R][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            a[h] = loose_load(from_w + k + h * V, k1 - k - h * V);
+#pragma unroll
+            for (int r = 0; r < R; ++r) b[r][h] = loose_load(from_x[r] + k + h * V, k1 - k - h * V);
+        }
+        products(a, b);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) red[wave][r][lane] = acc[r];
+    lds_barrier();
+    for (int m = wave; m < R; m += waves) {
+        f32x4 z = red[0][m][lane];
+        for (int q = 1; q < waves; ++q) z += red[q][m][lane];
+        const int64_t r = m * 16 + (lane & 15);
+        const int c = group * 16 + (lane >> 4) * 4;
+        if (r >= o.rows || c >= o.cols) continue;
+        if (part) *reinterpret_cast<f32x4 *>(part + (split * static_cast<int64_t>(o.rows) + r) * part_ld + c) = z;
+        else with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, z); });
+    }
+}
+
+// ---------------------------------------------------------------- backward
+
+// x and w laid out, where the tiles cannot read them as they are.
+template <typename S, int P>
+__global__ void __launch_bounds__(256) linear_pack_kernel(Pack p0, Pack p1)
+{
+    if (blockIdx.x < p0.blocks) pack_rows<S, P>(p0, blockIdx.x);
+    else pack_rows<S, P>(p1, blockIdx.x - p0.blocks);
+}
+
+// dz in Q planes, zeros behind its columns and in rows past the last, and its sums over rows.
+struct Slope {
+    const void *grad_y, *z;
+    int64_t grad_ld, z_ld;
+    const uint8_t *rest;
+    int32_t rows, cols, act;
+    uint16_t *dz;               // null: only the sums
+    int64_t out_rows, out_cols, ld, plane;      // as they are laid out
+    float *part;                // [chunks][out_cols], null: only dz
+    int32_t chunk;              // rows, of 8 at a time
+    int32_t wide;               // workgroups side by side
+};
+
+// 32 threads of eight columns by eight rows at a time.
+template <typename S, int Q>
+__global__ void __launch_bounds__(256) linear_slope_kernel(Slope p)
+{
+    __shared__ float red[8][256];
+    const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
+    const int64_t chunk = blockIdx.x / p.wide;
+    const int64_t c = static_cast<int64_t>(blockIdx.x % p.wide) * 256 + lane * 8, n = p.cols - c;
+    constexpr int V = kLooseElements<S>, H = 8 / V;
+    float sum[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+    with_act(p.act, [&](auto a) {
+        for (int64_t r = chunk * p.chunk + row; r < min((chunk + 1) * p.chunk, p.out_rows) && c < p.out_cols; r += 8) {
+            const int64_t left = r < p.rows ? n : 0;
+            float v[8], z[8];
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                const Loose<S> g = loose_load(static_cast<const S *>(p.grad_y) + r * p.grad_ld + c + h * V, left - h * V);
+                Loose<S> q{};
+                if (a.value != DOL_ACT_NONE) q = loose_load(static_cast<const S *>(p.z) + r * p.z_ld + c + h * V, left - h * V);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[h * V + e] = loose_get(g, e), z[h * V + e] = loose_get(q, e);
+            }
+            if (a.value != DOL_ACT_NONE) {
+                if (sizeof(S) == 2 && p.rest) {
+                    const uint8_t *from = p.rest + r * p.cols + c;
+                    struct __attribute__((packed, aligned(1))) Eight { uint32_t w[2]; } q{};
+                    if (left >= 8) q = *reinterpret_cast<const Eight *>(from);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (e < left) q.w[e >> 2] |= static_cast<uint32_t>(from[e]) << (e & 3) * 8;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = with_rest(z[e], q.w[e >> 2] >> (e & 3) * 8);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float slope;
+                    act_of<decltype(a)::value, true>(z[e], &slope);
+                    v[e] *= slope;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += v[e];
+            if (p.dz)
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    u32x4 o;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t lo = plane_of<Q>(q, v[2 * k]), hi = plane_of<Q>(q, v[2 * k + 1]);
+                        o[k] = lo | hi << 16;
+                    }
+                    *reinterpret_cast<u32x4 *>(p.dz + q * p.plane + r * p.ld + c) = o;
+                }
+        }
+    });
+    if (!p.part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[row][lane * 8 + e] = sum[e];
+    __syncthreads();
+    const int64_t at = static_cast<int64_t>(blockIdx.x % p.wide) * 256 + threadIdx.x;
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += red[k][threadIdx.x];
+    if (at < p.out_cols) p.part[chunk * p.out_cols + at] = s;
+}
+
+template <typename TX, typename TW, typename O>
+__global__ void __launch_bounds__(TX::NT, 2) linear_products_kernel(Product px, Product pw)
+{
+    static_assert(TX::LDS == TW::LDS && TX::NT == TW::NT, "one launch");
+    extern __shared__ __align__(128) char smem[];
+    // each XCD gets an eighth of both, which are of different lengths
+    const int first = px.tm * px.tn * px.splits, id = blockIdx.x;
+    if (id < first) product_tile<TX, O>(px, xcd_contiguous(id, first), smem);
+    else product_tile<TW, O>(pw, xcd_contiguous(id - first, gridDim.x - first), smem);
+}
+
+// Up to three sums in one launch: of grad_x's, of grad_w's and of grad_bias's parts.
+template <typename O>
+__global__ void __launch_bounds__(256) linear_finish_kernel(Sum x, Sum w, Sum bias)
+{
+    unsigned block = blockIdx.x;
+    if (block < x.blocks) return sum_parts<O>(x, block);
+    block -= x.blocks;
+    if (block < w.blocks) return sum_parts<O>(w, block);
+    sum_parts<float>(bias, block - w.blocks);
+}
+
+template <typename O>
+__global__ void __launch_bounds__(256) linear_zero_kernel(O *out, int64_t ld, int64_t rows, int32_t cols)
+{
+    for (int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; t < rows * cols; t += static_cast<int64_t>(gridDim.x) * 256)
+        out[t / cols * ld + t % cols] = static_cast<O>(0.0f);
+}
+
+// ---------------------------------------------------------------- host side
+
+constexpr int32_t kMostFew = 64;            // rows that linear_few_kernel takes
+constexpr int kTilesAtOnce = 256;           // tiles of 64 x 64 below which k is shared out
+
+// A forward pass.
+struct Layout {
+    int few;                                // 16 rows to a lane's R; 0: tiles
+    int32_t waves, each, groups;            // few: wavefronts of a workgroup, k of each, workgroups side by side
+    int size;                               // 2, 1, 0: of the tiles
+    Tiles tiles;
+    int64_t kp, ldk;                        // width as it is laid out, and from row to row
+    uint16_t *xp, *wp;
+    int64_t bytes;
+};
+
+template <int P>
+Layout lay_out(const dol_matrix *x, const dol_matrix *w, void *workspace)
+{
+    using Z = Shapes<P, P>;
+    Layout L{};
+    Carver c(workspace);
+    const int32_t rows = x->rows, width = x->cols, out = w->rows;
+    L.tiles.part_ld = round_up(out, 4), L.tiles.splits = 1;
+    if (rows <= kMostFew) {
+        L.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+        L.groups = tiles(out, 16);
+        const int32_t shares = std::min(tiles(width, 256), std::max(4, 4096 / L.groups));
+        L.waves = std::min(shares, kFewWaves), L.tiles.splits = tiles(shares, kFewWaves);
+        L.each = static_cast<int32_t>(round_up(tiles(width, L.waves * L.tiles.splits), 64));
+    } else {
+        L.kp = round_up(width, 64), L.ldk = spread(L.kp);
+        const int64_t big = int64_t(tiles(rows, Z::Big::BM)) * tiles(out, Z::Big::BN), small = int64_t(tiles(rows, 128)) * tiles(out, 128);
+        L.size = big >= (P == 3 ? 160 : 192) ? 2 : small >= 128 ? 1 : 0;
+        by_size(L.size, Type<typename Z::Big>(), Type<typename Z::Small>(), Type<typename Z::Tiny>(), [&](auto z) {
+            using T = typename decltype(z)::Tile;
+            L.tiles.tm = tiles(rows, T::BM), L.tiles.tn = tiles(out, T::BN), L.tiles.steps = static_cast<int32_t>(L.kp / T::BK);
+        });
+        if (L.size == 0) {
+            const int32_t n = L.tiles.tm * L.tiles.tn;
+            L.tiles.splits = std::max(1, std::min(kTilesAtOnce / n, L.tiles.steps / 4));
+        }
+        if (!direct(x)) L.xp = c.take<uint16_t>(P * int64_t(rows) * L.ldk);
+        if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(out) * L.ldk);
+    }
+    if (L.tiles.splits > 1) L.tiles.part = c.take<float>(int64_t(L.tiles.splits) * rows * L.tiles.part_ld);
+    L.bytes = c.used;
+    return L;
+}
+
+// A backward pass.
+struct Back {
+    int64_t kp, ldk, ko, ldo, n_pad;        // width, out and rows as they are laid out
+    uint16_t *xp, *wp, *dz;
+    bool x_direct;
+    int size, splits_x, splits_w;
+    float *part_x, *part_w, *bias_part;
+    int64_t part_ld;
+    int32_t chunk, chunks;
+    int64_t bytes;
+};
+
+template <int P, int Q>
+Back lay_back(const dol_matrix *x, const dol_matrix *w, void *workspace)
+{
+    using Z = Shapes<P, Q>;
+    Back L{};
+    Carver c(workspace);
+    const int32_t rows = x->rows, width = x->cols, out = w->rows;
+    L.kp = round_up(width, 64), L.ldk = spread(L.kp), L.ko = round_up(out, 64), L.ldo = spread(L.ko), L.n_pad = round_up(rows, 64);
+    L.part_ld = round_up(width, 4);
+    // (k of grad_w: rows past the last have to be zeros in both operands)
+    L.x_direct = direct(x) && rows % 64 == 0;
+    if (!L.x_direct) L.xp = c.take<uint16_t>(P * L.n_pad * L.ldk);
+    if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(out) * L.ldk);
+    L.dz = c.take<uint16_t>(Q * L.n_pad * L.ldo);
+    L.chunk = static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>(64, round_up(tiles(L.n_pad * tiles(L.ko, 256), 1024), 8))));
+    L.chunks = tiles(L.n_pad, L.chunk);
+    L.bias_part = c.take<float>(L.chunks * L.ko);
+    auto place = [&](int bm, int bn) { return (tiles(rows, bn) * int64_t(out) + tiles(out, bn) * int64_t(rows)) * tiles(width, bm) / kUnits; };
+    const int64_t big = place(Z::BigX::BM, Z::BigX::BN);
+    L.size = big >= 1024 || (P == 3 && big >= 384 && std::min(out, rows) >= 2 * big) ? 2 : place(Z::SmallX::BM, Z::SmallX::BN) >= (P == 3 ? 64 : 256) ? 1 : 0;
+    int bm = 0, bn = 0, lds = 0;
+    by_size(L.size, Type<typename Z::BigX>(), Type<typename Z::SmallX>(), Type<typename Z::TinyX>(), [&](auto z) {
+        using T = typename decltype(z)::Tile;
+        bm = T::BM, bn = T::BN, lds = T::LDS;
+    });
+    // shares so that the workgroups come out even on the places there are
+    const int64_t places = kUnits * std::max(1, kLds / lds), tx = int64_t(tiles(width, bm)) * tiles(rows, bn), tw = int64_t(tiles(width, bm)) * tiles(out, bn);
+    const int64_t even = (tx * out + tw * rows) / places;
+    double best = 0.0;
+    for (int q = 6; q <= 20; ++q) {
+        const int64_t share = std::max<int64_t>(256, even * q / 10), sx = std::max<int64_t>(1, (out + share / 2) / share), sw = std::max<int64_t>(1, (rows + share / 2) / share);
+        const double sums = (sx > 1 ? double(sx) * rows : 0.0) + (sw > 1 ? double(sw) * out : 0.0);
+        const double all = done(tx * sx, double(out) / sx + 160, tw * sw, double(rows) / sw + 160, places) * bm * bn * (places / kUnits) + sums * width * 6 / (P == 3 ? 6 : Q);
+        if (best == 0.0 || all < best) best = all, L.splits_x = static_cast<int>(sx), L.splits_w = static_cast<int>(sw);
+    }
+    if (L.splits_x > 1) L.part_x = c.take<float>(int64_t(L.splits_x) * rows * L.part_ld);
+    if (L.splits_w > 1) L.part_w = c.take<float>(int64_t(L.splits_w) * out * L.part_ld);
+    L.bytes = c.used;
+    return L;
+}
+
+// dz rounded to bf16 is off by 2^-9 in every term of a gradient.  Sums over many rows average that out; with few, where the products cost little, a second
+// plane takes it away.
+constexpr int32_t kFewRows = 512;
+
+template <typename F>
+auto with_planes(const dol_matrix *x, F f)
+{
+    if (x->dtype == DOL_F32) return f(std::integral_constant<int, 3>(), std::integral_constant<int, 3>());
+    if (x->rows <= kFewRows) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
+    return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+}
+
+template <int P>
+dol_status launch_pack(const Pack &a, const Pack &b, hipStream_t st)
+{
+    if (a.blocks + b.blocks == 0) return DOL_OK;
+    linear_pack_kernel<typename Source<P>::T, P><<<a.blocks + b.blocks, 256, 0, st>>>(a, b);
+    DOL_HIP(hipGetLastError());
+    return DOL_OK;
+}
+
+template <typename S>
+dol_status launch_join(const Layout &L, const Result &o, hipStream_t st)
+{
+    if (L.tiles.splits == 1) return DOL_OK;
+    const int64_t n = int64_t(o.rows) * tiles(o.cols, 4);
+    linear_join_kernel<S><<<blocks(std::min(n, kMostBlocks * 256)), 256, 0, st>>>(L.tiles.part, L.tiles.part_ld, L.tiles.splits, o);
+    DOL_HIP(hipGetLastError());
+    return DOL_OK;
+}
+
+template <int P>
+dol_status forward(const Layout &L, const dol_matrix *x, const dol_matrix *w, const Result &o, hipStream_t st)
+{
+    using S = typename Source<P>::T;
+    if (L.few) {
+        auto go = [&](auto r) {
+            linear_few_kernel<S, r.value><<<L.groups * L.tiles.splits, L.waves * 64, 0, st>>>(static_cast<const S *>(x->data), x->ld, static_cast<const S *>(w->data), w->ld, x->cols,
+                                                                                           L.each, L.groups, L.tiles.part, L.tiles.part_ld, o);
+            DOL_HIP(hipGetLastError());
+            return DOL_OK;
+        };
+        if (dol_status s = L.few == 1   ? go(std::integral_constant<int, 1>())
+                           : L.few == 2 ? go(std::integral_constant<int, 2>())
+                                        : go(std::integral_constant<int, 4>()))
+            return s;
+        return launch_join<S>(L, o, st);
+    }
+    Planes xp, wp;
+    const Pack a = pack_of<P>(x, nullptr, nullptr, 0, L.xp, x->rows, L.kp, L.ldk, &xp), b = pack_of<P>(w, nullptr, nullptr, 0, L.wp, w->rows, L.kp, L.ldk, &wp);
+    if (dol_status s = launch_pack<P>(a, b, st)) return s;
+    using Z = Shapes<P, P>;
+    if (dol_status s = by_size(L.size, Type<typename Z::Big>(), Type<typename Z::Small>(), Type<typename Z::Tiny>(), [&](auto z) {
+            using T = typename decltype(z)::Tile;
+            DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(linear_tiles_kernel<T, S>), T::LDS));
+            linear_tiles_kernel<T, S><<<L.tiles.tm * L.tiles.tn * L.tiles.splits, T::NT, T::LDS, st>>>(xp, wp, L.tiles, o);
+            DOL_HIP(hipGetLastError());
+            return DOL_OK;
+        }))
+        return s;
+    return launch_join<S>(L, o, st);
+}
+
+template <typename TX, typename TW, typename O>
+dol_status launch_products(Product x, Product w, hipStream_t st)
+{
+    DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(linear_products_kernel<TX, TW, O>), TX::LDS));
+    for (Product *p : {&x, &w})
+        if (p->M > 0) p->tm = tiles(p->M, TX::BM), p->tn = tiles(p->N, TX::BN), p->steps = tiles(p->k, TX::BK);
+    const int n = x.tm * x.tn * x.splits + w.tm * w.tn * w.splits;
+    if (n == 0) return DOL_OK;
+    linear_products_kernel<TX, TW, O><<<n, TX::NT, TX::LDS, st>>>(x, w);
+    DOL_HIP(hipGetLastError());
+    return DOL_OK;
+}
+
+template <int P, int Q>
+dol_status reverse(const Back &L, const dol_matrix *x, const dol_matrix *w, int act, const dol_matrix *z, const uint8_t *rest, const dol_matrix *grad_y,
+                   const dol_matrix *grad_x, const dol_matrix *grad_w, float *grad_bias, hipStream_t st)
+{
+    using S = typename Source<P>::T;
+    using Z = Shapes<P, Q>;
+    Planes xp{}, wp{}, dz{L.dz, L.ldo, L.n_pad * L.ldo};
+    Pack lx{}, lw{};
+    if (grad_w) lx = pack_of<P>(x, nullptr, nullptr, 0, L.xp, L.n_pad, L.kp, L.ldk, &xp);
+    if (grad_x) lw = pack_of<P>(w, nullptr, nullptr, 0, L.wp, w->rows, L.kp, L.ldk, &wp);
+    if (dol_status s = launch_pack<P>(lx, lw, st)) return s;
+    // dz is grad_y itself where the tiles can read that (in one plane)
+    const bool as_it_is = Q == 1 && act == DOL_ACT_NONE && direct(grad_y) && x->rows % 64 == 0, write = !as_it_is && (grad_x || grad_w);
+    if (as_it_is) dz = Planes{static_cast<const uint16_t *>(grad_y->data), grad_y->ld, 0};
+    if (write || grad_bias) {
+        const int32_t wide = tiles(L.ko, 256);
+        const Slope p{grad_y->data, z ? z->data : nullptr, grad_y->ld, z ? z->ld : 0, rest, x->rows, w->rows, act, write ? L.dz : nullptr, L.n_pad, L.ko, L.ldo, L.n_pad * L.ldo,
+                      grad_bias ? L.bias_part : nullptr, L.chunk, wide};
+        linear_slope_kernel<S, Q><<<static_cast<unsigned>(wide * L.chunks), 256, 0, st>>>(p);
+        DOL_HIP(hipGetLastError());
+    }
+    Product a{}, b{};
+    if (grad_x) {
+        a.a = wp, a.b = dz;
+        a.M = x->cols, a.N = x->rows, a.wide = static_cast<int32_t>(L.kp), a.tall = x->rows, a.splits = L.splits_x, a.k = a.have = w->rows;
+        a.part = L.part_x, a.part_ld = L.part_ld, a.out = grad_x->data, a.out_ld = grad_x->ld;
+    }
+    if (grad_w) {
+        b.a = xp, b.b = dz;
+        b.M = x->cols, b.N = w->rows, b.wide = static_cast<int32_t>(L.kp), b.tall = static_cast<int32_t>(L.ko), b.splits = L.splits_w, b.k = x->rows, b.have = L.n_pad;
+        b.part = L.part_w, b.part_ld = L.part_ld, b.out = grad_w->data, b.out_ld = grad_w->ld;
+    }
+    if (dol_status s = L.size == 2   ? launch_products<typename Z::BigX, typename Z::BigW, S>(a, b, st)
+                       : L.size == 1 ? launch_products<typename Z::SmallX, typename Z::SmallW, S>(a, b, st)
+                                     : launch_products<typename Z::TinyX, typename Z::TinyW, S>(a, b, st))
+        return s;
+    const Sum sx = sum_of(a), sw = sum_of(b), sb = grad_bias ? make_sum(L.bias_part, 1, w->rows, L.chunks, L.ko, grad_bias, w->rows) : Sum{};
+    const unsigned n = sx.blocks + sw.blocks + sb.blocks;
+    if (n == 0) return DOL_OK;
+    linear_finish_kernel<S><<<n, 256, 0, st>>>(sx, sw, sb);
+    DOL_HIP(hipGetLastError());
+    return DOL_OK;
+}
+
+template <typename S>
+dol_status zero(const dol_matrix *m, hipStream_t st)
+{
+    if (!m || m->rows == 0) return DOL_OK;
+    linear_zero_kernel<S><<<std::min(blocks(int64_t(m->rows) * m->cols), 4096u), 256, 0, st>>>(static_cast<S *>(m->data), m->ld, m->rows, m->cols);
+    DOL_HIP(hipGetLastError());
+    return DOL_OK;
+}
+
+dol_status check_operands(const dol_matrix *x, const dol_matrix *w)
+{
+    if (dol_status s = check_matrix(x, "x")) return s;
+    if (dol_status s = check_matrix(w, "weight")) return s;
+    if (x->dtype != w->dtype) return fail(DOL_EINVAL, "x and weight are of different types");
+    if (x->cols != w->cols) return fail(DOL_ESHAPE, "x has %d columns, weight %d", x->cols, w->cols);
+    if (w->rows < 1 || w->cols < 1) return fail(DOL_ESHAPE, "weight is %d x %d: there has to be one out of one element", w->rows, w->cols);
+    if (x->rows > kMostRows || w->rows > kMostRows || w->cols > kMostWidth)
+        return fail(DOL_EUNSUPPORTED, "%d rows, %d outs of %d elements: more than %d, or %d elements", x->rows, w->rows, w->cols, kMostRows, kMostWidth);
+    return DOL_OK;
+}
+
+dol_status check_as(const dol_matrix *m, int32_t rows, int32_t cols, int32_t dtype, const char *name)
+{
+    if (!m) return DOL_OK;
+    if (dol_status s = check_matrix(m, name)) return s;
+    if (m->dtype != dtype) return fail(DOL_EINVAL, "%s is of another type than x", name);
+    if (m->rows != rows || m->cols != cols) return fail(DOL_ESHAPE, "%s is %d x %d, not %d x %d", name, m->rows, m->cols, rows, cols);
+    return DOL_OK;
+}
+
+bool fours(const dol_matrix *m)             // rows from columns that are multiples of four on are aligned to four elements
+{
+    return !m || (m->ld % 4 == 0 && !(reinterpret_cast<uintptr_t>(m->data) & (m->dtype == DOL_F32 ? 15 : 7)));
+}
+
+}  // namespace
+}  // namespace dol
+
+using namespace dol;
+
+extern "C" {
+
+dol_status dol_linear_workspace(const dol_matrix *x, const dol_matrix *weight, int32_t backward, int64_t *bytes)
+{
+    if (dol_status s = check_operands(x, weight)) return s;
+    if (!bytes) return fail(DOL_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    if (x->rows > 0)
+        *bytes = with_planes(x, [&](auto p, auto q) { return backward ? lay_back<p.value, q.value>(x, weight, nullptr).bytes : lay_out<p.value>(x, weight, nullptr).bytes; });
+    return DOL_OK;
+}
+
+const char *dol_linear_kernel(const dol_matrix *x, const dol_matrix *weight, int32_t backward)
+{
+    static thread_local char name[64];
+    if (check_operands(x, weight) != DOL_OK || x->rows == 0) return "";
+    with_planes(x, [&](auto p, auto q) {
+        using Z = Shapes<p.value, q.value>;
+        auto at = [&](const char *kernel, auto z) {
+            using T = typename decltype(z)::Tile;
+            return snprintf(name, sizeof name, "%s %dx%dx%d", kernel, T::BM, T::BN, T::BK);
+        };
+        if (backward) {
+            const Back L = lay_back<p.value, q.value>(x, weight, nullptr);
+            return by_size(L.size, Type<typename Z::BigX>(), Type<typename Z::SmallX>(), Type<typename Z::TinyX>(), [&](auto z) { return at("linear_products_kernel", z); });
+        }
+        const Layout L = lay_out<p.value>(x, weight, nullptr);
+        if (L.few) return snprintf(name, sizeof name, "linear_few_kernel %d", 16 * L.few);
+        using F = Shapes<p.value, p.value>;
+        return by_size(L.size, Type<typename F::Big>(), Type<typename F::Small>(), Type<typename F::Tiny>(), [&](auto z) { return at("linear_tiles_kernel", z); });
+    });
+    return name;
+}
+
+dol_status dol_linear(const dol_matrix *x, const dol_matrix *weight, const float *bias, int32_t act, const dol_matrix *residual, const dol_matrix *y, const dol_matrix *z,
+                      uint8_t *z_rest, void *workspace, int64_t workspace_bytes, void *hip_stream)
+{
+    if (dol_status s = check_operands(x, weight)) return s;
+    if (act < DOL_ACT_NONE || act > DOL_ACT_GELU) return fail(DOL_EINVAL, "unknown activation function %d", act);
+    if (!y) return fail(DOL_EINVAL, "y is NULL");
+    for (const auto &m : {std::make_pair(residual, "residual"), std::make_pair(y, "y"), std::make_pair(z, "z")})
+        if (dol_status s = check_as(m.first, x->rows, weight->rows, x->dtype, m.second)) return s;
+    if (z_rest && (!z || x->dtype != DOL_BF16)) return fail(DOL_EINVAL, "z_rest without z in bf16");
+    if (x->rows == 0) return DOL_OK;
+    Result o{};
+    o.bias = bias, o.act = act, o.rows = x->rows, o.cols = weight->rows, o.y = y->data, o.y_ld = y->ld, o.rest = z_rest;
+    if (residual) o.residual = residual->data, o.residual_ld = residual->ld;
+    if (z) o.z = z->data, o.z_ld = z->ld;
+    o.vec = fours(residual) && fours(y) && fours(z) && (!z_rest || (weight->rows % 4 == 0 && !(reinterpret_cast<uintptr_t>(z_rest) & 3)));
+    auto go = [&](auto p) {
+        const Layout L = lay_out<p.value>(x, weight, workspace);
+        if (dol_status s = check_workspace(workspace, workspace_bytes, L.bytes)) return s;
+        return forward<p.value>(L, x, weight, o, static_cast<hipStream_t>(hip_stream));
+    };
+    return x->dtype == DOL_F32 ? go(std::integral_constant<int, 3>()) : go(std::integral_constant<int, 1>());
+}
+
+dol_status dol_linear_backward(const dol_matrix *x, const dol_matrix *weight, int32_t act, const dol_matrix *z, const uint8_t *z_rest, const dol_matrix *grad_y,
+                               const dol_matrix *grad_x, const dol_matrix *grad_weight, float *grad_bias, void *workspace, int64_t workspace_bytes, void *hip_stream)
+{
+    if (dol_status s = check_operands(x, weight)) return s;
+    if (act < DOL_ACT_NONE || act > DOL_ACT_GELU) return fail(DOL_EINVAL, "unknown activation function %d", act);
+    if (!grad_y) return fail(DOL_EINVAL, "grad_y is NULL");
+    if (act == DOL_ACT_NONE) z = nullptr, z_rest = nullptr;
+    else if (!z) return fail(DOL_EINVAL, "z is NULL");
+    if (z_rest && x->dtype != DOL_BF16) return fail(DOL_EINVAL, "z_rest without z in bf16");
+    for (const auto &m : {std::make_pair(z, "z"), std::make_pair(grad_y, "grad_y")})
+        if (dol_status s = check_as(m.first, x->rows, weight->rows, x->dtype, m.second)) return s;
+    if (dol_status s = check_as(grad_x, x->rows, x->cols, x->dtype, "grad_x")) return s;
+    if (dol_status s = check_as(grad_weight, weight->rows, weight->cols, x->dtype, "grad_weight")) return s;
+    if (!grad_x && !grad_weight && !grad_bias) return fail(DOL_EINVAL, "no gradient is asked for");
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (x->rows == 0) {                     // sums over no rows
+        if (dol_status s = x->dtype == DOL_BF16 ? zero<__bf16>(grad_weight, st) : zero<float>(grad_weight, st)) return s;
+        const dol_matrix b{DOL_F32, 1, weight->rows, weight->rows, grad_bias};
+        return grad_bias ? zero<float>(&b, st) : DOL_OK;
+    }
+    return with_planes(x, [&](auto p, auto q) {
+        const Back L = lay_back<p.value, q.value>(x, weight, workspace);
+        if (dol_status s = check_workspace(workspace, workspace_bytes, L.bytes)) return s;
+        return reverse<p.value, q.value>(L, x, weight, act, z, z_rest, grad_y, grad_x, grad_weight, grad_bias, st);
+    });
+}
+
+}  // extern "C"

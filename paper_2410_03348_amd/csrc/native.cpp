@@ -387,6 +387,51 @@ PyObject *newton_schulz(PyObject *, PyObject *const *v, Py_ssize_t n)
     DOL_CALL(dol_newton_schulz(g.p(), g_stride, o.p(), o_stride, batch, steps, abc, eps, ws, have, s));
 }
 
+PyObject *linear_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 3);
+    Matrix x(a, 0), w(a, 1);
+    const int32_t back = a.num32(2);
+    if (a.bad) return nullptr;
+    int64_t need = 0;
+    const dol_status st = dol_linear_workspace(x.p(), w.p(), back, &need);
+    return bytes(st, need);
+}
+
+PyObject *linear_kernel(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 3);
+    Matrix x(a, 0), w(a, 1);
+    const int32_t back = a.num32(2);
+    return a.bad ? nullptr : PyUnicode_FromString(dol_linear_kernel(x.p(), w.p(), back));
+}
+
+PyObject *linear(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 11);
+    Matrix x(a, 0), w(a, 1), res(a, 4), y(a, 5), z(a, 6);
+    auto *b = a.ptr<float>(2);
+    const int32_t act = a.num32(3);
+    auto *rest = a.ptr<uint8_t>(7);
+    auto *ws = a.ptr<void>(8);
+    const int64_t have = a.num(9);
+    void *s = a.stream(10);
+    DOL_CALL(dol_linear(x.p(), w.p(), b, act, res.p(), y.p(), z.p(), rest, ws, have, s));
+}
+
+PyObject *linear_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    Args a(v, n, 12);
+    Matrix x(a, 0), w(a, 1), z(a, 3), gy(a, 5), gx(a, 6), gw(a, 7);
+    const int32_t act = a.num32(2);
+    auto *rest = a.ptr<uint8_t>(4);
+    auto *gb = a.ptr<float>(8);
+    auto *ws = a.ptr<void>(9);
+    const int64_t have = a.num(10);
+    void *s = a.stream(11);
+    DOL_CALL(dol_linear_backward(x.p(), w.p(), act, z.p(), rest, gy.p(), gx.p(), gw.p(), gb, ws, have, s));
+}
+
 PyObject *residual_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     Args a(v, n, 13);
@@ -620,6 +665,10 @@ PyMethodDef g_methods[] = {
     {"group_norm_workspace", DOL_FAST(group_norm_workspace)},
     {"group_norm", DOL_FAST(group_norm)},
     {"group_norm_backward", DOL_FAST(group_norm_backward)},
+    {"linear_workspace", DOL_FAST(linear_workspace)},
+    {"linear_kernel", DOL_FAST(linear_kernel)},
+    {"linear", DOL_FAST(linear)},
+    {"linear_backward", DOL_FAST(linear_backward)},
     {"residual_norm", DOL_FAST(residual_norm)},
     {"residual_norm_workspace", DOL_FAST(residual_norm_workspace)},
     {"residual_norm_backward", DOL_FAST(residual_norm_backward)},

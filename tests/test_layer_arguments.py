@@ -64,3 +64,31 @@ def test_residual_norm_workspace(rows, gates, cols, dtype):
     n = dol._native.residual_norm_workspace(matrix(rows, cols, dtype), matrix(gates, cols, dtype) if gates else None)
     assert 0 < n and n % 256 == 0 and n <= max(3 * 1024 * (cols + 64) * 4, 3 * rows * cols * 4 + rows * 8) + 4096
     assert dol._native.residual_norm_workspace(matrix(0, cols, dtype), None) == 0
+
+
+@pytest.mark.parametrize("x,w,why", [
+    (matrix(8, 16), matrix(20, 15), "ESHAPE"), (matrix(8, 16), matrix(20, 16, BF16), "types"), (matrix(8, 16), matrix(0, 16), "one out"),
+    (matrix(8, 0), matrix(4, 0), "one out"), (matrix(8, 16, 7), matrix(4, 16), "type"), (matrix((1 << 22) + 1, 16), matrix(4, 16), "more than"),
+    (matrix(8, (1 << 20) + 1), matrix(4, (1 << 20) + 1), "more than"), (matrix(8, 16, ld=15), matrix(4, 16), "ESHAPE"), (None, matrix(4, 16), "NULL")])
+@pytest.mark.parametrize("backward", [0, 1])
+def test_linear_refusals(x, w, why, backward):
+    with pytest.raises(dol.DolError, match=why):
+        dol._native.linear_workspace(x, w, backward)
+    assert dol._native.linear_kernel(x, w, backward) == ""
+
+
+def test_linear_refuses_unknown_activation_functions():
+    for act in (-1, 4):
+        with pytest.raises(dol.DolError, match="activation"):
+            dol._native.linear(matrix(8, 16), matrix(4, 16), None, act, None, matrix(8, 4), None, None, None, 0, 0)
+        with pytest.raises(dol.DolError, match="activation"):
+            dol._native.linear_backward(matrix(8, 16), matrix(4, 16), act, None, None, matrix(8, 4), matrix(8, 16), None, None, None, 0, 0)
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,width,out", [(0, 1, 1), (1, 1, 1), (1, 4096, 16384), (64, 1568, 128), (1000, 777, 1501), (8192, 4096, 4096), (1 << 22, 3, 2), (7, 1 << 20, 1), (1, 8, 1 << 22)])
+def test_linear_workspace(rows, width, out, dtype, backward):
+    n = dol._native.linear_workspace(matrix(rows, width, dtype), matrix(out, width, dtype), backward)
+    assert 0 <= n < 1 << 36 and n % 256 == 0
+    assert n == dol._native.linear_workspace(matrix(rows, width, dtype), matrix(out, width, dtype), backward)
