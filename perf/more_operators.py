@@ -230,7 +230,7 @@ def _own_linear(s):
     from paper_2410_03348_amd import binding as dol
     z = s["z"] if s["train"] else None
     if z is not None and z.dtype == torch.bfloat16 and "rest" not in s:
-        s["rest"] = torch.empty(z.shape, dtype=torch.uint8, device=DEV)         # kept beside z
+        s["rest"] = torch.empty(z.shape, dtype=torch.int16, device=DEV)         # kept beside z
     rest = s.get("rest")
     dol.linear(s["x"], s["weight"], s["y"], bias=s["bias"], act=s["act"], residual=s["stream"], z=z, z_rest=rest)
     out = {"y": s["y"]}
