@@ -497,22 +497,22 @@ dol_status dol_group_norm_backward(const dol_activations *x, int32_t groups, con
  *   residual  [rows, out] or NULL, of the type of x
  *   y         [rows, out], of the type of x; may be the residual, not x
  *   z         [rows, out] or NULL, of the type of x: what the gradients need where act is not DOL_ACT_NONE; not y
- *   z_rest    device [rows, out] or NULL, only with z in DOL_BF16: what rounding z has left, in 256ths of its steps.  With it the slopes that
- *             grad_bias sums up are off by some 2^-17, without it by 2^-9
+ *   z_rest    device [rows, out] or NULL, only with z in DOL_BF16: what rounding z has left, in steps of a float.  With it the slopes that
+ *             grad_bias sums up are a float's, without it off by some 2^-9 each
  * (DOL_F32 multiplies in parts of numbers above 64 rows: an infinity in x or weight makes the sums that it is in NaN.)
  * At most 2^22 rows and outs and 2^20 elements of a row (else DOL_EUNSUPPORTED); at least one out of one element. */
 dol_status dol_linear_workspace(const dol_matrix *x, const dol_matrix *weight, int32_t backward, int64_t *bytes);
 /* As dol_cross_entropy_kernel: "linear_few_kernel 16" (rows), "linear_tiles_kernel 128x128x64", backward "linear_products_kernel 64x64x64". */
 const char *dol_linear_kernel(const dol_matrix *x, const dol_matrix *weight, int32_t backward);
 dol_status dol_linear(const dol_matrix *x, const dol_matrix *weight, const float *bias, int32_t act, const dol_matrix *residual,
-                      const dol_matrix *y, const dol_matrix *z, uint8_t *z_rest, void *workspace, int64_t workspace_bytes,
+                      const dol_matrix *y, const dol_matrix *z, int16_t *z_rest, void *workspace, int64_t workspace_bytes,
                       void *hip_stream);
 /* Its gradients, dz = grad_y act'(z):
  *   grad_x = dz weight,   grad_weight = dz^T x,   grad_bias[o] = sum_i dz[i, o];   the residual's is grad_y itself.
  * z and z_rest as the forward call left them, ignored with DOL_ACT_NONE.  Each gradient is OVERWRITTEN, of the type of x (grad_bias: float), none of them
  * an operand's own memory; any may be NULL.  Sums are taken in a fixed order: two runs give the same bits.  rows == 0 writes zeros.
  * DOL_BF16 above 512 rows rounds dz to bf16 before the two products; up to 512 rows dz keeps 16 bits. */
-dol_status dol_linear_backward(const dol_matrix *x, const dol_matrix *weight, int32_t act, const dol_matrix *z, const uint8_t *z_rest,
+dol_status dol_linear_backward(const dol_matrix *x, const dol_matrix *weight, int32_t act, const dol_matrix *z, const int16_t *z_rest,
                                const dol_matrix *grad_y, const dol_matrix *grad_x, const dol_matrix *grad_weight, float *grad_bias,
                                void *workspace, int64_t workspace_bytes, void *hip_stream);
 

@@ -808,12 +808,12 @@ def linear(x: torch.Tensor, weight: torch.Tensor, y: torch.Tensor, bias: Optiona
     """y = act(z) + residual, z = x weight^T + bias.
 
     x [rows, width], weight [out, width] (float32 or bfloat16); y, residual, z [rows, out] of that type, y may be the residual; bias float32
-    [out]; act: "none", "relu", "silu" or "gelu".  The gradients need z where act is not "none"; z_rest uint8 [rows, out], beside a z in bfloat16,
+    [out]; act: "none", "relu", "silu" or "gelu".  The gradients need z where act is not "none"; z_rest int16 [rows, out], beside a z in bfloat16,
     keeps grad_bias as exact as sums in 32 bits."""
     mx, mw = _matrix(x), _matrix(weight)
     rows, out = mx[1], mw[1]
     ws, n, _keep = _workspace(workspace, _native.linear_workspace(mx, mw, 0) if workspace is None else 0, x.device, stream)
-    _native.linear(mx, mw, _values(bias, _F, out), _ACTS[act], _matrix(residual), _matrix(y), _matrix(z), _values(z_rest, torch.uint8, rows, out), ws, n,
+    _native.linear(mx, mw, _values(bias, _F, out), _ACTS[act], _matrix(residual), _matrix(y), _matrix(z), _values(z_rest, torch.int16, rows, out), ws, n,
                    _handle(stream))
 
 
@@ -825,7 +825,7 @@ def linear_backward(x: torch.Tensor, weight: torch.Tensor, grad_y: torch.Tensor,
     mx, mw = _matrix(x), _matrix(weight)
     rows, out = mx[1], mw[1]
     ws, n, _keep = _workspace(workspace, _native.linear_workspace(mx, mw, 1) if workspace is None else 0, x.device, stream)
-    _native.linear_backward(mx, mw, _ACTS[act], _matrix(z), _values(z_rest, torch.uint8, rows, out), _matrix(grad_y), _matrix(grad_x),
+    _native.linear_backward(mx, mw, _ACTS[act], _matrix(z), _values(z_rest, torch.int16, rows, out), _matrix(grad_y), _matrix(grad_x),
                             _matrix(grad_weight), _values(grad_bias, _F, out), ws, n, _handle(stream))
 
 

@@ -24,23 +24,20 @@ struct Result {
     int64_t residual_ld;
     void *y, *z;
     int64_t y_ld, z_ld;
-    uint8_t *rest;              // [rows][cols]
+    int16_t *rest;              // [rows][cols]
     int32_t rows, cols, act;
     bool vec;                   // four neighbouring columns from a multiple of four on are aligned to their size, in all of them
 };
 
-// What rounding z to bf16 leaves, in 256ths of a step, of -128 .. 127: of the float's 24 bits 16 are kept, so that sums of act'(z) in 32 bits are
-// off by 2^-17 and not 2^-9 a term.  The bits of a float count its steps across powers of two as well.
+// What rounding z to bf16 leaves, in a float's steps (whose bits count them across powers of two as well): -32768 .. 32768, the last of which, where z lies
+// half way and the lower neighbour is even, is taken for 32767.  With it z is a float again, and sums of act'(z) in 32 bits are not off by 2^-9 a term.
 __device__ __forceinline__ uint32_t rest_of(float z)
 {
     const int r = static_cast<int>(__float_as_uint(z) - (bits16<__bf16>(z) << 16));
-    return __builtin_isfinite(z) ? static_cast<uint32_t>(min((r + 128) >> 8, 127)) & 0xFF : 0;
+    return __builtin_isfinite(z) ? static_cast<uint32_t>(min(r, 32767)) & 0xFFFF : 0;
 }
 
-__device__ __forceinline__ float with_rest(float z, uint32_t rest)
-{
-    return __uint_as_float(__float_as_uint(z) + (static_cast<uint32_t>(static_cast<int8_t>(rest)) << 8));
-}
+__device__ __forceinline__ float with_rest(float z, uint32_t rest) { return __uint_as_float(__float_as_uint(z) + static_cast<uint32_t>(static_cast<int16_t>(rest))); }
 
 // Columns c .. c + 3 of row r of z to what the call leaves; n of them are there.
 template <typename S, typename A>
@@ -54,12 +51,12 @@ __device__ __forceinline__ void leave(const Result &o, A, int64_t r, int c, f32x
     if (o.z) {
         store4(static_cast<S *>(o.z) + r * o.z_ld + c, z, n, o.vec);
         if (sizeof(S) == 2 && o.rest) {
-            uint8_t *to = o.rest + r * o.cols + c;
-            if (o.vec && n >= 4) *reinterpret_cast<uint32_t *>(to) = rest_of(z[0]) | rest_of(z[1]) << 8 | rest_of(z[2]) << 16 | rest_of(z[3]) << 24;
+            int16_t *to = o.rest + r * o.cols + c;
+            if (o.vec && n >= 4) *reinterpret_cast<u32x2 *>(to) = u32x2{rest_of(z[0]) | rest_of(z[1]) << 16, rest_of(z[2]) | rest_of(z[3]) << 16};
             else
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (k < n) to[k] = static_cast<uint8_t>(rest_of(z[k]));
+                    if (k < n) to[k] = static_cast<int16_t>(rest_of(z[k]));
         }
     }
 #pragma unroll
@@ -87,32 +84,73 @@ struct Tiles {
     int64_t part_ld;
 };
 
-template <typename T, typename S>
+// A whole tile to what the call leaves, from its row m0 and this lane's column c on.  The residual of the next rows is asked for before these rows' results
+// are written: it may lie in their place, and no load passes a store.
+template <int ACT, typename S, typename T>
+__device__ __forceinline__ void leave_whole(const Result &o, int64_t m0, int c, const f32x4 (&acc)[T::MI][T::NI])
+{
+    struct alignas(4 * sizeof(S)) Four { S e[4]; };
+    f32x4 b = {0, 0, 0, 0};
+    if (o.bias)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) b[k] = o.bias[c + k];
+    const int64_t first = m0 + T::row_of(0);
+    const S *from = static_cast<const S *>(o.residual) + first * o.residual_ld + c;
+    Four next[4];
+    auto ask = [&](int i) {
+        if (o.residual)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) next[e] = *reinterpret_cast<const Four *>(from + (i * 16 + e) * o.residual_ld);
+    };
+    ask(0);
+#pragma unroll
+    for (int i = 0; i < T::MI; ++i) {
+        Four r[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = next[e];
+        if (i + 1 < T::MI) ask(i + 1);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t row = first + i * 16 + e;
+            f32x4 z = f32x4{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]} + b;
+            if (o.z) store4(static_cast<S *>(o.z) + row * o.z_ld + c, z, 4, true);
+            if (sizeof(S) == 2 && o.rest)
+                *reinterpret_cast<u32x2 *>(o.rest + row * o.cols + c) = u32x2{rest_of(z[0]) | rest_of(z[1]) << 16, rest_of(z[2]) | rest_of(z[3]) << 16};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[k] = act_of<ACT, false>(z[k], nullptr);
+            if (o.residual)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) z[k] += static_cast<float>(r[e].e[k]);
+            store4(static_cast<S *>(o.y) + row * o.y_ld + c, z, 4, true);
+        }
+    }
+}
+
+template <typename T, typename S, int ACT>
 __global__ void __launch_bounds__(T::NT, 2) linear_tiles_kernel(Planes x, Planes w, Tiles g, Result o)
 {
     extern __shared__ __align__(128) char smem[];
     const int id = xcd_contiguous(blockIdx.x, gridDim.x), each = g.tm * g.tn, split = id / each;
     int mt, nt;
     tile_of(id - split * each, g.tm, g.tn, 8, mt, nt);
-    const int s0 = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<int64_t>(g.steps) * split / g.splits));
-    const int s1 = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<int64_t>(g.steps) * (split + 1) / g.splits));
+    const int s0 = static_cast<int>(static_cast<int64_t>(g.steps) * split / g.splits), s1 = static_cast<int>(static_cast<int64_t>(g.steps) * (split + 1) / g.splits);
     f32x4 acc[T::MI][T::NI];
     T::clear(acc);
-    const int m0 = __builtin_amdgcn_readfirstlane(mt * T::BM), n0 = __builtin_amdgcn_readfirstlane(nt * T::BN);     // (quotients, in vector registers)
+    const int m0 = mt * T::BM, n0 = nt * T::BN;
     T::run(x, m0, o.rows, w, n0, o.cols, static_cast<int64_t>(s0) * T::BK, s1 - s0, smem, acc);
     const int c = n0 + T::col_of();
+    if (!g.part && o.vec && m0 + T::BM <= o.rows && n0 + T::BN <= o.cols) return leave_whole<ACT, S, T>(o, m0, c, acc);
     if (c >= o.cols) return;
-    auto rows = [&](auto f) {
 #pragma unroll
-        for (int i = 0; i < T::MI; ++i)
+    for (int i = 0; i < T::MI; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t r = m0 + T::row_of(i) + e;
-                if (r < o.rows) f(r, f32x4{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]});
-            }
-    };
-    if (g.part) rows([&](int64_t r, f32x4 z) { *reinterpret_cast<f32x4 *>(g.part + (split * static_cast<int64_t>(o.rows) + r) * g.part_ld + c) = z; });
-    else rows([&](int64_t r, f32x4 z) { with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, z); }); });
+        for (int e = 0; e < 4; ++e) {
+            const int64_t r = m0 + T::row_of(i) + e;
+            const f32x4 z{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+            if (r >= o.rows) continue;
+            if (g.part) *reinterpret_cast<f32x4 *>(g.part + (split * static_cast<int64_t>(o.rows) + r) * g.part_ld + c) = z;
+            else leave<S>(o, Act<ACT>(), r, c, z);
+        }
 }
 
 // The shares of k added up, in their order, and what follows.
@@ -132,24 +170,24 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float *part, int
 
 // ---------------------------------------------------------------- few rows
 
-// Sixteen outs and up to 16 R rows to a workgroup, whose wavefronts share out its k.  A lane loads 32 neighbouring bytes of the row of w (l & 15) and
+// Sixteen outs and 16 R rows to a workgroup, whose wavefronts share out its k.  A lane loads 32 neighbouring bytes of the row of w (l & 15) and
 // of rows of x, four lanes a line of 128; which of a product's k these are does not matter, as long as both operands agree.
 // float as it is, by v_mfma_f32_16x16x4.
 constexpr int kFewWaves = 16;
 
 template <typename S, int R>
-__global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(const S *x, int64_t ldx, const S *w, int64_t ldw, int32_t width, int32_t each, int32_t groups, float *part,
-                                                                    int64_t part_ld, Result o)
+__global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(const S *x, int64_t ldx, const S *w, int64_t ldw, int32_t width, int32_t each, int32_t groups, int32_t sets,
+                                                                    float *part, int64_t part_ld, Result o)
 {
     constexpr int V = kLooseElements<S>, STEP = 8 * V;       // k of a step: two vectors to each of four lanes
     __shared__ f32x4 red[kFewWaves][R][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int group = blockIdx.x % groups, split = blockIdx.x / groups;
+    const int group = blockIdx.x % groups, set = blockIdx.x / groups % sets, split = blockIdx.x / groups / sets, row0 = set * (16 * R);
     const int64_t k0 = static_cast<int64_t>(split * waves + wave) * each, k1 = min(k0 + each, static_cast<int64_t>(width));
     const S *from_w = w + min(group * 16 + (lane & 15), o.cols - 1) * ldw, *from_x[R];
     f32x4 acc[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) from_x[r] = x + min(r * 16 + (lane & 15), o.rows - 1) * ldx, acc[r] = f32x4{0, 0, 0, 0};
+    for (int r = 0; r < R; ++r) from_x[r] = x + min(row0 + r * 16 + (lane & 15), o.rows - 1) * ldx, acc[r] = f32x4{0, 0, 0, 0};
     auto products = [&](const Loose<S> (&a)[2], const Loose<S> (&b)[R][2]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -195,7 +233,7 @@ __global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(const S *x, 
     for (int m = wave; m < R; m += waves) {
         f32x4 z = red[0][m][lane];
         for (int q = 1; q < waves; ++q) z += red[q][m][lane];
-        const int64_t r = m * 16 + (lane & 15);
+        const int64_t r = row0 + m * 16 + (lane & 15);
         const int c = group * 16 + (lane >> 4) * 4;
         if (r >= o.rows || c >= o.cols) continue;
         if (part) *reinterpret_cast<f32x4 *>(part + (split * static_cast<int64_t>(o.rows) + r) * part_ld + c) = z;
@@ -217,23 +255,24 @@ __global__ void __launch_bounds__(256) linear_pack_kernel(Pack p0, Pack p1)
 struct Slope {
     const void *grad_y, *z;
     int64_t grad_ld, z_ld;
-    const uint8_t *rest;
+    const int16_t *rest;
     int32_t rows, cols, act;
     uint16_t *dz;               // null: only the sums
     int64_t out_rows, out_cols, ld, plane;      // as they are laid out
     float *part;                // [chunks][out_cols], null: only dz
     int32_t chunk;              // rows, of 8 at a time
     int32_t wide;               // workgroups side by side
+    unsigned blocks;            // none where dz is grad_y as it is
 };
 
 // 32 threads of eight columns by eight rows at a time.
 template <typename S, int Q>
-__global__ void __launch_bounds__(256) linear_slope_kernel(Slope p)
+__device__ __forceinline__ void slope_rows(const Slope &p, unsigned block)
 {
     __shared__ float red[8][256];
     const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
-    const int64_t chunk = blockIdx.x / p.wide;
-    const int64_t c = static_cast<int64_t>(blockIdx.x % p.wide) * 256 + lane * 8, n = p.cols - c;
+    const int64_t chunk = block / p.wide;
+    const int64_t c = static_cast<int64_t>(block % p.wide) * 256 + lane * 8, n = p.cols - c;
     constexpr int V = kLooseElements<S>, H = 8 / V;
     float sum[8];
 #pragma unroll
@@ -252,15 +291,9 @@ __global__ void __launch_bounds__(256) linear_slope_kernel(Slope p)
             }
             if (a.value != DOL_ACT_NONE) {
                 if (sizeof(S) == 2 && p.rest) {
-                    const uint8_t *from = p.rest + r * p.cols + c;
-                    struct __attribute__((packed, aligned(1))) Eight { uint32_t w[2]; } q{};
-                    if (left >= 8) q = *reinterpret_cast<const Eight *>(from);
-                    else
+                    const Loose<S> q = loose_load(reinterpret_cast<const S *>(p.rest + r * p.cols + c), left);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (e < left) q.w[e >> 2] |= static_cast<uint32_t>(from[e]) << (e & 3) * 8;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = with_rest(z[e], q.w[e >> 2] >> (e & 3) * 8);
+                    for (int e = 0; e < 8; ++e) z[e] = with_rest(z[e], q.w[e >> 1 & 3] >> (e & 1) * 16);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -288,11 +321,22 @@ __global__ void __launch_bounds__(256) linear_slope_kernel(Slope p)
 #pragma unroll
     for (int e = 0; e < 8; ++e) red[row][lane * 8 + e] = sum[e];
     __syncthreads();
-    const int64_t at = static_cast<int64_t>(blockIdx.x % p.wide) * 256 + threadIdx.x;
+    const int64_t at = static_cast<int64_t>(block % p.wide) * 256 + threadIdx.x;
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) s += red[k][threadIdx.x];
     if (at < p.out_cols) p.part[chunk * p.out_cols + at] = s;
+}
+
+// All that a backward pass does before its products, in one launch.
+template <typename S, int P, int Q>
+__global__ void __launch_bounds__(256) linear_slope_kernel(Slope p, Pack x, Pack w)
+{
+    unsigned block = blockIdx.x;
+    if (block < p.blocks) return slope_rows<S, Q>(p, block);
+    block -= p.blocks;
+    if (block < x.blocks) return pack_rows<S, P>(x, block);
+    pack_rows<S, P>(w, block - x.blocks);
 }
 
 template <typename TX, typename TW, typename O>
@@ -332,7 +376,7 @@ constexpr int kTilesAtOnce = 256;           // tiles of 64 x 64 below which k is
 // A forward pass.
 struct Layout {
     int few;                                // 16 rows to a lane's R; 0: tiles
-    int32_t waves, each, groups;            // few: wavefronts of a workgroup, k of each, workgroups side by side
+    int32_t waves, each, groups, sets;      // few: wavefronts of a workgroup, k of each, workgroups to outs and to rows
     int size;                               // 2, 1, 0: of the tiles
     Tiles tiles;
     int64_t kp, ldk;                        // width as it is laid out, and from row to row
@@ -349,9 +393,11 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, void *workspace)
     const int32_t rows = x->rows, width = x->cols, out = w->rows;
     L.tiles.part_ld = round_up(out, 4), L.tiles.splits = 1;
     if (rows <= kMostFew) {
-        L.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
         L.groups = tiles(out, 16);
-        const int32_t shares = std::min(tiles(width, 256), std::max(4, 4096 / L.groups));
+        // (rows of their own for a workgroup read the weights again, which costs nothing where the chip is not full)
+        L.few = rows <= 16 || L.groups * tiles(rows, 16) <= 2 * kUnits ? 1 : rows <= 32 ? 2 : 4;
+        L.sets = tiles(rows, 16 * L.few);
+        const int32_t shares = std::min(tiles(width, 128), std::max(4, 4096 / (L.groups * L.sets)));
         L.waves = std::min(shares, kFewWaves), L.tiles.splits = tiles(shares, kFewWaves);
         L.each = static_cast<int32_t>(round_up(tiles(width, L.waves * L.tiles.splits), 64));
     } else {
@@ -464,8 +510,8 @@ dol_status forward(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
     using S = typename Source<P>::T;
     if (L.few) {
         auto go = [&](auto r) {
-            linear_few_kernel<S, r.value><<<L.groups * L.tiles.splits, L.waves * 64, 0, st>>>(static_cast<const S *>(x->data), x->ld, static_cast<const S *>(w->data), w->ld, x->cols,
-                                                                                           L.each, L.groups, L.tiles.part, L.tiles.part_ld, o);
+            linear_few_kernel<S, r.value><<<L.groups * L.sets * L.tiles.splits, L.waves * 64, 0, st>>>(static_cast<const S *>(x->data), x->ld, static_cast<const S *>(w->data), w->ld, x->cols,
+                                                                                           L.each, L.groups, L.sets, L.tiles.part, L.tiles.part_ld, o);
             DOL_HIP(hipGetLastError());
             return DOL_OK;
         };
@@ -481,10 +527,17 @@ dol_status forward(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
     using Z = Shapes<P, P>;
     if (dol_status s = by_size(L.size, Type<typename Z::Big>(), Type<typename Z::Small>(), Type<typename Z::Tiny>(), [&](auto z) {
             using T = typename decltype(z)::Tile;
-            DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(linear_tiles_kernel<T, S>), T::LDS));
-            linear_tiles_kernel<T, S><<<L.tiles.tm * L.tiles.tn * L.tiles.splits, T::NT, T::LDS, st>>>(xp, wp, L.tiles, o);
-            DOL_HIP(hipGetLastError());
-            return DOL_OK;
+            auto go = [&](auto a) {
+                const auto kernel = linear_tiles_kernel<T, S, a.value>;
+                DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(kernel), T::LDS));
+                kernel<<<L.tiles.tm * L.tiles.tn * L.tiles.splits, T::NT, T::LDS, st>>>(xp, wp, L.tiles, o);
+                DOL_HIP(hipGetLastError());
+                return DOL_OK;
+            };
+            return L.tiles.splits > 1 || o.act == DOL_ACT_NONE ? go(Act<DOL_ACT_NONE>())
+                   : o.act == DOL_ACT_RELU                     ? go(Act<DOL_ACT_RELU>())
+                   : o.act == DOL_ACT_SILU                     ? go(Act<DOL_ACT_SILU>())
+                                                               : go(Act<DOL_ACT_GELU>());
         }))
         return s;
     return launch_join<S>(L, o, st);
@@ -504,7 +557,7 @@ dol_status launch_products(Product x, Product w, hipStream_t st)
 }
 
 template <int P, int Q>
-dol_status reverse(const Back &L, const dol_matrix *x, const dol_matrix *w, int act, const dol_matrix *z, const uint8_t *rest, const dol_matrix *grad_y,
+dol_status reverse(const Back &L, const dol_matrix *x, const dol_matrix *w, int act, const dol_matrix *z, const int16_t *rest, const dol_matrix *grad_y,
                    const dol_matrix *grad_x, const dol_matrix *grad_w, float *grad_bias, hipStream_t st)
 {
     using S = typename Source<P>::T;
@@ -513,15 +566,17 @@ dol_status reverse(const Back &L, const dol_matrix *x, const dol_matrix *w, int 
     Pack lx{}, lw{};
     if (grad_w) lx = pack_of<P>(x, nullptr, nullptr, 0, L.xp, L.n_pad, L.kp, L.ldk, &xp);
     if (grad_x) lw = pack_of<P>(w, nullptr, nullptr, 0, L.wp, w->rows, L.kp, L.ldk, &wp);
-    if (dol_status s = launch_pack<P>(lx, lw, st)) return s;
     // dz is grad_y itself where the tiles can read that (in one plane)
     const bool as_it_is = Q == 1 && act == DOL_ACT_NONE && direct(grad_y) && x->rows % 64 == 0, write = !as_it_is && (grad_x || grad_w);
     if (as_it_is) dz = Planes{static_cast<const uint16_t *>(grad_y->data), grad_y->ld, 0};
+    Slope p{};
     if (write || grad_bias) {
         const int32_t wide = tiles(L.ko, 256);
-        const Slope p{grad_y->data, z ? z->data : nullptr, grad_y->ld, z ? z->ld : 0, rest, x->rows, w->rows, act, write ? L.dz : nullptr, L.n_pad, L.ko, L.ldo, L.n_pad * L.ldo,
-                      grad_bias ? L.bias_part : nullptr, L.chunk, wide};
-        linear_slope_kernel<S, Q><<<static_cast<unsigned>(wide * L.chunks), 256, 0, st>>>(p);
+        p = Slope{grad_y->data, z ? z->data : nullptr, grad_y->ld, z ? z->ld : 0, rest, x->rows, w->rows, act, write ? L.dz : nullptr, L.n_pad, L.ko, L.ldo, L.n_pad * L.ldo,
+                  grad_bias ? L.bias_part : nullptr, L.chunk, wide, static_cast<unsigned>(wide * L.chunks)};
+    }
+    if (const unsigned n = p.blocks + lx.blocks + lw.blocks) {
+        linear_slope_kernel<S, P, Q><<<n, 256, 0, st>>>(p, lx, lw);
         DOL_HIP(hipGetLastError());
     }
     Product a{}, b{};
@@ -622,7 +677,7 @@ const char *dol_linear_kernel(const dol_matrix *x, const dol_matrix *weight, int
 }
 
 dol_status dol_linear(const dol_matrix *x, const dol_matrix *weight, const float *bias, int32_t act, const dol_matrix *residual, const dol_matrix *y, const dol_matrix *z,
-                      uint8_t *z_rest, void *workspace, int64_t workspace_bytes, void *hip_stream)
+                      int16_t *z_rest, void *workspace, int64_t workspace_bytes, void *hip_stream)
 {
     if (dol_status s = check_operands(x, weight)) return s;
     if (act < DOL_ACT_NONE || act > DOL_ACT_GELU) return fail(DOL_EINVAL, "unknown activation function %d", act);
@@ -635,7 +690,7 @@ dol_status dol_linear(const dol_matrix *x, const dol_matrix *weight, const float
     o.bias = bias, o.act = act, o.rows = x->rows, o.cols = weight->rows, o.y = y->data, o.y_ld = y->ld, o.rest = z_rest;
     if (residual) o.residual = residual->data, o.residual_ld = residual->ld;
     if (z) o.z = z->data, o.z_ld = z->ld;
-    o.vec = fours(residual) && fours(y) && fours(z) && (!z_rest || (weight->rows % 4 == 0 && !(reinterpret_cast<uintptr_t>(z_rest) & 3)));
+    o.vec = fours(residual) && fours(y) && fours(z) && (!z_rest || (weight->rows % 4 == 0 && !(reinterpret_cast<uintptr_t>(z_rest) & 7)));
     auto go = [&](auto p) {
         const Layout L = lay_out<p.value>(x, weight, workspace);
         if (dol_status s = check_workspace(workspace, workspace_bytes, L.bytes)) return s;
@@ -644,7 +699,7 @@ dol_status dol_linear(const dol_matrix *x, const dol_matrix *weight, const float
     return x->dtype == DOL_F32 ? go(std::integral_constant<int, 3>()) : go(std::integral_constant<int, 1>());
 }
 
-dol_status dol_linear_backward(const dol_matrix *x, const dol_matrix *weight, int32_t act, const dol_matrix *z, const uint8_t *z_rest, const dol_matrix *grad_y,
+dol_status dol_linear_backward(const dol_matrix *x, const dol_matrix *weight, int32_t act, const dol_matrix *z, const int16_t *z_rest, const dol_matrix *grad_y,
                                const dol_matrix *grad_x, const dol_matrix *grad_weight, float *grad_bias, void *workspace, int64_t workspace_bytes, void *hip_stream)
 {
     if (dol_status s = check_operands(x, weight)) return s;

@@ -412,7 +412,7 @@ PyObject *linear(PyObject *, PyObject *const *v, Py_ssize_t n)
     Matrix x(a, 0), w(a, 1), res(a, 4), y(a, 5), z(a, 6);
     auto *b = a.ptr<float>(2);
     const int32_t act = a.num32(3);
-    auto *rest = a.ptr<uint8_t>(7);
+    auto *rest = a.ptr<int16_t>(7);
     auto *ws = a.ptr<void>(8);
     const int64_t have = a.num(9);
     void *s = a.stream(10);
@@ -424,7 +424,7 @@ PyObject *linear_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     Args a(v, n, 12);
     Matrix x(a, 0), w(a, 1), z(a, 3), gy(a, 5), gx(a, 6), gw(a, 7);
     const int32_t act = a.num32(2);
-    auto *rest = a.ptr<uint8_t>(4);
+    auto *rest = a.ptr<int16_t>(4);
     auto *gb = a.ptr<float>(8);
     auto *ws = a.ptr<void>(9);
     const int64_t have = a.num(10);
