@@ -50,6 +50,25 @@ __device__ __forceinline__ Loose<S> loose_load(const S *p, int64_t n)
     return v;
 }
 
+// The same where `before` elements of the row lie before p: the row's last vector, shifted, is one load, where one of each element would wait for
+// the one before it.
+template <typename S>
+__device__ __forceinline__ Loose<S> loose_load_end(const S *p, int n, int before)
+{
+    constexpr int V = kLooseElements<S>;
+    if (n >= V) return *reinterpret_cast<const Loose<S> *>(p);
+    if (n <= 0) return Loose<S>{};
+    if (before + n < V) return loose_load(p, n);
+    const Loose<S> v = *reinterpret_cast<const Loose<S> *>(p - (V - n));
+    uint64_t lo = v.w[0] | static_cast<uint64_t>(v.w[1]) << 32, hi = v.w[2] | static_cast<uint64_t>(v.w[3]) << 32;
+    const int shift = (V - n) * static_cast<int>(8 * sizeof(S));        // of 128 bits, 16 to 112
+    if (shift >= 64) lo = hi >> (shift - 64), hi = 0;
+    else lo = lo >> shift | hi << (64 - shift), hi >>= shift;
+    Loose<S> r;
+    r.w[0] = static_cast<uint32_t>(lo), r.w[1] = static_cast<uint32_t>(lo >> 32), r.w[2] = static_cast<uint32_t>(hi), r.w[3] = static_cast<uint32_t>(hi >> 32);
+    return r;
+}
+
 template <typename S>
 __device__ __forceinline__ void loose_store(S *p, const Loose<S> &v, int64_t n)
 {

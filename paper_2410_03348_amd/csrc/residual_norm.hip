@@ -5,8 +5,8 @@
 //   k = scale gate gamma_u,   m2 = mean(k dh uhat),   grad_u = rms(u) (k dh - uhat m2)   (or scale gate dh)
 //   grad_gate = scale sum dh v,   grad_gamma_u = sum scale gate dh uhat,   grad_gamma_y = sum dy hhat   over rows
 //
-// Memory bounds it: four tensors forward, six backward.  A row lies in the registers of a group of 4 to 1 024 threads, each with one or two
-// vectors of 16 bytes, and is read once.  Backward one round of sums is enough: with dh put into it, mean(k dh uhat) is
+// Memory bounds it: four tensors forward, six backward.  A row lies in the registers of a group of 4 to 1 024 threads, eight columns to
+// each, and is read once.  Backward one round of sums is enough: with dh put into it, mean(k dh uhat) is
 //   sum k uhat (grad_h + rms(h) a) - rms(h) m1 sum k uhat hhat,
 // three sums that need nothing of each other.  Sums over rows stay in registers while a group goes down its rows; a workgroup leaves one part of
 // each, which a second launch adds up in the order of the rows.  Rows too long for that are read twice (wide_*).
@@ -20,8 +20,14 @@
 namespace dol {
 namespace {
 
-constexpr int kThreads = 256;           // of a workgroup, where a row does not take more
+constexpr int kEight = 8;               // columns of a thread
+constexpr int kThreads = 256;
 constexpr int kWideThreads = 1024;
+// Groups of G threads, a row to each, that make a workgroup, forward and backward.
+template <int G>
+constexpr int kGroups = G < kThreads ? kThreads / G : 1;
+template <int G>
+constexpr int kBackGroups = G <= 128 ? kThreads / G : G <= 256 ? 512 / G : 1;
 constexpr int kFewPoints = 32;          // rows to a set, below which a group takes all rows of its sets by itself
 constexpr int kUnits = 256;             // compute units of the chip
 constexpr int64_t kMostBlocks = 1 << 20;        // of a launch, which has less than 2^32 threads
@@ -45,8 +51,16 @@ struct Args {
     int64_t chunk, chunks;              // backward: rows that a workgroup takes, and how many such a set is
     float *part_y, *part_u, *part_gate; // [workgroups][cols], null where not asked for
     float2 *row;                        // wide: m1 and m2 of each row
-    __device__ int64_t gate_of(int64_t r) const { return each || !gate.p ? r : r / points; }
+    __device__ int64_t gate_of(int64_t r) const { return each || !gate.p ? r : static_cast<uint32_t>(r) / static_cast<uint32_t>(points); }
 };
+
+// A group's number in its workgroup: the same for a whole wavefront where that is one group's, so that rows' addresses are.
+template <int G>
+__device__ __forceinline__ int group_of()
+{
+    const int g = threadIdx.x / G;
+    return G >= 64 ? __builtin_amdgcn_readfirstlane(g) : g;
+}
 
 template <int G>
 __device__ __forceinline__ float group_sum(float x)
@@ -84,94 +98,177 @@ __device__ __forceinline__ void group_sums(float (&x)[N], float *red)
     }
 }
 
-// n of a vector's values from p, `other` where there is no tensor.
-template <typename S, int V>
-__device__ __forceinline__ void get(float (&x)[V], const S *p, bool given, int n, float other)
-{
-    if (!given) {
+// Eight neighbouring elements as memory has them.
+template <typename S>
+struct Eight {
+    static constexpr int V = kLooseElements<S>, H = kEight / V;
+    Loose<S> v[H];
+    __device__ void all(const S *p)
+    {
 #pragma unroll
-        for (int k = 0; k < V; ++k) x[k] = other;
-        return;
+        for (int h = 0; h < H; ++h) v[h] = *reinterpret_cast<const Loose<S> *>(p + h * V);
     }
-    if constexpr (sizeof(S) == 4 && V == 8) {
-        const Loose<float> a = loose_load(p, n), b = loose_load(p + 4, n - 4);
+    // the first n of them, column c and its neighbours, zeros behind
+    __device__ void some(const S *p, int n, int c)
+    {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = loose_get(a, k), x[4 + k] = loose_get(b, k);
-    } else {
-        const Loose<S> a = loose_load(p, n);
+        for (int h = 0; h < H; ++h) v[h] = loose_load_end(p + h * V, n - h * V, c + h * V);
+    }
+    // zeros, where there is no tensor (and what was loaded for it is another's)
+    __device__ void only(bool given)
+    {
+        const uint32_t mask = given ? ~0u : 0u;
 #pragma unroll
-        for (int k = 0; k < V; ++k) x[k] = loose_get(a, k);
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[h].w[k] &= mask;
+    }
+    __device__ float get(int e) const { return loose_get(v[e / V], e % V); }
+    // elements 2 k and 2 k + 1
+    __device__ void set(int k, float x0, float x1)
+    {
+        if constexpr (sizeof(S) == 4) v[k / 2].w[k % 2 * 2] = __float_as_uint(x0), v[k / 2].w[k % 2 * 2 + 1] = __float_as_uint(x1);
+        else v[0].w[k] = __builtin_bit_cast(uint16_t, static_cast<S>(x0)) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<S>(x1))) << 16;
+    }
+    __device__ void store(S *p, int n) const
+    {
+#pragma unroll
+        for (int h = 0; h < H; ++h) loose_store(p + h * V, v[h], n - h * V);
+    }
+    // Nothing that was computed of it before is kept for what comes after: unpacked it would take two to four times its registers.
+    __device__ void again()
+    {
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t w = v[h].w[k];
+                asm("" : "+v"(w));
+                v[h].w[k] = w;
+            }
+    }
+};
+
+template <typename S>
+__device__ __forceinline__ void put(S *p, const float (&x)[kEight], int n)
+{
+    constexpr int V = kLooseElements<S>;
+#pragma unroll
+    for (int h = 0; h < kEight / V; ++h) {
+        float part[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) part[e] = x[h * V + e];
+        Loose<S> v;
+        loose_set(v, part);
+        loose_store(p + h * V, v, n - h * V);
     }
 }
 
-template <typename S, int V>
-__device__ __forceinline__ void put(S *p, const float (&x)[V], int n)
+// Factors of eight columns, 1 where there are none.
+__device__ __forceinline__ void factors(float (&x)[kEight], const float *p, int n, int c)
 {
-    Loose<S> v;
-    loose_set(v, x);
-    loose_store(p, v, n);
+#pragma unroll
+    for (int e = 0; e < kEight; ++e) x[e] = 1.0f;
+    if (!p) return;
+    Eight<float> v;
+    v.some(p + c, n, c);
+#pragma unroll
+    for (int e = 0; e < kEight; ++e) x[e] = v.get(e);
 }
 
 __device__ __forceinline__ float rms(float squares, float per_cols, float eps) { return 1.0f / __builtin_amdgcn_sqrtf(__builtin_fmaf(squares, per_cols, eps)); }
 
+// Both factors of a thread's eight columns, in registers, or (G threads to a row) in LDS: beside three sums over rows and a row of five tensors there are
+// no registers left for them.
+struct InRegisters {
+    float u[kEight], y[kEight];
+    template <typename S>
+    __device__ InRegisters(const Args<S> &a, int c, int n, void *)
+    {
+        factors(u, a.gamma_u, n, c);
+        factors(y, a.gamma_y, n, c);
+    }
+    __device__ void get(int k, float (&gu)[2], float (&gy)[2]) const { gu[0] = u[2 * k], gu[1] = u[2 * k + 1], gy[0] = y[2 * k], gy[1] = y[2 * k + 1]; }
+};
+
+template <int G>
+struct InLds {
+    struct alignas(16) Pair { float u[2], y[2]; };
+    const Pair *at;             // [4][G]: a wavefront's reads are next to each other
+    template <typename S>
+    __device__ InLds(const Args<S> &a, int c, int n, void *lds) : at(static_cast<const Pair *>(lds) + c / kEight)
+    {
+        float u[kEight], y[kEight];
+        factors(u, a.gamma_u, n, c);
+        factors(y, a.gamma_y, n, c);
+        // (the groups of a workgroup write the same)
+#pragma unroll
+        for (int k = 0; k < kEight / 2; ++k) static_cast<Pair *>(lds)[k * G + c / kEight] = Pair{{u[2 * k], u[2 * k + 1]}, {y[2 * k], y[2 * k + 1]}};
+        lds_barrier();
+    }
+    __device__ void get(int k, float (&gu)[2], float (&gy)[2]) const
+    {
+        const Pair p = at[k * G];
+        gu[0] = p.u[0], gu[1] = p.u[1], gy[0] = p.y[0], gy[1] = p.y[1];
+    }
+};
+
+// What a row's eight columns are read for.
+template <typename S>
+struct Columns {
+    Eight<S> x, u, gate;
+    // (one branch for all of them, and none for a tensor that is not there: a load behind a branch of its own is waited for at its end)
+    __device__ void load(const Args<S> &a, int64_t r, int64_t g, int c, int n)
+    {
+        const S *pu = a.u.at(r, c), *px = a.x.p ? a.x.at(r, c) : pu, *pg = a.gate.p ? a.gate.at(g, c) : pu;
+        if (n >= kEight) x.all(px), u.all(pu), gate.all(pg);
+        else x.some(px, n, c), u.some(pu, n, c), gate.some(pg, n, c);
+        x.only(a.x.p);
+    }
+    __device__ float factor(const Args<S> &a, int e) const { return a.gate.p ? a.scale * gate.get(e) : a.scale; }
+    // h of column e
+    __device__ float stream(const Args<S> &a, int e, float gamma_u, float rstd_u) const { return __builtin_fmaf(factor(a, e), gamma_u * (u.get(e) * rstd_u), x.get(e)); }
+};
+
 // ---------------------------------------------------------------- forward
 
-template <typename S, int G, int NV>
-__global__ void __launch_bounds__(G > kThreads ? G : kThreads) residual_norm_kernel(Args<S> a)
+// Bytes bound it: bf16 8 192 x 4 096 FORWARD_FIGURE.
+template <typename S, int G>
+__global__ void __launch_bounds__(G * kGroups<G>) residual_norm_kernel(Args<S> a)
 {
-    constexpr int V = kLooseElements<S>, T = G > kThreads ? G : kThreads, R = T / G;
-    __shared__ float red[2][T / 64];
-    const int lane = threadIdx.x % G, group = threadIdx.x / G;
+    constexpr int R = kGroups<G>;
+    __shared__ float red[2][(G * R + 63) / 64];
+    const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kEight;
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * R; first < a.rows; first += static_cast<int64_t>(gridDim.x) * R) {
         const int64_t r = first + group;
         const bool in = r < a.rows;
-        const int64_t g = in ? a.gate_of(r) : 0;
-        float h[NV][V], k[NV][V], x[NV][V];
-        float s[1] = {0.0f};
-#pragma unroll
-        for (int q = 0; q < NV; ++q) {
-            const int c = (q * G + lane) * V, n = in ? a.cols - c : 0;
-            get(x[q], a.x.at(r, c), a.x.p, n, 0.0f);
-            get(h[q], a.u.at(r, c), true, n, 0.0f);
-            get(k[q], a.gate.at(g, c), a.gate.p, n, 1.0f);
-            float gamma[V];
-            get(gamma, a.gamma_u + c, a.norm_u && a.gamma_u, n, 1.0f);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                s[0] = __builtin_fmaf(h[q][e], h[q][e], s[0]);
-                h[q][e] *= gamma[e], k[q][e] *= a.scale;
-            }
-        }
-        float rstd = 1.0f;
+        const int n = in ? a.cols - c : 0;
+        Columns<S> p;
+        float gamma_u[kEight], gamma_y[kEight], h[kEight], s[1] = {0.0f}, rstd = 1.0f;
+        p.load(a, r, in ? a.gate_of(r) : 0, c, n);
+        factors(gamma_u, a.gamma_u, n, c);
+        factors(gamma_y, a.gamma_y, n, c);
         if (a.norm_u) {
+#pragma unroll
+            for (int e = 0; e < kEight; ++e) s[0] = __builtin_fmaf(p.u.get(e), p.u.get(e), s[0]);
             group_sums<G, 1>(s, red[0]);
             rstd = rms(s[0], a.per_cols, a.eps);
             if (a.rstd_u && in && lane == 0) a.rstd_u[r] = rstd;
+            s[0] = 0.0f;
         }
-        s[0] = 0.0f;
 #pragma unroll
-        for (int q = 0; q < NV; ++q)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                h[q][e] = __builtin_fmaf(k[q][e], h[q][e] * rstd, x[q][e]);
-                s[0] = __builtin_fmaf(h[q][e], h[q][e], s[0]);
-            }
+        for (int e = 0; e < kEight; ++e) {
+            h[e] = p.stream(a, e, gamma_u[e], rstd);
+            s[0] = __builtin_fmaf(h[e], h[e], s[0]);
+        }
+        if (a.out_h.p && n > 0) put(a.out_h.at(r, c), h, n);
         if (a.out_y.p) {
             group_sums<G, 1>(s, red[1]);
             rstd = rms(s[0], a.per_cols, a.eps);
             if (a.rstd_h && in && lane == 0) a.rstd_h[r] = rstd;
-        }
 #pragma unroll
-        for (int q = 0; q < NV; ++q) {
-            const int c = (q * G + lane) * V, n = in ? a.cols - c : 0;
-            if (n <= 0) continue;
-            if (a.out_h.p) put(a.out_h.at(r, c), h[q], n);
-            if (!a.out_y.p) continue;
-            float gamma[V];
-            get(gamma, a.gamma_y + c, a.gamma_y, n, 1.0f);
-#pragma unroll
-            for (int e = 0; e < V; ++e) h[q][e] = h[q][e] * rstd * gamma[e];
-            put(a.out_y.at(r, c), h[q], n);
+            for (int e = 0; e < kEight; ++e) h[e] = h[e] * rstd * gamma_y[e];
+            if (n > 0) put(a.out_y.at(r, c), h, n);
         }
         if constexpr (G > 64) lds_barrier();            // (red is written again)
     }
@@ -179,144 +276,159 @@ __global__ void __launch_bounds__(G > kThreads ? G : kThreads) residual_norm_ker
 
 // ---------------------------------------------------------------- backward
 
-// What a vector of a row leaves, and what it adds to the sums over rows.
-template <typename S, int V>
+// Eight columns of a row.  h is made again from x and u: as it was rounded to bf16 it would be off by 2^-9 in every term of grad_gamma_y.
+template <typename S>
 struct Piece {
-    float h[V], u[V], gy[V], gh[V];             // hhat, uhat (or u), grad_y, grad_h
-    // gate: times scale.  h is made again from x and u: as it was rounded it would be off by 2^-9 in every term of grad_gamma_y.
-    __device__ void read(const Args<S> &a, int64_t r, int c, int n, const float (&gamma_u)[V], const float (&gate)[V], float rstd_u, float rstd_h)
+    Columns<S> p;
+    Eight<S> gy, gh;
+    __device__ void load(const Args<S> &a, int64_t r, int64_t g, int c, int n)
     {
-        get(h, a.x.at(r, c), a.x.p && a.grad_y.p, n, 0.0f);
-        get(u, a.u.at(r, c), true, n, 0.0f);
-        get(gy, a.grad_y.at(r, c), a.grad_y.p, n, 0.0f);
-        get(gh, a.grad_h.at(r, c), a.grad_h.p, n, 0.0f);
-#pragma unroll
-        for (int e = 0; e < V; ++e) u[e] *= rstd_u, h[e] = __builtin_fmaf(gate[e], gamma_u[e] * u[e], h[e]) * rstd_h;
+        const S *pu = a.u.at(r, c), *px = a.x.p ? a.x.at(r, c) : pu, *pg = a.gate.p ? a.gate.at(g, c) : pu;
+        const S *py = a.grad_y.p ? a.grad_y.at(r, c) : pu, *ph = a.grad_h.p ? a.grad_h.at(r, c) : pu;
+        if (n >= kEight) p.x.all(px), p.u.all(pu), p.gate.all(pg), gy.all(py), gh.all(ph);
+        else p.x.some(px, n, c), p.u.some(pu, n, c), p.gate.some(pg, n, c), gy.some(py, n, c), gh.some(ph, n, c);
+        p.x.only(a.x.p), gy.only(a.grad_y.p), gh.only(a.grad_h.p);
     }
-    __device__ void sums(float (&s)[3], const float (&gamma_u)[V], const float (&gamma_y)[V], const float (&gate)[V], float rstd_h) const
+    __device__ void again() { p.x.again(), p.u.again(), p.gate.again(), gy.again(), gh.again(); }
+    template <typename F>
+    __device__ void sums(const Args<S> &a, float (&s)[3], const F &gamma, float rstd_u, float rstd_h) const
     {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float ay = gamma_y[e] * gy[e], ku = gate[e] * gamma_u[e] * u[e];
-            s[0] = __builtin_fmaf(ay, h[e], s[0]);
-            s[1] = __builtin_fmaf(ku, __builtin_fmaf(rstd_h, ay, gh[e]), s[1]);
-            s[2] = __builtin_fmaf(ku, h[e], s[2]);
+        for (int k = 0; k < kEight / 2; ++k) {
+            float gamma_u[2], gamma_y[2];
+            gamma.get(k, gamma_u, gamma_y);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int e = 2 * k + q;
+                const float hhat = p.stream(a, e, gamma_u[q], rstd_u) * rstd_h, uhat = p.u.get(e) * rstd_u;
+                const float ay = gamma_y[q] * gy.get(e), ku = p.factor(a, e) * gamma_u[q] * uhat;
+                s[0] = __builtin_fmaf(ay, hhat, s[0]);
+                s[1] = __builtin_fmaf(ku, __builtin_fmaf(rstd_h, ay, gh.get(e)), s[1]);
+                s[2] = __builtin_fmaf(ku, hhat, s[2]);
+            }
+            __builtin_amdgcn_sched_barrier(0);      // (two columns' numbers in registers, not eight)
         }
     }
-    __device__ void leave(const Args<S> &a, int64_t r, int c, int n, const float (&gamma_u)[V], const float (&gamma_y)[V], const float (&gate)[V], float rstd_u,
-                          float rstd_h, float m1, float m2, bool own_gate, float (&sum_y)[V], float (&sum_u)[V], float (&sum_gate)[V]) const
+    template <typename F>
+    __device__ void leave(const Args<S> &a, int64_t r, int c, int n, const F &gamma, float rstd_u, float rstd_h, float m1, float m2, float (&sum_y)[kEight],
+                          float (&sum_u)[kEight], float (&sum_gate)[kEight]) const
     {
-        float dh[V], du[V], dg[V];
+        Eight<S> ox, ou, og;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            dh[e] = __builtin_fmaf(rstd_h, __builtin_fmaf(-h[e], m1, gamma_y[e] * gy[e]), gh[e]);
-            const float dv = gate[e] * dh[e], t = dh[e] * u[e];
-            du[e] = a.norm_u ? rstd_u * __builtin_fmaf(-u[e], m2, gamma_u[e] * dv) : dv;
-            dg[e] = a.scale * gamma_u[e] * t;
-            sum_y[e] = __builtin_fmaf(gy[e], h[e], sum_y[e]);
-            sum_u[e] = __builtin_fmaf(gate[e], t, sum_u[e]);
-            sum_gate[e] += dg[e];
+        for (int k = 0; k < kEight / 2; ++k) {
+            float dh[2], du[2], dg[2], gamma_u[2], gamma_y[2];
+            gamma.get(k, gamma_u, gamma_y);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int e = 2 * k + q;
+                const float hhat = p.stream(a, e, gamma_u[q], rstd_u) * rstd_h, uhat = p.u.get(e) * rstd_u, f = p.factor(a, e), g = gy.get(e);
+                dh[q] = __builtin_fmaf(rstd_h, __builtin_fmaf(-hhat, m1, gamma_y[q] * g), gh.get(e));
+                const float dv = f * dh[q], t = dh[q] * uhat;
+                du[q] = a.norm_u ? rstd_u * __builtin_fmaf(-uhat, m2, gamma_u[q] * dv) : dv;
+                dg[q] = a.scale * gamma_u[q] * t;
+                sum_y[e] = __builtin_fmaf(g, hhat, sum_y[e]);
+                sum_u[e] = __builtin_fmaf(f, t, sum_u[e]);
+                sum_gate[e] += dg[q];
+            }
+            ox.set(k, dh[0], dh[1]), ou.set(k, du[0], du[1]), og.set(k, dg[0], dg[1]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (n <= 0) return;
-        if (a.grad_x.p) put(a.grad_x.at(r, c), dh, n);
-        if (a.grad_u.p) put(a.grad_u.at(r, c), du, n);
-        if (own_gate) put(a.grad_gate.at(r, c), dg, n);
+        if (a.grad_x.p) ox.store(a.grad_x.at(r, c), n);
+        if (a.grad_u.p) ou.store(a.grad_u.at(r, c), n);
+        if (a.each && a.grad_gate.p) og.store(a.grad_gate.at(r, c), n);
     }
 };
 
 // The sums of a workgroup's groups over their rows, in the order of the groups, to to[c].
-template <int G, int NV, int V, int R>
-__device__ __forceinline__ void leave_part(const float (&sum)[NV][V], float *to, int cols, float *buf)
+template <int G, int R>
+__device__ __forceinline__ void leave_part(const float (&sum)[kEight], float *to, int cols, float *buf)
 {
     const int lane = threadIdx.x % G, group = threadIdx.x / G;
     if constexpr (R == 1) {
 #pragma unroll
-        for (int q = 0; q < NV; ++q)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const int c = (q * G + lane) * V + e;
-                if (c < cols) to[c] = sum[q][e];
-            }
+        for (int e = 0; e < kEight; ++e)
+            if (lane * kEight + e < cols) to[lane * kEight + e] = sum[e];
     } else {
-        constexpr int W = G * NV * V;
         lds_barrier();
 #pragma unroll
-        for (int q = 0; q < NV; ++q)
-#pragma unroll
-            for (int e = 0; e < V; ++e) buf[group * W + (q * G + lane) * V + e] = sum[q][e];
+        for (int e = 0; e < kEight; ++e) buf[(group * G + lane) * kEight + e] = sum[e];
         lds_barrier();
         for (int c = threadIdx.x; c < cols; c += R * G) {
             float s = 0.0f;
-            for (int g = 0; g < R; ++g) s += buf[g * W + c];
+            for (int g = 0; g < R; ++g) s += buf[g * G * kEight + c];
             to[c] = s;
         }
     }
 }
 
 // WHOLE: a group takes all rows of its sets; else a workgroup takes a chunk of the rows of one set.
-template <typename S, int G, int NV, bool WHOLE>
-__global__ void __launch_bounds__(G > kThreads ? G : kThreads) residual_norm_backward_kernel(Args<S> a)
+// Bytes bound it: bf16 8 192 x 4 096 BACKWARD_FIGURE.  A row is asked for before the one ahead of it is worked on, where registers allow (bf16).
+template <typename S, int G, bool WHOLE>
+__global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_norm_backward_kernel(Args<S> a)
 {
-    constexpr int V = kLooseElements<S>, T = G > kThreads ? G : kThreads, R = T / G;
-    __shared__ float red[2][3 * (T / 64)];
-    __shared__ float buf[R > 1 ? T * NV * V : 1];
-    const int lane = threadIdx.x % G, group = threadIdx.x / G;
-    const bool own_gate = a.grad_gate.p && a.each;
-    const int64_t set = WHOLE ? 0 : blockIdx.x / a.chunks, r0 = WHOLE ? 0 : set * a.points + blockIdx.x % a.chunks * a.chunk;
-    const int64_t r1 = WHOLE ? 0 : min(r0 + a.chunk, (set + 1) * a.points);
-    const int64_t sets = WHOLE ? (a.sets + static_cast<int64_t>(gridDim.x) * R - 1) / (static_cast<int64_t>(gridDim.x) * R) : 1;
-    float sum_y[NV][V], sum_u[NV][V], sum_gate[NV][V], gamma_y[NV][V], gamma_u[NV][V];
+    constexpr int R = kBackGroups<G>;
+    constexpr bool AHEAD = false;
+    __shared__ float red[2][3 * ((G * R + 63) / 64)];
+    __shared__ float buf[R > 1 ? G * R * kEight : 1];
+    const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kEight;
+    // rows of this group: `count` of each of `turns` sets (WHOLE), or `count` of the chunk, R apart
+    const int64_t set = WHOLE ? 0 : blockIdx.x / static_cast<unsigned>(a.chunks);
+    const int64_t r0 = WHOLE ? 0 : set * a.points + (blockIdx.x - set * a.chunks) * a.chunk, r1 = WHOLE ? 0 : min(r0 + a.chunk, (set + 1) * a.points);
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * R, mine = static_cast<int64_t>(blockIdx.x) * R + group;
+    const int64_t turns = WHOLE ? (a.sets + stride - 1) / stride : 1, count = WHOLE ? a.points : (r1 - r0 + R - 1) / R;
+    constexpr bool LDS = G >= 64 && G < 1024;
+    __shared__ __align__(16) float gammas[LDS ? 2 * G * kEight : 1];
+    const std::conditional_t<LDS, InLds<G>, InRegisters> gamma(a, c, a.cols - c, gammas);
+    float sum_y[kEight], sum_u[kEight], sum_gate[kEight];
 #pragma unroll
-    for (int q = 0; q < NV; ++q) {
-        const int c = (q * G + lane) * V, n = a.cols - c;
-        get(gamma_y[q], a.gamma_y + c, a.gamma_y, n, 1.0f);
-        get(gamma_u[q], a.gamma_u + c, a.norm_u && a.gamma_u, n, 1.0f);
-#pragma unroll
-        for (int e = 0; e < V; ++e) sum_y[q][e] = sum_u[q][e] = sum_gate[q][e] = 0.0f;
-    }
+    for (int e = 0; e < kEight; ++e) sum_y[e] = sum_u[e] = sum_gate[e] = 0.0f;
+    struct Row {
+        Piece<S> p;
+        int64_t r;
+        int n;
+        float rstd_u, rstd_h;
+    };
+    auto fetch = [&](Row &q, int64_t t, int64_t k) {
+        const int64_t m = mine + t * stride;
+        const bool in = WHOLE ? t < turns && m < a.sets : k < count && r0 + k * R + group < r1;
+        q.r = WHOLE ? m * a.points + k : r0 + k * R + group;
+        q.n = in ? a.cols - c : 0;
+        q.p.load(a, q.r, WHOLE ? m : a.each ? q.r : set, c, q.n);
+        q.rstd_u = a.norm_u && in ? a.rstd_u[q.r] : 1.0f, q.rstd_h = a.grad_y.p && in ? a.rstd_h[q.r] : 0.0f;
+    };
     int turn = 0;
-    for (int64_t t = 0; t < sets; ++t) {
-        const int64_t mine = (t * gridDim.x + blockIdx.x) * R + group;          // WHOLE: this group's set
-        const int64_t count = WHOLE ? a.points : (r1 - r0 + R - 1) / R;
+    Row q;
+    if constexpr (AHEAD) fetch(q, 0, 0);
+    for (int64_t t = 0; t < turns; ++t) {
         for (int64_t k = 0; k < count; ++k) {
-            const int64_t r = WHOLE ? mine * a.points + k : r0 + k * R + group;
-            const bool in = WHOLE ? mine < a.sets : r < r1;
-            const int64_t g = WHOLE ? mine : a.each ? r : set;
-            const float rstd_u = a.norm_u && in ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p && in ? a.rstd_h[r] : 0.0f;
-            Piece<S, V> p[NV];
-            float gate[NV][V], s[3] = {0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int q = 0; q < NV; ++q) {
-                const int c = (q * G + lane) * V, n = in ? a.cols - c : 0;
-                get(gate[q], a.gate.at(g, c), a.gate.p, n, 1.0f);
-#pragma unroll
-                for (int e = 0; e < V; ++e) gate[q][e] *= a.scale;
-                p[q].read(a, r, c, n, gamma_u[q], gate[q], rstd_u, rstd_h);
-                p[q].sums(s, gamma_u[q], gamma_y[q], gate[q], rstd_h);
-            }
+            Row now, next;
+            if constexpr (AHEAD) {
+                now = q;
+                const bool last = k + 1 == count;
+                fetch(next, WHOLE && last ? t + 1 : t, WHOLE && last ? 0 : k + 1);
+            } else
+                fetch(now, t, k);
+            float s[3] = {0.0f, 0.0f, 0.0f};
+            now.p.sums(a, s, gamma, now.rstd_u, now.rstd_h);
             group_sums<G, 3>(s, red[turn]);
             turn ^= 1;
-            const float m1 = s[0] * a.per_cols, m2 = __builtin_fmaf(-rstd_h * m1, s[2], s[1]) * a.per_cols;
-#pragma unroll
-            for (int q = 0; q < NV; ++q) {
-                const int c = (q * G + lane) * V, n = in ? a.cols - c : 0;
-                p[q].leave(a, r, c, n, gamma_u[q], gamma_y[q], gate[q], rstd_u, rstd_h, m1, m2, own_gate, sum_y[q], sum_u[q], sum_gate[q]);
-            }
+            const float m1 = s[0] * a.per_cols, m2 = __builtin_fmaf(-now.rstd_h * m1, s[2], s[1]) * a.per_cols;
+            now.p.again();
+            now.p.leave(a, now.r, c, now.n, gamma, now.rstd_u, now.rstd_h, m1, m2, sum_y, sum_u, sum_gate);
+            if constexpr (AHEAD) q = next;
         }
         if (WHOLE && a.grad_gate.p) {
+            const int64_t m = mine + t * stride;
+            if (m < a.sets && c < a.cols) put(a.grad_gate.at(m, c), sum_gate, a.cols - c);
 #pragma unroll
-            for (int q = 0; q < NV; ++q) {
-                const int c = (q * G + lane) * V, n = mine < a.sets ? a.cols - c : 0;
-                if (n > 0) put(a.grad_gate.at(mine, c), sum_gate[q], n);
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum_gate[q][e] = 0.0f;
-            }
+            for (int e = 0; e < kEight; ++e) sum_gate[e] = 0.0f;
         }
     }
     const int64_t at = static_cast<int64_t>(blockIdx.x) * a.cols;
-    if (a.part_y) leave_part<G, NV, V, R>(sum_y, a.part_y + at, a.cols, buf);
-    if (a.part_u) leave_part<G, NV, V, R>(sum_u, a.part_u + at, a.cols, buf);
-    if (!WHOLE && a.part_gate) leave_part<G, NV, V, R>(sum_gate, a.part_gate + at, a.cols, buf);
+    if (a.part_y) leave_part<G, R>(sum_y, a.part_y + at, a.cols, buf);
+    if (a.part_u) leave_part<G, R>(sum_u, a.part_u + at, a.cols, buf);
+    if (!WHOLE && a.part_gate) leave_part<G, R>(sum_gate, a.part_gate + at, a.cols, buf);
 }
 
 // ---------------------------------------------------------------- wide rows
@@ -325,37 +437,35 @@ __global__ void __launch_bounds__(G > kThreads ? G : kThreads) residual_norm_bac
 template <typename S>
 __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S> a)
 {
-    constexpr int V = kLooseElements<S>;
     __shared__ float red[2][kWideThreads / 64];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const int64_t g = a.gate_of(r);
         float rstd_u = 1.0f, rstd_h = 0.0f, s[1] = {0.0f};
-        auto stream = [&](int c, int n, float (&h)[V]) {        // h of the vector at c
-            float x[V], k[V], gamma[V];
-            get(x, a.x.at(r, c), a.x.p, n, 0.0f);
-            get(h, a.u.at(r, c), true, n, 0.0f);
-            get(k, a.gate.at(g, c), a.gate.p, n, 1.0f);
-            get(gamma, a.gamma_u + c, a.norm_u && a.gamma_u, n, 1.0f);
+        auto stream = [&](int c, int n, float (&h)[kEight]) {
+            Columns<S> p;
+            float gamma_u[kEight];
+            p.load(a, r, g, c, n);
+            factors(gamma_u, a.gamma_u, n, c);
 #pragma unroll
-            for (int e = 0; e < V; ++e) h[e] = __builtin_fmaf(k[e] * a.scale, h[e] * gamma[e] * rstd_u, x[e]);
+            for (int e = 0; e < kEight; ++e) h[e] = p.stream(a, e, gamma_u[e], rstd_u);
         };
         if (a.norm_u) {
-            for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * V) {
-                float u[V];
-                get(u, a.u.at(r, c), true, a.cols - c, 0.0f);
+            for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
+                Eight<S> u;
+                u.some(a.u.at(r, c), a.cols - c, c);
 #pragma unroll
-                for (int e = 0; e < V; ++e) s[0] = __builtin_fmaf(u[e], u[e], s[0]);
+                for (int e = 0; e < kEight; ++e) s[0] = __builtin_fmaf(u.get(e), u.get(e), s[0]);
             }
             group_sums<kWideThreads, 1>(s, red[0]);
             rstd_u = rms(s[0], a.per_cols, a.eps);
             s[0] = 0.0f;
         }
         if (a.out_y.p) {
-            for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * V) {
-                float h[V];
+            for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
+                float h[kEight];
                 stream(c, a.cols - c, h);
 #pragma unroll
-                for (int e = 0; e < V; ++e) s[0] = __builtin_fmaf(h[e], h[e], s[0]);
+                for (int e = 0; e < kEight; ++e) s[0] = __builtin_fmaf(h[e], h[e], s[0]);
             }
             group_sums<kWideThreads, 1>(s, red[1]);
             rstd_h = rms(s[0], a.per_cols, a.eps);
@@ -364,15 +474,15 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S
             if (a.norm_u && a.rstd_u) a.rstd_u[r] = rstd_u;
             if (a.out_y.p && a.rstd_h) a.rstd_h[r] = rstd_h;
         }
-        for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * V) {
+        for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
             const int n = a.cols - c;
-            float h[V], gamma[V];
+            float h[kEight], gamma_y[kEight];
             stream(c, n, h);
             if (a.out_h.p) put(a.out_h.at(r, c), h, n);
             if (!a.out_y.p) continue;
-            get(gamma, a.gamma_y + c, a.gamma_y, n, 1.0f);
+            factors(gamma_y, a.gamma_y, n, c);
 #pragma unroll
-            for (int e = 0; e < V; ++e) h[e] = h[e] * rstd_h * gamma[e];
+            for (int e = 0; e < kEight; ++e) h[e] = h[e] * rstd_h * gamma_y[e];
             put(a.out_y.at(r, c), h, n);
         }
         lds_barrier();          // (red is written again)
@@ -383,23 +493,16 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S
 template <typename S>
 __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_rows_kernel(Args<S> a)
 {
-    constexpr int V = kLooseElements<S>;
     __shared__ float red[3 * (kWideThreads / 64)];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const int64_t g = a.gate_of(r);
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
         float s[3] = {0.0f, 0.0f, 0.0f};
-        for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * V) {
+        for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
             const int n = a.cols - c;
-            Piece<S, V> p;
-            float gate[V], gamma_u[V], gamma_y[V];
-            get(gate, a.gate.at(g, c), a.gate.p, n, 1.0f);
-            get(gamma_y, a.gamma_y + c, a.gamma_y, n, 1.0f);
-            get(gamma_u, a.gamma_u + c, a.norm_u && a.gamma_u, n, 1.0f);
-#pragma unroll
-            for (int e = 0; e < V; ++e) gate[e] *= a.scale;
-            p.read(a, r, c, n, gamma_u, gate, rstd_u, rstd_h);
-            p.sums(s, gamma_u, gamma_y, gate, rstd_h);
+            Piece<S> p;
+            p.load(a, r, g, c, n);
+            p.sums(a, s, InRegisters(a, c, n, nullptr), rstd_u, rstd_h);
         }
         group_sums<kWideThreads, 3>(s, red);
         const float m1 = s[0] * a.per_cols;
@@ -408,35 +511,27 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_rows_kernel(A
     }
 }
 
-// A workgroup takes kThreads vectors of the columns of a chunk of one set's rows.
+// A workgroup takes eight columns a thread of a chunk of one set's rows.
 template <typename S>
 __global__ void __launch_bounds__(kThreads) residual_norm_wide_map_kernel(Args<S> a, int stripes)
 {
-    constexpr int V = kLooseElements<S>;
     const int64_t block = blockIdx.x / stripes, set = block / a.chunks, r0 = set * a.points + block % a.chunks * a.chunk, r1 = min(r0 + a.chunk, (set + 1) * a.points);
-    const int c = (static_cast<int>(blockIdx.x % stripes) * kThreads + threadIdx.x) * V, n = a.cols - c;
+    const int c = (static_cast<int>(blockIdx.x % stripes) * kThreads + threadIdx.x) * kEight, n = a.cols - c;
     if (n <= 0) return;
-    const bool own_gate = a.grad_gate.p && a.each;
-    float sum_y[V], sum_u[V], sum_gate[V], gamma_y[V], gamma_u[V];
-    get(gamma_y, a.gamma_y + c, a.gamma_y, n, 1.0f);
-    get(gamma_u, a.gamma_u + c, a.norm_u && a.gamma_u, n, 1.0f);
+    const InRegisters gamma(a, c, n, nullptr);
+    float sum_y[kEight], sum_u[kEight], sum_gate[kEight];
 #pragma unroll
-    for (int e = 0; e < V; ++e) sum_y[e] = sum_u[e] = sum_gate[e] = 0.0f;
+    for (int e = 0; e < kEight; ++e) sum_y[e] = sum_u[e] = sum_gate[e] = 0.0f;
     for (int64_t r = r0; r < r1; ++r) {
-        const int64_t g = a.each ? r : set;
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
         const float2 m = a.row[r];
-        Piece<S, V> p;
-        float gate[V];
-        get(gate, a.gate.at(g, c), a.gate.p, n, 1.0f);
-#pragma unroll
-        for (int e = 0; e < V; ++e) gate[e] *= a.scale;
-        p.read(a, r, c, n, gamma_u, gate, rstd_u, rstd_h);
-        p.leave(a, r, c, n, gamma_u, gamma_y, gate, rstd_u, rstd_h, m.x, m.y, own_gate, sum_y, sum_u, sum_gate);
+        Piece<S> p;
+        p.load(a, r, a.each ? r : set, c, n);
+        p.leave(a, r, c, n, gamma, rstd_u, rstd_h, m.x, m.y, sum_y, sum_u, sum_gate);
     }
     const int64_t at = block * a.cols + c;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
+    for (int e = 0; e < kEight; ++e) {
         if (e >= n) break;
         if (a.part_y) a.part_y[at + e] = sum_y[e];
         if (a.part_u) a.part_u[at + e] = sum_u[e];
@@ -493,43 +588,39 @@ __global__ void __launch_bounds__(1024) residual_norm_sums_kernel(Sums<S> s, int
 
 constexpr int32_t kMostCols = 1 << 24;
 
-// Threads to a row and vectors of each; 0 threads: a row too long for registers.
-struct Form {
-    int threads, vectors;
-};
-
-Form form_of(int32_t cols, int32_t dtype)
+// Threads to a row, eight columns to each; 0: a row too long for registers.
+int threads_of(int32_t cols)
 {
-    const int v = dtype == DOL_F32 ? 4 : 8;
-    const int64_t n = (static_cast<int64_t>(cols) + v - 1) / v;
-    for (const Form f : {Form{4, 1}, Form{8, 1}, Form{16, 1}, Form{32, 1}, Form{64, 1}, Form{64, 2}, Form{128, 2}, Form{256, 2}, Form{512, 2}, Form{1024, 2}})
-        if (n <= f.threads * f.vectors) return f;
-    return Form{0, 0};
+    const int n = (cols + kEight - 1) / kEight;
+    for (int g : {4, 8, 16, 32, 64, 128, 192, 256, 384, 512, 768, 1024})
+        if (n <= g) return g;
+    return 0;
 }
 
-// f(threads to a row, vectors) with both as types.
+// f(threads to a row) with them as a type.
 template <typename F>
-dol_status with_form(Form form, F f)
+dol_status with_threads(int threads, F f)
 {
     using std::integral_constant;
-    const integral_constant<int, 1> one;
-    const integral_constant<int, 2> two;
-    switch (form.threads) {
-    case 4: return f(integral_constant<int, 4>(), one);
-    case 8: return f(integral_constant<int, 8>(), one);
-    case 16: return f(integral_constant<int, 16>(), one);
-    case 32: return f(integral_constant<int, 32>(), one);
-    case 64: return form.vectors == 1 ? f(integral_constant<int, 64>(), one) : f(integral_constant<int, 64>(), two);
-    case 128: return f(integral_constant<int, 128>(), two);
-    case 256: return f(integral_constant<int, 256>(), two);
-    case 512: return f(integral_constant<int, 512>(), two);
-    default: return f(integral_constant<int, 1024>(), two);
+    switch (threads) {
+    case 4: return f(integral_constant<int, 4>());
+    case 8: return f(integral_constant<int, 8>());
+    case 16: return f(integral_constant<int, 16>());
+    case 32: return f(integral_constant<int, 32>());
+    case 64: return f(integral_constant<int, 64>());
+    case 128: return f(integral_constant<int, 128>());
+    case 192: return f(integral_constant<int, 192>());
+    case 256: return f(integral_constant<int, 256>());
+    case 384: return f(integral_constant<int, 384>());
+    case 512: return f(integral_constant<int, 512>());
+    case 768: return f(integral_constant<int, 768>());
+    default: return f(integral_constant<int, 1024>());
     }
 }
 
 // How the rows of a backward pass are dealt out.
 struct Plan {
-    Form form;
+    int threads;                        // to a row
     bool each, whole;                   // a gate for every row; a group takes all rows of its sets
     int64_t sets, points, chunk, chunks, blocks;
     float *part_y, *part_u, *part_gate;
@@ -540,14 +631,15 @@ struct Plan {
 Plan plan_of(const dol_matrix *u, const dol_matrix *gate, void *workspace)
 {
     Plan p{};
-    p.form = form_of(u->cols, u->dtype);
+    p.threads = threads_of(u->cols);
     p.each = gate && gate->rows == u->rows;
     p.sets = gate && !p.each ? gate->rows : 1, p.points = u->rows / p.sets;
-    const int groups = p.form.threads && p.form.threads < kThreads ? kThreads / p.form.threads : 1;
-    p.whole = p.sets > 1 && p.form.threads && (p.points < kFewPoints || p.sets > kMostBlocks);
-    if (p.whole) p.blocks = std::min<int64_t>((p.sets + groups - 1) / groups, 2 * kUnits);
+    const int groups = p.threads == 0 ? 1 : p.threads <= 128 ? kThreads / p.threads : p.threads <= 256 ? 512 / p.threads : 1;
+    const int64_t most_blocks = p.threads && p.threads <= 128 ? 4 * kUnits : p.threads <= 512 ? 2 * kUnits : kUnits;
+    p.whole = p.sets > 1 && p.threads && (p.points < kFewPoints || p.sets > kMostBlocks);
+    if (p.whole) p.blocks = std::min<int64_t>((p.sets + groups - 1) / groups, most_blocks);
     else {
-        const int64_t wanted = std::max<int64_t>(1, 2 * kUnits / p.sets), most = std::max<int64_t>(1, p.points / (4 * groups));
+        const int64_t wanted = std::max<int64_t>(1, most_blocks / p.sets), most = std::max<int64_t>(1, p.points / groups);
         p.chunks = std::min(wanted, most);
         p.chunk = (p.points + p.chunks - 1) / p.chunks;
         p.chunks = (p.points + p.chunk - 1) / p.chunk;
@@ -556,7 +648,7 @@ Plan plan_of(const dol_matrix *u, const dol_matrix *gate, void *workspace)
     Carver c(workspace);
     p.part_y = c.take<float>(p.blocks * u->cols), p.part_u = c.take<float>(p.blocks * u->cols);
     if (gate && !p.each && !p.whole) p.part_gate = c.take<float>(p.blocks * u->cols);
-    if (!p.form.threads) p.row = c.take<float2>(u->rows);
+    if (!p.threads) p.row = c.take<float2>(u->rows);
     p.bytes = c.used;
     return p;
 }
@@ -599,16 +691,16 @@ Args<S> args_of(const dol_matrix *u, int32_t norm_u, const float *gamma_u, const
 }
 
 template <typename S>
-dol_status forward(const Args<S> &a, Form form, hipStream_t st)
+dol_status forward(const Args<S> &a, int threads, hipStream_t st)
 {
-    if (!form.threads) {
+    if (!threads) {
         residual_norm_wide_kernel<S><<<static_cast<unsigned>(std::min<int64_t>(a.rows, kMostBlocks)), kWideThreads, 0, st>>>(a);
         DOL_HIP(hipGetLastError());
         return DOL_OK;
     }
-    return with_form(form, [&](auto g, auto nv) {
-        constexpr int T = std::max<int>(g.value, kThreads), R = T / g.value;
-        residual_norm_kernel<S, g.value, nv.value><<<static_cast<unsigned>(std::min<int64_t>((static_cast<int64_t>(a.rows) + R - 1) / R, kMostBlocks)), T, 0, st>>>(a);
+    return with_threads(threads, [&](auto g) {
+        constexpr int G = g.value, R = kGroups<G>;
+        residual_norm_kernel<S, G><<<static_cast<unsigned>(std::min<int64_t>((static_cast<int64_t>(a.rows) + R - 1) / R, kMostBlocks)), G * R, 0, st>>>(a);
         DOL_HIP(hipGetLastError());
         return DOL_OK;
     });
@@ -619,11 +711,11 @@ dol_status reverse(const Plan &p, Args<S> a, float *grad_gamma_u, const dol_matr
 {
     a.chunk = p.chunk, a.chunks = p.chunks, a.row = p.row, a.grad_gate = out_of<S>(grad_gate);
     a.part_y = grad_gamma_y ? p.part_y : nullptr, a.part_u = grad_gamma_u ? p.part_u : nullptr, a.part_gate = grad_gate ? p.part_gate : nullptr;
-    if (p.form.threads) {
-        const dol_status s = with_form(p.form, [&](auto g, auto nv) {
-            constexpr int T = std::max<int>(g.value, kThreads);
-            if (p.whole) residual_norm_backward_kernel<S, g.value, nv.value, true><<<static_cast<unsigned>(p.blocks), T, 0, st>>>(a);
-            else residual_norm_backward_kernel<S, g.value, nv.value, false><<<static_cast<unsigned>(p.blocks), T, 0, st>>>(a);
+    if (p.threads) {
+        const dol_status s = with_threads(p.threads, [&](auto g) {
+            constexpr int G = g.value, T = G * kBackGroups<G>;
+            if (p.whole) residual_norm_backward_kernel<S, G, true><<<static_cast<unsigned>(p.blocks), T, 0, st>>>(a);
+            else residual_norm_backward_kernel<S, G, false><<<static_cast<unsigned>(p.blocks), T, 0, st>>>(a);
             DOL_HIP(hipGetLastError());
             return DOL_OK;
         });
@@ -631,7 +723,7 @@ dol_status reverse(const Plan &p, Args<S> a, float *grad_gamma_u, const dol_matr
     } else {
         residual_norm_wide_rows_kernel<S><<<static_cast<unsigned>(std::min<int64_t>(a.rows, kMostBlocks)), kWideThreads, 0, st>>>(a);
         DOL_HIP(hipGetLastError());
-        const int stripes = (a.cols + kThreads * kLooseElements<S> - 1) / (kThreads * kLooseElements<S>);
+        const int stripes = (a.cols + kThreads * kEight - 1) / (kThreads * kEight);
         residual_norm_wide_map_kernel<S><<<static_cast<unsigned>(p.blocks * stripes), kThreads, 0, st>>>(a, stripes);
         DOL_HIP(hipGetLastError());
     }
@@ -672,7 +764,7 @@ dol_status dol_residual_norm(const dol_matrix *x, const dol_matrix *u, int32_t n
         using S = decltype(type);
         Args<S> a = args_of<S>(u, norm_u, gamma_u, gate, scale, gamma_y);
         a.x = in_of<S>(x), a.out_h = out_of<S>(h), a.out_y = out_of<S>(y), a.eps = eps, a.rstd_u = rstd_u, a.rstd_h = rstd_h;
-        return forward<S>(a, form_of(u->cols, u->dtype), static_cast<hipStream_t>(hip_stream));
+        return forward<S>(a, threads_of(u->cols), static_cast<hipStream_t>(hip_stream));
     };
     return u->dtype == DOL_F32 ? go(0.0f) : go(static_cast<__bf16>(0.0f));
 }
