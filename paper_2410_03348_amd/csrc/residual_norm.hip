@@ -6,9 +6,9 @@
 //   grad_gate = scale sum dh v,   grad_gamma_u = sum scale gate dh uhat,   grad_gamma_y = sum dy hhat   over rows
 //
 // Memory bounds it: four tensors forward, six backward.  A row lies in the registers of a group of 4 to 1 024 threads, eight columns to
-// each, and is read once.  Backward one round of sums is enough: with dh put into it, mean(k dh uhat) is
-//   sum k uhat (grad_h + rms(h) a) - rms(h) m1 sum k uhat hhat,
-// three sums that need nothing of each other.  Sums over rows stay in registers while a group goes down its rows; a workgroup leaves one part of
+// each, and is read once; memory gives it as fast as some 40 instructions an element take, so that rstd's stay out of all that is done by element.  Backward one round of sums is enough: with dh put into it and t = gate gamma_u u, the sum of k dh uhat is scale rms(u) times
+//   sum t grad_h + rms(h) sum t a - rms(h)^2 m1 sum t h,
+// sums that need nothing of each other.  Sums over rows stay in registers while a group goes down its rows; a workgroup leaves one part of
 // each, which a second launch adds up in the order of the rows.  Rows too long for that are read twice (wide_*).
 #include "internal.h"
 #include "loose.h"
@@ -50,7 +50,7 @@ struct Args {
     float scale, eps, per_cols;
     int64_t chunk, chunks;              // backward: rows that a workgroup takes, and how many such a set is
     float *part_y, *part_u, *part_gate; // [workgroups][cols], null where not asked for
-    float2 *row;                        // wide: m1 and m2 of each row
+    float2 *row;                        // wide: what the sums over each row give
     __device__ int64_t gate_of(int64_t r) const { return each || !gate.p ? r : static_cast<uint32_t>(r) / static_cast<uint32_t>(points); }
 };
 
@@ -114,14 +114,14 @@ struct Eight {
 #pragma unroll
         for (int h = 0; h < H; ++h) v[h] = loose_load_end(p + h * V, n - h * V, c + h * V);
     }
-    // zeros, where there is no tensor (and what was loaded for it is another's)
-    __device__ void only(bool given)
+    // `other` in all of them, where there is no tensor (and what was loaded for it is another's)
+    __device__ void only(bool given, float other)
     {
-        const uint32_t mask = given ? ~0u : 0u;
+        const uint32_t bits = __float_as_uint(other), w = sizeof(S) == 4 ? bits : bits >> 16 | (bits & 0xFFFF0000u);
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[h].w[k] &= mask;
+            for (int k = 0; k < 4; ++k) v[h].w[k] = given ? v[h].w[k] : w;
     }
     __device__ float get(int e) const { return loose_get(v[e / V], e % V); }
     // elements 2 k and 2 k + 1
@@ -213,6 +213,9 @@ struct InLds {
     }
 };
 
+template <int G>
+constexpr int kGammaLds = G >= 64 ? 2 * G * kEight * 4 : 0;
+
 // What a row's eight columns are read for.
 template <typename S>
 struct Columns {
@@ -223,11 +226,11 @@ struct Columns {
         const S *pu = a.u.at(r, c), *px = a.x.p ? a.x.at(r, c) : pu, *pg = a.gate.p ? a.gate.at(g, c) : pu;
         if (n >= kEight) x.all(px), u.all(pu), gate.all(pg);
         else x.some(px, n, c), u.some(pu, n, c), gate.some(pg, n, c);
-        x.only(a.x.p);
+        x.only(a.x.p, 0.0f), gate.only(a.gate.p, 1.0f);
     }
-    __device__ float factor(const Args<S> &a, int e) const { return a.gate.p ? a.scale * gate.get(e) : a.scale; }
-    // h of column e
-    __device__ float stream(const Args<S> &a, int e, float gamma_u, float rstd_u) const { return __builtin_fmaf(factor(a, e), gamma_u * (u.get(e) * rstd_u), x.get(e)); }
+    // gate gamma_u u of column e, and h, of which it is scale rstd_u
+    __device__ float part(int e, float gamma_u) const { return gate.get(e) * (gamma_u * u.get(e)); }
+    __device__ float stream(int e, float gamma_u, float f) const { return __builtin_fmaf(f, part(e, gamma_u), x.get(e)); }
 };
 
 // ---------------------------------------------------------------- forward
@@ -256,9 +259,10 @@ __global__ void __launch_bounds__(G * kGroups<G>) residual_norm_kernel(Args<S> a
             if (a.rstd_u && in && lane == 0) a.rstd_u[r] = rstd;
             s[0] = 0.0f;
         }
+        const float f = a.scale * rstd;
 #pragma unroll
         for (int e = 0; e < kEight; ++e) {
-            h[e] = p.stream(a, e, gamma_u[e], rstd);
+            h[e] = p.stream(e, gamma_u[e], f);
             s[0] = __builtin_fmaf(h[e], h[e], s[0]);
         }
         if (a.out_h.p && n > 0) put(a.out_h.at(r, c), h, n);
@@ -287,11 +291,22 @@ struct Piece {
         const S *py = a.grad_y.p ? a.grad_y.at(r, c) : pu, *ph = a.grad_h.p ? a.grad_h.at(r, c) : pu;
         if (n >= kEight) p.x.all(px), p.u.all(pu), p.gate.all(pg), gy.all(py), gh.all(ph);
         else p.x.some(px, n, c), p.u.some(pu, n, c), p.gate.some(pg, n, c), gy.some(py, n, c), gh.some(ph, n, c);
-        p.x.only(a.x.p), gy.only(a.grad_y.p), gh.only(a.grad_h.p);
+        p.x.only(a.x.p, 0.0f), p.gate.only(a.gate.p, 1.0f), gy.only(a.grad_y.p, 0.0f), gh.only(a.grad_h.p, 0.0f);
     }
     __device__ void again() { p.x.again(), p.u.again(), p.gate.again(), gy.again(), gh.again(); }
+    // What a row is multiplied with; sums() adds up four products of eight columns, which with rstd's left out of them are two instructions each.
+    struct Factors {
+        float f, rstd_h;                        // scale rstd_u
+        float kh, ku;                           // after the sums: rstd_h^2 m1, rstd_u^2 m2
+        __device__ void join(const float (&s)[4], bool norm_u, float rstd_u, float per_cols)
+        {
+            const float m1 = rstd_h * s[0] * per_cols;
+            kh = rstd_h * (rstd_h * m1);
+            ku = norm_u ? rstd_u * rstd_u * (f * per_cols) * __builtin_fmaf(rstd_h, s[2], __builtin_fmaf(-kh, s[3], s[1])) : 0.0f;
+        }
+    };
     template <typename F>
-    __device__ void sums(const Args<S> &a, float (&s)[3], const F &gamma, float rstd_u, float rstd_h) const
+    __device__ void sums(float (&s)[4], const F &gamma, float f) const
     {
 #pragma unroll
         for (int k = 0; k < kEight / 2; ++k) {
@@ -300,18 +315,18 @@ struct Piece {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 const int e = 2 * k + q;
-                const float hhat = p.stream(a, e, gamma_u[q], rstd_u) * rstd_h, uhat = p.u.get(e) * rstd_u;
-                const float ay = gamma_y[q] * gy.get(e), ku = p.factor(a, e) * gamma_u[q] * uhat;
-                s[0] = __builtin_fmaf(ay, hhat, s[0]);
-                s[1] = __builtin_fmaf(ku, __builtin_fmaf(rstd_h, ay, gh.get(e)), s[1]);
-                s[2] = __builtin_fmaf(ku, hhat, s[2]);
+                const float t = p.part(e, gamma_u[q]), h = __builtin_fmaf(f, t, p.x.get(e)), ay = gamma_y[q] * gy.get(e);
+                s[0] = __builtin_fmaf(ay, h, s[0]);
+                s[1] = __builtin_fmaf(t, gh.get(e), s[1]);
+                s[2] = __builtin_fmaf(t, ay, s[2]);
+                s[3] = __builtin_fmaf(t, h, s[3]);
             }
             __builtin_amdgcn_sched_barrier(0);      // (two columns' numbers in registers, not eight)
         }
     }
+    // sum_y and sum_t add up dy hhat and scale dh uhat (times the gate, where each row has its own).
     template <typename F>
-    __device__ void leave(const Args<S> &a, int64_t r, int c, int n, const F &gamma, float rstd_u, float rstd_h, float m1, float m2, float (&sum_y)[kEight],
-                          float (&sum_u)[kEight], float (&sum_gate)[kEight]) const
+    __device__ void leave(const Args<S> &a, int64_t r, int c, int n, const F &gamma, const Factors &m, float (&sum_y)[kEight], float (&sum_t)[kEight]) const
     {
         Eight<S> ox, ou, og;
 #pragma unroll
@@ -321,14 +336,13 @@ struct Piece {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 const int e = 2 * k + q;
-                const float hhat = p.stream(a, e, gamma_u[q], rstd_u) * rstd_h, uhat = p.u.get(e) * rstd_u, f = p.factor(a, e), g = gy.get(e);
-                dh[q] = __builtin_fmaf(rstd_h, __builtin_fmaf(-hhat, m1, gamma_y[q] * g), gh.get(e));
-                const float dv = f * dh[q], t = dh[q] * uhat;
-                du[q] = a.norm_u ? rstd_u * __builtin_fmaf(-uhat, m2, gamma_u[q] * dv) : dv;
-                dg[q] = a.scale * gamma_u[q] * t;
-                sum_y[e] = __builtin_fmaf(g, hhat, sum_y[e]);
-                sum_u[e] = __builtin_fmaf(f, t, sum_u[e]);
-                sum_gate[e] += dg[q];
+                const float u = p.u.get(e), gate = p.gate.get(e), h = p.stream(e, gamma_u[q], m.f), g = gy.get(e);
+                dh[q] = __builtin_fmaf(m.rstd_h, gamma_y[q] * g, __builtin_fmaf(-m.kh, h, gh.get(e)));
+                const float dv = gate * dh[q], v = m.f * u;
+                du[q] = __builtin_fmaf(m.f, gamma_u[q] * dv, -(m.ku * u));
+                dg[q] = gamma_u[q] * (dh[q] * v);
+                sum_y[e] = __builtin_fmaf(g, h * m.rstd_h, sum_y[e]);
+                sum_t[e] = __builtin_fmaf(a.each ? dv : dh[q], v, sum_t[e]);
             }
             ox.set(k, dh[0], dh[1]), ou.set(k, du[0], du[1]), og.set(k, dg[0], dg[1]);
             __builtin_amdgcn_sched_barrier(0);
@@ -339,6 +353,25 @@ struct Piece {
         if (a.each && a.grad_gate.p) og.store(a.grad_gate.at(r, c), n);
     }
 };
+
+// Of a set's sums of scale dh uhat: grad_gate's, times gamma_u, and grad_gamma_u's, times the gate (which a row of its own has multiplied already).
+template <typename S, typename F>
+__device__ __forceinline__ void spread_sums(const Args<S> &a, int64_t set, int c, const F &gamma, const float (&sum_t)[kEight], float (&to_gate)[kEight], float (&to_u)[kEight])
+{
+    Eight<S> gate{};
+    const bool given = a.gate.p && !a.each;
+    if (given) gate.some(a.gate.at(set, c), a.cols - c, c);
+#pragma unroll
+    for (int k = 0; k < kEight / 2; ++k) {
+        float gamma_u[2], gamma_y[2];
+        gamma.get(k, gamma_u, gamma_y);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int e = 2 * k + q;
+            to_gate[e] = gamma_u[q] * sum_t[e], to_u[e] = given ? gate.get(e) * sum_t[e] : sum_t[e];
+        }
+    }
+}
 
 // The sums of a workgroup's groups over their rows, in the order of the groups, to to[c].
 template <int G, int R>
@@ -369,7 +402,7 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
 {
     constexpr int R = kBackGroups<G>;
     constexpr bool AHEAD = false;
-    __shared__ float red[2][3 * ((G * R + 63) / 64)];
+    __shared__ float red[2][4 * ((G * R + 63) / 64)];
     __shared__ float buf[R > 1 ? G * R * kEight : 1];
     const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kEight;
     // rows of this group: `count` of each of `turns` sets (WHOLE), or `count` of the chunk, R apart
@@ -377,12 +410,11 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
     const int64_t r0 = WHOLE ? 0 : set * a.points + (blockIdx.x - set * a.chunks) * a.chunk, r1 = WHOLE ? 0 : min(r0 + a.chunk, (set + 1) * a.points);
     const int64_t stride = static_cast<int64_t>(gridDim.x) * R, mine = static_cast<int64_t>(blockIdx.x) * R + group;
     const int64_t turns = WHOLE ? (a.sets + stride - 1) / stride : 1, count = WHOLE ? a.points : (r1 - r0 + R - 1) / R;
-    constexpr bool LDS = G >= 64 && G < 1024;
-    __shared__ __align__(16) float gammas[LDS ? 2 * G * kEight : 1];
-    const std::conditional_t<LDS, InLds<G>, InRegisters> gamma(a, c, a.cols - c, gammas);
-    float sum_y[kEight], sum_u[kEight], sum_gate[kEight];
+    extern __shared__ __align__(16) char gammas[];
+    const std::conditional_t<(kGammaLds<G> > 0), InLds<G>, InRegisters> gamma(a, c, a.cols - c, gammas);
+    float sum_y[kEight], sum_t[kEight], sum_u[kEight], gates[kEight];
 #pragma unroll
-    for (int e = 0; e < kEight; ++e) sum_y[e] = sum_u[e] = sum_gate[e] = 0.0f;
+    for (int e = 0; e < kEight; ++e) sum_y[e] = sum_t[e] = sum_u[e] = 0.0f;
     struct Row {
         Piece<S> p;
         int64_t r;
@@ -409,26 +441,32 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
                 fetch(next, WHOLE && last ? t + 1 : t, WHOLE && last ? 0 : k + 1);
             } else
                 fetch(now, t, k);
-            float s[3] = {0.0f, 0.0f, 0.0f};
-            now.p.sums(a, s, gamma, now.rstd_u, now.rstd_h);
-            group_sums<G, 3>(s, red[turn]);
+            typename Piece<S>::Factors m{a.scale * now.rstd_u, now.rstd_h, 0.0f, 0.0f};
+            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            now.p.sums(s, gamma, m.f);
+            group_sums<G, 4>(s, red[turn]);
             turn ^= 1;
-            const float m1 = s[0] * a.per_cols, m2 = __builtin_fmaf(-now.rstd_h * m1, s[2], s[1]) * a.per_cols;
+            m.join(s, a.norm_u, now.rstd_u, a.per_cols);
             now.p.again();
-            now.p.leave(a, now.r, c, now.n, gamma, now.rstd_u, now.rstd_h, m1, m2, sum_y, sum_u, sum_gate);
+            now.p.leave(a, now.r, c, now.n, gamma, m, sum_y, sum_t);
             if constexpr (AHEAD) q = next;
         }
-        if (WHOLE && a.grad_gate.p) {
+        if constexpr (WHOLE) {
             const int64_t m = mine + t * stride;
-            if (m < a.sets && c < a.cols) put(a.grad_gate.at(m, c), sum_gate, a.cols - c);
+            if (m < a.sets) {
+                float to_u[kEight];
+                spread_sums(a, m, c, gamma, sum_t, gates, to_u);
+                if (a.grad_gate.p && c < a.cols) put(a.grad_gate.at(m, c), gates, a.cols - c);
 #pragma unroll
-            for (int e = 0; e < kEight; ++e) sum_gate[e] = 0.0f;
+                for (int e = 0; e < kEight; ++e) sum_u[e] += to_u[e], sum_t[e] = 0.0f;
+            }
         }
     }
+    if constexpr (!WHOLE) spread_sums(a, set, c, gamma, sum_t, gates, sum_u);
     const int64_t at = static_cast<int64_t>(blockIdx.x) * a.cols;
     if (a.part_y) leave_part<G, R>(sum_y, a.part_y + at, a.cols, buf);
     if (a.part_u) leave_part<G, R>(sum_u, a.part_u + at, a.cols, buf);
-    if (!WHOLE && a.part_gate) leave_part<G, R>(sum_gate, a.part_gate + at, a.cols, buf);
+    if (!WHOLE && a.part_gate) leave_part<G, R>(gates, a.part_gate + at, a.cols, buf);
 }
 
 // ---------------------------------------------------------------- wide rows
@@ -447,7 +485,7 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S
             p.load(a, r, g, c, n);
             factors(gamma_u, a.gamma_u, n, c);
 #pragma unroll
-            for (int e = 0; e < kEight; ++e) h[e] = p.stream(a, e, gamma_u[e], rstd_u);
+            for (int e = 0; e < kEight; ++e) h[e] = p.stream(e, gamma_u[e], a.scale * rstd_u);
         };
         if (a.norm_u) {
             for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
@@ -489,24 +527,25 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S
     }
 }
 
-// m1 and m2 of each row.
+// What a row's sums give (Factors) for each row.
 template <typename S>
 __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_rows_kernel(Args<S> a)
 {
-    __shared__ float red[3 * (kWideThreads / 64)];
+    __shared__ float red[4 * (kWideThreads / 64)];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const int64_t g = a.gate_of(r);
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
-        float s[3] = {0.0f, 0.0f, 0.0f};
+        typename Piece<S>::Factors m{a.scale * rstd_u, rstd_h, 0.0f, 0.0f};
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
             const int n = a.cols - c;
             Piece<S> p;
             p.load(a, r, g, c, n);
-            p.sums(a, s, InRegisters(a, c, n, nullptr), rstd_u, rstd_h);
+            p.sums(s, InRegisters(a, c, n, nullptr), m.f);
         }
-        group_sums<kWideThreads, 3>(s, red);
-        const float m1 = s[0] * a.per_cols;
-        if (threadIdx.x == 0) a.row[r] = make_float2(m1, __builtin_fmaf(-rstd_h * m1, s[2], s[1]) * a.per_cols);
+        group_sums<kWideThreads, 4>(s, red);
+        m.join(s, a.norm_u, rstd_u, a.per_cols);
+        if (threadIdx.x == 0) a.row[r] = make_float2(m.kh, m.ku);
         lds_barrier();
     }
 }
@@ -519,23 +558,24 @@ __global__ void __launch_bounds__(kThreads) residual_norm_wide_map_kernel(Args<S
     const int c = (static_cast<int>(blockIdx.x % stripes) * kThreads + threadIdx.x) * kEight, n = a.cols - c;
     if (n <= 0) return;
     const InRegisters gamma(a, c, n, nullptr);
-    float sum_y[kEight], sum_u[kEight], sum_gate[kEight];
+    float sum_y[kEight], sum_t[kEight], sum_u[kEight], gates[kEight];
 #pragma unroll
-    for (int e = 0; e < kEight; ++e) sum_y[e] = sum_u[e] = sum_gate[e] = 0.0f;
+    for (int e = 0; e < kEight; ++e) sum_y[e] = sum_t[e] = 0.0f;
     for (int64_t r = r0; r < r1; ++r) {
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
         const float2 m = a.row[r];
         Piece<S> p;
         p.load(a, r, a.each ? r : set, c, n);
-        p.leave(a, r, c, n, gamma, rstd_u, rstd_h, m.x, m.y, sum_y, sum_u, sum_gate);
+        p.leave(a, r, c, n, gamma, {a.scale * rstd_u, rstd_h, m.x, m.y}, sum_y, sum_t);
     }
+    spread_sums(a, set, c, gamma, sum_t, gates, sum_u);
     const int64_t at = block * a.cols + c;
 #pragma unroll
     for (int e = 0; e < kEight; ++e) {
         if (e >= n) break;
         if (a.part_y) a.part_y[at + e] = sum_y[e];
         if (a.part_u) a.part_u[at + e] = sum_u[e];
-        if (a.part_gate) a.part_gate[at + e] = sum_gate[e];
+        if (a.part_gate) a.part_gate[at + e] = gates[e];
     }
 }
 
@@ -713,9 +753,10 @@ dol_status reverse(const Plan &p, Args<S> a, float *grad_gamma_u, const dol_matr
     a.part_y = grad_gamma_y ? p.part_y : nullptr, a.part_u = grad_gamma_u ? p.part_u : nullptr, a.part_gate = grad_gate ? p.part_gate : nullptr;
     if (p.threads) {
         const dol_status s = with_threads(p.threads, [&](auto g) {
-            constexpr int G = g.value, T = G * kBackGroups<G>;
-            if (p.whole) residual_norm_backward_kernel<S, G, true><<<static_cast<unsigned>(p.blocks), T, 0, st>>>(a);
-            else residual_norm_backward_kernel<S, G, false><<<static_cast<unsigned>(p.blocks), T, 0, st>>>(a);
+            constexpr int G = g.value, T = G * kBackGroups<G>, LDS = kGammaLds<G>;
+            const auto kernel = p.whole ? residual_norm_backward_kernel<S, G, true> : residual_norm_backward_kernel<S, G, false>;
+            if (LDS >= 32 * 1024) DOL_HIP(allow_dynamic_lds(reinterpret_cast<const void *>(kernel), LDS));
+            kernel<<<static_cast<unsigned>(p.blocks), T, LDS, st>>>(a);
             DOL_HIP(hipGetLastError());
             return DOL_OK;
         });
