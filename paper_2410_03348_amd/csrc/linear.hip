@@ -371,7 +371,18 @@ __global__ void __launch_bounds__(256) linear_zero_kernel(O *out, int64_t ld, in
 // ---------------------------------------------------------------- host side
 
 constexpr int32_t kMostFew = 64;            // rows that linear_few_kernel takes
-constexpr int kTilesAtOnce = 256;           // tiles of 64 x 64 below which k is shared out
+
+// What tiles take, in elements of a result times k, some 2.35 G of which the chip does in a millisecond with one product of planes in the large tiles
+// (256 x 256; float 128 x 256, six products).  A tile takes kAround k more than it has, and two on a unit twice as long as one.  Smaller ones load more for what they multiply, by kSlower; adding up
+// shares costs kSumWeight an element of each and a launch kLaunchWeight, both in terms of one product.  us, as chosen / others: forward, bf16
+// 4 096 x 1 024 x 4 096 47 (256 x 256) / 50 (128 x 128), 2 000 x 2 048 x 2 048 27 (128 x 128) / 62 (256 x 256) / 31 (64 x 64), 1 000 x 777 x 1 501 22 (64 x 64) / 26
+// (128 x 128 in two shares), float 1 000 x 777 x 1 501 38 (128 x 128 in two shares) / 51 (64 x 64) / 58 (128 x 128); backward, bf16 4 096 x 1 024 x 4 096 107 (128 x 128)
+// / 116 (256 x 256 in two shares each) / 138 (256 x 256), 8 192 x 4 096 x 4 096 489 (256 x 256) / 563 (128 x 128), float 300 x 300 x 300 14 (64 x 64 in three shares) / 18 (in one).
+constexpr double kAround = 160, kSumWeight = 2.5, kLaunchWeight = 7e6;
+template <int P, int Q>
+constexpr double kSlower[3] = {P == 3 ? 3.0 : 2.2, P == 3 ? 1.33 : Q == 2 ? 1.0 : 1.16, 1.0};
+template <int P, int Q>
+constexpr int kProducts = P == 3 ? 6 : Q;
 
 // A forward pass.
 struct Layout {
@@ -402,16 +413,17 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, void *workspace)
         L.each = static_cast<int32_t>(round_up(tiles(width, L.waves * L.tiles.splits), 64));
     } else {
         L.kp = round_up(width, 64), L.ldk = spread(L.kp);
-        const int64_t big = int64_t(tiles(rows, Z::Big::BM)) * tiles(out, Z::Big::BN), small = int64_t(tiles(rows, 128)) * tiles(out, 128);
-        L.size = big >= (P == 3 ? 160 : 192) ? 2 : small >= 128 ? 1 : 0;
-        by_size(L.size, Type<typename Z::Big>(), Type<typename Z::Small>(), Type<typename Z::Tiny>(), [&](auto z) {
+        double best = 0.0;
+        auto consider = [&](int size, auto z) {
             using T = typename decltype(z)::Tile;
-            L.tiles.tm = tiles(rows, T::BM), L.tiles.tn = tiles(out, T::BN), L.tiles.steps = static_cast<int32_t>(L.kp / T::BK);
-        });
-        if (L.size == 0) {
-            const int32_t n = L.tiles.tm * L.tiles.tn;
-            L.tiles.splits = std::max(1, std::min(kTilesAtOnce / n, L.tiles.steps / 4));
-        }
+            const int32_t tm = tiles(rows, T::BM), tn = tiles(out, T::BN), steps = static_cast<int32_t>(L.kp / T::BK);
+            for (int32_t n = 1; n <= std::min(16, std::max(1, steps / 2)); ++n) {
+                const double all = done(int64_t(tm) * tn * n, double(width) / n + kAround, 0, 0.0, kUnits) * T::BM * T::BN * kSlower<P, P>[size] +
+                                   (n > 1 ? (kSumWeight * n * rows * out + kLaunchWeight) / kProducts<P, P> : 0.0);
+                if (best == 0.0 || all < best) best = all, L.size = size, L.tiles.tm = tm, L.tiles.tn = tn, L.tiles.steps = steps, L.tiles.splits = n;
+            }
+        };
+        consider(2, Type<typename Z::Big>()), consider(1, Type<typename Z::Small>()), consider(0, Type<typename Z::Tiny>());
         if (!direct(x)) L.xp = c.take<uint16_t>(P * int64_t(rows) * L.ldk);
         if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(out) * L.ldk);
     }
@@ -449,24 +461,21 @@ Back lay_back(const dol_matrix *x, const dol_matrix *w, void *workspace)
     L.chunk = static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>(64, round_up(tiles(L.n_pad * tiles(L.ko, 256), 1024), 8))));
     L.chunks = tiles(L.n_pad, L.chunk);
     L.bias_part = c.take<float>(L.chunks * L.ko);
-    auto place = [&](int bm, int bn) { return (tiles(rows, bn) * int64_t(out) + tiles(out, bn) * int64_t(rows)) * tiles(width, bm) / kUnits; };
-    const int64_t big = place(Z::BigX::BM, Z::BigX::BN);
-    L.size = big >= 1024 || (P == 3 && big >= 384 && std::min(out, rows) >= 2 * big) ? 2 : place(Z::SmallX::BM, Z::SmallX::BN) >= (P == 3 ? 64 : 256) ? 1 : 0;
-    int bm = 0, bn = 0, lds = 0;
-    by_size(L.size, Type<typename Z::BigX>(), Type<typename Z::SmallX>(), Type<typename Z::TinyX>(), [&](auto z) {
-        using T = typename decltype(z)::Tile;
-        bm = T::BM, bn = T::BN, lds = T::LDS;
-    });
-    // shares so that the workgroups come out even on the places there are
-    const int64_t places = kUnits * std::max(1, kLds / lds), tx = int64_t(tiles(width, bm)) * tiles(rows, bn), tw = int64_t(tiles(width, bm)) * tiles(out, bn);
-    const int64_t even = (tx * out + tw * rows) / places;
+    // shares of k so that the workgroups of both products come out even on the units
     double best = 0.0;
-    for (int q = 6; q <= 20; ++q) {
-        const int64_t share = std::max<int64_t>(256, even * q / 10), sx = std::max<int64_t>(1, (out + share / 2) / share), sw = std::max<int64_t>(1, (rows + share / 2) / share);
-        const double sums = (sx > 1 ? double(sx) * rows : 0.0) + (sw > 1 ? double(sw) * out : 0.0);
-        const double all = done(tx * sx, double(out) / sx + 160, tw * sw, double(rows) / sw + 160, places) * bm * bn * (places / kUnits) + sums * width * 6 / (P == 3 ? 6 : Q);
-        if (best == 0.0 || all < best) best = all, L.splits_x = static_cast<int>(sx), L.splits_w = static_cast<int>(sw);
-    }
+    auto consider = [&](int size, auto z) {
+        using T = typename decltype(z)::Tile;
+        const int64_t tx = int64_t(tiles(width, T::BM)) * tiles(rows, T::BN), tw = int64_t(tiles(width, T::BM)) * tiles(out, T::BN);
+        const int64_t even = (tx * out + tw * rows) / kUnits;
+        for (int q = 6; q <= 20; ++q) {
+            const int64_t share = std::max<int64_t>(96, even * q / 10), sx = std::max<int64_t>(1, (out + share / 2) / share), sw = std::max<int64_t>(1, (rows + share / 2) / share);
+            const double sums = (sx > 1 ? double(sx) * rows : 0.0) + (sw > 1 ? double(sw) * out : 0.0);
+            const double all = done(tx * sx, double(out) / sx + kAround, tw * sw, double(rows) / sw + kAround, kUnits) * T::BM * T::BN * kSlower<P, Q>[size] +
+                               sums * width * kSumWeight / kProducts<P, Q>;
+            if (best == 0.0 || all < best) best = all, L.size = size, L.splits_x = static_cast<int>(sx), L.splits_w = static_cast<int>(sw);
+        }
+    };
+    consider(2, Type<typename Z::BigX>()), consider(1, Type<typename Z::SmallX>()), consider(0, Type<typename Z::TinyX>());
     if (L.splits_x > 1) L.part_x = c.take<float>(int64_t(L.splits_x) * rows * L.part_ld);
     if (L.splits_w > 1) L.part_w = c.take<float>(int64_t(L.splits_w) * out * L.part_ld);
     L.bytes = c.used;

@@ -171,7 +171,7 @@ def test_activation_functions(dol, n, d, m, act, dtype):
 
 
 # every tile, and both sides of the rules that choose them
-TILES = [("bfloat16", 4096, 64, 3000, "256x256x64"), ("bfloat16", 2000, 64, 2000, "128x128x64"), ("bfloat16", 700, 128, 700, "64x64x64"),
+TILES = [("bfloat16", 4096, 256, 4096, "256x256x64"), ("bfloat16", 4000, 700, 3900, "256x256x64"), ("bfloat16", 2000, 64, 2000, "128x128x64"), ("bfloat16", 700, 128, 700, "64x64x64"),
          ("float32", 2560, 64, 2048, "128x256x32"), ("float32", 1500, 100, 1500, "128x128x32"), ("float32", 300, 100, 300, "64x64x64"),
          ("bfloat16", 16, 100, 100, "few_kernel 16"), ("bfloat16", 64, 100, 100, "few_kernel 16"), ("bfloat16", 17, 100, 8200, "few_kernel 32"),
          ("bfloat16", 33, 100, 8200, "few_kernel 64"), ("float32", 1, 100, 100, "few_kernel 16"), ("float32", 50, 100, 100, "few_kernel 16"),
@@ -185,7 +185,7 @@ def test_forward_tiles(dol, dtype, n, d, m, name):
     check_forward(c, "gelu", *forward(dol, c, "gelu"))
 
 
-BACK_TILES = [("bfloat16", 4096, 512, 4096, "256x256x64"), ("bfloat16", 1000, 700, 700, "128x128x64"), ("bfloat16", 600, 128, 200, "64x64x64"),
+BACK_TILES = [("bfloat16", 4096, 2048, 4096, "256x256x64"), ("bfloat16", 4000, 2048, 2048, "128x128x64"), ("bfloat16", 600, 128, 200, "64x64x64"),
               ("bfloat16", 512, 1024, 2048, "128x128x32"), ("bfloat16", 100, 100, 100, "64x64x64"),
               ("float32", 2048, 256, 4096, "128x256x32"), ("float32", 1000, 300, 500, "128x128x32"), ("float32", 100, 100, 100, "64x64x64")]
 
