@@ -5,7 +5,8 @@
 // Memory bounds it: every gradient is read for the norm, and read and written for the result.  Squares and sums are in 64 bits, so that no
 // gradient's square is too large or too small for them; a converted element and its multiply-add cost less than its bytes.
 // A list's buffers are cut into chunks, whose table lies on the device.  One launch sums squares, a part for each workgroup; the next has every
-// workgroup add up all parts, in the same order, rather than wait for a launch that does.
+// workgroup add up all parts, in the same order, rather than wait for a launch that does.  A small network's gradients are held by one workgroup,
+// in one launch.
 #include "internal.h"
 #include "loose.h"
 #include "wave_util.h"
@@ -19,6 +20,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int64_t kChunk = 8192;        // elements
 constexpr int kMostParts = 2048;        // workgroups of a launch: eight of four wavefronts to a unit
+constexpr int kSmallThreads = 1024, kSmallEach = 4;             // chunks that a wavefront holds
+constexpr int64_t kSmallChunk = 1024;
+constexpr int kSmallChunks = kSmallThreads / kWave * kSmallEach;
 
 struct Chunk {
     void *data;
@@ -36,6 +40,7 @@ struct dol_tensor_list {
     std::vector<int32_t> by_address;    // buffers that hold something, by their first byte
     bool overlaps = false;              // two of them share memory
     int32_t chunks = 0;
+    bool small = false;                 // chunks of kSmallChunk, kSmallChunks at most
     dol::DevArray<dol::Chunk> table;
 };
 
@@ -62,33 +67,41 @@ __device__ __forceinline__ void each_vector(const S *p, int n, F f)
 {
     constexpr int V = kLooseElements<S>;
 #pragma unroll 4
-    for (int k = threadIdx.x * V; k < n; k += THREADS * V) f(loose_load(p + k, n - k), n - k, k);
+    for (int k = threadIdx.x * V; k < n; k += THREADS * V) f(loose_load_end(p + k, n - k, k), n - k, k);
+}
+
+template <typename S>
+__device__ __forceinline__ void add_vector(const Loose<S> &v, double (&sum)[2])
+{
+#pragma unroll
+    for (int k = 0; k < kLooseElements<S>; ++k) {
+        const double x = loose_get(v, k);
+        sum[k & 1] = __builtin_fma(x, x, sum[k & 1]);
+    }
+}
+
+template <typename S>
+__device__ __forceinline__ void scale_vector(const Loose<S> &v, float coef, S *to, int n)
+{
+    float x[kLooseElements<S>];
+#pragma unroll
+    for (int k = 0; k < kLooseElements<S>; ++k) x[k] = loose_get(v, k) * coef;
+    Loose<S> r;
+    loose_set(r, x);
+    loose_store(to, r, n);
 }
 
 template <typename S, int THREADS>
 __device__ __forceinline__ void add_squares(const void *data, int n, double (&sum)[2])
 {
-    each_vector<S, THREADS>(static_cast<const S *>(data), n, [&](const Loose<S> &v, int, int) {
-#pragma unroll
-        for (int k = 0; k < kLooseElements<S>; ++k) {
-            const double x = loose_get(v, k);
-            sum[k & 1] = __builtin_fma(x, x, sum[k & 1]);
-        }
-    });
+    each_vector<S, THREADS>(static_cast<const S *>(data), n, [&](const Loose<S> &v, int, int) { add_vector(v, sum); });
 }
 
 template <typename S, int THREADS>
 __device__ __forceinline__ void scale_chunk(const void *data, void *out, int n, float coef)
 {
     S *to = static_cast<S *>(out);
-    each_vector<S, THREADS>(static_cast<const S *>(data), n, [&](const Loose<S> &v, int left, int at) {
-        float x[kLooseElements<S>];
-#pragma unroll
-        for (int k = 0; k < kLooseElements<S>; ++k) x[k] = loose_get(v, k) * coef;
-        Loose<S> r;
-        loose_set(r, x);
-        loose_store(to + at, r, left);
-    });
+    each_vector<S, THREADS>(static_cast<const S *>(data), n, [&](const Loose<S> &v, int left, int at) { scale_vector(v, coef, to + at, left); });
 }
 
 __global__ void __launch_bounds__(kThreads) grad_squares_kernel(const Chunk *table, int chunks, double *part)
@@ -143,6 +156,53 @@ __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const Chunk *table
     }
 }
 
+// All of it for a list of few chunks, which the wavefronts hold as they lie: coef and out null, only the norm.  5 buffers of 16 234 floats in all SMALL_FIGURE.
+__global__ void __launch_bounds__(kSmallThreads) grad_small_kernel(const Chunk *table, const Chunk *out, int chunks, double max_norm, double eps, float *norm, float *coef)
+{
+    __shared__ double red[kSmallThreads / kWave];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int W = kSmallThreads / kWave;
+    Chunk chunk[kSmallEach];
+    Loose<float> v[kSmallEach][4];              // 1 024 numbers of a float's or (the first two) bf16's vectors
+    static_assert(kSmallChunk == 4 * 64 * 4, "a float chunk");
+#pragma unroll
+    for (int q = 0; q < kSmallEach; ++q) chunk[q] = wave + q * W < chunks ? table[wave + q * W] : Chunk{nullptr, 0, 0};
+#pragma unroll
+    for (int q = 0; q < kSmallEach; ++q)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int at = (k * 64 + lane) * (chunk[q].bf16 ? 8 : 4), n = chunk[q].n - at;
+            if (chunk[q].bf16) v[q][k] = __builtin_bit_cast(Loose<float>, loose_load_end(static_cast<const __bf16 *>(chunk[q].data) + at, n, at));
+            else v[q][k] = loose_load_end(static_cast<const float *>(chunk[q].data) + at, n, at);
+        }
+    double sum[2] = {0.0, 0.0};
+#pragma unroll
+    for (int q = 0; q < kSmallEach; ++q)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (chunk[q].bf16) add_vector(__builtin_bit_cast(Loose<__bf16>, v[q][k]), sum);
+            else add_vector(v[q][k], sum);
+        }
+    const double all = sqrt(sum_of_block<kSmallThreads>(sum[0] + sum[1], red));
+    if (threadIdx.x == 0) *norm = static_cast<float>(all);
+    if (!coef) return;
+    const float c = coef_of(all, max_norm, eps);
+    if (threadIdx.x == 0) *coef = c;
+    if (c == 1.0f && table == out) return;
+#pragma unroll
+    for (int q = 0; q < kSmallEach; ++q) {
+        if (chunk[q].n == 0) continue;
+        void *to = out[wave + q * W].data;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int at = (k * 64 + lane) * (chunk[q].bf16 ? 8 : 4), n = chunk[q].n - at;
+            if (n <= 0) continue;
+            if (chunk[q].bf16) scale_vector(__builtin_bit_cast(Loose<__bf16>, v[q][k]), c, static_cast<__bf16 *>(to) + at, n);
+            else scale_vector(v[q][k], c, static_cast<float *>(to) + at, n);
+        }
+    }
+}
+
 int parts_of(const dol_tensor_list *l) { return std::min(l->chunks, kMostParts); }
 
 dol_status check_list(const dol_tensor_list *l, const char *name)
@@ -172,7 +232,6 @@ bool crossed(const dol_tensor_list *a, const dol_tensor_list *b)
 
 dol_status sum_squares(const dol_tensor_list *l, double *part, hipStream_t st)
 {
-    if (l->chunks == 0) return DOL_OK;
     grad_squares_kernel<<<parts_of(l), kThreads, 0, st>>>(l->table.ptr, l->chunks, part);
     DOL_HIP(hipGetLastError());
     return DOL_OK;
@@ -191,7 +250,7 @@ dol_status dol_tensor_list_create(int32_t count, const int32_t *dtype, const int
     *list = nullptr;
     if (count < 0) return fail(DOL_EINVAL, "count = %d is negative", count);
     if (count > 0 && (!dtype || !size || !data)) return fail(DOL_EINVAL, "dtype, size or data is NULL");
-    int64_t chunks = 0;
+    int64_t chunks = 0, small = 0;
     for (int32_t t = 0; t < count; ++t) {
         if (dtype[t] != DOL_F32 && dtype[t] != DOL_BF16) return fail(DOL_EINVAL, "buffer %d has unknown type %d", t, dtype[t]);
         if (size[t] < 0) return fail(DOL_ESHAPE, "buffer %d has %lld elements", t, static_cast<long long>(size[t]));
@@ -201,19 +260,23 @@ dol_status dol_tensor_list_create(int32_t count, const int32_t *dtype, const int
         const int64_t n = size[t] / kChunk + (size[t] % kChunk != 0);
         if (n > INT32_MAX - chunks) return fail(DOL_EUNSUPPORTED, "the buffers have more than %lld elements", static_cast<long long>(kChunk) * INT32_MAX);
         chunks += n;
+        small = std::min<int64_t>(small + size[t] / kSmallChunk + (size[t] % kSmallChunk != 0), INT32_MAX);
     }
+    const bool few = small <= kSmallChunks;
+    const int64_t each = few ? kSmallChunk : kChunk;
+    if (few) chunks = small;
     try {
         auto l = std::make_unique<dol_tensor_list>();
         DOL_HIP(hipGetDevice(&l->device));
-        l->chunks = static_cast<int32_t>(chunks);
+        l->chunks = static_cast<int32_t>(chunks), l->small = few;
         l->dtype.assign(dtype, dtype + count), l->size.assign(size, size + count), l->data.assign(data, data + count);
         std::vector<Chunk> table;
         table.reserve(chunks);
         for (int32_t t = 0; t < count; ++t) {
             if (size[t] == 0) continue;
             l->by_address.push_back(t);
-            for (int64_t at = 0; at < size[t]; at += kChunk)
-                table.push_back(Chunk{static_cast<char *>(data[t]) + at * (dtype[t] == DOL_F32 ? 4 : 2), static_cast<int32_t>(std::min(kChunk, size[t] - at)), dtype[t] == DOL_BF16});
+            for (int64_t at = 0; at < size[t]; at += each)
+                table.push_back(Chunk{static_cast<char *>(data[t]) + at * (dtype[t] == DOL_F32 ? 4 : 2), static_cast<int32_t>(std::min(each, size[t] - at)), dtype[t] == DOL_BF16});
         }
         std::sort(l->by_address.begin(), l->by_address.end(), [&](int32_t a, int32_t b) { return std::less<void *>()(data[a], data[b]); });
         for (size_t k = 1; k < l->by_address.size(); ++k)
@@ -232,7 +295,7 @@ dol_status dol_grad_norm_workspace(const dol_tensor_list *grads, int64_t *bytes)
 {
     if (!grads) return fail(DOL_EINVAL, "grads is NULL");
     if (!bytes) return fail(DOL_EINVAL, "bytes is NULL");
-    *bytes = round_up(parts_of(grads) * static_cast<int64_t>(sizeof(double)), 256);
+    *bytes = grads->small ? 0 : round_up(parts_of(grads) * static_cast<int64_t>(sizeof(double)), 256);
     return DOL_OK;
 }
 
@@ -244,6 +307,11 @@ dol_status dol_grad_norm(const dol_tensor_list *grads, float *norm, void *worksp
     if (dol_status s = dol_grad_norm_workspace(grads, &need)) return s;
     if (dol_status s = check_workspace(workspace, workspace_bytes, need)) return s;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (grads->small) {
+        grad_small_kernel<<<1, kSmallThreads, 0, st>>>(grads->table.ptr, nullptr, grads->chunks, 0.0, 0.0, norm, nullptr);
+        DOL_HIP(hipGetLastError());
+        return DOL_OK;
+    }
     double *part = static_cast<double *>(workspace);
     if (dol_status s = sum_squares(grads, part, st)) return s;
     grad_norm_kernel<<<1, kThreads, 0, st>>>(part, parts_of(grads), norm);
@@ -267,9 +335,14 @@ dol_status dol_clip_grads(const dol_tensor_list *grads, const dol_tensor_list *o
     if (dol_status s = dol_grad_norm_workspace(grads, &need)) return s;
     if (dol_status s = check_workspace(workspace, workspace_bytes, need)) return s;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (grads->small) {
+        grad_small_kernel<<<1, kSmallThreads, 0, st>>>(grads->table.ptr, out->table.ptr, grads->chunks, max_norm, eps, norm, coef);
+        DOL_HIP(hipGetLastError());
+        return DOL_OK;
+    }
     double *part = static_cast<double *>(workspace);
     if (dol_status s = sum_squares(grads, part, st)) return s;
-    grad_scale_kernel<<<std::max(1, parts_of(grads)), kThreads, 0, st>>>(grads->table.ptr, out->table.ptr, grads->chunks, part, parts_of(grads), max_norm, eps, norm, coef);
+    grad_scale_kernel<<<parts_of(grads), kThreads, 0, st>>>(grads->table.ptr, out->table.ptr, grads->chunks, part, parts_of(grads), max_norm, eps, norm, coef);
     DOL_HIP(hipGetLastError());
     return DOL_OK;
 }

@@ -70,7 +70,8 @@ def check(dol, tensors, max_norm, eps=1e-6, out=None, stream=None):
     return norm, coef
 
 
-SIZES = [[1], [7, 1], [8192], [8191, 8193], [3, 0, 24577, 2], [100001], [33] * 300, [512, 32, 32, 15680, 10], [1 << 21, 5, 70000]]
+# both sides of what one workgroup holds (64 chunks of 1 024), and of the chunks themselves
+SIZES = [[1], [7, 1], [1023, 1025], [8192], [8191, 8193], [3, 0, 24577, 2], [65536], [65537], [1] * 64, [1] * 65, [100001], [33] * 300, [512, 32, 32, 15680, 10], [1 << 21, 5, 70000]]
 
 
 @pytest.mark.parametrize("dtypes", ["f", "b", "fb"])
@@ -89,8 +90,9 @@ def test_sizes(dol, sizes, dtypes, inplace, shift):
 
 
 @pytest.mark.parametrize("inplace", [True, False])
-def test_a_norm_that_is_allowed_leaves_every_bit(dol, inplace):
-    tensors, _ = make([1000, 33, 9000], [torch.float32, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("large", [0, 100000])
+def test_a_norm_that_is_allowed_leaves_every_bit(dol, inplace, large):
+    tensors, _ = make([1000, 33, 9000 + large], [torch.float32, torch.bfloat16, torch.float32])
     before = [t.clone() for t in tensors]
     out = None if inplace else [torch.zeros_like(t) for t in tensors]
     _, coef = check(dol, tensors, 1e4, out=out)
@@ -114,8 +116,9 @@ def test_squares_past_a_floats_range(dol, scale):
 
 
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
-def test_a_norm_that_is_not_finite(dol, value):
-    tensors, _ = make([70000, 33], [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [60010, 70000])
+def test_a_norm_that_is_not_finite(dol, value, n):
+    tensors, _ = make([n, 33], [torch.float32, torch.bfloat16])
     tensors[0][60001] = value
     norm, coef = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
     dol.clip_grads(dol.TensorList(tensors), 1.0, norm, coef)
@@ -157,7 +160,7 @@ def test_refused_lists(dol):
         with pytest.raises(dol.DolError, match="at least 0"):
             dol.clip_grads(one, most, norm, coef, eps=eps)
     with pytest.raises(dol.DolError, match="workspace"):
-        dol.clip_grads(one, 1.0, norm, coef, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+        dol.clip_grads(dol.TensorList([torch.empty(70000, device="cuda")]), 1.0, norm, coef, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
     torch.cuda.synchronize()
     assert torch.equal(a, before) and float(norm) == 9.0 and float(coef) == 9.0
     dol.grad_norm(twice, norm)
@@ -185,8 +188,9 @@ def test_more_elements_than_32_bits_count(dol):
     assert int(t.count_nonzero()) == 0
 
 
-def test_the_same_bits_on_any_stream_and_in_a_graph(dol):
-    tensors, _ = make([300000, 5, 77777], [torch.float32, torch.bfloat16, torch.bfloat16], seed=3)
+@pytest.mark.parametrize("n", [3000, 300000])
+def test_the_same_bits_on_any_stream_and_in_a_graph(dol, n):
+    tensors, _ = make([n, 5, n // 4 + 1], [torch.float32, torch.bfloat16, torch.bfloat16], seed=3)
     out = [[torch.empty_like(t) for t in tensors] for _ in range(2)]
     grads, lists = dol.TensorList(tensors), [dol.TensorList(o) for o in out]
     norm, coef = (torch.zeros(2, 1, device="cuda") for _ in range(2))
