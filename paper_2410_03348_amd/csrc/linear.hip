@@ -26,7 +26,6 @@ struct Result {
     int64_t y_ld, z_ld;
     int16_t *rest;              // [rows][cols]
     int32_t rows, cols, act;
-    bool vec;                   // four neighbouring columns from a multiple of four on are aligned to their size, in all of them
 };
 
 // What rounding z to bf16 leaves, in a float's steps (whose bits count them across powers of two as well): -32768 .. 32768, the last of which, where z lies
@@ -37,22 +36,37 @@ __device__ __forceinline__ uint32_t rest_of(float z)
     return __builtin_isfinite(z) ? static_cast<uint32_t>(min(r, 32767)) & 0xFFFF : 0;
 }
 
+__device__ __forceinline__ void store_rest(int16_t *to, f32x4 z)
+{
+    struct __attribute__((packed, aligned(2))) Words { uint32_t w[2]; };
+    *reinterpret_cast<Words *>(to) = Words{{rest_of(z[0]) | rest_of(z[1]) << 16, rest_of(z[2]) | rest_of(z[3]) << 16}};
+}
+
 __device__ __forceinline__ float with_rest(float z, uint32_t rest) { return __uint_as_float(__float_as_uint(z) + static_cast<uint32_t>(static_cast<int16_t>(rest))); }
 
-// Columns c .. c + 3 of row r of z to what the call leaves; n of them are there.
+// The bias of columns c .. c + 3, asked for early: behind the products it would be one more wait.
+__device__ __forceinline__ f32x4 bias_of(const Result &o, int c)
+{
+    f32x4 b = {0, 0, 0, 0};
+    if (o.bias)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (c + k < o.cols) b[k] = o.bias[c + k];
+    return b;
+}
+
+// Columns c .. c + 3 of row r of z without its bias to what the call leaves; those of them that are there.
 template <typename S, typename A>
-__device__ __forceinline__ void leave(const Result &o, A, int64_t r, int c, f32x4 z)
+__device__ __forceinline__ void leave(const Result &o, A, int64_t r, int c, f32x4 bias, f32x4 z)
 {
     const int n = o.cols - c;
     S *y = static_cast<S *>(o.y) + r * o.y_ld + c;
-    if (o.bias)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) z[k] += k < n ? o.bias[c + k] : 0.0f;
+    z += bias;
     if (o.z) {
-        store4(static_cast<S *>(o.z) + r * o.z_ld + c, z, n, o.vec);
+        store4(static_cast<S *>(o.z) + r * o.z_ld + c, z, n);
         if (sizeof(S) == 2 && o.rest) {
             int16_t *to = o.rest + r * o.cols + c;
-            if (o.vec && n >= 4) *reinterpret_cast<u32x2 *>(to) = u32x2{rest_of(z[0]) | rest_of(z[1]) << 16, rest_of(z[2]) | rest_of(z[3]) << 16};
+            if (n >= 4) store_rest(to, z);
             else
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
@@ -63,9 +77,8 @@ __device__ __forceinline__ void leave(const Result &o, A, int64_t r, int c, f32x
     for (int k = 0; k < 4; ++k) z[k] = act_of<A::value, false>(z[k], nullptr);
     if (o.residual) {
         const S *from = static_cast<const S *>(o.residual) + r * o.residual_ld + c;
-        if (o.vec && n >= 4) {
-            struct alignas(4 * sizeof(S)) Four { S e[4]; };
-            const Four q = *reinterpret_cast<const Four *>(from);
+        if (n >= 4) {
+            const Four<S> q = *reinterpret_cast<const Four<S> *>(from);
 #pragma unroll
             for (int k = 0; k < 4; ++k) z[k] += static_cast<float>(q.e[k]);
         } else
@@ -73,7 +86,7 @@ __device__ __forceinline__ void leave(const Result &o, A, int64_t r, int c, f32x
             for (int k = 0; k < 4; ++k)
                 if (k < n) z[k] += static_cast<float>(from[k]);
     }
-    store4(y, z, n, o.vec);
+    store4(y, z, n);
 }
 
 // ---------------------------------------------------------------- tiles
@@ -89,23 +102,19 @@ struct Tiles {
 template <int ACT, typename S, typename T>
 __device__ __forceinline__ void leave_whole(const Result &o, int64_t m0, int c, const f32x4 (&acc)[T::MI][T::NI])
 {
-    struct alignas(4 * sizeof(S)) Four { S e[4]; };
-    f32x4 b = {0, 0, 0, 0};
-    if (o.bias)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) b[k] = o.bias[c + k];
+    const f32x4 b = bias_of(o, c);
     const int64_t first = m0 + T::row_of(0);
     const S *from = static_cast<const S *>(o.residual) + first * o.residual_ld + c;
-    Four next[4];
+    Four<S> next[4];
     auto ask = [&](int i) {
         if (o.residual)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) next[e] = *reinterpret_cast<const Four *>(from + (i * 16 + e) * o.residual_ld);
+            for (int e = 0; e < 4; ++e) next[e] = *reinterpret_cast<const Four<S> *>(from + (i * 16 + e) * o.residual_ld);
     };
     ask(0);
 #pragma unroll
     for (int i = 0; i < T::MI; ++i) {
-        Four r[4];
+        Four<S> r[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) r[e] = next[e];
         if (i + 1 < T::MI) ask(i + 1);
@@ -113,15 +122,15 @@ __device__ __forceinline__ void leave_whole(const Result &o, int64_t m0, int c, 
         for (int e = 0; e < 4; ++e) {
             const int64_t row = first + i * 16 + e;
             f32x4 z = f32x4{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]} + b;
-            if (o.z) store4(static_cast<S *>(o.z) + row * o.z_ld + c, z, 4, true);
+            if (o.z) store4(static_cast<S *>(o.z) + row * o.z_ld + c, z, 4);
             if (sizeof(S) == 2 && o.rest)
-                *reinterpret_cast<u32x2 *>(o.rest + row * o.cols + c) = u32x2{rest_of(z[0]) | rest_of(z[1]) << 16, rest_of(z[2]) | rest_of(z[3]) << 16};
+                store_rest(o.rest + row * o.cols + c, z);
 #pragma unroll
             for (int k = 0; k < 4; ++k) z[k] = act_of<ACT, false>(z[k], nullptr);
             if (o.residual)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) z[k] += static_cast<float>(r[e].e[k]);
-            store4(static_cast<S *>(o.y) + row * o.y_ld + c, z, 4, true);
+            store4(static_cast<S *>(o.y) + row * o.y_ld + c, z, 4);
         }
     }
 }
@@ -139,8 +148,9 @@ __global__ void __launch_bounds__(T::NT, 2) linear_tiles_kernel(Planes x, Planes
     const int m0 = mt * T::BM, n0 = nt * T::BN;
     T::run(x, m0, o.rows, w, n0, o.cols, static_cast<int64_t>(s0) * T::BK, s1 - s0, smem, acc);
     const int c = n0 + T::col_of();
-    if (!g.part && o.vec && m0 + T::BM <= o.rows && n0 + T::BN <= o.cols) return leave_whole<ACT, S, T>(o, m0, c, acc);
+    if (!g.part && m0 + T::BM <= o.rows && n0 + T::BN <= o.cols) return leave_whole<ACT, S, T>(o, m0, c, acc);
     if (c >= o.cols) return;
+    const f32x4 b = bias_of(o, c);
 #pragma unroll
     for (int i = 0; i < T::MI; ++i)
 #pragma unroll
@@ -149,7 +159,7 @@ __global__ void __launch_bounds__(T::NT, 2) linear_tiles_kernel(Planes x, Planes
             const f32x4 z{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
             if (r >= o.rows) continue;
             if (g.part) *reinterpret_cast<f32x4 *>(g.part + (split * static_cast<int64_t>(o.rows) + r) * g.part_ld + c) = z;
-            else leave<S>(o, Act<ACT>(), r, c, z);
+            else leave<S>(o, Act<ACT>(), r, c, b, z);
         }
 }
 
@@ -161,10 +171,11 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float *part, int
     for (int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; t < all; t += static_cast<int64_t>(gridDim.x) * 256) {
         const int64_t r = t / per;
         const int c = static_cast<int>(t - r * per) * 4;
+        const f32x4 b = bias_of(o, c);
         f32x4 z = {0, 0, 0, 0};
 #pragma unroll 8
         for (int k = 0; k < splits; ++k) z += *reinterpret_cast<const f32x4 *>(part + (static_cast<int64_t>(k) * o.rows + r) * part_ld + c);
-        with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, z); });
+        with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, b, z); });
     }
 }
 
@@ -186,6 +197,8 @@ __global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(const S *x, 
     const int64_t k0 = static_cast<int64_t>(split * waves + wave) * each, k1 = min(k0 + each, static_cast<int64_t>(width));
     const S *from_w = w + min(group * 16 + (lane & 15), o.cols - 1) * ldw, *from_x[R];
     f32x4 acc[R];
+    const int c = group * 16 + (lane >> 4) * 4;
+    const f32x4 bias = bias_of(o, c);
 #pragma unroll
     for (int r = 0; r < R; ++r) from_x[r] = x + min(row0 + r * 16 + (lane & 15), o.rows - 1) * ldx, acc[r] = f32x4{0, 0, 0, 0};
     auto products = [&](const Loose<S> (&a)[2], const Loose<S> (&b)[R][2]) {
@@ -221,9 +234,10 @@ __global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(const S *x, 
         Loose<S> a[2], b[R][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            a[h] = loose_load(from_w + k + h * V, k1 - k - h * V);
+            const int left = static_cast<int>(k1 - k) - h * V, before = static_cast<int>(k) + h * V;
+            a[h] = loose_load_end(from_w + k + h * V, left, before);
 #pragma unroll
-            for (int r = 0; r < R; ++r) b[r][h] = loose_load(from_x[r] + k + h * V, k1 - k - h * V);
+            for (int r = 0; r < R; ++r) b[r][h] = loose_load_end(from_x[r] + k + h * V, left, before);
         }
         products(a, b);
     }
@@ -232,12 +246,13 @@ __global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(const S *x, 
     lds_barrier();
     for (int m = wave; m < R; m += waves) {
         f32x4 z = red[0][m][lane];
-        for (int q = 1; q < waves; ++q) z += red[q][m][lane];
+#pragma unroll
+        for (int q = 1; q < kFewWaves; ++q)
+            if (q < waves) z += red[q][m][lane];
         const int64_t r = row0 + m * 16 + (lane & 15);
-        const int c = group * 16 + (lane >> 4) * 4;
         if (r >= o.rows || c >= o.cols) continue;
         if (part) *reinterpret_cast<f32x4 *>(part + (split * static_cast<int64_t>(o.rows) + r) * part_ld + c) = z;
-        else with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, z); });
+        else with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, bias, z); });
     }
 }
 
@@ -259,73 +274,99 @@ struct Slope {
     int32_t rows, cols, act;
     uint16_t *dz;               // null: only the sums
     int64_t out_rows, out_cols, ld, plane;      // as they are laid out
-    float *part;                // [chunks][out_cols], null: only dz
-    int32_t chunk;              // rows, of 8 at a time
+    float *part;                // [chunks][part_cols], null: only dz
+    int32_t part_cols;
+    int32_t chunk;              // rows of a workgroup
     int32_t wide;               // workgroups side by side
+    bool narrow;                // of 64 columns, or of 256
     unsigned blocks;            // none where dz is grad_y as it is
 };
 
-// 32 threads of eight columns by eight rows at a time.
-template <typename S, int Q>
-__device__ __forceinline__ void slope_rows(const Slope &p, unsigned block)
+// LANES threads of eight columns by 256 / LANES rows at a time.
+template <typename S, int Q, int LANES>
+__device__ __forceinline__ void slope_rows(const Slope &p, unsigned block, float *red)
 {
-    __shared__ float red[8][256];
-    const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
-    const int64_t chunk = block / p.wide;
-    const int64_t c = static_cast<int64_t>(block % p.wide) * 256 + lane * 8, n = p.cols - c;
-    constexpr int V = kLooseElements<S>, H = 8 / V;
+    constexpr int V = kLooseElements<S>, H = 8 / V, ROWS = 256 / LANES, WIDE = LANES * 8;
+    // what a row's eight columns are read for; kAhead rows are asked for before the first of them is worked on
+    struct Row {
+        Loose<S> g[H], z[H];
+        Loose<__bf16> rest;
+    };
+    constexpr int kAhead = sizeof(S) == 2 ? 4 : 2;
+    const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
+    const int64_t chunk = block / p.wide, column = static_cast<int64_t>(block % p.wide) * WIDE, c = column + lane * 8, n = p.cols - c;
+    const int64_t r0 = chunk * p.chunk + row, r1 = min((chunk + 1) * p.chunk, p.out_rows);
     float sum[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
     with_act(p.act, [&](auto a) {
-        for (int64_t r = chunk * p.chunk + row; r < min((chunk + 1) * p.chunk, p.out_rows) && c < p.out_cols; r += 8) {
-            const int64_t left = r < p.rows ? n : 0;
-            float v[8], z[8];
+        constexpr bool ACT = decltype(a)::value != DOL_ACT_NONE;
+        const bool rests = ACT && sizeof(S) == 2 && p.rest;
+        for (int64_t first = r0; first < r1 && c < p.out_cols; first += ROWS * kAhead) {
+            Row q[kAhead];
+            if (n >= 8 && first + ROWS * (kAhead - 1) < p.rows) {       // (one branch for all loads: each is waited for at a branch's end)
 #pragma unroll
-            for (int h = 0; h < H; ++h) {
-                const Loose<S> g = loose_load(static_cast<const S *>(p.grad_y) + r * p.grad_ld + c + h * V, left - h * V);
-                Loose<S> q{};
-                if (a.value != DOL_ACT_NONE) q = loose_load(static_cast<const S *>(p.z) + r * p.z_ld + c + h * V, left - h * V);
+                for (int t = 0; t < kAhead; ++t) {
+                    const int64_t r = first + ROWS * t;
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[h * V + e] = loose_get(g, e), z[h * V + e] = loose_get(q, e);
-            }
-            if (a.value != DOL_ACT_NONE) {
-                if (sizeof(S) == 2 && p.rest) {
-                    const Loose<S> q = loose_load(reinterpret_cast<const S *>(p.rest + r * p.cols + c), left);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = with_rest(z[e], q.w[e >> 1 & 3] >> (e & 1) * 16);
+                    for (int h = 0; h < H; ++h) {
+                        q[t].g[h] = *reinterpret_cast<const Loose<S> *>(static_cast<const S *>(p.grad_y) + r * p.grad_ld + c + h * V);
+                        if (ACT) q[t].z[h] = *reinterpret_cast<const Loose<S> *>(static_cast<const S *>(p.z) + r * p.z_ld + c + h * V);
+                    }
+                    if (rests) q[t].rest = *reinterpret_cast<const Loose<__bf16> *>(p.rest + r * p.cols + c);
                 }
+            } else
+#pragma unroll
+                for (int t = 0; t < kAhead; ++t) {
+                    const int64_t r = first + ROWS * t;
+                    const int left = r < p.rows ? static_cast<int>(min(n, static_cast<int64_t>(8))) : 0, before = static_cast<int>(c);
+#pragma unroll
+                    for (int h = 0; h < H; ++h) {
+                        q[t].g[h] = loose_load_end(static_cast<const S *>(p.grad_y) + r * p.grad_ld + c + h * V, left - h * V, before + h * V);
+                        if (ACT) q[t].z[h] = loose_load_end(static_cast<const S *>(p.z) + r * p.z_ld + c + h * V, left - h * V, before + h * V);
+                    }
+                    if (rests) q[t].rest = loose_load_end(reinterpret_cast<const __bf16 *>(p.rest) + r * p.cols + c, left, before);
+                }
+#pragma unroll
+            for (int t = 0; t < kAhead; ++t) {
+                const int64_t r = first + ROWS * t;
+                if (r >= r1) break;
+                float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    float slope;
-                    act_of<decltype(a)::value, true>(z[e], &slope);
-                    v[e] *= slope;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += v[e];
-            if (p.dz)
-#pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    u32x4 o;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t lo = plane_of<Q>(q, v[2 * k]), hi = plane_of<Q>(q, v[2 * k + 1]);
-                        o[k] = lo | hi << 16;
+                    v[e] = loose_get(q[t].g[e / V], e % V);
+                    if constexpr (ACT) {
+                        float z = loose_get(q[t].z[e / V], e % V), slope;
+                        if (rests) z = with_rest(z, q[t].rest.w[e >> 1] >> (e & 1) * 16);
+                        act_of<decltype(a)::value, true>(z, &slope);
+                        v[e] *= slope;
                     }
-                    *reinterpret_cast<u32x4 *>(p.dz + q * p.plane + r * p.ld + c) = o;
+                    sum[e] += v[e];
                 }
+                if (p.dz)
+#pragma unroll
+                    for (int s = 0; s < Q; ++s) {
+                        u32x4 o;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t lo = plane_of<Q>(s, v[2 * k]), hi = plane_of<Q>(s, v[2 * k + 1]);
+                            o[k] = lo | hi << 16;
+                        }
+                        *reinterpret_cast<u32x4 *>(p.dz + s * p.plane + r * p.ld + c) = o;
+                    }
+            }
         }
     });
     if (!p.part) return;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) red[row][lane * 8 + e] = sum[e];
+    for (int e = 0; e < 8; ++e) red[row * WIDE + lane * 8 + e] = sum[e];
     __syncthreads();
-    const int64_t at = static_cast<int64_t>(block % p.wide) * 256 + threadIdx.x;
+    if (threadIdx.x >= WIDE) return;
+    const int64_t at = column + threadIdx.x;
     float s = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s += red[k][threadIdx.x];
-    if (at < p.out_cols) p.part[chunk * p.out_cols + at] = s;
+    for (int k = 0; k < ROWS; ++k) s += red[k * WIDE + threadIdx.x];
+    if (at < p.part_cols) p.part[chunk * p.part_cols + at] = s;
 }
 
 // All that a backward pass does before its products, in one launch.
@@ -333,7 +374,8 @@ template <typename S, int P, int Q>
 __global__ void __launch_bounds__(256) linear_slope_kernel(Slope p, Pack x, Pack w)
 {
     unsigned block = blockIdx.x;
-    if (block < p.blocks) return slope_rows<S, Q>(p, block);
+    __shared__ float red[2048];
+    if (block < p.blocks) return p.narrow ? slope_rows<S, Q, 8>(p, block, red) : slope_rows<S, Q, 32>(p, block, red);
     block -= p.blocks;
     if (block < x.blocks) return pack_rows<S, P>(x, block);
     pack_rows<S, P>(w, block - x.blocks);
@@ -432,6 +474,8 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, void *workspace)
     return L;
 }
 
+constexpr int kOneChunk = 64;
+
 // A backward pass.
 struct Back {
     int64_t kp, ldk, ko, ldo, n_pad;        // width, out and rows as they are laid out
@@ -458,7 +502,8 @@ Back lay_back(const dol_matrix *x, const dol_matrix *w, void *workspace)
     if (!L.x_direct) L.xp = c.take<uint16_t>(P * L.n_pad * L.ldk);
     if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(out) * L.ldk);
     L.dz = c.take<uint16_t>(Q * L.n_pad * L.ldo);
-    L.chunk = static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>(64, round_up(tiles(L.n_pad * tiles(L.ko, 256), 1024), 8))));
+    // (few rows are one chunk, whose sums are grad_bias)
+    L.chunk = rows <= kOneChunk ? kOneChunk : static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>(64, round_up(tiles(L.n_pad * tiles(L.ko, 256), 1024), 8))));
     L.chunks = tiles(L.n_pad, L.chunk);
     L.bias_part = c.take<float>(L.chunks * L.ko);
     // shares of k so that the workgroups of both products come out even on the units
@@ -471,7 +516,7 @@ Back lay_back(const dol_matrix *x, const dol_matrix *w, void *workspace)
             const int64_t share = std::max<int64_t>(96, even * q / 10), sx = std::max<int64_t>(1, (out + share / 2) / share), sw = std::max<int64_t>(1, (rows + share / 2) / share);
             const double sums = (sx > 1 ? double(sx) * rows : 0.0) + (sw > 1 ? double(sw) * out : 0.0);
             const double all = done(tx * sx, double(out) / sx + kAround, tw * sw, double(rows) / sw + kAround, kUnits) * T::BM * T::BN * kSlower<P, Q>[size] +
-                               sums * width * kSumWeight / kProducts<P, Q>;
+                               (sums * width * kSumWeight + (sums > 0.0 && L.chunks == 1 ? kLaunchWeight : 0.0)) / kProducts<P, Q>;
             if (best == 0.0 || all < best) best = all, L.size = size, L.splits_x = static_cast<int>(sx), L.splits_w = static_cast<int>(sw);
         }
     };
@@ -580,9 +625,11 @@ dol_status reverse(const Back &L, const dol_matrix *x, const dol_matrix *w, int 
     if (as_it_is) dz = Planes{static_cast<const uint16_t *>(grad_y->data), grad_y->ld, 0};
     Slope p{};
     if (write || grad_bias) {
-        const int32_t wide = tiles(L.ko, 256);
+        const bool narrow = L.chunks == 1;
+        const int32_t wide = tiles(L.ko, narrow ? 64 : 256);
         p = Slope{grad_y->data, z ? z->data : nullptr, grad_y->ld, z ? z->ld : 0, rest, x->rows, w->rows, act, write ? L.dz : nullptr, L.n_pad, L.ko, L.ldo, L.n_pad * L.ldo,
-                  grad_bias ? L.bias_part : nullptr, L.chunk, wide, static_cast<unsigned>(wide * L.chunks)};
+                  grad_bias ? L.chunks == 1 ? grad_bias : L.bias_part : nullptr, L.chunks == 1 ? w->rows : static_cast<int32_t>(L.ko), L.chunk, wide,
+                  narrow, static_cast<unsigned>(wide * L.chunks)};
     }
     if (const unsigned n = p.blocks + lx.blocks + lw.blocks) {
         linear_slope_kernel<S, P, Q><<<n, 256, 0, st>>>(p, lx, lw);
@@ -603,7 +650,7 @@ dol_status reverse(const Back &L, const dol_matrix *x, const dol_matrix *w, int 
                        : L.size == 1 ? launch_products<typename Z::SmallX, typename Z::SmallW, S>(a, b, st)
                                      : launch_products<typename Z::TinyX, typename Z::TinyW, S>(a, b, st))
         return s;
-    const Sum sx = sum_of(a), sw = sum_of(b), sb = grad_bias ? make_sum(L.bias_part, 1, w->rows, L.chunks, L.ko, grad_bias, w->rows) : Sum{};
+    const Sum sx = sum_of(a), sw = sum_of(b), sb = grad_bias && L.chunks > 1 ? make_sum(L.bias_part, 1, w->rows, L.chunks, L.ko, grad_bias, w->rows) : Sum{};
     const unsigned n = sx.blocks + sw.blocks + sb.blocks;
     if (n == 0) return DOL_OK;
     linear_finish_kernel<S><<<n, 256, 0, st>>>(sx, sw, sb);
@@ -639,11 +686,6 @@ dol_status check_as(const dol_matrix *m, int32_t rows, int32_t cols, int32_t dty
     if (m->dtype != dtype) return fail(DOL_EINVAL, "%s is of another type than x", name);
     if (m->rows != rows || m->cols != cols) return fail(DOL_ESHAPE, "%s is %d x %d, not %d x %d", name, m->rows, m->cols, rows, cols);
     return DOL_OK;
-}
-
-bool fours(const dol_matrix *m)             // rows from columns that are multiples of four on are aligned to four elements
-{
-    return !m || (m->ld % 4 == 0 && !(reinterpret_cast<uintptr_t>(m->data) & (m->dtype == DOL_F32 ? 15 : 7)));
 }
 
 }  // namespace
@@ -699,7 +741,6 @@ dol_status dol_linear(const dol_matrix *x, const dol_matrix *weight, const float
     o.bias = bias, o.act = act, o.rows = x->rows, o.cols = weight->rows, o.y = y->data, o.y_ld = y->ld, o.rest = z_rest;
     if (residual) o.residual = residual->data, o.residual_ld = residual->ld;
     if (z) o.z = z->data, o.z_ld = z->ld;
-    o.vec = fours(residual) && fours(y) && fours(z) && (!z_rest || (weight->rows % 4 == 0 && !(reinterpret_cast<uintptr_t>(z_rest) & 7)));
     auto go = [&](auto p) {
         const Layout L = lay_out<p.value>(x, weight, workspace);
         if (dol_status s = check_workspace(workspace, workspace_bytes, L.bytes)) return s;

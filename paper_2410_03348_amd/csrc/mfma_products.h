@@ -2,6 +2,7 @@
 // mfma_tile.h, the two products of a backward pass, sums of shares of k, and when places are done with tiles of two lengths.
 #pragma once
 
+#include "loose.h"
 #include "mfma_tile.h"
 
 #include <type_traits>
@@ -73,7 +74,6 @@ struct Pack {
     int32_t classes;
     uint16_t *out;
     int64_t out_rows, kp, out_ld;
-    bool vec;
     unsigned blocks;            // none where the matrix is read as it is
 };
 
@@ -88,17 +88,13 @@ __device__ __forceinline__ void pack_rows(const Pack &p, unsigned block)
         const bool in = r < p.rows && (!p.target || (kept_row(p.target[r], p.classes) && p.lse[r] != -INFINITY));
         const S *from = static_cast<const S *>(p.src) + r * p.ld + c;
         float v[8];
-        if (in && p.vec && c + 8 <= p.cols) {
-            struct alignas(16) Piece { S e[16 / sizeof(S)]; };
+        constexpr int V = kLooseElements<S>;
 #pragma unroll
-            for (int h = 0; h < static_cast<int>(8 * sizeof(S) / 16); ++h) {
-                const Piece q = reinterpret_cast<const Piece *>(from)[h];
+        for (int h = 0; h < 8 / V; ++h) {
+            const Loose<S> q = loose_load_end(from + h * V, in ? p.cols - c - h * V : 0, c + h * V);
 #pragma unroll
-                for (int k = 0; k < static_cast<int>(16 / sizeof(S)); ++k) v[h * (16 / sizeof(S)) + k] = static_cast<float>(q.e[k]);
-            }
-        } else
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = in && c + k < p.cols ? static_cast<float>(from[k]) : 0.0f;
+            for (int k = 0; k < V; ++k) v[h * V + k] = loose_get(q, k);
+        }
 #pragma unroll
         for (int q = 0; q < P; ++q) {
             u32x4 w;
@@ -140,7 +136,6 @@ __device__ __forceinline__ void product_tile(const Product &p, int id, char *sme
     f32x4 acc[T::MI][T::NI];
     T::clear(acc);
     T::run(p.a, static_cast<int64_t>(mt) * T::BM, p.wide, p.b, static_cast<int64_t>(nt) * T::BN, p.tall, k0, s1 - s0, smem, acc, p.have - k0);
-    const bool vec = p.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (4 * sizeof(O) - 1)) == 0;
 #pragma unroll
     for (int j = 0; j < T::NI; ++j) {
         const int n = nt * T::BN + T::col_of(j);
@@ -153,7 +148,7 @@ __device__ __forceinline__ void product_tile(const Product &p, int id, char *sme
                 f32x4 *to = reinterpret_cast<f32x4 *>(p.part + (static_cast<int64_t>(split) * p.N + n) * p.part_ld + m);
                 *to = p.add ? *to + acc[i][j] : acc[i][j];
             } else
-                store4(static_cast<O *>(p.out) + n * p.out_ld + m, acc[i][j], p.M - m, vec);
+                store4(static_cast<O *>(p.out) + n * p.out_ld + m, acc[i][j], p.M - m);
         }
     }
 }
@@ -177,7 +172,6 @@ __device__ __forceinline__ void sum_parts(const Sum &s, unsigned block)
     __shared__ f32x4 red[4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t per = (s.N + 3) / 4, all = s.M * per;
-    const bool vec = s.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(s.out) & (4 * sizeof(O) - 1)) == 0;
     const int each = s.shared ? 64 : 256, at = s.shared ? lane : threadIdx.x;
     for (int64_t first = static_cast<int64_t>(block) * each; first < all; first += static_cast<int64_t>(s.blocks) * each) {
         const int64_t t = first + at, m = t / per;
@@ -194,7 +188,7 @@ __device__ __forceinline__ void sum_parts(const Sum &s, unsigned block)
             __syncthreads();
             if (wave != 0) continue;
         }
-        if (in) store4(static_cast<O *>(s.out) + m * s.out_ld + n, v, s.N - n, vec);
+        if (in) store4(static_cast<O *>(s.out) + m * s.out_ld + n, v, s.N - n);
     }
 }
 
@@ -238,14 +232,12 @@ auto by_size(int size, B big, S small, T tiny, F f) { return size == 2 ? f(big) 
 template <int P>
 Pack pack_of(const dol_matrix *m, const int32_t *target, const float *lse, int32_t classes, uint16_t *out, int64_t out_rows, int64_t kp, int64_t ld, Planes *p)
 {
-    using S = typename Source<P>::T;
     if (!out) {
         *p = Planes{static_cast<const uint16_t *>(m->data), m->ld, 0};
         return Pack{};
     }
     *p = Planes{out, ld, out_rows * ld};
-    const bool vec = !(reinterpret_cast<uintptr_t>(m->data) & 15) && m->ld % (16 / int64_t(sizeof(S))) == 0;
-    return Pack{m->data, m->ld, m->rows, m->cols, target, lse, classes, out, out_rows, kp, ld, vec, blocks(std::min(out_rows * (kp / 8), kMostBlocks * 256))};
+    return Pack{m->data, m->ld, m->rows, m->cols, target, lse, classes, out, out_rows, kp, ld, blocks(std::min(out_rows * (kp / 8), kMostBlocks * 256))};
 }
 
 // (few parts are read as fast by a thread each; a loop over many of them waits for every load)

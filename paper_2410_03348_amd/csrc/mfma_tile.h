@@ -335,17 +335,21 @@ struct MfmaTile {
     __device__ static int col_of(int j = 0) { return (threadIdx.x >> 6) % WN * TN + col_at(j, threadIdx.x & 15); }
 };
 
-// The first n (at most four) of v to p; `vec`: p is aligned to four elements.
+// Four neighbouring elements, of which only each is aligned: memory takes them at once all the same.
 template <typename O>
-__device__ __forceinline__ void store4(O *p, f32x4 v, int n, bool vec)
+struct __attribute__((packed, aligned(sizeof(O)))) Four {
+    O e[4];
+};
+
+// The first n (at most four) of v to p.
+template <typename O>
+__device__ __forceinline__ void store4(O *p, f32x4 v, int n)
 {
-    if (vec && n >= 4) {
-        if constexpr (sizeof(O) == 4) *reinterpret_cast<f32x4 *>(p) = v;
-        else {
-            u32x2 w;
-            w[0] = bits16<__bf16>(v[0]) | bits16<__bf16>(v[1]) << 16, w[1] = bits16<__bf16>(v[2]) | bits16<__bf16>(v[3]) << 16;
-            *reinterpret_cast<u32x2 *>(p) = w;
-        }
+    if (n >= 4) {
+        struct __attribute__((packed, aligned(sizeof(O)))) Words { uint32_t w[sizeof(O)]; } q;
+        if constexpr (sizeof(O) == 4) q.w[0] = __float_as_uint(v[0]), q.w[1] = __float_as_uint(v[1]), q.w[2] = __float_as_uint(v[2]), q.w[3] = __float_as_uint(v[3]);
+        else q.w[0] = bits16<__bf16>(v[0]) | bits16<__bf16>(v[1]) << 16, q.w[1] = bits16<__bf16>(v[2]) | bits16<__bf16>(v[3]) << 16;
+        *reinterpret_cast<Words *>(p) = q;
         return;
     }
 #pragma unroll

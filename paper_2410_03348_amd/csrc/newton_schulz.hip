@@ -247,7 +247,6 @@ __global__ void __launch_bounds__(T::NT, 2) ns_apply_kernel(Apply p)
     T::run(TURN ? pb : px, mt * T::BM, TURN ? p.mp : p.np, TURN ? px : pb, nt * T::BN, TURN ? p.np : p.mp, 0, p.mp / T::BK, smem, acc, p.mp);
     T::join(acc, smem);
     if (!T::first_set()) return;
-    const bool vec = p.out_ld % 4 == 0 && (reinterpret_cast<uintptr_t>(static_cast<O *>(p.out) + z * p.out_stride) & (4 * sizeof(O) - 1)) == 0;
 #pragma unroll
     for (int i = 0; i < T::MI; ++i) {
         const int64_t m = static_cast<int64_t>(mt) * T::BM + T::row_of(i);      // four rows of the tile from here: neighbours in memory
@@ -257,7 +256,7 @@ __global__ void __launch_bounds__(T::NT, 2) ns_apply_kernel(Apply p)
             const f32x4 v = p.alpha * acc[i][j];
             if (TURN || p.out) {
                 if (n < p.out_rows && m < p.out_cols)
-                    store4(static_cast<O *>(p.out) + z * p.out_stride + n * p.out_ld + m, v, static_cast<int>(p.out_cols - m), vec);
+                    store4(static_cast<O *>(p.out) + z * p.out_stride + n * p.out_ld + m, v, static_cast<int>(p.out_cols - m));
             } else
                 write4<2>(p.to + z * p.x_stride + n * p.np + m, plane, v);
         }
