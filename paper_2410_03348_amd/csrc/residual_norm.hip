@@ -23,6 +23,7 @@ namespace {
 constexpr int kEight = 8;               // columns of a thread
 constexpr int kThreads = 256;
 constexpr int kWideThreads = 1024;
+constexpr int kForwardThreads = 256 * 1536;
 // Groups of G threads, a row to each, that make a workgroup, forward and backward.
 template <int G>
 constexpr int kGroups = G < kThreads ? kThreads / G : 1;
@@ -241,16 +242,23 @@ __global__ void __launch_bounds__(G * kGroups<G>) residual_norm_kernel(Args<S> a
 {
     constexpr int R = kGroups<G>;
     __shared__ float red[2][(G * R + 63) / 64];
+    constexpr bool AHEAD = true;
     const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kEight;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * R; first < a.rows; first += static_cast<int64_t>(gridDim.x) * R) {
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * R;
+    float gamma_u[kEight], gamma_y[kEight];
+    factors(gamma_u, a.gamma_u, a.cols - c, c);
+    factors(gamma_y, a.gamma_y, a.cols - c, c);
+    Columns<S> q;
+    auto fetch = [&](int64_t r) { q.load(a, r, r < a.rows ? a.gate_of(r) : 0, c, r < a.rows ? a.cols - c : 0); };
+    if constexpr (AHEAD) fetch(static_cast<int64_t>(blockIdx.x) * R + group);
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * R; first < a.rows; first += stride) {
         const int64_t r = first + group;
         const bool in = r < a.rows;
         const int n = in ? a.cols - c : 0;
-        Columns<S> p;
-        float gamma_u[kEight], gamma_y[kEight], h[kEight], s[1] = {0.0f}, rstd = 1.0f;
-        p.load(a, r, in ? a.gate_of(r) : 0, c, n);
-        factors(gamma_u, a.gamma_u, n, c);
-        factors(gamma_y, a.gamma_y, n, c);
+        float h[kEight], s[1] = {0.0f}, rstd = 1.0f;
+        if constexpr (!AHEAD) fetch(r);
+        const Columns<S> p = q;
+        if constexpr (AHEAD) fetch(r + stride);
         if (a.norm_u) {
 #pragma unroll
             for (int e = 0; e < kEight; ++e) s[0] = __builtin_fmaf(p.u.get(e), p.u.get(e), s[0]);
@@ -740,7 +748,7 @@ dol_status forward(const Args<S> &a, int threads, hipStream_t st)
     }
     return with_threads(threads, [&](auto g) {
         constexpr int G = g.value, R = kGroups<G>;
-        residual_norm_kernel<S, G><<<static_cast<unsigned>(std::min<int64_t>((static_cast<int64_t>(a.rows) + R - 1) / R, kMostBlocks)), G * R, 0, st>>>(a);
+        residual_norm_kernel<S, G><<<static_cast<unsigned>(std::min<int64_t>((static_cast<int64_t>(a.rows) + R - 1) / R, kForwardThreads / (G * R))), G * R, 0, st>>>(a);
         DOL_HIP(hipGetLastError());
         return DOL_OK;
     });
