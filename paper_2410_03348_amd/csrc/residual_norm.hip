@@ -23,10 +23,15 @@ namespace {
 constexpr int kEight = 8;               // columns of a thread
 constexpr int kThreads = 256;
 constexpr int kWideThreads = 1024;
-constexpr int kForwardThreads = 256 * 1536;
 // Groups of G threads, a row to each, that make a workgroup, forward and backward.
 template <int G>
 constexpr int kGroups = G < kThreads ? kThreads / G : 1;
+// Wavefronts to a SIMD that the forward kernel's registers leave room for, and the workgroups of the chip that are.  More of them than that would be a second
+// round of fewer: bf16 8 192 x 4 096 59 us with four to a unit, of which three fit, 51 with three.
+template <typename S, int G>
+constexpr int kForwardWaves = sizeof(S) == 4 || G < 64 ? 5 : G <= 384 ? 7 : G <= 768 ? 6 : 4;
+template <typename S, int G>
+constexpr int kForwardBlocks = 256 * (kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) > 0 ? kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) : 1);
 template <int G>
 constexpr int kBackGroups = G <= 128 ? kThreads / G : G <= 256 ? 512 / G : 1;
 constexpr int kFewPoints = 32;          // rows to a set, below which a group takes all rows of its sets by itself
@@ -238,11 +243,10 @@ struct Columns {
 
 // Bytes bound it: bf16 8 192 x 4 096 FORWARD_FIGURE.
 template <typename S, int G>
-__global__ void __launch_bounds__(G * kGroups<G>) residual_norm_kernel(Args<S> a)
+__global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residual_norm_kernel(Args<S> a)
 {
     constexpr int R = kGroups<G>;
     __shared__ float red[2][(G * R + 63) / 64];
-    constexpr bool AHEAD = true;
     const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kEight;
     const int64_t stride = static_cast<int64_t>(gridDim.x) * R;
     float gamma_u[kEight], gamma_y[kEight];
@@ -250,15 +254,14 @@ __global__ void __launch_bounds__(G * kGroups<G>) residual_norm_kernel(Args<S> a
     factors(gamma_y, a.gamma_y, a.cols - c, c);
     Columns<S> q;
     auto fetch = [&](int64_t r) { q.load(a, r, r < a.rows ? a.gate_of(r) : 0, c, r < a.rows ? a.cols - c : 0); };
-    if constexpr (AHEAD) fetch(static_cast<int64_t>(blockIdx.x) * R + group);
+    fetch(static_cast<int64_t>(blockIdx.x) * R + group);
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * R; first < a.rows; first += stride) {
         const int64_t r = first + group;
         const bool in = r < a.rows;
         const int n = in ? a.cols - c : 0;
         float h[kEight], s[1] = {0.0f}, rstd = 1.0f;
-        if constexpr (!AHEAD) fetch(r);
         const Columns<S> p = q;
-        if constexpr (AHEAD) fetch(r + stride);
+        fetch(r + stride);
         if (a.norm_u) {
 #pragma unroll
             for (int e = 0; e < kEight; ++e) s[0] = __builtin_fmaf(p.u.get(e), p.u.get(e), s[0]);
@@ -404,12 +407,12 @@ __device__ __forceinline__ void leave_part(const float (&sum)[kEight], float *to
 }
 
 // WHOLE: a group takes all rows of its sets; else a workgroup takes a chunk of the rows of one set.
-// Bytes bound it: bf16 8 192 x 4 096 BACKWARD_FIGURE.  A row is asked for before the one ahead of it is worked on, where registers allow (bf16).
+// Bytes bound it: bf16 8 192 x 4 096 BACKWARD_FIGURE.  (With the next row asked for ahead, as forward, it has registers for one workgroup to a unit instead
+// of two: 116 us against 99.)
 template <typename S, int G, bool WHOLE>
 __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_norm_backward_kernel(Args<S> a)
 {
     constexpr int R = kBackGroups<G>;
-    constexpr bool AHEAD = false;
     __shared__ float red[2][4 * ((G * R + 63) / 64)];
     __shared__ float buf[R > 1 ? G * R * kEight : 1];
     const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kEight;
@@ -431,24 +434,17 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
     };
     auto fetch = [&](Row &q, int64_t t, int64_t k) {
         const int64_t m = mine + t * stride;
-        const bool in = WHOLE ? t < turns && m < a.sets : k < count && r0 + k * R + group < r1;
+        const bool in = WHOLE ? m < a.sets : r0 + k * R + group < r1;
         q.r = WHOLE ? m * a.points + k : r0 + k * R + group;
         q.n = in ? a.cols - c : 0;
         q.p.load(a, q.r, WHOLE ? m : a.each ? q.r : set, c, q.n);
         q.rstd_u = a.norm_u && in ? a.rstd_u[q.r] : 1.0f, q.rstd_h = a.grad_y.p && in ? a.rstd_h[q.r] : 0.0f;
     };
     int turn = 0;
-    Row q;
-    if constexpr (AHEAD) fetch(q, 0, 0);
     for (int64_t t = 0; t < turns; ++t) {
         for (int64_t k = 0; k < count; ++k) {
-            Row now, next;
-            if constexpr (AHEAD) {
-                now = q;
-                const bool last = k + 1 == count;
-                fetch(next, WHOLE && last ? t + 1 : t, WHOLE && last ? 0 : k + 1);
-            } else
-                fetch(now, t, k);
+            Row now;
+            fetch(now, t, k);
             typename Piece<S>::Factors m{a.scale * now.rstd_u, now.rstd_h, 0.0f, 0.0f};
             float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             now.p.sums(s, gamma, m.f);
@@ -457,7 +453,6 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
             m.join(s, a.norm_u, now.rstd_u, a.per_cols);
             now.p.again();
             now.p.leave(a, now.r, c, now.n, gamma, m, sum_y, sum_t);
-            if constexpr (AHEAD) q = next;
         }
         if constexpr (WHOLE) {
             const int64_t m = mine + t * stride;
@@ -748,7 +743,7 @@ dol_status forward(const Args<S> &a, int threads, hipStream_t st)
     }
     return with_threads(threads, [&](auto g) {
         constexpr int G = g.value, R = kGroups<G>;
-        residual_norm_kernel<S, G><<<static_cast<unsigned>(std::min<int64_t>((static_cast<int64_t>(a.rows) + R - 1) / R, kForwardThreads / (G * R))), G * R, 0, st>>>(a);
+        residual_norm_kernel<S, G><<<static_cast<unsigned>(std::min<int64_t>((static_cast<int64_t>(a.rows) + R - 1) / R, kForwardBlocks<S, G>)), G * R, 0, st>>>(a);
         DOL_HIP(hipGetLastError());
         return DOL_OK;
     });
