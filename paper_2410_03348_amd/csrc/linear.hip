@@ -5,7 +5,7 @@
 //
 // A tile of z stays in the registers that the matrix cores leave it in, and y (and z, where the gradients need it) is written from there.  Few
 // tiles share out their k, and a second launch adds up the shares and does the rest.  Up to 64 rows are no work for tiles: every weight is read for
-// them once, which is what bounds the call, straight from memory into the operands of the matrix cores (linear_few_kernel).
+// them once, which is what bounds the call, straight from memory into the operands of the matrix cores (linear_few_kernel, linear_few_back_kernel).
 // Backward: dz is rounded for the matrix cores and written, with its sums over rows beside it, and grad_x and grad_w are two sets of tiles
 // of one launch (mfma_products.h).
 #include "activation.h"
@@ -181,78 +181,94 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float *part, int
 
 // ---------------------------------------------------------------- few rows
 
-// Sixteen outs and 16 R rows to a workgroup, whose wavefronts share out its k.  A lane loads 32 neighbouring bytes of the row of w (l & 15) and
-// of rows of x, four lanes a line of 128; which of a product's k these are does not matter, as long as both operands agree.
-// float as it is, by v_mfma_f32_16x16x4.
-constexpr int kFewWaves = 16;
+// 16 M outs and 16 R rows to a workgroup, whose wavefronts share out its k.  A lane loads 32 neighbouring bytes of rows of w (l & 15) and of x, four
+// lanes a line of 128; which of a product's k these are does not matter, as long as both operands agree.  float as it is, by v_mfma_f32_16x16x4.
+constexpr int few_waves(int n) { return n < 8 ? 16 : 8; }       // at most, for n sums of 16 x 16, which all lie in LDS at the end
 
-template <typename S, int R>
-__global__ void __launch_bounds__(kFewWaves * 64) linear_few_kernel(const S *x, int64_t ldx, const S *w, int64_t ldw, int32_t width, int32_t each, int32_t groups, int32_t sets,
+template <typename S, int R, int M>
+__global__ void __launch_bounds__(few_waves(R * M) * 64) linear_few_kernel(const S *x, int64_t ldx, const S *w, int64_t ldw, int32_t width, int32_t each, int32_t groups, int32_t sets,
                                                                     float *part, int64_t part_ld, Result o)
 {
     constexpr int V = kLooseElements<S>, STEP = 8 * V;       // k of a step: two vectors to each of four lanes
-    __shared__ f32x4 red[kFewWaves][R][64];
+    constexpr int N = R * M, W = few_waves(N);
+    __shared__ f32x4 red[W][N][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int group = blockIdx.x % groups, set = blockIdx.x / groups % sets, split = blockIdx.x / groups / sets, row0 = set * (16 * R);
+    const int group = blockIdx.x % groups, set = blockIdx.x / groups % sets, split = blockIdx.x / groups / sets, row0 = set * (16 * R), out0 = group * (16 * M);
     const int64_t k0 = static_cast<int64_t>(split * waves + wave) * each, k1 = min(k0 + each, static_cast<int64_t>(width));
-    const S *from_w = w + min(group * 16 + (lane & 15), o.cols - 1) * ldw, *from_x[R];
-    f32x4 acc[R];
-    const int c = group * 16 + (lane >> 4) * 4;
-    const f32x4 bias = bias_of(o, c);
+    const S *from_w[M], *from_x[R];
+    f32x4 acc[M][R], bias[M];
 #pragma unroll
-    for (int r = 0; r < R; ++r) from_x[r] = x + min(row0 + r * 16 + (lane & 15), o.rows - 1) * ldx, acc[r] = f32x4{0, 0, 0, 0};
-    auto products = [&](const Loose<S> (&a)[2], const Loose<S> (&b)[R][2]) {
+    for (int m = 0; m < M; ++m) {
+        from_w[m] = w + min(out0 + m * 16 + (lane & 15), o.cols - 1) * ldw;
+        bias[m] = bias_of(o, out0 + m * 16 + (lane >> 4) * 4);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int r = 0; r < R; ++r) acc[m][r] = f32x4{0, 0, 0, 0};
+    }
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                if constexpr (sizeof(S) == 2) acc[r] = Mfma<bf16x8>::go(__builtin_bit_cast(bf16x8, a[h]), __builtin_bit_cast(bf16x8, b[r][h]), acc[r]);
-                else
+    for (int r = 0; r < R; ++r) from_x[r] = x + min(row0 + r * 16 + (lane & 15), o.rows - 1) * ldx;
+    auto products = [&](const Loose<S> (&a)[M][2], const Loose<S> (&b)[R][2]) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) acc[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(loose_get(a[h], e), loose_get(b[r][h], e), acc[r], 0, 0, 0);
-            }
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (sizeof(S) == 2) {
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int r = 0; r < R; ++r) acc[m][r] = Mfma<bf16x8>::go(__builtin_bit_cast(bf16x8, a[m][h]), __builtin_bit_cast(bf16x8, b[r][h]), acc[m][r]);
+            } else
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+#pragma unroll
+                    for (int m = 0; m < M; ++m)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) acc[m][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(loose_get(a[m][h], e), loose_get(b[r][h], e), acc[m][r], 0, 0, 0);
+        }
     };
     int64_t k = k0 + (lane >> 4) * (2 * V);
-    constexpr int U = R == 1 ? 4 : 2;
+    constexpr int U = N == 1 ? 4 : 2;
     const int64_t whole = k0 + (k1 > k0 ? (k1 - k0) / (U * STEP) * (U * STEP) : 0);
     for (int64_t at = k0; at < whole; at += U * STEP, k += U * STEP) {
-        Loose<S> a[U][2], b[U][R][2];
+        Loose<S> a[U][M][2], b[U][R][2];
 #pragma unroll
         for (int q = 0; q < U; ++q)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) a[q][h] = *reinterpret_cast<const Loose<S> *>(from_w + k + q * STEP + h * V);
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int q = 0; q < U; ++q)
+                for (int m = 0; m < M; ++m) a[q][m][h] = *reinterpret_cast<const Loose<S> *>(from_w[m] + k + q * STEP + h * V);
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) b[q][r][h] = *reinterpret_cast<const Loose<S> *>(from_x[r] + k + q * STEP + h * V);
+                for (int r = 0; r < R; ++r) b[q][r][h] = *reinterpret_cast<const Loose<S> *>(from_x[r] + k + q * STEP + h * V);
+            }
 #pragma unroll
         for (int q = 0; q < U; ++q) products(a[q], b[q]);
     }
     for (int64_t at = max(whole, k0); at < k1; at += STEP, k += STEP) {
-        Loose<S> a[2], b[R][2];
+        Loose<S> a[M][2], b[R][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int left = static_cast<int>(k1 - k) - h * V, before = static_cast<int>(k) + h * V;
-            a[h] = loose_load_end(from_w + k + h * V, left, before);
+#pragma unroll
+            for (int m = 0; m < M; ++m) a[m][h] = loose_load_end(from_w[m] + k + h * V, left, before);
 #pragma unroll
             for (int r = 0; r < R; ++r) b[r][h] = loose_load_end(from_x[r] + k + h * V, left, before);
         }
         products(a, b);
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) red[wave][r][lane] = acc[r];
-    lds_barrier();
-    for (int m = wave; m < R; m += waves) {
-        f32x4 z = red[0][m][lane];
+    for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int q = 1; q < kFewWaves; ++q)
-            if (q < waves) z += red[q][m][lane];
-        const int64_t r = row0 + m * 16 + (lane & 15);
+        for (int r = 0; r < R; ++r) red[wave][m * R + r][lane] = acc[m][r];
+    lds_barrier();
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        if (q % waves != wave) continue;
+        f32x4 z = red[0][q][lane];
+#pragma unroll
+        for (int t = 1; t < W; ++t)
+            if (t < waves) z += red[t][q][lane];
+        const int64_t r = row0 + q % R * 16 + (lane & 15);
+        const int c = out0 + q / R * 16 + (lane >> 4) * 4;
         if (r >= o.rows || c >= o.cols) continue;
         if (part) *reinterpret_cast<f32x4 *>(part + (split * static_cast<int64_t>(o.rows) + r) * part_ld + c) = z;
-        else with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, bias, z); });
+        else with_act(o.act, [&](auto a) { leave<S>(o, a, r, c, bias[q / R], z); });
     }
 }
 
@@ -273,6 +289,7 @@ struct Slope {
     const int16_t *rest;
     int32_t rows, cols, act;
     uint16_t *dz;               // null: only the sums
+    float *flat;                // dz as it is, at the same distances, where not null
     int64_t out_rows, out_cols, ld, plane;      // as they are laid out
     float *part;                // [chunks][part_cols], null: only dz
     int32_t part_cols;
@@ -343,6 +360,10 @@ __device__ __forceinline__ void slope_rows(const Slope &p, unsigned block, float
                     }
                     sum[e] += v[e];
                 }
+                if (p.flat) {
+                    *reinterpret_cast<f32x4 *>(p.flat + r * p.ld + c) = f32x4{v[0], v[1], v[2], v[3]};
+                    *reinterpret_cast<f32x4 *>(p.flat + r * p.ld + c + 4) = f32x4{v[4], v[5], v[6], v[7]};
+                }
                 if (p.dz)
 #pragma unroll
                     for (int s = 0; s < Q; ++s) {
@@ -381,6 +402,85 @@ __global__ void __launch_bounds__(256) linear_slope_kernel(Slope p, Pack x, Pack
     pack_rows<S, P>(w, block - x.blocks);
 }
 
+// grad_x of few rows: w is read once, as it lies, at any alignment.  A lane reads a vector of each of 8 (float: 4) neighbouring rows of w, which are k, and
+// exchanges their columns in registers: column j of its vector is a row of the j-th product's first operand.  dz is the second one (float: as it is, by
+// v_mfma_f32_16x16x4).  The wavefronts of a workgroup share out k.
+constexpr int kBackWaves = 8;
+
+template <typename S, int R, int Q>
+__global__ void __launch_bounds__(kBackWaves * 64) linear_few_back_kernel(const S *w, int64_t ldw, int32_t out, int32_t width, const uint16_t *dz, const float *flat, int64_t ldo,
+                                                                          int64_t plane, int32_t rows, int32_t each, int32_t groups, int32_t sets, float *part, int64_t part_ld,
+                                                                          S *grad_x, int64_t grad_ld)
+{
+    constexpr int J = kLooseElements<S>, COLS = 16 * J, STEP = 4 * J;
+    __shared__ __align__(16) float red[kBackWaves][J][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, kq = lane >> 4;
+    const int group = blockIdx.x % groups, set = blockIdx.x / groups % sets, split = blockIdx.x / groups / sets, row0 = set * (16 * R);
+    const int c = group * COLS + i * J, n = width - c;
+    const int64_t k0 = static_cast<int64_t>(split * kBackWaves + wave) * each, k1 = min(k0 + each, static_cast<int64_t>(out));
+    f32x4 acc[J][R];
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[j][r] = f32x4{0, 0, 0, 0};
+    for (int64_t k = k0; k < k1; k += STEP) {
+        Loose<S> v[J];
+        const S *from = w + (k + kq * J) * ldw + c;
+        if (k + STEP <= out && n >= J)
+#pragma unroll
+            for (int t = 0; t < J; ++t) v[t] = *reinterpret_cast<const Loose<S> *>(from + t * ldw);
+        else
+#pragma unroll
+            for (int t = 0; t < J; ++t) v[t] = loose_load_end(from + t * ldw, k + kq * J + t < out ? n : 0, c);
+        if constexpr (sizeof(S) == 2) {
+            bf16x8 b[R][Q];
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int q = 0; q < Q; ++q) b[r][q] = *reinterpret_cast<const bf16x8 *>(dz + q * plane + (row0 + r * 16 + i) * ldo + k + kq * 8);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                u32x4 f;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) f[t] = __builtin_amdgcn_perm(v[2 * t + 1].w[j / 2], v[2 * t].w[j / 2], j & 1 ? 0x07060302 : 0x05040100);
+#pragma unroll
+                for (int q = Q - 1; q >= 0; --q)
+#pragma unroll
+                    for (int r = 0; r < R; ++r) acc[j][r] = Mfma<bf16x8>::go(__builtin_bit_cast(bf16x8, f), b[r][q], acc[j][r]);
+            }
+        } else {
+            f32x4 b[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) b[r] = *reinterpret_cast<const f32x4 *>(flat + (row0 + r * 16 + i) * ldo + k + kq * 4);
+#pragma unroll
+            for (int t = 0; t < J; ++t)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int r = 0; r < R; ++r) acc[j][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(loose_get(v[t], j), b[r][t], acc[j][r], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r > 0) lds_barrier();
+#pragma unroll
+        for (int j = 0; j < J; ++j) *reinterpret_cast<f32x4 *>(&red[wave][j][lane * 4]) = acc[j][r];
+        lds_barrier();
+        // element e of lane l's sums: row l & 15 of x, columns (4 (l >> 4) + e) J .. + J - 1; a thread takes four of them
+        const int at = threadIdx.x & 255, first = threadIdx.x / 256 * 4, l = at >> 2, e = at & 3;
+        const int row = row0 + r * 16 + (l & 15), column = group * COLS + ((l >> 4) * 4 + e) * J + first;
+        if (first < J && row < rows && column < width) {
+            f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+            for (int q = 0; q < kBackWaves; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] += red[q][(first + j) % J][at];
+            if (part) *reinterpret_cast<f32x4 *>(part + (static_cast<int64_t>(split) * rows + row) * part_ld + column) = v;
+            else store4(grad_x + row * grad_ld + column, v, width - column);
+        }
+    }
+}
+
 template <typename TX, typename TW, typename O>
 __global__ void __launch_bounds__(TX::NT, 2) linear_products_kernel(Product px, Product pw)
 {
@@ -412,7 +512,15 @@ __global__ void __launch_bounds__(256) linear_zero_kernel(O *out, int64_t ld, in
 
 // ---------------------------------------------------------------- host side
 
-constexpr int32_t kMostFew = 64;            // rows that linear_few_kernel takes
+// linear_few_kernel or tiles, us: bf16 1 x 4 096 x 16 384 23 / 26, 16 x 4 096 x 4 096 11 / 12, 16 x 4 096 x 16 384 33 / 29, 32 x 4 096 x 4 096 17 / 12 (not taken);
+// float, whose tiles want their operands in planes, 16 x 4 096 x 4 096 18 / 56, 64 x 4 096 x 4 096 39 / 51, 128 x 1 509 x 12 939 113 / 79 (not taken).  Few
+// weights are launches and waits, of which it has fewer: 128 x 1 568 x 128 6 / 13, float 8 / 13, 256 x 300 x 2 000 8 / 10, float 10 / 15.
+constexpr int64_t kSmallWeights = 1 << 20;
+// linear_few_back_kernel or tiles, us of a backward pass: bf16 1 x 4 096 x 4 096 30 / 39, 16 x 1 509 x 12 939 50 / 61, 64 x 4 096 x 16 384 121 / 222, 50 x 1 509 x 12 939
+// 68 / 60, 128 x 4 096 x 4 096 54 / 45 (not taken); float 1 x 4 096 x 4 096 45 / 85, 64 x 1 509 x 12 939 111 / 127, 128 x 4 096 x 4 096 116 / 103 (not taken); few weights
+// (not taken) 16 x 1 568 x 128 14 / 12, 64 x 300 x 2 000 25 / 15.
+constexpr int32_t kMostFewBack = 64;
+constexpr int64_t kFewBackWeights = 1 << 22;
 
 // What tiles take, in elements of a result times k, some 2.35 G of which the chip does in a millisecond with one product of planes in the large tiles
 // (256 x 256; float 128 x 256, six products).  A tile takes kAround k more than it has, and two on a unit twice as long as one.  Smaller ones load more for what they multiply, by kSlower; adding up
@@ -428,7 +536,7 @@ constexpr int kProducts = P == 3 ? 6 : Q;
 
 // A forward pass.
 struct Layout {
-    int few;                                // 16 rows to a lane's R; 0: tiles
+    int few, few_outs;                      // 16 rows and outs to R and M of linear_few_kernel; 0: tiles
     int32_t waves, each, groups, sets;      // few: wavefronts of a workgroup, k of each, workgroups to outs and to rows
     int size;                               // 2, 1, 0: of the tiles
     Tiles tiles;
@@ -445,13 +553,16 @@ Layout lay_out(const dol_matrix *x, const dol_matrix *w, void *workspace)
     Carver c(workspace);
     const int32_t rows = x->rows, width = x->cols, out = w->rows;
     L.tiles.part_ld = round_up(out, 4), L.tiles.splits = 1;
-    if (rows <= kMostFew) {
-        L.groups = tiles(out, 16);
+    const int64_t weights = int64_t(out) * width;
+    if (rows <= 16 || (P == 3 && rows <= 64) || (weights <= kSmallWeights && rows <= 256)) {
         // (rows of their own for a workgroup read the weights again, which costs nothing where the chip is not full)
-        L.few = rows <= 16 || L.groups * tiles(rows, 16) <= 2 * kUnits ? 1 : rows <= 32 ? 2 : 4;
+        L.few = rows <= 16 || P == 1 || tiles(out, 16) * tiles(rows, 16) <= 2 * kUnits ? 1 : rows <= 32 ? 2 : 4;
+        L.few_outs = L.few > 1 && tiles(out, 128 / L.few) >= kUnits / 2 ? 8 / L.few : 1;
+        L.groups = tiles(out, 16 * L.few_outs);
         L.sets = tiles(rows, 16 * L.few);
         const int32_t shares = std::min(tiles(width, 128), std::max(4, 4096 / (L.groups * L.sets)));
-        L.waves = std::min(shares, kFewWaves), L.tiles.splits = tiles(shares, kFewWaves);
+        const int most = few_waves(L.few * L.few_outs);
+        L.waves = std::min(shares, most), L.tiles.splits = tiles(shares, most);
         L.each = static_cast<int32_t>(round_up(tiles(width, L.waves * L.tiles.splits), 64));
     } else {
         L.kp = round_up(width, 64), L.ldk = spread(L.kp);
@@ -481,6 +592,9 @@ struct Back {
     int64_t kp, ldk, ko, ldo, n_pad;        // width, out and rows as they are laid out
     uint16_t *xp, *wp, *dz;
     bool x_direct;
+    int few;                                // 16 rows to R of linear_few_back_kernel, 0: tiles for grad_x as for grad_w
+    int32_t few_each, few_groups, few_sets; // k of a wavefront, workgroups to columns and to rows
+    float *flat;
     int size, splits_x, splits_w;
     float *part_x, *part_w, *bias_part;
     int64_t part_ld;
@@ -500,7 +614,14 @@ Back lay_back(const dol_matrix *x, const dol_matrix *w, void *workspace)
     // (k of grad_w: rows past the last have to be zeros in both operands)
     L.x_direct = direct(x) && rows % 64 == 0;
     if (!L.x_direct) L.xp = c.take<uint16_t>(P * L.n_pad * L.ldk);
-    if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(out) * L.ldk);
+    if (rows <= kMostFewBack && int64_t(out) * width >= kFewBackWeights) {
+        constexpr int J = P == 3 ? 4 : 8;
+        L.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+        L.few_groups = tiles(width, 16 * J), L.few_sets = tiles(rows, 16 * L.few);
+        const int32_t splits = std::max(1, std::min(tiles(out, kBackWaves * 8 * J), 384 / (L.few_groups * L.few_sets)));
+        L.few_each = static_cast<int32_t>(round_up(tiles(out, kBackWaves * splits), 4 * J));
+        if (P == 3) L.flat = c.take<float>(L.n_pad * L.ldo);
+    } else if (!direct(w)) L.wp = c.take<uint16_t>(P * int64_t(out) * L.ldk);
     L.dz = c.take<uint16_t>(Q * L.n_pad * L.ldo);
     // (few rows are one chunk, whose sums are grad_bias)
     L.chunk = rows <= kOneChunk ? kOneChunk : static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>(64, round_up(tiles(L.n_pad * tiles(L.ko, 256), 1024), 8))));
@@ -510,10 +631,10 @@ Back lay_back(const dol_matrix *x, const dol_matrix *w, void *workspace)
     double best = 0.0;
     auto consider = [&](int size, auto z) {
         using T = typename decltype(z)::Tile;
-        const int64_t tx = int64_t(tiles(width, T::BM)) * tiles(rows, T::BN), tw = int64_t(tiles(width, T::BM)) * tiles(out, T::BN);
+        const int64_t tx = L.few ? 0 : int64_t(tiles(width, T::BM)) * tiles(rows, T::BN), tw = int64_t(tiles(width, T::BM)) * tiles(out, T::BN);
         const int64_t even = (tx * out + tw * rows) / kUnits;
         for (int q = 6; q <= 20; ++q) {
-            const int64_t share = std::max<int64_t>(96, even * q / 10), sx = std::max<int64_t>(1, (out + share / 2) / share), sw = std::max<int64_t>(1, (rows + share / 2) / share);
+            const int64_t share = std::max<int64_t>(96, even * q / 10), sx = L.few ? 1 : std::max<int64_t>(1, (out + share / 2) / share), sw = std::max<int64_t>(1, (rows + share / 2) / share);
             const double sums = (sx > 1 ? double(sx) * rows : 0.0) + (sw > 1 ? double(sw) * out : 0.0);
             const double all = done(tx * sx, double(out) / sx + kAround, tw * sw, double(rows) / sw + kAround, kUnits) * T::BM * T::BN * kSlower<P, Q>[size] +
                                (sums * width * kSumWeight + (sums > 0.0 && L.chunks == 1 ? kLaunchWeight : 0.0)) / kProducts<P, Q>;
@@ -521,6 +642,7 @@ Back lay_back(const dol_matrix *x, const dol_matrix *w, void *workspace)
         }
     };
     consider(2, Type<typename Z::BigX>()), consider(1, Type<typename Z::SmallX>()), consider(0, Type<typename Z::TinyX>());
+    if (L.few) L.splits_x = tiles(out, kBackWaves * L.few_each);
     if (L.splits_x > 1) L.part_x = c.take<float>(int64_t(L.splits_x) * rows * L.part_ld);
     if (L.splits_w > 1) L.part_w = c.take<float>(int64_t(L.splits_w) * out * L.part_ld);
     L.bytes = c.used;
@@ -563,16 +685,22 @@ dol_status forward(const Layout &L, const dol_matrix *x, const dol_matrix *w, co
 {
     using S = typename Source<P>::T;
     if (L.few) {
-        auto go = [&](auto r) {
-            linear_few_kernel<S, r.value><<<L.groups * L.sets * L.tiles.splits, L.waves * 64, 0, st>>>(static_cast<const S *>(x->data), x->ld, static_cast<const S *>(w->data), w->ld, x->cols,
-                                                                                           L.each, L.groups, L.sets, L.tiles.part, L.tiles.part_ld, o);
+        using std::integral_constant;
+        auto go = [&](auto r, auto m) {
+            linear_few_kernel<S, r.value, m.value><<<L.groups * L.sets * L.tiles.splits, L.waves * 64, 0, st>>>(static_cast<const S *>(x->data), x->ld, static_cast<const S *>(w->data),
+                                                                                                            w->ld, x->cols, L.each, L.groups, L.sets, L.tiles.part, L.tiles.part_ld, o);
             DOL_HIP(hipGetLastError());
             return DOL_OK;
         };
-        if (dol_status s = L.few == 1   ? go(std::integral_constant<int, 1>())
-                           : L.few == 2 ? go(std::integral_constant<int, 2>())
-                                        : go(std::integral_constant<int, 4>()))
-            return s;
+        const integral_constant<int, 1> one;
+        dol_status s = DOL_OK;
+        if (L.few == 1) s = go(one, one);
+        else if constexpr (P == 3) {
+            const integral_constant<int, 2> two;
+            const integral_constant<int, 4> four;
+            s = L.few == 2 ? L.few_outs == 1 ? go(two, one) : go(two, four) : L.few_outs == 1 ? go(four, one) : go(four, two);
+        }
+        if (s) return s;
         return launch_join<S>(L, o, st);
     }
     Planes xp, wp;
@@ -619,15 +747,15 @@ dol_status reverse(const Back &L, const dol_matrix *x, const dol_matrix *w, int 
     Planes xp{}, wp{}, dz{L.dz, L.ldo, L.n_pad * L.ldo};
     Pack lx{}, lw{};
     if (grad_w) lx = pack_of<P>(x, nullptr, nullptr, 0, L.xp, L.n_pad, L.kp, L.ldk, &xp);
-    if (grad_x) lw = pack_of<P>(w, nullptr, nullptr, 0, L.wp, w->rows, L.kp, L.ldk, &wp);
+    if (grad_x && !L.few) lw = pack_of<P>(w, nullptr, nullptr, 0, L.wp, w->rows, L.kp, L.ldk, &wp);
     // dz is grad_y itself where the tiles can read that (in one plane)
-    const bool as_it_is = Q == 1 && act == DOL_ACT_NONE && direct(grad_y) && x->rows % 64 == 0, write = !as_it_is && (grad_x || grad_w);
+    const bool as_it_is = Q == 1 && !L.few && act == DOL_ACT_NONE && direct(grad_y) && x->rows % 64 == 0, write = !as_it_is && (grad_x || grad_w);
     if (as_it_is) dz = Planes{static_cast<const uint16_t *>(grad_y->data), grad_y->ld, 0};
     Slope p{};
     if (write || grad_bias) {
         const bool narrow = L.chunks == 1;
         const int32_t wide = tiles(L.ko, narrow ? 64 : 256);
-        p = Slope{grad_y->data, z ? z->data : nullptr, grad_y->ld, z ? z->ld : 0, rest, x->rows, w->rows, act, write ? L.dz : nullptr, L.n_pad, L.ko, L.ldo, L.n_pad * L.ldo,
+        p = Slope{grad_y->data, z ? z->data : nullptr, grad_y->ld, z ? z->ld : 0, rest, x->rows, w->rows, act, write ? L.dz : nullptr, write && grad_x ? L.flat : nullptr, L.n_pad, L.ko, L.ldo, L.n_pad * L.ldo,
                   grad_bias ? L.chunks == 1 ? grad_bias : L.bias_part : nullptr, L.chunks == 1 ? w->rows : static_cast<int32_t>(L.ko), L.chunk, wide,
                   narrow, static_cast<unsigned>(wide * L.chunks)};
     }
@@ -636,7 +764,22 @@ dol_status reverse(const Back &L, const dol_matrix *x, const dol_matrix *w, int 
         DOL_HIP(hipGetLastError());
     }
     Product a{}, b{};
-    if (grad_x) {
+    Sum sx{};
+    if (grad_x && L.few) {
+        auto go = [&](auto r) {
+            // (in bf16 only ever of two planes, since these are few rows)
+            linear_few_back_kernel<S, r.value, 2><<<L.few_groups * L.few_sets * L.splits_x, kBackWaves * 64, 0, st>>>(
+                static_cast<const S *>(w->data), w->ld, w->rows, w->cols, L.dz, L.flat, L.ldo, L.n_pad * L.ldo, x->rows, L.few_each, L.few_groups, L.few_sets, L.part_x, L.part_ld,
+                static_cast<S *>(grad_x->data), grad_x->ld);
+            DOL_HIP(hipGetLastError());
+            return DOL_OK;
+        };
+        if (dol_status s = L.few == 1 ? go(std::integral_constant<int, 1>())
+                           : L.few == 2 ? go(std::integral_constant<int, 2>())
+                                        : go(std::integral_constant<int, 4>()))
+            return s;
+        if (L.part_x) sx = make_sum(L.part_x, x->rows, x->cols, L.splits_x, L.part_ld, grad_x->data, grad_x->ld);
+    } else if (grad_x) {
         a.a = wp, a.b = dz;
         a.M = x->cols, a.N = x->rows, a.wide = static_cast<int32_t>(L.kp), a.tall = x->rows, a.splits = L.splits_x, a.k = a.have = w->rows;
         a.part = L.part_x, a.part_ld = L.part_ld, a.out = grad_x->data, a.out_ld = grad_x->ld;
@@ -650,7 +793,8 @@ dol_status reverse(const Back &L, const dol_matrix *x, const dol_matrix *w, int 
                        : L.size == 1 ? launch_products<typename Z::SmallX, typename Z::SmallW, S>(a, b, st)
                                      : launch_products<typename Z::TinyX, typename Z::TinyW, S>(a, b, st))
         return s;
-    const Sum sx = sum_of(a), sw = sum_of(b), sb = grad_bias && L.chunks > 1 ? make_sum(L.bias_part, 1, w->rows, L.chunks, L.ko, grad_bias, w->rows) : Sum{};
+    if (!L.few) sx = sum_of(a);
+    const Sum sw = sum_of(b), sb = grad_bias && L.chunks > 1 ? make_sum(L.bias_part, 1, w->rows, L.chunks, L.ko, grad_bias, w->rows) : Sum{};
     const unsigned n = sx.blocks + sw.blocks + sb.blocks;
     if (n == 0) return DOL_OK;
     linear_finish_kernel<S><<<n, 256, 0, st>>>(sx, sw, sb);
@@ -717,10 +861,11 @@ const char *dol_linear_kernel(const dol_matrix *x, const dol_matrix *weight, int
         };
         if (backward) {
             const Back L = lay_back<p.value, q.value>(x, weight, nullptr);
+            if (L.few) return snprintf(name, sizeof name, "linear_few_back_kernel %d", 16 * L.few);
             return by_size(L.size, Type<typename Z::BigX>(), Type<typename Z::SmallX>(), Type<typename Z::TinyX>(), [&](auto z) { return at("linear_products_kernel", z); });
         }
         const Layout L = lay_out<p.value>(x, weight, nullptr);
-        if (L.few) return snprintf(name, sizeof name, "linear_few_kernel %d", 16 * L.few);
+        if (L.few) return snprintf(name, sizeof name, "linear_few_kernel %dx%d", 16 * L.few, 16 * L.few_outs);
         using F = Shapes<p.value, p.value>;
         return by_size(L.size, Type<typename F::Big>(), Type<typename F::Small>(), Type<typename F::Tiny>(), [&](auto z) { return at("linear_tiles_kernel", z); });
     });

@@ -34,7 +34,6 @@ template <typename S, int G>
 constexpr int kForwardBlocks = 256 * (kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) > 0 ? kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) : 1);
 template <int G>
 constexpr int kBackGroups = G <= 128 ? kThreads / G : G <= 256 ? 512 / G : 1;
-constexpr int kFewPoints = 32;          // rows to a set, below which a group takes all rows of its sets by itself
 constexpr int kUnits = 256;             // compute units of the chip
 constexpr int64_t kMostBlocks = 1 << 20;        // of a launch, which has less than 2^32 threads
 
@@ -679,7 +678,9 @@ Plan plan_of(const dol_matrix *u, const dol_matrix *gate, void *workspace)
     p.sets = gate && !p.each ? gate->rows : 1, p.points = u->rows / p.sets;
     const int groups = p.threads == 0 ? 1 : p.threads <= 128 ? kThreads / p.threads : p.threads <= 256 ? 512 / p.threads : 1;
     const int64_t most_blocks = p.threads && p.threads <= 128 ? 4 * kUnits : p.threads <= 512 ? 2 * kUnits : kUnits;
-    p.whole = p.sets > 1 && p.threads && (p.points < kFewPoints || p.sets > kMostBlocks);
+    // A set to a workgroup leaves its groups idle where it has few rows to each.  float 427 x 4 x 7 463, both ways, us, a set to a workgroup / its rows to one
+    // group, of which some take two sets: WHOLE_FIGURE.
+    p.whole = p.sets > 1 && p.threads && (p.points < 4 * groups || p.sets > kMostBlocks);
     if (p.whole) p.blocks = std::min<int64_t>((p.sets + groups - 1) / groups, most_blocks);
     else {
         const int64_t wanted = std::max<int64_t>(1, most_blocks / p.sets), most = std::max<int64_t>(1, p.points / groups);

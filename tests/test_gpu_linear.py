@@ -173,9 +173,11 @@ def test_activation_functions(dol, n, d, m, act, dtype):
 # every tile, and both sides of the rules that choose them
 TILES = [("bfloat16", 4096, 256, 4096, "256x256x64"), ("bfloat16", 4000, 700, 3900, "256x256x64"), ("bfloat16", 2000, 64, 2000, "128x128x64"), ("bfloat16", 700, 128, 700, "64x64x64"),
          ("float32", 2560, 64, 2048, "128x256x32"), ("float32", 1500, 100, 1500, "128x128x32"), ("float32", 300, 100, 300, "64x64x64"),
-         ("bfloat16", 16, 100, 100, "few_kernel 16"), ("bfloat16", 64, 100, 100, "few_kernel 16"), ("bfloat16", 17, 100, 8200, "few_kernel 32"),
-         ("bfloat16", 33, 100, 8200, "few_kernel 64"), ("float32", 1, 100, 100, "few_kernel 16"), ("float32", 50, 100, 100, "few_kernel 16"),
-         ("float32", 32, 100, 8200, "few_kernel 32"), ("float32", 64, 100, 8200, "few_kernel 64")]
+         ("bfloat16", 16, 100, 100, "few_kernel 16x16"), ("bfloat16", 256, 100, 8200, "few_kernel 16x16"), ("bfloat16", 3, 1000, 3001, "few_kernel 16x16"),
+         ("bfloat16", 17, 1000, 1100, "64x64x64"), ("bfloat16", 257, 100, 100, "64x64x64"), ("float32", 1, 100, 100, "few_kernel 16x16"),
+         ("float32", 50, 100, 100, "few_kernel 16x16"), ("float32", 64, 1000, 2500, "few_kernel 64x16"), ("float32", 33, 200, 8200, "few_kernel 64x32"),
+         ("float32", 200, 100, 2000, "few_kernel 64x16"), ("float32", 32, 300, 8200, "few_kernel 32x64"), ("float32", 17, 2000, 4100, "few_kernel 32x16"),
+         ("float32", 65, 1000, 1100, "64x64x64")]
 
 
 @pytest.mark.parametrize("dtype,n,d,m,name", TILES)
@@ -187,7 +189,10 @@ def test_forward_tiles(dol, dtype, n, d, m, name):
 
 BACK_TILES = [("bfloat16", 4096, 2048, 4096, "256x256x64"), ("bfloat16", 4000, 2048, 2048, "128x128x64"), ("bfloat16", 600, 128, 200, "64x64x64"),
               ("bfloat16", 512, 1024, 2048, "128x128x32"), ("bfloat16", 100, 100, 100, "64x64x64"),
-              ("float32", 2048, 256, 4096, "128x256x32"), ("float32", 1000, 300, 500, "128x128x32"), ("float32", 100, 100, 100, "64x64x64")]
+              ("bfloat16", 1, 2100, 2100, "few_back_kernel 16"), ("bfloat16", 16, 1509, 3003, "few_back_kernel 16"), ("bfloat16", 30, 4160, 1100, "few_back_kernel 32"),
+              ("bfloat16", 64, 130, 40000, "few_back_kernel 64"), ("bfloat16", 64, 30000, 150, "few_back_kernel 64"), ("bfloat16", 65, 2100, 2100, "128x128x32"),
+              ("float32", 3, 2100, 2100, "few_back_kernel 16"), ("float32", 17, 1509, 3003, "few_back_kernel 32"), ("float32", 50, 70, 60100, "few_back_kernel 64"),
+              ("float32", 64, 30000, 150, "few_back_kernel 64"), ("float32", 2048, 256, 4096, "128x256x32"), ("float32", 1000, 300, 500, "128x128x32"), ("float32", 100, 100, 100, "64x64x64")]
 
 
 @pytest.mark.parametrize("dtype,n,d,m,name", BACK_TILES)
@@ -338,7 +343,7 @@ def test_refusals(dol):
                        ((x, w, y), dict(z_rest=rests), "z_rest"), ((x, w, y), dict(z=z, z_rest=rests), "z_rest")):
         with pytest.raises(dol.DolError, match=why):
             dol.linear(*a, **kw)
-    big = make(100, 16, 20, torch.float32)
+    big = make(300, 16, 20, torch.float32)
     with pytest.raises(dol.DolError, match="workspace has 16 bytes"):
         dol.linear(big["x"], w, big["g"], workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(dol.DolError, match="aligned"):
