@@ -41,7 +41,12 @@ template <typename S>
 struct Mat {
     S *p;
     int64_t ld;
-    __device__ S *at(int64_t r, int c) const { return p + r * ld + c; }
+    // (a row's address is the same for the wavefronts of one row; its columns are an offset of 32 bits to it)
+    __device__ S *at(int64_t r, int c) const
+    {
+        using B = std::conditional_t<std::is_const_v<S>, const char, char>;
+        return reinterpret_cast<S *>(reinterpret_cast<B *>(p + r * ld) + static_cast<uint32_t>(c) * static_cast<uint32_t>(sizeof(S)));
+    }
 };
 
 template <typename S>
@@ -88,18 +93,17 @@ __device__ __forceinline__ void group_sums(float (&x)[N], float *red)
     for (int n = 0; n < N; ++n) x[n] = group_sum<G < 64 ? G : 64>(x[n]);
     if constexpr (G > 64) {
         constexpr int W = G / 64;
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0)
+        static_assert(W <= 16 && N <= 4, "a row of 16 lanes to a number");
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        float *mine = red + wave / W * (W * N);
+        if (lane == 0)
 #pragma unroll
-            for (int n = 0; n < N; ++n) red[wave * N + n] = x[n];
+            for (int n = 0; n < N; ++n) mine[n * W + wave % W] = x[n];
         lds_barrier();
-        const float *mine = red + wave / W * W * N;
+        // lanes 16 n .. + 15 add up the n-th (read one after the other they would take a register each)
+        const float v = group_sum<16>((lane & 15) < W && (lane >> 4) < N ? mine[(lane >> 4) * W + (lane & 15)] : 0.0f);
 #pragma unroll
-        for (int n = 0; n < N; ++n) x[n] = 0.0f;
-#pragma unroll
-        for (int w = 0; w < W; ++w)
-#pragma unroll
-            for (int n = 0; n < N; ++n) x[n] += mine[w * N + n];
+        for (int n = 0; n < N; ++n) x[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 16 * n));
     }
 }
 
@@ -384,14 +388,14 @@ __device__ __forceinline__ void spread_sums(const Args<S> &a, int64_t set, int c
 }
 
 // The sums of a workgroup's groups over their rows, in the order of the groups, to to[c].
-template <int G, int R>
-__device__ __forceinline__ void leave_part(const float (&sum)[kEight], float *to, int cols, float *buf)
+template <int G, int R, typename O>
+__device__ __forceinline__ void leave_part(const float (&sum)[kEight], O *to, int cols, float *buf)
 {
     const int lane = threadIdx.x % G, group = threadIdx.x / G;
     if constexpr (R == 1) {
 #pragma unroll
         for (int e = 0; e < kEight; ++e)
-            if (lane * kEight + e < cols) to[lane * kEight + e] = sum[e];
+            if (lane * kEight + e < cols) to[lane * kEight + e] = static_cast<O>(sum[e]);
     } else {
         lds_barrier();
 #pragma unroll
@@ -400,7 +404,7 @@ __device__ __forceinline__ void leave_part(const float (&sum)[kEight], float *to
         for (int c = threadIdx.x; c < cols; c += R * G) {
             float s = 0.0f;
             for (int g = 0; g < R; ++g) s += buf[g * G * kEight + c];
-            to[c] = s;
+            to[c] = static_cast<O>(s);
         }
     }
 }
@@ -468,7 +472,9 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
     const int64_t at = static_cast<int64_t>(blockIdx.x) * a.cols;
     if (a.part_y) leave_part<G, R>(sum_y, a.part_y + at, a.cols, buf);
     if (a.part_u) leave_part<G, R>(sum_u, a.part_u + at, a.cols, buf);
-    if (!WHOLE && a.part_gate) leave_part<G, R>(gates, a.part_gate + at, a.cols, buf);
+    if (WHOLE || a.each || !a.grad_gate.p) return;
+    if (a.part_gate) leave_part<G, R>(gates, a.part_gate + at, a.cols, buf);
+    else leave_part<G, R>(gates, a.grad_gate.at(set, 0), a.cols, buf);             // (a set is one chunk)
 }
 
 // ---------------------------------------------------------------- wide rows
@@ -578,6 +584,7 @@ __global__ void __launch_bounds__(kThreads) residual_norm_wide_map_kernel(Args<S
         if (a.part_y) a.part_y[at + e] = sum_y[e];
         if (a.part_u) a.part_u[at + e] = sum_u[e];
         if (a.part_gate) a.part_gate[at + e] = gates[e];
+        else if (!a.each && a.grad_gate.p) *a.grad_gate.at(set, c + e) = static_cast<S>(gates[e]);         // (a set is one chunk)
     }
 }
 
@@ -593,14 +600,24 @@ struct Sums {
     int32_t cols;
 };
 
-// 64 columns by 16 shares of the parts to a workgroup; a share's parts lie 16 apart.
+// 64 columns by 16 shares of the parts to a workgroup; a share's parts lie 16 apart.  Gates of few parts are a wavefront's each, behind those.
 template <typename S>
-__global__ void __launch_bounds__(1024) residual_norm_sums_kernel(Sums<S> s, int64_t jobs)
+__global__ void __launch_bounds__(1024) residual_norm_sums_kernel(Sums<S> s, int64_t shared, int64_t alone)
 {
     __shared__ float red[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t wide = (s.cols + 63) / 64;
-    for (int64_t j = blockIdx.x; j < jobs; j += gridDim.x) {
+    for (int64_t j = blockIdx.x; j < shared + (alone + 15) / 16; j += gridDim.x) {
+        if (j >= shared) {
+            const int64_t q = (j - shared) * 16 + wave, g = q / wide;
+            const int c = static_cast<int>(q % wide) * 64 + lane;
+            if (q >= alone || c >= s.cols) continue;
+            float v = 0.0f;
+#pragma unroll 4
+            for (int64_t k = 0; k < s.per_gate; ++k) v += s.part_gate[(g * s.per_gate + k) * s.cols + c];
+            *s.grad_gate.at(g, c) = static_cast<S>(v);
+            continue;
+        }
         int64_t what = j / wide;
         const int c = static_cast<int>(j % wide) * 64 + lane;
         const float *from = nullptr;
@@ -691,7 +708,7 @@ Plan plan_of(const dol_matrix *u, const dol_matrix *gate, void *workspace)
     }
     Carver c(workspace);
     p.part_y = c.take<float>(p.blocks * u->cols), p.part_u = c.take<float>(p.blocks * u->cols);
-    if (gate && !p.each && !p.whole) p.part_gate = c.take<float>(p.blocks * u->cols);
+    if (gate && !p.each && !p.whole && p.chunks > 1) p.part_gate = c.take<float>(p.blocks * u->cols);
     if (!p.threads) p.row = c.take<float2>(u->rows);
     p.bytes = c.used;
     return p;
@@ -773,9 +790,11 @@ dol_status reverse(const Plan &p, Args<S> a, float *grad_gamma_u, const dol_matr
         DOL_HIP(hipGetLastError());
     }
     const Sums<S> s{a.part_y, a.part_u, a.part_gate, grad_gamma_y, grad_gamma_u, a.grad_gate, p.blocks, p.chunks, a.cols};
-    const int64_t jobs = (a.cols + 63) / 64 * ((a.part_y != nullptr) + (a.part_u != nullptr) + (a.part_gate ? p.sets : 0));
+    const int64_t wide = (a.cols + 63) / 64, gates = a.part_gate ? p.sets : 0;
+    const bool few = p.chunks < 64;         // parts of a gate
+    const int64_t shared = wide * ((a.part_y != nullptr) + (a.part_u != nullptr) + (few ? 0 : gates)), alone = few ? wide * gates : 0, jobs = shared + (alone + 15) / 16;
     if (jobs == 0) return DOL_OK;
-    residual_norm_sums_kernel<S><<<static_cast<unsigned>(std::min(jobs, kMostBlocks)), 1024, 0, st>>>(s, jobs);
+    residual_norm_sums_kernel<S><<<static_cast<unsigned>(std::min(jobs, kMostBlocks)), 1024, 0, st>>>(s, shared, alone);
     DOL_HIP(hipGetLastError());
     return DOL_OK;
 }
