@@ -695,17 +695,18 @@ Plan plan_of(const dol_matrix *u, const dol_matrix *gate, void *workspace)
     p.sets = gate && !p.each ? gate->rows : 1, p.points = u->rows / p.sets;
     const int groups = p.threads == 0 ? 1 : p.threads <= 128 ? kThreads / p.threads : p.threads <= 256 ? 512 / p.threads : 1;
     const int64_t most_blocks = p.threads && p.threads <= 128 ? 4 * kUnits : p.threads <= 512 ? 2 * kUnits : kUnits;
-    // A set to a workgroup leaves its groups idle where it has few rows to each.  float 427 x 4 x 7 463, both ways, us, a set to a workgroup / its rows to one
-    // group, of which some take two sets: WHOLE_FIGURE.
-    p.whole = p.sets > 1 && p.threads && (p.points < 4 * groups || p.sets > kMostBlocks);
+    // As chunks of a set's rows to workgroups, or as whole sets to groups: what takes fewer rows in a row, where leaving a chunk's parts takes as long as three
+    // rows.  Both ways, us, chunks / whole: bf16 900 x 20 x 300 50 / 88, 2 000 x 30 x 300 155 / 192, 4 000 x 10 x 1 024 211 / 189, 8 000 x 40 x 96 214 / 164,
+    // 100 000 x 3 x 16 1 078 / 50, float 427 x 4 x 7 463 214 / 201, 128 x 50 x 7 463 577 / 791.
+    const int64_t wanted = std::max<int64_t>(1, most_blocks / p.sets), most = std::max<int64_t>(1, p.points / groups);
+    p.chunks = std::min(wanted, most);
+    p.chunk = (p.points + p.chunks - 1) / p.chunks;
+    p.chunks = (p.points + p.chunk - 1) / p.chunk;
+    p.blocks = p.sets * p.chunks;
+    const int64_t by_chunk = (p.blocks + most_blocks - 1) / most_blocks * ((p.chunk + groups - 1) / groups + 3);
+    const int64_t by_set = (p.sets + most_blocks * groups - 1) / (most_blocks * groups) * p.points;
+    p.whole = p.sets > 1 && p.threads && (by_set < by_chunk || p.blocks > kMostBlocks);
     if (p.whole) p.blocks = std::min<int64_t>((p.sets + groups - 1) / groups, most_blocks);
-    else {
-        const int64_t wanted = std::max<int64_t>(1, most_blocks / p.sets), most = std::max<int64_t>(1, p.points / groups);
-        p.chunks = std::min(wanted, most);
-        p.chunk = (p.points + p.chunks - 1) / p.chunks;
-        p.chunks = (p.points + p.chunk - 1) / p.chunk;
-        p.blocks = p.sets * p.chunks;
-    }
     Carver c(workspace);
     p.part_y = c.take<float>(p.blocks * u->cols), p.part_u = c.take<float>(p.blocks * u->cols);
     if (gate && !p.each && !p.whole && p.chunks > 1) p.part_gate = c.take<float>(p.blocks * u->cols);
