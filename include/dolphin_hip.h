@@ -495,12 +495,12 @@ dol_status dol_group_norm_backward(const dol_activations *x, int32_t groups, con
  *   x         [rows, width],   weight  [out, width], same type
  *   bias      device [out] or NULL
  *   residual  [rows, out] or NULL, of the type of x
- *   y         [rows, out], of the type of x; may be the residual, not x
+ *   y         [rows, out], of the type of x; may be the residual, not x or weight
  *   z         [rows, out] or NULL, of the type of x: what the gradients need where act is not DOL_ACT_NONE; not y
  *   z_rest    device [rows, out] or NULL, only with z in DOL_BF16: what rounding z has left, in steps of a float.  With it the slopes that
  *             grad_bias sums up are a float's, without it off by some 2^-9 each
  * (DOL_F32 multiplies in parts of numbers where it takes tiles (dol_linear_kernel), as grad_weight always does: an infinity in an operand
- * makes the sums that it is in NaN.)
+ * makes the sums that it is in NaN, and numbers below 2^-109 lose their last bits.)
  * At most 2^22 rows and outs and 2^20 elements of a row (else DOL_EUNSUPPORTED); at least one out of one element. */
 dol_status dol_linear_workspace(const dol_matrix *x, const dol_matrix *weight, int32_t backward, int64_t *bytes);
 /* As dol_cross_entropy_kernel: "linear_few_kernel 16x16" (rows and outs), "linear_tiles_kernel 128x128x64", backward (what grad_x is made by)
@@ -528,7 +528,7 @@ dol_status dol_linear_backward(const dol_matrix *x, const dol_matrix *weight, in
  *   gate      [gates, cols] or NULL = 1, of the type of u; gates divides rows, and row i has gate i / (rows / gates): one for all rows, one
  *             for a sample of neighbouring rows, or one for each row
  *   h, y      [rows, cols], of the type of u; either may be NULL, and either may be x or u
- *   rstd_u, rstd_h  device [rows], written where not NULL (the gradients need them)
+ *   rstd_u, rstd_h  device [rows], written where not NULL, rstd_u with norm_u and rstd_h with y (the gradients need them)
  * At least one column, and at most 2^24; numbers whose squares pass a float's range are off its definition. */
 dol_status dol_residual_norm(const dol_matrix *x, const dol_matrix *u, int32_t norm_u, const float *gamma_u, const dol_matrix *gate,
                              float scale, const float *gamma_y, float eps, const dol_matrix *h, const dol_matrix *y, float *rstd_u,

@@ -677,6 +677,9 @@ dol_status with_threads(int threads, F f)
     }
 }
 
+// Workgroups side by side of residual_norm_wide_map_kernel.
+int stripes_of(int32_t cols) { return (cols + kThreads * kEight - 1) / (kThreads * kEight); }
+
 // How the rows of a backward pass are dealt out.
 struct Plan {
     int threads;                        // to a row
@@ -694,7 +697,8 @@ Plan plan_of(const dol_matrix *u, const dol_matrix *gate, void *workspace)
     p.each = gate && gate->rows == u->rows;
     p.sets = gate && !p.each ? gate->rows : 1, p.points = u->rows / p.sets;
     const int groups = p.threads == 0 ? 1 : p.threads <= 128 ? kThreads / p.threads : p.threads <= 256 ? 512 / p.threads : 1;
-    const int64_t most_blocks = p.threads && p.threads <= 128 ? 4 * kUnits : p.threads <= 512 ? 2 * kUnits : kUnits;
+    // (rows too long for registers: as many of kThreads as lie side by side)
+    const int64_t most_blocks = !p.threads ? std::max(1, 4 * kUnits / stripes_of(u->cols)) : p.threads <= 128 ? 4 * kUnits : p.threads <= 512 ? 2 * kUnits : kUnits;
     // As chunks of a set's rows to workgroups, or as whole sets to groups: what takes fewer rows in a row, where leaving a chunk's parts takes as long as three
     // rows.  Both ways, us, chunks / whole: bf16 900 x 20 x 300 50 / 88, 2 000 x 30 x 300 155 / 192, 4 000 x 10 x 1 024 211 / 189, 8 000 x 40 x 96 214 / 164,
     // 100 000 x 3 x 16 1 078 / 50, float 427 x 4 x 7 463 214 / 201, 128 x 50 x 7 463 577 / 791.
@@ -786,7 +790,7 @@ dol_status reverse(const Plan &p, Args<S> a, float *grad_gamma_u, const dol_matr
     } else {
         residual_norm_wide_rows_kernel<S><<<static_cast<unsigned>(std::min<int64_t>(a.rows, kMostBlocks)), kWideThreads, 0, st>>>(a);
         DOL_HIP(hipGetLastError());
-        const int stripes = (a.cols + kThreads * kEight - 1) / (kThreads * kEight);
+        const int stripes = stripes_of(a.cols);
         residual_norm_wide_map_kernel<S><<<static_cast<unsigned>(p.blocks * stripes), kThreads, 0, st>>>(a, stripes);
         DOL_HIP(hipGetLastError());
     }
@@ -822,6 +826,7 @@ dol_status dol_residual_norm(const dol_matrix *x, const dol_matrix *u, int32_t n
     for (const auto &m : {std::make_pair(x, "x"), std::make_pair(h, "h"), std::make_pair(y, "y")})
         if (dol_status s = check_like(m.first, u, m.second)) return s;
     if (!h && !y) return fail(DOL_EINVAL, "neither h nor y is asked for");
+    if (on_top(h, y) || on_top(h, gate) || on_top(y, gate)) return fail(DOL_EINVAL, "two of h, y and gate are the same");
     if (gamma_u && !norm_u) return fail(DOL_EINVAL, "gamma_u without norm_u");
     if (!(eps >= 0.0f)) return fail(DOL_EINVAL, "eps = %g is not a number of at least 0", static_cast<double>(eps));
     if (u->rows == 0) return DOL_OK;
@@ -859,7 +864,10 @@ dol_status dol_residual_norm_backward(const dol_matrix *x, const dol_matrix *u, 
         if (grad_gate->dtype != u->dtype) return fail(DOL_EINVAL, "grad_gate is of another type than u");
         if (grad_gate->rows != gate->rows || grad_gate->cols != gate->cols)
             return fail(DOL_ESHAPE, "grad_gate is %d x %d, not %d x %d", grad_gate->rows, grad_gate->cols, gate->rows, gate->cols);
+        for (const dol_matrix *m : {x, u, gate, grad_h, grad_y, grad_x, grad_u})
+            if (on_top(grad_gate, m)) return fail(DOL_EINVAL, "grad_gate is another operand's or result's memory");
     }
+    if (on_top(grad_x, grad_u) || on_top(grad_x, gate) || on_top(grad_u, gate)) return fail(DOL_EINVAL, "two of grad_x, grad_u and gate are the same");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (u->rows == 0) {                     // sums over nothing
         if (grad_gate && grad_gate->rows > 0) return fail(DOL_ESHAPE, "%d gates for no rows", grad_gate->rows);

@@ -92,3 +92,29 @@ def test_linear_workspace(rows, width, out, dtype, backward):
     n = dol._native.linear_workspace(matrix(rows, width, dtype), matrix(out, width, dtype), backward)
     assert 0 <= n < 1 << 36 and n % 256 == 0
     assert n == dol._native.linear_workspace(matrix(rows, width, dtype), matrix(out, width, dtype), backward)
+
+
+def at(k, rows, cols):
+    return matrix(rows, cols, data=4096 * k)
+
+
+def test_linear_refuses_results_on_operands():
+    x, w, r, y, z = at(1, 8, 4), at(2, 4, 4), at(3, 8, 4), at(4, 8, 4), at(5, 8, 4)
+    for y_, z_ in ((x, z), (at(2, 8, 4), z), (z, z), (y, x), (y, at(2, 8, 4)), (y, r)):
+        with pytest.raises(dol.DolError, match="y is x|z is x"):
+            dol._native.linear(x, w, None, 2, r, y_, z_, None, None, 0, 0)
+    g, gw = at(4, 8, 4), at(6, 4, 4)
+    for gx_, gw_ in ((x, gw), (at(2, 8, 4), gw), (z, gw), (y, gw), (at(7, 8, 4), w), (at(7, 8, 4), at(1, 4, 4)), (at(6, 8, 4), gw)):
+        with pytest.raises(dol.DolError, match="grad_x"):
+            dol._native.linear_backward(x, w, 2, z, None, g, gx_, gw_, None, None, 0, 0)
+
+
+def test_residual_norm_refuses_results_on_each_other_and_on_gates():
+    x, u, gate, h, y = (at(k, 8, 16) for k in range(1, 6))
+    for h_, y_ in ((h, h), (gate, y), (h, gate)):
+        with pytest.raises(dol.DolError, match="the same"):
+            dol._native.residual_norm(x, u, 0, None, gate, 1.0, None, 1e-6, h_, y_, None, None, 0)
+    gx, gu, gg = (at(k, 8, 16) for k in range(6, 9))
+    for gx_, gu_, gg_ in ((gx, gx, gg), (gate, gu, gg), (gx, gate, gg), (gx, gu, gate), (gx, gu, gx), (gx, gu, x), (gx, gu, h)):
+        with pytest.raises(dol.DolError, match="the same|grad_gate is"):
+            dol._native.residual_norm_backward(x, u, 0, None, gate, 1.0, None, None, 4096, h, y, gx_, gu_, None, gg_, None, None, 0, 0)
