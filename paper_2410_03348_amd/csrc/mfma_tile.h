@@ -1,4 +1,5 @@
-// Tiles of matrix products on the matrix cores, for the operators that are made of them (cross_entropy.hip, newton_schulz.hip).
+// Tiles of matrix products on the matrix cores, for the operators that are made of them (cross_entropy.hip, newton_schulz.hip,
+// linear.hip).
 //
 // C[m, n] = sum_k A[m, k] * B[n, k], both operands row-major with k contiguous ("planes" of 16-bit elements), sums in 32 bits.
 // A number that 16 bits do not hold is the sum of up to three planes, and a product of such numbers the products of their

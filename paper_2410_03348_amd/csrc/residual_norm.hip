@@ -20,7 +20,11 @@
 namespace dol {
 namespace {
 
-constexpr int kEight = 8;               // columns of a thread
+constexpr int kEight = 8;               // columns of a thread: one vector of bf16, or two of float
+// Columns from one of a thread's vectors to the next in a row of G threads: each load is of neighbouring vectors (of float, whose vectors in a thread
+// side by side leave half of every line to the next load: 8 192 x 2 048 forward 73 us, 56 so, backward 95 and 88).
+template <typename S, int G>
+constexpr int kApart = sizeof(S) == 4 ? 4 * G : 4;
 constexpr int kThreads = 256;
 constexpr int kWideThreads = 1024;
 // Groups of G threads, a row to each, that make a workgroup, forward and backward.
@@ -107,21 +111,22 @@ __device__ __forceinline__ void group_sums(float (&x)[N], float *red)
     }
 }
 
-// Eight neighbouring elements as memory has them.
-template <typename S>
+// A thread's eight elements as memory has them, vectors D apart.
+template <typename S, int D>
 struct Eight {
-    static constexpr int V = kLooseElements<S>, H = kEight / V;
+    static constexpr int V = kLooseElements<S>, H = kEight / V, kSpan = (H - 1) * D + V;
+    static constexpr int column(int e) { return e / V * D + e % V; }
     Loose<S> v[H];
     __device__ void all(const S *p)
     {
 #pragma unroll
-        for (int h = 0; h < H; ++h) v[h] = *reinterpret_cast<const Loose<S> *>(p + h * V);
+        for (int h = 0; h < H; ++h) v[h] = *reinterpret_cast<const Loose<S> *>(p + h * D);
     }
-    // the first n of them, column c and its neighbours, zeros behind
+    // those of them that are in the n columns from column c on, zeros behind
     __device__ void some(const S *p, int n, int c)
     {
 #pragma unroll
-        for (int h = 0; h < H; ++h) v[h] = loose_load_end(p + h * V, n - h * V, c + h * V);
+        for (int h = 0; h < H; ++h) v[h] = loose_load_end(p + h * D, n - h * D, c + h * D);
     }
     // `other` in all of them, where there is no tensor (and what was loaded for it is another's)
     __device__ void only(bool given, float other)
@@ -142,7 +147,7 @@ struct Eight {
     __device__ void store(S *p, int n) const
     {
 #pragma unroll
-        for (int h = 0; h < H; ++h) loose_store(p + h * V, v[h], n - h * V);
+        for (int h = 0; h < H; ++h) loose_store(p + h * D, v[h], n - h * D);
     }
     // Nothing that was computed of it before is kept for what comes after: unpacked it would take two to four times its registers.
     __device__ void again()
@@ -158,7 +163,7 @@ struct Eight {
     }
 };
 
-template <typename S>
+template <int D, typename S>
 __device__ __forceinline__ void put(S *p, const float (&x)[kEight], int n)
 {
     constexpr int V = kLooseElements<S>;
@@ -169,17 +174,18 @@ __device__ __forceinline__ void put(S *p, const float (&x)[kEight], int n)
         for (int e = 0; e < V; ++e) part[e] = x[h * V + e];
         Loose<S> v;
         loose_set(v, part);
-        loose_store(p + h * V, v, n - h * V);
+        loose_store(p + h * D, v, n - h * D);
     }
 }
 
 // Factors of eight columns, 1 where there are none.
+template <int D>
 __device__ __forceinline__ void factors(float (&x)[kEight], const float *p, int n, int c)
 {
 #pragma unroll
     for (int e = 0; e < kEight; ++e) x[e] = 1.0f;
     if (!p) return;
-    Eight<float> v;
+    Eight<float, D> v;
     v.some(p + c, n, c);
 #pragma unroll
     for (int e = 0; e < kEight; ++e) x[e] = v.get(e);
@@ -189,30 +195,31 @@ __device__ __forceinline__ float rms(float squares, float per_cols, float eps) {
 
 // Both factors of a thread's eight columns, in registers, or (G threads to a row) in LDS: beside three sums over rows and a row of five tensors there are
 // no registers left for them.
+template <int D>
 struct InRegisters {
     float u[kEight], y[kEight];
     template <typename S>
     __device__ InRegisters(const Args<S> &a, int c, int n, void *)
     {
-        factors(u, a.gamma_u, n, c);
-        factors(y, a.gamma_y, n, c);
+        factors<D>(u, a.gamma_u, n, c);
+        factors<D>(y, a.gamma_y, n, c);
     }
     __device__ void get(int k, float (&gu)[2], float (&gy)[2]) const { gu[0] = u[2 * k], gu[1] = u[2 * k + 1], gy[0] = y[2 * k], gy[1] = y[2 * k + 1]; }
 };
 
-template <int G>
+template <int G, int D>
 struct InLds {
     struct alignas(16) Pair { float u[2], y[2]; };
     const Pair *at;             // [4][G]: a wavefront's reads are next to each other
     template <typename S>
-    __device__ InLds(const Args<S> &a, int c, int n, void *lds) : at(static_cast<const Pair *>(lds) + c / kEight)
+    __device__ InLds(const Args<S> &a, int c, int n, void *lds) : at(static_cast<const Pair *>(lds) + c / kLooseElements<S>)
     {
         float u[kEight], y[kEight];
-        factors(u, a.gamma_u, n, c);
-        factors(y, a.gamma_y, n, c);
+        factors<D>(u, a.gamma_u, n, c);
+        factors<D>(y, a.gamma_y, n, c);
         // (the groups of a workgroup write the same)
 #pragma unroll
-        for (int k = 0; k < kEight / 2; ++k) static_cast<Pair *>(lds)[k * G + c / kEight] = Pair{{u[2 * k], u[2 * k + 1]}, {y[2 * k], y[2 * k + 1]}};
+        for (int k = 0; k < kEight / 2; ++k) static_cast<Pair *>(lds)[k * G + c / kLooseElements<S>] = Pair{{u[2 * k], u[2 * k + 1]}, {y[2 * k], y[2 * k + 1]}};
         lds_barrier();
     }
     __device__ void get(int k, float (&gu)[2], float (&gy)[2]) const
@@ -226,14 +233,14 @@ template <int G>
 constexpr int kGammaLds = G >= 64 ? 2 * G * kEight * 4 : 0;
 
 // What a row's eight columns are read for.
-template <typename S>
+template <typename S, int D>
 struct Columns {
-    Eight<S> x, u, gate;
+    Eight<S, D> x, u, gate;
     // (one branch for all of them, and none for a tensor that is not there: a load behind a branch of its own is waited for at its end)
     __device__ void load(const Args<S> &a, int64_t r, int64_t g, int c, int n)
     {
         const S *pu = a.u.at(r, c), *px = a.x.p ? a.x.at(r, c) : pu, *pg = a.gate.p ? a.gate.at(g, c) : pu;
-        if (n >= kEight) x.all(px), u.all(pu), gate.all(pg);
+        if (n >= Eight<S, D>::kSpan) x.all(px), u.all(pu), gate.all(pg);
         else x.some(px, n, c), u.some(pu, n, c), gate.some(pg, n, c);
         x.only(a.x.p, 0.0f), gate.only(a.gate.p, 1.0f);
     }
@@ -244,18 +251,18 @@ struct Columns {
 
 // ---------------------------------------------------------------- forward
 
-// Bytes bound it: bf16 8 192 x 4 096 FORWARD_FIGURE.
+// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 51 us, 5.3 TB/s.
 template <typename S, int G>
 __global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residual_norm_kernel(Args<S> a)
 {
-    constexpr int R = kGroups<G>;
+    constexpr int R = kGroups<G>, D = kApart<S, G>;
     __shared__ float red[2][(G * R + 63) / 64];
-    const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kEight;
+    const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kLooseElements<S>;
     const int64_t stride = static_cast<int64_t>(gridDim.x) * R;
     float gamma_u[kEight], gamma_y[kEight];
-    factors(gamma_u, a.gamma_u, a.cols - c, c);
-    factors(gamma_y, a.gamma_y, a.cols - c, c);
-    Columns<S> q;
+    factors<D>(gamma_u, a.gamma_u, a.cols - c, c);
+    factors<D>(gamma_y, a.gamma_y, a.cols - c, c);
+    Columns<S, D> q;
     auto fetch = [&](int64_t r) { q.load(a, r, r < a.rows ? a.gate_of(r) : 0, c, r < a.rows ? a.cols - c : 0); };
     fetch(static_cast<int64_t>(blockIdx.x) * R + group);
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * R; first < a.rows; first += stride) {
@@ -263,7 +270,7 @@ __global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residua
         const bool in = r < a.rows;
         const int n = in ? a.cols - c : 0;
         float h[kEight], s[1] = {0.0f}, rstd = 1.0f;
-        const Columns<S> p = q;
+        const Columns<S, D> p = q;
         fetch(r + stride);
         if (a.norm_u) {
 #pragma unroll
@@ -279,14 +286,14 @@ __global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residua
             h[e] = p.stream(e, gamma_u[e], f);
             s[0] = __builtin_fmaf(h[e], h[e], s[0]);
         }
-        if (a.out_h.p && n > 0) put(a.out_h.at(r, c), h, n);
+        if (a.out_h.p && n > 0) put<D>(a.out_h.at(r, c), h, n);
         if (a.out_y.p) {
             group_sums<G, 1>(s, red[1]);
             rstd = rms(s[0], a.per_cols, a.eps);
             if (a.rstd_h && in && lane == 0) a.rstd_h[r] = rstd;
 #pragma unroll
             for (int e = 0; e < kEight; ++e) h[e] = h[e] * rstd * gamma_y[e];
-            if (n > 0) put(a.out_y.at(r, c), h, n);
+            if (n > 0) put<D>(a.out_y.at(r, c), h, n);
         }
         if constexpr (G > 64) lds_barrier();            // (red is written again)
     }
@@ -295,15 +302,15 @@ __global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residua
 // ---------------------------------------------------------------- backward
 
 // Eight columns of a row.  h is made again from x and u: as it was rounded to bf16 it would be off by 2^-9 in every term of grad_gamma_y.
-template <typename S>
+template <typename S, int D>
 struct Piece {
-    Columns<S> p;
-    Eight<S> gy, gh;
+    Columns<S, D> p;
+    Eight<S, D> gy, gh;
     __device__ void load(const Args<S> &a, int64_t r, int64_t g, int c, int n)
     {
         const S *pu = a.u.at(r, c), *px = a.x.p ? a.x.at(r, c) : pu, *pg = a.gate.p ? a.gate.at(g, c) : pu;
         const S *py = a.grad_y.p ? a.grad_y.at(r, c) : pu, *ph = a.grad_h.p ? a.grad_h.at(r, c) : pu;
-        if (n >= kEight) p.x.all(px), p.u.all(pu), p.gate.all(pg), gy.all(py), gh.all(ph);
+        if (n >= Eight<S, D>::kSpan) p.x.all(px), p.u.all(pu), p.gate.all(pg), gy.all(py), gh.all(ph);
         else p.x.some(px, n, c), p.u.some(pu, n, c), p.gate.some(pg, n, c), gy.some(py, n, c), gh.some(ph, n, c);
         p.x.only(a.x.p, 0.0f), p.gate.only(a.gate.p, 1.0f), gy.only(a.grad_y.p, 0.0f), gh.only(a.grad_h.p, 0.0f);
     }
@@ -342,7 +349,7 @@ struct Piece {
     template <typename F>
     __device__ void leave(const Args<S> &a, int64_t r, int c, int n, const F &gamma, const Factors &m, float (&sum_y)[kEight], float (&sum_t)[kEight]) const
     {
-        Eight<S> ox, ou, og;
+        Eight<S, D> ox, ou, og;
 #pragma unroll
         for (int k = 0; k < kEight / 2; ++k) {
             float dh[2], du[2], dg[2], gamma_u[2], gamma_y[2];
@@ -369,10 +376,10 @@ struct Piece {
 };
 
 // Of a set's sums of scale dh uhat: grad_gate's, times gamma_u, and grad_gamma_u's, times the gate (which a row of its own has multiplied already).
-template <typename S, typename F>
+template <int D, typename S, typename F>
 __device__ __forceinline__ void spread_sums(const Args<S> &a, int64_t set, int c, const F &gamma, const float (&sum_t)[kEight], float (&to_gate)[kEight], float (&to_u)[kEight])
 {
-    Eight<S> gate{};
+    Eight<S, D> gate{};
     const bool given = a.gate.p && !a.each;
     if (given) gate.some(a.gate.at(set, c), a.cols - c, c);
 #pragma unroll
@@ -388,18 +395,19 @@ __device__ __forceinline__ void spread_sums(const Args<S> &a, int64_t set, int c
 }
 
 // The sums of a workgroup's groups over their rows, in the order of the groups, to to[c].
-template <int G, int R, typename O>
+template <typename S, int G, int R, typename O>
 __device__ __forceinline__ void leave_part(const float (&sum)[kEight], O *to, int cols, float *buf)
 {
-    const int lane = threadIdx.x % G, group = threadIdx.x / G;
+    using E = Eight<S, kApart<S, G>>;
+    const int first = threadIdx.x % G * E::V, group = threadIdx.x / G;
     if constexpr (R == 1) {
 #pragma unroll
         for (int e = 0; e < kEight; ++e)
-            if (lane * kEight + e < cols) to[lane * kEight + e] = static_cast<O>(sum[e]);
+            if (first + E::column(e) < cols) to[first + E::column(e)] = static_cast<O>(sum[e]);
     } else {
         lds_barrier();
 #pragma unroll
-        for (int e = 0; e < kEight; ++e) buf[(group * G + lane) * kEight + e] = sum[e];
+        for (int e = 0; e < kEight; ++e) buf[group * G * kEight + first + E::column(e)] = sum[e];
         lds_barrier();
         for (int c = threadIdx.x; c < cols; c += R * G) {
             float s = 0.0f;
@@ -410,27 +418,27 @@ __device__ __forceinline__ void leave_part(const float (&sum)[kEight], O *to, in
 }
 
 // WHOLE: a group takes all rows of its sets; else a workgroup takes a chunk of the rows of one set.
-// Bytes bound it: bf16 8 192 x 4 096 BACKWARD_FIGURE.  (With the next row asked for ahead, as forward, it has registers for one workgroup to a unit instead
+// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 100 us, 4.0 TB/s.  (With the next row asked for ahead, as forward, it has registers for one workgroup to a unit instead
 // of two: 116 us against 99.)
 template <typename S, int G, bool WHOLE>
 __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_norm_backward_kernel(Args<S> a)
 {
-    constexpr int R = kBackGroups<G>;
+    constexpr int R = kBackGroups<G>, D = kApart<S, G>;
     __shared__ float red[2][4 * ((G * R + 63) / 64)];
     __shared__ float buf[R > 1 ? G * R * kEight : 1];
-    const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kEight;
+    const int lane = threadIdx.x % G, group = group_of<G>(), c = lane * kLooseElements<S>;
     // rows of this group: `count` of each of `turns` sets (WHOLE), or `count` of the chunk, R apart
     const int64_t set = WHOLE ? 0 : blockIdx.x / static_cast<unsigned>(a.chunks);
     const int64_t r0 = WHOLE ? 0 : set * a.points + (blockIdx.x - set * a.chunks) * a.chunk, r1 = WHOLE ? 0 : min(r0 + a.chunk, (set + 1) * a.points);
     const int64_t stride = static_cast<int64_t>(gridDim.x) * R, mine = static_cast<int64_t>(blockIdx.x) * R + group;
     const int64_t turns = WHOLE ? (a.sets + stride - 1) / stride : 1, count = WHOLE ? a.points : (r1 - r0 + R - 1) / R;
     extern __shared__ __align__(16) char gammas[];
-    const std::conditional_t<(kGammaLds<G> > 0), InLds<G>, InRegisters> gamma(a, c, a.cols - c, gammas);
+    const std::conditional_t<(kGammaLds<G> > 0), InLds<G, D>, InRegisters<D>> gamma(a, c, a.cols - c, gammas);
     float sum_y[kEight], sum_t[kEight], sum_u[kEight], gates[kEight];
 #pragma unroll
     for (int e = 0; e < kEight; ++e) sum_y[e] = sum_t[e] = sum_u[e] = 0.0f;
     struct Row {
-        Piece<S> p;
+        Piece<S, D> p;
         int64_t r;
         int n;
         float rstd_u, rstd_h;
@@ -448,7 +456,7 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
         for (int64_t k = 0; k < count; ++k) {
             Row now;
             fetch(now, t, k);
-            typename Piece<S>::Factors m{a.scale * now.rstd_u, now.rstd_h, 0.0f, 0.0f};
+            typename Piece<S, D>::Factors m{a.scale * now.rstd_u, now.rstd_h, 0.0f, 0.0f};
             float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             now.p.sums(s, gamma, m.f);
             group_sums<G, 4>(s, red[turn]);
@@ -461,20 +469,20 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
             const int64_t m = mine + t * stride;
             if (m < a.sets) {
                 float to_u[kEight];
-                spread_sums(a, m, c, gamma, sum_t, gates, to_u);
-                if (a.grad_gate.p && c < a.cols) put(a.grad_gate.at(m, c), gates, a.cols - c);
+                spread_sums<D>(a, m, c, gamma, sum_t, gates, to_u);
+                if (a.grad_gate.p && c < a.cols) put<D>(a.grad_gate.at(m, c), gates, a.cols - c);
 #pragma unroll
                 for (int e = 0; e < kEight; ++e) sum_u[e] += to_u[e], sum_t[e] = 0.0f;
             }
         }
     }
-    if constexpr (!WHOLE) spread_sums(a, set, c, gamma, sum_t, gates, sum_u);
+    if constexpr (!WHOLE) spread_sums<D>(a, set, c, gamma, sum_t, gates, sum_u);
     const int64_t at = static_cast<int64_t>(blockIdx.x) * a.cols;
-    if (a.part_y) leave_part<G, R>(sum_y, a.part_y + at, a.cols, buf);
-    if (a.part_u) leave_part<G, R>(sum_u, a.part_u + at, a.cols, buf);
+    if (a.part_y) leave_part<S, G, R>(sum_y, a.part_y + at, a.cols, buf);
+    if (a.part_u) leave_part<S, G, R>(sum_u, a.part_u + at, a.cols, buf);
     if (WHOLE || a.each || !a.grad_gate.p) return;
-    if (a.part_gate) leave_part<G, R>(gates, a.part_gate + at, a.cols, buf);
-    else leave_part<G, R>(gates, a.grad_gate.at(set, 0), a.cols, buf);             // (a set is one chunk)
+    if (a.part_gate) leave_part<S, G, R>(gates, a.part_gate + at, a.cols, buf);
+    else leave_part<S, G, R>(gates, a.grad_gate.at(set, 0), a.cols, buf);             // (a set is one chunk)
 }
 
 // ---------------------------------------------------------------- wide rows
@@ -483,21 +491,22 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
 template <typename S>
 __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S> a)
 {
+    constexpr int D = kApart<S, kWideThreads>, V = kLooseElements<S>;
     __shared__ float red[2][kWideThreads / 64];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const int64_t g = a.gate_of(r);
         float rstd_u = 1.0f, rstd_h = 0.0f, s[1] = {0.0f};
         auto stream = [&](int c, int n, float (&h)[kEight]) {
-            Columns<S> p;
+            Columns<S, D> p;
             float gamma_u[kEight];
             p.load(a, r, g, c, n);
-            factors(gamma_u, a.gamma_u, n, c);
+            factors<D>(gamma_u, a.gamma_u, n, c);
 #pragma unroll
             for (int e = 0; e < kEight; ++e) h[e] = p.stream(e, gamma_u[e], a.scale * rstd_u);
         };
         if (a.norm_u) {
-            for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
-                Eight<S> u;
+            for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * kEight) {
+                Eight<S, D> u;
                 u.some(a.u.at(r, c), a.cols - c, c);
 #pragma unroll
                 for (int e = 0; e < kEight; ++e) s[0] = __builtin_fmaf(u.get(e), u.get(e), s[0]);
@@ -507,7 +516,7 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S
             s[0] = 0.0f;
         }
         if (a.out_y.p) {
-            for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
+            for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * kEight) {
                 float h[kEight];
                 stream(c, a.cols - c, h);
 #pragma unroll
@@ -520,16 +529,16 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S
             if (a.norm_u && a.rstd_u) a.rstd_u[r] = rstd_u;
             if (a.out_y.p && a.rstd_h) a.rstd_h[r] = rstd_h;
         }
-        for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
+        for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * kEight) {
             const int n = a.cols - c;
             float h[kEight], gamma_y[kEight];
             stream(c, n, h);
-            if (a.out_h.p) put(a.out_h.at(r, c), h, n);
+            if (a.out_h.p) put<D>(a.out_h.at(r, c), h, n);
             if (!a.out_y.p) continue;
-            factors(gamma_y, a.gamma_y, n, c);
+            factors<D>(gamma_y, a.gamma_y, n, c);
 #pragma unroll
             for (int e = 0; e < kEight; ++e) h[e] = h[e] * rstd_h * gamma_y[e];
-            put(a.out_y.at(r, c), h, n);
+            put<D>(a.out_y.at(r, c), h, n);
         }
         lds_barrier();          // (red is written again)
     }
@@ -539,17 +548,18 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S
 template <typename S>
 __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_rows_kernel(Args<S> a)
 {
+    constexpr int D = kApart<S, kWideThreads>, V = kLooseElements<S>;
     __shared__ float red[4 * (kWideThreads / 64)];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const int64_t g = a.gate_of(r);
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
-        typename Piece<S>::Factors m{a.scale * rstd_u, rstd_h, 0.0f, 0.0f};
+        typename Piece<S, D>::Factors m{a.scale * rstd_u, rstd_h, 0.0f, 0.0f};
         float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int c = threadIdx.x * kEight; c < a.cols; c += kWideThreads * kEight) {
+        for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * kEight) {
             const int n = a.cols - c;
-            Piece<S> p;
+            Piece<S, D> p;
             p.load(a, r, g, c, n);
-            p.sums(s, InRegisters(a, c, n, nullptr), m.f);
+            p.sums(s, InRegisters<D>(a, c, n, nullptr), m.f);
         }
         group_sums<kWideThreads, 4>(s, red);
         m.join(s, a.norm_u, rstd_u, a.per_cols);
@@ -562,29 +572,31 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_rows_kernel(A
 template <typename S>
 __global__ void __launch_bounds__(kThreads) residual_norm_wide_map_kernel(Args<S> a, int stripes)
 {
+    constexpr int D = kApart<S, kThreads>;
     const int64_t block = blockIdx.x / stripes, set = block / a.chunks, r0 = set * a.points + block % a.chunks * a.chunk, r1 = min(r0 + a.chunk, (set + 1) * a.points);
-    const int c = (static_cast<int>(blockIdx.x % stripes) * kThreads + threadIdx.x) * kEight, n = a.cols - c;
+    const int c = static_cast<int>(blockIdx.x % stripes) * (kThreads * kEight) + threadIdx.x * kLooseElements<S>, n = a.cols - c;
     if (n <= 0) return;
-    const InRegisters gamma(a, c, n, nullptr);
+    const InRegisters<D> gamma(a, c, n, nullptr);
     float sum_y[kEight], sum_t[kEight], sum_u[kEight], gates[kEight];
 #pragma unroll
     for (int e = 0; e < kEight; ++e) sum_y[e] = sum_t[e] = 0.0f;
     for (int64_t r = r0; r < r1; ++r) {
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
         const float2 m = a.row[r];
-        Piece<S> p;
+        Piece<S, D> p;
         p.load(a, r, a.each ? r : set, c, n);
         p.leave(a, r, c, n, gamma, {a.scale * rstd_u, rstd_h, m.x, m.y}, sum_y, sum_t);
     }
-    spread_sums(a, set, c, gamma, sum_t, gates, sum_u);
+    spread_sums<D>(a, set, c, gamma, sum_t, gates, sum_u);
     const int64_t at = block * a.cols + c;
 #pragma unroll
     for (int e = 0; e < kEight; ++e) {
-        if (e >= n) break;
-        if (a.part_y) a.part_y[at + e] = sum_y[e];
-        if (a.part_u) a.part_u[at + e] = sum_u[e];
-        if (a.part_gate) a.part_gate[at + e] = gates[e];
-        else if (!a.each && a.grad_gate.p) *a.grad_gate.at(set, c + e) = static_cast<S>(gates[e]);         // (a set is one chunk)
+        const int k = Eight<S, D>::column(e);
+        if (k >= n) break;
+        if (a.part_y) a.part_y[at + k] = sum_y[e];
+        if (a.part_u) a.part_u[at + k] = sum_u[e];
+        if (a.part_gate) a.part_gate[at + k] = gates[e];
+        else if (!a.each && a.grad_gate.p) *a.grad_gate.at(set, c + k) = static_cast<S>(gates[e]);         // (a set is one chunk)
     }
 }
 
