@@ -36,8 +36,13 @@ template <typename S, int G>
 constexpr int kForwardWaves = sizeof(S) == 4 || G < 64 ? 5 : G <= 384 ? 7 : G <= 768 ? 6 : 4;
 template <typename S, int G>
 constexpr int kForwardBlocks = 256 * (kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) > 0 ? kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) : 1);
+// Backward fewer workgroups leave fewer parts, but a set of few rows leaves most of a large one idle.  Both ways, us, four to a unit / two / one: bf16 39 574 x 361
+// 112 / 109 / 106, but 900 x 20 x 300 with a gate to each sample 50 / - / 70, float 31 360 x 32 20 / 25 / 27, bf16 16 384 x 1 000 83 / 78 / 81; two / one: bf16
+// 8 192 x 1 500 84 / 80, 8 192 x 4 096 154 / 149.
+constexpr int back_groups(int threads) { return threads == 0 ? 1 : threads <= 64 ? kThreads / threads : threads == 128 ? 4 : 1024 / threads; }
+constexpr int back_blocks(int threads) { return threads <= 64 ? 4 : threads == 128 ? 2 : 1; }    // to a unit
 template <int G>
-constexpr int kBackGroups = G <= 128 ? kThreads / G : G <= 256 ? 512 / G : 1;
+constexpr int kBackGroups = back_groups(G);
 constexpr int kUnits = 256;             // compute units of the chip
 constexpr int64_t kMostBlocks = 1 << 20;        // of a launch, which has less than 2^32 threads
 
@@ -418,8 +423,8 @@ __device__ __forceinline__ void leave_part(const float (&sum)[kEight], O *to, in
 }
 
 // WHOLE: a group takes all rows of its sets; else a workgroup takes a chunk of the rows of one set.
-// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 100 us, 4.0 TB/s.  (With the next row asked for ahead, as forward, it has registers for one workgroup to a unit instead
-// of two: 116 us against 99.)
+// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 98 us, 4.1 TB/s.  (With the next row asked for ahead, as forward, it has registers for one row on a
+// unit at a time instead of two: 116 us against 99.)
 template <typename S, int G, bool WHOLE>
 __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_norm_backward_kernel(Args<S> a)
 {
@@ -708,12 +713,12 @@ Plan plan_of(const dol_matrix *u, const dol_matrix *gate, void *workspace)
     p.threads = threads_of(u->cols);
     p.each = gate && gate->rows == u->rows;
     p.sets = gate && !p.each ? gate->rows : 1, p.points = u->rows / p.sets;
-    const int groups = p.threads == 0 ? 1 : p.threads <= 128 ? kThreads / p.threads : p.threads <= 256 ? 512 / p.threads : 1;
+    const int groups = back_groups(p.threads);
     // (rows too long for registers: as many of kThreads as lie side by side)
-    const int64_t most_blocks = !p.threads ? std::max(1, 4 * kUnits / stripes_of(u->cols)) : p.threads <= 128 ? 4 * kUnits : p.threads <= 512 ? 2 * kUnits : kUnits;
+    const int64_t most_blocks = p.threads ? back_blocks(p.threads) * kUnits : std::max(1, 4 * kUnits / stripes_of(u->cols));
     // As chunks of a set's rows to workgroups, or as whole sets to groups: what takes fewer rows in a row, where leaving a chunk's parts takes as long as three
-    // rows.  Both ways, us, chunks / whole: bf16 900 x 20 x 300 50 / 88, 2 000 x 30 x 300 155 / 192, 4 000 x 10 x 1 024 211 / 189, 8 000 x 40 x 96 214 / 164,
-    // 100 000 x 3 x 16 1 078 / 50, float 427 x 4 x 7 463 214 / 201, 128 x 50 x 7 463 577 / 791.
+    // rows.  Both ways, us, chunks / whole: bf16 900 x 20 x 300 50 / 88, 2 000 x 30 x 300 155 / 192, 4 000 x 10 x 1 024 225 / 188, 8 000 x 40 x 96 223 / 164,
+    // 100 000 x 3 x 16 1 078 / 50, float 3 000 x 3 x 2 048 240 / 180, 128 x 50 x 7 463 530 / 767.
     const int64_t wanted = std::max<int64_t>(1, most_blocks / p.sets), most = std::max<int64_t>(1, p.points / groups);
     p.chunks = std::min(wanted, most);
     p.chunk = (p.points + p.chunks - 1) / p.chunks;
