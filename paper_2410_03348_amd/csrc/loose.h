@@ -50,8 +50,23 @@ __device__ __forceinline__ Loose<S> loose_load(const S *p, int64_t n)
     return v;
 }
 
-// The same where `before` elements of the row lie before p: the row's last vector, shifted, is one load, where one of each element would wait for
-// the one before it.
+// v's elements from the k-th on (k > 0), zeros behind them.
+template <typename S>
+__device__ __forceinline__ Loose<S> loose_from(const Loose<S> &v, int k)
+{
+    const int bytes = k * static_cast<int>(sizeof(S));
+    Loose<S> r = v;
+    // (by eight, four and two of them: one shift of the whole would hold twice the registers)
+    if (bytes & 8) r.w[0] = r.w[2], r.w[1] = r.w[3], r.w[2] = r.w[3] = 0;
+    if (bytes & 4) r.w[0] = r.w[1], r.w[1] = r.w[2], r.w[2] = r.w[3], r.w[3] = 0;
+    if (sizeof(S) == 2 && (bytes & 2))
+        r.w[0] = r.w[0] >> 16 | r.w[1] << 16, r.w[1] = r.w[1] >> 16 | r.w[2] << 16, r.w[2] = r.w[2] >> 16 | r.w[3] << 16, r.w[3] >>= 16;
+    if (bytes >= 16) r.w[0] = r.w[1] = r.w[2] = r.w[3] = 0;
+    return r;
+}
+
+// The first n elements at p where `before` elements of the row lie before it: the row's last vector, shifted, is one load, where one of each element would
+// wait for the one before it.
 template <typename S>
 __device__ __forceinline__ Loose<S> loose_load_end(const S *p, int n, int before)
 {
@@ -59,14 +74,7 @@ __device__ __forceinline__ Loose<S> loose_load_end(const S *p, int n, int before
     if (n >= V) return *reinterpret_cast<const Loose<S> *>(p);
     if (n <= 0) return Loose<S>{};
     if (before + n < V) return loose_load(p, n);
-    const Loose<S> v = *reinterpret_cast<const Loose<S> *>(p - (V - n));
-    uint64_t lo = v.w[0] | static_cast<uint64_t>(v.w[1]) << 32, hi = v.w[2] | static_cast<uint64_t>(v.w[3]) << 32;
-    const int shift = (V - n) * static_cast<int>(8 * sizeof(S));        // of 128 bits, 16 to 112
-    if (shift >= 64) lo = hi >> (shift - 64), hi = 0;
-    else lo = lo >> shift | hi << (64 - shift), hi >>= shift;
-    Loose<S> r;
-    r.w[0] = static_cast<uint32_t>(lo), r.w[1] = static_cast<uint32_t>(lo >> 32), r.w[2] = static_cast<uint32_t>(hi), r.w[3] = static_cast<uint32_t>(hi >> 32);
-    return r;
+    return loose_from(*reinterpret_cast<const Loose<S> *>(p - (V - n)), V - n);
 }
 
 template <typename S>

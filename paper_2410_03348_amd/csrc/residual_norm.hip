@@ -33,7 +33,7 @@ constexpr int kGroups = G < kThreads ? kThreads / G : 1;
 // Wavefronts to a SIMD that the forward kernel's registers leave room for, and the workgroups of the chip that are.  More of them than that would be a second
 // round of fewer: bf16 8 192 x 4 096 59 us with four to a unit, of which three fit, 51 with three.
 template <typename S, int G>
-constexpr int kForwardWaves = sizeof(S) == 4 || G < 64 ? 5 : G <= 384 ? 7 : G <= 768 ? 6 : 4;
+constexpr int kForwardWaves = G == 4 ? 4 : sizeof(S) == 4 || G < 64 ? 5 : G <= 384 ? 7 : G <= 768 ? 6 : 4;
 template <typename S, int G>
 constexpr int kForwardBlocks = 256 * (kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) > 0 ? kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) : 1);
 // Backward fewer workgroups leave fewer parts, but a set of few rows leaves most of a large one idle.  Both ways, us, four to a unit / two / one: bf16 39 574 x 361
@@ -44,6 +44,7 @@ constexpr int back_blocks(int threads) { return threads <= 64 ? 4 : threads == 1
 template <int G>
 constexpr int kBackGroups = back_groups(G);
 constexpr int kUnits = 256;             // compute units of the chip
+constexpr int kNoRow = -(1 << 20);      // in place of the columns that are left of a row, where there is no row
 constexpr int64_t kMostBlocks = 1 << 20;        // of a launch, which has less than 2^32 threads
 
 template <typename S>
@@ -122,10 +123,20 @@ struct Eight {
     static constexpr int V = kLooseElements<S>, H = kEight / V, kSpan = (H - 1) * D + V;
     static constexpr int column(int e) { return e / V * D + e % V; }
     Loose<S> v[H];
-    __device__ void all(const S *p)
+    // The row's, of at least a vector, from column c on; where a vector is not all there the row's last one, so that all threads load at once, and cut() does
+    // the rest.
+    __device__ void all(const Mat<const S> &m, int64_t r, int c, int cols)
     {
 #pragma unroll
-        for (int h = 0; h < H; ++h) v[h] = *reinterpret_cast<const Loose<S> *>(p + h * D);
+        for (int h = 0; h < H; ++h) v[h] = *reinterpret_cast<const Loose<S> *>(m.at(r, min(c + h * D, cols - V)));
+    }
+    __device__ void cut(int n)
+    {
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            if (n - h * D < V) v[h] = loose_from(v[h], V - (n - h * D));
+            __builtin_amdgcn_sched_barrier(0);      // (one vector's numbers in registers at a time)
+        }
     }
     // those of them that are in the n columns from column c on, zeros behind
     __device__ void some(const S *p, int n, int c)
@@ -237,16 +248,23 @@ struct InLds {
 template <int G>
 constexpr int kGammaLds = G >= 64 ? 2 * G * kEight * 4 : 0;
 
-// What a row's eight columns are read for.
-template <typename S, int D>
+// What a row's eight columns are read for; FEW: a row may have less than a vector.
+template <typename S, int D, bool FEW>
 struct Columns {
     Eight<S, D> x, u, gate;
-    // (one branch for all of them, and none for a tensor that is not there: a load behind a branch of its own is waited for at its end)
+    // n columns of row r of x and u, and g of gate, from c on.  (One branch for all of them, and none for a tensor that is not there: a load behind a branch of its
+    // own is waited for at its end.)
     __device__ void load(const Args<S> &a, int64_t r, int64_t g, int c, int n)
     {
-        const S *pu = a.u.at(r, c), *px = a.x.p ? a.x.at(r, c) : pu, *pg = a.gate.p ? a.gate.at(g, c) : pu;
-        if (n >= Eight<S, D>::kSpan) x.all(px), u.all(pu), gate.all(pg);
-        else x.some(px, n, c), u.some(pu, n, c), gate.some(pg, n, c);
+        const Mat<const S> mx = a.x.p ? a.x : a.u, mg = a.gate.p ? a.gate : a.u;
+        if (!a.gate.p) g = r;
+        if (FEW && a.cols < Eight<S, D>::V) x.some(mx.at(r, c), n, c), u.some(a.u.at(r, c), n, c), gate.some(mg.at(g, c), n, c);
+        else if (n != kNoRow) x.all(mx, r, c, a.cols), u.all(a.u, r, c, a.cols), gate.all(mg, g, c, a.cols);
+    }
+    // Before they are used, as late as can be: nothing of it is done before the loads are there.
+    __device__ void ready(const Args<S> &a, int n)
+    {
+        if ((!FEW || a.cols >= Eight<S, D>::V) && n < Eight<S, D>::kSpan) x.cut(n), u.cut(n), gate.cut(n);
         x.only(a.x.p, 0.0f), gate.only(a.gate.p, 1.0f);
     }
     // gate gamma_u u of column e, and h, of which it is scale rstd_u
@@ -267,16 +285,17 @@ __global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residua
     float gamma_u[kEight], gamma_y[kEight];
     factors<D>(gamma_u, a.gamma_u, a.cols - c, c);
     factors<D>(gamma_y, a.gamma_y, a.cols - c, c);
-    Columns<S, D> q;
-    auto fetch = [&](int64_t r) { q.load(a, r, r < a.rows ? a.gate_of(r) : 0, c, r < a.rows ? a.cols - c : 0); };
+    Columns<S, D, (G == 4)> q;
+    auto fetch = [&](int64_t r) { q.load(a, r, r < a.rows ? a.gate_of(r) : 0, c, r < a.rows ? a.cols - c : kNoRow); };
     fetch(static_cast<int64_t>(blockIdx.x) * R + group);
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * R; first < a.rows; first += stride) {
         const int64_t r = first + group;
         const bool in = r < a.rows;
-        const int n = in ? a.cols - c : 0;
+        const int n = in ? a.cols - c : kNoRow;
         float h[kEight], s[1] = {0.0f}, rstd = 1.0f;
-        const Columns<S, D> p = q;
+        Columns<S, D, (G == 4)> p = q;
         fetch(r + stride);
+        p.ready(a, n);
         if (a.norm_u) {
 #pragma unroll
             for (int e = 0; e < kEight; ++e) s[0] = __builtin_fmaf(p.u.get(e), p.u.get(e), s[0]);
@@ -307,17 +326,21 @@ __global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residua
 // ---------------------------------------------------------------- backward
 
 // Eight columns of a row.  h is made again from x and u: as it was rounded to bf16 it would be off by 2^-9 in every term of grad_gamma_y.
-template <typename S, int D>
+template <typename S, int D, bool FEW>
 struct Piece {
-    Columns<S, D> p;
+    Columns<S, D, FEW> p;
     Eight<S, D> gy, gh;
     __device__ void load(const Args<S> &a, int64_t r, int64_t g, int c, int n)
     {
-        const S *pu = a.u.at(r, c), *px = a.x.p ? a.x.at(r, c) : pu, *pg = a.gate.p ? a.gate.at(g, c) : pu;
-        const S *py = a.grad_y.p ? a.grad_y.at(r, c) : pu, *ph = a.grad_h.p ? a.grad_h.at(r, c) : pu;
-        if (n >= Eight<S, D>::kSpan) p.x.all(px), p.u.all(pu), p.gate.all(pg), gy.all(py), gh.all(ph);
-        else p.x.some(px, n, c), p.u.some(pu, n, c), p.gate.some(pg, n, c), gy.some(py, n, c), gh.some(ph, n, c);
-        p.x.only(a.x.p, 0.0f), p.gate.only(a.gate.p, 1.0f), gy.only(a.grad_y.p, 0.0f), gh.only(a.grad_h.p, 0.0f);
+        const Mat<const S> mx = a.x.p ? a.x : a.u, mg = a.gate.p ? a.gate : a.u, my = a.grad_y.p ? a.grad_y : a.u, mh = a.grad_h.p ? a.grad_h : a.u;
+        if (!a.gate.p) g = r;
+        if (FEW && a.cols < Eight<S, D>::V)
+            p.x.some(mx.at(r, c), n, c), p.u.some(a.u.at(r, c), n, c), p.gate.some(mg.at(g, c), n, c), gy.some(my.at(r, c), n, c), gh.some(mh.at(r, c), n, c);
+        else
+            p.x.all(mx, r, c, a.cols), p.u.all(a.u, r, c, a.cols), p.gate.all(mg, g, c, a.cols), gy.all(my, r, c, a.cols), gh.all(mh, r, c, a.cols);
+        p.ready(a, n);
+        if ((!FEW || a.cols >= Eight<S, D>::V) && n < Eight<S, D>::kSpan) gy.cut(n), gh.cut(n);
+        gy.only(a.grad_y.p, 0.0f), gh.only(a.grad_h.p, 0.0f);
     }
     __device__ void again() { p.x.again(), p.u.again(), p.gate.again(), gy.again(), gh.again(); }
     // What a row is multiplied with; sums() adds up four products of eight columns, which with rstd's left out of them are two instructions each.
@@ -443,17 +466,17 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
 #pragma unroll
     for (int e = 0; e < kEight; ++e) sum_y[e] = sum_t[e] = sum_u[e] = 0.0f;
     struct Row {
-        Piece<S, D> p;
+        Piece<S, D, (G == 4)> p;
         int64_t r;
         int n;
         float rstd_u, rstd_h;
     };
     auto fetch = [&](Row &q, int64_t t, int64_t k) {
         const int64_t m = mine + t * stride;
-        const bool in = WHOLE ? m < a.sets : r0 + k * R + group < r1;
-        q.r = WHOLE ? m * a.points + k : r0 + k * R + group;
-        q.n = in ? a.cols - c : 0;
-        q.p.load(a, q.r, WHOLE ? m : a.each ? q.r : set, c, q.n);
+        const bool in = WHOLE ? m < a.sets : r0 + k * R + group < r1;       // (else row 0 is read, and none of it kept)
+        q.r = !in ? 0 : WHOLE ? m * a.points + k : r0 + k * R + group;
+        q.n = in ? a.cols - c : kNoRow;
+        q.p.load(a, q.r, WHOLE ? in ? m : 0 : a.each ? q.r : set, c, q.n);
         q.rstd_u = a.norm_u && in ? a.rstd_u[q.r] : 1.0f, q.rstd_h = a.grad_y.p && in ? a.rstd_h[q.r] : 0.0f;
     };
     int turn = 0;
@@ -461,7 +484,7 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
         for (int64_t k = 0; k < count; ++k) {
             Row now;
             fetch(now, t, k);
-            typename Piece<S, D>::Factors m{a.scale * now.rstd_u, now.rstd_h, 0.0f, 0.0f};
+            typename Piece<S, D, (G == 4)>::Factors m{a.scale * now.rstd_u, now.rstd_h, 0.0f, 0.0f};
             float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             now.p.sums(s, gamma, m.f);
             group_sums<G, 4>(s, red[turn]);
@@ -502,9 +525,10 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(Args<S
         const int64_t g = a.gate_of(r);
         float rstd_u = 1.0f, rstd_h = 0.0f, s[1] = {0.0f};
         auto stream = [&](int c, int n, float (&h)[kEight]) {
-            Columns<S, D> p;
+            Columns<S, D, false> p;
             float gamma_u[kEight];
             p.load(a, r, g, c, n);
+            p.ready(a, n);
             factors<D>(gamma_u, a.gamma_u, n, c);
 #pragma unroll
             for (int e = 0; e < kEight; ++e) h[e] = p.stream(e, gamma_u[e], a.scale * rstd_u);
@@ -558,11 +582,11 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_rows_kernel(A
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const int64_t g = a.gate_of(r);
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
-        typename Piece<S, D>::Factors m{a.scale * rstd_u, rstd_h, 0.0f, 0.0f};
+        typename Piece<S, D, false>::Factors m{a.scale * rstd_u, rstd_h, 0.0f, 0.0f};
         float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * kEight) {
             const int n = a.cols - c;
-            Piece<S, D> p;
+            Piece<S, D, false> p;
             p.load(a, r, g, c, n);
             p.sums(s, InRegisters<D>(a, c, n, nullptr), m.f);
         }
@@ -588,7 +612,7 @@ __global__ void __launch_bounds__(kThreads) residual_norm_wide_map_kernel(Args<S
     for (int64_t r = r0; r < r1; ++r) {
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
         const float2 m = a.row[r];
-        Piece<S, D> p;
+        Piece<S, D, false> p;
         p.load(a, r, a.each ? r : set, c, n);
         p.leave(a, r, c, n, gamma, {a.scale * rstd_u, rstd_h, m.x, m.y}, sum_y, sum_t);
     }
