@@ -321,22 +321,36 @@ __device__ __forceinline__ void slope_rows(const Slope &p, unsigned block, float
         const bool rests = ACT && sizeof(S) == 2 && p.rest;
         for (int64_t first = r0; first < r1 && c < p.out_cols; first += ROWS * kAhead) {
             Row q[kAhead];
-            if (n >= 8 && first + ROWS * (kAhead - 1) < p.rows) {       // (one branch for all loads: each is waited for at a branch's end)
+            // (one branch for all loads: each is waited for at a branch's end; where a vector is not all there the row's last one, shifted)
+            if (p.cols >= 8) {
 #pragma unroll
                 for (int t = 0; t < kAhead; ++t) {
-                    const int64_t r = first + ROWS * t;
+                    const int64_t r = min(first + ROWS * t, static_cast<int64_t>(p.rows) - 1);
 #pragma unroll
                     for (int h = 0; h < H; ++h) {
-                        q[t].g[h] = *reinterpret_cast<const Loose<S> *>(static_cast<const S *>(p.grad_y) + r * p.grad_ld + c + h * V);
-                        if (ACT) q[t].z[h] = *reinterpret_cast<const Loose<S> *>(static_cast<const S *>(p.z) + r * p.z_ld + c + h * V);
+                        const int64_t at = min(c + h * V, static_cast<int64_t>(p.cols) - V);
+                        q[t].g[h] = *reinterpret_cast<const Loose<S> *>(static_cast<const S *>(p.grad_y) + r * p.grad_ld + at);
+                        if (ACT) q[t].z[h] = *reinterpret_cast<const Loose<S> *>(static_cast<const S *>(p.z) + r * p.z_ld + at);
                     }
-                    if (rests) q[t].rest = *reinterpret_cast<const Loose<__bf16> *>(p.rest + r * p.cols + c);
+                    if (rests) q[t].rest = *reinterpret_cast<const Loose<__bf16> *>(p.rest + r * p.cols + min(c, static_cast<int64_t>(p.cols) - 8));
                 }
+                if (n < 8 || first + ROWS * (kAhead - 1) >= p.rows)
+#pragma unroll
+                    for (int t = 0; t < kAhead; ++t) {
+                        const int left = first + ROWS * t < p.rows ? static_cast<int>(n) : 0;
+#pragma unroll
+                        for (int h = 0; h < H; ++h)
+                            if (left - h * V < V) {
+                                q[t].g[h] = loose_from(q[t].g[h], V - (left - h * V));
+                                if (ACT) q[t].z[h] = loose_from(q[t].z[h], V - (left - h * V));
+                            }
+                        if (rests && left < 8) q[t].rest = loose_from(q[t].rest, 8 - left);
+                    }
             } else
 #pragma unroll
                 for (int t = 0; t < kAhead; ++t) {
                     const int64_t r = first + ROWS * t;
-                    const int left = r < p.rows ? static_cast<int>(min(n, static_cast<int64_t>(8))) : 0, before = static_cast<int>(c);
+                    const int left = r < p.rows ? static_cast<int>(n) : 0, before = static_cast<int>(c);
 #pragma unroll
                     for (int h = 0; h < H; ++h) {
                         q[t].g[h] = loose_load_end(static_cast<const S *>(p.grad_y) + r * p.grad_ld + c + h * V, left - h * V, before + h * V);
