@@ -254,6 +254,27 @@ def test_in_place(dol, cols, dtype):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("cols", [1, 2, 5, 7, 9, 13, 20, 31, 129, 250, 361, 1111, 2101, 7463, 8193])
+def test_ends_of_rows(dol, cols, dtype):
+    """Where a row's last vector is read shifted: with NaN beside every row, and in place, the same bits."""
+    t = getattr(torch, dtype)
+    c = Case(70, cols, t, gates=14)
+    h, y, ru, rh = forward(dol, c)
+    check_forward(c, h, y, ru, rh)
+    want = backward(dol, c, ru, rh, c.grad_h, c.grad_y)
+    check_backward(c, ru, rh, c.grad_h, c.grad_y, want)
+    d = Case(70, cols, t, gates=14)
+    for name in ("x", "u", "gate", "grad_h", "grad_y"):
+        v, b = view(getattr(c, name), 9, 1)
+        b.fill_(math.nan)
+        setattr(d, name, v.copy_(getattr(c, name)))
+    got = backward(dol, d, ru, rh, d.grad_h, d.grad_y, d.grad_h, d.grad_y)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    hh, yy, ru2, rh2 = forward(dol, d, d.x, d.u)
+    assert torch.equal(hh, h) and torch.equal(yy, y) and torch.equal(ru2, ru) and torch.equal(rh2, rh)
+
+
 def test_differences(dol):
     """Gradients against differences of the forward call itself, in float."""
     c = Case(12, 96, torch.float32, gates=4, seed=2)
