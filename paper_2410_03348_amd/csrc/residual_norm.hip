@@ -124,7 +124,7 @@ struct Eight {
     static constexpr int column(int e) { return e / V * D + e % V; }
     Loose<S> v[H];
     // The row's, of at least a vector, from column c on; where a vector is not all there the row's last one, so that all threads load at once, and cut() does
-    // the rest.
+    // the rest (behind a branch for those threads each load is waited for by itself: bf16 39 574 x 361 both ways 94 us, 114 so).
     __device__ void all(const Mat<const S> &m, int64_t r, int c, int cols)
     {
 #pragma unroll
@@ -274,7 +274,7 @@ struct Columns {
 
 // ---------------------------------------------------------------- forward
 
-// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 51 us, 5.3 TB/s.
+// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 49 us, 5.5 TB/s.
 template <typename S, int G>
 __global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residual_norm_kernel(Args<S> a)
 {
@@ -446,7 +446,7 @@ __device__ __forceinline__ void leave_part(const float (&sum)[kEight], O *to, in
 }
 
 // WHOLE: a group takes all rows of its sets; else a workgroup takes a chunk of the rows of one set.
-// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 98 us, 4.1 TB/s.  (With the next row asked for ahead, as forward, it has registers for one row on a
+// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 93 us, 4.3 TB/s.  (With the next row asked for ahead, as forward, it has registers for one row on a
 // unit at a time instead of two: 116 us against 99.)
 template <typename S, int G, bool WHOLE>
 __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_norm_backward_kernel(Args<S> a)
@@ -741,8 +741,8 @@ Plan plan_of(const dol_matrix *u, const dol_matrix *gate, void *workspace)
     // (rows too long for registers: as many of kThreads as lie side by side)
     const int64_t most_blocks = p.threads ? back_blocks(p.threads) * kUnits : std::max(1, 4 * kUnits / stripes_of(u->cols));
     // As chunks of a set's rows to workgroups, or as whole sets to groups: what takes fewer rows in a row, where leaving a chunk's parts takes as long as three
-    // rows.  Both ways, us, chunks / whole: bf16 900 x 20 x 300 50 / 88, 2 000 x 30 x 300 155 / 192, 4 000 x 10 x 1 024 225 / 188, 8 000 x 40 x 96 223 / 164,
-    // 100 000 x 3 x 16 1 078 / 50, float 3 000 x 3 x 2 048 240 / 180, 128 x 50 x 7 463 530 / 767.
+    // rows.  Both ways, us, chunks / whole: bf16 900 x 20 x 300 45 / 63, 2 000 x 30 x 300 120 / 130, 4 000 x 10 x 1 024 218 / 185, 8 000 x 40 x 96 207 / 167,
+    // 100 000 x 3 x 16 1 111 / 51, float 3 000 x 3 x 2 048 239 / 174, 128 x 50 x 7 463 426 / 560.
     const int64_t wanted = std::max<int64_t>(1, most_blocks / p.sets), most = std::max<int64_t>(1, p.points / groups);
     p.chunks = std::min(wanted, most);
     p.chunk = (p.points + p.chunks - 1) / p.chunks;
