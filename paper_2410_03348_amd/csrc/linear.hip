@@ -439,13 +439,24 @@ __global__ void __launch_bounds__(kBackWaves * 64) linear_few_back_kernel(const 
         for (int r = 0; r < R; ++r) acc[j][r] = f32x4{0, 0, 0, 0};
     for (int64_t k = k0; k < k1; k += STEP) {
         Loose<S> v[J];
-        const S *from = w + (k + kq * J) * ldw + c;
-        if (k + STEP <= out && n >= J)
+        if (width >= J) {       // (all loads at once; past the end of a row its last vector, shifted, and past the last row zeros)
+            const S *from = w + min(c, width - J);
+            if (k + STEP <= out)
 #pragma unroll
-            for (int t = 0; t < J; ++t) v[t] = *reinterpret_cast<const Loose<S> *>(from + t * ldw);
-        else
+                for (int t = 0; t < J; ++t) v[t] = *reinterpret_cast<const Loose<S> *>(from + (k + kq * J + t) * ldw);
+            else {
 #pragma unroll
-            for (int t = 0; t < J; ++t) v[t] = loose_load_end(from + t * ldw, k + kq * J + t < out ? n : 0, c);
+                for (int t = 0; t < J; ++t) v[t] = *reinterpret_cast<const Loose<S> *>(from + min(k + kq * J + t, static_cast<int64_t>(out) - 1) * ldw);
+#pragma unroll
+                for (int t = 0; t < J; ++t)
+                    if (k + kq * J + t >= out) v[t] = Loose<S>{};
+            }
+            if (n < J)
+#pragma unroll
+                for (int t = 0; t < J; ++t) v[t] = loose_from(v[t], J - n);
+        } else
+#pragma unroll
+            for (int t = 0; t < J; ++t) v[t] = loose_load(w + (k + kq * J + t) * ldw + c, k + kq * J + t < out ? n : 0);
         if constexpr (sizeof(S) == 2) {
             bf16x8 b[R][Q];
 #pragma unroll
