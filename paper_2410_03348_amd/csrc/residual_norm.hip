@@ -6,7 +6,8 @@
 //   grad_gate = scale sum dh v,   grad_gamma_u = sum scale gate dh uhat,   grad_gamma_y = sum dy hhat   over rows
 //
 // Memory bounds it: four tensors forward, six backward.  A row lies in the registers of a group of 4 to 1 024 threads, eight columns to
-// each, and is read once; memory gives it as fast as some 40 instructions an element take, so that rstd's stay out of all that is done by element.  Backward one round of sums is enough: with dh put into it and t = gate gamma_u u, the sum of k dh uhat is scale rms(u) times
+// each, and is read once; memory gives it as fast as some 40 instructions an element take, so that rstd's stay out of all that is done by element.
+// Backward one round of sums is enough: with dh put into it and t = gate gamma_u u, the sum of k dh uhat is scale rms(u) times
 //   sum t grad_h + rms(h) sum t a - rms(h)^2 m1 sum t h,
 // sums that need nothing of each other.  Sums over rows stay in registers while a group goes down its rows; a workgroup leaves one part of
 // each, which a second launch adds up in the order of the rows.  Rows too long for that are read twice (wide_*).

@@ -192,7 +192,8 @@ BACK_TILES = [("bfloat16", 4096, 2048, 4096, "256x256x64"), ("bfloat16", 4000, 2
               ("bfloat16", 1, 2100, 2100, "few_back_kernel 16"), ("bfloat16", 16, 1509, 3003, "few_back_kernel 16"), ("bfloat16", 30, 4160, 1100, "few_back_kernel 32"),
               ("bfloat16", 64, 130, 40000, "few_back_kernel 64"), ("bfloat16", 64, 30000, 150, "few_back_kernel 64"), ("bfloat16", 65, 2100, 2100, "128x128x32"),
               ("float32", 3, 2100, 2100, "few_back_kernel 16"), ("float32", 17, 1509, 3003, "few_back_kernel 32"), ("float32", 50, 70, 60100, "few_back_kernel 64"),
-              ("float32", 64, 30000, 150, "few_back_kernel 64"), ("float32", 2048, 256, 4096, "128x256x32"), ("float32", 1000, 300, 500, "128x128x32"), ("float32", 100, 100, 100, "64x64x64")]
+              ("float32", 64, 30000, 150, "few_back_kernel 64"), ("bfloat16", 3, 5, 900001, "few_back_kernel 16"), ("bfloat16", 18, 9, 500003, "few_back_kernel 32"),
+              ("float32", 3, 3, 1500001, "few_back_kernel 16"), ("float32", 33, 7, 700001, "few_back_kernel 64"), ("float32", 2048, 256, 4096, "128x256x32"), ("float32", 1000, 300, 500, "128x128x32"), ("float32", 100, 100, 100, "64x64x64")]
 
 
 @pytest.mark.parametrize("dtype,n,d,m,name", BACK_TILES)
