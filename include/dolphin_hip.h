@@ -500,7 +500,8 @@ dol_status dol_group_norm_backward(const dol_activations *x, int32_t groups, con
  *   z_rest    device [rows, out] or NULL, only with z in DOL_BF16: what rounding z has left, in steps of a float.  With it the slopes that
  *             grad_bias sums up are a float's, without it off by some 2^-9 each
  * (DOL_F32 multiplies in parts of numbers where it takes tiles (dol_linear_kernel), as grad_weight always does: an infinity in an operand
- * makes the sums that it is in NaN, and numbers below 2^-109 lose their last bits.)
+ * makes the sums that it is in NaN, and numbers below 2^-109 lose their last bits.  In DOL_BF16 an infinity in x or weight may do so to the
+ * gradients that it is in.)
  * At most 2^22 rows and outs and 2^20 elements of a row (else DOL_EUNSUPPORTED); at least one out of one element. */
 dol_status dol_linear_workspace(const dol_matrix *x, const dol_matrix *weight, int32_t backward, int64_t *bytes);
 /* As dol_cross_entropy_kernel: "linear_few_kernel 16x16" (rows and outs), "linear_tiles_kernel 128x128x64", backward (what grad_x is made by)

@@ -296,6 +296,23 @@ def test_nan_stays_in_its_row(dol, n, dtype):
     assert bool(gw2.isnan().all()) and bool(gb2.isnan().all())
 
 
+@pytest.mark.parametrize("n,d,m", [(100, 100, 100), (600, 200, 130), (1, 2100, 2100), (40, 2101, 2100), (64, 64, 70)])
+def test_an_infinity_stays_in_its_sums(dol, n, d, m):
+    """bf16: results forward are infinite where the sums are; gradients may be NaN there, and nowhere else."""
+    c = make(n, d, m, torch.bfloat16, seed=6)
+    c["x"][n - 1, 5], c["w"][m - 1, 3] = math.inf, math.inf
+    y, z, rest = forward(dol, c, "none")
+    gx, gw, gb = backward(dol, c, "none", z, rest)
+    want = c["x"].double().cpu() @ c["w"].double().cpu().T
+    assert torch.equal(z.isnan().cpu(), want.isnan()) and torch.equal(z.isinf().cpu(), want.isinf())
+    off = torch.zeros(n, d, dtype=torch.bool, device="cuda")
+    off[:, 3] = True
+    assert torch.equal(~gx.isfinite(), off) and bool(gb.isfinite().all())
+    off = torch.zeros(m, d, dtype=torch.bool, device="cuda")
+    off[:, 5] = True
+    assert torch.equal(~gw.isfinite(), off)
+
+
 def test_on_another_stream_and_in_a_graph(dol):
     """Replayed graphs beside eager work, two graphs one after the other that share a workspace, and eager gradients of the same operands alive."""
     for n in (8, 300):
