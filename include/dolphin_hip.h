@@ -540,13 +540,21 @@ dol_status dol_residual_norm(const dol_matrix *x, const dol_matrix *u, int32_t n
  *   grad_gate[g] = scale sum dh v over the gate's rows,   grad_gamma_u = sum dv uhat,   grad_gamma_y = sum grad_y hhat over all rows.
  * x, u, gamma_u, gate, scale, gamma_y as in, rstd_u and rstd_h from the forward call (rstd_h only with grad_y, rstd_u only with norm_u); h is
  * made again from them, unrounded.  Each is OVERWRITTEN and may be NULL; grad_x and grad_u, each its own, may be grad_h, grad_y, x or u.
- * Sums are taken in a fixed order: two runs give the same bits. */
+ * Sums are taken in a fixed order: two runs give the same bits.
+ * dol_residual_norm_backward_from_h, for a program that keeps what is behind the block and not x: the same gradients at h as the forward call has
+ * left it (NULL only without grad_y; grad_x and grad_u may be h).  In DOL_F32 they are as exact; h in DOL_BF16 has lost up to 2^-8 of each number, and with it so
+ * has each of the terms that grad_gamma_y adds up: a bf16 program that wants that sum as exact as the others keeps x. */
 dol_status dol_residual_norm_workspace(const dol_matrix *u, const dol_matrix *gate, int64_t *bytes);
 dol_status dol_residual_norm_backward(const dol_matrix *x, const dol_matrix *u, int32_t norm_u, const float *gamma_u, const dol_matrix *gate,
                                       float scale, const float *gamma_y, const float *rstd_u, const float *rstd_h, const dol_matrix *grad_h,
                                       const dol_matrix *grad_y, const dol_matrix *grad_x, const dol_matrix *grad_u, float *grad_gamma_u,
                                       const dol_matrix *grad_gate, float *grad_gamma_y, void *workspace, int64_t workspace_bytes,
                                       void *hip_stream);
+dol_status dol_residual_norm_backward_from_h(const dol_matrix *h, const dol_matrix *u, int32_t norm_u, const float *gamma_u,
+                                             const dol_matrix *gate, float scale, const float *gamma_y, const float *rstd_u,
+                                             const float *rstd_h, const dol_matrix *grad_h, const dol_matrix *grad_y, const dol_matrix *grad_x,
+                                             const dol_matrix *grad_u, float *grad_gamma_u, const dol_matrix *grad_gate, float *grad_gamma_y,
+                                             void *workspace, int64_t workspace_bytes, void *hip_stream);
 
 /* The buffers of a network's gradients (or of what is made of them), which a training program keeps: `count` of them, buffer t at data[t]
  * with size[t] >= 0 neighbouring elements of type dtype[t] (dol_dtype).  All three arrays are host memory, read during the call only.

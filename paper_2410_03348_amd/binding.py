@@ -855,14 +855,21 @@ def residual_norm_backward(x: Optional[torch.Tensor], u: torch.Tensor, gamma_u: 
                            grad_gamma_y: Optional[torch.Tensor], norm_u: bool = True, scale: float = 1.0,
                            workspace: Optional[torch.Tensor] = None, stream=None):
     """Gradients of sum(grad_h * h) + sum(grad_y * y); rstd_u and rstd_h as residual_norm left them.  Gradients that are None are not
-    computed; grad_x and grad_u may be grad_h, grad_y, x or u, but not one tensor."""
+    computed; grad_x and grad_u may be grad_h, grad_y, x or u, but not one tensor.
+
+    A program that keeps h and not x calls residual_norm_backward(u, gamma_u, gate, gamma_y, h, rstd_u, ...), the same from there on: with h behind
+    gamma_y in place of x before u, which the vector gamma_u (or None) in the place of the matrix u tells apart.  In bfloat16 grad_gamma_y is then
+    off by what rounding h has left, some 2^-9 a term."""
+    call = _native.residual_norm_backward
+    if u is None or u.dim() == 1:
+        x, u, gamma_u, gate, gamma_y = gamma_y, x, u, gamma_u, gate
+        call = _native.residual_norm_backward_from_h
     mu, mg = _matrix(u), _matrix(gate)
     rows, cols = mu[1], mu[2]
     ws, n, _keep = _workspace(workspace, _native.residual_norm_workspace(mu, mg) if workspace is None else 0, u.device, stream)
-    _native.residual_norm_backward(_matrix(x), mu, int(norm_u), _values(gamma_u, _F, cols), mg, scale, _values(gamma_y, _F, cols),
-                                   _values(rstd_u, _F, rows), _values(rstd_h, _F, rows), _matrix(grad_h), _matrix(grad_y), _matrix(grad_x),
-                                   _matrix(grad_u), _values(grad_gamma_u, _F, cols), _matrix(grad_gate), _values(grad_gamma_y, _F, cols), ws, n,
-                                   _handle(stream))
+    call(_matrix(x), mu, int(norm_u), _values(gamma_u, _F, cols), mg, scale, _values(gamma_y, _F, cols), _values(rstd_u, _F, rows),
+         _values(rstd_h, _F, rows), _matrix(grad_h), _matrix(grad_y), _matrix(grad_x), _matrix(grad_u), _values(grad_gamma_u, _F, cols),
+         _matrix(grad_gate), _values(grad_gamma_y, _F, cols), ws, n, _handle(stream))
 
 
 _lib.dol_tensor_list_create.argtypes = [C.c_int32, _i32p, C.POINTER(C.c_int64), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p)]

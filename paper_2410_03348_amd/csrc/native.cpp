@@ -454,6 +454,7 @@ PyObject *residual_norm_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
     return bytes(st, need);
 }
 
+template <auto CALL>
 PyObject *residual_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     Args a(v, n, 19);
@@ -465,8 +466,7 @@ PyObject *residual_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     auto *ws = a.ptr<void>(16);
     const int64_t have = a.num(17);
     void *s = a.stream(18);
-    DOL_CALL(dol_residual_norm_backward(x.p(), u.p(), norm_u, gamma_u, gate.p(), scale, gamma_y, rstd_u, rstd_h, gh.p(), gy.p(), gx.p(), gu.p(), ggu, gg.p(), ggy,
-                                        ws, have, s));
+    DOL_CALL(CALL(x.p(), u.p(), norm_u, gamma_u, gate.p(), scale, gamma_y, rstd_u, rstd_h, gh.p(), gy.p(), gx.p(), gu.p(), ggu, gg.p(), ggy, ws, have, s));
 }
 
 PyObject *grad_norm_workspace(PyObject *, PyObject *const *v, Py_ssize_t n)
@@ -671,7 +671,8 @@ PyMethodDef g_methods[] = {
     {"linear_backward", DOL_FAST(linear_backward)},
     {"residual_norm", DOL_FAST(residual_norm)},
     {"residual_norm_workspace", DOL_FAST(residual_norm_workspace)},
-    {"residual_norm_backward", DOL_FAST(residual_norm_backward)},
+    {"residual_norm_backward", DOL_FAST(residual_norm_backward<dol_residual_norm_backward>)},
+    {"residual_norm_backward_from_h", DOL_FAST(residual_norm_backward<dol_residual_norm_backward_from_h>)},
     {"grad_norm_workspace", DOL_FAST(grad_norm_workspace)},
     {"grad_norm", DOL_FAST(grad_norm)},
     {"clip_grads", DOL_FAST(clip_grads)},

@@ -66,7 +66,9 @@ struct Args {
     Mat<S> out_h, out_y, grad_x, grad_u, grad_gate;
     const float *gamma_u, *gamma_y;
     float *rstd_u, *rstd_h;             // written forward, read backward
-    int32_t rows, cols, norm_u, each;   // each: a gate for every row; else rows come in `sets` of `points`, a gate (or none) to a set
+    int32_t rows, cols, norm_u;
+    bool given_h;                       // backward: x is h itself
+    int32_t each;                       // a gate for every row; else rows come in `sets` of `points`, a gate (or none) to a set
     int64_t sets, points;
     float scale, eps, per_cols;
     int64_t chunk, chunks;              // backward: rows that a workgroup takes, and how many such a set is
@@ -326,7 +328,8 @@ __global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residua
 
 // ---------------------------------------------------------------- backward
 
-// Eight columns of a row.  h is made again from x and u: as it was rounded to bf16 it would be off by 2^-9 in every term of grad_gamma_y.
+// Eight columns of a row.  h is made again from x and u: as it was rounded to bf16 it would be off by 2^-9 in every term of grad_gamma_y.  Where the caller has only
+// h (given_h), that is what x holds, and nothing of u goes into it.
 template <typename S, int D, bool FEW>
 struct Piece {
     Columns<S, D, FEW> p;
@@ -347,7 +350,9 @@ struct Piece {
     // What a row is multiplied with; sums() adds up four products of eight columns, which with rstd's left out of them are two instructions each.
     struct Factors {
         float f, rstd_h;                        // scale rstd_u
+        float in_h;                             // f, or 0 where h is given: what the block's part is in h
         float kh, ku;                           // after the sums: rstd_h^2 m1, rstd_u^2 m2
+        __device__ Factors(const Args<S> &a, float rstd_u, float rstd) : f(a.scale * rstd_u), rstd_h(rstd), in_h(a.given_h ? 0.0f : f), kh(0.0f), ku(0.0f) {}
         __device__ void join(const float (&s)[4], bool norm_u, float rstd_u, float per_cols)
         {
             const float m1 = rstd_h * s[0] * per_cols;
@@ -356,7 +361,7 @@ struct Piece {
         }
     };
     template <typename F>
-    __device__ void sums(float (&s)[4], const F &gamma, float f) const
+    __device__ void sums(float (&s)[4], const F &gamma, const Factors &m) const
     {
 #pragma unroll
         for (int k = 0; k < kEight / 2; ++k) {
@@ -365,7 +370,7 @@ struct Piece {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 const int e = 2 * k + q;
-                const float t = p.part(e, gamma_u[q]), h = __builtin_fmaf(f, t, p.x.get(e)), ay = gamma_y[q] * gy.get(e);
+                const float t = p.part(e, gamma_u[q]), h = __builtin_fmaf(m.in_h, t, p.x.get(e)), ay = gamma_y[q] * gy.get(e);
                 s[0] = __builtin_fmaf(ay, h, s[0]);
                 s[1] = __builtin_fmaf(t, gh.get(e), s[1]);
                 s[2] = __builtin_fmaf(t, ay, s[2]);
@@ -386,7 +391,7 @@ struct Piece {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 const int e = 2 * k + q;
-                const float u = p.u.get(e), gate = p.gate.get(e), h = p.stream(e, gamma_u[q], m.f), g = gy.get(e);
+                const float u = p.u.get(e), gate = p.gate.get(e), h = p.stream(e, gamma_u[q], m.in_h), g = gy.get(e);
                 dh[q] = __builtin_fmaf(m.rstd_h, gamma_y[q] * g, __builtin_fmaf(-m.kh, h, gh.get(e)));
                 const float dv = gate * dh[q], v = m.f * u;
                 du[q] = __builtin_fmaf(m.f, gamma_u[q] * dv, -(m.ku * u));
@@ -485,9 +490,9 @@ __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_n
         for (int64_t k = 0; k < count; ++k) {
             Row now;
             fetch(now, t, k);
-            typename Piece<S, D, (G == 4)>::Factors m{a.scale * now.rstd_u, now.rstd_h, 0.0f, 0.0f};
+            typename Piece<S, D, (G == 4)>::Factors m(a, now.rstd_u, now.rstd_h);
             float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            now.p.sums(s, gamma, m.f);
+            now.p.sums(s, gamma, m);
             group_sums<G, 4>(s, red[turn]);
             turn ^= 1;
             m.join(s, a.norm_u, now.rstd_u, a.per_cols);
@@ -583,13 +588,13 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_rows_kernel(A
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const int64_t g = a.gate_of(r);
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
-        typename Piece<S, D, false>::Factors m{a.scale * rstd_u, rstd_h, 0.0f, 0.0f};
+        typename Piece<S, D, false>::Factors m(a, rstd_u, rstd_h);
         float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int c = threadIdx.x * V; c < a.cols; c += kWideThreads * kEight) {
             const int n = a.cols - c;
             Piece<S, D, false> p;
             p.load(a, r, g, c, n);
-            p.sums(s, InRegisters<D>(a, c, n, nullptr), m.f);
+            p.sums(s, InRegisters<D>(a, c, n, nullptr), m);
         }
         group_sums<kWideThreads, 4>(s, red);
         m.join(s, a.norm_u, rstd_u, a.per_cols);
@@ -612,10 +617,11 @@ __global__ void __launch_bounds__(kThreads) residual_norm_wide_map_kernel(Args<S
     for (int e = 0; e < kEight; ++e) sum_y[e] = sum_t[e] = 0.0f;
     for (int64_t r = r0; r < r1; ++r) {
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
-        const float2 m = a.row[r];
+        typename Piece<S, D, false>::Factors m(a, rstd_u, rstd_h);
+        m.kh = a.row[r].x, m.ku = a.row[r].y;
         Piece<S, D, false> p;
         p.load(a, r, a.each ? r : set, c, n);
-        p.leave(a, r, c, n, gamma, {a.scale * rstd_u, rstd_h, m.x, m.y}, sum_y, sum_t);
+        p.leave(a, r, c, n, gamma, m, sum_y, sum_t);
     }
     spread_sums<D>(a, set, c, gamma, sum_t, gates, sum_u);
     const int64_t at = block * a.cols + c;
@@ -854,6 +860,49 @@ __global__ void __launch_bounds__(kThreads) residual_norm_zero_kernel(float *a, 
     if (b) b[t] = 0.0f;
 }
 
+dol_status backward(bool given_h, const dol_matrix *x, const dol_matrix *u, int32_t norm_u, const float *gamma_u, const dol_matrix *gate, float scale,
+                    const float *gamma_y, const float *rstd_u, const float *rstd_h, const dol_matrix *grad_h, const dol_matrix *grad_y,
+                    const dol_matrix *grad_x, const dol_matrix *grad_u, float *grad_gamma_u, const dol_matrix *grad_gate, float *grad_gamma_y,
+                    void *workspace, int64_t workspace_bytes, void *hip_stream)
+{
+    if (dol_status s = check_call(u, gate)) return s;
+    for (const auto &m : {std::make_pair(x, given_h ? "h" : "x"), std::make_pair(grad_h, "grad_h"), std::make_pair(grad_y, "grad_y"), std::make_pair(grad_x, "grad_x"),
+                          std::make_pair(grad_u, "grad_u")})
+        if (dol_status s = check_like(m.first, u, m.second)) return s;
+    if (!grad_x && !grad_u && !grad_gamma_u && !grad_gate && !grad_gamma_y) return fail(DOL_EINVAL, "no gradient is asked for");
+    if ((gamma_u || grad_gamma_u) && !norm_u) return fail(DOL_EINVAL, "gamma_u or grad_gamma_u without norm_u");
+    if (grad_gate) {
+        if (!gate) return fail(DOL_EINVAL, "grad_gate without gate");
+        if (dol_status s = check_matrix(grad_gate, "grad_gate")) return s;
+        if (grad_gate->dtype != u->dtype) return fail(DOL_EINVAL, "grad_gate is of another type than u");
+        if (grad_gate->rows != gate->rows || grad_gate->cols != gate->cols)
+            return fail(DOL_ESHAPE, "grad_gate is %d x %d, not %d x %d", grad_gate->rows, grad_gate->cols, gate->rows, gate->cols);
+        for (const dol_matrix *m : {x, u, gate, grad_h, grad_y, grad_x, grad_u})
+            if (on_top(grad_gate, m)) return fail(DOL_EINVAL, "grad_gate is another operand's or result's memory");
+    }
+    if (on_top(grad_x, grad_u) || on_top(grad_x, gate) || on_top(grad_u, gate)) return fail(DOL_EINVAL, "two of grad_x, grad_u and gate are the same");
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (u->rows == 0) {                     // sums over nothing
+        if (grad_gate && grad_gate->rows > 0) return fail(DOL_ESHAPE, "%d gates for no rows", grad_gate->rows);
+        residual_norm_zero_kernel<<<(u->cols + kThreads - 1) / kThreads, kThreads, 0, st>>>(grad_gamma_u, grad_gamma_y, u->cols);
+        DOL_HIP(hipGetLastError());
+        return DOL_OK;
+    }
+    if (norm_u && !rstd_u) return fail(DOL_EINVAL, "rstd_u is NULL");
+    if (grad_y && !rstd_h) return fail(DOL_EINVAL, "rstd_h is NULL");
+    if (grad_y && given_h && !x) return fail(DOL_EINVAL, "h is NULL");
+    auto go = [&](auto type) {
+        using S = decltype(type);
+        const Plan p = plan_of(u, gate, workspace);
+        if (dol_status s = check_workspace(workspace, workspace_bytes, p.bytes)) return s;
+        Args<S> a = args_of<S>(u, norm_u, gamma_u, gate, scale, gamma_y);
+        a.given_h = given_h, a.x = in_of<S>(x), a.grad_h = in_of<S>(grad_h), a.grad_y = in_of<S>(grad_y), a.grad_x = out_of<S>(grad_x), a.grad_u = out_of<S>(grad_u);
+        a.rstd_u = const_cast<float *>(rstd_u), a.rstd_h = const_cast<float *>(rstd_h);
+        return reverse<S>(p, a, grad_gamma_u, grad_gate, grad_gamma_y, st);
+    };
+    return u->dtype == DOL_F32 ? go(0.0f) : go(static_cast<__bf16>(0.0f));
+}
+
 }  // namespace
 }  // namespace dol
 
@@ -894,41 +943,17 @@ dol_status dol_residual_norm_backward(const dol_matrix *x, const dol_matrix *u, 
                                       const dol_matrix *grad_x, const dol_matrix *grad_u, float *grad_gamma_u, const dol_matrix *grad_gate, float *grad_gamma_y,
                                       void *workspace, int64_t workspace_bytes, void *hip_stream)
 {
-    if (dol_status s = check_call(u, gate)) return s;
-    for (const auto &m : {std::make_pair(x, "x"), std::make_pair(grad_h, "grad_h"), std::make_pair(grad_y, "grad_y"), std::make_pair(grad_x, "grad_x"),
-                          std::make_pair(grad_u, "grad_u")})
-        if (dol_status s = check_like(m.first, u, m.second)) return s;
-    if (!grad_x && !grad_u && !grad_gamma_u && !grad_gate && !grad_gamma_y) return fail(DOL_EINVAL, "no gradient is asked for");
-    if ((gamma_u || grad_gamma_u) && !norm_u) return fail(DOL_EINVAL, "gamma_u or grad_gamma_u without norm_u");
-    if (grad_gate) {
-        if (!gate) return fail(DOL_EINVAL, "grad_gate without gate");
-        if (dol_status s = check_matrix(grad_gate, "grad_gate")) return s;
-        if (grad_gate->dtype != u->dtype) return fail(DOL_EINVAL, "grad_gate is of another type than u");
-        if (grad_gate->rows != gate->rows || grad_gate->cols != gate->cols)
-            return fail(DOL_ESHAPE, "grad_gate is %d x %d, not %d x %d", grad_gate->rows, grad_gate->cols, gate->rows, gate->cols);
-        for (const dol_matrix *m : {x, u, gate, grad_h, grad_y, grad_x, grad_u})
-            if (on_top(grad_gate, m)) return fail(DOL_EINVAL, "grad_gate is another operand's or result's memory");
-    }
-    if (on_top(grad_x, grad_u) || on_top(grad_x, gate) || on_top(grad_u, gate)) return fail(DOL_EINVAL, "two of grad_x, grad_u and gate are the same");
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (u->rows == 0) {                     // sums over nothing
-        if (grad_gate && grad_gate->rows > 0) return fail(DOL_ESHAPE, "%d gates for no rows", grad_gate->rows);
-        residual_norm_zero_kernel<<<(u->cols + kThreads - 1) / kThreads, kThreads, 0, st>>>(grad_gamma_u, grad_gamma_y, u->cols);
-        DOL_HIP(hipGetLastError());
-        return DOL_OK;
-    }
-    if (norm_u && !rstd_u) return fail(DOL_EINVAL, "rstd_u is NULL");
-    if (grad_y && !rstd_h) return fail(DOL_EINVAL, "rstd_h is NULL");
-    auto go = [&](auto type) {
-        using S = decltype(type);
-        const Plan p = plan_of(u, gate, workspace);
-        if (dol_status s = check_workspace(workspace, workspace_bytes, p.bytes)) return s;
-        Args<S> a = args_of<S>(u, norm_u, gamma_u, gate, scale, gamma_y);
-        a.x = in_of<S>(x), a.grad_h = in_of<S>(grad_h), a.grad_y = in_of<S>(grad_y), a.grad_x = out_of<S>(grad_x), a.grad_u = out_of<S>(grad_u);
-        a.rstd_u = const_cast<float *>(rstd_u), a.rstd_h = const_cast<float *>(rstd_h);
-        return reverse<S>(p, a, grad_gamma_u, grad_gate, grad_gamma_y, st);
-    };
-    return u->dtype == DOL_F32 ? go(0.0f) : go(static_cast<__bf16>(0.0f));
+    return backward(false, x, u, norm_u, gamma_u, gate, scale, gamma_y, rstd_u, rstd_h, grad_h, grad_y, grad_x, grad_u, grad_gamma_u, grad_gate, grad_gamma_y, workspace,
+                    workspace_bytes, hip_stream);
+}
+
+dol_status dol_residual_norm_backward_from_h(const dol_matrix *h, const dol_matrix *u, int32_t norm_u, const float *gamma_u, const dol_matrix *gate, float scale,
+                                             const float *gamma_y, const float *rstd_u, const float *rstd_h, const dol_matrix *grad_h, const dol_matrix *grad_y,
+                                             const dol_matrix *grad_x, const dol_matrix *grad_u, float *grad_gamma_u, const dol_matrix *grad_gate, float *grad_gamma_y,
+                                             void *workspace, int64_t workspace_bytes, void *hip_stream)
+{
+    return backward(true, h, u, norm_u, gamma_u, gate, scale, gamma_y, rstd_u, rstd_h, grad_h, grad_y, grad_x, grad_u, grad_gamma_u, grad_gate, grad_gamma_y, workspace,
+                    workspace_bytes, hip_stream);
 }
 
 }  // extern "C"
