@@ -229,16 +229,12 @@ def _plain_clip(s):
 def _own_linear(s):
     from paper_2410_03348_amd import binding as dol
     z = s["z"] if s["train"] else None
-    if z is not None and z.dtype == torch.bfloat16 and "rest" not in s:
-        s["rest"] = torch.empty(z.shape, dtype=torch.int16, device=DEV)         # kept beside z
-    rest = s.get("rest")
-    dol.linear(s["x"], s["weight"], s["y"], bias=s["bias"], act=s["act"], residual=s["stream"], z=z, z_rest=rest)
+    dol.linear(s["x"], s["weight"], s["y"], bias=s["bias"], act=s["act"], residual=s["stream"], z=z)
     out = {"y": s["y"]}
     if s["train"]:
         if z is not None:
             out["z"] = z
-        dol.linear_backward(s["x"], s["weight"], s["grad_y"], s["grad_x"], s["grad_weight"], grad_bias=s["grad_bias"], act=s["act"], z=z,
-                            z_rest=rest)
+        dol.linear_backward(s["x"], s["weight"], s["grad_y"], s["grad_x"], s["grad_weight"], grad_bias=s["grad_bias"], act=s["act"], z=z)
         out["grad_x"], out["grad_weight"], out["grad_bias"] = s["grad_x"], s["grad_weight"], s["grad_bias"]
     return out
 
@@ -249,7 +245,7 @@ def _own_residual_norm(s):
                       scale=s["scale"], eps=NORM_EPS)
     keys = ["h", "y", "rstd_h"] + (["rstd_u"] if s["post"] else [])
     if s["train"]:
-        dol.residual_norm_backward(s["x"], s["u"], s["gamma_u"], s["gates"], s["gamma_y"], s["rstd_u"], s["rstd_h"], s["grad_h"], s["grad_y"],
+        dol.residual_norm_backward(s["u"], s["gamma_u"], s["gates"], s["gamma_y"], s["h"], s["rstd_u"], s["rstd_h"], s["grad_h"], s["grad_y"],
                                    s["grad_x"], s["grad_u"], s["grad_gamma_u"], s["grad_gates"], s["grad_gamma_y"], norm_u=s["post"],
                                    scale=s["scale"])
         keys += ["grad_x", "grad_u", "grad_gamma_y"] + (["grad_gamma_u"] if s["post"] else []) + (["grad_gates"] if s["gates"] is not None else [])
