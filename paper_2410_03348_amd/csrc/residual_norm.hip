@@ -351,13 +351,13 @@ struct Piece {
     struct Factors {
         float f, rstd_h;                        // scale rstd_u
         float in_h;                             // f, or 0 where h is given: what the block's part is in h
-        float kh, ku;                           // after the sums: rstd_h^2 m1, rstd_u^2 m2
-        __device__ Factors(const Args<S> &a, float rstd_u, float rstd) : f(a.scale * rstd_u), rstd_h(rstd), in_h(a.given_h ? 0.0f : f), kh(0.0f), ku(0.0f) {}
+        float kh, kv;                           // after the sums, of hhat and of v = scale uhat: rstd_h m1, and rstd_u m2 / scale
+        __device__ Factors(const Args<S> &a, float rstd_u, float rstd) : f(a.scale * rstd_u), rstd_h(rstd), in_h(a.given_h ? 0.0f : f), kh(0.0f), kv(0.0f) {}
         __device__ void join(const float (&s)[4], bool norm_u, float rstd_u, float per_cols)
         {
-            const float m1 = rstd_h * s[0] * per_cols;
-            kh = rstd_h * (rstd_h * m1);
-            ku = norm_u ? rstd_u * rstd_u * (f * per_cols) * __builtin_fmaf(rstd_h, s[2], __builtin_fmaf(-kh, s[3], s[1])) : 0.0f;
+            kh = rstd_h * (rstd_h * (s[0] * per_cols));
+            // (a sum before the rstd that its numbers go with: rstd's by themselves multiply out of a float's range long before any square does)
+            kv = norm_u ? rstd_u * (rstd_u * (per_cols * __builtin_fmaf(rstd_h, s[2], __builtin_fmaf(-kh, rstd_h * s[3], s[1])))) : 0.0f;
         }
     };
     template <typename F>
@@ -392,11 +392,12 @@ struct Piece {
             for (int q = 0; q < 2; ++q) {
                 const int e = 2 * k + q;
                 const float u = p.u.get(e), gate = p.gate.get(e), h = p.stream(e, gamma_u[q], m.in_h), g = gy.get(e);
-                dh[q] = __builtin_fmaf(m.rstd_h, gamma_y[q] * g, __builtin_fmaf(-m.kh, h, gh.get(e)));
+                const float hhat = h * m.rstd_h;
+                dh[q] = __builtin_fmaf(m.rstd_h, gamma_y[q] * g, __builtin_fmaf(-m.kh, hhat, gh.get(e)));
                 const float dv = gate * dh[q], v = m.f * u;
-                du[q] = __builtin_fmaf(m.f, gamma_u[q] * dv, -(m.ku * u));
+                du[q] = __builtin_fmaf(m.f, gamma_u[q] * dv, -(m.kv * v));
                 dg[q] = gamma_u[q] * (dh[q] * v);
-                sum_y[e] = __builtin_fmaf(g, h * m.rstd_h, sum_y[e]);
+                sum_y[e] = __builtin_fmaf(g, hhat, sum_y[e]);
                 sum_t[e] = __builtin_fmaf(a.each ? dv : dh[q], v, sum_t[e]);
             }
             ox.set(k, dh[0], dh[1]), ou.set(k, du[0], du[1]), og.set(k, dg[0], dg[1]);
@@ -598,7 +599,7 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_rows_kernel(A
         }
         group_sums<kWideThreads, 4>(s, red);
         m.join(s, a.norm_u, rstd_u, a.per_cols);
-        if (threadIdx.x == 0) a.row[r] = make_float2(m.kh, m.ku);
+        if (threadIdx.x == 0) a.row[r] = make_float2(m.kh, m.kv);
         lds_barrier();
     }
 }
@@ -618,7 +619,7 @@ __global__ void __launch_bounds__(kThreads) residual_norm_wide_map_kernel(Args<S
     for (int64_t r = r0; r < r1; ++r) {
         const float rstd_u = a.norm_u ? a.rstd_u[r] : 1.0f, rstd_h = a.grad_y.p ? a.rstd_h[r] : 0.0f;
         typename Piece<S, D, false>::Factors m(a, rstd_u, rstd_h);
-        m.kh = a.row[r].x, m.ku = a.row[r].y;
+        m.kh = a.row[r].x, m.kv = a.row[r].y;
         Piece<S, D, false> p;
         p.load(a, r, a.each ? r : set, c, n);
         p.leave(a, r, c, n, gamma, m, sum_y, sum_t);
