@@ -853,12 +853,16 @@ dol_status reverse(const Plan &p, Args<S> a, float *grad_gamma_u, const dol_matr
     return DOL_OK;
 }
 
-__global__ void __launch_bounds__(kThreads) residual_norm_zero_kernel(float *a, float *b, int32_t n)
+// Sums over no rows.
+template <typename S>
+__global__ void __launch_bounds__(kThreads) residual_norm_zero_kernel(float *a, float *b, Mat<S> gates, int64_t count, int32_t n)
 {
-    const int t = blockIdx.x * kThreads + threadIdx.x;
-    if (t >= n) return;
-    if (a) a[t] = 0.0f;
-    if (b) b[t] = 0.0f;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (t < n) {
+        if (a) a[t] = 0.0f;
+        if (b) b[t] = 0.0f;
+    }
+    for (int64_t k = t; k < count * n; k += static_cast<int64_t>(gridDim.x) * kThreads) *gates.at(k / n, static_cast<int>(k % n)) = static_cast<S>(0.0f);
 }
 
 dol_status backward(bool given_h, const dol_matrix *x, const dol_matrix *u, int32_t norm_u, const float *gamma_u, const dol_matrix *gate, float scale,
@@ -883,11 +887,15 @@ dol_status backward(bool given_h, const dol_matrix *x, const dol_matrix *u, int3
     }
     if (on_top(grad_x, grad_u) || on_top(grad_x, gate) || on_top(grad_u, gate)) return fail(DOL_EINVAL, "two of grad_x, grad_u and gate are the same");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (u->rows == 0) {                     // sums over nothing
-        if (grad_gate && grad_gate->rows > 0) return fail(DOL_ESHAPE, "%d gates for no rows", grad_gate->rows);
-        residual_norm_zero_kernel<<<(u->cols + kThreads - 1) / kThreads, kThreads, 0, st>>>(grad_gamma_u, grad_gamma_y, u->cols);
-        DOL_HIP(hipGetLastError());
-        return DOL_OK;
+    if (u->rows == 0) {
+        auto zero = [&](auto type) {
+            using S = decltype(type);
+            const int64_t gates = grad_gate ? grad_gate->rows : 0, blocks = (std::max<int64_t>(gates, 1) * u->cols + kThreads - 1) / kThreads;
+            residual_norm_zero_kernel<S><<<static_cast<unsigned>(std::min<int64_t>(blocks, kMostCols / kThreads)), kThreads, 0, st>>>(grad_gamma_u, grad_gamma_y, out_of<S>(grad_gate), gates, u->cols);
+            DOL_HIP(hipGetLastError());
+            return DOL_OK;
+        };
+        return u->dtype == DOL_F32 ? zero(0.0f) : zero(static_cast<__bf16>(0.0f));
     }
     if (norm_u && !rstd_u) return fail(DOL_EINVAL, "rstd_u is NULL");
     if (grad_y && !rstd_h) return fail(DOL_EINVAL, "rstd_h is NULL");
