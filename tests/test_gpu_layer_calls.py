@@ -1,10 +1,51 @@
-"""Calls of linear layers and of norms between blocks that the other tests do not make (needs an MI355X)."""
+"""Calls of linear layers and of norms between blocks that the other tests do not make (needs an MI355X).
+
+Bars of the linear layer's as in test_gpu_linear.py.  Against the exact z, from which z as the call is given it is off by e_z (L + 2^-8 |z|, with z_rest
+L + 2^-23 |z|), each dz is off by |g| e_z more, the second derivative of an activation function being below 1 (gelu's is 0.8 at 0); relu's slope is that of a
+z of the same sign, which rounding leaves.
+"""
 import pytest
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
-from test_gpu_residual_norm import dol  # noqa: E402,F401
+import test_gpu_linear as lin  # noqa: E402
+from test_gpu_linear import U, W8, act_of, dol, make, within  # noqa: E402,F401
+
+
+def check_at_exact_z(c, act, rest, got):
+    x, w, g = c["x"].double(), c["w"].double(), c["g"].double()
+    z = x @ w.t()
+    e = 16 * U * (x.abs() @ w.t().abs())
+    if c["b"] is not None:
+        z = z + c["b"].double()
+        e = e + U * z.abs()
+    half = W8 if c["x"].dtype == torch.bfloat16 else 0.0
+    e = e + (2.0 ** -23 if rest is not None else half) * z.abs()
+    slope = act_of(z, act)[1]
+    dz = g * slope
+    off = torch.zeros_like(g) if act in ("none", "relu") else 16 * U * (1 + z * z) * g.abs() * (1 + slope.abs()) + g.abs() * e
+    keep = 1 if act != "relu" else (z.abs() > e).double()           # (relu: what lies nearer to 0 than z is off may be on either side)
+    off = off + (0 if act != "relu" else (1 - keep) * g.abs())
+    for name, t, a, d, k in (("grad_x", got[0], w, dz, off), ("grad_weight", got[1], x, dz.t(), off.t())):
+        size = d.abs() @ a.abs()
+        rounding = (half if x.shape[0] > 512 else W8 * half) if act != "none" else 0.0
+        bar, want = size * (16 * U + rounding) + k @ a.abs() * (1 + half), d @ a
+        within(t, want, bar + half * (want.abs() + bar) + 1e-37, name)
+    within(got[2], dz.sum(0), dz.abs().sum(0) * 16 * U + off.sum(0) + 1e-37, "grad_bias")
+
+
+@pytest.mark.parametrize("n,d,m", [(1, 300, 70), (5, 200, 70), (40, 2101, 2100), (64, 300, 33), (130, 200, 70), (600, 64, 128), (1000, 513, 300)])
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+def test_bf16_gradients_with_and_without_what_rounding_z_left(dol, n, d, m, act):
+    """Without z_rest the gradients are those at z as it was rounded; either way at the exact z within what z is off there."""
+    c = make(n, d, m, torch.bfloat16, seed=n + m)
+    for kept in (False, True):
+        y, z, rest = lin.forward(dol, c, act, rest=kept)
+        assert (rest is not None) == kept
+        got = lin.backward(dol, c, act, z, rest)
+        lin.check_backward(c, act, z, rest, got)
+        check_at_exact_z(c, act, rest, got)
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
