@@ -495,14 +495,15 @@ dol_status dol_group_norm_backward(const dol_activations *x, int32_t groups, con
  *   x         [rows, width],   weight  [out, width], same type
  *   bias      device [out] or NULL
  *   residual  [rows, out] or NULL, of the type of x
- *   y         [rows, out], of the type of x; may be the residual, not x or weight
- *   z         [rows, out] or NULL, of the type of x: what the gradients need where act is not DOL_ACT_NONE; not y
+ *   y         [rows, out], of the type of x; may be the residual, each row in its own place
+ *   z         [rows, out] or NULL, of the type of x: what the gradients need where act is not DOL_ACT_NONE
  *   z_rest    device [rows, out] or NULL, only with z in DOL_BF16: what rounding z has left, in steps of a float.  With it the slopes that
  *             grad_bias sums up are a float's, without it off by some 2^-9 each
  * (DOL_F32 multiplies in parts of numbers where it takes tiles (dol_linear_kernel), as grad_weight always does: an infinity in an operand
  * makes the sums that it is in NaN, and numbers below 2^-109 lose their last bits.  In DOL_BF16 an infinity in x or weight may do so to the
  * gradients that it is in.)
- * At most 2^22 rows and outs and 2^20 elements of a row (else DOL_EUNSUPPORTED); at least one out of one element. */
+ * No result may lie over an operand or over another result, not over a part of it either (DOL_EINVAL), but where it says so above; columns of one
+ * buffer side by side do not.  At most 2^22 rows and outs and 2^20 elements of a row (else DOL_EUNSUPPORTED); at least one out of one element. */
 dol_status dol_linear_workspace(const dol_matrix *x, const dol_matrix *weight, int32_t backward, int64_t *bytes);
 /* As dol_cross_entropy_kernel: "linear_few_kernel 16x16" (rows and outs), "linear_tiles_kernel 128x128x64", backward (what grad_x is made by)
  * "linear_few_back_kernel 16", "linear_products_kernel 64x64x64". */
@@ -513,7 +514,7 @@ dol_status dol_linear(const dol_matrix *x, const dol_matrix *weight, const float
 /* Its gradients, dz = grad_y act'(z):
  *   grad_x = dz weight,   grad_weight = dz^T x,   grad_bias[o] = sum_i dz[i, o];   the residual's is grad_y itself.
  * z and z_rest as the forward call left them, ignored with DOL_ACT_NONE.  Each gradient is OVERWRITTEN, of the type of x (grad_bias: float), none of them
- * an operand's own memory; any may be NULL.  Sums are taken in a fixed order: two runs give the same bits.  rows == 0 writes zeros.
+ * over an operand or another; any may be NULL.  Sums are taken in a fixed order: two runs give the same bits.  rows == 0 writes zeros.
  * DOL_BF16 above 512 rows rounds dz to bf16 before the two products; up to 512 rows dz keeps 16 bits. */
 dol_status dol_linear_backward(const dol_matrix *x, const dol_matrix *weight, int32_t act, const dol_matrix *z, const int16_t *z_rest,
                                const dol_matrix *grad_y, const dol_matrix *grad_x, const dol_matrix *grad_weight, float *grad_bias,
@@ -528,9 +529,10 @@ dol_status dol_linear_backward(const dol_matrix *x, const dol_matrix *weight, in
  *   gamma_u, gamma_y  device [cols] or NULL = 1
  *   gate      [gates, cols] or NULL = 1, of the type of u; gates divides rows, and row i has gate i / (rows / gates): one for all rows, one
  *             for a sample of neighbouring rows, or one for each row
- *   h, y      [rows, cols], of the type of u; either may be NULL, and either may be x or u
+ *   h, y      [rows, cols], of the type of u; either may be NULL, and either may be x or u, each row in its own place
  *   rstd_u, rstd_h  device [rows], written where not NULL, rstd_u with norm_u and rstd_h with y (the gradients need them)
- * At least one column, and at most 2^24; numbers whose squares pass a float's range are off its definition. */
+ * Results lie over nothing else of the call (DOL_EINVAL).  At least one column, and at most 2^24; numbers whose squares pass a float's
+ * range are off its definition. */
 dol_status dol_residual_norm(const dol_matrix *x, const dol_matrix *u, int32_t norm_u, const float *gamma_u, const dol_matrix *gate,
                              float scale, const float *gamma_y, float eps, const dol_matrix *h, const dol_matrix *y, float *rstd_u,
                              float *rstd_h, void *hip_stream);
@@ -539,8 +541,9 @@ dol_status dol_residual_norm(const dol_matrix *x, const dol_matrix *u, int32_t n
  *   grad_u = rstd_u (gamma_u dv - uhat mean(gamma_u dv uhat)), uhat = u rstd_u, where norm_u is not 0;   dv where it is
  *   grad_gate[g] = scale sum dh v over the gate's rows,   grad_gamma_u = sum dv uhat,   grad_gamma_y = sum grad_y hhat over all rows.
  * x, u, gamma_u, gate, scale, gamma_y as in, rstd_u and rstd_h from the forward call (rstd_h only with grad_y, rstd_u only with norm_u); h is
- * made again from them, unrounded.  Each is OVERWRITTEN and may be NULL; grad_x and grad_u, each its own, may be grad_h, grad_y, x or u.
- * Sums are taken in a fixed order: two runs give the same bits.
+ * made again from them, unrounded.  Each is OVERWRITTEN and may be NULL; grad_x and grad_u, each its own, may be grad_h, grad_y, x or u, each row
+ * in its own place.  Where else a matrix shares memory with a result the call is refused (DOL_EINVAL).  Sums are taken in a fixed order: two runs
+ * give the same bits.
  * dol_residual_norm_backward_from_h, for a program that keeps what is behind the block and not x: the same gradients at h as the forward call has
  * left it (NULL only without grad_y; grad_x and grad_u may be h).  In DOL_F32 they are as exact; h in DOL_BF16 has lost up to 2^-8 of each number, and with it so
  * has each of the terms that grad_gamma_y adds up: a bf16 program that wants that sum as exact as the others keeps x. */

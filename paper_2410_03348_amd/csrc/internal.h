@@ -24,8 +24,34 @@ dol_status hip_fail(hipError_t e, const char *what);
 // Checks of the training operators' arguments (cross_entropy.hip).
 dol_status check_matrix(const dol_matrix *m, const char *name);
 dol_status check_workspace(const void *workspace, int64_t has, int64_t needs);
-// A result that would be written over `other`, which the call still reads or writes.
-inline bool on_top(const dol_matrix *result, const dol_matrix *other) { return result && other && result->rows > 0 && result->data == other->data; }
+// What a call reads or writes of memory: `rows` rows of `width` bytes, `pitch` from one to the next.
+struct Span {
+    uint64_t at, rows, pitch, width;
+    Span(const dol_matrix *m) : at(0), rows(0), pitch(0), width(0)
+    {
+        if (!m || m->rows < 1 || m->cols < 1) return;
+        const uint64_t size = m->dtype == DOL_F32 ? 4 : 2;
+        at = reinterpret_cast<uintptr_t>(m->data), rows = m->rows, pitch = m->ld * size, width = m->cols * size;
+    }
+    Span(const void *p, uint64_t bytes) : at(reinterpret_cast<uintptr_t>(p)), rows(p && bytes ? 1 : 0), pitch(0), width(bytes) {}
+    uint64_t end() const { return at + (rows - 1) * pitch + width; }
+};
+// Whether a result and what else the call reads or writes share memory.  Columns of one buffer side by side do not; what lies between each other's rows in another
+// way counts as shared.
+inline bool meet(const Span &a, const Span &b)
+{
+    if (!a.rows || !b.rows || a.at >= b.end() || b.at >= a.end()) return false;
+    const uint64_t pitch = std::gcd(a.rows > 1 ? a.pitch : 0, b.rows > 1 ? b.pitch : 0);
+    if (!pitch) return true;
+    const uint64_t apart = b.at >= a.at ? (b.at - a.at) % pitch : (pitch - (a.at - b.at) % pitch) % pitch;
+    return apart < a.width || apart + b.width > pitch;
+}
+// The same where a result may be written in the place of what it is made of: each row in its own.
+inline bool cross(const dol_matrix *result, const dol_matrix *other)
+{
+    if (!result || !other || (result->data == other->data && (result->ld == other->ld || result->rows == 1))) return false;
+    return meet(result, other);
+}
 // Whether `outer` sets of `inner` rows of n elements share none: sets one behind the other, or the rows of all sets side by side.
 inline bool apart(int64_t inner, int64_t ld_inner, int64_t outer, int64_t ld_outer, int64_t n)
 {

@@ -905,11 +905,15 @@ dol_status dol_linear(const dol_matrix *x, const dol_matrix *weight, const float
     if (!y) return fail(DOL_EINVAL, "y is NULL");
     for (const auto &m : {std::make_pair(residual, "residual"), std::make_pair(y, "y"), std::make_pair(z, "z")})
         if (dol_status s = check_as(m.first, x->rows, weight->rows, x->dtype, m.second)) return s;
-    for (const dol_matrix *m : {x, weight, z})
-        if (on_top(y, m)) return fail(DOL_EINVAL, "y is x, weight or z");
-    for (const dol_matrix *m : {x, weight, residual})
-        if (on_top(z, m)) return fail(DOL_EINVAL, "z is x, weight or the residual");
     if (z_rest && (!z || x->dtype != DOL_BF16)) return fail(DOL_EINVAL, "z_rest without z in bf16");
+    const Span bias_(bias, weight->rows * sizeof(float)), rest(z_rest, static_cast<uint64_t>(x->rows) * weight->rows * sizeof(int16_t));
+    for (const Span &m : {Span(x), Span(weight), Span(z), bias_, rest})
+        if (meet(y, m)) return fail(DOL_EINVAL, "y is x, weight, z or another operand, or lies over part of it");
+    for (const Span &m : {Span(x), Span(weight), Span(residual), bias_, rest})
+        if (meet(z, m)) return fail(DOL_EINVAL, "z is x, weight, the residual or another operand, or lies over part of it");
+    for (const Span &m : {Span(x), Span(weight), Span(residual), bias_})
+        if (meet(rest, m)) return fail(DOL_EINVAL, "z_rest lies over an operand");
+    if (cross(y, residual)) return fail(DOL_EINVAL, "y lies over the residual, but not each row over its own");
     if (x->rows == 0) return DOL_OK;
     Result o{};
     o.bias = bias, o.act = act, o.rows = x->rows, o.cols = weight->rows, o.y = y->data, o.y_ld = y->ld, o.rest = z_rest;
@@ -937,9 +941,12 @@ dol_status dol_linear_backward(const dol_matrix *x, const dol_matrix *weight, in
     if (dol_status s = check_as(grad_x, x->rows, x->cols, x->dtype, "grad_x")) return s;
     if (dol_status s = check_as(grad_weight, weight->rows, weight->cols, x->dtype, "grad_weight")) return s;
     if (!grad_x && !grad_weight && !grad_bias) return fail(DOL_EINVAL, "no gradient is asked for");
-    for (const dol_matrix *m : {x, weight, z, grad_y})
-        if (on_top(grad_x, m) || on_top(grad_weight, m)) return fail(DOL_EINVAL, "grad_x or grad_weight is x, weight, z or grad_y");
-    if (on_top(grad_x, grad_weight)) return fail(DOL_EINVAL, "grad_x is grad_weight");
+    const Span bias(grad_bias, weight->rows * sizeof(float)), rest(z_rest, static_cast<uint64_t>(x->rows) * weight->rows * sizeof(int16_t));
+    for (const Span &m : {Span(x), Span(weight), Span(z), Span(grad_y), rest}) {
+        if (meet(grad_x, m) || meet(grad_weight, m)) return fail(DOL_EINVAL, "grad_x or grad_weight is x, weight, z or grad_y, or lies over part of it");
+        if (meet(bias, m)) return fail(DOL_EINVAL, "grad_bias lies over an operand");
+    }
+    if (meet(grad_x, grad_weight) || meet(grad_x, bias) || meet(grad_weight, bias)) return fail(DOL_EINVAL, "grad_x, grad_weight and grad_bias lie over each other");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (x->rows == 0) {                     // sums over no rows
         if (dol_status s = x->dtype == DOL_BF16 ? zero<__bf16>(grad_weight, st) : zero<float>(grad_weight, st)) return s;

@@ -883,9 +883,18 @@ dol_status backward(bool given_h, const dol_matrix *x, const dol_matrix *u, int3
         if (grad_gate->rows != gate->rows || grad_gate->cols != gate->cols)
             return fail(DOL_ESHAPE, "grad_gate is %d x %d, not %d x %d", grad_gate->rows, grad_gate->cols, gate->rows, gate->cols);
         for (const dol_matrix *m : {x, u, gate, grad_h, grad_y, grad_x, grad_u})
-            if (on_top(grad_gate, m)) return fail(DOL_EINVAL, "grad_gate is another operand's or result's memory");
+            if (meet(grad_gate, m)) return fail(DOL_EINVAL, "grad_gate is another operand's or result's memory");
     }
-    if (on_top(grad_x, grad_u) || on_top(grad_x, gate) || on_top(grad_u, gate)) return fail(DOL_EINVAL, "two of grad_x, grad_u and gate are the same");
+    if (meet(grad_x, grad_u) || meet(grad_x, gate) || meet(grad_u, gate)) return fail(DOL_EINVAL, "two of grad_x, grad_u and gate are the same, or lie over each other");
+    for (const dol_matrix *m : {x, u, grad_h, grad_y})
+        if (cross(grad_x, m) || cross(grad_u, m)) return fail(DOL_EINVAL, "grad_x or grad_u lies over an operand, but not each row over its own");
+    const uint64_t per_row = u->rows * sizeof(float), per_col = u->cols * sizeof(float);
+    const Span sums_u(grad_gamma_u, per_col), sums_y(grad_gamma_y, per_col);
+    for (const Span &m : {Span(gamma_u, per_col), Span(gamma_y, per_col), Span(norm_u ? rstd_u : nullptr, per_row), Span(grad_y ? rstd_h : nullptr, per_row), sums_u, sums_y})
+        if (meet(grad_x, m) || meet(grad_u, m) || meet(grad_gate, m)) return fail(DOL_EINVAL, "grad_x, grad_u or grad_gate lies over a vector of the call");
+    for (const dol_matrix *m : {x, u, gate, grad_h, grad_y})
+        if (meet(sums_u, m) || meet(sums_y, m)) return fail(DOL_EINVAL, "grad_gamma_u or grad_gamma_y lies over an operand");
+    if (meet(sums_u, sums_y)) return fail(DOL_EINVAL, "grad_gamma_u and grad_gamma_y lie over each other");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (u->rows == 0) {
         auto zero = [&](auto type) {
@@ -926,7 +935,16 @@ dol_status dol_residual_norm(const dol_matrix *x, const dol_matrix *u, int32_t n
     for (const auto &m : {std::make_pair(x, "x"), std::make_pair(h, "h"), std::make_pair(y, "y")})
         if (dol_status s = check_like(m.first, u, m.second)) return s;
     if (!h && !y) return fail(DOL_EINVAL, "neither h nor y is asked for");
-    if (on_top(h, y) || on_top(h, gate) || on_top(y, gate)) return fail(DOL_EINVAL, "two of h, y and gate are the same");
+    if (meet(h, y) || meet(h, gate) || meet(y, gate)) return fail(DOL_EINVAL, "two of h, y and gate are the same, or lie over each other");
+    for (const dol_matrix *m : {x, u})
+        if (cross(h, m) || cross(y, m)) return fail(DOL_EINVAL, "h or y lies over x or u, but not each row over its own");
+    const uint64_t per_row = u->rows * sizeof(float), per_col = u->cols * sizeof(float);
+    const Span of_u(norm_u ? rstd_u : nullptr, per_row), of_h(y ? rstd_h : nullptr, per_row);
+    for (const Span &m : {Span(gamma_u, per_col), Span(gamma_y, per_col), of_u, of_h})
+        if (meet(h, m) || meet(y, m)) return fail(DOL_EINVAL, "h or y lies over a vector of the call");
+    for (const Span &m : {Span(x), Span(u), Span(gate), Span(gamma_u, per_col), Span(gamma_y, per_col)})
+        if (meet(of_u, m) || meet(of_h, m)) return fail(DOL_EINVAL, "rstd_u or rstd_h lies over an operand");
+    if (meet(of_u, of_h)) return fail(DOL_EINVAL, "rstd_u and rstd_h lie over each other");
     if (gamma_u && !norm_u) return fail(DOL_EINVAL, "gamma_u without norm_u");
     if (!(eps >= 0.0f)) return fail(DOL_EINVAL, "eps = %g is not a number of at least 0", static_cast<double>(eps));
     if (u->rows == 0) return DOL_OK;

@@ -66,3 +66,43 @@ def test_no_rows_leave_a_gate_without_gradient(dol, gates, dtype):
     gg.fill_(5.0)
     dol.residual_norm_backward(u, u, None, gate, None, none, none, u, u, u, u, None, gg, None)
     assert not gg.any()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows", [5, 300])
+def test_operands_and_results_as_columns_of_one_buffer(dol, rows, dtype):
+    """The same bits as in buffers of their own, and every other column as it was; a result that shares a column is refused, in place it is taken."""
+    t = getattr(torch, dtype)
+    c = make(rows, 40, 40, t, seed=rows)
+    y, z, rest = lin.forward(dol, c, "silu")
+    gx, gw, gb = lin.backward(dol, c, "silu", z, rest)
+    buf = torch.full((rows, 300), 7.0, dtype=t, device="cuda")
+    x, r, g, y2, z2, gx2 = (buf[:, 41 * k:41 * k + 40] for k in range(6))
+    for to, v in ((x, c["x"]), (r, c["r"]), (g, c["g"])):
+        to.copy_(v)
+    dol.linear(x, c["w"], y2, bias=c["b"], act="silu", residual=r, z=z2, z_rest=None if rest is None else rest.clone())
+    gw2, gb2 = torch.empty_like(gw), torch.empty_like(gb)
+    dol.linear_backward(x, c["w"], g, gx2, gw2, grad_bias=gb2, act="silu", z=z2, z_rest=rest)
+    for a, b in ((y, y2), (z, z2), (gx, gx2), (gw, gw2), (gb, gb2)):
+        assert torch.equal(a, b)
+    with pytest.raises(dol.DolError, match="y is x"):
+        dol.linear(x, c["w"], buf[:, 1:41], act="silu", residual=r)
+    dol.linear(x, c["w"], r, bias=c["b"], act="silu", residual=r)
+    assert torch.equal(r, y)
+    r.copy_(c["r"])
+    # x, u, grad_h, grad_y and h, y, grad_x, grad_u
+    h, v, ru, rh = torch.empty_like(y), torch.empty_like(y), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    dol.residual_norm(c["r"], c["g"], None, None, None, h, v, ru, rh)
+    dol.residual_norm(r, g, None, None, None, y2, z2, ru, rh)
+    assert torch.equal(h, y2) and torch.equal(v, z2)
+    a, b = torch.empty_like(y), torch.empty_like(y)
+    dol.residual_norm_backward(c["r"], c["g"], None, None, None, ru, rh, h, v, a, b, None, None, None)
+    dol.residual_norm_backward(r, g, None, None, None, ru, rh, y2, z2, gx2, x, None, None, None)
+    assert torch.equal(a, gx2) and torch.equal(b, x)
+    with pytest.raises(dol.DolError, match="own"):
+        dol.residual_norm_backward(r, g, None, None, None, ru, rh, y2, z2, buf[:, 42:82], x, None, None, None)
+    dol.residual_norm_backward(r, g, None, None, None, ru, rh, y2, z2, z2, r, None, None, None)
+    assert torch.equal(a, z2) and torch.equal(b, r)
+    for to in (x, r, g, y2, z2, gx2):
+        to.fill_(7.0)
+    assert bool((buf == 7).all())
