@@ -499,9 +499,9 @@ dol_status dol_group_norm_backward(const dol_activations *x, int32_t groups, con
  *   z         [rows, out] or NULL, of the type of x: what the gradients need where act is not DOL_ACT_NONE
  *   z_rest    device [rows, out] or NULL, only with z in DOL_BF16: what rounding z has left, in steps of a float.  With it the slopes that
  *             grad_bias sums up are a float's, without it off by some 2^-9 each
- * (DOL_F32 multiplies in parts of numbers where it takes tiles (dol_linear_kernel), as grad_weight always does: an infinity in an operand
- * makes the sums that it is in NaN, and numbers below 2^-109 lose their last bits.  In DOL_BF16 an infinity in x or weight may do so to the
- * gradients that it is in.)
+ * (DOL_F32 multiplies in parts of numbers where it takes tiles (dol_linear_kernel), as grad_weight always does: numbers below 2^-109 lose their
+ * last bits.  An infinity in an operand makes the sums that it is in infinite, or NaN where what it meets is a zero (in tiles any number below 2^-126 may be) or
+ * another infinity of the other sign; in gradients it may make them NaN, and no others.)
  * No result may lie over an operand or over another result, not over a part of it either (DOL_EINVAL), but where it says so above; columns of one
  * buffer side by side do not.  At most 2^22 rows and outs and 2^20 elements of a row (else DOL_EUNSUPPORTED); at least one out of one element. */
 dol_status dol_linear_workspace(const dol_matrix *x, const dol_matrix *weight, int32_t backward, int64_t *bytes);

@@ -278,8 +278,8 @@ __global__ void __launch_bounds__(few_waves(R * M) * 64) linear_few_kernel(const
 template <typename S, int P>
 __global__ void __launch_bounds__(256) linear_pack_kernel(Pack p0, Pack p1)
 {
-    if (blockIdx.x < p0.blocks) pack_rows<S, P>(p0, blockIdx.x);
-    else pack_rows<S, P>(p1, blockIdx.x - p0.blocks);
+    if (blockIdx.x < p0.blocks) pack_rows<S, P, true>(p0, blockIdx.x);
+    else pack_rows<S, P, true>(p1, blockIdx.x - p0.blocks);
 }
 
 // dz in Q planes, zeros behind its columns and in rows past the last, and its sums over rows.

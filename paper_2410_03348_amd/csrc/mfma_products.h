@@ -77,8 +77,18 @@ struct Pack {
     unsigned blocks;            // none where the matrix is read as it is
 };
 
-// This workgroup's share (of 256 threads, eight elements to each at a time).
-template <typename S, int P>
+// Plane k of three, an infinity as 1, 0 and itself with its sign: of its products with another number's planes (none of the dropped ones among them) the
+// one with that number's first plane is infinite, or NaN beside a zero, and the others are finite or the same infinity, as the product of the two is.  (With
+// itself as the plane that plane_of gives it, it meets what is left of the other number, whose sign may be another: NaN.)
+__device__ __forceinline__ uint32_t plane_or_infinity(int k, float &x)
+{
+    if (!__builtin_isinf(x)) return plane_of<3>(k, x);
+    const uint32_t sign = __float_as_uint(x) >> 16 & 0x8000;
+    return k == 0 ? sign | 0x3F80 : k == 1 ? 0 : sign | 0x7F80;
+}
+
+// This workgroup's share (of 256 threads, eight elements to each at a time).  INF: products with infinities are infinities.
+template <typename S, int P, bool INF = false>
 __device__ __forceinline__ void pack_rows(const Pack &p, unsigned block)
 {
     const int64_t per = p.kp / 8, all = p.out_rows * per;
@@ -100,7 +110,8 @@ __device__ __forceinline__ void pack_rows(const Pack &p, unsigned block)
             u32x4 w;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const uint32_t lo = plane_of<P>(q, v[2 * k]), hi = plane_of<P>(q, v[2 * k + 1]);
+                auto plane = [&](float &x) { return INF && P == 3 ? plane_or_infinity(q, x) : plane_of<P>(q, x); };
+                const uint32_t lo = plane(v[2 * k]), hi = plane(v[2 * k + 1]);
                 w[k] = lo | hi << 16;
             }
             *reinterpret_cast<u32x4 *>(p.out + (q * p.out_rows + r) * p.out_ld + c) = w;

@@ -106,3 +106,28 @@ def test_operands_and_results_as_columns_of_one_buffer(dol, rows, dtype):
     for to in (x, r, g, y2, z2, gx2):
         to.fill_(7.0)
     assert bool((buf == 7).all())
+
+
+# one for each form of the forward call in float: few rows, and tiles in one share of k or several
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,d,m", [(1, 300, 70), (64, 300, 33), (65, 300, 1100), (300, 100, 300), (300, 777, 150), (1500, 100, 1500), (257, 65, 3)])
+def test_infinities_forward_do_not_go_by_the_number_of_rows(dol, n, d, m, dtype):
+    """z is infinite, NaN and finite where the sums in 64 bits are, whatever computes it: infinities of either sign beside numbers of many bits, large ones
+    among them, a zero, each other and a NaN."""
+    t = getattr(torch, dtype)
+    c = make(n, d, m, t, seed=n)
+    x, w = c["x"], c["w"]
+    w[0] *= 1e4
+    x[0, 5], x[n - 1, 7], x[n // 2, d - 1] = float("inf"), float("-inf"), float("inf")
+    w[m - 1, 3], w[1, 5], w[2, 5], w[2, 9] = float("-inf"), 0.0, float("-inf"), float("inf")
+    x[n // 3, 20] = float("nan")
+    y, z, _ = lin.forward(dol, dict(c, r=None), "none")
+    want = x.double().cpu() @ w.double().cpu().t() + c["b"].double().cpu()
+    got = z.double().cpu()
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+    assert torch.equal(got[want.isinf()], want[want.isinf()]) and torch.equal(y.isnan(), z.isnan())
+    finite = want.isfinite()
+    xs, ws = (v.double().cpu().nan_to_num(0.0, 0.0, 0.0) for v in (x, w))
+    L = 16 * U * (xs.abs() @ ws.abs().t()) + U * want.abs()
+    half = W8 if dtype == "bfloat16" else 0.0
+    assert bool(((got - want).abs() <= L + half * (want.abs() + L) + 1e-37)[finite].all())
