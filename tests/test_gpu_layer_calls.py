@@ -131,3 +131,16 @@ def test_infinities_forward_do_not_go_by_the_number_of_rows(dol, n, d, m, dtype)
     L = 16 * U * (xs.abs() @ ws.abs().t()) + U * want.abs()
     half = W8 if dtype == "bfloat16" else 0.0
     assert bool(((got - want).abs() <= L + half * (want.abs() + L) + 1e-37)[finite].all())
+
+
+@pytest.mark.parametrize("n,d,m", [(100, 100, 100), (600, 200, 130), (1, 2100, 2100), (40, 2101, 2100), (64, 64, 70)])
+def test_infinities_in_float_stay_in_their_gradients(dol, n, d, m):
+    c = make(n, d, m, torch.float32, seed=6)
+    c["x"][n - 1, 5], c["w"][m - 1, 3] = float("inf"), float("-inf")
+    gx, gw, gb = lin.backward(dol, c, "none", None, None)
+    off = torch.zeros(n, d, dtype=torch.bool, device="cuda")
+    off[:, 3] = True
+    assert torch.equal(~gx.isfinite(), off) and bool(gb.isfinite().all())
+    off = torch.zeros(m, d, dtype=torch.bool, device="cuda")
+    off[:, 5] = True
+    assert torch.equal(~gw.isfinite(), off)
