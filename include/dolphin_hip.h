@@ -497,8 +497,9 @@ dol_status dol_group_norm_backward(const dol_activations *x, int32_t groups, con
  *   residual  [rows, out] or NULL, of the type of x
  *   y         [rows, out], of the type of x; may be the residual, each row in its own place
  *   z         [rows, out] or NULL, of the type of x: what the gradients need where act is not DOL_ACT_NONE
- *   z_rest    device [rows, out] or NULL, only with z in DOL_BF16: what rounding z has left, in steps of a float.  With it the slopes that
- *             grad_bias sums up are a float's, without it off by some 2^-9 each
+ *   z_rest    device [rows, out] or NULL, only with z in DOL_BF16: what rounding z has left, in steps of a float.  A training program keeps
+ *             it: with it grad_bias is a float's sum of a float's slopes (1.6e-7 in the norm over 4 096 rows), without it the slopes are those
+ *             at z as it was rounded, off by some 2^-9 each (5.6e-4)
  * (DOL_F32 multiplies in parts of numbers where it takes tiles (dol_linear_kernel), as grad_weight always does: numbers below 2^-109 lose their
  * last bits.  An infinity in an operand makes the sums that it is in infinite, or NaN where what it meets is a zero (in tiles any number below 2^-126 may be) or
  * another infinity of the other sign; in gradients it may make them NaN, and no others.)
@@ -570,7 +571,7 @@ void dol_tensor_list_destroy(dol_tensor_list *list);
  * fixed order.  A buffer that is in the list twice counts twice. */
 dol_status dol_grad_norm_workspace(const dol_tensor_list *grads, int64_t *bytes);
 dol_status dol_grad_norm(const dol_tensor_list *grads, float *norm, void *workspace, int64_t workspace_bytes, void *hip_stream);
-/* Clipping by it:  coef[0] = min(1, max_norm / (norm + eps)),   out = coef grads, each element rounded once.
+/* Clipping by it:  coef[0] = min(1, max_norm / (norm + eps)), a float;   out = coef grads, products in 32 bits.
  *   out         a list of the same types and sizes, or `grads` itself (in place).  No two buffers of either list share memory, nor a
  *               buffer of `grads` with another than its own of `out` (DOL_EINVAL)
  *   norm, coef  device [1], both written.  A norm that is not finite leaves max_norm / (norm + eps) as it comes: NaN makes all of

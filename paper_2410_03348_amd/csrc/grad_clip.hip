@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const Chunk *table
 }
 
 // All of it for a list of few chunks, which the wavefronts hold as they lie: coef and out null, only the norm.  5 buffers of 16 234
-// floats in all 6.6 us from Python, 10 by the two launches of longer lists.
+// floats in all 7.0 us from Python, 10 by the two launches of longer lists.
 __global__ void __launch_bounds__(kSmallThreads) grad_small_kernel(const Chunk *table, const Chunk *out, int chunks, double max_norm, double eps, float *norm, float *coef)
 {
     __shared__ double red[kSmallThreads / kWave];

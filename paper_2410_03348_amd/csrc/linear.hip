@@ -4,8 +4,9 @@
 //   dz = grad_y act'(z),   grad_x = dz w,   grad_w = dz^T x,   grad_bias[o] = sum_i dz[i, o]
 //
 // A tile of z stays in the registers that the matrix cores leave it in, and y (and z, where the gradients need it) is written from there.  Few
-// tiles share out their k, and a second launch adds up the shares and does the rest.  Up to 64 rows are no work for tiles: every weight is read for
-// them once, which is what bounds the call, straight from memory into the operands of the matrix cores (linear_few_kernel, linear_few_back_kernel).
+// tiles share out their k, and a second launch adds up the shares and does the rest.  Few rows are no work for tiles: weights go straight from memory into
+// the operands of the matrix cores, and their bytes bound the call.  Forward (linear_few_kernel) that is up to 16 rows in bf16 and 64 in float, and up to 256 of
+// a layer with few weights, which sets of 16 to 64 rows then read again; grad_x (linear_few_back_kernel) up to 64 rows of a layer with many weights.
 // Backward: dz is rounded for the matrix cores and written, with its sums over rows beside it, and grad_x and grad_w are two sets of tiles
 // of one launch (mfma_products.h).
 #include "activation.h"
@@ -537,22 +538,23 @@ __global__ void __launch_bounds__(256) linear_zero_kernel(O *out, int64_t ld, in
 
 // ---------------------------------------------------------------- host side
 
-// linear_few_kernel or tiles, us: bf16 1 x 4 096 x 16 384 23 / 26, 16 x 4 096 x 4 096 11 / 12, 16 x 4 096 x 16 384 33 / 29, 32 x 4 096 x 4 096 17 / 12 (not taken);
-// float, whose tiles want their operands in planes, 16 x 4 096 x 4 096 18 / 56, 64 x 4 096 x 4 096 39 / 51, 128 x 1 509 x 12 939 113 / 79 (not taken).  Few
-// weights are launches and waits, of which it has fewer: 128 x 1 568 x 128 6 / 13, float 8 / 13, 256 x 300 x 2 000 8 / 10, float 10 / 15.
+// linear_few_kernel or tiles, us: bf16 1 x 4 096 x 16 384 23 / 25, 16 x 4 096 x 4 096 11 / 12, 32 x 4 096 x 4 096 17 / 12 (not taken), but 16 x 4 096 x 16 384 33 / 28,
+// which a rule that goes by rows takes all the same; float, whose tiles want their operands in planes, 16 x 4 096 x 4 096 18 / 55, 64 x 4 096 x 4 096 39 / 50,
+// 128 x 1 509 x 12 939 107 / 78 (not taken).  Few weights are launches and waits, of which it has fewer: 128 x 1 568 x 128 6 / 14, float 8 / 14, 256 x 300 x 2 000
+// 7 / 11, float 10 / 15.
 constexpr int64_t kSmallWeights = 1 << 20;
-// linear_few_back_kernel or tiles, us of a backward pass: bf16 1 x 4 096 x 4 096 30 / 39, 16 x 1 509 x 12 939 50 / 61, 64 x 4 096 x 16 384 121 / 222, 50 x 1 509 x 12 939
-// 68 / 60, 128 x 4 096 x 4 096 54 / 45 (not taken); float 1 x 4 096 x 4 096 45 / 85, 64 x 1 509 x 12 939 111 / 127, 128 x 4 096 x 4 096 116 / 103 (not taken); few weights
-// (not taken) 16 x 1 568 x 128 14 / 12, 64 x 300 x 2 000 25 / 15.
+// linear_few_back_kernel or tiles, us of a backward pass: bf16 1 x 4 096 x 4 096 30 / 39, 16 x 1 509 x 12 939 46 / 62, 64 x 4 096 x 16 384 126 / 222, 128 x 4 096 x 4 096
+// 54 / 45 (not taken), but 50 x 1 509 x 12 939 63 / 60, which is taken all the same; float 1 x 4 096 x 4 096 45 / 83, 64 x 1 509 x 12 939 99 / 126, 128 x 4 096 x 4 096
+// 111 / 101 (not taken); few weights (not taken) 16 x 1 568 x 128 15 / 12, 64 x 300 x 2 000 23 / 16.
 constexpr int32_t kMostFewBack = 64;
 constexpr int64_t kFewBackWeights = 1 << 22;
 
 // What tiles take, in elements of a result times k, some 2.35 G of which the chip does in a millisecond with one product of planes in the large tiles
 // (256 x 256; float 128 x 256, six products).  A tile takes kAround k more than it has, and two on a unit twice as long as one.  Smaller ones load more for what they multiply, by kSlower; adding up
-// shares costs kSumWeight an element of each and a launch kLaunchWeight, both in terms of one product.  us, as chosen / others: forward, bf16
-// 4 096 x 1 024 x 4 096 47 (256 x 256) / 50 (128 x 128), 2 000 x 2 048 x 2 048 27 (128 x 128) / 62 (256 x 256) / 31 (64 x 64), 1 000 x 777 x 1 501 22 (64 x 64) / 26
-// (128 x 128 in two shares), float 1 000 x 777 x 1 501 38 (128 x 128 in two shares) / 51 (64 x 64) / 58 (128 x 128); backward, bf16 4 096 x 1 024 x 4 096 107 (128 x 128)
-// / 116 (256 x 256 in two shares each) / 138 (256 x 256), 8 192 x 4 096 x 4 096 489 (256 x 256) / 563 (128 x 128), float 300 x 300 x 300 14 (64 x 64 in three shares) / 18 (in one).
+// shares costs kSumWeight an element of each and a launch kLaunchWeight, both in terms of one product.  us, as chosen / others, a pass one way without z: forward, bf16
+// 4 096 x 1 024 x 4 096 42 (256 x 256) / 45 (128 x 128), 2 000 x 2 048 x 2 048 26 (128 x 128) / 58 (256 x 256) / 32 (64 x 64), 1 000 x 777 x 1 501 15 (64 x 64) / 21
+// (128 x 128 in two shares), float 1 000 x 777 x 1 501 32 (128 x 128 in two shares) / 41 (64 x 64) / 47 (128 x 128); backward, bf16 4 096 x 1 024 x 4 096 105 (128 x 128)
+// / 116 (256 x 256 in two shares each) / 134 (256 x 256), 8 192 x 4 096 x 4 096 490 (256 x 256) / 576 (128 x 128), float 300 x 300 x 300 16 (64 x 64 in three shares) / 19 (in one).
 constexpr double kAround = 160, kSumWeight = 2.5, kLaunchWeight = 7e6;
 template <int P, int Q>
 constexpr double kSlower[3] = {P == 3 ? 3.0 : 2.2, P == 3 ? 1.33 : Q == 2 ? 1.0 : 1.16, 1.0};
@@ -674,8 +676,9 @@ Back lay_back(const dol_matrix *x, const dol_matrix *w, void *workspace)
     return L;
 }
 
-// dz rounded to bf16 is off by 2^-9 in every term of a gradient.  Sums over many rows average that out; with few, where the products cost little, a second
-// plane takes it away.
+// dz rounded to bf16 is off by up to 2^-8 of each number, which adds to grad_x and grad_weight about as much error as their own rounding does: 2.4e-3 in the norm
+// in all where it is 1.7e-3, whatever the sizes.  A second plane takes it away, and is a second product: with few rows, where the products cost little, it is
+// taken; above, it would double the largest launch.
 constexpr int32_t kFewRows = 512;
 
 template <typename F>

@@ -32,14 +32,14 @@ constexpr int kWideThreads = 1024;
 template <int G>
 constexpr int kGroups = G < kThreads ? kThreads / G : 1;
 // Wavefronts to a SIMD that the forward kernel's registers leave room for, and the workgroups of the chip that are.  More of them than that would be a second
-// round of fewer: bf16 8 192 x 4 096 59 us with four to a unit, of which three fit, 51 with three.
+// round of fewer: bf16 8 192 x 4 096 58 us with four to a unit, of which three fit, 52 with three.
 template <typename S, int G>
 constexpr int kForwardWaves = G == 4 ? 4 : sizeof(S) == 4 || G < 64 ? 5 : G <= 384 ? 7 : G <= 768 ? 6 : 4;
 template <typename S, int G>
 constexpr int kForwardBlocks = 256 * (kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) > 0 ? kForwardWaves<S, G> * 4 / ((G * kGroups<G> + 63) / 64) : 1);
-// Backward fewer workgroups leave fewer parts, but a set of few rows leaves most of a large one idle.  Both ways, us, four to a unit / two / one: bf16 39 574 x 361
-// 112 / 109 / 106, but 900 x 20 x 300 with a gate to each sample 50 / - / 70, float 31 360 x 32 20 / 25 / 27, bf16 16 384 x 1 000 83 / 78 / 81; two / one: bf16
-// 8 192 x 1 500 84 / 80, 8 192 x 4 096 154 / 149.
+// Backward fewer workgroups leave fewer parts, but they have to fill a unit.  Both ways, us, four to a unit / two / one: bf16 39 574 x 361 90 / 104 / 134,
+// 900 x 20 x 300 with a gate to each sample 42 / 42 / 61, float 31 360 x 32 20 / 20 / 21, bf16 16 384 x 1 000 85 / 77 / 87, 8 192 x 1 500 85 / 73 / 67, 8 192 x 4 096
+// 165 / 152 / 143.
 constexpr int back_groups(int threads) { return threads == 0 ? 1 : threads <= 64 ? kThreads / threads : threads == 128 ? 4 : 1024 / threads; }
 constexpr int back_blocks(int threads) { return threads <= 64 ? 4 : threads == 128 ? 2 : 1; }    // to a unit
 template <int G>
@@ -127,7 +127,7 @@ struct Eight {
     static constexpr int column(int e) { return e / V * D + e % V; }
     Loose<S> v[H];
     // The row's, of at least a vector, from column c on; where a vector is not all there the row's last one, so that all threads load at once, and cut() does
-    // the rest (behind a branch for those threads each load is waited for by itself: bf16 39 574 x 361 both ways 94 us, 114 so).
+    // the rest (behind a branch for those threads each load is waited for by itself: bf16 39 574 x 361 both ways 90 us, 110 so).
     __device__ void all(const Mat<const S> &m, int64_t r, int c, int cols)
     {
 #pragma unroll
@@ -277,7 +277,7 @@ struct Columns {
 
 // ---------------------------------------------------------------- forward
 
-// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 49 us, 5.5 TB/s.
+// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 48 us, 5.6 TB/s.
 template <typename S, int G>
 __global__ void __launch_bounds__(G * kGroups<G>, (kForwardWaves<S, G>)) residual_norm_kernel(Args<S> a)
 {
@@ -453,8 +453,8 @@ __device__ __forceinline__ void leave_part(const float (&sum)[kEight], O *to, in
 }
 
 // WHOLE: a group takes all rows of its sets; else a workgroup takes a chunk of the rows of one set.
-// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 93 us, 4.3 TB/s.  (With the next row asked for ahead, as forward, it has registers for one row on a
-// unit at a time instead of two: 116 us against 99.)
+// Bytes bound it: bf16 8 192 x 4 096, a gate to 1 024 rows, 92 us, 4.4 TB/s.  (With the next row asked for ahead, as forward, it had registers for one row on a
+// unit at a time instead of two: 116 us, 99 at that time without.)
 template <typename S, int G, bool WHOLE>
 __global__ void __launch_bounds__(G * kBackGroups<G>, G < 64 ? 2 : 4) residual_norm_backward_kernel(Args<S> a)
 {
@@ -749,8 +749,8 @@ Plan plan_of(const dol_matrix *u, const dol_matrix *gate, void *workspace)
     // (rows too long for registers: as many of kThreads as lie side by side)
     const int64_t most_blocks = p.threads ? back_blocks(p.threads) * kUnits : std::max(1, 4 * kUnits / stripes_of(u->cols));
     // As chunks of a set's rows to workgroups, or as whole sets to groups: what takes fewer rows in a row, where leaving a chunk's parts takes as long as three
-    // rows.  Both ways, us, chunks / whole: bf16 900 x 20 x 300 45 / 63, 2 000 x 30 x 300 120 / 130, 4 000 x 10 x 1 024 218 / 185, 8 000 x 40 x 96 207 / 167,
-    // 100 000 x 3 x 16 1 111 / 51, float 3 000 x 3 x 2 048 239 / 174, 128 x 50 x 7 463 426 / 560.
+    // rows.  Both ways, us, chunks / whole: bf16 900 x 20 x 300 42 / 61, 2 000 x 30 x 300 119 / 131, 4 000 x 10 x 1 024 217 / 182, 8 000 x 40 x 96 193 / 167,
+    // 100 000 x 3 x 16 1 127 / 50, float 3 000 x 3 x 2 048 239 / 172, 128 x 50 x 7 463 425 / 564.
     const int64_t wanted = std::max<int64_t>(1, most_blocks / p.sets), most = std::max<int64_t>(1, p.points / groups);
     p.chunks = std::min(wanted, most);
     p.chunk = (p.points + p.chunks - 1) / p.chunks;
